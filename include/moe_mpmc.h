@@ -320,6 +320,87 @@ typedef struct moe_layer_args {
 int moe_layer_forward(const moe_layer_args *args, void *stream);
 
 /* =======================================================================================
+ * Training the gate and the predictor, and serving the predictor step by step.  The matrix products between these
+ * calls are the caller's; what is here moves or scans rows.
+ *
+ * Gradients of the routed layer.  With out = moe_combine_topk(y_perm, x, inv, w) and x_perm =
+ * moe_dispatch_topk(x), for dout = dL/dout and dx_perm = dL/dx_perm (k = 1 serves moe_combine and moe_dispatch):
+ * moe_combine_topk_backward, per token s and choice j with r = inv[j*T+s] >= 0:
+ *     dy_perm[r] = expert_weight[j*T+s] * dout[s]           (rounded once to dtype)
+ *     dweight[j*T+s] = <dout[s], y_perm[r]>                  (binary32; 0 for a dropped choice)
+ *     dx[s] = dout[s] where residual = 1 or no choice was kept (the passthrough), else 0
+ *   Rows of dy_perm that no inv names (those behind the last kept one) are left as they were.  dweight may be NULL
+ *   (y_perm is then not read and may be NULL), and so may dx.
+ * moe_dispatch_topk_backward, which is also the gradient of the gather in moe_expert_ffn_rows:
+ *     dx[s] = (dx_add ? dx_add[s] : 0) + sum over j with inv[j*T+s] >= 0, in the order of j, of dx_perm[inv[j*T+s]]
+ *   summed in binary32, rounded once.  dx_add [T,d] (moe_combine_topk_backward's dx) may be NULL, or dx itself.
+ * moe_route_topk_backward: from the logits that moe_route_topk wrote (logits_opt) and its ids, dL/dlogits [T,E]
+ *   of expert_weight: p = softmax(logits[s]); renormalize = 0: dlogits_i = [i = e_j] dw_j p_i - p_i sum_j dw_j p_ej;
+ *   renormalize = 1: w_j (dw_j - sum_l dw_l w_l) at i = e_j with w the weights, 0 elsewhere.  E <= MOE_MAX_EXPERTS.  An
+ *   id outside [0,E) is taken as a choice that was not made.  dlogits must not lie on logits.
+ * Ids of a token must differ from each other, and so must the rows that inv names (as moe_route_topk and
+ * moe_dispatch_topk give them): an entry of inv has to be negative or below k*T.
+ */
+int moe_combine_topk_backward(const void *dout, const void *y_perm, const int32_t *inv, const float *expert_weight,
+                              int T, int k, int d, int dtype, int residual, void *dy_perm, float *dweight, void *dx,
+                              void *stream);
+int moe_dispatch_topk_backward(const void *dx_perm, const int32_t *inv, const void *dx_add, int T, int k, int d,
+                               int dtype, void *dx, void *stream);
+int moe_route_topk_backward(const float *logits, const int32_t *expert_idx, const float *dweight, int T, int E, int k,
+                            int renormalize, float *dlogits, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * sru_scan -- the recurrence of one SRU layer (the equations of sru_predict) over pre-activations that the caller's
+ * product made: u [B, L, n_blocks*H], column blocks W x | W_f x | W_r x and, with n_blocks = 4, W_h x; with n_blocks =
+ * 3 the highway term is x [B, L, H].  Per channel, t = 0..lengths[b]-1, c_{-1} = c0 [B, H]:
+ *     f = sigmoid(u1 + b_f);  r = sigmoid(u2 + b_r);  c_t = f*c_{t-1} + (1-f)*u0;  h_t = r*tanh(c_t) + (1-r)*w_t
+ * h [B, L, H] in dtype, rows behind a sequence's end zero; c_last [B, H] the state after its last token.  States and
+ * all arithmetic are binary32.  b_f, b_r [H] binary32, c0 and lengths [B] (int32, taken to 0..L; NULL: all L) may be
+ * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H.
+ * states (NULL, or sru_scan_states_bytes): what sru_scan_backward needs beside the inputs.
+ *
+ * sru_scan_backward -- from dh = dL/dh and dc_last = dL/dc_last (binary32, NULL: 0): du [B, L, n_blocks*H], dx [B, L, H]
+ * (n_blocks = 3: the highway's part only), db_f, db_r [H], dc0 [B, H] (binary32, each may be NULL).
+ *     d_t = dc_t + dh_t r (1 - tanh(c_t)^2);  du0 = d_t (1-f);  du1 = d_t (c_{t-1} - u0) f (1-f);  dc_{t-1} = d_t f
+ *     du2 = dh_t (tanh(c_t) - w_t) r (1-r);  dw_t = dh_t (1-r)
+ * Behind a sequence's end du and dx are zero; dh, u and x are not read there.  The sums of db_f and db_r have a fixed
+ * order: equal calls give equal bits.  dc0 may be dc_last.
+ * The workspaces may be NULL where the size is 0.
+ */
+size_t sru_scan_states_bytes(int B, int L, int H);
+size_t sru_scan_workspace_bytes(int B, int L, int H, int dtype);
+int sru_scan(const void *u, const void *x, const float *b_f, const float *b_r, const float *c0, const int32_t *lengths,
+             int B, int L, int H, int n_blocks, int dtype, void *h, float *c_last, void *states, void *ws,
+             size_t ws_bytes, void *stream);
+size_t sru_scan_backward_workspace_bytes(int B, int L, int H, int dtype);
+int sru_scan_backward(const void *dh, const float *dc_last, const void *u, const void *x, const float *b_f,
+                      const float *b_r, const void *states, const int32_t *lengths, int B, int L, int H, int n_blocks,
+                      int dtype, void *du, void *dx, float *db_f, float *db_r, float *dc0, void *ws, size_t ws_bytes,
+                      void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_token_logprobs -- rows of logits (a predictor's over experts, a gate's, a vocabulary's) scored: logits [N, V] in
+ * dtype, rows row_stride elements apart (>= V; any alignment of the element), target [N].  With p = softmax(row):
+ *     logprob = log p[target]  (0 for a target outside [0,V): a padded position);   lse = log sum exp(row)
+ *     entropy = -sum p log p;   top_idx, top_logprob [N, k]: the k largest logits in falling order, lowest id first
+ *     among equals, and their log probabilities (0 <= k <= min(MOE_MAX_TOPK, V); NULL with k = 0)
+ * Logits of -infinity are masked: probability 0, nothing to the entropy.  Where all are, log probabilities and lse are
+ * -infinity and the entropy is 0.  A NaN or +infinity makes the row's numbers NaN; among the alternatives a NaN counts as
+ * masked.  Sums in binary32, in a fixed order.
+ * moe_token_logprobs_backward -- dL/dlogits (dtype) from dlogprob [N] and dentropy [N] (NULL: 0), with the lse and
+ * entropy that the forward wrote (entropy may be NULL without dentropy):
+ *     dlogits_i = g ([i = target] - p_i) - dentropy p_i (log p_i + entropy),   g = dlogprob, 0 for a padded position
+ * 0 at masked logits other than the target and in rows that are masked throughout.  dlogits may lie on logits with the same stride.
+ */
+size_t moe_token_logprobs_workspace_bytes(int N, int V, int k, int dtype);
+int moe_token_logprobs(const void *logits, long long row_stride, const int32_t *target, int N, int V, int dtype, int k,
+                       float *logprob, float *entropy, float *lse, int32_t *top_idx, float *top_logprob, void *ws,
+                       size_t ws_bytes, void *stream);
+int moe_token_logprobs_backward(const void *logits, long long row_stride, const int32_t *target, const float *lse,
+                                const float *entropy, const float *dlogprob, const float *dentropy, int N, int V,
+                                int dtype, void *dlogits, long long dlogits_stride, void *stream);
+
+/* =======================================================================================
  * Measurement (not part of the method; used by the benchmark only).
  * moe_expert_ffn_timed: moe_expert_ffn_rows (with row_index NULL: moe_expert_ffn, n_x_rows =
  * max_rows) that also records three hipEvent_t handles (passed as void*, any may be NULL) on the

@@ -34,6 +34,9 @@ EXPORTS = (
     "moe_combine",
     "moe_route_topk", "moe_dispatch_topk", "moe_expert_ffn_rows", "moe_combine_topk",
     "moe_plan_dispatch_workspace_bytes", "moe_plan_dispatch", "moe_layer_forward",
+    "moe_combine_topk_backward", "moe_dispatch_topk_backward", "moe_route_topk_backward",
+    "sru_scan_states_bytes", "sru_scan_workspace_bytes", "sru_scan", "sru_scan_backward_workspace_bytes", "sru_scan_backward",
+    "moe_token_logprobs_workspace_bytes", "moe_token_logprobs", "moe_token_logprobs_backward",
     "moe_measure_sink_bytes", "moe_measure_stream_read", "moe_measure_mfma_bf16_flops", "moe_measure_mfma_bf16",
 )
 
@@ -41,7 +44,8 @@ EXPORTS = (
 # the calls that go through the extension
 MARSHALLED = ("moe_route", "moe_route_topk", "sru_predict", "replica_plan", "moe_dispatch", "moe_dispatch_static", "moe_dispatch_topk",
               "moe_plan_dispatch", "moe_pack_weights", "moe_expert_ffn", "moe_expert_ffn_rows", "moe_combine", "moe_combine_topk",
-              "moe_layer_forward")
+              "moe_layer_forward", "moe_combine_topk_backward", "moe_dispatch_topk_backward", "moe_route_topk_backward", "sru_scan",
+              "sru_scan_backward", "moe_token_logprobs", "moe_token_logprobs_backward")
 
 
 class MoeError(RuntimeError):
@@ -121,6 +125,18 @@ def lib():
         _lib.moe_plan_dispatch_workspace_bytes.argtypes = [I, I, I, I]
         _lib.moe_plan_dispatch.argtypes = [P, I, P, I, I, I, I, I, I] + [P] * 12 + [P, S, P]
         _lib.moe_layer_forward.argtypes = [P, P]
+        Q = C.c_longlong
+        _lib.moe_combine_topk_backward.argtypes = [P, P, P, P, I, I, I, I, I, P, P, P, P]
+        _lib.moe_dispatch_topk_backward.argtypes = [P, P, P, I, I, I, I, P, P]
+        _lib.moe_route_topk_backward.argtypes = [P, P, P, I, I, I, I, P, P]
+        _lib.sru_scan_states_bytes.argtypes = [I, I, I]
+        _lib.sru_scan_workspace_bytes.argtypes = [I, I, I, I]
+        _lib.sru_scan.argtypes = [P] * 6 + [I] * 5 + [P] * 4 + [S, P]
+        _lib.sru_scan_backward_workspace_bytes.argtypes = [I, I, I, I]
+        _lib.sru_scan_backward.argtypes = [P] * 8 + [I] * 5 + [P] * 6 + [S, P]
+        _lib.moe_token_logprobs_workspace_bytes.argtypes = [I, I, I, I]
+        _lib.moe_token_logprobs.argtypes = [P, Q, P, I, I, I, I, P, P, P, P, P, P, S, P]
+        _lib.moe_token_logprobs_backward.argtypes = [P, Q, P, P, P, P, P, I, I, I, P, Q, P]
     return _lib
 
 
@@ -484,6 +500,173 @@ def moe_combine_topk(y_perm, x, inv, expert_weight, residual=0, out=None):
     _check(_c().moe_combine_topk(y_perm, x, inv, expert_weight, T, k, d, _dt(x),
                                   int(residual), o, _stream()))
     return o
+
+
+# --------------------------------------------------------------------------- training the gate and the predictor
+def _expect(who, lead, *tensors):
+    """Each (name, tensor, shape, dtype) as the call reads it, on the lead tensor's device, which has to be the current one: its stream
+    is the one that the call's kernels go to.  None: an argument that was left out."""
+    if not lead.is_cuda:
+        raise ValueError("device-resident contiguous tensors only")
+    at = lead.get_device()
+    if at != torch.cuda.current_device():
+        raise ValueError(f"{who}: tensors on device {at}, the current device is {torch.cuda.current_device()}")
+    for name, t, shape, dtype in tensors:
+        if t is None:
+            continue
+        if t.shape != shape or t.dtype != dtype:
+            raise ValueError(f"{who}: {name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
+        if t.get_device() != at:
+            raise ValueError(f"{who}: {name} is not on device {at}")
+
+
+def moe_combine_topk_backward(dout, y_perm, inv, expert_weight, residual=0, out=None):
+    """Gradient of moe_combine_topk (k = 1: of moe_combine) with respect to y_perm, the weights and x.  dout [T,d], y_perm [k*T,d],
+    inv int32[k,T] or [T], expert_weight f32 likewise -> dict(dy_perm [k*T,d], dweight, dx [T,d]).  Rows of dy_perm behind the last kept
+    assignment are left as they were (zero when allocated here).  With ``out``, dweight and dx may be None: they are not computed, and y_perm
+    may be None without dweight."""
+    T, d = dout.shape
+    k = inv.shape[0] if inv.dim() == 2 else 1
+    f32, dt = torch.float32, dout.dtype
+    shape = (k, T) if inv.dim() == 2 else (T,)
+    o = out if out is not None else dict(dy_perm=torch.zeros(k * T, d, dtype=dt, device=dout.device),
+                                         dweight=torch.empty(shape, dtype=f32, device=dout.device), dx=torch.empty_like(dout))
+    _expect("moe_combine_topk_backward", dout, ("y_perm", y_perm, (k * T, d), dt), ("inv", inv, shape, torch.int32),
+            ("expert_weight", expert_weight, shape, f32), ("dy_perm", o["dy_perm"], (k * T, d), dt),
+            ("dweight", o["dweight"], shape, f32), ("dx", o["dx"], (T, d), dt))
+    _check(_c().moe_combine_topk_backward(dout, y_perm, inv, expert_weight, T, k, d, _dt(dout), int(residual), o["dy_perm"], o["dweight"],
+                                          o["dx"], _stream()))
+    return o
+
+
+def moe_dispatch_topk_backward(dx_perm, inv, dx_add=None, out=None):
+    """Gradient of moe_dispatch_topk (k = 1: of moe_dispatch), and of moe_expert_ffn_rows's gather, with respect to x: the rows of
+    dx_perm [k*T,d] back to their tokens and added, behind dx_add [T,d] where given.  inv int32[k,T] or [T] -> dx [T,d].  out may be
+    dx_add."""
+    k = inv.shape[0] if inv.dim() == 2 else 1
+    T, d = inv.shape[-1], dx_perm.shape[1]
+    dt = dx_perm.dtype
+    dx = out if out is not None else torch.empty(T, d, dtype=dt, device=dx_perm.device)
+    _expect("moe_dispatch_topk_backward", dx_perm, ("dx_perm", dx_perm, (k * T, d), dt),
+            ("inv", inv, (k, T) if inv.dim() == 2 else (T,), torch.int32), ("dx_add", dx_add, (T, d), dt), ("out", dx, (T, d), dt))
+    _check(_c().moe_dispatch_topk_backward(dx_perm, inv, dx_add, T, k, d, _dt(dx_perm), dx, _stream()))
+    return dx
+
+
+def moe_route_topk_backward(logits, expert_idx, dweight, renormalize=False, out=None):
+    """Gradient of moe_route_topk's weights (k = 1: of moe_route's probability) with respect to the logits: logits f32[T,E] as that
+    call returned them, expert_idx int32[k,T] or [T], dweight f32 likewise -> dlogits f32[T,E]."""
+    T, E = logits.shape
+    k = expert_idx.shape[0] if expert_idx.dim() == 2 else 1
+    shape = (k, T) if expert_idx.dim() == 2 else (T,)
+    dl = out if out is not None else torch.empty_like(logits)
+    f32 = torch.float32
+    _expect("moe_route_topk_backward", logits, ("logits", logits, (T, E), f32), ("expert_idx", expert_idx, shape, torch.int32),
+            ("dweight", dweight, shape, f32), ("out", dl, (T, E), f32))
+    _check(_c().moe_route_topk_backward(logits, expert_idx, dweight, T, E, k, int(bool(renormalize)), dl, _stream()))
+    return dl
+
+
+def _scan_blocks(who, u, x, H):
+    n = 3 if x is not None else 4
+    if H * n != u.shape[2]:
+        raise ValueError(f"{who}: u has {u.shape[2]} columns, {n} blocks of {H} wanted ({'with' if x is not None else 'without'} x)")
+    return n
+
+
+def sru_scan(u, x=None, b_f=None, b_r=None, c0=None, lengths=None, want_states=False, out=None, ws=None):
+    """The recurrence of one SRU layer over its pre-activations u [B,L,3H] with the highway input x [B,L,H], or u [B,L,4H] without.
+    -> (h [B,L,H], c_last f32[B,H], states or None).  c0 f32[B,H] is the state before the first token, lengths int32[B] the sequences'
+    own lengths (rows of h behind them are zero).  states go to sru_scan_backward.  out: (h, c_last, states) to write; c_last may be c0."""
+    B, L, W = u.shape
+    H = x.shape[2] if x is not None else W // 4
+    n = _scan_blocks("sru_scan", u, x, H)
+    dev, f32, dt = u.device, torch.float32, _dt(u)
+    if out is None:
+        out = (torch.empty(B, L, H, dtype=u.dtype, device=dev), torch.empty(B, H, dtype=f32, device=dev),
+               torch.empty(lib().sru_scan_states_bytes(B, L, H) // 4, dtype=f32, device=dev) if want_states else None)
+    h, c_last, states = out
+    if states is not None and states.numel() * states.element_size() < lib().sru_scan_states_bytes(B, L, H):
+        raise ValueError("sru_scan: states are smaller than sru_scan_states_bytes")
+    _expect("sru_scan", u, ("x", x, (B, L, H), u.dtype), ("b_f", b_f, (H,), f32), ("b_r", b_r, (H,), f32), ("c0", c0, (B, H), f32),
+            ("lengths", lengths, (B,), torch.int32), ("h", h, (B, L, H), u.dtype), ("c_last", c_last, (B, H), f32),
+            ("states", states, states.shape if states is not None else None, f32))
+    if ws is None:
+        need = lib().sru_scan_workspace_bytes(B, L, H, dt)
+        ws = _ws(need, dev) if need else None
+    _check(_c().sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, ws.numel() if ws is not None else 0, _stream()))
+    return out
+
+
+def sru_scan_backward(dh, u, states, x=None, b_f=None, b_r=None, dc_last=None, lengths=None, out=None, ws=None):
+    """Gradient of sru_scan: dh [B,L,H] and dc_last f32[B,H] (None: zero), with the forward's inputs and states -> dict(du, dx (None
+    without x), db_f, db_r f32[H], dc0 f32[B,H]).  With ``out``, db_f, db_r and dc0 may be None; dc0 may be dc_last."""
+    B, L, H = dh.shape
+    if u.dim() != 3 or u.shape[:2] != dh.shape[:2]:
+        raise ValueError(f"sru_scan_backward: u {list(u.shape)} does not fit dh {list(dh.shape)}")
+    n = _scan_blocks("sru_scan_backward", u, x, H)
+    dev, f32, t, dt = u.device, torch.float32, u.dtype, _dt(u)
+    o = out if out is not None else dict(
+        du=torch.empty_like(u), dx=torch.empty_like(x) if x is not None else None, db_f=torch.empty(H, dtype=f32, device=dev),
+        db_r=torch.empty(H, dtype=f32, device=dev), dc0=torch.empty(B, H, dtype=f32, device=dev))
+    if states.numel() * states.element_size() < lib().sru_scan_states_bytes(B, L, H):
+        raise ValueError("sru_scan_backward: states are smaller than sru_scan_states_bytes")
+    _expect("sru_scan_backward", dh, ("u", u, (B, L, n * H), dh.dtype), ("x", x, (B, L, H), t), ("b_f", b_f, (H,), f32), ("b_r", b_r, (H,), f32),
+            ("states", states, states.shape, f32), ("dc_last", dc_last, (B, H), f32), ("lengths", lengths, (B,), torch.int32),
+            ("du", o["du"], (B, L, n * H), t), ("dx", o["dx"], (B, L, H), t), ("db_f", o["db_f"], (H,), f32),
+            ("db_r", o["db_r"], (H,), f32), ("dc0", o["dc0"], (B, H), f32))
+    if ws is None:
+        need = lib().sru_scan_backward_workspace_bytes(B, L, H, dt)
+        ws = _ws(need, dev) if need else None
+    _check(_c().sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, o["du"], o["dx"], o["db_f"], o["db_r"],
+                                  o["dc0"], ws, ws.numel() if ws is not None else 0, _stream()))
+    return o
+
+
+def _rows(t):
+    """(pointer-bearing tensor, row stride) of a matrix whose rows are contiguous; rows may lie further apart than they are long."""
+    N, V = t.shape
+    if t.is_contiguous() or N == 0:
+        return t, V
+    if (V > 1 and t.stride(1) != 1) or (N > 1 and t.stride(0) < V):
+        raise ValueError("rows of logits must be contiguous and must not overlap")
+    return t[0], max(t.stride(0), V)
+
+
+def moe_token_logprobs(logits, target, k=0, out=None, ws=None):
+    """logits [N,V] (rows contiguous, any distance apart), target int32[N] -> dict(logprob, entropy, lse f32[N], top_idx int32[N,k],
+    top_logprob f32[N,k]).  A target outside [0,V) is a padded position: logprob 0.  Logits of -inf are masked."""
+    N, V = logits.shape
+    dev, f32, dt = logits.device, torch.float32, _dt(logits)
+    o = out if out is not None else dict(
+        logprob=torch.empty(N, dtype=f32, device=dev), entropy=torch.empty(N, dtype=f32, device=dev),
+        lse=torch.empty(N, dtype=f32, device=dev), top_idx=torch.empty(N, k, dtype=torch.int32, device=dev),
+        top_logprob=torch.empty(N, k, dtype=f32, device=dev))
+    _expect("moe_token_logprobs", logits, ("target", target, (N,), torch.int32), ("logprob", o["logprob"], (N,), f32),
+            ("entropy", o["entropy"], (N,), f32), ("lse", o["lse"], (N,), f32),
+            *((("top_idx", o["top_idx"], (N, k), torch.int32), ("top_logprob", o["top_logprob"], (N, k), f32)) if k else ()))
+    rows, stride = _rows(logits)
+    if ws is None:
+        need = lib().moe_token_logprobs_workspace_bytes(N, V, k, dt)
+        ws = _ws(need, dev) if need else None
+    _check(_c().moe_token_logprobs(rows, stride, target, N, V, dt, k, o["logprob"], o["entropy"], o["lse"], o["top_idx"] if k else None,
+                                   o["top_logprob"] if k else None, ws, ws.numel() if ws is not None else 0, _stream()))
+    return o
+
+
+def moe_token_logprobs_backward(logits, target, lse, entropy, dlogprob, dentropy=None, out=None):
+    """Gradient of moe_token_logprobs' logprob (dlogprob f32[N]) and entropy (dentropy f32[N] or None) with respect to the logits, with
+    the forward's lse and entropy -> dlogits [N,V].  out may be logits."""
+    N, V = logits.shape
+    f32, dt = torch.float32, _dt(logits)
+    dl = out if out is not None else torch.empty(N, V, dtype=logits.dtype, device=logits.device)
+    _expect("moe_token_logprobs_backward", logits, ("target", target, (N,), torch.int32), ("lse", lse, (N,), f32),
+            ("entropy", entropy, (N,), f32), ("dlogprob", dlogprob, (N,), f32), ("dentropy", dentropy, (N,), f32),
+            ("out", dl, (N, V), logits.dtype))
+    rows, stride = _rows(logits)
+    to, dstride = _rows(dl)
+    _check(_c().moe_token_logprobs_backward(rows, stride, target, lse, entropy, dlogprob, dentropy, N, V, dt, to, dstride, _stream()))
+    return dl
 
 
 class MoeLayerTopK:

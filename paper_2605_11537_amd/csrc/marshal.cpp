@@ -158,7 +158,9 @@ PyObject *call(const char *name, int (*f)(A...), PyObject *const *args, Py_ssize
 
 #define CALLS(X)                                                                                                          \
     X(moe_route) X(moe_route_topk) X(sru_predict) X(replica_plan) X(moe_dispatch) X(moe_dispatch_static) X(moe_dispatch_topk)  \
-    X(moe_plan_dispatch) X(moe_pack_weights) X(moe_expert_ffn) X(moe_expert_ffn_rows) X(moe_combine) X(moe_combine_topk)
+    X(moe_plan_dispatch) X(moe_pack_weights) X(moe_expert_ffn) X(moe_expert_ffn_rows) X(moe_combine) X(moe_combine_topk)   \
+    X(moe_combine_topk_backward) X(moe_dispatch_topk_backward) X(moe_route_topk_backward) X(sru_scan) X(sru_scan_backward) \
+    X(moe_token_logprobs) X(moe_token_logprobs_backward)
 
 #define DECLARE(NAME)                                                                                                     \
     decltype(&NAME) bound_##NAME = nullptr;                                                                               \

@@ -1,113 +1,483 @@
 // sru_scan and its gradient: the recurrence of an SRU layer over pre-activations that lie in memory.
+//
+// c_t = f_t c_{t-1} + b_t composes: a run of steps is a pair (A, C), c_out = A c_in + C, and the pair of two runs is (A2 A1, A2 C1 + C2).
+// The gradient dc_{t-1} = f_t (dc_t + e_t) is the same from the other end.  So a wavefront takes SCAN_STEPS steps of 64 lanes' channels with
+// everything they read in registers, finds its pair from zero, and learns its start from the pairs of the wavefronts before it, through
+// LDS: the wavefronts of a workgroup lie one behind the other on the sequence, and a round of them is read once and written once.
+// Where sequences and channels alone are too few for the card, the sequence is cut into segments for several workgroups, whose pairs a launch
+// before finds (it reads half of what the main one reads, again).
 #include "scalar_math.h"
+#include "sru_scan_rules.h"
 
 namespace moe {
 
-constexpr int SCAN_THREADS = 64;
-constexpr int SCAN_STEPS = 16;         // steps per saved state
+// V values of consecutive channels, as they lie in memory
+template <class T, int V> struct ScanRaw;
+template <> struct ScanRaw<bf16_t, 1> { typedef bf16_t type; };
+template <> struct ScanRaw<bf16_t, 2> { typedef uint32_t type; };
+template <> struct ScanRaw<float, 1> { typedef float type; };
+template <class T, int V> using scan_raw_t = typename ScanRaw<T, V>::type;
 
-template <class T, bool HIGHWAY>
-__global__ __launch_bounds__(SCAN_THREADS) void sru_scan_kernel(const T *__restrict__ u, const T *__restrict__ x,
-                                                                const float *__restrict__ b_f, const float *__restrict__ b_r,
-                                                                const float *c0, const int32_t *__restrict__ lengths, int L, int H,
-                                                                int blocks, T *__restrict__ h, float *c_last, float *__restrict__ states)
+__device__ __forceinline__ float scan_value(float r, int) { return r; }
+__device__ __forceinline__ float scan_value(bf16_t r, int) { return bf16_to_f32(r); }
+__device__ __forceinline__ float scan_value(uint32_t r, int v) { return __uint_as_float(v ? r & 0xffff0000u : r << 16); }
+
+template <class T, int V>
+__device__ __forceinline__ scan_raw_t<T, V> scan_pack(const float (&v)[V])
+{
+    if constexpr (sizeof(T) == 4) return v[0];
+    else if constexpr (V == 2) return pack_bf16x2(v[0], v[1]);
+    else return f32_to_bf16(v[0]);
+}
+
+// Where a workgroup stands: channels, sequence, segment.  Everything but the channel is the same for a whole wavefront.
+template <class T, int V>
+struct ScanPlace {
+    typedef scan_raw_t<T, V> raw_t;
+    int b, seg, lane, wave, waves, n, first, last;     // first .. last-1: the segment's steps
+    unsigned ch, col;                                  // this lane's first channel; one that exists
+    bool on;
+    __device__ __forceinline__ bool find(const ScanShape &g, const int32_t *lengths, int segments)
+    {
+        const unsigned wg = blockIdx.y * gridDim.x + blockIdx.x;
+        const unsigned groups = g.groups, at = wg / groups;
+        b = at / segments;
+        seg = at - (unsigned)b * segments;
+        if (b >= g.B) return false;
+        lane = threadIdx.x % WAVE;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+        waves = blockDim.x / WAVE;
+        ch = ((wg - at * groups) * WAVE + lane) * V;
+        on = ch < (unsigned)g.H;
+        col = on ? ch : 0;
+        n = lengths ? min(max(lengths[b], 0), g.L) : g.L;
+        n = __builtin_amdgcn_readfirstlane(n);
+        first = seg * g.seg_steps;
+        last = min(g.L, first + g.seg_steps);
+        return true;
+    }
+};
+
+// the steps t0 .. t0+SCAN_STEPS-1 of one column block, those below end only
+template <class T, int V>
+__device__ __forceinline__ void scan_load(scan_raw_t<T, V> (&to)[SCAN_STEPS], const T *row0, size_t row_len, unsigned col, int count)
+{
+    typedef scan_raw_t<T, V> raw_t;
+    if (count >= SCAN_STEPS) {
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) to[i] = *(const raw_t *)(row0 + i * row_len + col);
+    } else {
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) {
+            to[i] = 0;
+            if (i < count) to[i] = *(const raw_t *)(row0 + i * row_len + col);
+        }
+    }
+}
+
+// the state that a pair list before this place leads to
+__device__ __forceinline__ float scan_fold(float c, const float2 *pairs, size_t step, int count)
+{
+    for (int j = 0; j < count; ++j) {
+        const float2 p = pairs[j * step];
+        c = fmaf(p.x, c, p.y);
+    }
+    return c;
+}
+
+template <class T, int V, bool HIGHWAY>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShape g, const T *__restrict__ u, const T *__restrict__ x,
+                                                                       const float *__restrict__ b_f, const float *__restrict__ b_r,
+                                                                       const float *c0, const int32_t *__restrict__ lengths,
+                                                                       const float2 *__restrict__ pairs, T *__restrict__ h, float *c_last,
+                                                                       float *__restrict__ states)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    const int b = blockIdx.x / blocks, ch = blockIdx.x % blocks * SCAN_THREADS + threadIdx.x;
-    if (ch >= H) return;
-    const int n = lengths ? min(max(lengths[b], 0), L) : L;
-    const float bf = b_f ? b_f[ch] : 0.f, br = b_r ? b_r[ch] : 0.f;
-    const int saved = (L + SCAN_STEPS - 1) / SCAN_STEPS;
-    float c = c0 ? c0[(size_t)b * H + ch] : 0.f;
-    for (int t = 0; t < L; ++t) {
-        const size_t row = (size_t)b * L + t;
-        if (states && t % SCAN_STEPS == 0) states[((size_t)b * saved + t / SCAN_STEPS) * H + ch] = c;
-        if (t >= n) {
-            store_value(h + row * H + ch, 0.f);
-            continue;
-        }
-        const T *ur = u + row * K * H + ch;
-        const float z = value_of(ur[0]), w = HIGHWAY ? value_of(x[row * H + ch]) : value_of(ur[(size_t)(K - 1) * H]);
-        float f, fr, r, rr, slope;
-        gate_of<PRECISE>(value_of(ur[H]) + bf, f, fr);
-        gate_of<PRECISE>(value_of(ur[2 * (size_t)H]) + br, r, rr);
-        c = fmaf(f, c, fr * z);
-        store_value(h + row * H + ch, fmaf(r, tanh_of<PRECISE>(c, slope), rr * w));
+    typedef scan_raw_t<T, V> raw_t;
+    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE * V];
+    ScanPlace<T, V> p;
+    if (!p.find(g, lengths, g.segments)) return;
+    const size_t H = g.H, row_len = K * H;
+    float bf[V], br[V], c_in[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bf[v] = b_f ? b_f[p.col + v] : 0.f;
+        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        c_in[v] = c0 ? c0[(size_t)p.b * H + p.col + v] : 0.f;
+        c_in[v] = scan_fold(c_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, p.seg);
     }
-    if (c_last) c_last[(size_t)b * H + ch] = c;
+    const int round = p.waves * SCAN_STEPS;
+    for (int t = p.first, parity = 0; t < p.last; t += round, parity ^= 1) {
+        const int t0 = t + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);    // this wavefront's steps inside the sequence
+        const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
+        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
+        scan_load<T, V>(z, rows, row_len, p.col, count);
+        scan_load<T, V>(a, rows + H, row_len, p.col, count);
+        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
+        if (HIGHWAY) scan_load<T, V>(w, x + ((size_t)p.b * g.L + t0) * H, H, p.col, count);
+        else scan_load<T, V>(w, rows + 3 * H, row_len, p.col, count);
+        float f[SCAN_STEPS][V], in[SCAN_STEPS][V], A[V], C[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.f, C[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) {
+            if (i >= count) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float rest;
+                gate_of<PRECISE>(scan_value(a[i], v) + bf[v], f[i][v], rest);
+                in[i][v] = rest * scan_value(z[i], v);
+                A[v] *= f[i][v];
+                C[v] = fmaf(f[i][v], C[v], in[i][v]);
+            }
+        }
+        float c[V];
+        if (p.waves > 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                c[v] = c_in[v];
+                for (int j = 0; j < p.waves; ++j) {
+                    const float2 q = sums[parity][j][p.lane * V + v];
+                    c_in[v] = fmaf(q.x, c_in[v], q.y);
+                    if (j + 1 == p.wave) c[v] = c_in[v];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) c[v] = c_in[v], c_in[v] = fmaf(A[v], c_in[v], C[v]);
+        }
+        if (states && t0 < g.L && p.on) {
+            const size_t at = ((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch;
+#pragma unroll
+            for (int v = 0; v < V; ++v) states[at + v] = c[v];
+        }
+        T *hr = h + ((size_t)p.b * g.L + t0) * H;
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) {
+            if (i >= count) {
+                if (t0 + i < p.last && p.on) *(raw_t *)(hr + i * H + p.ch) = 0;
+                continue;
+            }
+            float out[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float s, rest, slope;
+                c[v] = fmaf(f[i][v], c[v], in[i][v]);
+                gate_of<PRECISE>(scan_value(r[i], v) + br[v], s, rest);
+                out[v] = fmaf(s, tanh_of<PRECISE>(c[v], slope), rest * scan_value(w[i], v));
+            }
+            if (p.on) *(raw_t *)(hr + i * H + p.ch) = scan_pack<T, V>(out);
+        }
+    }
+    if (c_last && p.seg == g.segments - 1 && p.wave == 0 && p.on) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) c_last[(size_t)p.b * H + p.ch + v] = c_in[v];
+    }
 }
 
-template <class T, bool HIGHWAY>
-__global__ __launch_bounds__(SCAN_THREADS) void sru_scan_backward_kernel(
-    const T *__restrict__ dh, const float *dc_last, const T *__restrict__ u, const T *__restrict__ x, const float *__restrict__ b_f,
-    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, int L, int H, int blocks,
+// The pairs of the first segments, [b][segment][channel]; a wavefront walks its own part of the segment from one end to the other.  Segment
+// 0 lays c0 down beside them: c_last may be c0, and the main launch's last segment writes it while others still read.
+template <class T, int V>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(ScanShape g, const T *__restrict__ u, int blocks,
+                                                                             const float *__restrict__ b_f, const float *__restrict__ c0,
+                                                                             const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
+                                                                             float *__restrict__ c0_copy)
+{
+    constexpr bool PRECISE = sizeof(T) == 4;
+    typedef scan_raw_t<T, V> raw_t;
+    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE * V];
+    ScanPlace<T, V> p;
+    if (!p.find(g, lengths, g.segments - 1)) return;
+    const size_t H = g.H, row_len = blocks * H;
+    float bf[V], A[V], C[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) bf[v] = b_f ? b_f[p.col + v] : 0.f, A[v] = 1.f, C[v] = 0.f;
+    const int part = g.seg_steps / p.waves, from = p.first + p.wave * part, to = from + part;     // whole runs: seg_steps is whole rounds
+    for (int t0 = from; t0 < to; t0 += SCAN_STEPS) {
+        const int count = min(p.n - t0, SCAN_STEPS);
+        const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
+        raw_t z[SCAN_STEPS], a[SCAN_STEPS];
+        scan_load<T, V>(z, rows, row_len, p.col, count);
+        scan_load<T, V>(a, rows + H, row_len, p.col, count);
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) {
+            if (i >= count) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float f, rest;
+                gate_of<PRECISE>(scan_value(a[i], v) + bf[v], f, rest);
+                A[v] *= f;
+                C[v] = fmaf(f, C[v], rest * scan_value(z[i], v));
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
+    __syncthreads();
+    if (p.wave != 0 || !p.on) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        for (int j = 1; j < p.waves; ++j) {
+            const float2 q = sums[j][p.lane * V + v];
+            C[v] = fmaf(q.x, C[v], q.y);
+            A[v] *= q.x;
+        }
+        pairs[((size_t)p.b * (g.segments - 1) + p.seg) * H + p.ch + v] = make_float2(A[v], C[v]);
+        if (p.seg == 0) c0_copy[(size_t)p.b * H + p.ch + v] = c0 ? c0[(size_t)p.b * H + p.ch + v] : 0.f;
+    }
+}
+
+// what a step of the gradient needs of the forward, from the state before it: e and the factors of the outputs
+template <bool PRECISE>
+struct ScanStep {
+    float f, rest, e, gap;       // gate, 1 - gate, dh r tanh'(c), (c_{t-1} - z) f (1 - f)
+    float d_r, d_w;              // du2 and dw
+    __device__ __forceinline__ void make(float &c, float z, float a, float r, float w, float dh)
+    {
+        float s, off, slope;
+        gate_of<PRECISE>(a, f, rest);
+        gate_of<PRECISE>(r, s, off);
+        gap = (c - z) * (f * rest);
+        c = fmaf(f, c, rest * z);
+        const float t = tanh_of<PRECISE>(c, slope);
+        e = dh * s * slope;
+        d_w = dh * off;
+        d_r = dh * (t - w) * (s * off);
+    }
+};
+
+template <class T, int V, bool HIGHWAY>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel(
+    ScanShape g, const T *__restrict__ dh, const float *dc_last, const T *__restrict__ u, const T *__restrict__ x, const float *__restrict__ b_f,
+    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, const float2 *__restrict__ pairs,
     T *__restrict__ du, T *__restrict__ dx, float *__restrict__ db, float *dc0)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    const int b = blockIdx.x / blocks, ch = blockIdx.x % blocks * SCAN_THREADS + threadIdx.x;
-    if (ch >= H) return;
-    const int n = lengths ? min(max(lengths[b], 0), L) : L;
-    const float bf = b_f ? b_f[ch] : 0.f, br = b_r ? b_r[ch] : 0.f;
-    const int saved = (L + SCAN_STEPS - 1) / SCAN_STEPS;
-    float dc = dc_last ? dc_last[(size_t)b * H + ch] : 0.f, sum_f = 0.f, sum_r = 0.f;
-    for (int part = saved - 1; part >= 0; --part) {
-        const int t0 = part * SCAN_STEPS, t1 = min(L, t0 + SCAN_STEPS);
-        float before[SCAN_STEPS];
-        float c = states[((size_t)b * saved + part) * H + ch];
+    typedef scan_raw_t<T, V> raw_t;
+    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE * V];
+    ScanPlace<T, V> p;
+    if (!p.find(g, lengths, g.segments)) return;
+    const size_t H = g.H, row_len = K * H;
+    float bf[V], br[V], d_in[V], sum_f[V], sum_r[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bf[v] = b_f ? b_f[p.col + v] : 0.f;
+        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        d_in[v] = dc_last ? dc_last[(size_t)p.b * H + p.col + v] : 0.f;
+        d_in[v] = scan_fold(d_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, g.segments - 1 - p.seg);
+        sum_f[v] = sum_r[v] = 0.f;
+    }
+    const int round = p.waves * SCAN_STEPS, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
+    for (int at = rounds - 1, parity = 0; at >= 0; --at, parity ^= 1) {
+        const int t0 = p.first + at * round + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);
+        const size_t row = (size_t)p.b * g.L + t0;
+        const T *rows = u + row * row_len;
+        T *out = du + row * row_len, *out_w = HIGHWAY ? dx + row * H : out + 3 * H;
+        const size_t w_len = HIGHWAY ? H : row_len;
+        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
+        scan_load<T, V>(z, rows, row_len, p.col, count);
+        scan_load<T, V>(a, rows + H, row_len, p.col, count);
+        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
+        scan_load<T, V>(w, HIGHWAY ? x + row * H : rows + 3 * H, w_len, p.col, count);
+        scan_load<T, V>(d, dh + row * H, H, p.col, count);
+        float f[SCAN_STEPS][V], rest[SCAN_STEPS][V], e[SCAN_STEPS][V], gap[SCAN_STEPS][V], c[V], A[V], D[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            c[v] = count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v] : 0.f;
+            A[v] = 1.f, D[v] = 0.f;
+        }
 #pragma unroll
         for (int i = 0; i < SCAN_STEPS; ++i) {
-            before[i] = c;
-            if (t0 + i >= n) continue;
-            const T *ur = u + ((size_t)b * L + t0 + i) * K * H + ch;
-            float f, fr;
-            gate_of<PRECISE>(value_of(ur[H]) + bf, f, fr);
-            c = fmaf(f, c, fr * value_of(ur[0]));
+            if (i >= count) {
+                if (t0 + i < p.last && p.on) {
+                    *(raw_t *)(out + i * row_len + p.ch) = 0;
+                    *(raw_t *)(out + i * row_len + H + p.ch) = 0;
+                    *(raw_t *)(out + i * row_len + 2 * H + p.ch) = 0;
+                    *(raw_t *)(out_w + i * w_len + p.ch) = 0;
+                }
+                continue;
+            }
+            float d_r[V], d_w[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                ScanStep<PRECISE> s;
+                s.make(c[v], scan_value(z[i], v), scan_value(a[i], v) + bf[v], scan_value(r[i], v) + br[v], scan_value(w[i], v),
+                       scan_value(d[i], v));
+                f[i][v] = s.f, rest[i][v] = s.rest, e[i][v] = s.e, gap[i][v] = s.gap;
+                d_r[v] = s.d_r, d_w[v] = s.d_w;
+                sum_r[v] += s.d_r;
+            }
+            if (p.on) {
+                *(raw_t *)(out + i * row_len + 2 * H + p.ch) = scan_pack<T, V>(d_r);
+                *(raw_t *)(out_w + i * w_len + p.ch) = scan_pack<T, V>(d_w);
+            }
         }
 #pragma unroll
         for (int i = SCAN_STEPS - 1; i >= 0; --i) {
-            const int t = t0 + i;
-            if (t >= t1) continue;
-            const size_t row = (size_t)b * L + t;
-            T *dr = du + row * K * H + ch, *dw = HIGHWAY ? dx + row * H + ch : dr + (size_t)(K - 1) * H;
-            if (t >= n) {
-                store_value(dr, 0.f), store_value(dr + H, 0.f), store_value(dr + 2 * (size_t)H, 0.f), store_value(dw, 0.f);
-                continue;
+            if (i >= count) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                D[v] = (D[v] + e[i][v]) * f[i][v];
+                A[v] *= f[i][v];
             }
-            const T *ur = u + row * K * H + ch;
-            const float z = value_of(ur[0]), w = HIGHWAY ? value_of(x[row * H + ch]) : value_of(ur[(size_t)(K - 1) * H]);
-            float f, fr, r, rr, slope;
-            gate_of<PRECISE>(value_of(ur[H]) + bf, f, fr);
-            gate_of<PRECISE>(value_of(ur[2 * (size_t)H]) + br, r, rr);
-            const float g = tanh_of<PRECISE>(fmaf(f, before[i], fr * z), slope), d = value_of(dh[row * H + ch]);
-            const float full = fmaf(d * r, slope, dc);
-            const float d_f = full * (before[i] - z) * (f * fr), d_r = d * (g - w) * (r * rr);
-            store_value(dw, d * rr);
-            store_value(dr, full * fr);
-            store_value(dr + H, d_f);
-            store_value(dr + 2 * (size_t)H, d_r);
-            sum_f += d_f;
-            sum_r += d_r;
-            dc = full * f;
+        }
+        float dc[V];
+        if (p.waves > 1) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                dc[v] = d_in[v];
+                for (int j = p.waves - 1; j >= 0; --j) {
+                    const float2 q = sums[parity][j][p.lane * V + v];
+                    d_in[v] = fmaf(q.x, d_in[v], q.y);
+                    if (j - 1 == p.wave) dc[v] = d_in[v];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) dc[v] = d_in[v], d_in[v] = fmaf(A[v], d_in[v], D[v]);
+        }
+#pragma unroll
+        for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+            if (i >= count) continue;
+            float d_z[V], d_f[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float full = dc[v] + e[i][v];
+                d_z[v] = full * rest[i][v];
+                d_f[v] = full * gap[i][v];
+                sum_f[v] += d_f[v];
+                dc[v] = full * f[i][v];
+            }
+            if (p.on) {
+                *(raw_t *)(out + i * row_len + p.ch) = scan_pack<T, V>(d_z);
+                *(raw_t *)(out + i * row_len + H + p.ch) = scan_pack<T, V>(d_f);
+            }
         }
     }
-    if (dc0) dc0[(size_t)b * H + ch] = dc;
-    db[(size_t)b * 2 * H + ch] = sum_f;
-    db[((size_t)b * 2 + 1) * H + ch] = sum_r;
+    if (dc0 && p.seg == 0 && p.wave == 0 && p.on) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) dc0[(size_t)p.b * H + p.ch + v] = d_in[v];
+    }
+    if (!db) return;
+    // the wavefronts' sums in their order, a row of [2 H] for each sequence and segment
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) sums[0][p.wave][p.lane * V + v] = make_float2(sum_f[v], sum_r[v]);
+    __syncthreads();
+    if (p.wave != 0 || !p.on) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        for (int j = 1; j < p.waves; ++j) {
+            const float2 q = sums[0][j][p.lane * V + v];
+            sum_f[v] += q.x;
+            sum_r[v] += q.y;
+        }
+        float *to = db + ((size_t)p.b * g.segments + p.seg) * 2 * H + p.ch + v;
+        to[0] = sum_f[v];
+        to[H] = sum_r[v];
+    }
 }
 
-// db_f and db_r: the parts' sums in their order
-__global__ __launch_bounds__(SCAN_THREADS) void sru_scan_bias_kernel(const float *__restrict__ db, int parts, int H, float *__restrict__ db_f,
-                                                                     float *__restrict__ db_r)
+// The gradient's pairs of the last segments, [b][segments-1-segment][channel] (the order they are met in), and dc_last beside them, as above.
+template <class T, int V>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_kernel(
+    ScanShape g, const T *__restrict__ dh, const float *__restrict__ dc_last, const T *__restrict__ u, int blocks, const float *__restrict__ b_f,
+    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
+    float *__restrict__ dc_copy)
 {
-    const int ch = blockIdx.x * SCAN_THREADS + threadIdx.x;
-    if (ch >= 2 * H) return;
-    float *out = ch < H ? db_f : db_r;
-    if (!out) return;
+    constexpr bool PRECISE = sizeof(T) == 4;
+    typedef scan_raw_t<T, V> raw_t;
+    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE * V];
+    ScanPlace<T, V> p;
+    if (!p.find(g, lengths, g.segments - 1)) return;
+    p.seg += 1, p.first += g.seg_steps;                // segment 0 has no one before it
+    const size_t H = g.H, row_len = blocks * H;
+    float bf[V], br[V], A[V], D[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bf[v] = b_f ? b_f[p.col + v] : 0.f;
+        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        A[v] = 1.f, D[v] = 0.f;
+    }
+    const int part = g.seg_steps / p.waves, from = p.first + p.wave * part;
+    for (int t0 = from + part - SCAN_STEPS; t0 >= from; t0 -= SCAN_STEPS) {
+        const int count = min(p.n - t0, SCAN_STEPS);
+        if (count <= 0) continue;
+        const size_t row = (size_t)p.b * g.L + t0;
+        const T *rows = u + row * row_len;
+        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
+        scan_load<T, V>(z, rows, row_len, p.col, count);
+        scan_load<T, V>(a, rows + H, row_len, p.col, count);
+        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
+        scan_load<T, V>(d, dh + row * H, H, p.col, count);
+        float f[SCAN_STEPS][V], e[SCAN_STEPS][V], c[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v];
+#pragma unroll
+        for (int i = 0; i < SCAN_STEPS; ++i) {
+            if (i >= count) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                ScanStep<PRECISE> s;
+                s.make(c[v], scan_value(z[i], v), scan_value(a[i], v) + bf[v], scan_value(r[i], v) + br[v], 0.f, scan_value(d[i], v));
+                f[i][v] = s.f, e[i][v] = s.e;
+            }
+        }
+#pragma unroll
+        for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+            if (i >= count) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                D[v] = (D[v] + e[i][v]) * f[i][v];
+                A[v] *= f[i][v];
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
+    __syncthreads();
+    if (p.wave != p.waves - 1 || !p.on) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        for (int j = p.waves - 2; j >= 0; --j) {
+            const float2 q = sums[j][p.lane * V + v];
+            D[v] = fmaf(q.x, D[v], q.y);
+            A[v] *= q.x;
+        }
+        pairs[((size_t)p.b * (g.segments - 1) + (g.segments - 1 - p.seg)) * H + p.ch + v] = make_float2(A[v], D[v]);
+        if (p.seg == g.segments - 1) dc_copy[(size_t)p.b * H + p.ch + v] = dc_last ? dc_last[(size_t)p.b * H + p.ch + v] : 0.f;
+    }
+}
+
+// db_f and db_r: 64 channels per workgroup; its wavefronts take the parts' sums in turn, and are added in their order
+constexpr int BIAS_WAVES = 16;
+
+__global__ __launch_bounds__(BIAS_WAVES *WAVE) void sru_scan_bias_kernel(const float *__restrict__ db, int parts, int H, float *__restrict__ db_f,
+                                                                        float *__restrict__ db_r)
+{
+    __shared__ float sums[BIAS_WAVES][WAVE];
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    const size_t col = (size_t)blockIdx.x * WAVE + lane, width = 2 * (size_t)H;
     float sum = 0.f;
-    for (int p = 0; p < parts; ++p) sum += db[(size_t)p * 2 * H + ch];
-    out[ch < H ? ch : ch - H] = sum;
+    if (col < width) {
+#pragma unroll 8
+        for (int i = wave; i < parts; i += BIAS_WAVES) sum += db[i * width + col];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0 || col >= width) return;
+#pragma unroll
+    for (int j = 1; j < BIAS_WAVES; ++j) sum += sums[j][lane];
+    float *out = col < (size_t)H ? db_f : db_r;
+    if (out) out[col < (size_t)H ? col : col - H] = sum;
 }
 
 static int scan_check(const char *who, int B, int L, int H, int n_blocks, int dtype, const void *x)
@@ -116,8 +486,20 @@ static int scan_check(const char *who, int B, int L, int H, int n_blocks, int dt
     MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
     MOE_REQUIRE(n_blocks == 3 || n_blocks == 4, MOE_ERR_INVALID_ARG, "%s: n_blocks=%d (3 with x, 4 without)", who, n_blocks);
     MOE_REQUIRE(n_blocks == 3 || !x, MOE_ERR_INVALID_ARG, "%s: x given beside a fourth block", who);
-    MOE_REQUIRE((long long)B * ((H + SCAN_THREADS - 1) / SCAN_THREADS) < (1 << 26), MOE_ERR_UNSUPPORTED, "%s: B=%d H=%d too large", who, B, H);
+    MOE_REQUIRE(scan_takes(B, L, H), MOE_ERR_UNSUPPORTED, "%s: B=%d L=%d H=%d too large", who, B, L, H);
     return MOE_OK;
+}
+
+// pairs, then the copy of the state that the first workgroup starts from
+static size_t scan_pairs_bytes(const ScanShape &g)
+{
+    return g.segments < 2 ? 0 : ((size_t)g.B * (g.segments - 1) * sizeof(float2) + (size_t)g.B * sizeof(float)) * g.H;
+}
+
+static dim3 scan_grid(const ScanShape &g, int segments)
+{
+    const long long n = (long long)g.B * segments * g.groups, across = n < (1 << 22) ? n : 1 << 22;
+    return dim3((unsigned)across, (unsigned)((n + across - 1) / across));
 }
 
 }  // namespace moe
@@ -132,16 +514,24 @@ extern "C" size_t sru_scan_states_bytes(int B, int L, int H)
 
 extern "C" size_t sru_scan_workspace_bytes(int B, int L, int H, int dtype)
 {
-    (void)B, (void)L, (void)H, (void)dtype;
-    return 0;
+    if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
+    return scan_pairs_bytes(scan_shape(B, L, H, dtype));
 }
 
 extern "C" size_t sru_scan_backward_workspace_bytes(int B, int L, int H, int dtype)
 {
-    (void)L, (void)dtype;
-    if (B <= 0 || H <= 0) return 0;
-    return (size_t)B * 2 * H * sizeof(float);
+    if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
+    const ScanShape g = scan_shape(B, L, H, dtype);
+    return scan_pairs_bytes(g) + (size_t)B * g.segments * 2 * H * sizeof(float);
 }
+
+// FORM(T, V): the builds for a type and a width
+#define MOE_SCAN_FORMS(FORM)                                    \
+    do {                                                        \
+        if (dtype == MOE_F32) FORM(float, 1);                   \
+        else if (scan_width(H, dtype) == 2) FORM(bf16_t, 2);    \
+        else FORM(bf16_t, 1);                                   \
+    } while (0)
 
 extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const float *b_r, const float *c0, const int32_t *lengths, int B,
                         int L, int H, int n_blocks, int dtype, void *h, float *c_last, void *states, void *ws, size_t ws_bytes, void *stream)
@@ -153,18 +543,33 @@ extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const fl
         MOE_REQUIRE(h != u && h != x, MOE_ERR_INVALID_ARG, "sru_scan: h aliases an input");
         MOE_REQUIRE(aligned16(u) && aligned16(x) && aligned16(h) && aligned16(states), MOE_ERR_INVALID_ARG, "sru_scan: tensor misaligned");
     }
-    const int blocks = (H + SCAN_THREADS - 1) / SCAN_THREADS;
+    const ScanShape g = scan_shape(B, L, H, dtype);
+    const size_t need = scan_pairs_bytes(g);
+    MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "sru_scan: workspace of %zu bytes given, %zu needed",
+                ws ? ws_bytes : 0, need);
     hipStream_t st = (hipStream_t)stream;
-#define MOE_SCAN(T, HW)                                                                                                          \
-    hipLaunchKernelGGL((sru_scan_kernel<T, HW>), dim3(B *blocks), dim3(SCAN_THREADS), 0, st, (const T *)u, (const T *)x, b_f, b_r, c0, \
-                       lengths, L, H, blocks, (T *)h, c_last, (float *)states)
-    if (dtype == MOE_BF16) {
-        if (n_blocks == 3) MOE_SCAN(bf16_t, true);
-        else MOE_SCAN(bf16_t, false);
-    } else {
-        if (n_blocks == 3) MOE_SCAN(float, true);
-        else MOE_SCAN(float, false);
+    float2 *pairs = (float2 *)ws;
+    const dim3 threads(g.waves * WAVE);
+    if (g.segments > 1) {
+        float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
+#define MOE_PAIRS(T, V)                                                                                                                        \
+    hipLaunchKernelGGL((sru_scan_pairs_kernel<T, V>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)u, n_blocks, b_f, c0, lengths, \
+                       pairs, copy)
+        MOE_SCAN_FORMS(MOE_PAIRS);
+#undef MOE_PAIRS
+        MOE_CHECK_LAUNCH("sru_scan");
+        c0 = copy;
     }
+#define MOE_SCAN(T, V, HW)                                                                                                                 \
+    hipLaunchKernelGGL((sru_scan_kernel<T, V, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, \
+                       pairs, (T *)h, c_last, (float *)states)
+#define MOE_MAIN(T, V)                              \
+    do {                                            \
+        if (n_blocks == 3) MOE_SCAN(T, V, true);    \
+        else MOE_SCAN(T, V, false);                 \
+    } while (0)
+    MOE_SCAN_FORMS(MOE_MAIN);
+#undef MOE_MAIN
 #undef MOE_SCAN
     MOE_CHECK_LAUNCH("sru_scan");
     return MOE_OK;
@@ -187,25 +592,38 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
     const size_t need = sru_scan_backward_workspace_bytes(B, L, H, dtype);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
                 "sru_scan_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
-    const int blocks = (H + SCAN_THREADS - 1) / SCAN_THREADS;
     hipStream_t st = (hipStream_t)stream;
-#define MOE_SCAN(T, HW)                                                                                                                   \
-    hipLaunchKernelGGL((sru_scan_backward_kernel<T, HW>), dim3(B *blocks), dim3(SCAN_THREADS), 0, st, (const T *)dh, dc_last, (const T *)u, \
-                       (const T *)x, b_f, b_r, (const float *)states, lengths, L, H, blocks, (T *)du, (T *)dx, (float *)ws, dc0)
+    const ScanShape g = scan_shape(B, L, H, dtype);
+    float2 *pairs = (float2 *)ws;
+    float *db = db_f || db_r ? (float *)((char *)ws + scan_pairs_bytes(g)) : nullptr;
     if (B > 0) {
-        if (dtype == MOE_BF16) {
-            if (n_blocks == 3) MOE_SCAN(bf16_t, true);
-            else MOE_SCAN(bf16_t, false);
-        } else {
-            if (n_blocks == 3) MOE_SCAN(float, true);
-            else MOE_SCAN(float, false);
+        const dim3 threads(g.waves * WAVE);
+        if (g.segments > 1) {
+            float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
+#define MOE_PAIRS(T, V)                                                                                                                       \
+    hipLaunchKernelGGL((sru_scan_backward_pairs_kernel<T, V>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+                       n_blocks, b_f, b_r, (const float *)states, lengths, pairs, copy)
+            MOE_SCAN_FORMS(MOE_PAIRS);
+#undef MOE_PAIRS
+            MOE_CHECK_LAUNCH("sru_scan_backward");
+            dc_last = copy;
         }
+#define MOE_SCAN(T, V, HW)                                                                                                                    \
+    hipLaunchKernelGGL((sru_scan_backward_kernel<T, V, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+                       (const T *)x, b_f, b_r, (const float *)states, lengths, pairs, (T *)du, (T *)dx, db, dc0)
+#define MOE_MAIN(T, V)                              \
+    do {                                            \
+        if (n_blocks == 3) MOE_SCAN(T, V, true);    \
+        else MOE_SCAN(T, V, false);                 \
+    } while (0)
+        MOE_SCAN_FORMS(MOE_MAIN);
+#undef MOE_MAIN
+#undef MOE_SCAN
         MOE_CHECK_LAUNCH("sru_scan_backward");
     }
-#undef MOE_SCAN
     if (db_f || db_r) {
-        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3((2 * H + SCAN_THREADS - 1) / SCAN_THREADS), dim3(SCAN_THREADS), 0, st, (const float *)ws,
-                           B, H, db_f, db_r);
+        const unsigned across = (unsigned)((2 * (size_t)H + WAVE - 1) / WAVE);
+        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3(across), dim3(BIAS_WAVES * WAVE), 0, st, db, B * g.segments, H, db_f, db_r);
         MOE_CHECK_LAUNCH("sru_scan_backward");
     }
     return MOE_OK;

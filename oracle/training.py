@@ -1,7 +1,9 @@
 """Plain float64 forms of the gradients and of the calls that train the gate and the predictor, token by token or row by row.
 
 Arguments are float64 numpy arrays (index arrays: integers); nothing is rounded.  Beside a value, the scan gives a bound for the error
-of a binary32 evaluation: ``steps`` half-units in the last place (2^-24) relative for every gate, product and sum, carried along the same recurrence.
+of a binary32 evaluation: ``steps`` half-units in the last place (2^-24) relative for every gate, product and sum, carried along the same recurrence.  With ``bf16``, the bound of what bfloat16 results are made from:
+c = z + f (c - z) and h = w + r (tanh c - w) round the differences and have 1 - f and 1 - r from f and r, 4 half-units of the terms' own
+magnitudes, and tanh is off by up to 2.5e-5 of itself.
 """
 from __future__ import annotations
 
@@ -22,7 +24,7 @@ def _scan_terms(u, x, b_f, b_r):
     return blocks[:, :, 0], _sigmoid(zf), _sigmoid(-zf), _sigmoid(zr), _sigmoid(-zr), x if x is not None else blocks[:, :, 3]
 
 
-def sru_scan(u, x, b_f, b_r, c0, lengths, steps=32):
+def sru_scan(u, x, b_f, b_r, c0, lengths, steps=32, bf16=False):
     """-> dict(h, c_last, c [B,L+1,H] the states from c0 on, c_err their bounds, h_err)."""
     z, f, fr, r, rr, w = _scan_terms(u, x, b_f, b_r)
     B, L, H = z.shape
@@ -31,6 +33,7 @@ def sru_scan(u, x, b_f, b_r, c0, lengths, steps=32):
     h, h_err = np.zeros((B, L, H)), np.zeros((B, L, H))
     c[:, 0] = c0
     e = steps * EPS
+    blend, off = (4 * EPS, 2.5e-5) if bf16 else (0.0, 0.0)
     for b in range(B):
         for t in range(L):
             if t >= lengths[b]:
@@ -38,16 +41,18 @@ def sru_scan(u, x, b_f, b_r, c0, lengths, steps=32):
                 continue
             keep, new = f[b, t] * c[b, t], fr[b, t] * z[b, t]
             c[b, t + 1] = keep + new
-            err[b, t + 1] = f[b, t] * err[b, t] + e * (np.abs(keep) + np.abs(new))
+            err[b, t + 1] = f[b, t] * err[b, t] + e * (np.abs(keep) + np.abs(new)) + blend * (np.abs(c[b, t]) + np.abs(z[b, t]))
             g = np.tanh(c[b, t + 1])
             h[b, t] = r[b, t] * g + rr[b, t] * w[b, t]
-            h_err[b, t] = r[b, t] * (1 - g * g) * err[b, t + 1] + err[b, t + 1] ** 2 + e * (np.abs(r[b, t] * g) + np.abs(rr[b, t] * w[b, t]))
+            h_err[b, t] = r[b, t] * (1 - g * g) * err[b, t + 1] + err[b, t + 1] ** 2 + e * (np.abs(r[b, t] * g) + np.abs(rr[b, t] * w[b, t])) \
+                + blend * (np.abs(g) + np.abs(w[b, t])) + off * np.abs(r[b, t] * g)
     return dict(h=h, c_last=c[:, -1].copy(), c=c, c_err=err, h_err=h_err)
 
 
-def sru_scan_backward(dh, dc_last, u, x, b_f, b_r, c0, lengths, steps=32):
+def sru_scan_backward(dh, dc_last, u, x, b_f, b_r, c0, lengths, steps=32, bf16=False):
     """-> dict(du, dx, db_f, db_r, dc0) and a dict of bounds under the same keys."""
-    fw = sru_scan(u, x, b_f, b_r, c0, lengths, steps)
+    fw = sru_scan(u, x, b_f, b_r, c0, lengths, steps, bf16)
+    off = 2.5e-5 if bf16 else 0.0
     c, c_err = fw["c"], fw["c_err"]
     z, f, fr, r, rr, w = _scan_terms(u, x, b_f, b_r)
     B, L, H = z.shape
@@ -70,7 +75,7 @@ def sru_scan_backward(dh, dc_last, u, x, b_f, b_r, c0, lengths, steps=32):
             parts[1][b, t] = full * gap * s
             errs[1][b, t] = s * (full_e * (np.abs(gap) + c_err[b, t]) + np.abs(full) * (c_err[b, t] + e * (np.abs(c[b, t]) + np.abs(z[b, t]))))
             parts[2][b, t] = d * (g - w[b, t]) * r[b, t] * rr[b, t]
-            errs[2][b, t] = np.abs(d) * r[b, t] * rr[b, t] * (slope * ce + ce ** 2 + e * (np.abs(g) + np.abs(w[b, t])))
+            errs[2][b, t] = np.abs(d) * r[b, t] * rr[b, t] * (slope * ce + ce ** 2 + e * (np.abs(g) + np.abs(w[b, t])) + off * np.abs(g))
             parts[3][b, t], errs[3][b, t] = d * rr[b, t], e * np.abs(d * rr[b, t])
             dc, dc_e = full * f[b, t], f[b, t] * (full_e + e * np.abs(full))
         dc0[b], dc0_err[b] = dc, dc_e

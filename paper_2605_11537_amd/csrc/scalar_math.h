@@ -1,15 +1,18 @@
-// Exponentials, gates and conversions of one value, for kernels that read and write a stream of them.
+// Exponentials, gates and conversions of one value, for kernels that read and write a stream of them.  PRECISE: for binary32 results;
+// without it for bfloat16 ones, where a kernel that streams two bytes a value has some ten vector instructions for each and the
+// transcendental ones count four times.
 #pragma once
 #include "common.h"
 
 namespace moe {
 
+constexpr float LOG2E = 1.44269504f, LOG2E_LOW = 1.92596299e-8f, LN2 = 0.693147181f;
+
 // e^x.  The hardware gives 2^y; y = x log2(e) rounded once is off by |x| 2^-24 relative, which a bfloat16 result does not see.  PRECISE
-// (binary32 results) takes the product's error along: four more operations, off by little more than the hardware's own last bit.
+// takes the product's error along: four more operations, off by little more than the hardware's own last bit.
 template <bool PRECISE>
 __device__ __forceinline__ float exp_of(float x)
 {
-    constexpr float LOG2E = 1.44269504f, LOG2E_LOW = 1.92596299e-8f, LN2 = 0.693147181f;
     const float y = x * LOG2E, e = __builtin_amdgcn_exp2f(y);
     if (!PRECISE) return e;
     const float low = fmaf(x, LOG2E_LOW, fmaf(x, LOG2E, -y));
@@ -17,28 +20,63 @@ __device__ __forceinline__ float exp_of(float x)
     return fabsf(x) < 126.f ? fmaf(e, low * LN2, e) : e;
 }
 
-// s = 1 / (1 + e^-z) and 1 - s, each with its own relative accuracy (1 - s taken from s would have lost a closed gate's bits).  e^-z is kept
-// finite, so that the second is no infinity times zero; a NaN passes.
+// A gate's bias as gate_of and gate_open take it: without PRECISE -b log2(e), so that the exponent is one multiply-add of the
+// pre-activation.
 template <bool PRECISE>
-__device__ __forceinline__ void gate_of(float z, float &s, float &rest)
+__device__ __forceinline__ float gate_bias(float b) { return PRECISE ? b : -LOG2E * b; }
+
+// s = 1 / (1 + e^-(a + b))
+template <bool PRECISE>
+__device__ __forceinline__ float gate_open(float a, float bias)
 {
-    const float e = exp_of<PRECISE>(z < -80.f ? 80.f : -z);
+    const float e = PRECISE ? exp_of<true>(-(a + bias)) : __builtin_amdgcn_exp2f(fmaf(a, -LOG2E, bias));
+    return __builtin_amdgcn_rcpf(1.f + e);
+}
+
+// The same with 1 - s, each with its own relative accuracy (1 - s taken from s would have lost a closed gate's bits).  The exponential is kept
+// finite, so that the second is no infinity times zero: neither goes below e^-80; a NaN passes.
+template <bool PRECISE>
+__device__ __forceinline__ void gate_of(float a, float bias, float &s, float &rest)
+{
+    float e;
+    if (PRECISE) {
+        const float z = a + bias;
+        e = exp_of<true>(z < -80.f ? 80.f : -z);
+    } else {
+        const float y = fmaf(a, -LOG2E, bias);
+        e = __builtin_amdgcn_exp2f(y > 115.4f ? 115.4f : y);
+    }
     s = __builtin_amdgcn_rcpf(1.f + e);
     rest = e * s;
 }
 
-// tanh c, and 1 - tanh^2 c = 4 a / (1 + a)^2 with a = e^(-2|c|): no overflow and no cancellation.  Small arguments take the series, since
-// 1 - a loses bits there: up to |c| = 0.25 with five terms, off by 1e-8 (PRECISE), up to 0.06 with two, off by 2e-6.
+// tanh c = (1 - a) / (1 + a), a = e^(-2|c|).  1 - a loses bits where c is small: there PRECISE takes the series (up to 0.25, five terms, off by
+// 1e-8), a bfloat16 result c itself (up to 0.007: c^2 / 3 and what 1 - a has lost are both below 2e-5).
+template <bool PRECISE>
+__device__ __forceinline__ float tanh_of(float c)
+{
+    if (!PRECISE) {
+        const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * LOG2E * c)), 1.f);
+        return fabsf(c) < 0.007f ? c : t;
+    }
+    const float a = exp_of<true>(-2.f * fabsf(c)), c2 = c * c;
+    const float t = copysignf((1.f - a) * __builtin_amdgcn_rcpf(1.f + a), c);
+    const float series = fmaf(c2, fmaf(c2, fmaf(c2, fmaf(c2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return fabsf(c) < 0.25f ? c * series : t;
+}
+
+// with its slope, 1 - tanh^2 c = 4 a / (1 + a)^2: no overflow and no cancellation
 template <bool PRECISE>
 __device__ __forceinline__ float tanh_of(float c, float &slope)
 {
     const float a = exp_of<PRECISE>(-2.f * fabsf(c));
     const float q = __builtin_amdgcn_rcpf(1.f + a);
-    const float t = copysignf((1.f - a) * q, c), c2 = c * c;
-    slope = 4.f * a * (q * q);
-    const float series = PRECISE ? fmaf(c2, fmaf(c2, fmaf(c2, fmaf(c2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f)
-                                 : fmaf(c2, -1.f / 3.f, 1.f);
-    return fabsf(c) < (PRECISE ? 0.25f : 0.06f) ? c * series : t;
+    slope = a * q * (4.f * q);
+    const float t = copysignf((1.f - a) * q, c);
+    if (!PRECISE) return fabsf(c) < 0.007f ? c : t;
+    const float c2 = c * c;
+    const float series = fmaf(c2, fmaf(c2, fmaf(c2, fmaf(c2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return fabsf(c) < 0.25f ? c * series : t;
 }
 
 // a stored value as binary32 and back (one rounding)

@@ -58,22 +58,39 @@ struct ScanPlace {
     }
 };
 
-// the steps t0 .. t0+SCAN_STEPS-1 of one column block, those below end only
-template <class T, int V>
+// A wavefront's steps are all inside the sequence (FULL: no step is asked for), or some are not.
+struct ScanFull { static constexpr bool FULL = true; };
+struct ScanPart { static constexpr bool FULL = false; };
+template <bool FULL> __device__ __forceinline__ bool scan_in(int i, int count) { return FULL || i < count; }
+
+// the steps of one column block, the first count of them
+template <class T, int V, bool FULL>
 __device__ __forceinline__ void scan_load(scan_raw_t<T, V> (&to)[SCAN_STEPS], const T *row0, size_t row_len, unsigned col, int count)
 {
-    typedef scan_raw_t<T, V> raw_t;
-    if (count >= SCAN_STEPS) {
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) to[i] = *(const raw_t *)(row0 + i * row_len + col);
-    } else {
-#pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            to[i] = 0;
-            if (i < count) to[i] = *(const raw_t *)(row0 + i * row_len + col);
-        }
+    for (int i = 0; i < SCAN_STEPS; ++i) {
+        if (!FULL) to[i] = 0;
+        if (scan_in<FULL>(i, count)) to[i] = *(const scan_raw_t<T, V> *)(row0 + i * row_len + col);
     }
 }
+
+// c_t from c_{t-1}: f c + (1 - f) z with both gates' own accuracy, or z + f (c - z) for bfloat16 results
+template <bool PRECISE>
+struct ScanForward {
+    float f, in;
+    __device__ __forceinline__ void make(float a, float bias, float z)
+    {
+        if (PRECISE) {
+            float rest;
+            gate_of<true>(a, bias, f, rest);
+            in = rest * z;
+        } else {
+            f = gate_open<false>(a, bias);
+            in = z;
+        }
+    }
+    __device__ __forceinline__ float next(float c) const { return PRECISE ? fmaf(f, c, in) : fmaf(f, c - in, in); }
+};
 
 // the state that a pair list before this place leads to
 __device__ __forceinline__ float scan_fold(float c, const float2 *pairs, size_t step, int count)
@@ -102,76 +119,84 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
     float bf[V], br[V], c_in[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bf[v] = b_f ? b_f[p.col + v] : 0.f;
-        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
+        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
         c_in[v] = c0 ? c0[(size_t)p.b * H + p.col + v] : 0.f;
         c_in[v] = scan_fold(c_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, p.seg);
     }
     const int round = p.waves * SCAN_STEPS;
     for (int t = p.first, parity = 0; t < p.last; t += round, parity ^= 1) {
         const int t0 = t + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);    // this wavefront's steps inside the sequence
-        const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
-        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
-        scan_load<T, V>(z, rows, row_len, p.col, count);
-        scan_load<T, V>(a, rows + H, row_len, p.col, count);
-        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
-        if (HIGHWAY) scan_load<T, V>(w, x + ((size_t)p.b * g.L + t0) * H, H, p.col, count);
-        else scan_load<T, V>(w, rows + 3 * H, row_len, p.col, count);
-        float f[SCAN_STEPS][V], in[SCAN_STEPS][V], A[V], C[V];
+        auto steps = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
+            const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
+            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
+            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
+            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
+            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
+            if (HIGHWAY) scan_load<T, V, FULL>(w, x + ((size_t)p.b * g.L + t0) * H, H, p.col, count);
+            else scan_load<T, V, FULL>(w, rows + 3 * H, row_len, p.col, count);
+            ScanForward<PRECISE> s[SCAN_STEPS][V];
+            float A[V], C[V], c[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.f, C[v] = 0.f;
+            for (int v = 0; v < V; ++v) A[v] = 1.f, C[v] = 0.f;
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            if (i >= count) continue;
+            for (int i = 0; i < SCAN_STEPS; ++i) {
+                if (!scan_in<FULL>(i, count)) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float rest;
-                gate_of<PRECISE>(scan_value(a[i], v) + bf[v], f[i][v], rest);
-                in[i][v] = rest * scan_value(z[i], v);
-                A[v] *= f[i][v];
-                C[v] = fmaf(f[i][v], C[v], in[i][v]);
-            }
-        }
-        float c[V];
-        if (p.waves > 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
-            __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = c_in[v];
-                for (int j = 0; j < p.waves; ++j) {
-                    const float2 q = sums[parity][j][p.lane * V + v];
-                    c_in[v] = fmaf(q.x, c_in[v], q.y);
-                    if (j + 1 == p.wave) c[v] = c_in[v];
+                for (int v = 0; v < V; ++v) {
+                    s[i][v].make(scan_value(a[i], v), bf[v], scan_value(z[i], v));
+                    A[v] *= s[i][v].f;
+                    C[v] = s[i][v].next(C[v]);
                 }
             }
-        } else {
+            if (p.waves > 1) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) c[v] = c_in[v], c_in[v] = fmaf(A[v], c_in[v], C[v]);
-        }
-        if (states && t0 < g.L && p.on) {
-            const size_t at = ((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch;
+                for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
+                barrier_anywhere();                    // a full and a partial wavefront wait for each other here
 #pragma unroll
-            for (int v = 0; v < V; ++v) states[at + v] = c[v];
-        }
-        T *hr = h + ((size_t)p.b * g.L + t0) * H;
+                for (int v = 0; v < V; ++v) {
+                    c[v] = c_in[v];
+                    for (int j = 0; j < p.waves; ++j) {
+                        const float2 q = sums[parity][j][p.lane * V + v];
+                        c_in[v] = fmaf(q.x, c_in[v], q.y);
+                        if (j + 1 == p.wave) c[v] = c_in[v];
+                    }
+                }
+            } else {
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            if (i >= count) {
-                if (t0 + i < p.last && p.on) *(raw_t *)(hr + i * H + p.ch) = 0;
-                continue;
+                for (int v = 0; v < V; ++v) c[v] = c_in[v], c_in[v] = fmaf(A[v], c_in[v], C[v]);
             }
-            float out[V];
+            if (states && (FULL || t0 < g.L) && p.on) {
+                const size_t at = ((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float s, rest, slope;
-                c[v] = fmaf(f[i][v], c[v], in[i][v]);
-                gate_of<PRECISE>(scan_value(r[i], v) + br[v], s, rest);
-                out[v] = fmaf(s, tanh_of<PRECISE>(c[v], slope), rest * scan_value(w[i], v));
+                for (int v = 0; v < V; ++v) states[at + v] = c[v];
             }
-            if (p.on) *(raw_t *)(hr + i * H + p.ch) = scan_pack<T, V>(out);
-        }
+            T *hr = h + ((size_t)p.b * g.L + t0) * H;
+#pragma unroll
+            for (int i = 0; i < SCAN_STEPS; ++i) {
+                if (!scan_in<FULL>(i, count)) {
+                    if (t0 + i < p.last && p.on) *(raw_t *)(hr + i * H + p.ch) = 0;
+                    continue;
+                }
+                float out[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    c[v] = s[i][v].next(c[v]);
+                    const float wv = scan_value(w[i], v), t = tanh_of<PRECISE>(c[v]);
+                    if (PRECISE) {
+                        float on, rest;
+                        gate_of<true>(scan_value(r[i], v), br[v], on, rest);
+                        out[v] = fmaf(on, t, rest * wv);
+                    } else {
+                        out[v] = fmaf(gate_open<false>(scan_value(r[i], v), br[v]), t - wv, wv);
+                    }
+                }
+                if (p.on) *(raw_t *)(hr + i * H + p.ch) = scan_pack<T, V>(out);
+            }
+        };
+        if (count >= SCAN_STEPS) steps(ScanFull());
+        else steps(ScanPart());
     }
     if (c_last && p.seg == g.segments - 1 && p.wave == 0 && p.on) {
 #pragma unroll
@@ -195,25 +220,30 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(Sc
     const size_t H = g.H, row_len = blocks * H;
     float bf[V], A[V], C[V];
 #pragma unroll
-    for (int v = 0; v < V; ++v) bf[v] = b_f ? b_f[p.col + v] : 0.f, A[v] = 1.f, C[v] = 0.f;
+    for (int v = 0; v < V; ++v) bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f), A[v] = 1.f, C[v] = 0.f;
     const int part = g.seg_steps / p.waves, from = p.first + p.wave * part, to = from + part;     // whole runs: seg_steps is whole rounds
     for (int t0 = from; t0 < to; t0 += SCAN_STEPS) {
         const int count = min(p.n - t0, SCAN_STEPS);
         const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
-        raw_t z[SCAN_STEPS], a[SCAN_STEPS];
-        scan_load<T, V>(z, rows, row_len, p.col, count);
-        scan_load<T, V>(a, rows + H, row_len, p.col, count);
+        auto steps = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
+            raw_t z[SCAN_STEPS], a[SCAN_STEPS];
+            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
+            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            if (i >= count) continue;
+            for (int i = 0; i < SCAN_STEPS; ++i) {
+                if (!scan_in<FULL>(i, count)) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float f, rest;
-                gate_of<PRECISE>(scan_value(a[i], v) + bf[v], f, rest);
-                A[v] *= f;
-                C[v] = fmaf(f, C[v], rest * scan_value(z[i], v));
+                for (int v = 0; v < V; ++v) {
+                    ScanForward<PRECISE> s;
+                    s.make(scan_value(a[i], v), bf[v], scan_value(z[i], v));
+                    A[v] *= s.f;
+                    C[v] = s.next(C[v]);
+                }
             }
-        }
+        };
+        if (count >= SCAN_STEPS) steps(ScanFull());
+        else steps(ScanPart());
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
@@ -236,11 +266,11 @@ template <bool PRECISE>
 struct ScanStep {
     float f, rest, e, gap;       // gate, 1 - gate, dh r tanh'(c), (c_{t-1} - z) f (1 - f)
     float d_r, d_w;              // du2 and dw
-    __device__ __forceinline__ void make(float &c, float z, float a, float r, float w, float dh)
+    __device__ __forceinline__ void make(float &c, float z, float a, float bf, float r, float br, float w, float dh)
     {
         float s, off, slope;
-        gate_of<PRECISE>(a, f, rest);
-        gate_of<PRECISE>(r, s, off);
+        gate_of<PRECISE>(a, bf, f, rest);
+        gate_of<PRECISE>(r, br, s, off);
         gap = (c - z) * (f * rest);
         c = fmaf(f, c, rest * z);
         const float t = tanh_of<PRECISE>(c, slope);
@@ -266,8 +296,8 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
     float bf[V], br[V], d_in[V], sum_f[V], sum_r[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bf[v] = b_f ? b_f[p.col + v] : 0.f;
-        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
+        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
         d_in[v] = dc_last ? dc_last[(size_t)p.b * H + p.col + v] : 0.f;
         d_in[v] = scan_fold(d_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, g.segments - 1 - p.seg);
         sum_f[v] = sum_r[v] = 0.f;
@@ -279,88 +309,92 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
         const T *rows = u + row * row_len;
         T *out = du + row * row_len, *out_w = HIGHWAY ? dx + row * H : out + 3 * H;
         const size_t w_len = HIGHWAY ? H : row_len;
-        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
-        scan_load<T, V>(z, rows, row_len, p.col, count);
-        scan_load<T, V>(a, rows + H, row_len, p.col, count);
-        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
-        scan_load<T, V>(w, HIGHWAY ? x + row * H : rows + 3 * H, w_len, p.col, count);
-        scan_load<T, V>(d, dh + row * H, H, p.col, count);
-        float f[SCAN_STEPS][V], rest[SCAN_STEPS][V], e[SCAN_STEPS][V], gap[SCAN_STEPS][V], c[V], A[V], D[V];
+        auto steps = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
+            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
+            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
+            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
+            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
+            scan_load<T, V, FULL>(w, HIGHWAY ? x + row * H : rows + 3 * H, w_len, p.col, count);
+            scan_load<T, V, FULL>(d, dh + row * H, H, p.col, count);
+            float f[SCAN_STEPS][V], rest[SCAN_STEPS][V], e[SCAN_STEPS][V], gap[SCAN_STEPS][V], c[V], A[V], D[V], dc[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            c[v] = count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v] : 0.f;
-            A[v] = 1.f, D[v] = 0.f;
-        }
+            for (int v = 0; v < V; ++v) {
+                c[v] = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v] : 0.f;
+                A[v] = 1.f, D[v] = 0.f;
+            }
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            if (i >= count) {
-                if (t0 + i < p.last && p.on) {
-                    *(raw_t *)(out + i * row_len + p.ch) = 0;
-                    *(raw_t *)(out + i * row_len + H + p.ch) = 0;
-                    *(raw_t *)(out + i * row_len + 2 * H + p.ch) = 0;
-                    *(raw_t *)(out_w + i * w_len + p.ch) = 0;
+            for (int i = 0; i < SCAN_STEPS; ++i) {
+                if (!scan_in<FULL>(i, count)) {
+                    if (t0 + i < p.last && p.on) {
+                        *(raw_t *)(out + i * row_len + p.ch) = 0;
+                        *(raw_t *)(out + i * row_len + H + p.ch) = 0;
+                        *(raw_t *)(out + i * row_len + 2 * H + p.ch) = 0;
+                        *(raw_t *)(out_w + i * w_len + p.ch) = 0;
+                    }
+                    continue;
                 }
-                continue;
-            }
-            float d_r[V], d_w[V];
+                float d_r[V], d_w[V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                ScanStep<PRECISE> s;
-                s.make(c[v], scan_value(z[i], v), scan_value(a[i], v) + bf[v], scan_value(r[i], v) + br[v], scan_value(w[i], v),
-                       scan_value(d[i], v));
-                f[i][v] = s.f, rest[i][v] = s.rest, e[i][v] = s.e, gap[i][v] = s.gap;
-                d_r[v] = s.d_r, d_w[v] = s.d_w;
-                sum_r[v] += s.d_r;
-            }
-            if (p.on) {
-                *(raw_t *)(out + i * row_len + 2 * H + p.ch) = scan_pack<T, V>(d_r);
-                *(raw_t *)(out_w + i * w_len + p.ch) = scan_pack<T, V>(d_w);
-            }
-        }
-#pragma unroll
-        for (int i = SCAN_STEPS - 1; i >= 0; --i) {
-            if (i >= count) continue;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                D[v] = (D[v] + e[i][v]) * f[i][v];
-                A[v] *= f[i][v];
-            }
-        }
-        float dc[V];
-        if (p.waves > 1) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
-            __syncthreads();
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                dc[v] = d_in[v];
-                for (int j = p.waves - 1; j >= 0; --j) {
-                    const float2 q = sums[parity][j][p.lane * V + v];
-                    d_in[v] = fmaf(q.x, d_in[v], q.y);
-                    if (j - 1 == p.wave) dc[v] = d_in[v];
+                for (int v = 0; v < V; ++v) {
+                    ScanStep<PRECISE> s;
+                    s.make(c[v], scan_value(z[i], v), scan_value(a[i], v), bf[v], scan_value(r[i], v), br[v], scan_value(w[i], v),
+                           scan_value(d[i], v));
+                    f[i][v] = s.f, rest[i][v] = s.rest, e[i][v] = s.e, gap[i][v] = s.gap;
+                    d_r[v] = s.d_r, d_w[v] = s.d_w;
+                    sum_r[v] += s.d_r;
+                }
+                if (p.on) {
+                    *(raw_t *)(out + i * row_len + 2 * H + p.ch) = scan_pack<T, V>(d_r);
+                    *(raw_t *)(out_w + i * w_len + p.ch) = scan_pack<T, V>(d_w);
                 }
             }
-        } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) dc[v] = d_in[v], d_in[v] = fmaf(A[v], d_in[v], D[v]);
-        }
+            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+                if (!scan_in<FULL>(i, count)) continue;
 #pragma unroll
-        for (int i = SCAN_STEPS - 1; i >= 0; --i) {
-            if (i >= count) continue;
-            float d_z[V], d_f[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float full = dc[v] + e[i][v];
-                d_z[v] = full * rest[i][v];
-                d_f[v] = full * gap[i][v];
-                sum_f[v] += d_f[v];
-                dc[v] = full * f[i][v];
+                for (int v = 0; v < V; ++v) {
+                    D[v] = (D[v] + e[i][v]) * f[i][v];
+                    A[v] *= f[i][v];
+                }
             }
-            if (p.on) {
-                *(raw_t *)(out + i * row_len + p.ch) = scan_pack<T, V>(d_z);
-                *(raw_t *)(out + i * row_len + H + p.ch) = scan_pack<T, V>(d_f);
+            if (p.waves > 1) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
+                barrier_anywhere();
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    dc[v] = d_in[v];
+                    for (int j = p.waves - 1; j >= 0; --j) {
+                        const float2 q = sums[parity][j][p.lane * V + v];
+                        d_in[v] = fmaf(q.x, d_in[v], q.y);
+                        if (j - 1 == p.wave) dc[v] = d_in[v];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v) dc[v] = d_in[v], d_in[v] = fmaf(A[v], d_in[v], D[v]);
             }
-        }
+#pragma unroll
+            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+                if (!scan_in<FULL>(i, count)) continue;
+                float d_z[V], d_f[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const float full = dc[v] + e[i][v];
+                    d_z[v] = full * rest[i][v];
+                    d_f[v] = full * gap[i][v];
+                    sum_f[v] += d_f[v];
+                    dc[v] = full * f[i][v];
+                }
+                if (p.on) {
+                    *(raw_t *)(out + i * row_len + p.ch) = scan_pack<T, V>(d_z);
+                    *(raw_t *)(out + i * row_len + H + p.ch) = scan_pack<T, V>(d_f);
+                }
+            }
+        };
+        if (count >= SCAN_STEPS) steps(ScanFull());
+        else steps(ScanPart());
     }
     if (dc0 && p.seg == 0 && p.wave == 0 && p.on) {
 #pragma unroll
@@ -403,8 +437,8 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_
     float bf[V], br[V], A[V], D[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        bf[v] = b_f ? b_f[p.col + v] : 0.f;
-        br[v] = b_r ? b_r[p.col + v] : 0.f;
+        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
+        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
         A[v] = 1.f, D[v] = 0.f;
     }
     const int part = g.seg_steps / p.waves, from = p.first + p.wave * part;
@@ -413,33 +447,38 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_
         if (count <= 0) continue;
         const size_t row = (size_t)p.b * g.L + t0;
         const T *rows = u + row * row_len;
-        raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
-        scan_load<T, V>(z, rows, row_len, p.col, count);
-        scan_load<T, V>(a, rows + H, row_len, p.col, count);
-        scan_load<T, V>(r, rows + 2 * H, row_len, p.col, count);
-        scan_load<T, V>(d, dh + row * H, H, p.col, count);
-        float f[SCAN_STEPS][V], e[SCAN_STEPS][V], c[V];
+        auto steps = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
+            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
+            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
+            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
+            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
+            scan_load<T, V, FULL>(d, dh + row * H, H, p.col, count);
+            float f[SCAN_STEPS][V], e[SCAN_STEPS][V], c[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) c[v] = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v];
+            for (int v = 0; v < V; ++v) c[v] = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v];
 #pragma unroll
-        for (int i = 0; i < SCAN_STEPS; ++i) {
-            if (i >= count) continue;
+            for (int i = 0; i < SCAN_STEPS; ++i) {
+                if (!scan_in<FULL>(i, count)) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                ScanStep<PRECISE> s;
-                s.make(c[v], scan_value(z[i], v), scan_value(a[i], v) + bf[v], scan_value(r[i], v) + br[v], 0.f, scan_value(d[i], v));
-                f[i][v] = s.f, e[i][v] = s.e;
+                for (int v = 0; v < V; ++v) {
+                    ScanStep<PRECISE> s;
+                    s.make(c[v], scan_value(z[i], v), scan_value(a[i], v), bf[v], scan_value(r[i], v), br[v], 0.f, scan_value(d[i], v));
+                    f[i][v] = s.f, e[i][v] = s.e;
+                }
             }
-        }
 #pragma unroll
-        for (int i = SCAN_STEPS - 1; i >= 0; --i) {
-            if (i >= count) continue;
+            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+                if (!scan_in<FULL>(i, count)) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                D[v] = (D[v] + e[i][v]) * f[i][v];
-                A[v] *= f[i][v];
+                for (int v = 0; v < V; ++v) {
+                    D[v] = (D[v] + e[i][v]) * f[i][v];
+                    A[v] *= f[i][v];
+                }
             }
-        }
+        };
+        if (count >= SCAN_STEPS) steps(ScanFull());
+        else steps(ScanPart());
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], D[v]);

@@ -4,7 +4,7 @@
 
 namespace moe {
 
-constexpr int SCAN_STEPS = 16;         // steps of a wavefront, and between saved states
+constexpr int SCAN_STEPS = 8;          // steps of a wavefront, and between saved states
 constexpr int SCAN_MAX_WAVES = 8;      // wavefronts of a workgroup, one behind the other on the sequence
 constexpr int SCAN_MAX_SEGMENTS = 64;
 constexpr int SCAN_WORKGROUPS = 512;   // two for each compute unit

@@ -30,26 +30,51 @@ __device__ __forceinline__ scan_raw_t<T, V> scan_pack(const float (&v)[V])
     else return f32_to_bf16(v[0]);
 }
 
+// A run's rows of a tensor as a buffer: the lane's offset in a register, the step's in a scalar one (addresses of 64 bits for every step and
+// tensor spilled scalar registers into vector ones).  An offset from 2^31 on is outside: lanes without a channel ask for nothing and store nothing.
+constexpr unsigned SCAN_NOWHERE = 0x80000000u;
+typedef __amdgpu_buffer_rsrc_t scan_rows_t;
+
+__device__ __forceinline__ scan_rows_t scan_rows(const void *first)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(first), 0, 0x7fffffff, 0x27000);
+}
+template <class R>
+__device__ __forceinline__ R scan_get(scan_rows_t rows, unsigned lane_at, unsigned step_at)
+{
+    if constexpr (sizeof(R) == 2) return __builtin_amdgcn_raw_buffer_load_b16(rows, lane_at, step_at, 0);
+    else return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b32(rows, lane_at, step_at, 0));
+}
+template <class R>
+__device__ __forceinline__ void scan_put(R v, scan_rows_t rows, unsigned lane_at, unsigned step_at)
+{
+    if constexpr (sizeof(R) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, rows, lane_at, step_at, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rows, lane_at, step_at, 0);
+}
+
 // Where a workgroup stands: channels, sequence, segment.  Everything but the channel is the same for a whole wavefront.
 template <class T, int V>
 struct ScanPlace {
     typedef scan_raw_t<T, V> raw_t;
     int b, seg, lane, wave, waves, n, first, last;     // first .. last-1: the segment's steps
     unsigned ch, col;                                  // this lane's first channel; one that exists
+    unsigned at, block;                                // its offset in a row of one block, and a block's length, in bytes
     bool on;
     __device__ __forceinline__ bool find(const ScanShape &g, const int32_t *lengths, int segments)
     {
         const unsigned wg = blockIdx.y * gridDim.x + blockIdx.x;
-        const unsigned groups = g.groups, at = wg / groups;
-        b = at / segments;
-        seg = at - (unsigned)b * segments;
+        const unsigned groups = g.groups, line = wg / groups;
+        b = line / segments;
+        seg = line - (unsigned)b * segments;
         if (b >= g.B) return false;
         lane = threadIdx.x % WAVE;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
         waves = blockDim.x / WAVE;
-        ch = ((wg - at * groups) * WAVE + lane) * V;
+        ch = ((wg - line * groups) * WAVE + lane) * V;
         on = ch < (unsigned)g.H;
         col = on ? ch : 0;
+        at = on ? ch * (unsigned)sizeof(T) : SCAN_NOWHERE;
+        block = g.H * (unsigned)sizeof(T);
         n = lengths ? min(max(lengths[b], 0), g.L) : g.L;
         n = __builtin_amdgcn_readfirstlane(n);
         first = seg * g.seg_steps;
@@ -64,13 +89,13 @@ struct ScanPart { static constexpr bool FULL = false; };
 template <bool FULL> __device__ __forceinline__ bool scan_in(int i, int count) { return FULL || i < count; }
 
 // the steps of one column block, the first count of them
-template <class T, int V, bool FULL>
-__device__ __forceinline__ void scan_load(scan_raw_t<T, V> (&to)[SCAN_STEPS], const T *row0, size_t row_len, unsigned col, int count)
+template <class R, bool FULL>
+__device__ __forceinline__ void scan_load(R (&to)[SCAN_STEPS], scan_rows_t rows, unsigned lane_at, unsigned row_bytes, int count)
 {
 #pragma unroll
     for (int i = 0; i < SCAN_STEPS; ++i) {
         if (!FULL) to[i] = 0;
-        if (scan_in<FULL>(i, count)) to[i] = *(const scan_raw_t<T, V> *)(row0 + i * row_len + col);
+        if (scan_in<FULL>(i, count)) to[i] = scan_get<R>(rows, lane_at, i * row_bytes);
     }
 }
 
@@ -95,6 +120,7 @@ struct ScanForward {
 // the state that a pair list before this place leads to
 __device__ __forceinline__ float scan_fold(float c, const float2 *pairs, size_t step, int count)
 {
+#pragma unroll 16
     for (int j = 0; j < count; ++j) {
         const float2 p = pairs[j * step];
         c = fmaf(p.x, c, p.y);
@@ -129,13 +155,14 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
         const int t0 = t + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);    // this wavefront's steps inside the sequence
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
+            const size_t row = (size_t)p.b * g.L + t0;
+            const scan_rows_t ur = scan_rows(u + row * row_len), xr = HIGHWAY ? scan_rows(x + row * H) : ur, hr = scan_rows(h + row * H);
             raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
-            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
-            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
-            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
-            if (HIGHWAY) scan_load<T, V, FULL>(w, x + ((size_t)p.b * g.L + t0) * H, H, p.col, count);
-            else scan_load<T, V, FULL>(w, rows + 3 * H, row_len, p.col, count);
+            scan_load<raw_t, FULL>(z, ur, p.at, K * p.block, count);
+            scan_load<raw_t, FULL>(a, ur, p.at + p.block, K * p.block, count);
+            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, K * p.block, count);
+            if (HIGHWAY) scan_load<raw_t, FULL>(w, xr, p.at, p.block, count);
+            else scan_load<raw_t, FULL>(w, ur, p.at + 3 * p.block, K * p.block, count);
             ScanForward<PRECISE> s[SCAN_STEPS][V];
             float A[V], C[V], c[V];
 #pragma unroll
@@ -172,11 +199,10 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
 #pragma unroll
                 for (int v = 0; v < V; ++v) states[at + v] = c[v];
             }
-            T *hr = h + ((size_t)p.b * g.L + t0) * H;
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) {
-                    if (t0 + i < p.last && p.on) *(raw_t *)(hr + i * H + p.ch) = 0;
+                    if (t0 + i < p.last) scan_put<raw_t>(0, hr, p.at, i * p.block);
                     continue;
                 }
                 float out[V];
@@ -192,7 +218,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
                         out[v] = fmaf(gate_open<false>(scan_value(r[i], v), br[v]), t - wv, wv);
                     }
                 }
-                if (p.on) *(raw_t *)(hr + i * H + p.ch) = scan_pack<T, V>(out);
+                scan_put<raw_t>(scan_pack<T, V>(out), hr, p.at, i * p.block);
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
@@ -224,12 +250,13 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(Sc
     const int part = g.seg_steps / p.waves, from = p.first + p.wave * part, to = from + part;     // whole runs: seg_steps is whole rounds
     for (int t0 = from; t0 < to; t0 += SCAN_STEPS) {
         const int count = min(p.n - t0, SCAN_STEPS);
-        const T *rows = u + ((size_t)p.b * g.L + t0) * row_len;
+        const scan_rows_t ur = scan_rows(u + ((size_t)p.b * g.L + t0) * row_len);
+        const unsigned row_bytes = blocks * p.block;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
             raw_t z[SCAN_STEPS], a[SCAN_STEPS];
-            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
-            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
+            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
@@ -306,17 +333,17 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
     for (int at = rounds - 1, parity = 0; at >= 0; --at, parity ^= 1) {
         const int t0 = p.first + at * round + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);
         const size_t row = (size_t)p.b * g.L + t0;
-        const T *rows = u + row * row_len;
-        T *out = du + row * row_len, *out_w = HIGHWAY ? dx + row * H : out + 3 * H;
-        const size_t w_len = HIGHWAY ? H : row_len;
+        const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H), out = scan_rows(du + row * row_len);
+        const scan_rows_t xr = HIGHWAY ? scan_rows(x + row * H) : ur, out_w = HIGHWAY ? scan_rows(dx + row * H) : out;
+        const unsigned at_w = HIGHWAY ? p.at : p.at + 3 * p.block, row_bytes = K * p.block, w_bytes = HIGHWAY ? p.block : row_bytes;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
             raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
-            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
-            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
-            scan_load<T, V, FULL>(w, HIGHWAY ? x + row * H : rows + 3 * H, w_len, p.col, count);
-            scan_load<T, V, FULL>(d, dh + row * H, H, p.col, count);
+            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
+            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
+            scan_load<raw_t, FULL>(w, xr, at_w, w_bytes, count);
+            scan_load<raw_t, FULL>(d, dr, p.at, p.block, count);
             float f[SCAN_STEPS][V], rest[SCAN_STEPS][V], e[SCAN_STEPS][V], gap[SCAN_STEPS][V], c[V], A[V], D[V], dc[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -326,11 +353,9 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) {
-                    if (t0 + i < p.last && p.on) {
-                        *(raw_t *)(out + i * row_len + p.ch) = 0;
-                        *(raw_t *)(out + i * row_len + H + p.ch) = 0;
-                        *(raw_t *)(out + i * row_len + 2 * H + p.ch) = 0;
-                        *(raw_t *)(out_w + i * w_len + p.ch) = 0;
+                    if (t0 + i < p.last) {
+                        for (int k = 0; k < 3; ++k) scan_put<raw_t>(0, out, p.at + k * p.block, i * row_bytes);
+                        scan_put<raw_t>(0, out_w, at_w, i * w_bytes);
                     }
                     continue;
                 }
@@ -344,10 +369,8 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
                     d_r[v] = s.d_r, d_w[v] = s.d_w;
                     sum_r[v] += s.d_r;
                 }
-                if (p.on) {
-                    *(raw_t *)(out + i * row_len + 2 * H + p.ch) = scan_pack<T, V>(d_r);
-                    *(raw_t *)(out_w + i * w_len + p.ch) = scan_pack<T, V>(d_w);
-                }
+                scan_put<raw_t>(scan_pack<T, V>(d_r), out, p.at + 2 * p.block, i * row_bytes);
+                scan_put<raw_t>(scan_pack<T, V>(d_w), out_w, at_w, i * w_bytes);
             }
 #pragma unroll
             for (int i = SCAN_STEPS - 1; i >= 0; --i) {
@@ -387,10 +410,8 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
                     sum_f[v] += d_f[v];
                     dc[v] = full * f[i][v];
                 }
-                if (p.on) {
-                    *(raw_t *)(out + i * row_len + p.ch) = scan_pack<T, V>(d_z);
-                    *(raw_t *)(out + i * row_len + H + p.ch) = scan_pack<T, V>(d_f);
-                }
+                scan_put<raw_t>(scan_pack<T, V>(d_z), out, p.at, i * row_bytes);
+                scan_put<raw_t>(scan_pack<T, V>(d_f), out, p.at + p.block, i * row_bytes);
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
@@ -446,14 +467,15 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_
         const int count = min(p.n - t0, SCAN_STEPS);
         if (count <= 0) continue;
         const size_t row = (size_t)p.b * g.L + t0;
-        const T *rows = u + row * row_len;
+        const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H);
+        const unsigned row_bytes = blocks * p.block;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
             raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<T, V, FULL>(z, rows, row_len, p.col, count);
-            scan_load<T, V, FULL>(a, rows + H, row_len, p.col, count);
-            scan_load<T, V, FULL>(r, rows + 2 * H, row_len, p.col, count);
-            scan_load<T, V, FULL>(d, dh + row * H, H, p.col, count);
+            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
+            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
+            scan_load<raw_t, FULL>(d, dr, p.at, p.block, count);
             float f[SCAN_STEPS][V], e[SCAN_STEPS][V], c[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) c[v] = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v];

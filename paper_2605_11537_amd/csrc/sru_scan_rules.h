@@ -19,10 +19,10 @@ struct ScanShape {
 // channels of a lane
 static inline int scan_width(int H, int dtype) { return dtype == MOE_BF16 && H % 2 == 0 ? 2 : 1; }
 
-// sizes whose counts of workgroups and parts fit an int
+// sizes whose counts of workgroups and parts fit an int, and whose runs of SCAN_STEPS rows of four blocks lie within 2^31 bytes
 static inline bool scan_takes(int B, int L, int H)
 {
-    return H <= (1 << 24) && L <= (1 << 30) && (long long)B * ((H + WAVE - 1) / WAVE) < (1 << 26);
+    return H <= (1 << 23) && L <= (1 << 30) && (long long)B * ((H + WAVE - 1) / WAVE) < (1 << 26);
 }
 
 static inline ScanShape scan_shape(int B, int L, int H, int dtype)

@@ -386,7 +386,7 @@ int sru_scan_backward(const void *dh, const float *dc_last, const void *u, const
  *     among equals, and their log probabilities (0 <= k <= min(MOE_MAX_TOPK, V); NULL with k = 0)
  * Logits of -infinity are masked: probability 0, nothing to the entropy.  Where all are, log probabilities and lse are
  * -infinity and the entropy is 0.  A NaN or +infinity makes the row's numbers NaN; among the alternatives a NaN counts as
- * masked.  Sums in binary32, in a fixed order.
+ * masked.  Sums in binary32, in an order that the shape fixes.  V <= 2^21, N <= 2^22.
  * moe_token_logprobs_backward -- dL/dlogits (dtype) from dlogprob [N] and dentropy [N] (NULL: 0), with the lse and
  * entropy that the forward wrote (entropy may be NULL without dentropy):
  *     dlogits_i = g ([i = target] - p_i) - dentropy p_i (log p_i + entropy),   g = dlogprob, 0 for a padded position

@@ -7,7 +7,7 @@ namespace moe {
 constexpr int SCAN_STEPS = 8;          // steps of a wavefront, and between saved states
 constexpr int SCAN_MAX_WAVES = 8;      // wavefronts of a workgroup, one behind the other on the sequence
 constexpr int SCAN_MAX_SEGMENTS = 64;
-constexpr int SCAN_WORKGROUPS = 512;   // two for each compute unit
+constexpr int SCAN_WORKGROUPS = 256;   // one for each compute unit
 
 struct ScanShape {
     int B, L, H;

@@ -1,110 +1,463 @@
 // moe_token_logprobs and its gradient: log probabilities of given ids, entropy and the best alternatives of rows of logits.
+//
+// With m the largest logit, d = x - m, s = sum e^d and t = sum d e^d: lse = m + log s, log p_i = d_i - log s, entropy = log s - t / s.  Parts
+// of a row join by bringing (m, s, t) to the larger maximum: s e^(m - M), (t + (m - M) s) e^(m - M).
+// A row is read once, into registers.  The sums are found while it arrives.  The alternatives then cost next to nothing: a bound that k logits
+// reach for certain (the k-th largest of the maxima of sixteen groups of threads), the few logits that reach it collected, and each ranked
+// among them.  Rows where more than LP_LIST reach it (equal logits) or fewer than k lie above minus infinity take k searches of the registers.
 #include <float.h>
 
 #include "scalar_math.h"
+#include "token_logprobs_rules.h"
 
 namespace moe {
 
-constexpr int LP_THREADS = 256;
-constexpr int LP_WAVES = LP_THREADS / WAVE;
+constexpr int LP_THREADS = 256;        // of a workgroup over short rows, and of the gradient's
+constexpr int LP_GROUPS = 16;
+constexpr int LP_LIST = 64;
+typedef unsigned lp_u32x4_t __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ float lp_max(float v, float *scratch)
-{
-#pragma unroll
-    for (int o = 1; o < WAVE; o <<= 1) v = fmaxf(v, __shfl_xor(v, o, WAVE));
-    if (threadIdx.x % WAVE == 0) scratch[threadIdx.x / WAVE] = v;
-    __syncthreads();
-    for (int i = 0; i < LP_WAVES; ++i) v = fmaxf(v, scratch[i]);
-    __syncthreads();
-    return v;
-}
-__device__ __forceinline__ float lp_sum(float v, float *scratch)
-{
-    v = sum_over<WAVE>(v);
-    if (threadIdx.x % WAVE == 0) scratch[threadIdx.x / WAVE] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int i = 0; i < LP_WAVES; ++i) v += scratch[i];
-    __syncthreads();
-    return v;
-}
+template <class X> struct LogitPiece;
+template <> struct LogitPiece<float> {
+    static constexpr int N = 4;
+    static constexpr unsigned MASKED = 0xff800000u;        // minus infinity
+    static __device__ __forceinline__ float get(const lp_u32x4_t &p, int q) { return __uint_as_float(p[q]); }
+};
+template <> struct LogitPiece<bf16_t> {
+    static constexpr int N = 8;
+    static constexpr unsigned MASKED = 0xff80ff80u;
+    static __device__ __forceinline__ float get(const lp_u32x4_t &p, int q)
+    {
+        return __uint_as_float(q & 1 ? p[q >> 1] & 0xffff0000u : p[q >> 1] << 16);
+    }
+};
 
-// one workgroup per row: the maximum, the sums, then the alternatives one by one
-template <class X>
-__global__ __launch_bounds__(LP_THREADS) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride, const int32_t *__restrict__ target,
-                                                                    int V, int k, float *__restrict__ logprob, float *__restrict__ entropy,
-                                                                    float *__restrict__ lse, int32_t *__restrict__ top_idx,
-                                                                    float *__restrict__ top_logprob)
-{
-    __shared__ float scratch[LP_WAVES];
-    __shared__ int scratch_id[LP_WAVES];
-    const size_t n = blockIdx.x;
-    const X *row = logits + n * stride;
-    float m = -FLT_MAX;                                  // finite where everything is masked: the sum is then zero
-    for (int i = threadIdx.x; i < V; i += LP_THREADS) m = fmaxf(m, value_of(row[i]));
-    m = lp_max(m, scratch);
-    float s = 0.f, t = 0.f;
-    for (int i = threadIdx.x; i < V; i += LP_THREADS) {
-        const float d = value_of(row[i]) - m, e = exp_of<true>(d);
+// A logit as the alternatives see it: no number counts as masked.
+__device__ __forceinline__ float lp_ranked(float x) { return x == x ? x : -INFINITY; }
+
+// Running maximum and sums.  The maximum is never below the lowest finite value, so a row that is masked throughout has s = 0 and no
+// infinity is taken from another; a NaN passes into s.
+struct LogitSums {
+    float m, s, t;
+    __device__ __forceinline__ void clear() { m = -FLT_MAX, s = t = 0.f; }
+    __device__ __forceinline__ void raise(float to)
+    {
+        if (to > m) {
+            const float d = fmaxf(m - to, -1e4f), e = exp_of<true>(d);     // from the lowest value on: e = 0, and no infinity times it
+            t = (t + d * s) * e;
+            s *= e;
+            m = to;
+        }
+    }
+    // a value not above m: d is kept off minus infinity, which times zero would be no number
+    __device__ __forceinline__ void add(float x)
+    {
+        const float d = x - m, e = __builtin_amdgcn_exp2f(d * LOG2E);
         s += e;
-        if (e != 0.f) t = fmaf(d, e, t);                 // a masked logit: zero, not zero times infinity
+        t = fmaf(fmaxf(d, -1e4f), e, t);
     }
-    s = lp_sum(s, scratch);
-    t = lp_sum(t, scratch);
-    const bool none = s == 0.f;
-    const float log_s = logf(s);
-    if (threadIdx.x == 0) {
-        const int a = target[n];
-        logprob[n] = a < 0 || a >= V ? 0.f : none ? -INFINITY : value_of(row[a]) - m - log_s;
-        entropy[n] = none ? 0.f : log_s - t / s;
-        lse[n] = none ? -INFINITY : m + log_s;
+    __device__ __forceinline__ void join(LogitSums o)
+    {
+        raise(o.m);
+        o.raise(m);
+        s += o.s;
+        t += o.t;
     }
+    template <int STEP>
+    __device__ __forceinline__ LogitSums partner() const
+    {
+        return {group_exchange<STEP>(m), group_exchange<STEP>(s), group_exchange<STEP>(t)};
+    }
+};
+template <int LANES, int STEP = 0>
+__device__ __forceinline__ void lp_join_lanes(LogitSums &a)
+{
+    if constexpr ((1 << STEP) < LANES) {
+        a.join(a.partner<STEP>());
+        lp_join_lanes<LANES, STEP + 1>(a);
+    }
+}
+template <int LANES, int STEP = 0>
+__device__ __forceinline__ float lp_max_lanes(float v)
+{
+    if constexpr ((1 << STEP) < LANES) return lp_max_lanes<LANES, STEP + 1>(fmaxf(v, group_exchange<STEP>(v)));
+    else return v;
+}
+template <int LANES, int STEP = 0>
+__device__ __forceinline__ int lp_min_lanes(int v)
+{
+    if constexpr ((1 << STEP) < LANES) return lp_min_lanes<LANES, STEP + 1>(min(v, group_exchange<STEP>(v)));
+    else return v;
+}
+
+struct LogprobOut {
+    float *logprob, *entropy, *lse;
+    int32_t *top_idx;
+    float *top_logprob;
+};
+
+// what a row's sums give; xt: the target's logit
+__device__ __forceinline__ void lp_finish(const LogitSums &a, float log_s, size_t n, int target, int V, float xt, const LogprobOut &o)
+{
+    const bool none = a.s == 0.f;
+    o.logprob[n] = target < 0 || target >= V ? 0.f : none ? -INFINITY : xt - a.m - log_s;
+    o.entropy[n] = none ? 0.f : log_s - a.t / a.s;
+    o.lse[n] = none ? -INFINITY : a.m + log_s;
+}
+__device__ __forceinline__ float lp_of(float x, const LogitSums &a, float log_s) { return a.s == 0.f ? -INFINITY : x - a.m - log_s; }
+
+// Short rows: LANES lanes each, LP_SMALL logits a lane in registers.  PIECES: rows begin on 16 bytes.
+template <class X, int LANES, bool PIECES>
+__global__ __launch_bounds__(LP_THREADS) void token_logprobs_short_kernel(const X *__restrict__ logits, size_t stride,
+                                                                          const int32_t *__restrict__ target, int N, int V, int k, LogprobOut out)
+{
+    typedef LogitPiece<X> piece;
+    constexpr int P = PIECES ? piece::N : 1;             // consecutive logits of a lane
+    const unsigned n = blockIdx.x * (LP_THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    if (n >= (unsigned)N) return;
+    const X *row = logits + n * stride;
+    // behind the row: NaN, which no maximum takes and no comparison meets
+    float v[LP_SMALL];
+#pragma unroll
+    for (int i = 0; i < LP_SMALL; i += P) {
+        const int at = i * LANES + lane * P;
+        if (PIECES) {
+            lp_u32x4_t p;
+            if (at + P <= V) p = *(const lp_u32x4_t *)(row + at);
+#pragma unroll
+            for (int q = 0; q < P; ++q) v[i + q] = at + P <= V ? piece::get(p, q) : NAN;
+            if (at < V && at + P > V) {
+#pragma unroll
+                for (int q = 0; q < P; ++q) v[i + q] = at + q < V ? value_of(row[at + q]) : NAN;
+            }
+        } else {
+            v[i] = at < V ? value_of(row[at]) : NAN;
+        }
+    }
+    const auto place = [&](int i) { return i / P * P * LANES + lane * P + i % P; };
+    LogitSums a;
+    a.clear();
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < LP_SMALL; ++i) top = fmaxf(top, v[i]);
+    top = lp_max_lanes<LANES>(top);
+    a.m = fmaxf(a.m, top);
+#pragma unroll
+    for (int i = 0; i < LP_SMALL; ++i)
+        if (place(i) < V) a.add(v[i]);
+    a.s = sum_over<LANES>(a.s);
+    a.t = sum_over<LANES>(a.t);
+    const float log_s = logf(a.s);
+    if (lane == 0) {
+        const int id = target[n];
+        lp_finish(a, log_s, n, id, V, id >= 0 && id < V ? value_of(row[id]) : 0.f, out);
+    }
+    if (k == 0) return;
+#pragma unroll
+    for (int i = 0; i < LP_SMALL; ++i)
+        if (place(i) < V) v[i] = lp_ranked(v[i]);
+    for (int j = 0; j < k; ++j) {
+        if (j > 0) {
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < LP_SMALL; ++i) top = fmaxf(top, v[i]);
+            top = lp_max_lanes<LANES>(top);
+        }
+        int id = INT32_MAX;
+#pragma unroll
+        for (int i = LP_SMALL - 1; i >= 0; --i) id = v[i] == top ? place(i) : id;
+        id = lp_min_lanes<LANES>(id);
+#pragma unroll
+        for (int i = 0; i < LP_SMALL; ++i) v[i] = place(i) == id ? NAN : v[i];     // taken
+        if (lane == 0) {
+            out.top_idx[(size_t)n * k + j] = id;
+            out.top_logprob[(size_t)n * k + j] = lp_of(top, a, log_s);
+        }
+    }
+}
+
+// The best k of (value, id) entries of LDS, each ranked by those before it: entry of rank r to put(r, value, id).
+template <class F>
+__device__ __forceinline__ void lp_rank(const float *value, const int *id, int count, int k, F put)
+{
+    const int at = threadIdx.x;
+    if (at >= count) return;
+    const float v = value[at];
+    const int i = id[at];
+    int rank = 0;
+    for (int j = 0; j < count; ++j) {
+        const float ov = value[j];
+        rank += ov > v || (ov == v && id[j] < i) ? 1 : 0;
+    }
+    if (rank < k) put(rank, v, i);
+}
+
+// Long rows: a workgroup takes a part of a row, LP_VECS pieces a thread in registers.  WHOLE: the part is the row; else its numbers go to
+// a record of LP_RECORD floats.
+template <class X, bool WHOLE>
+__global__ __launch_bounds__(LP_MAX_THREADS) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,
+                                                                        const int32_t *__restrict__ target, int V, int parts, int part, int k,
+                                                                        float *__restrict__ records, LogprobOut out)
+{
+    typedef LogitPiece<X> piece;
+    constexpr int P = piece::N;
+    __shared__ float wave_m[LP_MAX_THREADS / WAVE], wave_s[LP_MAX_THREADS / WAVE], wave_t[LP_MAX_THREADS / WAVE];
+    __shared__ float groups[LP_GROUPS], list_v[LP_LIST];
+    __shared__ int list_id[LP_LIST], listed;
+    const unsigned n = WHOLE ? blockIdx.x : blockIdx.x / parts, which = WHOLE ? 0 : blockIdx.x - n * parts;
+    const int lo = which * part, len = min(part, V - lo), tid = threadIdx.x, lane = tid % WAVE;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+    const int threads = blockDim.x, waves = threads / WAVE;
+    const X *row = logits + n * stride + lo;
+    // pieces of 16 bytes from the first address that is one; what lies before and behind them is one logit a thread
+    const int head = min(len, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(X)), pieces = (len - head) / P;
+    const int behind = head + pieces * P, ends = len - pieces * P;
+    const int end_at = tid < head ? tid : behind + (tid - head);       // this thread's single logit, for tid < ends
+    const lp_u32x4_t *body = (const lp_u32x4_t *)(row + head);
+    lp_u32x4_t held[LP_VECS];
+    X single = 0;
+    if (tid < ends) single = row[end_at];
+#pragma unroll
+    for (int i = 0; i < LP_VECS; ++i) {                   // masked behind the last piece
+        held[i] = {piece::MASKED, piece::MASKED, piece::MASKED, piece::MASKED};
+        if (i * threads + tid < pieces) held[i] = __builtin_nontemporal_load(body + i * threads + tid);
+    }
+    if (tid == 0) listed = 0;
+    LogitSums a;
+    a.clear();
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < LP_VECS; ++i) {
+        if (i * threads + wave * WAVE >= pieces) break;  // the whole wavefront
+        float most = piece::get(held[i], 0);
+#pragma unroll
+        for (int q = 1; q < P; ++q) most = fmaxf(most, piece::get(held[i], q));
+        top = fmaxf(top, most);
+        a.raise(most);
+#pragma unroll
+        for (int q = 0; q < P; ++q) a.add(piece::get(held[i], q));
+    }
+    const float end_v = tid < ends ? value_of(single) : -INFINITY;
+    if (tid < ends) {
+        top = fmaxf(top, end_v);
+        a.raise(end_v);
+        a.add(end_v);
+    }
+    // the groups of threads that the bound is taken from: threads / LP_GROUPS neighbours
+    {
+        float v = top;
+        const int size = threads / LP_GROUPS;
+        v = lp_max_lanes<4>(v);
+        if (size >= 8) v = fmaxf(v, group_exchange<2>(v));
+        if (size >= 16) v = fmaxf(v, group_exchange<3>(v));
+        if (size >= 32) v = fmaxf(v, group_exchange<4>(v));
+        if (size >= 64) v = fmaxf(v, group_exchange<5>(v));
+        if (tid % size == 0) groups[tid / size] = v;
+    }
+    lp_join_lanes<WAVE>(a);
+    if (lane == 0) wave_m[wave] = a.m, wave_s[wave] = a.s, wave_t[wave] = a.t;
+    __syncthreads();
+    a.m = wave_m[0], a.s = wave_s[0], a.t = wave_t[0];
+    for (int w = 1; w < waves; ++w) a.join({wave_m[w], wave_s[w], wave_t[w]});
+    const float log_s = logf(a.s);
+    float *record = WHOLE ? nullptr : records + ((size_t)n * parts + which) * LP_RECORD;
+    if (tid == 0) {
+        const int id = target[n];
+        if (WHOLE) {
+            lp_finish(a, log_s, n, id, V, id >= 0 && id < V ? value_of(row[id]) : 0.f, out);
+        } else {
+            record[0] = a.m, record[1] = a.s, record[2] = a.t;
+            record[3] = id >= lo && id < lo + len ? value_of(row[id - lo]) : 0.f;
+        }
+    }
+    if (k == 0) return;
+    const auto put = [&](int rank, float v, int id) {
+        if (WHOLE) {
+            out.top_idx[(size_t)n * k + rank] = id;
+            out.top_logprob[(size_t)n * k + rank] = lp_of(v, a, log_s);
+        } else {
+            record[4 + rank] = v;
+            record[4 + MOE_MAX_TOPK + rank] = __int_as_float(id + lo);
+        }
+    };
+    // the bound: the k-th largest of the groups' maxima
+    float bound = -INFINITY;
+    {
+        const float v = groups[lane % LP_GROUPS];
+        int rank = 0;
+        for (int j = 0; j < LP_GROUPS; ++j) {
+            const float o = groups[j];
+            rank += o > v || (o == v && j < lane % LP_GROUPS) ? 1 : 0;
+        }
+        const unsigned long long mine = __ballot(rank == k - 1);
+        bound = __shfl(v, __ffsll(mine) - 1, WAVE);
+    }
+    int count = LP_LIST + 1;
+    if (bound > -INFINITY) {
+        if (top >= bound) {
+            const auto offer = [&](float v, int id) {
+                if (v >= bound) {
+                    const int at = atomicAdd(&listed, 1);
+                    if (at < LP_LIST) list_v[at] = v, list_id[at] = id;
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < LP_VECS; ++i) {
+                if (i * threads + wave * WAVE >= pieces) break;
+                asm("" : "+v"(held[i]));               // unpacked again: the logits themselves would fill the registers
+#pragma unroll
+                for (int q = 0; q < P; ++q) offer(piece::get(held[i], q), head + (i * threads + tid) * P + q);
+            }
+            if (tid < ends) offer(end_v, end_at);
+        }
+        __syncthreads();
+        count = listed;
+    }
+    if (count <= LP_LIST) {
+        lp_rank(list_v, list_id, count, k, put);
+        return;
+    }
+    // one by one: the largest behind the one before, smaller or equal with a higher id
     float after = INFINITY;
     int after_id = -1;
-    for (int j = 0; j < k; ++j) {                        // the largest behind the one before: smaller, or equal with a higher id
+    for (int j = 0; j < min(k, len); ++j) {
         float best = -INFINITY;
-        int id = V;
-        for (int i = threadIdx.x; i < V; i += LP_THREADS) {
-            float v = value_of(row[i]);
-            if (v != v) v = -INFINITY;
-            if ((v < after || (v == after && i > after_id)) && (v > best || id == V)) best = v, id = i;
-        }
+        int id = INT32_MAX;
+        const auto offer = [&](float x, int at) {
+            const float v = lp_ranked(x);
+            if ((v < after || (v == after && at > after_id)) && (v > best || (v == best && at < id))) best = v, id = at;
+        };
+        if (tid < ends) offer(end_v, end_at);
 #pragma unroll
-        for (int o = 1; o < WAVE; o <<= 1) {
-            const float ov = __shfl_xor(best, o, WAVE);
-            const int oi = __shfl_xor(id, o, WAVE);
-            argmax_merge(best, id, ov, oi);
+        for (int i = 0; i < LP_VECS; ++i) {
+            asm("" : "+v"(held[i]));
+            if (i * threads + tid >= pieces) continue;
+#pragma unroll
+            for (int q = 0; q < P; ++q) offer(piece::get(held[i], q), head + (i * threads + tid) * P + q);
         }
-        if (threadIdx.x % WAVE == 0) scratch[threadIdx.x / WAVE] = best, scratch_id[threadIdx.x / WAVE] = id;
+        argmax_over<WAVE>(best, id);
+        __syncthreads();                               // the round before has been read
+        if (lane == 0) list_v[wave] = best, list_id[wave] = id;
         __syncthreads();
-        for (int i = 0; i < LP_WAVES; ++i) argmax_merge(best, id, scratch[i], scratch_id[i]);
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            top_idx[n * k + j] = id;
-            top_logprob[n * k + j] = none ? -INFINITY : best - m - log_s;
-        }
+        best = list_v[0], id = list_id[0];
+        for (int w = 1; w < waves; ++w) argmax_merge(best, id, list_v[w], list_id[w]);
+        if (tid == 0) put(j, best, id);
         after = best;
         after_id = id;
     }
+    if (!WHOLE && tid == 0)
+        for (int j = len; j < k; ++j) record[4 + j] = -INFINITY, record[4 + MOE_MAX_TOPK + j] = __int_as_float(INT32_MAX);
 }
 
+// the parts of a row, one lane each; a lane's best entries are in order, so only the first that is left can be the next
+__global__ __launch_bounds__(WAVE) void token_logprobs_join_kernel(const float *__restrict__ records, const int32_t *__restrict__ target, int V,
+                                                                   int parts, int part, int k, LogprobOut out)
+{
+    const size_t n = blockIdx.x;
+    const int lane = threadIdx.x;
+    const float *record = records + (n * parts + min(lane, parts - 1)) * LP_RECORD;
+    LogitSums a;
+    a.clear();
+    if (lane < parts) a = {record[0], record[1], record[2]};
+    float best[MOE_MAX_TOPK];
+    int ids[MOE_MAX_TOPK];
+#pragma unroll
+    for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+        best[j] = j < k && lane < parts ? record[4 + j] : -INFINITY;
+        ids[j] = j < k && lane < parts ? __float_as_int(record[4 + MOE_MAX_TOPK + j]) : INT32_MAX;
+    }
+    const int id = target[n];
+    const float xt = id >= 0 && id < V ? records[(n * parts + id / part) * LP_RECORD + 3] : 0.f;
+    lp_join_lanes<WAVE>(a);
+    const float log_s = logf(a.s);
+    if (lane == 0) lp_finish(a, log_s, n, id, V, xt, out);
+    for (int j = 0; j < k; ++j) {
+        float v = best[0];
+        int i = ids[0];
+        argmax_over<WAVE>(v, i);
+        if (i == ids[0]) {
+#pragma unroll
+            for (int q = 0; q + 1 < MOE_MAX_TOPK; ++q) best[q] = best[q + 1], ids[q] = ids[q + 1];
+            best[MOE_MAX_TOPK - 1] = -INFINITY, ids[MOE_MAX_TOPK - 1] = INT32_MAX;
+        }
+        if (lane == 0) {
+            out.top_idx[n * k + j] = i;
+            out.top_logprob[n * k + j] = lp_of(v, a, log_s);
+        }
+    }
+}
+
+// The gradient, elementwise: -p (g + q (log p + H)), and g more at the target.
+template <class X>
+struct LogprobSlope {
+    static constexpr bool PRECISE = sizeof(X) == 4;
+    float lse, base, q, g;
+    int target;
+    bool none;
+    __device__ __forceinline__ float at(float x, int i) const
+    {
+        const float lp = x - lse, p = exp_of<PRECISE>(lp);
+        float d = p * fmaf(-q, lp, base);
+        d = p == 0.f || none ? 0.f : d;                  // a masked logit: log p is no number to multiply with
+        return i == target && !none ? d + g : d;
+    }
+};
+
+constexpr int LP_SLOPE_PIECES = 4;     // pieces of a thread
+
+// 2^lg threads share a row; blockIdx.y: its run of 2^lg * LP_SLOPE_PIECES pieces
 template <class X>
 __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(const X *logits, size_t stride, const int32_t *__restrict__ target,
                                                                              const float *__restrict__ lse, const float *__restrict__ entropy,
                                                                              const float *__restrict__ dlogprob, const float *__restrict__ dentropy,
-                                                                             int V, X *dlogits, size_t dstride)
+                                                                             int N, int V, int lg, X *dlogits, size_t dstride)
 {
-    const size_t n = blockIdx.x;
-    const int a = target[n];
-    const float g = a < 0 || a >= V ? 0.f : dlogprob[n], q = dentropy ? dentropy[n] : 0.f, z = lse[n], H = dentropy ? entropy[n] : 0.f;
-    for (int i = threadIdx.x; i < V; i += LP_THREADS) {
-        const float lp = value_of(logits[n * stride + i]) - z, p = exp_of<true>(lp);
-        float d = 0.f;
-        if (z != -INFINITY) {                            // nothing was left of the row
-            d = p == 0.f ? 0.f : -p * fmaf(q, lp + H, g);
-            if (i == a) d += g;
+    typedef LogitPiece<X> piece;
+    constexpr int P = piece::N;
+    const unsigned n = blockIdx.x * (LP_THREADS >> lg) + (threadIdx.x >> lg);
+    const int lanes = 1 << lg, lane = threadIdx.x & (lanes - 1);
+    if (n >= (unsigned)N) return;
+    const X *row = logits + n * stride;
+    X *out = dlogits + n * dstride;
+    LogprobSlope<X> f;
+    f.target = target[n];
+    f.lse = lse[n];
+    f.none = f.lse == -INFINITY;
+    f.g = f.target < 0 || f.target >= V ? 0.f : dlogprob[n];
+    f.q = dentropy ? dentropy[n] : 0.f;
+    f.base = -f.g - (dentropy ? f.q * entropy[n] : 0.f);
+    const int run = lanes * LP_SLOPE_PIECES;
+    if ((((uintptr_t)row ^ (uintptr_t)out) & 15) == 0) {
+        const int head = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(X)), pieces = (V - head) / P;
+        const lp_u32x4_t *body = (const lp_u32x4_t *)(row + head);
+        lp_u32x4_t *to = (lp_u32x4_t *)(out + head), held[LP_SLOPE_PIECES];
+        const int first = blockIdx.y * run + lane;
+#pragma unroll
+        for (int i = 0; i < LP_SLOPE_PIECES; ++i)
+            if (first + i * lanes < pieces) held[i] = body[first + i * lanes];
+#pragma unroll
+        for (int i = 0; i < LP_SLOPE_PIECES; ++i) {
+            const int at = first + i * lanes;
+            if (at >= pieces) continue;
+            lp_u32x4_t r;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int c = head + at * P + w * (P / 4);
+                if constexpr (P == 4) r[w] = __float_as_uint(f.at(piece::get(held[i], w), c));
+                else r[w] = pack_bf16x2(f.at(piece::get(held[i], 2 * w), c), f.at(piece::get(held[i], 2 * w + 1), c + 1));
+            }
+            to[at] = r;
         }
-        store_value(dlogits + n * dstride + i, d);
+        if (blockIdx.y == 0) {
+            const int ends = V - pieces * P;
+            for (int e = lane; e < ends; e += lanes) {
+                const int c = e < head ? e : pieces * P + e;
+                store_value(out + c, f.at(value_of(row[c]), c));
+            }
+        }
+    } else {                                             // rows that lie differently inside 16 bytes
+        const int last = min(V, (int)(blockIdx.y + 1) * run * P + (blockIdx.y + 1 == gridDim.y ? 2 * P : 0));
+        for (int c = blockIdx.y * run * P + lane; c < last; c += lanes) store_value(out + c, f.at(value_of(row[c]), c));
     }
 }
 
@@ -113,6 +466,8 @@ static int logprobs_check(const char *who, int N, int V, long long stride, int d
     MOE_REQUIRE(N >= 0 && V > 0, MOE_ERR_INVALID_ARG, "%s: N=%d V=%d out of range", who, N, V);
     MOE_REQUIRE(stride >= V, MOE_ERR_INVALID_ARG, "%s: rows of %d logits lie %lld apart", who, V, stride);
     MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+    MOE_REQUIRE(V <= LP_MAX_V, MOE_ERR_UNSUPPORTED, "%s: V=%d > %d", who, V, LP_MAX_V);
+    MOE_REQUIRE(N <= LP_MAX_N, MOE_ERR_UNSUPPORTED, "%s: N=%d > %d", who, N, LP_MAX_N);
     return MOE_OK;
 }
 
@@ -122,8 +477,33 @@ using namespace moe;
 
 extern "C" size_t moe_token_logprobs_workspace_bytes(int N, int V, int k, int dtype)
 {
-    (void)N, (void)V, (void)k, (void)dtype;
-    return 0;
+    (void)k;
+    if (N <= 0 || V <= 0 || V > LP_MAX_V || N > LP_MAX_N) return 0;
+    const LogprobShape g = logprob_shape(N, V, dtype);
+    return g.parts > 1 ? (size_t)N * g.parts * LP_RECORD * sizeof(float) : 0;
+}
+
+template <class X>
+static void logprobs_launch(const LogprobShape &g, const X *logits, size_t stride, const int32_t *target, int N, int V, int k, float *records,
+                            const LogprobOut &out, hipStream_t st)
+{
+    if (g.lanes) {
+        const bool pieces = ((uintptr_t)logits & 15) == 0 && stride * sizeof(X) % 16 == 0;
+        const dim3 grid(ceil_div(N, LP_THREADS / g.lanes)), threads(LP_THREADS);
+#define MOE_SHORT(L)                                                                                                                          do {                                                                                                                                          if (pieces) hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, true>), grid, threads, 0, st, logits, stride, target, N, V, k, out);         else hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, false>), grid, threads, 0, st, logits, stride, target, N, V, k, out);       } while (0)
+        if (g.lanes == 4) MOE_SHORT(4);
+        else if (g.lanes == 16) MOE_SHORT(16);
+        else MOE_SHORT(64);
+#undef MOE_SHORT
+        return;
+    }
+    const dim3 grid((unsigned)N * g.parts), threads(g.threads);
+    if (g.parts == 1) {
+        hipLaunchKernelGGL((token_logprobs_kernel<X, true>), grid, threads, 0, st, logits, stride, target, V, 1, g.part, k, nullptr, out);
+        return;
+    }
+    hipLaunchKernelGGL((token_logprobs_kernel<X, false>), grid, threads, 0, st, logits, stride, target, V, g.parts, g.part, k, records, out);
+    hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(N), dim3(WAVE), 0, st, records, target, V, g.parts, g.part, k, out);
 }
 
 extern "C" int moe_token_logprobs(const void *logits, long long row_stride, const int32_t *target, int N, int V, int dtype, int k,
@@ -136,13 +516,14 @@ extern "C" int moe_token_logprobs(const void *logits, long long row_stride, cons
     if (N == 0) return MOE_OK;
     MOE_REQUIRE(logits && target && logprob && entropy && lse && (k == 0 || (top_idx && top_logprob)), MOE_ERR_INVALID_ARG,
                 "moe_token_logprobs: null pointer");
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype == MOE_BF16)
-        hipLaunchKernelGGL(token_logprobs_kernel<bf16_t>, dim3(N), dim3(LP_THREADS), 0, st, (const bf16_t *)logits, (size_t)row_stride, target, V, k,
-                           logprob, entropy, lse, top_idx, top_logprob);
-    else
-        hipLaunchKernelGGL(token_logprobs_kernel<float>, dim3(N), dim3(LP_THREADS), 0, st, (const float *)logits, (size_t)row_stride, target, V, k,
-                           logprob, entropy, lse, top_idx, top_logprob);
+    MOE_REQUIRE((uintptr_t)logits % (dtype == MOE_F32 ? 4 : 2) == 0, MOE_ERR_INVALID_ARG, "moe_token_logprobs: tensor misaligned");
+    const LogprobShape g = logprob_shape(N, V, dtype);
+    const size_t need = moe_token_logprobs_workspace_bytes(N, V, k, dtype);
+    MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
+                "moe_token_logprobs: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
+    const LogprobOut out = {logprob, entropy, lse, top_idx, top_logprob};
+    if (dtype == MOE_BF16) logprobs_launch(g, (const bf16_t *)logits, (size_t)row_stride, target, N, V, k, (float *)ws, out, (hipStream_t)stream);
+    else logprobs_launch(g, (const float *)logits, (size_t)row_stride, target, N, V, k, (float *)ws, out, (hipStream_t)stream);
     MOE_CHECK_LAUNCH("moe_token_logprobs");
     return MOE_OK;
 }
@@ -157,13 +538,18 @@ extern "C" int moe_token_logprobs_backward(const void *logits, long long row_str
                 "moe_token_logprobs_backward: null pointer");
     MOE_REQUIRE(dlogits != logits || dlogits_stride == row_stride, MOE_ERR_INVALID_ARG,
                 "moe_token_logprobs_backward: dlogits lies on logits with another stride");
+    const int size = dtype == MOE_F32 ? 4 : 2, pieces = V / (16 / size) + 1;
+    MOE_REQUIRE((uintptr_t)logits % size == 0 && (uintptr_t)dlogits % size == 0, MOE_ERR_INVALID_ARG, "moe_token_logprobs_backward: tensor misaligned");
+    int lg = 0;
+    while ((1 << lg) < LP_THREADS && (LP_SLOPE_PIECES << lg) < pieces) ++lg;
+    const dim3 grid(ceil_div(N, LP_THREADS >> lg), ceil_div(pieces, LP_SLOPE_PIECES << lg));
     hipStream_t st = (hipStream_t)stream;
     if (dtype == MOE_BF16)
-        hipLaunchKernelGGL(token_logprobs_backward_kernel<bf16_t>, dim3(N), dim3(LP_THREADS), 0, st, (const bf16_t *)logits, (size_t)row_stride,
-                           target, lse, entropy, dlogprob, dentropy, V, (bf16_t *)dlogits, (size_t)dlogits_stride);
+        hipLaunchKernelGGL(token_logprobs_backward_kernel<bf16_t>, grid, dim3(LP_THREADS), 0, st, (const bf16_t *)logits, (size_t)row_stride,
+                           target, lse, entropy, dlogprob, dentropy, N, V, lg, (bf16_t *)dlogits, (size_t)dlogits_stride);
     else
-        hipLaunchKernelGGL(token_logprobs_backward_kernel<float>, dim3(N), dim3(LP_THREADS), 0, st, (const float *)logits, (size_t)row_stride,
-                           target, lse, entropy, dlogprob, dentropy, V, (float *)dlogits, (size_t)dlogits_stride);
+        hipLaunchKernelGGL(token_logprobs_backward_kernel<float>, grid, dim3(LP_THREADS), 0, st, (const float *)logits, (size_t)row_stride,
+                           target, lse, entropy, dlogprob, dentropy, N, V, lg, (float *)dlogits, (size_t)dlogits_stride);
     MOE_CHECK_LAUNCH("moe_token_logprobs_backward");
     return MOE_OK;
 }

@@ -1,0 +1,45 @@
+// How moe_token_logprobs cuts rows of logits: host rules.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+constexpr int LP_SMALL = 16;                  // logits of a lane that shares a short row
+constexpr int LP_VECS = 8;                    // 16-byte pieces of a thread that shares a long one
+constexpr int LP_MAX_THREADS = 1024;
+constexpr int LP_MAX_PARTS = 64;              // of a row: one lane each where they are joined
+constexpr int LP_MAX_V = 1 << 21;
+constexpr int LP_MAX_N = 1 << 22;             // a launch holds fewer than 2^32 threads
+constexpr int LP_RECORD = 4 + 2 * MOE_MAX_TOPK;   // floats of a part: maximum, sums, target's logit; the best logits and ids
+
+struct LogprobShape {
+    int lanes;                                // short rows: lanes of a row; 0: long ones
+    int threads, parts, part;                 // long: threads of a workgroup, parts of a row, logits of a part
+};
+
+static inline LogprobShape logprob_shape(int N, int V, int dtype)
+{
+    LogprobShape g = {0, 0, 1, V};
+    if (V <= WAVE * LP_SMALL) {
+        g.lanes = V <= 4 * LP_SMALL ? 4 : V <= 16 * LP_SMALL ? 16 : WAVE;
+        return g;
+    }
+    const int per = dtype == MOE_BF16 ? 8 : 4;                               // logits of a piece
+    const int most = (LP_MAX_THREADS * LP_VECS - 1) * per;                   // one piece less: a row may begin inside one
+    int parts = (V + most - 1) / most;
+    // few rows: two workgroups for each compute unit, parts of at least a piece for each lane of four wavefronts
+    const int want = N < 512 ? (512 + N - 1) / N : 1, room = V / (4 * WAVE * per);
+    const int split = want < room ? want : room;
+    if (split > parts) parts = split;
+    if (parts > LP_MAX_PARTS) parts = LP_MAX_PARTS;
+    g.part = ((V + parts - 1) / parts + 63) / 64 * 64;                       // parts begin alike inside a piece
+    g.parts = (V + g.part - 1) / g.part;
+    const int pieces = (g.part < V ? g.part : V) / per + 1;
+    // few workgroups: one or two pieces a thread; many: as few threads as hold the row
+    const int each = (long long)N * g.parts < 2048 ? 2 : LP_VECS;
+    g.threads = WAVE;
+    while (g.threads < LP_MAX_THREADS && g.threads * each < pieces) g.threads *= 2;
+    return g;
+}
+
+}  // namespace moe

@@ -35,48 +35,26 @@ template <> struct LogitPiece<bf16_t> {
 // A logit as the alternatives see it: no number counts as masked.
 __device__ __forceinline__ float lp_ranked(float x) { return x == x ? x : -INFINITY; }
 
-// Running maximum and sums.  The maximum is never below the lowest finite value, so a row that is masked throughout has s = 0 and no
-// infinity is taken from another; a NaN passes into s.
+// Sums under a maximum.  It is never below the lowest finite value: a row that is masked throughout has s = 0, and no infinity is taken
+// from another; a NaN passes into s.
 struct LogitSums {
     float m, s, t;
-    __device__ __forceinline__ void clear() { m = -FLT_MAX, s = t = 0.f; }
-    __device__ __forceinline__ void raise(float to)
-    {
-        if (to > m) {
-            const float d = fmaxf(m - to, -1e4f), e = exp_of<true>(d);     // from the lowest value on: e = 0, and no infinity times it
-            t = (t + d * s) * e;
-            s *= e;
-            m = to;
-        }
-    }
-    // a value not above m: d is kept off minus infinity, which times zero would be no number
     __device__ __forceinline__ void add(float x)
     {
         const float d = x - m, e = __builtin_amdgcn_exp2f(d * LOG2E);
         s += e;
-        t = fmaf(fmaxf(d, -1e4f), e, t);
+        t = fmaf(fmaxf(d, -1e4f), e, t);                 // d off minus infinity, which times zero would be no number
     }
-    __device__ __forceinline__ void join(LogitSums o)
+    // to >= m.  Products rounded as they are: one that a sum over lanes took in unrounded would differ from lane to lane.
+    __device__ __forceinline__ void raise(float to)
     {
-        raise(o.m);
-        o.raise(m);
-        s += o.s;
-        t += o.t;
-    }
-    template <int STEP>
-    __device__ __forceinline__ LogitSums partner() const
-    {
-        return {group_exchange<STEP>(m), group_exchange<STEP>(s), group_exchange<STEP>(t)};
+#pragma clang fp contract(off)
+        const float d = fmaxf(m - to, -1e4f), e = exp_of<true>(d);
+        t = (t + d * s) * e;
+        s *= e;
+        m = to;
     }
 };
-template <int LANES, int STEP = 0>
-__device__ __forceinline__ void lp_join_lanes(LogitSums &a)
-{
-    if constexpr ((1 << STEP) < LANES) {
-        a.join(a.partner<STEP>());
-        lp_join_lanes<LANES, STEP + 1>(a);
-    }
-}
 template <int LANES, int STEP = 0>
 __device__ __forceinline__ float lp_max_lanes(float v)
 {
@@ -88,6 +66,14 @@ __device__ __forceinline__ int lp_min_lanes(int v)
 {
     if constexpr ((1 << STEP) < LANES) return lp_min_lanes<LANES, STEP + 1>(min(v, group_exchange<STEP>(v)));
     else return v;
+}
+// the lanes' sums under the largest of their maxima
+template <int LANES>
+__device__ __forceinline__ void lp_join_lanes(LogitSums &a)
+{
+    a.raise(lp_max_lanes<LANES>(a.m));
+    a.s = sum_over<LANES>(a.s);
+    a.t = sum_over<LANES>(a.t);
 }
 
 struct LogprobOut {
@@ -135,13 +121,11 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_short_kernel(const 
         }
     }
     const auto place = [&](int i) { return i / P * P * LANES + lane * P + i % P; };
-    LogitSums a;
-    a.clear();
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < LP_SMALL; ++i) top = fmaxf(top, v[i]);
     top = lp_max_lanes<LANES>(top);
-    a.m = fmaxf(a.m, top);
+    LogitSums a = {fmaxf(top, -FLT_MAX), 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < LP_SMALL; ++i)
         if (place(i) < V) a.add(v[i]);
@@ -195,7 +179,7 @@ __device__ __forceinline__ void lp_rank(const float *value, const int *id, int c
 // Long rows: a workgroup takes a part of a row, LP_VECS pieces a thread in registers.  WHOLE: the part is the row; else its numbers go to
 // a record of LP_RECORD floats.
 template <class X, bool WHOLE>
-__global__ __launch_bounds__(LP_MAX_THREADS) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,
+__global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,
                                                                         const int32_t *__restrict__ target, int V, int parts, int part, int k,
                                                                         float *__restrict__ records, LogprobOut out)
 {
@@ -223,42 +207,48 @@ __global__ __launch_bounds__(LP_MAX_THREADS) void token_logprobs_kernel(const X 
         if (i * threads + tid < pieces) held[i] = __builtin_nontemporal_load(body + i * threads + tid);
     }
     if (tid == 0) listed = 0;
-    LogitSums a;
-    a.clear();
-    float top = -INFINITY;
+    const float end_v = tid < ends ? value_of(single) : -INFINITY;
+    float top = end_v;
 #pragma unroll
     for (int i = 0; i < LP_VECS; ++i) {
         if (i * threads + wave * WAVE >= pieces) break;  // the whole wavefront
-        float most = piece::get(held[i], 0);
 #pragma unroll
-        for (int q = 1; q < P; ++q) most = fmaxf(most, piece::get(held[i], q));
-        top = fmaxf(top, most);
-        a.raise(most);
+        for (int q = 0; q < P; ++q) top = fmaxf(top, piece::get(held[i], q));
+    }
+    // the groups of threads that the bound is taken from: threads / LP_GROUPS neighbours, a wavefront at most
+    float most = lp_max_lanes<4>(top);
+    {
+        const int size = threads / LP_GROUPS;
+        float group = most;
+        most = fmaxf(most, group_exchange<2>(most));
+        if (size >= 8) group = most;
+        most = fmaxf(most, group_exchange<3>(most));
+        if (size >= 16) group = most;
+        most = fmaxf(most, group_exchange<4>(most));
+        if (size >= 32) group = most;
+        most = fmaxf(most, group_exchange<5>(most));
+        if (size >= 64) group = most;
+        if (tid % size == 0) groups[tid / size] = group;
+    }
+    LogitSums a = {fmaxf(most, -FLT_MAX), 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < LP_VECS; ++i) {
+        if (i * threads + wave * WAVE >= pieces) break;
 #pragma unroll
         for (int q = 0; q < P; ++q) a.add(piece::get(held[i], q));
     }
-    const float end_v = tid < ends ? value_of(single) : -INFINITY;
-    if (tid < ends) {
-        top = fmaxf(top, end_v);
-        a.raise(end_v);
-        a.add(end_v);
-    }
-    // the groups of threads that the bound is taken from: threads / LP_GROUPS neighbours
-    {
-        float v = top;
-        const int size = threads / LP_GROUPS;
-        v = lp_max_lanes<4>(v);
-        if (size >= 8) v = fmaxf(v, group_exchange<2>(v));
-        if (size >= 16) v = fmaxf(v, group_exchange<3>(v));
-        if (size >= 32) v = fmaxf(v, group_exchange<4>(v));
-        if (size >= 64) v = fmaxf(v, group_exchange<5>(v));
-        if (tid % size == 0) groups[tid / size] = v;
-    }
-    lp_join_lanes<WAVE>(a);
+    if (ends) a.add(end_v);
+    a.s = sum_over<WAVE>(a.s);
+    a.t = sum_over<WAVE>(a.t);
     if (lane == 0) wave_m[wave] = a.m, wave_s[wave] = a.s, wave_t[wave] = a.t;
     __syncthreads();
-    a.m = wave_m[0], a.s = wave_s[0], a.t = wave_t[0];
-    for (int w = 1; w < waves; ++w) a.join({wave_m[w], wave_s[w], wave_t[w]});
+    {                                                    // the wavefronts' sums, one a lane
+        const int w = lane % LP_GROUPS;
+        a.m = w < waves ? wave_m[w] : -FLT_MAX;
+        a.s = w < waves ? wave_s[w] : 0.f;
+        a.t = w < waves ? wave_t[w] : 0.f;
+        lp_join_lanes<LP_GROUPS>(a);
+    }
     const float log_s = logf(a.s);
     float *record = WHOLE ? nullptr : records + ((size_t)n * parts + which) * LP_RECORD;
     if (tid == 0) {
@@ -280,18 +270,15 @@ __global__ __launch_bounds__(LP_MAX_THREADS) void token_logprobs_kernel(const X 
             record[4 + MOE_MAX_TOPK + rank] = __int_as_float(id + lo);
         }
     };
-    // the bound: the k-th largest of the groups' maxima
-    float bound = -INFINITY;
-    {
-        const float v = groups[lane % LP_GROUPS];
-        int rank = 0;
-        for (int j = 0; j < LP_GROUPS; ++j) {
-            const float o = groups[j];
-            rank += o > v || (o == v && j < lane % LP_GROUPS) ? 1 : 0;
-        }
-        const unsigned long long mine = __ballot(rank == k - 1);
-        bound = __shfl(v, __ffsll(mine) - 1, WAVE);
+    // the bound: the least of the groups' maxima that fewer than k are above
+    const float mine = groups[lane % LP_GROUPS];
+    unsigned few = 0;
+#pragma unroll
+    for (int j = 0; j < LP_GROUPS; ++j) {
+        const float o = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
+        few |= __popcll(__ballot(mine > o) & ((1u << LP_GROUPS) - 1)) < k ? 1u << j : 0u;
     }
+    const float bound = -lp_max_lanes<LP_GROUPS>(few >> lane % LP_GROUPS & 1 ? -mine : -INFINITY);
     int count = LP_LIST + 1;
     if (bound > -INFINITY) {
         if (top >= bound) {
@@ -305,6 +292,10 @@ __global__ __launch_bounds__(LP_MAX_THREADS) void token_logprobs_kernel(const X 
             for (int i = 0; i < LP_VECS; ++i) {
                 if (i * threads + wave * WAVE >= pieces) break;
                 asm("" : "+v"(held[i]));               // unpacked again: the logits themselves would fill the registers
+                float best = piece::get(held[i], 0);
+#pragma unroll
+                for (int q = 1; q < P; ++q) best = fmaxf(best, piece::get(held[i], q));
+                if (best < bound) continue;
 #pragma unroll
                 for (int q = 0; q < P; ++q) offer(piece::get(held[i], q), head + (i * threads + tid) * P + q);
             }
@@ -356,8 +347,7 @@ __global__ __launch_bounds__(WAVE) void token_logprobs_join_kernel(const float *
     const size_t n = blockIdx.x;
     const int lane = threadIdx.x;
     const float *record = records + (n * parts + min(lane, parts - 1)) * LP_RECORD;
-    LogitSums a;
-    a.clear();
+    LogitSums a = {-FLT_MAX, 0.f, 0.f};
     if (lane < parts) a = {record[0], record[1], record[2]};
     float best[MOE_MAX_TOPK];
     int ids[MOE_MAX_TOPK];

@@ -1,4 +1,5 @@
 // The gradient of sorting tokens by expert and back: moe_combine_topk_backward, moe_dispatch_topk_backward, moe_route_topk_backward.
+#include "row_groups.h"
 #include "scalar_math.h"
 
 namespace moe {
@@ -24,65 +25,111 @@ __device__ __forceinline__ rb_u32x4_t piece_of(const float (&v)[BF16 ? 8 : 4])
     return r;
 }
 
-// one wavefront per token: its dout once, the k rows of y it met, their gradients
-template <bool BF16>
+// The row of this thread's group of 2^lg lanes (256 at most: a workgroup).
+__device__ __forceinline__ unsigned rb_row(int lg, int &lane)
+{
+    lane = threadIdx.x & ((1 << lg) - 1);
+    return ((blockIdx.y * gridDim.x + blockIdx.x) << (8 - lg)) + (threadIdx.x >> lg);
+}
+
+// A group of lanes per token: its dout once, PIECES pieces a lane at a time, the k rows of y it met, their gradients.  dweight: lanes' sums,
+// then the wavefronts' in their order where a workgroup shares a row.
+template <bool BF16, int PIECES>
 __global__ __launch_bounds__(RB_THREADS) void combine_backward_kernel(const rb_u32x4_t *__restrict__ dout, const rb_u32x4_t *__restrict__ y_perm,
                                                                       const int32_t *__restrict__ inv, const float *__restrict__ weight, int T,
-                                                                      int k, int vec_per_row, int residual, rb_u32x4_t *__restrict__ dy_perm,
+                                                                      int k, int vec_per_row, int lg, int residual, rb_u32x4_t *__restrict__ dy_perm,
                                                                       float *__restrict__ dweight, rb_u32x4_t *__restrict__ dx)
 {
     constexpr int V = BF16 ? 8 : 4;
-    const int s = blockIdx.x * (RB_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-    if (s >= T) return;
+    __shared__ float sums[RB_THREADS / WAVE][MOE_MAX_TOPK];
+    int lane;
+    const unsigned s = rb_row(lg, lane);
+    if (s >= (unsigned)T) return;                        // where a workgroup has a row: the whole workgroup
+    const int lanes = 1 << lg;
     int pos[MOE_MAX_TOPK];
     float p[MOE_MAX_TOPK], dot[MOE_MAX_TOPK];
     bool any = false;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
-        pos[j] = j < k ? inv[(size_t)j * T + s] : -1;
-        p[j] = j < k ? weight[(size_t)j * T + s] : 0.f;
-        dot[j] = 0.f;
+        pos[j] = -1, p[j] = dot[j] = 0.f;
+        if (j >= k) continue;
+        pos[j] = inv[(size_t)j * T + s];
+        p[j] = weight[(size_t)j * T + s];
         any = any || pos[j] >= 0;
     }
-    const rb_u32x4_t zero = {0, 0, 0, 0};
-    for (int c = lane; c < vec_per_row; c += WAVE) {
-        const rb_u32x4_t g = dout[(size_t)s * vec_per_row + c];
-        if (dx) dx[(size_t)s * vec_per_row + c] = residual || !any ? g : zero;
+    const bool pass = residual || !any;
+    for (int c0 = lane; c0 < vec_per_row; c0 += lanes * PIECES) {
+        rb_u32x4_t g[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+            if (c0 + i * lanes < vec_per_row) g[i] = dout[(size_t)s * vec_per_row + c0 + i * lanes];
 #pragma unroll
         for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+            if (j >= k) break;
             if (pos[j] < 0) continue;
+            const size_t row = (size_t)pos[j] * vec_per_row;
+            rb_u32x4_t y[PIECES];
             if (dweight) {
-                const rb_u32x4_t y = y_perm[(size_t)pos[j] * vec_per_row + c];
 #pragma unroll
-                for (int q = 0; q < V; ++q) dot[j] = fmaf(piece_value<BF16>(g, q), piece_value<BF16>(y, q), dot[j]);
+                for (int i = 0; i < PIECES; ++i)
+                    if (c0 + i * lanes < vec_per_row) y[i] = y_perm[row + c0 + i * lanes];
             }
-            float v[V];
 #pragma unroll
-            for (int q = 0; q < V; ++q) v[q] = p[j] * piece_value<BF16>(g, q);
-            dy_perm[(size_t)pos[j] * vec_per_row + c] = piece_of<BF16>(v);
+            for (int i = 0; i < PIECES; ++i) {
+                if (c0 + i * lanes >= vec_per_row) continue;
+                float v[V];
+#pragma unroll
+                for (int q = 0; q < V; ++q) v[q] = p[j] * piece_value<BF16>(g[i], q);
+                dy_perm[row + c0 + i * lanes] = piece_of<BF16>(v);
+                if (dweight) {
+#pragma unroll
+                    for (int q = 0; q < V; ++q) dot[j] = fmaf(piece_value<BF16>(g[i], q), piece_value<BF16>(y[i], q), dot[j]);
+                }
+            }
+        }
+        if (dx) {
+            const rb_u32x4_t zero = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (c0 + i * lanes < vec_per_row) dx[(size_t)s * vec_per_row + c0 + i * lanes] = pass ? g[i] : zero;
         }
     }
     if (!dweight) return;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
-        if (j >= k) continue;
-        const float sum = sum_over<WAVE>(dot[j]);
-        if (lane == 0) dweight[(size_t)j * T + s] = sum;
+        if (j >= k) break;
+        float v = dot[j];
+        if (lg >= 1) v += group_exchange<0>(v);
+        if (lg >= 2) v += group_exchange<1>(v);
+        if (lg >= 3) v += group_exchange<2>(v);
+        if (lg >= 4) v += group_exchange<3>(v);
+        if (lg >= 5) v += group_exchange<4>(v);
+        if (lg >= 6) v += group_exchange<5>(v);
+        if (lg <= 6 && lane == 0) dweight[(size_t)j * T + s] = v;
+        if (lg > 6 && lane % WAVE == 0) sums[lane / WAVE][j] = v;
+    }
+    if (lg <= 6) return;
+    __syncthreads();
+    if (lane < k) {
+        float v = sums[0][lane];
+        for (int w = 1; w < lanes / WAVE; ++w) v += sums[w][lane];
+        dweight[(size_t)lane * T + s] = v;
     }
 }
 
-// one wavefront per token: the gradients of its k copies, added in choice order behind dx_add
+// A group of lanes per token: the gradients of its k copies, added in choice order behind dx_add.
 template <bool BF16>
 __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_u32x4_t *__restrict__ dx_perm, const int32_t *__restrict__ inv,
-                                                                       const rb_u32x4_t *dx_add, int T, int k, int vec_per_row, rb_u32x4_t *dx)
+                                                                       const rb_u32x4_t *dx_add, int T, int k, int vec_per_row, int lg, rb_u32x4_t *dx)
 {
     constexpr int V = BF16 ? 8 : 4;
-    const int s = blockIdx.x * (RB_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-    if (s >= T) return;
+    int lane;
+    const unsigned s = rb_row(lg, lane);
+    if (s >= (unsigned)T) return;
     int pos[MOE_MAX_TOPK];
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) pos[j] = j < k ? inv[(size_t)j * T + s] : -1;
-    for (int c = lane; c < vec_per_row; c += WAVE) {
+    for (int c = lane; c < vec_per_row; c += 1 << lg) {
         rb_u32x4_t g[MOE_MAX_TOPK], a = {0, 0, 0, 0};
         if (dx_add) a = dx_add[(size_t)s * vec_per_row + c];
 #pragma unroll
@@ -101,65 +148,103 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
     }
 }
 
-// one wavefront per token, its logits held in registers
-constexpr int RB_LOGITS = MOE_MAX_EXPERTS / WAVE;
+// LANES lanes per token, RB_LOGITS logits a lane in registers; PIECES: four consecutive ones (rows begin on 16 bytes).  With renormalize the
+// other experts' logits take no part and are not read.
+constexpr int RB_LOGITS = 16;
 
+template <int LANES, bool PIECES>
 __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float *__restrict__ logits, const int32_t *__restrict__ idx,
                                                                     const float *__restrict__ dweight, int T, int E, int k, int renormalize,
                                                                     float *__restrict__ dlogits)
 {
-    const int s = blockIdx.x * (RB_THREADS / WAVE) + threadIdx.x / WAVE, lane = threadIdx.x % WAVE;
-    if (s >= T) return;
+    constexpr int P = PIECES ? 4 : 1;
+    typedef float piece_t __attribute__((ext_vector_type(P)));
+    const unsigned s = blockIdx.x * (RB_THREADS / LANES) + threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES;
+    if (s >= (unsigned)T) return;
     const float *row = logits + (size_t)s * E;
     int e[MOE_MAX_TOPK];
     float dw[MOE_MAX_TOPK], w[MOE_MAX_TOPK];
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
-        const int id = j < k ? idx[(size_t)j * T + s] : -1;
-        e[j] = id >= 0 && id < E ? id : -1;
-        dw[j] = e[j] >= 0 ? dweight[(size_t)j * T + s] : 0.f;
-        w[j] = e[j] >= 0 ? row[e[j]] : -INFINITY;
+        e[j] = -1, dw[j] = 0.f, w[j] = -INFINITY;
+        if (j >= k) continue;
+        const int id = idx[(size_t)j * T + s];
+        const float d = dweight[(size_t)j * T + s];
+        if (id >= 0 && id < E) e[j] = id, dw[j] = d, w[j] = row[id];
         top = fmaxf(top, w[j]);
     }
+    const auto place = [&](int i) { return i / P * P * LANES + lane * P; };     // of the piece that i lies in
     float v[RB_LOGITS], total = 0.f;
     if (!renormalize) {
 #pragma unroll
-        for (int i = 0; i < RB_LOGITS; ++i) {
-            const int c = i * WAVE + lane;
-            v[i] = c < E ? row[c] : -INFINITY;
-            top = fmaxf(top, v[i]);
+        for (int i = 0; i < RB_LOGITS; i += P) {
+            piece_t x = -INFINITY;
+            if (place(i) < E) x = *(const piece_t *)(row + place(i));
+#pragma unroll
+            for (int q = 0; q < P; ++q) {
+                if constexpr (P > 1) v[i + q] = x[q];
+                else v[i] = x[0];
+                top = fmaxf(top, v[i + q]);
+            }
         }
 #pragma unroll
-        for (int o = 1; o < WAVE; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
+        for (int o = 1; o < LANES; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, WAVE));
 #pragma unroll
         for (int i = 0; i < RB_LOGITS; ++i) {
-            v[i] = i * WAVE + lane < E ? exp_of<true>(v[i] - top) : 0.f;
+            v[i] = place(i) < E ? exp_of<true>(v[i] - top) : 0.f;
             total += v[i];
         }
-        total = sum_over<WAVE>(total);
+        total = sum_over<LANES>(total);
     }
     float mean = 0.f;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+        if (j >= k) continue;
         w[j] = e[j] >= 0 ? exp_of<true>(w[j] - top) : 0.f;
         if (renormalize) total += w[j];
     }
+    const float share = 1.f / total;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
-        w[j] = e[j] >= 0 ? w[j] / total : 0.f;
+        if (j >= k) continue;
+        w[j] = e[j] >= 0 ? w[j] * share : 0.f;
         mean = fmaf(w[j], dw[j], mean);
     }
+    const float all = renormalize ? 0.f : -mean * share, off = renormalize ? mean : 0.f;
 #pragma unroll
-    for (int i = 0; i < RB_LOGITS; ++i) {
-        const int c = i * WAVE + lane;
-        if (c >= E) continue;
-        float g = renormalize ? 0.f : -(v[i] / total) * mean;
+    for (int i = 0; i < RB_LOGITS; ++i) v[i] = renormalize ? 0.f : v[i] * all;
 #pragma unroll
-        for (int j = 0; j < MOE_MAX_TOPK; ++j)
-            if (e[j] == c) g += renormalize ? w[j] * (dw[j] - mean) : w[j] * dw[j];
-        dlogits[(size_t)s * E + c] = g;
+    for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+        if (j >= k) break;
+        const float more = w[j] * (dw[j] - off);
+        const int at = e[j] - lane * P;                  // the place in this lane, if it has it
+#pragma unroll
+        for (int i = 0; i < RB_LOGITS; ++i) v[i] += at == i / P * P * LANES + i % P ? more : 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < RB_LOGITS; i += P) {
+        if (place(i) >= E) continue;
+        piece_t x;
+#pragma unroll
+        for (int q = 0; q < P; ++q) x[q] = v[i + q];
+        *(piece_t *)(dlogits + (size_t)s * E + place(i)) = x;
+    }
+}
+
+// combine's gradient: log2 of the lanes per row, one piece per lane and trip (a wavefront's at most, or a whole workgroup); -1: 32 lanes with
+// three pieces each
+static int combine_backward_lanes(int T, int vec_per_row)
+{
+    const int lg = row_lanes(vec_per_row);
+    if (lg <= 5) return lg;
+    return T > 2048 ? -1 : lg < 8 ? 6 : 8;
+}
+static int dispatch_backward_lanes(int T, int vec_per_row)
+{
+    const int lg = combine_topk_lanes(T, vec_per_row);
+    return lg < 8 ? lg : 8;
 }
 
 static int rows_check(const char *who, int T, int k, int d, int dtype)
@@ -189,9 +274,12 @@ extern "C" int moe_combine_topk_backward(const void *dout, const void *y_perm, c
     MOE_REQUIRE(aligned16(dout) && aligned16(y_perm) && aligned16(dy_perm) && aligned16(dx), MOE_ERR_INVALID_ARG,
                 "moe_combine_topk_backward: tensor misaligned");
     const int vec = (int)((size_t)d * (dtype == MOE_F32 ? 4 : 2) / 16);
-    auto kern = dtype == MOE_BF16 ? combine_backward_kernel<true> : combine_backward_kernel<false>;
-    hipLaunchKernelGGL(kern, dim3(ceil_div(T, RB_THREADS / WAVE)), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dout,
-                       (const rb_u32x4_t *)y_perm, inv, expert_weight, T, k, vec, residual, (rb_u32x4_t *)dy_perm, dweight, (rb_u32x4_t *)dx);
+    const int lg = combine_backward_lanes(T, vec), wide = lg < 0;
+    auto kern = dtype == MOE_BF16 ? (wide ? combine_backward_kernel<true, 3> : combine_backward_kernel<true, 1>)
+                                  : (wide ? combine_backward_kernel<false, 3> : combine_backward_kernel<false, 1>);
+    hipLaunchKernelGGL(kern, rows_grid(T, wide ? 5 : lg), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dout,
+                       (const rb_u32x4_t *)y_perm, inv, expert_weight, T, k, vec, wide ? 5 : lg, residual, (rb_u32x4_t *)dy_perm, dweight,
+                       (rb_u32x4_t *)dx);
     MOE_CHECK_LAUNCH("moe_combine_topk_backward");
     return MOE_OK;
 }
@@ -206,8 +294,9 @@ extern "C" int moe_dispatch_topk_backward(const void *dx_perm, const int32_t *in
     MOE_REQUIRE(aligned16(dx_perm) && aligned16(dx_add) && aligned16(dx), MOE_ERR_INVALID_ARG, "moe_dispatch_topk_backward: tensor misaligned");
     const int vec = (int)((size_t)d * (dtype == MOE_F32 ? 4 : 2) / 16);
     auto kern = dtype == MOE_BF16 ? dispatch_backward_kernel<true> : dispatch_backward_kernel<false>;
-    hipLaunchKernelGGL(kern, dim3(ceil_div(T, RB_THREADS / WAVE)), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dx_perm, inv,
-                       (const rb_u32x4_t *)dx_add, T, k, vec, (rb_u32x4_t *)dx);
+    const int lg = dispatch_backward_lanes(T, vec);
+    hipLaunchKernelGGL(kern, rows_grid(T, lg), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dx_perm, inv,
+                       (const rb_u32x4_t *)dx_add, T, k, vec, lg, (rb_u32x4_t *)dx);
     MOE_CHECK_LAUNCH("moe_dispatch_topk_backward");
     return MOE_OK;
 }
@@ -222,8 +311,14 @@ extern "C" int moe_route_topk_backward(const float *logits, const int32_t *exper
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(logits && expert_idx && dweight && dlogits, MOE_ERR_INVALID_ARG, "moe_route_topk_backward: null pointer");
     MOE_REQUIRE(dlogits != logits && dlogits != dweight, MOE_ERR_INVALID_ARG, "moe_route_topk_backward: dlogits aliases an input");
-    hipLaunchKernelGGL(route_backward_kernel, dim3(ceil_div(T, RB_THREADS / WAVE)), dim3(RB_THREADS), 0, (hipStream_t)stream, logits, expert_idx,
-                       dweight, T, E, k, renormalize, dlogits);
+    const bool pieces = E % 4 == 0 && aligned16(logits) && aligned16(dlogits);
+#define MOE_GATE(L)                                                                                                                            \
+    hipLaunchKernelGGL((pieces ? route_backward_kernel<L, true> : route_backward_kernel<L, false>), dim3(ceil_div(T, RB_THREADS / L)),          \
+                       dim3(RB_THREADS), 0, (hipStream_t)stream, logits, expert_idx, dweight, T, E, k, renormalize, dlogits)
+    if (E <= 4 * RB_LOGITS) MOE_GATE(4);
+    else if (E <= 16 * RB_LOGITS) MOE_GATE(16);
+    else MOE_GATE(64);
+#undef MOE_GATE
     MOE_CHECK_LAUNCH("moe_route_topk_backward");
     return MOE_OK;
 }

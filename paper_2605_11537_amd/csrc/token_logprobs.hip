@@ -204,7 +204,7 @@ __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const
 #pragma unroll
     for (int i = 0; i < LP_VECS; ++i) {                   // masked behind the last piece
         held[i] = {piece::MASKED, piece::MASKED, piece::MASKED, piece::MASKED};
-        if (i * threads + tid < pieces) held[i] = __builtin_nontemporal_load(body + i * threads + tid);
+        if (i * threads + tid < pieces) held[i] = body[i * threads + tid];
     }
     if (tid == 0) listed = 0;
     const float end_v = tid < ends ? value_of(single) : -INFINITY;

@@ -27,10 +27,13 @@ static inline LogprobShape logprob_shape(int N, int V, int dtype)
     const int per = dtype == MOE_BF16 ? 8 : 4;                               // logits of a piece
     const int most = (LP_MAX_THREADS * LP_VECS - 1) * per;                   // one piece less: a row may begin inside one
     int parts = (V + most - 1) / most;
-    // few rows: two workgroups for each compute unit, parts of at least a piece for each lane of four wavefronts
-    const int want = N < 512 ? (512 + N - 1) / N : 1, room = V / (4 * WAVE * per);
-    const int split = want < room ? want : room;
-    if (split > parts) parts = split;
+    // A row that one workgroup holds is not cut, however few there are: the join is a launch of its own (1 x 32000 bf16 6.7 us whole, 9.5 in
+    // parts; 64 x 50257 8.0 and 9.1; 300 x 50257 15 and 18).  A longer one, in few rows: two workgroups for each compute unit, parts of
+    // at least a piece for each lane of four wavefronts (3 x 131072: 12 us; two parts: 15).
+    if (parts > 1) {
+        const int want = N < 512 ? (512 + N - 1) / N : 1, room = V / (4 * WAVE * per), split = want < room ? want : room;
+        if (split > parts) parts = split;
+    }
     if (parts > LP_MAX_PARTS) parts = LP_MAX_PARTS;
     g.part = ((V + parts - 1) / parts + 63) / 64 * 64;                       // parts begin alike inside a piece
     g.parts = (V + g.part - 1) / g.part;

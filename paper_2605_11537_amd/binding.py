@@ -9,6 +9,7 @@ missing or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import importlib
 import os
 
@@ -503,68 +504,79 @@ def moe_combine_topk(y_perm, x, inv, expert_weight, residual=0, out=None):
 
 
 # --------------------------------------------------------------------------- training the gate and the predictor
-def _expect(who, lead, *tensors):
-    """Each (name, tensor, shape, dtype) as the call reads it, on the lead tensor's device, which has to be the current one: its stream
-    is the one that the call's kernels go to.  None: an argument that was left out."""
-    if not lead.is_cuda:
-        raise ValueError("device-resident contiguous tensors only")
-    at = lead.get_device()
-    if at != torch.cuda.current_device():
-        raise ValueError(f"{who}: tensors on device {at}, the current device is {torch.cuda.current_device()}")
-    for name, t, shape, dtype in tensors:
-        if t is None:
-            continue
-        if t.shape != shape or t.dtype != dtype:
-            raise ValueError(f"{who}: {name} must be {list(shape)} of {dtype}, not {list(t.shape)} of {t.dtype}")
-        if t.get_device() != at:
-            raise ValueError(f"{who}: {name} is not on device {at}")
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)     # as for the stream: the same without the initialisation check
 
 
+@functools.lru_cache(maxsize=256)
+def _size(query, *args):
+    """A workspace's size; the queries are functions of their arguments alone."""
+    return getattr(lib(), query)(*args)
+
+
+def _room(query, lead, *args):
+    """A fresh workspace beside lead, or None where none is needed."""
+    need = _size(query, *args)
+    return _c().fresh(lead, torch.uint8, (need,))[0] if need else None
+
+
+def _bytes(ws):
+    return 0 if ws is None else ws.numel()
+
+
+# Each call below checks that its tensors have the shapes and types that it will read and write, and that they lie on the current device, whose
+# stream its kernels go to (expect, fresh: csrc/marshal.cpp).
 def moe_combine_topk_backward(dout, y_perm, inv, expert_weight, residual=0, out=None):
     """Gradient of moe_combine_topk (k = 1: of moe_combine) with respect to y_perm, the weights and x.  dout [T,d], y_perm [k*T,d],
     inv int32[k,T] or [T], expert_weight f32 likewise -> dict(dy_perm [k*T,d], dweight, dx [T,d]).  Rows of dy_perm behind the last kept
     assignment are left as they were (zero when allocated here).  With ``out``, dweight and dx may be None: they are not computed, and y_perm
     may be None without dweight."""
     T, d = dout.shape
-    k = inv.shape[0] if inv.dim() == 2 else 1
-    f32, dt = torch.float32, dout.dtype
-    shape = (k, T) if inv.dim() == 2 else (T,)
-    o = out if out is not None else dict(dy_perm=torch.zeros(k * T, d, dtype=dt, device=dout.device),
-                                         dweight=torch.empty(shape, dtype=f32, device=dout.device), dx=torch.empty_like(dout))
-    _expect("moe_combine_topk_backward", dout, ("y_perm", y_perm, (k * T, d), dt), ("inv", inv, shape, torch.int32),
-            ("expert_weight", expert_weight, shape, f32), ("dy_perm", o["dy_perm"], (k * T, d), dt),
-            ("dweight", o["dweight"], shape, f32), ("dx", o["dx"], (T, d), dt))
-    _check(_c().moe_combine_topk_backward(dout, y_perm, inv, expert_weight, T, k, d, _dt(dout), int(residual), o["dy_perm"], o["dweight"],
-                                          o["dx"], _stream()))
-    return o
+    shape = tuple(inv.shape)
+    k = shape[0] if len(shape) == 2 else 1
+    shape = (k, T) if len(shape) == 2 else (T,)
+    f32, dt, c = torch.float32, dout.dtype, _c()
+    if out is None:
+        c.expect("moe_combine_topk_backward", _device, dout)
+        dweight, dx = c.fresh(dout, f32, shape, dt, (T, d))
+        out = dict(dy_perm=torch.zeros(k * T, d, dtype=dt, device=dout.device), dweight=dweight, dx=dx)
+    dy_perm, dweight, dx = out["dy_perm"], out["dweight"], out["dx"]
+    c.expect("moe_combine_topk_backward", _device, dout, "y_perm", y_perm, dt, (k * T, d), "inv", inv, torch.int32, shape,
+             "expert_weight", expert_weight, f32, shape, "dy_perm", dy_perm, dt, (k * T, d), "dweight", dweight, f32, shape,
+             "dx", dx, dt, (T, d))
+    _check(c.moe_combine_topk_backward(dout, y_perm, inv, expert_weight, T, k, d, _dt(dout), int(residual), dy_perm, dweight, dx, _stream()))
+    return out
 
 
 def moe_dispatch_topk_backward(dx_perm, inv, dx_add=None, out=None):
     """Gradient of moe_dispatch_topk (k = 1: of moe_dispatch), and of moe_expert_ffn_rows's gather, with respect to x: the rows of
     dx_perm [k*T,d] back to their tokens and added, behind dx_add [T,d] where given.  inv int32[k,T] or [T] -> dx [T,d].  out may be
     dx_add."""
-    k = inv.shape[0] if inv.dim() == 2 else 1
-    T, d = inv.shape[-1], dx_perm.shape[1]
-    dt = dx_perm.dtype
-    dx = out if out is not None else torch.empty(T, d, dtype=dt, device=dx_perm.device)
-    _expect("moe_dispatch_topk_backward", dx_perm, ("dx_perm", dx_perm, (k * T, d), dt),
-            ("inv", inv, (k, T) if inv.dim() == 2 else (T,), torch.int32), ("dx_add", dx_add, (T, d), dt), ("out", dx, (T, d), dt))
-    _check(_c().moe_dispatch_topk_backward(dx_perm, inv, dx_add, T, k, d, _dt(dx_perm), dx, _stream()))
-    return dx
+    shape = tuple(inv.shape)
+    k = shape[0] if len(shape) == 2 else 1
+    T, d = shape[-1], dx_perm.shape[1]
+    dt, c = dx_perm.dtype, _c()
+    c.expect("moe_dispatch_topk_backward", _device, dx_perm, "dx_perm", dx_perm, dt, (k * T, d),
+             "inv", inv, torch.int32, (k, T) if len(shape) == 2 else (T,), "dx_add", dx_add, dt, (T, d), "out", out, dt, (T, d))
+    if out is None:
+        out, = c.fresh(dx_perm, dt, (T, d))
+    _check(c.moe_dispatch_topk_backward(dx_perm, inv, dx_add, T, k, d, _dt(dx_perm), out, _stream()))
+    return out
 
 
 def moe_route_topk_backward(logits, expert_idx, dweight, renormalize=False, out=None):
     """Gradient of moe_route_topk's weights (k = 1: of moe_route's probability) with respect to the logits: logits f32[T,E] as that
     call returned them, expert_idx int32[k,T] or [T], dweight f32 likewise -> dlogits f32[T,E]."""
     T, E = logits.shape
-    k = expert_idx.shape[0] if expert_idx.dim() == 2 else 1
-    shape = (k, T) if expert_idx.dim() == 2 else (T,)
-    dl = out if out is not None else torch.empty_like(logits)
-    f32 = torch.float32
-    _expect("moe_route_topk_backward", logits, ("logits", logits, (T, E), f32), ("expert_idx", expert_idx, shape, torch.int32),
-            ("dweight", dweight, shape, f32), ("out", dl, (T, E), f32))
-    _check(_c().moe_route_topk_backward(logits, expert_idx, dweight, T, E, k, int(bool(renormalize)), dl, _stream()))
-    return dl
+    shape = tuple(expert_idx.shape)
+    k = shape[0] if len(shape) == 2 else 1
+    shape = (k, T) if len(shape) == 2 else (T,)
+    f32, c = torch.float32, _c()
+    c.expect("moe_route_topk_backward", _device, logits, "logits", logits, f32, (T, E), "expert_idx", expert_idx, torch.int32, shape,
+             "dweight", dweight, f32, shape, "out", out, f32, (T, E))
+    if out is None:
+        out, = c.fresh(logits, f32, (T, E))
+    _check(c.moe_route_topk_backward(logits, expert_idx, dweight, T, E, k, int(bool(renormalize)), out, _stream()))
+    return out
 
 
 def _scan_blocks(who, u, x, H):
@@ -581,50 +593,58 @@ def sru_scan(u, x=None, b_f=None, b_r=None, c0=None, lengths=None, want_states=F
     B, L, W = u.shape
     H = x.shape[2] if x is not None else W // 4
     n = _scan_blocks("sru_scan", u, x, H)
-    dev, f32, dt = u.device, torch.float32, _dt(u)
+    f32, t, dt, c = torch.float32, u.dtype, _dt(u), _c()
+    c.expect("sru_scan", _device, u, "x", x, t, (B, L, H), "b_f", b_f, f32, (H,), "b_r", b_r, f32, (H,), "c0", c0, f32, (B, H),
+             "lengths", lengths, torch.int32, (B,))
     if out is None:
-        out = (torch.empty(B, L, H, dtype=u.dtype, device=dev), torch.empty(B, H, dtype=f32, device=dev),
-               torch.empty(lib().sru_scan_states_bytes(B, L, H) // 4, dtype=f32, device=dev) if want_states else None)
-    h, c_last, states = out
-    if states is not None and states.numel() * states.element_size() < lib().sru_scan_states_bytes(B, L, H):
-        raise ValueError("sru_scan: states are smaller than sru_scan_states_bytes")
-    _expect("sru_scan", u, ("x", x, (B, L, H), u.dtype), ("b_f", b_f, (H,), f32), ("b_r", b_r, (H,), f32), ("c0", c0, (B, H), f32),
-            ("lengths", lengths, (B,), torch.int32), ("h", h, (B, L, H), u.dtype), ("c_last", c_last, (B, H), f32),
-            ("states", states, states.shape if states is not None else None, f32))
+        states = _size("sru_scan_states_bytes", B, L, H) // 4 if want_states else 0
+        out = c.fresh(u, t, (B, L, H), f32, (B, H), f32 if want_states else None, (states,))
+        h, c_last, states = out
+    else:
+        h, c_last, states = out
+        c.expect("sru_scan", _device, u, "h", h, t, (B, L, H), "c_last", c_last, f32, (B, H))
+        _check_states("sru_scan", u, states, B, L, H)
     if ws is None:
-        need = lib().sru_scan_workspace_bytes(B, L, H, dt)
-        ws = _ws(need, dev) if need else None
-    _check(_c().sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, ws.numel() if ws is not None else 0, _stream()))
+        ws = _room("sru_scan_workspace_bytes", u, B, L, H, dt)
+    _check(c.sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, _bytes(ws), _stream()))
     return out
+
+
+def _check_states(who, u, states, B, L, H):
+    if states is None:
+        return
+    _c().expect(who, _device, u, "states", states, torch.float32, tuple(states.shape))
+    if states.numel() * 4 < _size("sru_scan_states_bytes", B, L, H):
+        raise ValueError(f"{who}: states are smaller than sru_scan_states_bytes")
 
 
 def sru_scan_backward(dh, u, states, x=None, b_f=None, b_r=None, dc_last=None, lengths=None, out=None, ws=None):
     """Gradient of sru_scan: dh [B,L,H] and dc_last f32[B,H] (None: zero), with the forward's inputs and states -> dict(du, dx (None
     without x), db_f, db_r f32[H], dc0 f32[B,H]).  With ``out``, db_f, db_r and dc0 may be None; dc0 may be dc_last."""
     B, L, H = dh.shape
-    if u.dim() != 3 or u.shape[:2] != dh.shape[:2]:
+    if u.dim() != 3:
         raise ValueError(f"sru_scan_backward: u {list(u.shape)} does not fit dh {list(dh.shape)}")
     n = _scan_blocks("sru_scan_backward", u, x, H)
-    dev, f32, t, dt = u.device, torch.float32, u.dtype, _dt(u)
-    o = out if out is not None else dict(
-        du=torch.empty_like(u), dx=torch.empty_like(x) if x is not None else None, db_f=torch.empty(H, dtype=f32, device=dev),
-        db_r=torch.empty(H, dtype=f32, device=dev), dc0=torch.empty(B, H, dtype=f32, device=dev))
-    if states.numel() * states.element_size() < lib().sru_scan_states_bytes(B, L, H):
-        raise ValueError("sru_scan_backward: states are smaller than sru_scan_states_bytes")
-    _expect("sru_scan_backward", dh, ("u", u, (B, L, n * H), dh.dtype), ("x", x, (B, L, H), t), ("b_f", b_f, (H,), f32), ("b_r", b_r, (H,), f32),
-            ("states", states, states.shape, f32), ("dc_last", dc_last, (B, H), f32), ("lengths", lengths, (B,), torch.int32),
-            ("du", o["du"], (B, L, n * H), t), ("dx", o["dx"], (B, L, H), t), ("db_f", o["db_f"], (H,), f32),
-            ("db_r", o["db_r"], (H,), f32), ("dc0", o["dc0"], (B, H), f32))
+    f32, t, dt, c = torch.float32, dh.dtype, _dt(dh), _c()
+    c.expect("sru_scan_backward", _device, dh, "u", u, t, (B, L, n * H), "x", x, t, (B, L, H), "b_f", b_f, f32, (H,), "b_r", b_r, f32, (H,),
+             "dc_last", dc_last, f32, (B, H), "lengths", lengths, torch.int32, (B,))
+    _check_states("sru_scan_backward", dh, states, B, L, H)
+    if out is None:
+        du, dx, db_f, db_r, dc0 = c.fresh(dh, t, (B, L, n * H), t if x is not None else None, (B, L, H), f32, (H,), f32, (H,), f32, (B, H))
+        out = dict(du=du, dx=dx, db_f=db_f, db_r=db_r, dc0=dc0)
+    else:
+        du, dx, db_f, db_r, dc0 = out["du"], out["dx"], out["db_f"], out["db_r"], out["dc0"]
+        c.expect("sru_scan_backward", _device, dh, "du", du, t, (B, L, n * H), "dx", dx, t, (B, L, H), "db_f", db_f, f32, (H,),
+                 "db_r", db_r, f32, (H,), "dc0", dc0, f32, (B, H))
     if ws is None:
-        need = lib().sru_scan_backward_workspace_bytes(B, L, H, dt)
-        ws = _ws(need, dev) if need else None
-    _check(_c().sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, o["du"], o["dx"], o["db_f"], o["db_r"],
-                                  o["dc0"], ws, ws.numel() if ws is not None else 0, _stream()))
-    return o
+        ws = _room("sru_scan_backward_workspace_bytes", dh, B, L, H, dt)
+    _check(c.sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, du, dx, db_f, db_r, dc0, ws, _bytes(ws), _stream()))
+    return out
 
 
 def _rows(t):
-    """(pointer-bearing tensor, row stride) of a matrix whose rows are contiguous; rows may lie further apart than they are long."""
+    """(tensor that begins where the rows do, row stride) of a matrix whose rows are contiguous; they may lie further apart than they are
+    long."""
     N, V = t.shape
     if t.is_contiguous() or N == 0:
         return t, V
@@ -637,36 +657,38 @@ def moe_token_logprobs(logits, target, k=0, out=None, ws=None):
     """logits [N,V] (rows contiguous, any distance apart), target int32[N] -> dict(logprob, entropy, lse f32[N], top_idx int32[N,k],
     top_logprob f32[N,k]).  A target outside [0,V) is a padded position: logprob 0.  Logits of -inf are masked."""
     N, V = logits.shape
-    dev, f32, dt = logits.device, torch.float32, _dt(logits)
-    o = out if out is not None else dict(
-        logprob=torch.empty(N, dtype=f32, device=dev), entropy=torch.empty(N, dtype=f32, device=dev),
-        lse=torch.empty(N, dtype=f32, device=dev), top_idx=torch.empty(N, k, dtype=torch.int32, device=dev),
-        top_logprob=torch.empty(N, k, dtype=f32, device=dev))
-    _expect("moe_token_logprobs", logits, ("target", target, (N,), torch.int32), ("logprob", o["logprob"], (N,), f32),
-            ("entropy", o["entropy"], (N,), f32), ("lse", o["lse"], (N,), f32),
-            *((("top_idx", o["top_idx"], (N, k), torch.int32), ("top_logprob", o["top_logprob"], (N, k), f32)) if k else ()))
+    f32, dt, c = torch.float32, _dt(logits), _c()
+    c.expect("moe_token_logprobs", _device, logits, "target", target, torch.int32, (N,))
+    if out is None:
+        logprob, entropy, lse, top_idx, top_logprob = c.fresh(logits, f32, (N,), f32, (N,), f32, (N,), torch.int32, (N, max(k, 0)),
+                                                              f32, (N, max(k, 0)))
+        out = dict(logprob=logprob, entropy=entropy, lse=lse, top_idx=top_idx, top_logprob=top_logprob)
+    else:
+        logprob, entropy, lse = out["logprob"], out["entropy"], out["lse"]
+        top_idx, top_logprob = (out["top_idx"], out["top_logprob"]) if k else (None, None)
+        c.expect("moe_token_logprobs", _device, logits, "logprob", logprob, f32, (N,), "entropy", entropy, f32, (N,), "lse", lse, f32, (N,),
+                 "top_idx", top_idx, torch.int32, (N, k), "top_logprob", top_logprob, f32, (N, k))
     rows, stride = _rows(logits)
     if ws is None:
-        need = lib().moe_token_logprobs_workspace_bytes(N, V, k, dt)
-        ws = _ws(need, dev) if need else None
-    _check(_c().moe_token_logprobs(rows, stride, target, N, V, dt, k, o["logprob"], o["entropy"], o["lse"], o["top_idx"] if k else None,
-                                   o["top_logprob"] if k else None, ws, ws.numel() if ws is not None else 0, _stream()))
-    return o
+        ws = _room("moe_token_logprobs_workspace_bytes", logits, N, V, k, dt)
+    _check(c.moe_token_logprobs(rows, stride, target, N, V, dt, k, logprob, entropy, lse, top_idx if k else None, top_logprob if k else None,
+                                ws, _bytes(ws), _stream()))
+    return out
 
 
 def moe_token_logprobs_backward(logits, target, lse, entropy, dlogprob, dentropy=None, out=None):
     """Gradient of moe_token_logprobs' logprob (dlogprob f32[N]) and entropy (dentropy f32[N] or None) with respect to the logits, with
     the forward's lse and entropy -> dlogits [N,V].  out may be logits."""
     N, V = logits.shape
-    f32, dt = torch.float32, _dt(logits)
-    dl = out if out is not None else torch.empty(N, V, dtype=logits.dtype, device=logits.device)
-    _expect("moe_token_logprobs_backward", logits, ("target", target, (N,), torch.int32), ("lse", lse, (N,), f32),
-            ("entropy", entropy, (N,), f32), ("dlogprob", dlogprob, (N,), f32), ("dentropy", dentropy, (N,), f32),
-            ("out", dl, (N, V), logits.dtype))
+    f32, t, dt, c = torch.float32, logits.dtype, _dt(logits), _c()
+    c.expect("moe_token_logprobs_backward", _device, logits, "target", target, torch.int32, (N,), "lse", lse, f32, (N,),
+             "entropy", entropy, f32, (N,), "dlogprob", dlogprob, f32, (N,), "dentropy", dentropy, f32, (N,), "out", out, t, (N, V))
+    if out is None:
+        out, = c.fresh(logits, t, (N, V))
     rows, stride = _rows(logits)
-    to, dstride = _rows(dl)
-    _check(_c().moe_token_logprobs_backward(rows, stride, target, lse, entropy, dlogprob, dentropy, N, V, dt, to, dstride, _stream()))
-    return dl
+    to, dstride = _rows(out)
+    _check(c.moe_token_logprobs_backward(rows, stride, target, lse, entropy, dlogprob, dentropy, N, V, dt, to, dstride, _stream()))
+    return out
 
 
 class MoeLayerTopK:

@@ -6,6 +6,8 @@
 // number, numpy's too (TypeError else).  The fields of a layer have to fit the struct's (OverflowError else); arguments of the other calls are
 // reduced to their parameter's width, as ctypes does.
 // Functions are typed by the C header and bound to the addresses of the library that binding.lib() has loaded and checked.
+#include <ATen/ops/empty.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
@@ -197,6 +199,110 @@ PyObject *py_moe_layer_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
     });
 }
 
+// expect(who, device, lead, name, tensor, dtype, sizes, ...): each tensor (None: left out) has that dtype and those sizes and lies where lead
+// does, which is the current device (device() asks for it).  ValueError else.  In Python these checks took 2 us a call.
+PyObject *py_expect(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n < 3 || (n - 3) % 4) {
+        PyErr_SetString(PyExc_TypeError, "expect takes who, device, lead and groups of name, tensor, dtype, sizes");
+        return nullptr;
+    }
+    try {
+        auto tensor = [&](PyObject *o, PyObject *name) -> const at::Tensor & {
+            if (!THPVariable_Check(o)) {
+                PyErr_Format(PyExc_TypeError, "%U: %U must be a tensor, not %s", args[0], name, Py_TYPE(o)->tp_name);
+                throw Failed();
+            }
+            return THPVariable_Unpack(o);
+        };
+        const at::Tensor &lead = tensor(args[2], args[0]);
+        if (!lead.is_cuda()) {
+            PyErr_SetString(PyExc_ValueError, "device-resident contiguous tensors only");
+            return nullptr;
+        }
+        PyObject *current = PyObject_CallNoArgs(args[1]);
+        if (!current) return nullptr;
+        const long here = PyLong_AsLong(current);
+        Py_DECREF(current);
+        if (here == -1 && PyErr_Occurred()) return nullptr;
+        if (lead.get_device() != here) {
+            PyErr_Format(PyExc_ValueError, "%U: tensors on device %d, the current device is %ld", args[0], (int)lead.get_device(), here);
+            return nullptr;
+        }
+        for (Py_ssize_t i = 3; i < n; i += 4) {
+            if (args[i + 1] == Py_None) continue;
+            const at::Tensor &t = tensor(args[i + 1], args[i]);
+            if (!THPDtype_Check(args[i + 2]) || !PyTuple_Check(args[i + 3])) {
+                PyErr_SetString(PyExc_TypeError, "expect: a dtype and a tuple of sizes");
+                return nullptr;
+            }
+            bool fits = t.scalar_type() == reinterpret_cast<THPDtype *>(args[i + 2])->scalar_type && t.dim() == PyTuple_GET_SIZE(args[i + 3]);
+            for (int64_t d = 0; fits && d < t.dim(); ++d) {
+                const long long want = PyLong_AsLongLong(PyTuple_GET_ITEM(args[i + 3], d));
+                if (want == -1 && PyErr_Occurred()) return nullptr;
+                fits = t.size(d) == want;
+            }
+            if (!fits) {
+                PyObject *sizes = PyObject_GetAttrString(args[i + 1], "shape"), *dtype = PyObject_GetAttrString(args[i + 1], "dtype");
+                if (sizes && dtype)
+                    PyErr_Format(PyExc_ValueError, "%U: %U must be %R of %S, not %R of %S", args[0], args[i], args[i + 3], args[i + 2], sizes, dtype);
+                Py_XDECREF(sizes);
+                Py_XDECREF(dtype);
+                return nullptr;
+            }
+            if (t.device() != lead.device()) {
+                PyErr_Format(PyExc_ValueError, "%U: %U is not on device %ld", args[0], args[i], here);
+                return nullptr;
+            }
+        }
+    } catch (const Failed &) {
+        return nullptr;
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    Py_RETURN_NONE;
+}
+
+// fresh(lead, dtype, sizes, ...) -> tuple of uninitialised tensors beside lead; a dtype of None: None in its place
+PyObject *py_fresh(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n < 1 || n % 2 == 0 || !THPVariable_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "fresh takes a tensor and pairs of dtype, sizes");
+        return nullptr;
+    }
+    PyObject *out = PyTuple_New((n - 1) / 2);
+    if (!out) return nullptr;
+    try {
+        const at::TensorOptions beside = at::TensorOptions().device(THPVariable_Unpack(args[0]).device());
+        for (Py_ssize_t i = 1; i < n; i += 2) {
+            if (args[i] == Py_None) {
+                Py_INCREF(Py_None);
+                PyTuple_SET_ITEM(out, i / 2, Py_None);
+                continue;
+            }
+            if (!THPDtype_Check(args[i]) || !PyTuple_Check(args[i + 1])) {
+                PyErr_SetString(PyExc_TypeError, "fresh: a dtype and a tuple of sizes");
+                throw Failed();
+            }
+            c10::SmallVector<int64_t, 4> sizes;
+            for (Py_ssize_t d = 0; d < PyTuple_GET_SIZE(args[i + 1]); ++d) {
+                sizes.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(args[i + 1], d)));
+                if (sizes.back() == -1 && PyErr_Occurred()) throw Failed();
+            }
+            PyObject *t = THPVariable_Wrap(at::empty(sizes, beside.dtype(reinterpret_cast<THPDtype *>(args[i])->scalar_type)));
+            if (!t) throw Failed();
+            PyTuple_SET_ITEM(out, i / 2, t);
+        }
+        return out;
+    } catch (const Failed &) {
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    Py_DECREF(out);
+    return nullptr;
+}
+
 // bind(name, address)
 PyObject *py_bind(PyObject *, PyObject *args)
 {
@@ -219,6 +325,8 @@ PyMethodDef methods[] = {
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))py_##NAME, METH_FASTCALL, nullptr},
     CALLS(METHOD) METHOD(moe_layer_forward)
 #undef METHOD
+    {"expect", (PyCFunction)(void (*)(void))py_expect, METH_FASTCALL, nullptr},
+    {"fresh", (PyCFunction)(void (*)(void))py_fresh, METH_FASTCALL, nullptr},
     {"bind", py_bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -11,25 +11,6 @@
 
 namespace moe {
 
-// V values of consecutive channels, as they lie in memory
-template <class T, int V> struct ScanRaw;
-template <> struct ScanRaw<bf16_t, 1> { typedef bf16_t type; };
-template <> struct ScanRaw<bf16_t, 2> { typedef uint32_t type; };
-template <> struct ScanRaw<float, 1> { typedef float type; };
-template <class T, int V> using scan_raw_t = typename ScanRaw<T, V>::type;
-
-__device__ __forceinline__ float scan_value(float r, int) { return r; }
-__device__ __forceinline__ float scan_value(bf16_t r, int) { return bf16_to_f32(r); }
-__device__ __forceinline__ float scan_value(uint32_t r, int v) { return __uint_as_float(v ? r & 0xffff0000u : r << 16); }
-
-template <class T, int V>
-__device__ __forceinline__ scan_raw_t<T, V> scan_pack(const float (&v)[V])
-{
-    if constexpr (sizeof(T) == 4) return v[0];
-    else if constexpr (V == 2) return pack_bf16x2(v[0], v[1]);
-    else return f32_to_bf16(v[0]);
-}
-
 // A run's rows of a tensor as a buffer: the lane's offset in a register, the step's in a scalar one (addresses of 64 bits for every step and
 // tensor spilled scalar registers into vector ones).  An offset from 2^31 on is outside: lanes without a channel ask for nothing and store nothing.
 constexpr unsigned SCAN_NOWHERE = 0x80000000u;
@@ -39,25 +20,24 @@ __device__ __forceinline__ scan_rows_t scan_rows(const void *first)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(first), 0, 0x7fffffff, 0x27000);
 }
-template <class R>
-__device__ __forceinline__ R scan_get(scan_rows_t rows, unsigned lane_at, unsigned step_at)
+template <class T>
+__device__ __forceinline__ T scan_get(scan_rows_t rows, unsigned lane_at, unsigned step_at)
 {
-    if constexpr (sizeof(R) == 2) return __builtin_amdgcn_raw_buffer_load_b16(rows, lane_at, step_at, 0);
-    else return __builtin_bit_cast(R, __builtin_amdgcn_raw_buffer_load_b32(rows, lane_at, step_at, 0));
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(rows, lane_at, step_at, 0);
+    else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(rows, lane_at, step_at, 0));
 }
-template <class R>
-__device__ __forceinline__ void scan_put(R v, scan_rows_t rows, unsigned lane_at, unsigned step_at)
+template <class T>
+__device__ __forceinline__ void scan_put(float v, scan_rows_t rows, unsigned lane_at, unsigned step_at)
 {
-    if constexpr (sizeof(R) == 2) __builtin_amdgcn_raw_buffer_store_b16(v, rows, lane_at, step_at, 0);
-    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), rows, lane_at, step_at, 0);
+    if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(f32_to_bf16(v), rows, lane_at, step_at, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rows, lane_at, step_at, 0);
 }
 
 // Where a workgroup stands: channels, sequence, segment.  Everything but the channel is the same for a whole wavefront.
-template <class T, int V>
+template <class T>
 struct ScanPlace {
-    typedef scan_raw_t<T, V> raw_t;
     int b, seg, lane, wave, waves, n, first, last;     // first .. last-1: the segment's steps
-    unsigned ch, col;                                  // this lane's first channel; one that exists
+    unsigned ch, col;                                  // this lane's channel; one that exists
     unsigned at, block;                                // its offset in a row of one block, and a block's length, in bytes
     bool on;
     __device__ __forceinline__ bool find(const ScanShape &g, const int32_t *lengths, int segments)
@@ -70,7 +50,7 @@ struct ScanPlace {
         lane = threadIdx.x % WAVE;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
         waves = blockDim.x / WAVE;
-        ch = ((wg - line * groups) * WAVE + lane) * V;
+        ch = (wg - line * groups) * WAVE + lane;
         on = ch < (unsigned)g.H;
         col = on ? ch : 0;
         at = on ? ch * (unsigned)sizeof(T) : SCAN_NOWHERE;
@@ -89,13 +69,13 @@ struct ScanPart { static constexpr bool FULL = false; };
 template <bool FULL> __device__ __forceinline__ bool scan_in(int i, int count) { return FULL || i < count; }
 
 // the steps of one column block, the first count of them
-template <class R, bool FULL>
-__device__ __forceinline__ void scan_load(R (&to)[SCAN_STEPS], scan_rows_t rows, unsigned lane_at, unsigned row_bytes, int count)
+template <class T, bool FULL>
+__device__ __forceinline__ void scan_load(T (&to)[SCAN_STEPS], scan_rows_t rows, unsigned lane_at, unsigned row_bytes, int count)
 {
 #pragma unroll
     for (int i = 0; i < SCAN_STEPS; ++i) {
         if (!FULL) to[i] = 0;
-        if (scan_in<FULL>(i, count)) to[i] = scan_get<R>(rows, lane_at, i * row_bytes);
+        if (scan_in<FULL>(i, count)) to[i] = scan_get<T>(rows, lane_at, i * row_bytes);
     }
 }
 
@@ -128,7 +108,7 @@ __device__ __forceinline__ float scan_fold(float c, const float2 *pairs, size_t 
     return c;
 }
 
-template <class T, int V, bool HIGHWAY>
+template <class T, bool HIGHWAY>
 __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShape g, const T *__restrict__ u, const T *__restrict__ x,
                                                                        const float *__restrict__ b_f, const float *__restrict__ b_r,
                                                                        const float *c0, const int32_t *__restrict__ lengths,
@@ -137,19 +117,13 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    typedef scan_raw_t<T, V> raw_t;
-    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE * V];
-    ScanPlace<T, V> p;
+    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE];
+    ScanPlace<T> p;
     if (!p.find(g, lengths, g.segments)) return;
     const size_t H = g.H, row_len = K * H;
-    float bf[V], br[V], c_in[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
-        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
-        c_in[v] = c0 ? c0[(size_t)p.b * H + p.col + v] : 0.f;
-        c_in[v] = scan_fold(c_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, p.seg);
-    }
+    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
+    float c_in = c0 ? c0[(size_t)p.b * H + p.col] : 0.f;
+    c_in = scan_fold(c_in, pairs + (size_t)p.b * (g.segments - 1) * H + p.col, H, p.seg);
     const int round = p.waves * SCAN_STEPS;
     for (int t = p.first, parity = 0; t < p.last; t += round, parity ^= 1) {
         const int t0 = t + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);    // this wavefront's steps inside the sequence
@@ -157,96 +131,74 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
             constexpr bool FULL = decltype(how)::FULL;
             const size_t row = (size_t)p.b * g.L + t0;
             const scan_rows_t ur = scan_rows(u + row * row_len), xr = HIGHWAY ? scan_rows(x + row * H) : ur, hr = scan_rows(h + row * H);
-            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
-            scan_load<raw_t, FULL>(z, ur, p.at, K * p.block, count);
-            scan_load<raw_t, FULL>(a, ur, p.at + p.block, K * p.block, count);
-            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, K * p.block, count);
-            if (HIGHWAY) scan_load<raw_t, FULL>(w, xr, p.at, p.block, count);
-            else scan_load<raw_t, FULL>(w, ur, p.at + 3 * p.block, K * p.block, count);
-            ScanForward<PRECISE> s[SCAN_STEPS][V];
-            float A[V], C[V], c[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) A[v] = 1.f, C[v] = 0.f;
+            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
+            scan_load<T, FULL>(z, ur, p.at, K * p.block, count);
+            scan_load<T, FULL>(a, ur, p.at + p.block, K * p.block, count);
+            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, K * p.block, count);
+            if (HIGHWAY) scan_load<T, FULL>(w, xr, p.at, p.block, count);
+            else scan_load<T, FULL>(w, ur, p.at + 3 * p.block, K * p.block, count);
+            ScanForward<PRECISE> s[SCAN_STEPS];
+            float A = 1.f, C = 0.f, c;
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    s[i][v].make(scan_value(a[i], v), bf[v], scan_value(z[i], v));
-                    A[v] *= s[i][v].f;
-                    C[v] = s[i][v].next(C[v]);
-                }
+                s[i].make(value_of(a[i]), bf, value_of(z[i]));
+                A *= s[i].f;
+                C = s[i].next(C);
             }
             if (p.waves > 1) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
+                sums[parity][p.wave][p.lane] = make_float2(A, C);
                 barrier_anywhere();                    // a full and a partial wavefront wait for each other here
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    c[v] = c_in[v];
-                    for (int j = 0; j < p.waves; ++j) {
-                        const float2 q = sums[parity][j][p.lane * V + v];
-                        c_in[v] = fmaf(q.x, c_in[v], q.y);
-                        if (j + 1 == p.wave) c[v] = c_in[v];
-                    }
+                c = c_in;
+                for (int j = 0; j < p.waves; ++j) {
+                    const float2 q = sums[parity][j][p.lane];
+                    c_in = fmaf(q.x, c_in, q.y);
+                    if (j + 1 == p.wave) c = c_in;
                 }
             } else {
-#pragma unroll
-                for (int v = 0; v < V; ++v) c[v] = c_in[v], c_in[v] = fmaf(A[v], c_in[v], C[v]);
+                c = c_in, c_in = fmaf(A, c_in, C);
             }
-            if (states && (FULL || t0 < g.L) && p.on) {
-                const size_t at = ((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch;
-#pragma unroll
-                for (int v = 0; v < V; ++v) states[at + v] = c[v];
-            }
+            if (states && (FULL || t0 < g.L) && p.on) states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch] = c;
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) {
-                    if (t0 + i < p.last) scan_put<raw_t>(0, hr, p.at, i * p.block);
+                    if (t0 + i < p.last) scan_put<T>(0.f, hr, p.at, i * p.block);
                     continue;
                 }
-                float out[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    c[v] = s[i][v].next(c[v]);
-                    const float wv = scan_value(w[i], v), t = tanh_of<PRECISE>(c[v]);
-                    if (PRECISE) {
-                        float on, rest;
-                        gate_of<true>(scan_value(r[i], v), br[v], on, rest);
-                        out[v] = fmaf(on, t, rest * wv);
-                    } else {
-                        out[v] = fmaf(gate_open<false>(scan_value(r[i], v), br[v]), t - wv, wv);
-                    }
+                c = s[i].next(c);
+                const float wv = value_of(w[i]), t = tanh_of<PRECISE>(c);
+                float out;
+                if (PRECISE) {
+                    float on, rest;
+                    gate_of<true>(value_of(r[i]), br, on, rest);
+                    out = fmaf(on, t, rest * wv);
+                } else {
+                    out = fmaf(gate_open<false>(value_of(r[i]), br), t - wv, wv);
                 }
-                scan_put<raw_t>(scan_pack<T, V>(out), hr, p.at, i * p.block);
+                scan_put<T>(out, hr, p.at, i * p.block);
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
         else steps(ScanPart());
     }
-    if (c_last && p.seg == g.segments - 1 && p.wave == 0 && p.on) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) c_last[(size_t)p.b * H + p.ch + v] = c_in[v];
-    }
+    if (c_last && p.seg == g.segments - 1 && p.wave == 0 && p.on) c_last[(size_t)p.b * H + p.ch] = c_in;
 }
 
 // The pairs of the first segments, [b][segment][channel]; a wavefront walks its own part of the segment from one end to the other.  Segment
 // 0 lays c0 down beside them: c_last may be c0, and the main launch's last segment writes it while others still read.
-template <class T, int V>
+template <class T>
 __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(ScanShape g, const T *__restrict__ u, int blocks,
                                                                              const float *__restrict__ b_f, const float *__restrict__ c0,
                                                                              const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
                                                                              float *__restrict__ c0_copy)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
-    typedef scan_raw_t<T, V> raw_t;
-    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE * V];
-    ScanPlace<T, V> p;
+    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE];
+    ScanPlace<T> p;
     if (!p.find(g, lengths, g.segments - 1)) return;
     const size_t H = g.H, row_len = blocks * H;
-    float bf[V], A[V], C[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f), A[v] = 1.f, C[v] = 0.f;
+    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f);
+    float A = 1.f, C = 0.f;
     const int part = g.seg_steps / p.waves, from = p.first + p.wave * part, to = from + part;     // whole runs: seg_steps is whole rounds
     for (int t0 = from; t0 < to; t0 += SCAN_STEPS) {
         const int count = min(p.n - t0, SCAN_STEPS);
@@ -254,38 +206,31 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(Sc
         const unsigned row_bytes = blocks * p.block;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            raw_t z[SCAN_STEPS], a[SCAN_STEPS];
-            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
+            T z[SCAN_STEPS], a[SCAN_STEPS];
+            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    ScanForward<PRECISE> s;
-                    s.make(scan_value(a[i], v), bf[v], scan_value(z[i], v));
-                    A[v] *= s.f;
-                    C[v] = s.next(C[v]);
-                }
+                ScanForward<PRECISE> s;
+                s.make(value_of(a[i]), bf, value_of(z[i]));
+                A *= s.f;
+                C = s.next(C);
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
         else steps(ScanPart());
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], C[v]);
+    sums[p.wave][p.lane] = make_float2(A, C);
     __syncthreads();
     if (p.wave != 0 || !p.on) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        for (int j = 1; j < p.waves; ++j) {
-            const float2 q = sums[j][p.lane * V + v];
-            C[v] = fmaf(q.x, C[v], q.y);
-            A[v] *= q.x;
-        }
-        pairs[((size_t)p.b * (g.segments - 1) + p.seg) * H + p.ch + v] = make_float2(A[v], C[v]);
-        if (p.seg == 0) c0_copy[(size_t)p.b * H + p.ch + v] = c0 ? c0[(size_t)p.b * H + p.ch + v] : 0.f;
+    for (int j = 1; j < p.waves; ++j) {
+        const float2 q = sums[j][p.lane];
+        C = fmaf(q.x, C, q.y);
+        A *= q.x;
     }
+    pairs[((size_t)p.b * (g.segments - 1) + p.seg) * H + p.ch] = make_float2(A, C);
+    if (p.seg == 0) c0_copy[(size_t)p.b * H + p.ch] = c0 ? c0[(size_t)p.b * H + p.ch] : 0.f;
 }
 
 // what a step of the gradient needs of the forward, from the state before it: e and the factors of the outputs
@@ -307,7 +252,7 @@ struct ScanStep {
     }
 };
 
-template <class T, int V, bool HIGHWAY>
+template <class T, bool HIGHWAY>
 __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel(
     ScanShape g, const T *__restrict__ dh, const float *dc_last, const T *__restrict__ u, const T *__restrict__ x, const float *__restrict__ b_f,
     const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, const float2 *__restrict__ pairs,
@@ -315,20 +260,13 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    typedef scan_raw_t<T, V> raw_t;
-    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE * V];
-    ScanPlace<T, V> p;
+    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE];
+    ScanPlace<T> p;
     if (!p.find(g, lengths, g.segments)) return;
     const size_t H = g.H, row_len = K * H;
-    float bf[V], br[V], d_in[V], sum_f[V], sum_r[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
-        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
-        d_in[v] = dc_last ? dc_last[(size_t)p.b * H + p.col + v] : 0.f;
-        d_in[v] = scan_fold(d_in[v], pairs + (size_t)p.b * (g.segments - 1) * H + p.col + v, H, g.segments - 1 - p.seg);
-        sum_f[v] = sum_r[v] = 0.f;
-    }
+    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
+    float sum_f = 0.f, sum_r = 0.f, d_in = dc_last ? dc_last[(size_t)p.b * H + p.col] : 0.f;
+    d_in = scan_fold(d_in, pairs + (size_t)p.b * (g.segments - 1) * H + p.col, H, g.segments - 1 - p.seg);
     const int round = p.waves * SCAN_STEPS, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
     for (int at = rounds - 1, parity = 0; at >= 0; --at, parity ^= 1) {
         const int t0 = p.first + at * round + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);
@@ -338,130 +276,93 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
         const unsigned at_w = HIGHWAY ? p.at : p.at + 3 * p.block, row_bytes = K * p.block, w_bytes = HIGHWAY ? p.block : row_bytes;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
-            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
-            scan_load<raw_t, FULL>(w, xr, at_w, w_bytes, count);
-            scan_load<raw_t, FULL>(d, dr, p.at, p.block, count);
-            float f[SCAN_STEPS][V], rest[SCAN_STEPS][V], e[SCAN_STEPS][V], gap[SCAN_STEPS][V], c[V], A[V], D[V], dc[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                c[v] = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v] : 0.f;
-                A[v] = 1.f, D[v] = 0.f;
-            }
+            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
+            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
+            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
+            scan_load<T, FULL>(w, xr, at_w, w_bytes, count);
+            scan_load<T, FULL>(d, dr, p.at, p.block, count);
+            float f[SCAN_STEPS], rest[SCAN_STEPS], e[SCAN_STEPS], gap[SCAN_STEPS], A = 1.f, D = 0.f, dc;
+            float c = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col] : 0.f;
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) {
                     if (t0 + i < p.last) {
-                        for (int k = 0; k < 3; ++k) scan_put<raw_t>(0, out, p.at + k * p.block, i * row_bytes);
-                        scan_put<raw_t>(0, out_w, at_w, i * w_bytes);
+                        for (int k = 0; k < 3; ++k) scan_put<T>(0.f, out, p.at + k * p.block, i * row_bytes);
+                        scan_put<T>(0.f, out_w, at_w, i * w_bytes);
                     }
                     continue;
                 }
-                float d_r[V], d_w[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    ScanStep<PRECISE> s;
-                    s.make(c[v], scan_value(z[i], v), scan_value(a[i], v), bf[v], scan_value(r[i], v), br[v], scan_value(w[i], v),
-                           scan_value(d[i], v));
-                    f[i][v] = s.f, rest[i][v] = s.rest, e[i][v] = s.e, gap[i][v] = s.gap;
-                    d_r[v] = s.d_r, d_w[v] = s.d_w;
-                    sum_r[v] += s.d_r;
-                }
-                scan_put<raw_t>(scan_pack<T, V>(d_r), out, p.at + 2 * p.block, i * row_bytes);
-                scan_put<raw_t>(scan_pack<T, V>(d_w), out_w, at_w, i * w_bytes);
+                ScanStep<PRECISE> s;
+                s.make(c, value_of(z[i]), value_of(a[i]), bf, value_of(r[i]), br, value_of(w[i]), value_of(d[i]));
+                f[i] = s.f, rest[i] = s.rest, e[i] = s.e, gap[i] = s.gap;
+                sum_r += s.d_r;
+                scan_put<T>(s.d_r, out, p.at + 2 * p.block, i * row_bytes);
+                scan_put<T>(s.d_w, out_w, at_w, i * w_bytes);
             }
 #pragma unroll
             for (int i = SCAN_STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    D[v] = (D[v] + e[i][v]) * f[i][v];
-                    A[v] *= f[i][v];
-                }
+                D = (D + e[i]) * f[i];
+                A *= f[i];
             }
             if (p.waves > 1) {
-#pragma unroll
-                for (int v = 0; v < V; ++v) sums[parity][p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
+                sums[parity][p.wave][p.lane] = make_float2(A, D);
                 barrier_anywhere();
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    dc[v] = d_in[v];
-                    for (int j = p.waves - 1; j >= 0; --j) {
-                        const float2 q = sums[parity][j][p.lane * V + v];
-                        d_in[v] = fmaf(q.x, d_in[v], q.y);
-                        if (j - 1 == p.wave) dc[v] = d_in[v];
-                    }
+                dc = d_in;
+                for (int j = p.waves - 1; j >= 0; --j) {
+                    const float2 q = sums[parity][j][p.lane];
+                    d_in = fmaf(q.x, d_in, q.y);
+                    if (j - 1 == p.wave) dc = d_in;
                 }
             } else {
-#pragma unroll
-                for (int v = 0; v < V; ++v) dc[v] = d_in[v], d_in[v] = fmaf(A[v], d_in[v], D[v]);
+                dc = d_in, d_in = fmaf(A, d_in, D);
             }
 #pragma unroll
             for (int i = SCAN_STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
-                float d_z[V], d_f[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float full = dc[v] + e[i][v];
-                    d_z[v] = full * rest[i][v];
-                    d_f[v] = full * gap[i][v];
-                    sum_f[v] += d_f[v];
-                    dc[v] = full * f[i][v];
-                }
-                scan_put<raw_t>(scan_pack<T, V>(d_z), out, p.at, i * row_bytes);
-                scan_put<raw_t>(scan_pack<T, V>(d_f), out, p.at + p.block, i * row_bytes);
+                const float full = dc + e[i], d_f = full * gap[i];
+                sum_f += d_f;
+                dc = full * f[i];
+                scan_put<T>(full * rest[i], out, p.at, i * row_bytes);
+                scan_put<T>(d_f, out, p.at + p.block, i * row_bytes);
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
         else steps(ScanPart());
     }
-    if (dc0 && p.seg == 0 && p.wave == 0 && p.on) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) dc0[(size_t)p.b * H + p.ch + v] = d_in[v];
-    }
+    if (dc0 && p.seg == 0 && p.wave == 0 && p.on) dc0[(size_t)p.b * H + p.ch] = d_in;
     if (!db) return;
     // the wavefronts' sums in their order, a row of [2 H] for each sequence and segment
     __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) sums[0][p.wave][p.lane * V + v] = make_float2(sum_f[v], sum_r[v]);
+    sums[0][p.wave][p.lane] = make_float2(sum_f, sum_r);
     __syncthreads();
     if (p.wave != 0 || !p.on) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        for (int j = 1; j < p.waves; ++j) {
-            const float2 q = sums[0][j][p.lane * V + v];
-            sum_f[v] += q.x;
-            sum_r[v] += q.y;
-        }
-        float *to = db + ((size_t)p.b * g.segments + p.seg) * 2 * H + p.ch + v;
-        to[0] = sum_f[v];
-        to[H] = sum_r[v];
+    for (int j = 1; j < p.waves; ++j) {
+        const float2 q = sums[0][j][p.lane];
+        sum_f += q.x;
+        sum_r += q.y;
     }
+    float *to = db + ((size_t)p.b * g.segments + p.seg) * 2 * H + p.ch;
+    to[0] = sum_f;
+    to[H] = sum_r;
 }
 
 // The gradient's pairs of the last segments, [b][segments-1-segment][channel] (the order they are met in), and dc_last beside them, as above.
-template <class T, int V>
+template <class T>
 __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_kernel(
     ScanShape g, const T *__restrict__ dh, const float *__restrict__ dc_last, const T *__restrict__ u, int blocks, const float *__restrict__ b_f,
     const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
     float *__restrict__ dc_copy)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
-    typedef scan_raw_t<T, V> raw_t;
-    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE * V];
-    ScanPlace<T, V> p;
+    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE];
+    ScanPlace<T> p;
     if (!p.find(g, lengths, g.segments - 1)) return;
     p.seg += 1, p.first += g.seg_steps;                // segment 0 has no one before it
     const size_t H = g.H, row_len = blocks * H;
-    float bf[V], br[V], A[V], D[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        bf[v] = gate_bias<PRECISE>(b_f ? b_f[p.col + v] : 0.f);
-        br[v] = gate_bias<PRECISE>(b_r ? b_r[p.col + v] : 0.f);
-        A[v] = 1.f, D[v] = 0.f;
-    }
+    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
+    float A = 1.f, D = 0.f;
     const int part = g.seg_steps / p.waves, from = p.first + p.wave * part;
     for (int t0 = from + part - SCAN_STEPS; t0 >= from; t0 -= SCAN_STEPS) {
         const int count = min(p.n - t0, SCAN_STEPS);
@@ -471,51 +372,39 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_
         const unsigned row_bytes = blocks * p.block;
         auto steps = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            raw_t z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<raw_t, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<raw_t, FULL>(a, ur, p.at + p.block, row_bytes, count);
-            scan_load<raw_t, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
-            scan_load<raw_t, FULL>(d, dr, p.at, p.block, count);
-            float f[SCAN_STEPS][V], e[SCAN_STEPS][V], c[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) c[v] = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col + v];
+            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
+            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
+            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
+            scan_load<T, FULL>(d, dr, p.at, p.block, count);
+            float f[SCAN_STEPS], e[SCAN_STEPS], c = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col];
 #pragma unroll
             for (int i = 0; i < SCAN_STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    ScanStep<PRECISE> s;
-                    s.make(c[v], scan_value(z[i], v), scan_value(a[i], v), bf[v], scan_value(r[i], v), br[v], 0.f, scan_value(d[i], v));
-                    f[i][v] = s.f, e[i][v] = s.e;
-                }
+                ScanStep<PRECISE> s;
+                s.make(c, value_of(z[i]), value_of(a[i]), bf, value_of(r[i]), br, 0.f, value_of(d[i]));
+                f[i] = s.f, e[i] = s.e;
             }
 #pragma unroll
             for (int i = SCAN_STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    D[v] = (D[v] + e[i][v]) * f[i][v];
-                    A[v] *= f[i][v];
-                }
+                D = (D + e[i]) * f[i];
+                A *= f[i];
             }
         };
         if (count >= SCAN_STEPS) steps(ScanFull());
         else steps(ScanPart());
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) sums[p.wave][p.lane * V + v] = make_float2(A[v], D[v]);
+    sums[p.wave][p.lane] = make_float2(A, D);
     __syncthreads();
     if (p.wave != p.waves - 1 || !p.on) return;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        for (int j = p.waves - 2; j >= 0; --j) {
-            const float2 q = sums[j][p.lane * V + v];
-            D[v] = fmaf(q.x, D[v], q.y);
-            A[v] *= q.x;
-        }
-        pairs[((size_t)p.b * (g.segments - 1) + (g.segments - 1 - p.seg)) * H + p.ch + v] = make_float2(A[v], D[v]);
-        if (p.seg == g.segments - 1) dc_copy[(size_t)p.b * H + p.ch + v] = dc_last ? dc_last[(size_t)p.b * H + p.ch + v] : 0.f;
+    for (int j = p.waves - 2; j >= 0; --j) {
+        const float2 q = sums[j][p.lane];
+        D = fmaf(q.x, D, q.y);
+        A *= q.x;
     }
+    pairs[((size_t)p.b * (g.segments - 1) + (g.segments - 1 - p.seg)) * H + p.ch] = make_float2(A, D);
+    if (p.seg == g.segments - 1) dc_copy[(size_t)p.b * H + p.ch] = dc_last ? dc_last[(size_t)p.b * H + p.ch] : 0.f;
 }
 
 // db_f and db_r: 64 channels per workgroup; its wavefronts take the parts' sums in turn, and are added in their order
@@ -576,22 +465,21 @@ extern "C" size_t sru_scan_states_bytes(int B, int L, int H)
 extern "C" size_t sru_scan_workspace_bytes(int B, int L, int H, int dtype)
 {
     if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
-    return scan_pairs_bytes(scan_shape(B, L, H, dtype));
+    return scan_pairs_bytes(scan_shape(B, L, H));
 }
 
 extern "C" size_t sru_scan_backward_workspace_bytes(int B, int L, int H, int dtype)
 {
     if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
-    const ScanShape g = scan_shape(B, L, H, dtype);
+    const ScanShape g = scan_shape(B, L, H);
     return scan_pairs_bytes(g) + (size_t)B * g.segments * 2 * H * sizeof(float);
 }
 
-// FORM(T, V): the builds for a type and a width
-#define MOE_SCAN_FORMS(FORM)                                    \
-    do {                                                        \
-        if (dtype == MOE_F32) FORM(float, 1);                   \
-        else if (scan_width(H, dtype) == 2) FORM(bf16_t, 2);    \
-        else FORM(bf16_t, 1);                                   \
+// FORM(T): the build for a type
+#define MOE_SCAN_FORMS(FORM)                    \
+    do {                                        \
+        if (dtype == MOE_F32) FORM(float);      \
+        else FORM(bf16_t);                      \
     } while (0)
 
 extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const float *b_r, const float *c0, const int32_t *lengths, int B,
@@ -604,7 +492,7 @@ extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const fl
         MOE_REQUIRE(h != u && h != x, MOE_ERR_INVALID_ARG, "sru_scan: h aliases an input");
         MOE_REQUIRE(aligned16(u) && aligned16(x) && aligned16(h) && aligned16(states), MOE_ERR_INVALID_ARG, "sru_scan: tensor misaligned");
     }
-    const ScanShape g = scan_shape(B, L, H, dtype);
+    const ScanShape g = scan_shape(B, L, H);
     const size_t need = scan_pairs_bytes(g);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "sru_scan: workspace of %zu bytes given, %zu needed",
                 ws ? ws_bytes : 0, need);
@@ -613,21 +501,21 @@ extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const fl
     const dim3 threads(g.waves * WAVE);
     if (g.segments > 1) {
         float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
-#define MOE_PAIRS(T, V)                                                                                                                        \
-    hipLaunchKernelGGL((sru_scan_pairs_kernel<T, V>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)u, n_blocks, b_f, c0, lengths, \
+#define MOE_PAIRS(T)                                                                                                                        \
+    hipLaunchKernelGGL((sru_scan_pairs_kernel<T>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)u, n_blocks, b_f, c0, lengths, \
                        pairs, copy)
         MOE_SCAN_FORMS(MOE_PAIRS);
 #undef MOE_PAIRS
         MOE_CHECK_LAUNCH("sru_scan");
         c0 = copy;
     }
-#define MOE_SCAN(T, V, HW)                                                                                                                 \
-    hipLaunchKernelGGL((sru_scan_kernel<T, V, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, \
+#define MOE_SCAN(T, HW)                                                                                                                 \
+    hipLaunchKernelGGL((sru_scan_kernel<T, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, \
                        pairs, (T *)h, c_last, (float *)states)
-#define MOE_MAIN(T, V)                              \
+#define MOE_MAIN(T)                              \
     do {                                            \
-        if (n_blocks == 3) MOE_SCAN(T, V, true);    \
-        else MOE_SCAN(T, V, false);                 \
+        if (n_blocks == 3) MOE_SCAN(T, true);    \
+        else MOE_SCAN(T, false);                 \
     } while (0)
     MOE_SCAN_FORMS(MOE_MAIN);
 #undef MOE_MAIN
@@ -654,28 +542,28 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
                 "sru_scan_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
     hipStream_t st = (hipStream_t)stream;
-    const ScanShape g = scan_shape(B, L, H, dtype);
+    const ScanShape g = scan_shape(B, L, H);
     float2 *pairs = (float2 *)ws;
     float *db = db_f || db_r ? (float *)((char *)ws + scan_pairs_bytes(g)) : nullptr;
     if (B > 0) {
         const dim3 threads(g.waves * WAVE);
         if (g.segments > 1) {
             float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
-#define MOE_PAIRS(T, V)                                                                                                                       \
-    hipLaunchKernelGGL((sru_scan_backward_pairs_kernel<T, V>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+#define MOE_PAIRS(T)                                                                                                                       \
+    hipLaunchKernelGGL((sru_scan_backward_pairs_kernel<T>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
                        n_blocks, b_f, b_r, (const float *)states, lengths, pairs, copy)
             MOE_SCAN_FORMS(MOE_PAIRS);
 #undef MOE_PAIRS
             MOE_CHECK_LAUNCH("sru_scan_backward");
             dc_last = copy;
         }
-#define MOE_SCAN(T, V, HW)                                                                                                                    \
-    hipLaunchKernelGGL((sru_scan_backward_kernel<T, V, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+#define MOE_SCAN(T, HW)                                                                                                                    \
+    hipLaunchKernelGGL((sru_scan_backward_kernel<T, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
                        (const T *)x, b_f, b_r, (const float *)states, lengths, pairs, (T *)du, (T *)dx, db, dc0)
-#define MOE_MAIN(T, V)                              \
+#define MOE_MAIN(T)                              \
     do {                                            \
-        if (n_blocks == 3) MOE_SCAN(T, V, true);    \
-        else MOE_SCAN(T, V, false);                 \
+        if (n_blocks == 3) MOE_SCAN(T, true);    \
+        else MOE_SCAN(T, false);                 \
     } while (0)
         MOE_SCAN_FORMS(MOE_MAIN);
 #undef MOE_MAIN

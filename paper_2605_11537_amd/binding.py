@@ -513,10 +513,10 @@ def _size(query, *args):
     return getattr(lib(), query)(*args)
 
 
-def _room(query, lead, *args):
-    """A fresh workspace beside lead, or None where none is needed."""
-    need = _size(query, *args)
-    return _c().fresh(lead, torch.uint8, (need,))[0] if need else None
+def _room(ws, query, *args):
+    """(dtype, sizes) of a workspace to make, (None, ()) where one is given or none is needed."""
+    need = 0 if ws is not None else _size(query, *args)
+    return (torch.uint8, (need,)) if need else (None, ())
 
 
 def _bytes(ws):
@@ -596,18 +596,18 @@ def sru_scan(u, x=None, b_f=None, b_r=None, c0=None, lengths=None, want_states=F
     f32, t, dt, c = torch.float32, u.dtype, _dt(u), _c()
     c.expect("sru_scan", _device, u, "x", x, t, (B, L, H), "b_f", b_f, f32, (H,), "b_r", b_r, f32, (H,), "c0", c0, f32, (B, H),
              "lengths", lengths, torch.int32, (B,))
+    room = _room(ws, "sru_scan_workspace_bytes", B, L, H, dt)
     if out is None:
         states = _size("sru_scan_states_bytes", B, L, H) // 4 if want_states else 0
-        out = c.fresh(u, t, (B, L, H), f32, (B, H), f32 if want_states else None, (states,))
-        h, c_last, states = out
+        h, c_last, states, made = c.fresh(u, t, (B, L, H), f32, (B, H), f32 if want_states else None, (states,), *room)
     else:
         h, c_last, states = out
         c.expect("sru_scan", _device, u, "h", h, t, (B, L, H), "c_last", c_last, f32, (B, H))
         _check_states("sru_scan", u, states, B, L, H)
-    if ws is None:
-        ws = _room("sru_scan_workspace_bytes", u, B, L, H, dt)
+        made, = c.fresh(u, *room)
+    ws = made if ws is None else ws
     _check(c.sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, _bytes(ws), _stream()))
-    return out
+    return h, c_last, states
 
 
 def _check_states(who, u, states, B, L, H):
@@ -629,15 +629,17 @@ def sru_scan_backward(dh, u, states, x=None, b_f=None, b_r=None, dc_last=None, l
     c.expect("sru_scan_backward", _device, dh, "u", u, t, (B, L, n * H), "x", x, t, (B, L, H), "b_f", b_f, f32, (H,), "b_r", b_r, f32, (H,),
              "dc_last", dc_last, f32, (B, H), "lengths", lengths, torch.int32, (B,))
     _check_states("sru_scan_backward", dh, states, B, L, H)
+    room = _room(ws, "sru_scan_backward_workspace_bytes", B, L, H, dt)
     if out is None:
-        du, dx, db_f, db_r, dc0 = c.fresh(dh, t, (B, L, n * H), t if x is not None else None, (B, L, H), f32, (H,), f32, (H,), f32, (B, H))
+        du, dx, db_f, db_r, dc0, made = c.fresh(dh, t, (B, L, n * H), t if x is not None else None, (B, L, H), f32, (H,), f32, (H,),
+                                                f32, (B, H), *room)
         out = dict(du=du, dx=dx, db_f=db_f, db_r=db_r, dc0=dc0)
     else:
         du, dx, db_f, db_r, dc0 = out["du"], out["dx"], out["db_f"], out["db_r"], out["dc0"]
         c.expect("sru_scan_backward", _device, dh, "du", du, t, (B, L, n * H), "dx", dx, t, (B, L, H), "db_f", db_f, f32, (H,),
                  "db_r", db_r, f32, (H,), "dc0", dc0, f32, (B, H))
-    if ws is None:
-        ws = _room("sru_scan_backward_workspace_bytes", dh, B, L, H, dt)
+        made, = c.fresh(dh, *room)
+    ws = made if ws is None else ws
     _check(c.sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, du, dx, db_f, db_r, dc0, ws, _bytes(ws), _stream()))
     return out
 
@@ -659,18 +661,19 @@ def moe_token_logprobs(logits, target, k=0, out=None, ws=None):
     N, V = logits.shape
     f32, dt, c = torch.float32, _dt(logits), _c()
     c.expect("moe_token_logprobs", _device, logits, "target", target, torch.int32, (N,))
+    room = _room(ws, "moe_token_logprobs_workspace_bytes", N, V, k, dt)
     if out is None:
-        logprob, entropy, lse, top_idx, top_logprob = c.fresh(logits, f32, (N,), f32, (N,), f32, (N,), torch.int32, (N, max(k, 0)),
-                                                              f32, (N, max(k, 0)))
+        logprob, entropy, lse, top_idx, top_logprob, made = c.fresh(logits, f32, (N,), f32, (N,), f32, (N,), torch.int32, (N, max(k, 0)),
+                                                                    f32, (N, max(k, 0)), *room)
         out = dict(logprob=logprob, entropy=entropy, lse=lse, top_idx=top_idx, top_logprob=top_logprob)
     else:
         logprob, entropy, lse = out["logprob"], out["entropy"], out["lse"]
         top_idx, top_logprob = (out["top_idx"], out["top_logprob"]) if k else (None, None)
         c.expect("moe_token_logprobs", _device, logits, "logprob", logprob, f32, (N,), "entropy", entropy, f32, (N,), "lse", lse, f32, (N,),
                  "top_idx", top_idx, torch.int32, (N, k), "top_logprob", top_logprob, f32, (N, k))
+        made, = c.fresh(logits, *room)
     rows, stride = _rows(logits)
-    if ws is None:
-        ws = _room("moe_token_logprobs_workspace_bytes", logits, N, V, k, dt)
+    ws = made if ws is None else ws
     _check(c.moe_token_logprobs(rows, stride, target, N, V, dt, k, logprob, entropy, lse, top_idx if k else None, top_logprob if k else None,
                                 ws, _bytes(ws), _stream()))
     return out

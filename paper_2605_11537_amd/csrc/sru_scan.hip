@@ -1,11 +1,11 @@
 // sru_scan and its gradient: the recurrence of an SRU layer over pre-activations that lie in memory.
 //
 // c_t = f_t c_{t-1} + b_t composes: a run of steps is a pair (A, C), c_out = A c_in + C, and the pair of two runs is (A2 A1, A2 C1 + C2).
-// The gradient dc_{t-1} = f_t (dc_t + e_t) is the same from the other end.  So a wavefront takes SCAN_STEPS steps of 64 lanes' channels with
+// The gradient dc_{t-1} = f_t (dc_t + e_t) is the same from the other end.  So a wavefront takes 8 or 16 steps of 64 lanes' channels with
 // everything they read in registers, finds its pair from zero, and learns its start from the pairs of the wavefronts before it, through
 // LDS: the wavefronts of a workgroup lie one behind the other on the sequence, and a round of them is read once and written once.
-// Where sequences and channels alone are too few for the card, the sequence is cut into segments for several workgroups, whose pairs a launch
-// before finds (it reads half of what the main one reads, again).
+// Where sequences and channels alone are too few for the card, every round of a sequence is a workgroup of its own (a tile), and the pairs go
+// from tile to tile through memory: see scan_look_back.
 #include "scalar_math.h"
 #include "sru_scan_rules.h"
 
@@ -33,47 +33,49 @@ __device__ __forceinline__ void scan_put(float v, scan_rows_t rows, unsigned lan
     else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rows, lane_at, step_at, 0);
 }
 
-// Where a workgroup stands: channels, sequence, segment.  Everything but the channel is the same for a whole wavefront.
+// Where a workgroup stands: channels, sequence, and for a tile which one.  Everything but the channel is the same for a whole wavefront.
 template <class T>
 struct ScanPlace {
-    int b, seg, lane, wave, waves, n, first, last;     // first .. last-1: the segment's steps
+    int b, tile, lane, wave, waves, n, first, last;    // first .. last-1: the workgroup's steps
     unsigned ch, col;                                  // this lane's channel; one that exists
     unsigned at, block;                                // its offset in a row of one block, and a block's length, in bytes
     bool on;
-    __device__ __forceinline__ bool find(const ScanShape &g, const int32_t *lengths, int segments)
+    template <bool TILES>
+    __device__ __forceinline__ void find(const ScanShape &g, const int32_t *lengths, unsigned line, int which)
     {
-        const unsigned wg = blockIdx.y * gridDim.x + blockIdx.x;
-        const unsigned groups = g.groups, line = wg / groups;
-        b = line / segments;
-        seg = line - (unsigned)b * segments;
-        if (b >= g.B) return false;
+        b = line / (unsigned)g.groups;
+        tile = which;
         lane = threadIdx.x % WAVE;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-        waves = blockDim.x / WAVE;
-        ch = (wg - line * groups) * WAVE + lane;
+        waves = g.waves;
+        ch = (line - b * (unsigned)g.groups) * WAVE + lane;
         on = ch < (unsigned)g.H;
         col = on ? ch : 0;
         at = on ? ch * (unsigned)sizeof(T) : SCAN_NOWHERE;
         block = g.H * (unsigned)sizeof(T);
         n = lengths ? min(max(lengths[b], 0), g.L) : g.L;
         n = __builtin_amdgcn_readfirstlane(n);
-        first = seg * g.seg_steps;
-        last = min(g.L, first + g.seg_steps);
-        return true;
+        first = TILES ? tile * waves * g.steps : 0;
+        last = TILES ? min(g.L, first + waves * g.steps) : g.L;
     }
 };
 
 // A wavefront's steps are all inside the sequence (FULL: no step is asked for), or some are not.
 struct ScanFull { static constexpr bool FULL = true; };
 struct ScanPart { static constexpr bool FULL = false; };
-template <bool FULL> __device__ __forceinline__ bool scan_in(int i, int count) { return FULL || i < count; }
+template <bool FULL>
+__device__ __forceinline__ bool scan_in(int i, int count)
+{
+    if (!FULL) asm("" : "+s"(count));                    // asked each time: sixteen answers kept would spill scalar registers
+    return FULL || i < count;
+}
 
 // the steps of one column block, the first count of them
-template <class T, bool FULL>
-__device__ __forceinline__ void scan_load(T (&to)[SCAN_STEPS], scan_rows_t rows, unsigned lane_at, unsigned row_bytes, int count)
+template <bool FULL, class T, int STEPS>
+__device__ __forceinline__ void scan_load(T (&to)[STEPS], scan_rows_t rows, unsigned lane_at, unsigned row_bytes, int count)
 {
 #pragma unroll
-    for (int i = 0; i < SCAN_STEPS; ++i) {
+    for (int i = 0; i < STEPS; ++i) {
         if (!FULL) to[i] = 0;
         if (scan_in<FULL>(i, count)) to[i] = scan_get<T>(rows, lane_at, i * row_bytes);
     }
@@ -97,70 +99,182 @@ struct ScanForward {
     __device__ __forceinline__ float next(float c) const { return PRECISE ? fmaf(f, c, in) : fmaf(f, c - in, in); }
 };
 
-// the state that a pair list before this place leads to
-__device__ __forceinline__ float scan_fold(float c, const float2 *pairs, size_t step, int count)
-{
-#pragma unroll 16
-    for (int j = 0; j < count; ++j) {
-        const float2 p = pairs[j * step];
-        c = fmaf(p.x, c, p.y);
+// what leads from the state before a run to the state behind two runs
+__device__ __forceinline__ float2 scan_then(float2 a, float2 b) { return make_float2(b.x * a.x, fmaf(b.x, a.y, b.y)); }
+__device__ __forceinline__ float scan_through(float2 a, float c) { return fmaf(a.x, c, a.y); }
+
+// Pairs of tiles in memory.  A pair is one word of 64 bits, written and read whole by atomic operations of device scope (the eight L2 caches do
+// not see each other's ordinary writes), and SCAN_UNKNOWN until then: the word is its own flag, so no order between two words is relied on.
+// A workgroup draws its tile with a ticket, tile 0 of all chains first, and waits only for tiles whose tickets were drawn before its own: their
+// workgroups run already, and publish their own pair before they wait themselves.  So the tile of the lowest unfinished ticket waits for no one,
+// and every wait ends.  (A wait gives up after SCAN_PATIENCE looks, some seconds, and makes its outputs NaN: that takes a card that does not run
+// what it has begun.)
+// To find its start a tile takes the pairs of the tiles before it in its run of SCAN_RUN, the pairs of the whole runs before that one in its
+// stretch of SCAN_RUN runs, and the state at the stretch's start: at most 15 + 15 + 1 words a channel however long the sequence, all in flight at
+// once, and always folded in the same order.
+struct ScanChain {
+    unsigned long long *tiles, *runs, *stretches;       // of this chain, [place][lane]
+    __device__ __forceinline__ void find(const ScanShape &g, unsigned long long *words, unsigned line)
+    {
+        const size_t runs_of = g.runs, stretches_of = g.stretches, chains = (size_t)g.B * g.groups;
+        tiles = words + (size_t)line * g.tiles * WAVE;
+        runs = words + (chains * g.tiles + line * runs_of) * WAVE;
+        stretches = words + (chains * (g.tiles + runs_of) + line * stretches_of) * WAVE;
     }
-    return c;
+};
+
+__device__ __forceinline__ void scan_publish(unsigned long long *word, float2 pair)
+{
+    unsigned long long v = __builtin_bit_cast(unsigned long long, pair);
+    if (v == SCAN_UNKNOWN) v = 0x7fc000007fc00000ull;    // two NaNs of that very pattern: two other NaNs
+    __hip_atomic_store(word, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long scan_look(const unsigned long long *word)
+{
+    return __hip_atomic_load(word, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 scan_await(const unsigned long long *word, unsigned long long v)
+{
+    for (int i = 0; i < SCAN_PATIENCE && __any(v == SCAN_UNKNOWN); ++i) {
+        __builtin_amdgcn_s_sleep(1);
+        v = scan_look(word);
+    }
+    return __builtin_bit_cast(float2, v);                // what never came is two NaNs
+}
+// the pairs of up to two neighbours, the first count of them
+__device__ __forceinline__ float2 scan_await_two(const unsigned long long *words, unsigned long long v0, unsigned long long v1, int count)
+{
+    float2 a = make_float2(1.f, 0.f);
+    if (count > 0) a = scan_await(words, v0);
+    if (count > 1) a = scan_then(a, scan_await(words + WAVE, v1));
+    return a;
 }
 
-template <class T, bool HIGHWAY>
-__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShape g, const T *__restrict__ u, const T *__restrict__ x,
+// The state at the start of the tile at `at` (its place in the order of the recurrence), from the sequence's own start and the tile's pair, which
+// every wavefront knows.  Each wavefront looks for two tiles and two runs.
+__device__ float scan_look_back(const ScanChain &chain, int tiles, int at, int lane, int wave, float2 own, float start,
+                                float2 (*of_tiles)[WAVE], float2 (*of_runs)[WAVE])
+{
+    const int run = at / SCAN_RUN, in_run = at % SCAN_RUN, stretch = run / SCAN_RUN, in_stretch = run % SCAN_RUN;
+    const bool last = at + 1 == tiles;
+    if (wave == 0 && !last && in_run + 1 < SCAN_RUN) scan_publish(chain.tiles + (size_t)at * WAVE + lane, own);
+    const unsigned long long *t = chain.tiles + ((size_t)run * SCAN_RUN + 2 * wave) * WAVE + lane;
+    const unsigned long long *r = chain.runs + ((size_t)stretch * SCAN_RUN + 2 * wave) * WAVE + lane;
+    const unsigned long long *s = chain.stretches + (size_t)(stretch > 0 ? stretch - 1 : 0) * WAVE + lane;
+    const int n_t = min(max(in_run - 2 * wave, 0), 2), n_r = min(max(in_stretch - 2 * wave, 0), 2);
+    unsigned long long t0 = 0, t1 = 0, r0 = 0, r1 = 0, s0 = 0;
+    if (n_t > 0) t0 = scan_look(t);
+    if (n_t > 1) t1 = scan_look(t + WAVE);
+    if (n_r > 0) r0 = scan_look(r);
+    if (n_r > 1) r1 = scan_look(r + WAVE);
+    if (stretch > 0) s0 = scan_look(s);
+    of_tiles[wave][lane] = scan_await_two(t, t0, t1, n_t);
+    __syncthreads();
+    float2 before = make_float2(1.f, 0.f);
+    for (int w = 0; w < SCAN_MAX_WAVES; ++w) before = scan_then(before, of_tiles[w][lane]);
+    const float2 whole = scan_then(before, own);         // a run's pair needs no other run's, and is out before one is waited for
+    const bool ends = !last && in_run + 1 == SCAN_RUN, ends_stretch = ends && in_stretch + 1 == SCAN_RUN;
+    if (wave == 0 && ends && !ends_stretch) scan_publish(chain.runs + (size_t)run * WAVE + lane, whole);
+    of_runs[wave][lane] = scan_await_two(r, r0, r1, n_r);
+    float c = stretch > 0 ? scan_await(s, s0).y : start;
+    __syncthreads();
+    for (int w = 0; w < SCAN_MAX_WAVES; ++w) c = scan_through(of_runs[w][lane], c);
+    if (wave == 0 && ends_stretch) scan_publish(chain.stretches + (size_t)stretch * WAVE + lane, make_float2(0.f, scan_through(whole, c)));
+    return scan_through(before, c);
+}
+
+// Before the tiles: every word unknown, no ticket drawn; the state at the start beside them, since c_last may be c0 and is written while others
+// still read.
+__global__ __launch_bounds__(SCAN_CLEAR_THREADS) void sru_scan_clear_kernel(unsigned long long *__restrict__ words, size_t count,
+                                                                            const float *__restrict__ start, float *__restrict__ copy, size_t channels,
+                                                                            unsigned *__restrict__ ticket, unsigned blocks)
+{
+    const size_t first = (size_t)blockIdx.x * SCAN_CLEAR_THREADS + threadIdx.x, step = (size_t)blocks * SCAN_CLEAR_THREADS;
+    for (size_t i = first; i < count; i += step) words[i] = SCAN_UNKNOWN;
+    for (size_t i = first; i < channels; i += step) copy[i] = start ? start[i] : 0.f;
+    if (first == 0) *ticket = 0;
+}
+
+// the workgroup's line (sequence and channels) and, with tiles, its place in the chain
+template <bool TILES>
+__device__ __forceinline__ bool scan_draw(const ScanShape &g, unsigned *ticket, unsigned *drawn, unsigned &line, int &at)
+{
+    const unsigned lines = (unsigned)g.B * g.groups;
+    if (!TILES) {
+        line = blockIdx.y * g.across + blockIdx.x, at = 0;
+        return line < lines;
+    }
+    if (threadIdx.x == 0) *drawn = atomicAdd(ticket, 1u);
+    __syncthreads();
+    const unsigned t = __builtin_amdgcn_readfirstlane(*drawn);
+    at = t / lines;
+    line = t - at * lines;
+    return at < g.tiles;
+}
+
+template <class T, bool HIGHWAY, bool TILES, int STEPS>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanShape g, const T *__restrict__ u, const T *__restrict__ x,
                                                                        const float *__restrict__ b_f, const float *__restrict__ b_r,
                                                                        const float *c0, const int32_t *__restrict__ lengths,
-                                                                       const float2 *__restrict__ pairs, T *__restrict__ h, float *c_last,
-                                                                       float *__restrict__ states)
+                                                                       unsigned *ticket, unsigned long long *words, T *__restrict__ h,
+                                                                       float *c_last, float *__restrict__ states)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE];
+    __shared__ float2 sums[3][SCAN_MAX_WAVES][WAVE];
+    __shared__ unsigned drawn;
+    unsigned line;
+    int at;
+    if (!scan_draw<TILES>(g, ticket, &drawn, line, at)) return;
     ScanPlace<T> p;
-    if (!p.find(g, lengths, g.segments)) return;
+    p.template find<TILES>(g, lengths, line, at);
+    ScanChain chain;
+    if (TILES) chain.find(g, words, line);
     const size_t H = g.H, row_len = K * H;
     const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
     float c_in = c0 ? c0[(size_t)p.b * H + p.col] : 0.f;
-    c_in = scan_fold(c_in, pairs + (size_t)p.b * (g.segments - 1) * H + p.col, H, p.seg);
-    const int round = p.waves * SCAN_STEPS;
+    const int round = p.waves * STEPS;
     for (int t = p.first, parity = 0; t < p.last; t += round, parity ^= 1) {
-        const int t0 = t + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);    // this wavefront's steps inside the sequence
-        auto steps = [&](auto how) {
+        const int t0 = t + p.wave * STEPS, count = min(p.n - t0, STEPS);    // this wavefront's steps inside the sequence
+        const size_t row = (size_t)p.b * g.L + t0;
+        T z[STEPS], a[STEPS], r[STEPS], w[STEPS];
+        ScanForward<PRECISE> s[STEPS];
+        float A = 1.f, C = 0.f;
+        auto gates = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            const size_t row = (size_t)p.b * g.L + t0;
-            const scan_rows_t ur = scan_rows(u + row * row_len), xr = HIGHWAY ? scan_rows(x + row * H) : ur, hr = scan_rows(h + row * H);
-            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS];
-            scan_load<T, FULL>(z, ur, p.at, K * p.block, count);
-            scan_load<T, FULL>(a, ur, p.at + p.block, K * p.block, count);
-            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, K * p.block, count);
-            if (HIGHWAY) scan_load<T, FULL>(w, xr, p.at, p.block, count);
-            else scan_load<T, FULL>(w, ur, p.at + 3 * p.block, K * p.block, count);
-            ScanForward<PRECISE> s[SCAN_STEPS];
-            float A = 1.f, C = 0.f, c;
+            const scan_rows_t ur = scan_rows(u + row * row_len), xr = HIGHWAY ? scan_rows(x + row * H) : ur;
+            scan_load<FULL>(z, ur, p.at, K * p.block, count);
+            scan_load<FULL>(a, ur, p.at + p.block, K * p.block, count);
+            scan_load<FULL>(r, ur, p.at + 2 * p.block, K * p.block, count);
+            if (HIGHWAY) scan_load<FULL>(w, xr, p.at, p.block, count);
+            else scan_load<FULL>(w, ur, p.at + 3 * p.block, K * p.block, count);
 #pragma unroll
-            for (int i = 0; i < SCAN_STEPS; ++i) {
+            for (int i = 0; i < STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 s[i].make(value_of(a[i]), bf, value_of(z[i]));
                 A *= s[i].f;
                 C = s[i].next(C);
             }
-            if (p.waves > 1) {
-                sums[parity][p.wave][p.lane] = make_float2(A, C);
-                barrier_anywhere();                    // a full and a partial wavefront wait for each other here
-                c = c_in;
-                for (int j = 0; j < p.waves; ++j) {
-                    const float2 q = sums[parity][j][p.lane];
-                    c_in = fmaf(q.x, c_in, q.y);
-                    if (j + 1 == p.wave) c = c_in;
-                }
-            } else {
-                c = c_in, c_in = fmaf(A, c_in, C);
-            }
-            if (states && (FULL || t0 < g.L) && p.on) states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.ch] = c;
+        };
+        if (count >= STEPS) gates(ScanFull());
+        else gates(ScanPart());
+        sums[parity][p.wave][p.lane] = make_float2(A, C);
+        __syncthreads();
+        float2 all = make_float2(1.f, 0.f), before = all;
+        for (int j = 0; j < p.waves; ++j) {
+            if (j == p.wave) before = all;
+            all = scan_then(all, sums[parity][j][p.lane]);
+        }
+        if (TILES) c_in = scan_look_back(chain, g.tiles, at, p.lane, p.wave, all, c_in, sums[1], sums[2]);
+        float c = scan_through(before, c_in);
+        c_in = scan_through(all, c_in);
+        auto outputs = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
+            const scan_rows_t hr = scan_rows(h + row * H);
 #pragma unroll
-            for (int i = 0; i < SCAN_STEPS; ++i) {
+            for (int i = 0; i < STEPS; ++i) {
+                if (i % SCAN_SAVED == 0 && states && (FULL || t0 + i < g.L) && p.on)
+                    states[((size_t)p.b * g.saved + (t0 + i) / SCAN_SAVED) * H + p.ch] = c;
                 if (!scan_in<FULL>(i, count)) {
                     if (t0 + i < p.last) scan_put<T>(0.f, hr, p.at, i * p.block);
                     continue;
@@ -178,59 +292,10 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_kernel(ScanShap
                 scan_put<T>(out, hr, p.at, i * p.block);
             }
         };
-        if (count >= SCAN_STEPS) steps(ScanFull());
-        else steps(ScanPart());
+        if (count >= STEPS) outputs(ScanFull());
+        else outputs(ScanPart());
     }
-    if (c_last && p.seg == g.segments - 1 && p.wave == 0 && p.on) c_last[(size_t)p.b * H + p.ch] = c_in;
-}
-
-// The pairs of the first segments, [b][segment][channel]; a wavefront walks its own part of the segment from one end to the other.  Segment
-// 0 lays c0 down beside them: c_last may be c0, and the main launch's last segment writes it while others still read.
-template <class T>
-__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_pairs_kernel(ScanShape g, const T *__restrict__ u, int blocks,
-                                                                             const float *__restrict__ b_f, const float *__restrict__ c0,
-                                                                             const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
-                                                                             float *__restrict__ c0_copy)
-{
-    constexpr bool PRECISE = sizeof(T) == 4;
-    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE];
-    ScanPlace<T> p;
-    if (!p.find(g, lengths, g.segments - 1)) return;
-    const size_t H = g.H, row_len = blocks * H;
-    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f);
-    float A = 1.f, C = 0.f;
-    const int part = g.seg_steps / p.waves, from = p.first + p.wave * part, to = from + part;     // whole runs: seg_steps is whole rounds
-    for (int t0 = from; t0 < to; t0 += SCAN_STEPS) {
-        const int count = min(p.n - t0, SCAN_STEPS);
-        const scan_rows_t ur = scan_rows(u + ((size_t)p.b * g.L + t0) * row_len);
-        const unsigned row_bytes = blocks * p.block;
-        auto steps = [&](auto how) {
-            constexpr bool FULL = decltype(how)::FULL;
-            T z[SCAN_STEPS], a[SCAN_STEPS];
-            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
-#pragma unroll
-            for (int i = 0; i < SCAN_STEPS; ++i) {
-                if (!scan_in<FULL>(i, count)) continue;
-                ScanForward<PRECISE> s;
-                s.make(value_of(a[i]), bf, value_of(z[i]));
-                A *= s.f;
-                C = s.next(C);
-            }
-        };
-        if (count >= SCAN_STEPS) steps(ScanFull());
-        else steps(ScanPart());
-    }
-    sums[p.wave][p.lane] = make_float2(A, C);
-    __syncthreads();
-    if (p.wave != 0 || !p.on) return;
-    for (int j = 1; j < p.waves; ++j) {
-        const float2 q = sums[j][p.lane];
-        C = fmaf(q.x, C, q.y);
-        A *= q.x;
-    }
-    pairs[((size_t)p.b * (g.segments - 1) + p.seg) * H + p.ch] = make_float2(A, C);
-    if (p.seg == 0) c0_copy[(size_t)p.b * H + p.ch] = c0 ? c0[(size_t)p.b * H + p.ch] : 0.f;
+    if (c_last && p.tile == g.tiles - 1 && p.wave == 0 && p.on) c_last[(size_t)p.b * H + p.ch] = c_in;
 }
 
 // what a step of the gradient needs of the forward, from the state before it: e and the factors of the outputs
@@ -252,40 +317,45 @@ struct ScanStep {
     }
 };
 
-template <class T, bool HIGHWAY>
-__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel(
+template <class T, bool HIGHWAY, bool TILES>
+__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_kernel(
     ScanShape g, const T *__restrict__ dh, const float *dc_last, const T *__restrict__ u, const T *__restrict__ x, const float *__restrict__ b_f,
-    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, const float2 *__restrict__ pairs,
-    T *__restrict__ du, T *__restrict__ dx, float *__restrict__ db, float *dc0)
+    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, unsigned *ticket,
+    unsigned long long *words, T *__restrict__ du, T *__restrict__ dx, float *__restrict__ db, float *dc0)
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    __shared__ float2 sums[2][SCAN_MAX_WAVES][WAVE];
+    __shared__ float2 sums[3][SCAN_MAX_WAVES][WAVE];
+    __shared__ unsigned drawn;
+    unsigned line;
+    int at;
+    if (!scan_draw<TILES>(g, ticket, &drawn, line, at)) return;
     ScanPlace<T> p;
-    if (!p.find(g, lengths, g.segments)) return;
+    p.template find<TILES>(g, lengths, line, g.tiles - 1 - at);
+    ScanChain chain;
+    if (TILES) chain.find(g, words, line);
     const size_t H = g.H, row_len = K * H;
     const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
     float sum_f = 0.f, sum_r = 0.f, d_in = dc_last ? dc_last[(size_t)p.b * H + p.col] : 0.f;
-    d_in = scan_fold(d_in, pairs + (size_t)p.b * (g.segments - 1) * H + p.col, H, g.segments - 1 - p.seg);
-    const int round = p.waves * SCAN_STEPS, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
-    for (int at = rounds - 1, parity = 0; at >= 0; --at, parity ^= 1) {
-        const int t0 = p.first + at * round + p.wave * SCAN_STEPS, count = min(p.n - t0, SCAN_STEPS);
+    const int round = p.waves * SCAN_SAVED, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
+    for (int back = rounds - 1, parity = 0; back >= 0; --back, parity ^= 1) {
+        const int t0 = p.first + back * round + p.wave * SCAN_SAVED, count = min(p.n - t0, SCAN_SAVED);
         const size_t row = (size_t)p.b * g.L + t0;
         const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H), out = scan_rows(du + row * row_len);
         const scan_rows_t xr = HIGHWAY ? scan_rows(x + row * H) : ur, out_w = HIGHWAY ? scan_rows(dx + row * H) : out;
         const unsigned at_w = HIGHWAY ? p.at : p.at + 3 * p.block, row_bytes = K * p.block, w_bytes = HIGHWAY ? p.block : row_bytes;
-        auto steps = [&](auto how) {
+        float f[SCAN_SAVED], rest[SCAN_SAVED], e[SCAN_SAVED], gap[SCAN_SAVED], A = 1.f, D = 0.f;
+        auto forward = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], w[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
-            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
-            scan_load<T, FULL>(w, xr, at_w, w_bytes, count);
-            scan_load<T, FULL>(d, dr, p.at, p.block, count);
-            float f[SCAN_STEPS], rest[SCAN_STEPS], e[SCAN_STEPS], gap[SCAN_STEPS], A = 1.f, D = 0.f, dc;
-            float c = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col] : 0.f;
+            T z[SCAN_SAVED], a[SCAN_SAVED], r[SCAN_SAVED], w[SCAN_SAVED], d[SCAN_SAVED];
+            scan_load<FULL>(z, ur, p.at, row_bytes, count);
+            scan_load<FULL>(a, ur, p.at + p.block, row_bytes, count);
+            scan_load<FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
+            scan_load<FULL>(w, xr, at_w, w_bytes, count);
+            scan_load<FULL>(d, dr, p.at, p.block, count);
+            float c = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_SAVED) * H + p.col] : 0.f;
 #pragma unroll
-            for (int i = 0; i < SCAN_STEPS; ++i) {
+            for (int i = 0; i < SCAN_SAVED; ++i) {
                 if (!scan_in<FULL>(i, count)) {
                     if (t0 + i < p.last) {
                         for (int k = 0; k < 3; ++k) scan_put<T>(0.f, out, p.at + k * p.block, i * row_bytes);
@@ -301,25 +371,28 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
                 scan_put<T>(s.d_w, out_w, at_w, i * w_bytes);
             }
 #pragma unroll
-            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+            for (int i = SCAN_SAVED - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 D = (D + e[i]) * f[i];
                 A *= f[i];
             }
-            if (p.waves > 1) {
-                sums[parity][p.wave][p.lane] = make_float2(A, D);
-                barrier_anywhere();
-                dc = d_in;
-                for (int j = p.waves - 1; j >= 0; --j) {
-                    const float2 q = sums[parity][j][p.lane];
-                    d_in = fmaf(q.x, d_in, q.y);
-                    if (j - 1 == p.wave) dc = d_in;
-                }
-            } else {
-                dc = d_in, d_in = fmaf(A, d_in, D);
-            }
+        };
+        if (count >= SCAN_SAVED) forward(ScanFull());
+        else forward(ScanPart());
+        sums[parity][p.wave][p.lane] = make_float2(A, D);
+        __syncthreads();
+        float2 all = make_float2(1.f, 0.f), before = all;
+        for (int j = p.waves - 1; j >= 0; --j) {
+            if (j == p.wave) before = all;
+            all = scan_then(all, sums[parity][j][p.lane]);
+        }
+        if (TILES) d_in = scan_look_back(chain, g.tiles, at, p.lane, p.wave, all, d_in, sums[1], sums[2]);
+        float dc = scan_through(before, d_in);
+        d_in = scan_through(all, d_in);
+        auto backward = [&](auto how) {
+            constexpr bool FULL = decltype(how)::FULL;
 #pragma unroll
-            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
+            for (int i = SCAN_SAVED - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 const float full = dc + e[i], d_f = full * gap[i];
                 sum_f += d_f;
@@ -328,12 +401,12 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
                 scan_put<T>(d_f, out, p.at + p.block, i * row_bytes);
             }
         };
-        if (count >= SCAN_STEPS) steps(ScanFull());
-        else steps(ScanPart());
+        if (count >= SCAN_SAVED) backward(ScanFull());
+        else backward(ScanPart());
     }
-    if (dc0 && p.seg == 0 && p.wave == 0 && p.on) dc0[(size_t)p.b * H + p.ch] = d_in;
+    if (dc0 && p.tile == 0 && p.wave == 0 && p.on) dc0[(size_t)p.b * H + p.ch] = d_in;
     if (!db) return;
-    // the wavefronts' sums in their order, a row of [2 H] for each sequence and segment
+    // the wavefronts' sums in their order, a row of [2 H] for each sequence and tile
     __syncthreads();
     sums[0][p.wave][p.lane] = make_float2(sum_f, sum_r);
     __syncthreads();
@@ -343,68 +416,9 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_kernel
         sum_f += q.x;
         sum_r += q.y;
     }
-    float *to = db + ((size_t)p.b * g.segments + p.seg) * 2 * H + p.ch;
+    float *to = db + ((size_t)p.b * g.tiles + p.tile) * 2 * H + p.ch;
     to[0] = sum_f;
     to[H] = sum_r;
-}
-
-// The gradient's pairs of the last segments, [b][segments-1-segment][channel] (the order they are met in), and dc_last beside them, as above.
-template <class T>
-__global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE) void sru_scan_backward_pairs_kernel(
-    ScanShape g, const T *__restrict__ dh, const float *__restrict__ dc_last, const T *__restrict__ u, int blocks, const float *__restrict__ b_f,
-    const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, float2 *__restrict__ pairs,
-    float *__restrict__ dc_copy)
-{
-    constexpr bool PRECISE = sizeof(T) == 4;
-    __shared__ float2 sums[SCAN_MAX_WAVES][WAVE];
-    ScanPlace<T> p;
-    if (!p.find(g, lengths, g.segments - 1)) return;
-    p.seg += 1, p.first += g.seg_steps;                // segment 0 has no one before it
-    const size_t H = g.H, row_len = blocks * H;
-    const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
-    float A = 1.f, D = 0.f;
-    const int part = g.seg_steps / p.waves, from = p.first + p.wave * part;
-    for (int t0 = from + part - SCAN_STEPS; t0 >= from; t0 -= SCAN_STEPS) {
-        const int count = min(p.n - t0, SCAN_STEPS);
-        if (count <= 0) continue;
-        const size_t row = (size_t)p.b * g.L + t0;
-        const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H);
-        const unsigned row_bytes = blocks * p.block;
-        auto steps = [&](auto how) {
-            constexpr bool FULL = decltype(how)::FULL;
-            T z[SCAN_STEPS], a[SCAN_STEPS], r[SCAN_STEPS], d[SCAN_STEPS];
-            scan_load<T, FULL>(z, ur, p.at, row_bytes, count);
-            scan_load<T, FULL>(a, ur, p.at + p.block, row_bytes, count);
-            scan_load<T, FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
-            scan_load<T, FULL>(d, dr, p.at, p.block, count);
-            float f[SCAN_STEPS], e[SCAN_STEPS], c = states[((size_t)p.b * g.saved + t0 / SCAN_STEPS) * H + p.col];
-#pragma unroll
-            for (int i = 0; i < SCAN_STEPS; ++i) {
-                if (!scan_in<FULL>(i, count)) continue;
-                ScanStep<PRECISE> s;
-                s.make(c, value_of(z[i]), value_of(a[i]), bf, value_of(r[i]), br, 0.f, value_of(d[i]));
-                f[i] = s.f, e[i] = s.e;
-            }
-#pragma unroll
-            for (int i = SCAN_STEPS - 1; i >= 0; --i) {
-                if (!scan_in<FULL>(i, count)) continue;
-                D = (D + e[i]) * f[i];
-                A *= f[i];
-            }
-        };
-        if (count >= SCAN_STEPS) steps(ScanFull());
-        else steps(ScanPart());
-    }
-    sums[p.wave][p.lane] = make_float2(A, D);
-    __syncthreads();
-    if (p.wave != p.waves - 1 || !p.on) return;
-    for (int j = p.waves - 2; j >= 0; --j) {
-        const float2 q = sums[j][p.lane];
-        D = fmaf(q.x, D, q.y);
-        A *= q.x;
-    }
-    pairs[((size_t)p.b * (g.segments - 1) + (g.segments - 1 - p.seg)) * H + p.ch] = make_float2(A, D);
-    if (p.seg == g.segments - 1) dc_copy[(size_t)p.b * H + p.ch] = dc_last ? dc_last[(size_t)p.b * H + p.ch] : 0.f;
 }
 
 // db_f and db_r: 64 channels per workgroup; its wavefronts take the parts' sums in turn, and are added in their order
@@ -418,7 +432,7 @@ __global__ __launch_bounds__(BIAS_WAVES *WAVE) void sru_scan_bias_kernel(const f
     const size_t col = (size_t)blockIdx.x * WAVE + lane, width = 2 * (size_t)H;
     float sum = 0.f;
     if (col < width) {
-#pragma unroll 8
+#pragma unroll 16
         for (int i = wave; i < parts; i += BIAS_WAVES) sum += db[i * width + col];
     }
     sums[wave][lane] = sum;
@@ -440,16 +454,41 @@ static int scan_check(const char *who, int B, int L, int H, int n_blocks, int dt
     return MOE_OK;
 }
 
-// pairs, then the copy of the state that the first workgroup starts from
-static size_t scan_pairs_bytes(const ScanShape &g)
+// the workspace of tiles: words, the copy of the state at the start, the ticket
+static size_t scan_words(const ScanShape &g) { return g.tiles == 1 ? 0 : (size_t)g.B * g.groups * (g.tiles + g.runs + g.stretches) * WAVE; }
+static size_t scan_tiles_bytes(const ScanShape &g)
 {
-    return g.segments < 2 ? 0 : ((size_t)g.B * (g.segments - 1) * sizeof(float2) + (size_t)g.B * sizeof(float)) * g.H;
+    return g.tiles == 1 ? 0 : align_up(scan_words(g) * sizeof(unsigned long long) + (size_t)g.B * g.H * sizeof(float) + sizeof(unsigned), 16);
 }
 
-static dim3 scan_grid(const ScanShape &g, int segments)
+struct ScanTiles {
+    unsigned long long *words;
+    float *copy;
+    unsigned *ticket;
+};
+static ScanTiles scan_tiles(const ScanShape &g, void *ws)
 {
-    const long long n = (long long)g.B * segments * g.groups, across = n < (1 << 22) ? n : 1 << 22;
-    return dim3((unsigned)across, (unsigned)((n + across - 1) / across));
+    ScanTiles t = {(unsigned long long *)ws, nullptr, nullptr};
+    t.copy = (float *)(t.words + scan_words(g));
+    t.ticket = (unsigned *)(t.copy + (size_t)g.B * g.H);
+    return t;
+}
+// prepares the tiles of a call; start becomes the copy
+static int scan_clear(const ScanShape &g, const ScanTiles &t, const float *&start, hipStream_t st, const char *who)
+{
+    if (g.tiles == 1) return MOE_OK;
+    const size_t words = scan_words(g), channels = (size_t)g.B * g.H, wanted = (words + SCAN_CLEAR_THREADS - 1) / SCAN_CLEAR_THREADS;
+    const unsigned blocks = wanted < 2048 ? (unsigned)wanted : 2048;
+    hipLaunchKernelGGL(sru_scan_clear_kernel, dim3(blocks), dim3(SCAN_CLEAR_THREADS), 0, st, t.words, words, start, t.copy, channels, t.ticket, blocks);
+    MOE_CHECK_LAUNCH(who);
+    start = t.copy;
+    return MOE_OK;
+}
+
+static dim3 scan_grid(const ScanShape &g)
+{
+    const long long n = (long long)g.B * g.groups * g.tiles;
+    return dim3((unsigned)g.across, (unsigned)((n + g.across - 1) / g.across));
 }
 
 }  // namespace moe
@@ -459,20 +498,20 @@ using namespace moe;
 extern "C" size_t sru_scan_states_bytes(int B, int L, int H)
 {
     if (B <= 0 || L <= 0 || H <= 0) return 0;
-    return (size_t)B * ((L + SCAN_STEPS - 1) / SCAN_STEPS) * H * sizeof(float);
+    return (size_t)B * ((L + SCAN_SAVED - 1) / SCAN_SAVED) * H * sizeof(float);
 }
 
 extern "C" size_t sru_scan_workspace_bytes(int B, int L, int H, int dtype)
 {
     if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
-    return scan_pairs_bytes(scan_shape(B, L, H));
+    return scan_tiles_bytes(scan_forward_shape(B, L, H));
 }
 
 extern "C" size_t sru_scan_backward_workspace_bytes(int B, int L, int H, int dtype)
 {
     if (B <= 0 || L < 0 || H <= 0 || !scan_takes(B, L, H)) return 0;
-    const ScanShape g = scan_shape(B, L, H);
-    return scan_pairs_bytes(g) + (size_t)B * g.segments * 2 * H * sizeof(float);
+    const ScanShape g = scan_backward_shape(B, L, H);
+    return scan_tiles_bytes(g) + (size_t)B * g.tiles * 2 * H * sizeof(float);
 }
 
 // FORM(T): the build for a type
@@ -492,26 +531,19 @@ extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const fl
         MOE_REQUIRE(h != u && h != x, MOE_ERR_INVALID_ARG, "sru_scan: h aliases an input");
         MOE_REQUIRE(aligned16(u) && aligned16(x) && aligned16(h) && aligned16(states), MOE_ERR_INVALID_ARG, "sru_scan: tensor misaligned");
     }
-    const ScanShape g = scan_shape(B, L, H);
-    const size_t need = scan_pairs_bytes(g);
+    const ScanShape g = scan_forward_shape(B, L, H);
+    const size_t need = scan_tiles_bytes(g);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "sru_scan: workspace of %zu bytes given, %zu needed",
                 ws ? ws_bytes : 0, need);
     hipStream_t st = (hipStream_t)stream;
-    float2 *pairs = (float2 *)ws;
-    const dim3 threads(g.waves * WAVE);
-    if (g.segments > 1) {
-        float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
-#define MOE_PAIRS(T)                                                                                                                        \
-    hipLaunchKernelGGL((sru_scan_pairs_kernel<T>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)u, n_blocks, b_f, c0, lengths, \
-                       pairs, copy)
-        MOE_SCAN_FORMS(MOE_PAIRS);
-#undef MOE_PAIRS
-        MOE_CHECK_LAUNCH("sru_scan");
-        c0 = copy;
-    }
-#define MOE_SCAN(T, HW)                                                                                                                 \
-    hipLaunchKernelGGL((sru_scan_kernel<T, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, \
-                       pairs, (T *)h, c_last, (float *)states)
+    const ScanTiles tiles = scan_tiles(g, ws);
+    const int cleared = scan_clear(g, tiles, c0, st, "sru_scan");
+    if (cleared != MOE_OK) return cleared;
+#define MOE_SCAN(T, HW)                                                                                                                          \
+    hipLaunchKernelGGL((g.tiles == 1 ? sru_scan_kernel<T, HW, false, SCAN_LONG> : g.steps == SCAN_LONG ? sru_scan_kernel<T, HW, true, SCAN_LONG>  \
+                                                                                : sru_scan_kernel<T, HW, true, SCAN_SAVED>),                      \
+                       scan_grid(g), dim3(g.waves *WAVE), 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, tiles.ticket, tiles.words, \
+                       (T *)h, c_last, (float *)states)
 #define MOE_MAIN(T)                              \
     do {                                            \
         if (n_blocks == 3) MOE_SCAN(T, true);    \
@@ -542,24 +574,15 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
                 "sru_scan_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
     hipStream_t st = (hipStream_t)stream;
-    const ScanShape g = scan_shape(B, L, H);
-    float2 *pairs = (float2 *)ws;
-    float *db = db_f || db_r ? (float *)((char *)ws + scan_pairs_bytes(g)) : nullptr;
+    const ScanShape g = scan_backward_shape(B, L, H);
+    const ScanTiles tiles = scan_tiles(g, ws);
+    float *db = db_f || db_r ? (float *)((char *)ws + scan_tiles_bytes(g)) : nullptr;
     if (B > 0) {
-        const dim3 threads(g.waves * WAVE);
-        if (g.segments > 1) {
-            float *copy = (float *)(pairs + (size_t)B * (g.segments - 1) * H);
-#define MOE_PAIRS(T)                                                                                                                       \
-    hipLaunchKernelGGL((sru_scan_backward_pairs_kernel<T>), scan_grid(g, g.segments - 1), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
-                       n_blocks, b_f, b_r, (const float *)states, lengths, pairs, copy)
-            MOE_SCAN_FORMS(MOE_PAIRS);
-#undef MOE_PAIRS
-            MOE_CHECK_LAUNCH("sru_scan_backward");
-            dc_last = copy;
-        }
+        const int cleared = scan_clear(g, tiles, dc_last, st, "sru_scan_backward");
+        if (cleared != MOE_OK) return cleared;
 #define MOE_SCAN(T, HW)                                                                                                                    \
-    hipLaunchKernelGGL((sru_scan_backward_kernel<T, HW>), scan_grid(g, g.segments), threads, 0, st, g, (const T *)dh, dc_last, (const T *)u, \
-                       (const T *)x, b_f, b_r, (const float *)states, lengths, pairs, (T *)du, (T *)dx, db, dc0)
+    hipLaunchKernelGGL((g.tiles > 1 ? sru_scan_backward_kernel<T, HW, true> : sru_scan_backward_kernel<T, HW, false>), scan_grid(g), dim3(g.waves *WAVE), 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+                       (const T *)x, b_f, b_r, (const float *)states, lengths, tiles.ticket, tiles.words, (T *)du, (T *)dx, db, dc0)
 #define MOE_MAIN(T)                              \
     do {                                            \
         if (n_blocks == 3) MOE_SCAN(T, true);    \
@@ -572,7 +595,7 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
     }
     if (db_f || db_r) {
         const unsigned across = (unsigned)((2 * (size_t)H + WAVE - 1) / WAVE);
-        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3(across), dim3(BIAS_WAVES * WAVE), 0, st, db, B * g.segments, H, db_f, db_r);
+        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3(across), dim3(BIAS_WAVES * WAVE), 0, st, db, B * g.tiles, H, db_f, db_r);
         MOE_CHECK_LAUNCH("sru_scan_backward");
     }
     return MOE_OK;

@@ -4,42 +4,56 @@
 
 namespace moe {
 
-constexpr int SCAN_STEPS = 16;         // steps of a wavefront, and between saved states
+constexpr int SCAN_LONG = 16;          // steps of a wavefront of the forward where there is work for the card
+constexpr int SCAN_SAVED = 8;          // steps of a wavefront of the gradient (and the forward's few ones), and between saved states
 constexpr int SCAN_MAX_WAVES = 8;      // wavefronts of a workgroup, one behind the other on the sequence
-constexpr int SCAN_MAX_SEGMENTS = 64;
-constexpr int SCAN_ENOUGH = 256;       // workgroups from which on no sequence is cut
-constexpr int SCAN_WORKGROUPS = 768;   // that cut sequences give
+constexpr int SCAN_ENOUGH = 256;       // workgroups from which on a sequence is not cut into tiles
+constexpr int SCAN_FEW = 64;           // tiles below which the forward's are cut finer
+
+// tiles (sru_scan.hip)
+constexpr int SCAN_RUN = 16;           // tiles of a run, runs of a stretch: two for each wavefront to look for
+constexpr unsigned long long SCAN_UNKNOWN = ~0ull;
+constexpr int SCAN_PATIENCE = 1 << 22;
+constexpr int SCAN_CLEAR_THREADS = 256;
+static_assert(SCAN_RUN == 2 * SCAN_MAX_WAVES, "");
 
 struct ScanShape {
     int B, L, H;
     int groups;                        // of 64 channels, a lane each
-    int waves, segments, seg_steps;    // seg_steps: whole rounds of the workgroup's wavefronts
+    int waves, steps;                  // of a workgroup; of a wavefront
+    int tiles, runs, stretches;        // of a sequence; tiles = 1: one workgroup walks it round by round
     int saved;                         // saved states of a sequence
+    int across;                        // the grid's x
 };
 
-// sizes whose counts of workgroups and parts fit an int, and whose runs of SCAN_STEPS rows of four blocks lie within 2^31 bytes
+// sizes whose counts of workgroups and parts fit an int, and whose runs of SCAN_LONG rows of four blocks lie within 2^31 bytes
 static inline bool scan_takes(int B, int L, int H)
 {
     return H <= (1 << 23) && L <= (1 << 30) && (long long)B * ((H + WAVE - 1) / WAVE) < (1 << 26);
 }
 
-static inline ScanShape scan_shape(int B, int L, int H)
+static inline ScanShape scan_shape(int B, int L, int H, int steps)
 {
     ScanShape g;
-    g.B = B, g.L = L, g.H = H;
+    g.B = B, g.L = L, g.H = H, g.steps = steps;
     g.groups = (H + WAVE - 1) / WAVE;
     g.waves = 1;
-    while (g.waves < SCAN_MAX_WAVES && g.waves * SCAN_STEPS < L) g.waves *= 2;
-    const int round = g.waves * SCAN_STEPS, rounds = L > 0 ? (L + round - 1) / round : 1;
-    const long long have = (long long)(B > 0 ? B : 1) * g.groups;
-    long long want = have >= SCAN_ENOUGH ? 1 : (SCAN_WORKGROUPS + have - 1) / have;
-    if (want > SCAN_MAX_SEGMENTS) want = SCAN_MAX_SEGMENTS;
-    if (want > rounds) want = rounds;
-    const int per = (int)((rounds + want - 1) / want);
-    g.seg_steps = per * round;
-    g.segments = (rounds + per - 1) / per;
-    g.saved = L > 0 ? (L + SCAN_STEPS - 1) / SCAN_STEPS : 0;
+    while (g.waves < SCAN_MAX_WAVES && g.waves * steps < L) g.waves *= 2;
+    const int round = g.waves * steps, rounds = L > 0 ? (L + round - 1) / round : 1;
+    const long long lines = (long long)(B > 0 ? B : 1) * g.groups;
+    g.tiles = lines < SCAN_ENOUGH ? rounds : 1;
+    g.runs = (g.tiles + SCAN_RUN - 1) / SCAN_RUN;
+    g.stretches = (g.runs + SCAN_RUN - 1) / SCAN_RUN;
+    g.saved = L > 0 ? (L + SCAN_SAVED - 1) / SCAN_SAVED : 0;
+    const long long n = lines * g.tiles;
+    g.across = (int)(n < (1 << 22) ? n : 1 << 22);
     return g;
 }
+static inline ScanShape scan_forward_shape(int B, int L, int H)
+{
+    const ScanShape g = scan_shape(B, L, H, SCAN_LONG);
+    return g.tiles > 1 && (long long)B * g.groups * g.tiles < SCAN_FEW ? scan_shape(B, L, H, SCAN_SAVED) : g;
+}
+static inline ScanShape scan_backward_shape(int B, int L, int H) { return scan_shape(B, L, H, SCAN_SAVED); }
 
 }  // namespace moe

@@ -75,6 +75,13 @@ def test_sizes(dtype, B, L, H, k):
     _check(dtype, c, f"{dtype} {B}x{L}x{H} k={k}")
 
 
+@pytest.mark.parametrize("dtype,lengths", [("f32", None), ("bf16", [70001, 32768, 35000])])
+def test_very_long(dtype, lengths):
+    """Beyond 32768 steps, where a sequence's pairs go through states at every 256th tile."""
+    B, L, H = (1, 70001, 2) if lengths is None else (3, 70001, 1)
+    _check(dtype, _inputs(dtype, B, L, H, 3, 6, lengths), f"{dtype} {L}")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("k,lengths,L,H", [
     (3, [9, 0, 1, 5], 9, 34), (4, [0], 3, 8), (3, [16, 17, 15, 32], 32, 65), (4, [260, 0, 1, 128, 129, 255], 300, 66), (3, [1, 2300, 1111], 2300, 30),

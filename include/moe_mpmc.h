@@ -339,7 +339,7 @@ int moe_layer_forward(const moe_layer_args *args, void *stream);
  *   renormalize = 1: w_j (dw_j - sum_l dw_l w_l) at i = e_j with w the weights, 0 elsewhere.  E <= MOE_MAX_EXPERTS.  An
  *   id outside [0,E) is taken as a choice that was not made.  dlogits must not lie on logits.
  * Ids of a token must differ from each other, and so must the rows that inv names (as moe_route_topk and
- * moe_dispatch_topk give them): an entry of inv has to be negative or below k*T.
+ * moe_dispatch_topk give them).  y_perm, dy_perm and dx_perm have k*T rows; an entry of inv outside them names none.
  */
 int moe_combine_topk_backward(const void *dout, const void *y_perm, const int32_t *inv, const float *expert_weight,
                               int T, int k, int d, int dtype, int residual, void *dy_perm, float *dweight, void *dx,
@@ -356,7 +356,7 @@ int moe_route_topk_backward(const float *logits, const int32_t *expert_idx, cons
  *     f = sigmoid(u1 + b_f);  r = sigmoid(u2 + b_r);  c_t = f*c_{t-1} + (1-f)*u0;  h_t = r*tanh(c_t) + (1-r)*w_t
  * h [B, L, H] in dtype, rows behind a sequence's end zero; c_last [B, H] the state after its last token.  States and
  * all arithmetic are binary32.  b_f, b_r [H] binary32, c0 and lengths [B] (int32, taken to 0..L; NULL: all L) may be
- * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H.
+ * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H up to 2^22.
  * states (NULL, or sru_scan_states_bytes): what sru_scan_backward needs beside the inputs.
  *
  * sru_scan_backward -- from dh = dL/dh and dc_last = dL/dc_last (binary32, NULL: 0): du [B, L, n_blocks*H], dx [B, L, H]
@@ -386,7 +386,7 @@ int sru_scan_backward(const void *dh, const float *dc_last, const void *u, const
  *     among equals, and their log probabilities (0 <= k <= min(MOE_MAX_TOPK, V); NULL with k = 0)
  * Logits of -infinity are masked: probability 0, nothing to the entropy.  Where all are, log probabilities and lse are
  * -infinity and the entropy is 0.  A NaN or +infinity makes the row's numbers NaN; among the alternatives a NaN counts as
- * masked.  Sums in binary32, in an order that the shape fixes.  V <= 2^21, N <= 2^22.
+ * masked.  Sums in binary32, in an order that the shape fixes.  V <= 2^21.
  * moe_token_logprobs_backward -- dL/dlogits (dtype) from dlogprob [N] and dentropy [N] (NULL: 0), with the lse and
  * entropy that the forward wrote (entropy may be NULL without dentropy):
  *     dlogits_i = g ([i = target] - p_i) - dentropy p_i (log p_i + entropy),   g = dlogprob, 0 for a padded position

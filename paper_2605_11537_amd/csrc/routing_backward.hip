@@ -25,11 +25,18 @@ __device__ __forceinline__ rb_u32x4_t piece_of(const float (&v)[BF16 ? 8 : 4])
     return r;
 }
 
-// The row of this thread's group of 2^lg lanes (256 at most: a workgroup).
+// The row of this thread's group of 2^lg lanes (256 at most: a workgroup), in a grid of rows_grid.
 __device__ __forceinline__ unsigned rb_row(int lg, int &lane)
 {
     lane = threadIdx.x & ((1 << lg) - 1);
-    return ((blockIdx.y * gridDim.x + blockIdx.x) << (8 - lg)) + (threadIdx.x >> lg);
+    return (((blockIdx.y << ROWS_GRID_LG) + blockIdx.x) << (8 - lg)) + (threadIdx.x >> lg);
+}
+
+// The row of x_perm that an assignment went to, below rows; -1: none.  An entry of inv beyond the rows names none.
+__device__ __forceinline__ int rb_place(const int32_t *inv, size_t a, unsigned rows)
+{
+    const int r = inv[a];
+    return (unsigned)r < rows ? r : -1;
 }
 
 // A group of lanes per token: its dout once, PIECES pieces a lane at a time, the k rows of y it met, their gradients.  dweight: lanes' sums,
@@ -53,7 +60,7 @@ __global__ __launch_bounds__(RB_THREADS) void combine_backward_kernel(const rb_u
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
         pos[j] = -1, p[j] = dot[j] = 0.f;
         if (j >= k) continue;
-        pos[j] = inv[(size_t)j * T + s];
+        pos[j] = rb_place(inv, (size_t)j * T + s, (unsigned)k * T);
         p[j] = weight[(size_t)j * T + s];
         any = any || pos[j] >= 0;
     }
@@ -128,7 +135,7 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
     if (s >= (unsigned)T) return;
     int pos[MOE_MAX_TOPK];
 #pragma unroll
-    for (int j = 0; j < MOE_MAX_TOPK; ++j) pos[j] = j < k ? inv[(size_t)j * T + s] : -1;
+    for (int j = 0; j < MOE_MAX_TOPK; ++j) pos[j] = j < k ? rb_place(inv, (size_t)j * T + s, (unsigned)k * T) : -1;
     for (int c = lane; c < vec_per_row; c += 1 << lg) {
         rb_u32x4_t g[MOE_MAX_TOPK], a = {0, 0, 0, 0};
         if (dx_add) a = dx_add[(size_t)s * vec_per_row + c];
@@ -159,8 +166,8 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
 {
     constexpr int P = PIECES ? 4 : 1;
     typedef float piece_t __attribute__((ext_vector_type(P)));
-    const unsigned s = blockIdx.x * (RB_THREADS / LANES) + threadIdx.x / LANES;
-    const int lane = threadIdx.x % LANES;
+    int lane;
+    const unsigned s = rb_row(LANES == 64 ? 6 : LANES == 16 ? 4 : 2, lane);
     if (s >= (unsigned)T) return;
     const float *row = logits + (size_t)s * E;
     int e[MOE_MAX_TOPK];
@@ -252,6 +259,7 @@ static int rows_check(const char *who, int T, int k, int d, int dtype)
     MOE_REQUIRE(T >= 0 && d > 0 && k >= 1 && k <= MOE_MAX_TOPK, MOE_ERR_INVALID_ARG, "%s: T=%d d=%d k=%d out of range (k <= %d)", who, T, d, k,
                 MOE_MAX_TOPK);
     MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+    MOE_REQUIRE((long long)T * k <= INT32_MAX, MOE_ERR_INVALID_ARG, "%s: T=%d tokens of k=%d choices", who, T, k);
     const size_t row = (size_t)d * (dtype == MOE_F32 ? 4 : 2);
     MOE_REQUIRE(row % 16 == 0, MOE_ERR_INVALID_ARG, "%s: row size %zu bytes is not a multiple of 16", who, row);
     return MOE_OK;
@@ -313,7 +321,7 @@ extern "C" int moe_route_topk_backward(const float *logits, const int32_t *exper
     MOE_REQUIRE(dlogits != logits && dlogits != dweight, MOE_ERR_INVALID_ARG, "moe_route_topk_backward: dlogits aliases an input");
     const bool pieces = E % 4 == 0 && aligned16(logits) && aligned16(dlogits);
 #define MOE_GATE(L)                                                                                                                            \
-    hipLaunchKernelGGL((pieces ? route_backward_kernel<L, true> : route_backward_kernel<L, false>), dim3(ceil_div(T, RB_THREADS / L)),          \
+    hipLaunchKernelGGL((pieces ? route_backward_kernel<L, true> : route_backward_kernel<L, false>), rows_grid(T, L == 64 ? 6 : L == 16 ? 4 : 2), \
                        dim3(RB_THREADS), 0, (hipStream_t)stream, logits, expert_idx, dweight, T, E, k, renormalize, dlogits)
     if (E <= 4 * RB_LOGITS) MOE_GATE(4);
     else if (E <= 16 * RB_LOGITS) MOE_GATE(16);

@@ -26,10 +26,10 @@ struct ScanShape {
     int across;                        // the grid's x
 };
 
-// sizes whose counts of workgroups and parts fit an int, and whose runs of SCAN_LONG rows of four blocks lie within 2^31 bytes
+// sizes whose counts of workgroups and parts fit an int, and whose runs of SCAN_LONG rows of four blocks lie well within 2^31 bytes
 static inline bool scan_takes(int B, int L, int H)
 {
-    return H <= (1 << 23) && L <= (1 << 30) && (long long)B * ((H + WAVE - 1) / WAVE) < (1 << 26);
+    return H <= (1 << 22) && L <= (1 << 30) && (long long)B * ((H + WAVE - 1) / WAVE) < (1 << 26);
 }
 
 static inline ScanShape scan_shape(int B, int L, int H, int steps)

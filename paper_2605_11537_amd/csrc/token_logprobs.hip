@@ -181,17 +181,17 @@ __device__ __forceinline__ void lp_rank(const float *value, const int *id, int c
 template <class X, bool WHOLE>
 __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,
                                                                         const int32_t *__restrict__ target, int V, int parts, int part, int k,
-                                                                        float *__restrict__ records, LogprobOut out)
+                                                                        int threads, float *__restrict__ records, LogprobOut out)
 {
     typedef LogitPiece<X> piece;
     constexpr int P = piece::N;
     __shared__ float wave_m[LP_MAX_THREADS / WAVE], wave_s[LP_MAX_THREADS / WAVE], wave_t[LP_MAX_THREADS / WAVE];
     __shared__ float groups[LP_GROUPS], list_v[LP_LIST];
     __shared__ int list_id[LP_LIST], listed;
-    const unsigned n = WHOLE ? blockIdx.x : blockIdx.x / parts, which = WHOLE ? 0 : blockIdx.x - n * parts;
+    const unsigned n = blockIdx.x, which = WHOLE ? 0 : blockIdx.y;
     const int lo = which * part, len = min(part, V - lo), tid = threadIdx.x, lane = tid % WAVE;
     const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
-    const int threads = blockDim.x, waves = threads / WAVE;
+    const int waves = threads / WAVE;
     const X *row = logits + n * stride + lo;
     // pieces of 16 bytes from the first address that is one; what lies before and behind them is one logit a thread
     const int head = min(len, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(X)), pieces = (len - head) / P;
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(con
             }
         }
     } else {                                             // rows that lie differently inside 16 bytes
-        const int last = min(V, (int)(blockIdx.y + 1) * run * P + (blockIdx.y + 1 == gridDim.y ? 2 * P : 0));
+        const int last = min(V, (int)(blockIdx.y + 1) * run * P);
         for (int c = blockIdx.y * run * P + lane; c < last; c += lanes) store_value(out + c, f.at(value_of(row[c]), c));
     }
 }
@@ -456,8 +456,7 @@ static int logprobs_check(const char *who, int N, int V, long long stride, int d
     MOE_REQUIRE(N >= 0 && V > 0, MOE_ERR_INVALID_ARG, "%s: N=%d V=%d out of range", who, N, V);
     MOE_REQUIRE(stride >= V, MOE_ERR_INVALID_ARG, "%s: rows of %d logits lie %lld apart", who, V, stride);
     MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
-    MOE_REQUIRE(V <= LP_MAX_V, MOE_ERR_UNSUPPORTED, "%s: V=%d > %d", who, V, LP_MAX_V);
-    MOE_REQUIRE(N <= LP_MAX_N, MOE_ERR_UNSUPPORTED, "%s: N=%d > %d", who, N, LP_MAX_N);
+    MOE_REQUIRE(logprob_takes(N, V, dtype), MOE_ERR_UNSUPPORTED, "%s: N=%d V=%d too large (V <= %d)", who, N, V, LP_MAX_V);
     return MOE_OK;
 }
 
@@ -468,7 +467,7 @@ using namespace moe;
 extern "C" size_t moe_token_logprobs_workspace_bytes(int N, int V, int k, int dtype)
 {
     (void)k;
-    if (N <= 0 || V <= 0 || V > LP_MAX_V || N > LP_MAX_N) return 0;
+    if (N <= 0 || V <= 0 || (dtype != MOE_F32 && dtype != MOE_BF16) || !logprob_takes(N, V, dtype)) return 0;
     const LogprobShape g = logprob_shape(N, V, dtype);
     return g.parts > 1 ? (size_t)N * g.parts * LP_RECORD * sizeof(float) : 0;
 }
@@ -487,12 +486,13 @@ static void logprobs_launch(const LogprobShape &g, const X *logits, size_t strid
 #undef MOE_SHORT
         return;
     }
-    const dim3 grid((unsigned)N * g.parts), threads(g.threads);
+    const dim3 grid(N, g.parts), threads(g.threads);
     if (g.parts == 1) {
-        hipLaunchKernelGGL((token_logprobs_kernel<X, true>), grid, threads, 0, st, logits, stride, target, V, 1, g.part, k, nullptr, out);
+        hipLaunchKernelGGL((token_logprobs_kernel<X, true>), grid, threads, 0, st, logits, stride, target, V, 1, g.part, k, g.threads, nullptr, out);
         return;
     }
-    hipLaunchKernelGGL((token_logprobs_kernel<X, false>), grid, threads, 0, st, logits, stride, target, V, g.parts, g.part, k, records, out);
+    hipLaunchKernelGGL((token_logprobs_kernel<X, false>), grid, threads, 0, st, logits, stride, target, V, g.parts, g.part, k, g.threads, records,
+                       out);
     hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(N), dim3(WAVE), 0, st, records, target, V, g.parts, g.part, k, out);
 }
 

@@ -9,7 +9,6 @@ constexpr int LP_VECS = 8;                    // 16-byte pieces of a thread that
 constexpr int LP_MAX_THREADS = 1024;
 constexpr int LP_MAX_PARTS = 64;              // of a row: one lane each where they are joined
 constexpr int LP_MAX_V = 1 << 21;
-constexpr int LP_MAX_N = 1 << 22;             // a launch holds fewer than 2^32 threads
 constexpr int LP_RECORD = 4 + 2 * MOE_MAX_TOPK;   // floats of a part: maximum, sums, target's logit; the best logits and ids
 
 struct LogprobShape {
@@ -43,6 +42,16 @@ static inline LogprobShape logprob_shape(int N, int V, int dtype)
     g.threads = WAVE;
     while (g.threads < LP_MAX_THREADS && g.threads * each < pieces) g.threads *= 2;
     return g;
+}
+
+// a launch holds fewer than 2^32 threads in a dimension: short rows `lanes` each, long ones a workgroup each and their parts across the other
+// dimension; the gradient gives a row at most 256 threads
+static inline bool logprob_takes(int N, int V, int dtype)
+{
+    if (V > LP_MAX_V) return false;
+    const LogprobShape g = logprob_shape(N > 0 ? N : 1, V, dtype);
+    const int each = g.lanes ? g.lanes : g.threads;
+    return (long long)N * (each > 256 ? each : 256) < (1ll << 32) - 1024;
 }
 
 }  // namespace moe

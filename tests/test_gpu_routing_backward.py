@@ -154,3 +154,22 @@ def test_shapes_that_do_not_fit_are_refused():
         moe.moe_dispatch_topk_backward(f(12, 8), inv.cpu())
     with pytest.raises(moe.MoeError, match="multiple of 16"):
         moe.moe_dispatch_topk_backward(f(12, 7), inv)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_outside_the_permuted_ones_are_named_by_no_one(dtype):
+    """An entry of inv behind the last row is a choice without a row."""
+    import paper_2605_11537_amd as moe
+    T, k, d = 50, 2, 64
+    g = torch.Generator().manual_seed(4)
+    inv, _ = _tables(T, k, 0.2, 4)
+    wild = inv.copy()
+    out_of = np.flatnonzero(inv.reshape(-1) < 0)
+    wild.reshape(-1)[out_of] = np.array([k * T, k * T + 1, 2 ** 31 - 1, -2 ** 31])[np.arange(len(out_of)) % 4]
+    dt = DT[dtype]
+    dout, y = (torch.randn(n, d, generator=g).to(dt).cuda() for n in (T, k * T))
+    w = torch.rand(k, T, generator=g).cuda()
+    a, b = (torch.from_numpy(i).int().cuda() for i in (inv, wild))
+    x, z = (moe.moe_combine_topk_backward(dout, y, i, w) for i in (a, b))
+    assert all(torch.equal(x[key], z[key]) for key in x)
+    assert torch.equal(moe.moe_dispatch_topk_backward(y, a, dout), moe.moe_dispatch_topk_backward(y, b, dout))

@@ -23,6 +23,7 @@ def test_combine_backward(buf):
     assert f(p, q, i, w, 4, 0, 8, 0, 0, o, dw, dx, None) == INV                     # k
     assert f(p, q, i, w, 4, 9, 8, 0, 0, o, dw, dx, None) == INV
     assert f(p, q, i, w, 4, 1, 6, 0, 0, o, dw, dx, None) == INV                     # row bytes
+    assert f(p, q, i, w, 1 << 30, 3, 8, 0, 0, o, dw, dx, None) == INV               # more rows than an int counts
     assert f(p, q, i, w, 4, 1, 8, 2, 0, o, dw, dx, None) == INV                     # dtype
     assert f(p, q, i, w, 4, 1, 8, 0, 2, o, dw, dx, None) == INV                     # residual
     assert f(None, q, i, w, 4, 1, 8, 0, 0, o, dw, dx, None) == INV
@@ -73,7 +74,7 @@ def test_scan(buf):
     assert call(u=None) == INV and call(x=None) == INV and call(h=None) == INV
     assert call(h=u) == INV and call(h=x) == INV
     assert call(u=C.c_void_p(u.value + 8)) == INV
-    assert call(B=1 << 30, H=1 << 20) == UNS
+    assert call(B=1 << 30, H=1 << 20) == UNS and call(H=(1 << 22) + 1) == UNS
     assert call(B=0, u=None, x=x, h=None) == 0
     need = L.sru_scan_workspace_bytes(1, 16384, 128, 1)
     if need:
@@ -110,6 +111,8 @@ def test_token_logprobs(buf):
     assert call(k=-1) == INV and call(k=9) == INV and call(V=1, k=2) == INV
     assert call(x=None) == INV and call(a=None) == INV and call(i=None) == INV
     assert call(N=0, x=None, a=None, i=None) == 0
+    assert call(V=(1 << 21) + 1, stride=1 << 22) == UNS and call(N=(1 << 31) - 1, V=2000, stride=2000) == UNS
+    assert L.moe_token_logprobs_workspace_bytes(4, (1 << 21) + 1, 2, 1) == 0 and L.moe_token_logprobs_workspace_bytes(4, 1 << 21, 2, 7) == 0
     need = L.moe_token_logprobs_workspace_bytes(1, 1 << 18, 8, 1)
     if need:
         assert call(N=1, V=1 << 18, stride=1 << 18, dtype=1, k=8, size=need - 1) == WS

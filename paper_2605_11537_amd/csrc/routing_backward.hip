@@ -39,25 +39,25 @@ __device__ __forceinline__ int rb_place(const int32_t *inv, size_t a, unsigned r
     return (unsigned)r < rows ? r : -1;
 }
 
-// A group of lanes per token: its dout once, PIECES pieces a lane at a time, the k rows of y it met, their gradients.  dweight: lanes' sums,
-// then the wavefronts' in their order where a workgroup shares a row.
-template <bool BF16, int PIECES>
+// A group of lanes per token: its dout once, PIECES pieces a lane at a time, the rows of y it met (KMAX at most, all asked for before the
+// first is used), their gradients.  dweight: lanes' sums, then the wavefronts' in their order where a workgroup shares a row.
+template <bool BF16, int PIECES, int KMAX>
 __global__ __launch_bounds__(RB_THREADS) void combine_backward_kernel(const rb_u32x4_t *__restrict__ dout, const rb_u32x4_t *__restrict__ y_perm,
                                                                       const int32_t *__restrict__ inv, const float *__restrict__ weight, int T,
                                                                       int k, int vec_per_row, int lg, int residual, rb_u32x4_t *__restrict__ dy_perm,
                                                                       float *__restrict__ dweight, rb_u32x4_t *__restrict__ dx)
 {
     constexpr int V = BF16 ? 8 : 4;
-    __shared__ float sums[RB_THREADS / WAVE][MOE_MAX_TOPK];
+    __shared__ float sums[RB_THREADS / WAVE][KMAX];
     int lane;
     const unsigned s = rb_row(lg, lane);
     if (s >= (unsigned)T) return;                        // where a workgroup has a row: the whole workgroup
     const int lanes = 1 << lg;
-    int pos[MOE_MAX_TOPK];
-    float p[MOE_MAX_TOPK], dot[MOE_MAX_TOPK];
+    int pos[KMAX];
+    float p[KMAX], dot[KMAX];
     bool any = false;
 #pragma unroll
-    for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+    for (int j = 0; j < KMAX; ++j) {
         pos[j] = -1, p[j] = dot[j] = 0.f;
         if (j >= k) continue;
         pos[j] = rb_place(inv, (size_t)j * T + s, (unsigned)k * T);
@@ -70,27 +70,29 @@ __global__ __launch_bounds__(RB_THREADS) void combine_backward_kernel(const rb_u
 #pragma unroll
         for (int i = 0; i < PIECES; ++i)
             if (c0 + i * lanes < vec_per_row) g[i] = dout[(size_t)s * vec_per_row + c0 + i * lanes];
+        rb_u32x4_t y[KMAX][PIECES];
+        if (dweight) {
 #pragma unroll
-        for (int j = 0; j < MOE_MAX_TOPK; ++j) {
-            if (j >= k) break;
-            if (pos[j] < 0) continue;
-            const size_t row = (size_t)pos[j] * vec_per_row;
-            rb_u32x4_t y[PIECES];
-            if (dweight) {
+            for (int j = 0; j < KMAX; ++j) {
+                if (pos[j] < 0) continue;
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i)
-                    if (c0 + i * lanes < vec_per_row) y[i] = y_perm[row + c0 + i * lanes];
+                    if (c0 + i * lanes < vec_per_row) y[j][i] = y_perm[(size_t)pos[j] * vec_per_row + c0 + i * lanes];
             }
+        }
+#pragma unroll
+        for (int j = 0; j < KMAX; ++j) {
+            if (pos[j] < 0) continue;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 if (c0 + i * lanes >= vec_per_row) continue;
                 float v[V];
 #pragma unroll
                 for (int q = 0; q < V; ++q) v[q] = p[j] * piece_value<BF16>(g[i], q);
-                dy_perm[row + c0 + i * lanes] = piece_of<BF16>(v);
+                dy_perm[(size_t)pos[j] * vec_per_row + c0 + i * lanes] = piece_of<BF16>(v);
                 if (dweight) {
 #pragma unroll
-                    for (int q = 0; q < V; ++q) dot[j] = fmaf(piece_value<BF16>(g[i], q), piece_value<BF16>(y[i], q), dot[j]);
+                    for (int q = 0; q < V; ++q) dot[j] = fmaf(piece_value<BF16>(g[i], q), piece_value<BF16>(y[j][i], q), dot[j]);
                 }
             }
         }
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(RB_THREADS) void combine_backward_kernel(const rb_u
     }
     if (!dweight) return;
 #pragma unroll
-    for (int j = 0; j < MOE_MAX_TOPK; ++j) {
+    for (int j = 0; j < KMAX; ++j) {
         if (j >= k) break;
         float v = dot[j];
         if (lg >= 1) v += group_exchange<0>(v);
@@ -240,13 +242,13 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
     }
 }
 
-// combine's gradient: log2 of the lanes per row, one piece per lane and trip (a wavefront's at most, or a whole workgroup); -1: 32 lanes with
-// three pieces each
-static int combine_backward_lanes(int T, int vec_per_row)
+// combine's gradient: log2 of the lanes per row, one piece per lane and trip, a wavefront's at most or a whole workgroup; -1: 32 lanes with
+// three pieces each, for many rows with one choice (with more, their rows keep a lane's loads in flight).
+static int combine_backward_lanes(int T, int k, int vec_per_row)
 {
     const int lg = row_lanes(vec_per_row);
     if (lg <= 5) return lg;
-    return T > 2048 ? -1 : lg < 8 ? 6 : 8;
+    return lg > 7 ? 8 : k == 1 && T > 16384 ? -1 : 6;
 }
 static int dispatch_backward_lanes(int T, int vec_per_row)
 {
@@ -282,9 +284,10 @@ extern "C" int moe_combine_topk_backward(const void *dout, const void *y_perm, c
     MOE_REQUIRE(aligned16(dout) && aligned16(y_perm) && aligned16(dy_perm) && aligned16(dx), MOE_ERR_INVALID_ARG,
                 "moe_combine_topk_backward: tensor misaligned");
     const int vec = (int)((size_t)d * (dtype == MOE_F32 ? 4 : 2) / 16);
-    const int lg = combine_backward_lanes(T, vec), wide = lg < 0;
-    auto kern = dtype == MOE_BF16 ? (wide ? combine_backward_kernel<true, 3> : combine_backward_kernel<true, 1>)
-                                  : (wide ? combine_backward_kernel<false, 3> : combine_backward_kernel<false, 1>);
+    const int lg = combine_backward_lanes(T, k, vec), wide = lg < 0;
+#define MOE_CMB_BACK(B) (wide ? combine_backward_kernel<B, 3, 1> : k == 1 ? combine_backward_kernel<B, 1, 1> : k <= 4 ? combine_backward_kernel<B, 1, 4> : combine_backward_kernel<B, 1, MOE_MAX_TOPK>)
+    auto kern = dtype == MOE_BF16 ? MOE_CMB_BACK(true) : MOE_CMB_BACK(false);
+#undef MOE_CMB_BACK
     hipLaunchKernelGGL(kern, rows_grid(T, wide ? 5 : lg), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dout,
                        (const rb_u32x4_t *)y_perm, inv, expert_weight, T, k, vec, wide ? 5 : lg, residual, (rb_u32x4_t *)dy_perm, dweight,
                        (rb_u32x4_t *)dx);

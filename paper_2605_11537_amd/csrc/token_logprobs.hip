@@ -32,8 +32,8 @@ template <> struct LogitPiece<bf16_t> {
     }
 };
 
-// A logit as the alternatives see it: no number counts as masked.
-__device__ __forceinline__ float lp_ranked(float x) { return x == x ? x : -INFINITY; }
+// A logit as the alternatives see it: no number counts as masked (the maximum of a NaN and a value is the value).
+__device__ __forceinline__ float lp_ranked(float x) { return fmaxf(x, -INFINITY); }
 
 // Sums under a maximum.  It is never below the lowest finite value: a row that is masked throughout has s = 0, and no infinity is taken
 // from another; a NaN passes into s.
@@ -55,17 +55,17 @@ struct LogitSums {
         m = to;
     }
 };
-template <int LANES, int STEP = 0>
-__device__ __forceinline__ float lp_max_lanes(float v)
+// a reduction over groups of LANES lanes
+template <int LANES, int STEP = 0, class V, class F>
+__device__ __forceinline__ V lp_over(V v, F f)
 {
-    if constexpr ((1 << STEP) < LANES) return lp_max_lanes<LANES, STEP + 1>(fmaxf(v, group_exchange<STEP>(v)));
+    if constexpr ((1 << STEP) < LANES) return lp_over<LANES, STEP + 1>(f(v, group_exchange<STEP>(v)), f);
     else return v;
 }
-template <int LANES, int STEP = 0>
-__device__ __forceinline__ int lp_min_lanes(int v)
+template <int LANES>
+__device__ __forceinline__ float lp_max_lanes(float v)
 {
-    if constexpr ((1 << STEP) < LANES) return lp_min_lanes<LANES, STEP + 1>(min(v, group_exchange<STEP>(v)));
-    else return v;
+    return lp_over<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 // the lanes' sums under the largest of their maxima
 template <int LANES>
@@ -102,7 +102,9 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_short_kernel(const 
     const unsigned n = blockIdx.x * (LP_THREADS / LANES) + threadIdx.x / LANES, lane = threadIdx.x % LANES;
     if (n >= (unsigned)N) return;
     const X *row = logits + n * stride;
-    // behind the row: NaN, which no maximum takes and no comparison meets
+    const int wanted = target[n];                        // asked for with the row, not behind the sums
+    const float wanted_v = wanted >= 0 && wanted < V ? value_of(row[wanted]) : 0.f;
+    // behind the row: masked, and after every logit of the row where equals are ranked
     float v[LP_SMALL];
 #pragma unroll
     for (int i = 0; i < LP_SMALL; i += P) {
@@ -111,13 +113,13 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_short_kernel(const 
             lp_u32x4_t p;
             if (at + P <= V) p = *(const lp_u32x4_t *)(row + at);
 #pragma unroll
-            for (int q = 0; q < P; ++q) v[i + q] = at + P <= V ? piece::get(p, q) : NAN;
+            for (int q = 0; q < P; ++q) v[i + q] = at + P <= V ? piece::get(p, q) : -INFINITY;
             if (at < V && at + P > V) {
 #pragma unroll
-                for (int q = 0; q < P; ++q) v[i + q] = at + q < V ? value_of(row[at + q]) : NAN;
+                for (int q = 0; q < P; ++q) v[i + q] = at + q < V ? value_of(row[at + q]) : -INFINITY;
             }
         } else {
-            v[i] = at < V ? value_of(row[at]) : NAN;
+            v[i] = at < V ? value_of(row[at]) : -INFINITY;
         }
     }
     const auto place = [&](int i) { return i / P * P * LANES + lane * P + i % P; };
@@ -127,35 +129,56 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_short_kernel(const 
     top = lp_max_lanes<LANES>(top);
     LogitSums a = {fmaxf(top, -FLT_MAX), 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < LP_SMALL; ++i)
-        if (place(i) < V) a.add(v[i]);
+    for (int i = 0; i < LP_SMALL; ++i) a.add(v[i]);
     a.s = sum_over<LANES>(a.s);
     a.t = sum_over<LANES>(a.t);
     const float log_s = logf(a.s);
-    if (lane == 0) {
-        const int id = target[n];
-        lp_finish(a, log_s, n, id, V, id >= 0 && id < V ? value_of(row[id]) : 0.f, out);
-    }
+    if (lane == 0) lp_finish(a, log_s, n, wanted, V, wanted_v, out);
     if (k == 0) return;
+    const auto put = [&](int j, float x, int id) {
+        if (lane != 0) return;
+        out.top_idx[(size_t)n * k + j] = id;
+        out.top_logprob[(size_t)n * k + j] = lp_of(x, a, log_s);
+    };
+    if constexpr (sizeof(X) == 2) {
+        // value and place in one word that grows with the value and falls with the place: one maximum finds both
+        unsigned key[LP_SMALL];
 #pragma unroll
-    for (int i = 0; i < LP_SMALL; ++i)
-        if (place(i) < V) v[i] = lp_ranked(v[i]);
-    for (int j = 0; j < k; ++j) {
-        if (j > 0) {
-            top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < LP_SMALL; ++i) top = fmaxf(top, v[i]);
-            top = lp_max_lanes<LANES>(top);
+        for (int i = 0; i < LP_SMALL; ++i) {
+            const unsigned u = __float_as_uint(lp_ranked(v[i]) + 0.f);                 // -0 is 0
+            key[i] = ((u ^ ((unsigned)((int)u >> 31) | 0x80000000u)) & 0xffff0000u) | (0xffffu - place(i));
         }
-        int id = INT32_MAX;
+        for (int j = 0; j < k; ++j) {
+            unsigned best = 0;
 #pragma unroll
-        for (int i = LP_SMALL - 1; i >= 0; --i) id = v[i] == top ? place(i) : id;
-        id = lp_min_lanes<LANES>(id);
+            for (int i = 0; i < LP_SMALL; ++i) best = max(best, key[i]);
+            best = (unsigned)lp_over<LANES>((int)best, [](int x, int y) { return (int)max((unsigned)x, (unsigned)y); });
+            if (j + 1 < k) {
 #pragma unroll
-        for (int i = 0; i < LP_SMALL; ++i) v[i] = place(i) == id ? NAN : v[i];     // taken
-        if (lane == 0) {
-            out.top_idx[(size_t)n * k + j] = id;
-            out.top_logprob[(size_t)n * k + j] = lp_of(top, a, log_s);
+                for (int i = 0; i < LP_SMALL; ++i) key[i] = key[i] == best ? 0u : key[i];
+            }
+            const unsigned u = best & 0xffff0000u;
+            put(j, __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u & 0xffff0000u), (int)(0xffffu - (best & 0xffffu)));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < LP_SMALL; ++i) v[i] = lp_ranked(v[i]);
+        for (int j = 0; j < k; ++j) {
+            if (j > 0) {
+                top = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < LP_SMALL; ++i) top = fmaxf(top, v[i]);
+                top = lp_max_lanes<LANES>(top);
+            }
+            int id = INT32_MAX;
+#pragma unroll
+            for (int i = LP_SMALL - 1; i >= 0; --i) id = v[i] == top ? place(i) : id;
+            id = lp_over<LANES>(id, [](int x, int y) { return min(x, y); });
+            if (j + 1 < k) {
+#pragma unroll
+                for (int i = 0; i < LP_SMALL; ++i) v[i] = place(i) == id ? NAN : v[i];     // taken
+            }
+            put(j, top, id);
         }
     }
 }
@@ -198,6 +221,8 @@ __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const
     const int behind = head + pieces * P, ends = len - pieces * P;
     const int end_at = tid < head ? tid : behind + (tid - head);       // this thread's single logit, for tid < ends
     const lp_u32x4_t *body = (const lp_u32x4_t *)(row + head);
+    const int wanted = target[n];                        // asked for with the row, not behind the sums
+    const float wanted_v = wanted >= lo && wanted < lo + len ? value_of(row[wanted - lo]) : 0.f;
     lp_u32x4_t held[LP_VECS];
     X single = 0;
     if (tid < ends) single = row[end_at];
@@ -252,13 +277,8 @@ __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const
     const float log_s = logf(a.s);
     float *record = WHOLE ? nullptr : records + ((size_t)n * parts + which) * LP_RECORD;
     if (tid == 0) {
-        const int id = target[n];
-        if (WHOLE) {
-            lp_finish(a, log_s, n, id, V, id >= 0 && id < V ? value_of(row[id]) : 0.f, out);
-        } else {
-            record[0] = a.m, record[1] = a.s, record[2] = a.t;
-            record[3] = id >= lo && id < lo + len ? value_of(row[id - lo]) : 0.f;
-        }
+        if (WHOLE) lp_finish(a, log_s, n, wanted, V, wanted_v, out);
+        else record[0] = a.m, record[1] = a.s, record[2] = a.t, record[3] = wanted_v;
     }
     if (k == 0) return;
     const auto put = [&](int rank, float v, int id) {
@@ -356,11 +376,11 @@ __global__ __launch_bounds__(WAVE) void token_logprobs_join_kernel(const float *
         best[j] = j < k && lane < parts ? record[4 + j] : -INFINITY;
         ids[j] = j < k && lane < parts ? __float_as_int(record[4 + MOE_MAX_TOPK + j]) : INT32_MAX;
     }
-    const int id = target[n];
-    const float xt = id >= 0 && id < V ? records[(n * parts + id / part) * LP_RECORD + 3] : 0.f;
+    const int wanted = target[n];
+    const float wanted_v = wanted >= 0 && wanted < V ? records[(n * parts + wanted / part) * LP_RECORD + 3] : 0.f;
     lp_join_lanes<WAVE>(a);
     const float log_s = logf(a.s);
-    if (lane == 0) lp_finish(a, log_s, n, id, V, xt, out);
+    if (lane == 0) lp_finish(a, log_s, n, wanted, V, wanted_v, out);
     for (int j = 0; j < k; ++j) {
         float v = best[0];
         int i = ids[0];

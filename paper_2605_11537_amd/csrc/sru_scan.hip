@@ -33,23 +33,29 @@ __device__ __forceinline__ void scan_put(float v, scan_rows_t rows, unsigned lan
     else __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), rows, lane_at, step_at, 0);
 }
 
-// Where a workgroup stands: channels, sequence, and for a tile which one.  Everything but the channel is the same for a whole wavefront.
+// Where a wavefront stands: channels and sequence (its line), for a tile which one, and its place among the line's wavefronts.  A workgroup has
+// several lines where one or two wavefronts do for a line's steps.
 template <class T>
 struct ScanPlace {
-    int b, tile, lane, wave, waves, n, first, last;    // first .. last-1: the workgroup's steps
-    unsigned ch, col;                                  // this lane's channel; one that exists
-    unsigned at, block;                                // its offset in a row of one block, and a block's length, in bytes
+    int b, tile, lane, wave, waves, base, n, first, last;   // base: the line's first wavefront in the workgroup; first .. last-1: its steps
+    unsigned ch, col;                                       // this lane's channel; one that exists
+    unsigned at, block;                                     // its offset in a row of one block, and a block's length, in bytes
     bool on;
     template <bool TILES>
     __device__ __forceinline__ void find(const ScanShape &g, const int32_t *lengths, unsigned line, int which)
     {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+        waves = g.waves;
+        wave = TILES ? w : w & (waves - 1);
+        base = w - wave;
+        if (!TILES) line = line * g.pack + (w >> g.waves_lg);
+        const bool live = TILES || line < (unsigned)g.B * g.groups;     // the last workgroup may have lines to spare
+        if (!live) line = 0;
         b = line / (unsigned)g.groups;
         tile = which;
         lane = threadIdx.x % WAVE;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-        waves = g.waves;
         ch = (line - b * (unsigned)g.groups) * WAVE + lane;
-        on = ch < (unsigned)g.H;
+        on = live && ch < (unsigned)g.H;
         col = on ? ch : 0;
         at = on ? ch * (unsigned)sizeof(T) : SCAN_NOWHERE;
         block = g.H * (unsigned)sizeof(T);
@@ -195,15 +201,15 @@ __global__ __launch_bounds__(SCAN_CLEAR_THREADS) void sru_scan_clear_kernel(unsi
     if (first == 0) *ticket = 0;
 }
 
-// the workgroup's line (sequence and channels) and, with tiles, its place in the chain
+// the workgroup's number or, with tiles, its line and its place in the chain
 template <bool TILES>
 __device__ __forceinline__ bool scan_draw(const ScanShape &g, unsigned *ticket, unsigned *drawn, unsigned &line, int &at)
 {
-    const unsigned lines = (unsigned)g.B * g.groups;
     if (!TILES) {
         line = blockIdx.y * g.across + blockIdx.x, at = 0;
-        return line < lines;
+        return line < (unsigned)g.workgroups;
     }
+    const unsigned lines = (unsigned)g.B * g.groups;
     if (threadIdx.x == 0) *drawn = atomicAdd(ticket, 1u);
     __syncthreads();
     const unsigned t = __builtin_amdgcn_readfirstlane(*drawn);
@@ -258,12 +264,12 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
         };
         if (count >= STEPS) gates(ScanFull());
         else gates(ScanPart());
-        sums[parity][p.wave][p.lane] = make_float2(A, C);
+        sums[parity][p.base + p.wave][p.lane] = make_float2(A, C);
         __syncthreads();
         float2 all = make_float2(1.f, 0.f), before = all;
         for (int j = 0; j < p.waves; ++j) {
             if (j == p.wave) before = all;
-            all = scan_then(all, sums[parity][j][p.lane]);
+            all = scan_then(all, sums[parity][p.base + j][p.lane]);
         }
         if (TILES) c_in = scan_look_back(chain, g.tiles, at, p.lane, p.wave, all, c_in, sums[1], sums[2]);
         float c = scan_through(before, c_in);
@@ -317,7 +323,7 @@ struct ScanStep {
     }
 };
 
-template <class T, bool HIGHWAY, bool TILES>
+template <class T, bool HIGHWAY, bool TILES, int STEPS>
 __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_kernel(
     ScanShape g, const T *__restrict__ dh, const float *dc_last, const T *__restrict__ u, const T *__restrict__ x, const float *__restrict__ b_f,
     const float *__restrict__ b_r, const float *__restrict__ states, const int32_t *__restrict__ lengths, unsigned *ticket,
@@ -337,17 +343,17 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
     const size_t H = g.H, row_len = K * H;
     const float bf = gate_bias<PRECISE>(b_f ? b_f[p.col] : 0.f), br = gate_bias<PRECISE>(b_r ? b_r[p.col] : 0.f);
     float sum_f = 0.f, sum_r = 0.f, d_in = dc_last ? dc_last[(size_t)p.b * H + p.col] : 0.f;
-    const int round = p.waves * SCAN_SAVED, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
+    const int round = p.waves * STEPS, rounds = p.last > p.first ? (p.last - p.first + round - 1) / round : 0;
     for (int back = rounds - 1, parity = 0; back >= 0; --back, parity ^= 1) {
-        const int t0 = p.first + back * round + p.wave * SCAN_SAVED, count = min(p.n - t0, SCAN_SAVED);
+        const int t0 = p.first + back * round + p.wave * STEPS, count = min(p.n - t0, STEPS);
         const size_t row = (size_t)p.b * g.L + t0;
         const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H), out = scan_rows(du + row * row_len);
         const scan_rows_t xr = HIGHWAY ? scan_rows(x + row * H) : ur, out_w = HIGHWAY ? scan_rows(dx + row * H) : out;
         const unsigned at_w = HIGHWAY ? p.at : p.at + 3 * p.block, row_bytes = K * p.block, w_bytes = HIGHWAY ? p.block : row_bytes;
-        float f[SCAN_SAVED], rest[SCAN_SAVED], e[SCAN_SAVED], gap[SCAN_SAVED], A = 1.f, D = 0.f;
+        float f[STEPS], rest[STEPS], e[STEPS], gap[STEPS], A = 1.f, D = 0.f;
         auto forward = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
-            T z[SCAN_SAVED], a[SCAN_SAVED], r[SCAN_SAVED], w[SCAN_SAVED], d[SCAN_SAVED];
+            T z[STEPS], a[STEPS], r[STEPS], w[STEPS], d[STEPS];
             scan_load<FULL>(z, ur, p.at, row_bytes, count);
             scan_load<FULL>(a, ur, p.at + p.block, row_bytes, count);
             scan_load<FULL>(r, ur, p.at + 2 * p.block, row_bytes, count);
@@ -355,7 +361,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
             scan_load<FULL>(d, dr, p.at, p.block, count);
             float c = FULL || count > 0 ? states[((size_t)p.b * g.saved + t0 / SCAN_SAVED) * H + p.col] : 0.f;
 #pragma unroll
-            for (int i = 0; i < SCAN_SAVED; ++i) {
+            for (int i = 0; i < STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) {
                     if (t0 + i < p.last) {
                         for (int k = 0; k < 3; ++k) scan_put<T>(0.f, out, p.at + k * p.block, i * row_bytes);
@@ -371,20 +377,20 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
                 scan_put<T>(s.d_w, out_w, at_w, i * w_bytes);
             }
 #pragma unroll
-            for (int i = SCAN_SAVED - 1; i >= 0; --i) {
+            for (int i = STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 D = (D + e[i]) * f[i];
                 A *= f[i];
             }
         };
-        if (count >= SCAN_SAVED) forward(ScanFull());
+        if (count >= STEPS) forward(ScanFull());
         else forward(ScanPart());
-        sums[parity][p.wave][p.lane] = make_float2(A, D);
+        sums[parity][p.base + p.wave][p.lane] = make_float2(A, D);
         __syncthreads();
         float2 all = make_float2(1.f, 0.f), before = all;
         for (int j = p.waves - 1; j >= 0; --j) {
             if (j == p.wave) before = all;
-            all = scan_then(all, sums[parity][j][p.lane]);
+            all = scan_then(all, sums[parity][p.base + j][p.lane]);
         }
         if (TILES) d_in = scan_look_back(chain, g.tiles, at, p.lane, p.wave, all, d_in, sums[1], sums[2]);
         float dc = scan_through(before, d_in);
@@ -392,7 +398,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
         auto backward = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
 #pragma unroll
-            for (int i = SCAN_SAVED - 1; i >= 0; --i) {
+            for (int i = STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 const float full = dc + e[i], d_f = full * gap[i];
                 sum_f += d_f;
@@ -401,18 +407,18 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
                 scan_put<T>(d_f, out, p.at + p.block, i * row_bytes);
             }
         };
-        if (count >= SCAN_SAVED) backward(ScanFull());
+        if (count >= STEPS) backward(ScanFull());
         else backward(ScanPart());
     }
     if (dc0 && p.tile == 0 && p.wave == 0 && p.on) dc0[(size_t)p.b * H + p.ch] = d_in;
     if (!db) return;
     // the wavefronts' sums in their order, a row of [2 H] for each sequence and tile
     __syncthreads();
-    sums[0][p.wave][p.lane] = make_float2(sum_f, sum_r);
+    sums[0][p.base + p.wave][p.lane] = make_float2(sum_f, sum_r);
     __syncthreads();
     if (p.wave != 0 || !p.on) return;
     for (int j = 1; j < p.waves; ++j) {
-        const float2 q = sums[0][j][p.lane];
+        const float2 q = sums[0][p.base + j][p.lane];
         sum_f += q.x;
         sum_r += q.y;
     }
@@ -421,25 +427,25 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
     to[H] = sum_r;
 }
 
-// db_f and db_r: 64 channels per workgroup; its wavefronts take the parts' sums in turn, and are added in their order
-constexpr int BIAS_WAVES = 16;
+// db_f and db_r: 32 columns per workgroup; 32 groups of lanes take the parts' sums in turn and are added in their order
+constexpr int BIAS_LANES = 32, BIAS_GROUPS = 32;
 
-__global__ __launch_bounds__(BIAS_WAVES *WAVE) void sru_scan_bias_kernel(const float *__restrict__ db, int parts, int H, float *__restrict__ db_f,
-                                                                        float *__restrict__ db_r)
+__global__ __launch_bounds__(BIAS_LANES *BIAS_GROUPS) void sru_scan_bias_kernel(const float *__restrict__ db, int parts, int H,
+                                                                               float *__restrict__ db_f, float *__restrict__ db_r)
 {
-    __shared__ float sums[BIAS_WAVES][WAVE];
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-    const size_t col = (size_t)blockIdx.x * WAVE + lane, width = 2 * (size_t)H;
+    __shared__ float sums[BIAS_GROUPS][BIAS_LANES];
+    const int lane = threadIdx.x % BIAS_LANES, group = threadIdx.x / BIAS_LANES;
+    const size_t col = (size_t)blockIdx.x * BIAS_LANES + lane, width = 2 * (size_t)H;
     float sum = 0.f;
     if (col < width) {
 #pragma unroll 16
-        for (int i = wave; i < parts; i += BIAS_WAVES) sum += db[i * width + col];
+        for (int i = group; i < parts; i += BIAS_GROUPS) sum += db[i * width + col];
     }
-    sums[wave][lane] = sum;
+    sums[group][lane] = sum;
     __syncthreads();
-    if (wave != 0 || col >= width) return;
+    if (group != 0 || col >= width) return;
 #pragma unroll
-    for (int j = 1; j < BIAS_WAVES; ++j) sum += sums[j][lane];
+    for (int j = 1; j < BIAS_GROUPS; ++j) sum += sums[j][lane];
     float *out = col < (size_t)H ? db_f : db_r;
     if (out) out[col < (size_t)H ? col : col - H] = sum;
 }
@@ -487,8 +493,7 @@ static int scan_clear(const ScanShape &g, const ScanTiles &t, const float *&star
 
 static dim3 scan_grid(const ScanShape &g)
 {
-    const long long n = (long long)g.B * g.groups * g.tiles;
-    return dim3((unsigned)g.across, (unsigned)((n + g.across - 1) / g.across));
+    return dim3((unsigned)g.across, (unsigned)((g.workgroups + g.across - 1) / g.across));
 }
 
 }  // namespace moe
@@ -540,10 +545,12 @@ extern "C" int sru_scan(const void *u, const void *x, const float *b_f, const fl
     const int cleared = scan_clear(g, tiles, c0, st, "sru_scan");
     if (cleared != MOE_OK) return cleared;
 #define MOE_SCAN(T, HW)                                                                                                                          \
-    hipLaunchKernelGGL((g.tiles == 1 ? sru_scan_kernel<T, HW, false, SCAN_LONG> : g.steps == SCAN_LONG ? sru_scan_kernel<T, HW, true, SCAN_LONG>  \
-                                                                                : sru_scan_kernel<T, HW, true, SCAN_SAVED>),                      \
-                       scan_grid(g), dim3(g.waves *WAVE), 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, tiles.ticket, tiles.words, \
-                       (T *)h, c_last, (float *)states)
+    hipLaunchKernelGGL((g.tiles > 1 ? (g.steps == SCAN_LONG ? sru_scan_kernel<T, HW, true, SCAN_LONG> : sru_scan_kernel<T, HW, true, SCAN_SAVED>) \
+                        : g.steps == SCAN_LONG  ? sru_scan_kernel<T, HW, false, SCAN_LONG>                                                        \
+                        : g.steps == SCAN_SAVED ? sru_scan_kernel<T, HW, false, SCAN_SAVED>                                                       \
+                                                : sru_scan_kernel<T, HW, false, 1>),                                                              \
+                       scan_grid(g), dim3(g.waves *g.pack *WAVE), 0, st, g, (const T *)u, (const T *)x, b_f, b_r, c0, lengths, tiles.ticket,      \
+                       tiles.words, (T *)h, c_last, (float *)states)
 #define MOE_MAIN(T)                              \
     do {                                            \
         if (n_blocks == 3) MOE_SCAN(T, true);    \
@@ -581,7 +588,7 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
         const int cleared = scan_clear(g, tiles, dc_last, st, "sru_scan_backward");
         if (cleared != MOE_OK) return cleared;
 #define MOE_SCAN(T, HW)                                                                                                                    \
-    hipLaunchKernelGGL((g.tiles > 1 ? sru_scan_backward_kernel<T, HW, true> : sru_scan_backward_kernel<T, HW, false>), scan_grid(g), dim3(g.waves *WAVE), 0, st, g, (const T *)dh, dc_last, (const T *)u, \
+    hipLaunchKernelGGL((g.tiles > 1 ? sru_scan_backward_kernel<T, HW, true, SCAN_SAVED> : g.steps == SCAN_SAVED ? sru_scan_backward_kernel<T, HW, false, SCAN_SAVED> : sru_scan_backward_kernel<T, HW, false, 1>), scan_grid(g), dim3(g.waves *g.pack *WAVE), 0, st, g, (const T *)dh, dc_last, (const T *)u, \
                        (const T *)x, b_f, b_r, (const float *)states, lengths, tiles.ticket, tiles.words, (T *)du, (T *)dx, db, dc0)
 #define MOE_MAIN(T)                              \
     do {                                            \
@@ -594,8 +601,8 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
         MOE_CHECK_LAUNCH("sru_scan_backward");
     }
     if (db_f || db_r) {
-        const unsigned across = (unsigned)((2 * (size_t)H + WAVE - 1) / WAVE);
-        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3(across), dim3(BIAS_WAVES * WAVE), 0, st, db, B * g.tiles, H, db_f, db_r);
+        const unsigned across = (unsigned)((2 * (size_t)H + BIAS_LANES - 1) / BIAS_LANES);
+        hipLaunchKernelGGL(sru_scan_bias_kernel, dim3(across), dim3(BIAS_LANES * BIAS_GROUPS), 0, st, db, B * g.tiles, H, db_f, db_r);
         MOE_CHECK_LAUNCH("sru_scan_backward");
     }
     return MOE_OK;

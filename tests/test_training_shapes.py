@@ -21,7 +21,7 @@ int main()
         if (kind == 'f' || kind == 'b') {
             if (!scan_takes(a, b, c)) { printf("-1\\n"); continue; }
             const ScanShape g = kind == 'f' ? scan_forward_shape(a, b, c) : scan_backward_shape(a, b, c);
-            printf("%d %d %d %d %d %d %d %d %d %d\\n", g.groups, g.waves, g.steps, g.tiles, g.runs, g.stretches, g.saved, g.across, SCAN_RUN, SCAN_MAX_WAVES);
+            printf("%d %d %d %d %d %d %d %d %d %d %d %lld\\n", g.groups, g.waves, g.steps, g.tiles, g.runs, g.stretches, g.saved, g.across, SCAN_RUN, SCAN_MAX_WAVES, g.pack, g.workgroups);
         } else if (kind == 'g') {
             const dim3 g = rows_grid(a, b);
             printf("%u %u %d\\n", g.x, g.y, ROWS_GRID_LG);
@@ -63,17 +63,20 @@ def test_scan_shapes(ask):
         if got == [-1]:
             assert H > 1 << 22 or lines >= 1 << 26
             continue
-        groups, waves, steps, tiles, runs, stretches, saved, across, RUN, MAX = got
-        assert groups == -(-H // 64) and waves in (1, 2, 4, 8) and waves <= MAX and steps in (8, 16) and (kind == "f" or steps == 8)
+        groups, waves, steps, tiles, runs, stretches, saved, across, RUN, MAX, pack, workgroups = got
+        assert groups == -(-H // 64) and waves in (1, 2, 4, 8) and waves <= MAX
+        assert steps in (8, 16) and (kind == "f" or steps == 8) if L > 1 else steps == 1
         round_ = waves * steps
-        assert saved == -(-L // 8) and steps % 8 == 0
+        assert saved == -(-L // 8) and (steps % 8 == 0 or L <= 1)
+        assert waves * pack in (4, 8) and (pack == 1 or tiles == 1) and waves * pack <= MAX
         if tiles > 1:
             # tiles are whole, the look-back has its eight wavefronts, and every list holds what indexes it
             assert waves == MAX and RUN == 2 * MAX and (tiles - 1) * round_ < L <= tiles * round_
             assert (tiles - 1) // RUN < runs and (runs - 1) // RUN < stretches
         else:
             assert lines >= 256 or L <= round_
-        n = lines * tiles
+        n = lines * tiles if pack == 1 else -(-lines // pack)
+        assert n == workgroups
         assert across * 512 < 1 << 32 and -(-n // across) < 1 << 16
         assert 15 * 4 * H * 4 + 4 * H * 4 < 0x7fffffff              # the farthest step's row of binary32 in four blocks
     assert ask([("f", 1, 5, 1 << 23)]) == [[-1]]

@@ -365,7 +365,8 @@ int moe_route_topk_backward(const float *logits, const int32_t *expert_idx, cons
  *     du2 = dh_t (tanh(c_t) - w_t) r (1-r);  dw_t = dh_t (1-r)
  * Behind a sequence's end du and dx are zero; dh, u and x are not read there.  The sums of db_f and db_r have a fixed
  * order: equal calls give equal bits.  dc0 may be dc_last.
- * The workspaces may be NULL where the size is 0.
+ * The workspaces may be NULL where the size is 0.  Where sequences and channels are few, workgroups of a call's launch wait
+ * for others of it that have begun before them, through words of the workspace, which the call sets first.
  */
 size_t sru_scan_states_bytes(int B, int L, int H);
 size_t sru_scan_workspace_bytes(int B, int L, int H, int dtype);

@@ -1,6 +1,6 @@
 """Binding of ``libmoe_mpmc.so``: the library's calls under the same names (the six steps
-of the layer, weight packing, the fused plan + dispatch front end, the top-k variants) on torch
-tensors, and three small classes that hold preallocated buffers and issue the calls in order.
+of the layer, weight packing, the fused plan + dispatch front end, the top-k variants, the calls that train the gate and the
+predictor) on torch tensors, and three small classes that hold preallocated buffers and issue the calls in order.
 Argument marshalling only -- every step of the path runs in the HIP kernels.  The library is loaded through ctypes;
 the calls that enqueue work go through the extension ``_marshal`` (csrc/marshal.cpp), which reads the tensors' pointers itself.  Torch is used for
 device memory and the current stream, nothing else.  There is no CPU fallback: if the library is

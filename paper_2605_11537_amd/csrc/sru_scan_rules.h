@@ -4,11 +4,17 @@
 
 namespace moe {
 
-constexpr int SCAN_LONG = 16;          // steps of a wavefront of the forward where there is work for the card
-constexpr int SCAN_SAVED = 8;          // steps of a wavefront of the gradient (and the forward's few ones), and between saved states
+// Steps of a wavefront: 16 in the forward where there is work for the card (2 x 16384 x 768 bf16 72 us, with 8 93 us: more tiles to wait for), 8 in the
+// gradient, whose registers hold more for each (126 us, with 16 and no more than two workgroups' registers 132 us; 8 x 1000 x 768 43 and 61 us).
+// States are saved every 8 steps: 5 % of the forward's bytes.
+constexpr int SCAN_LONG = 16;
+constexpr int SCAN_SAVED = 8;
 constexpr int SCAN_MAX_WAVES = 8;      // wavefronts of a workgroup, one behind the other on the sequence
-constexpr int SCAN_ENOUGH = 256;       // workgroups from which on a sequence is not cut into tiles
-constexpr int SCAN_FEW = 64;           // tiles below which the forward's are cut finer
+// Lines (sequences by 64 channels) from which on a sequence is walked by one workgroup instead of cut into tiles: 32 x 512 x 1024, 512 lines, 42 us
+// walked, 50 us in tiles; 16 x 2048 x 1024, 256 lines, 84 and 93; 12 x 1024 x 1024 fp32, 192 lines, 64 and 62 (gradient 112 and 103).
+constexpr int SCAN_ENOUGH = 256;
+// Tiles below which the forward's are cut finer: 16 of them (1 x 200 x 512) 11 us, finer 9; 210 (5 x 777 x 321 fp32) 13.5 and 16.
+constexpr int SCAN_FEW = 64;
 
 // tiles (sru_scan.hip)
 constexpr int SCAN_RUN = 16;           // tiles of a run, runs of a stretch: two for each wavefront to look for

@@ -5,6 +5,9 @@
 // A row is read once, into registers.  The sums are found while it arrives.  The alternatives then cost next to nothing: a bound that k logits
 // reach for certain (the k-th largest of the maxima of sixteen groups of threads), the few logits that reach it collected, and each ranked
 // among them.  Rows where more than LP_LIST reach it (equal logits) or fewer than k lie above minus infinity take k searches of the registers.
+// Measured: 8192 x 50257 bf16, k = 4, 170 us (4.8 TB/s; memory, and some nine vector operations a logit beside it), 2048 x 32000 fp32 46 us (5.7
+// TB/s); 32768 x 256 fp32, k = 1, 9 us (3.8 TB/s), 65536 x 256 bf16, k = 8, 21 us (the searches' operations bind).  The gradient reads and writes once:
+// 342 us (4.8 TB/s) for the first, 13 us (5.2 TB/s) for the third.
 #include <float.h>
 
 #include "scalar_math.h"
@@ -199,7 +202,8 @@ __device__ __forceinline__ void lp_rank(const float *value, const int *id, int c
     if (rank < k) put(rank, v, i);
 }
 
-// Long rows: a workgroup takes a part of a row, LP_VECS pieces a thread in registers.  WHOLE: the part is the row; else its numbers go to
+// Long rows: a workgroup takes a part of a row, LP_VECS pieces a thread in registers; 64 registers, so that two workgroups of 1024 share a compute unit
+// and one loads while the other sums (one alone: 8192 x 50257 400 us).  WHOLE: the part is the row; else its numbers go to
 // a record of LP_RECORD floats.
 template <class X, bool WHOLE>
 __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,

@@ -200,7 +200,8 @@ PyObject *py_moe_layer_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
 }
 
 // expect(who, device, lead, name, tensor, dtype, sizes, ...): each tensor (None: left out) has that dtype and those sizes and lies where lead
-// does, which is the current device (device() asks for it).  ValueError else.  In Python these checks took 2 us a call.
+// does, which is the current device (device() asks for it).  ValueError else, and where a size does not fit an int.  In Python these checks took 2 us
+// a call.
 PyObject *py_expect(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n < 3 || (n - 3) % 4) {
@@ -214,6 +215,14 @@ PyObject *py_expect(PyObject *, PyObject *const *args, Py_ssize_t n)
                 throw Failed();
             }
             return THPVariable_Unpack(o);
+        };
+        // the library counts in ints, to which a call's arguments are reduced; buffers of one dimension are counted in bytes
+        auto countable = [&](const at::Tensor &t) {
+            for (int64_t d = 0; t.dim() > 1 && d < t.dim(); ++d)
+                if (t.size(d) > INT_MAX) {
+                    PyErr_Format(PyExc_ValueError, "%U: a size of %lld does not fit an int", args[0], (long long)t.size(d));
+                    throw Failed();
+                }
         };
         const at::Tensor &lead = tensor(args[2], args[0]);
         if (!lead.is_cuda()) {
@@ -229,9 +238,11 @@ PyObject *py_expect(PyObject *, PyObject *const *args, Py_ssize_t n)
             PyErr_Format(PyExc_ValueError, "%U: tensors on device %d, the current device is %ld", args[0], (int)lead.get_device(), here);
             return nullptr;
         }
+        countable(lead);
         for (Py_ssize_t i = 3; i < n; i += 4) {
             if (args[i + 1] == Py_None) continue;
             const at::Tensor &t = tensor(args[i + 1], args[i]);
+            countable(t);
             if (!THPDtype_Check(args[i + 2]) || !PyTuple_Check(args[i + 3])) {
                 PyErr_SetString(PyExc_TypeError, "expect: a dtype and a tuple of sizes");
                 return nullptr;

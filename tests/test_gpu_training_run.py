@@ -307,3 +307,25 @@ def test_another_device_is_refused(monkeypatch):
                  lambda: moe.sru_scan(torch.zeros(1, 4, 24, device="cuda"), torch.zeros(1, 4, 8, device="cuda"))):
         with pytest.raises(ValueError, match="the current device is 1"):
             call()
+
+
+def test_sizes_past_an_int_are_refused():
+    """A size is never reduced to the int that the library counts in: 2^32 + 8 is not 8."""
+    import paper_2605_11537_amd as moe
+    far = 2 ** 32 + 8
+    e = lambda *s, dt=torch.float32: torch.zeros(*[1] * len(s), dtype=dt, device="cuda").expand(*s)
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, device="cuda")
+    out = torch.zeros(1, 1, device="cuda").expand(1, far)
+    for call in (lambda: moe.moe_token_logprobs(e(1, far), one),
+                 lambda: moe.moe_token_logprobs_backward(e(1, far), one, q, q, q, out=out),
+                 lambda: moe.moe_token_logprobs(e(far, 8), e(far, dt=torch.int32)),
+                 lambda: moe.moe_route_topk_backward(e(1, far), one[None], q[None], out=out),
+                 lambda: moe.moe_route_topk_backward(e(1, 8), e(far, 1, dt=torch.int32), e(far, 1), out=e(1, 8)),
+                 lambda: moe.moe_combine_topk_backward(e(far, 8), e(far, 8), e(far, dt=torch.int32), e(far),
+                                                       out=dict(dy_perm=e(far, 8), dweight=None, dx=None)),
+                 lambda: moe.moe_dispatch_topk_backward(e(far, 8), e(far, dt=torch.int32), out=e(far, 8)),
+                 lambda: moe.sru_scan(e(1, far, 24), e(1, far, 8)),
+                 lambda: moe.sru_scan_backward(e(1, far, 8), e(1, far, 24), None, e(1, far, 8))):
+        with pytest.raises(ValueError, match="does not fit an int"):
+            call()

@@ -519,8 +519,12 @@ def _room(ws, query, *args):
     return (torch.uint8, (need,)) if need else (None, ())
 
 
-def _bytes(ws):
-    return 0 if ws is None else ws.numel()
+def _workspace(who, lead, ws, made):
+    """(workspace, bytes): the given one, which has to lie beside lead as any other tensor, or the one made."""
+    if ws is None:
+        return made, 0 if made is None else made.numel()
+    _c().expect(who, _device, lead, "ws", ws, torch.uint8, (ws.numel(),))
+    return ws, ws.numel()
 
 
 # Each call below checks that its tensors have the shapes and types that it will read and write, and that they lie on the current device, whose
@@ -605,8 +609,8 @@ def sru_scan(u, x=None, b_f=None, b_r=None, c0=None, lengths=None, want_states=F
         c.expect("sru_scan", _device, u, "h", h, t, (B, L, H), "c_last", c_last, f32, (B, H))
         _check_states("sru_scan", u, states, B, L, H)
         made, = c.fresh(u, *room)
-    ws = made if ws is None else ws
-    _check(c.sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, _bytes(ws), _stream()))
+    ws, ws_bytes = _workspace("sru_scan", u, ws, made)
+    _check(c.sru_scan(u, x, b_f, b_r, c0, lengths, B, L, H, n, dt, h, c_last, states, ws, ws_bytes, _stream()))
     return h, c_last, states
 
 
@@ -639,8 +643,8 @@ def sru_scan_backward(dh, u, states, x=None, b_f=None, b_r=None, dc_last=None, l
         c.expect("sru_scan_backward", _device, dh, "du", du, t, (B, L, n * H), "dx", dx, t, (B, L, H), "db_f", db_f, f32, (H,),
                  "db_r", db_r, f32, (H,), "dc0", dc0, f32, (B, H))
         made, = c.fresh(dh, *room)
-    ws = made if ws is None else ws
-    _check(c.sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, du, dx, db_f, db_r, dc0, ws, _bytes(ws), _stream()))
+    ws, ws_bytes = _workspace("sru_scan_backward", dh, ws, made)
+    _check(c.sru_scan_backward(dh, dc_last, u, x, b_f, b_r, states, lengths, B, L, H, n, dt, du, dx, db_f, db_r, dc0, ws, ws_bytes, _stream()))
     return out
 
 
@@ -673,9 +677,9 @@ def moe_token_logprobs(logits, target, k=0, out=None, ws=None):
                  "top_idx", top_idx, torch.int32, (N, k), "top_logprob", top_logprob, f32, (N, k))
         made, = c.fresh(logits, *room)
     rows, stride = _rows(logits)
-    ws = made if ws is None else ws
+    ws, ws_bytes = _workspace("moe_token_logprobs", logits, ws, made)
     _check(c.moe_token_logprobs(rows, stride, target, N, V, dt, k, logprob, entropy, lse, top_idx if k else None, top_logprob if k else None,
-                                ws, _bytes(ws), _stream()))
+                                ws, ws_bytes, _stream()))
     return out
 
 

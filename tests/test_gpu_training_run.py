@@ -329,3 +329,46 @@ def test_sizes_past_an_int_are_refused():
                  lambda: moe.sru_scan_backward(e(1, far, 8), e(1, far, 24), None, e(1, far, 8))):
         with pytest.raises(ValueError, match="does not fit an int"):
             call()
+
+
+def test_workspaces_lie_beside_the_tensors():
+    """A workspace of another place or type is refused as any other tensor is."""
+    import paper_2605_11537_amd as moe
+    s = _buffers(moe)
+    for ws in (s["ws"].cpu(), s["ws"].view(torch.float32)):
+        for call in (lambda: moe.sru_scan(s["u"], s["x"], ws=ws), lambda: moe.sru_scan_backward(s["dh"], s["u"], s["scan"][2], s["x"], ws=ws),
+                     lambda: moe.moe_token_logprobs(s["logits"], s["target"], ws=ws)):
+            with pytest.raises(ValueError, match="ws "):
+                call()
+
+
+def test_captured_with_tensors_of_its_own():
+    """A graph whose calls allocate their outputs and workspaces themselves, replayed on new inputs between eager calls."""
+    import paper_2605_11537_amd as moe
+
+    def chain(s):
+        h, c, states = moe.sru_scan(s["u"], s["x"], s["b"], s["b"], s["c0"], s["len"], want_states=True)
+        grads = moe.sru_scan_backward(s["dh"], s["u"], states, s["x"], s["b"], s["b"], s["dc"], s["len"])
+        score = moe.moe_token_logprobs(s["logits"], s["target"], 4)
+        slope = moe.moe_token_logprobs_backward(s["logits"], s["target"], score["lse"], score["entropy"], s["q"], s["q"])
+        back = moe.moe_combine_topk_backward(s["dout"], s["y"], s["inv"], s["w"])
+        dx = moe.moe_dispatch_topk_backward(s["y"], s["inv"], back["dx"])
+        gate = moe.moe_route_topk_backward(s["gate"], s["idx"], back["dweight"])
+        return [h, c, *grads.values(), *score.values(), slope, *back.values(), dx, gate]
+
+    s, other = _buffers(moe), _buffers(moe)
+    _fill(s, 40)
+    chain(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = chain(s)
+    for seed in range(41, 45):
+        _fill(other, seed)
+        want = [t.clone() for t in chain(other)]
+        _fill(s, seed)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a, b), (seed, i)

@@ -159,8 +159,8 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
     }
 }
 
-// LANES lanes per token, RB_LOGITS logits a lane in registers (one wavefront to every token and 1024 places asked: 61 us for 65536 x 256); PIECES: four consecutive ones (rows begin on 16 bytes).  With renormalize the
-// other experts' logits take no part and are not read.
+// LANES lanes per token, RB_LOGITS logits a lane in registers (one wavefront to every token and 1024 places asked: 61 us for 65536 x 256); PIECES:
+// four consecutive ones (rows begin on 16 bytes).  With renormalize the other experts' logits take no part and are not read.
 constexpr int RB_LOGITS = 16;
 
 template <int LANES, bool PIECES>
@@ -287,7 +287,11 @@ extern "C" int moe_combine_topk_backward(const void *dout, const void *y_perm, c
                 "moe_combine_topk_backward: tensor misaligned");
     const int vec = (int)((size_t)d * (dtype == MOE_F32 ? 4 : 2) / 16);
     const int lg = combine_backward_lanes(T, k, vec), wide = lg < 0;
-#define MOE_CMB_BACK(B) (wide ? combine_backward_kernel<B, 3, 1> : k == 1 ? combine_backward_kernel<B, 1, 1> : k <= 4 ? combine_backward_kernel<B, 1, 4> : combine_backward_kernel<B, 1, MOE_MAX_TOPK>)
+#define MOE_CMB_BACK(B)                                               \
+    (wide     ? combine_backward_kernel<B, 3, 1>                      \
+     : k == 1 ? combine_backward_kernel<B, 1, 1>                      \
+     : k <= 4 ? combine_backward_kernel<B, 1, 4>                      \
+              : combine_backward_kernel<B, 1, MOE_MAX_TOPK>)
     auto kern = dtype == MOE_BF16 ? MOE_CMB_BACK(true) : MOE_CMB_BACK(false);
 #undef MOE_CMB_BACK
     hipLaunchKernelGGL(kern, rows_grid(T, wide ? 5 : lg), dim3(RB_THREADS), 0, (hipStream_t)stream, (const rb_u32x4_t *)dout,

@@ -594,9 +594,12 @@ extern "C" int sru_scan_backward(const void *dh, const float *dc_last, const voi
     if (B > 0) {
         const int cleared = scan_clear(g, tiles, dc_last, st, "sru_scan_backward");
         if (cleared != MOE_OK) return cleared;
-#define MOE_SCAN(T, HW)                                                                                                                    \
-    hipLaunchKernelGGL((g.tiles > 1 ? sru_scan_backward_kernel<T, HW, true, SCAN_SAVED> : g.steps == SCAN_SAVED ? sru_scan_backward_kernel<T, HW, false, SCAN_SAVED> : sru_scan_backward_kernel<T, HW, false, 1>), scan_grid(g), dim3(g.waves *g.pack *WAVE), 0, st, g, (const T *)dh, dc_last, (const T *)u, \
-                       (const T *)x, b_f, b_r, (const float *)states, lengths, tiles.ticket, tiles.words, (T *)du, (T *)dx, db, dc0)
+#define MOE_SCAN(T, HW)                                                                                                                             \
+    hipLaunchKernelGGL((g.tiles > 1             ? sru_scan_backward_kernel<T, HW, true, SCAN_SAVED>                                                 \
+                        : g.steps == SCAN_SAVED ? sru_scan_backward_kernel<T, HW, false, SCAN_SAVED>                                                \
+                                                : sru_scan_backward_kernel<T, HW, false, 1>),                                                       \
+                       scan_grid(g), dim3(g.waves *g.pack *WAVE), 0, st, g, (const T *)dh, dc_last, (const T *)u, (const T *)x, b_f, b_r,           \
+                       (const float *)states, lengths, tiles.ticket, tiles.words, (T *)du, (T *)dx, db, dc0)
 #define MOE_MAIN(T)                              \
     do {                                            \
         if (n_blocks == 3) MOE_SCAN(T, true);    \

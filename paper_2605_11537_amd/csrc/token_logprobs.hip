@@ -503,7 +503,11 @@ static void logprobs_launch(const LogprobShape &g, const X *logits, size_t strid
     if (g.lanes) {
         const bool pieces = ((uintptr_t)logits & 15) == 0 && stride * sizeof(X) % 16 == 0;
         const dim3 grid(ceil_div(N, LP_THREADS / g.lanes)), threads(LP_THREADS);
-#define MOE_SHORT(L)                                                                                                                          do {                                                                                                                                          if (pieces) hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, true>), grid, threads, 0, st, logits, stride, target, N, V, k, out);         else hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, false>), grid, threads, 0, st, logits, stride, target, N, V, k, out);       } while (0)
+#define MOE_SHORT(L)                                                                                                                                \
+    do {                                                                                                                                            \
+        if (pieces) hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, true>), grid, threads, 0, st, logits, stride, target, N, V, k, out);      \
+        else hipLaunchKernelGGL((token_logprobs_short_kernel<X, L, false>), grid, threads, 0, st, logits, stride, target, N, V, k, out);            \
+    } while (0)
         if (g.lanes == 4) MOE_SHORT(4);
         else if (g.lanes == 16) MOE_SHORT(16);
         else MOE_SHORT(64);

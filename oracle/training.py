@@ -121,11 +121,12 @@ def dispatch_backward(dx_perm, inv, dx_add):
 
 
 def route_weights(logits, idx, renormalize):
-    """The weights [k,T] of moe_route_topk for given ids."""
-    p = np.exp(logits - logits.max(1, keepdims=True))
-    p /= p.sum(1, keepdims=True)
-    w = np.stack([p[np.arange(len(p)), i] for i in idx])
-    return w / w.sum(0) if renormalize else w
+    """The weights [k,T] of moe_route_topk for given ids.  Renormalised they are the softmax of the chosen logits: a quotient of probabilities that
+    have underflowed would be none."""
+    chosen = np.stack([logits[np.arange(len(logits)), i] for i in idx])
+    top = (chosen.max(0) if renormalize else logits.max(1))[None, :]
+    w = np.exp(chosen - top)
+    return w / (w.sum(0) if renormalize else np.exp(logits - top.T).sum(1))
 
 
 def route_backward(logits, idx, dweight, renormalize):

@@ -1,6 +1,8 @@
 // The gradient of sorting tokens by expert and back: moe_combine_topk_backward, moe_dispatch_topk_backward, moe_route_topk_backward.
 // Rows are moved once and memory binds.  65536 tokens of 768 bf16, one choice: combine 76 us (5.0 TB/s), dispatch 56 us (5.2 TB/s), the gate over 256
 // experts 27 us (5.0 TB/s); 4096 tokens, three choices: 10 and 7 us, of which launch and first load are half.
+#include <float.h>
+
 #include "row_groups.h"
 #include "scalar_math.h"
 
@@ -159,6 +161,8 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
     }
 }
 
+// The largest logit is never below the lowest finite value: a row (with renormalize, its chosen logits) that is masked throughout has exponentials of
+// 0, a total of 0 and a gradient of 0, and no infinity is taken from another.  A NaN passes into the total.
 // LANES lanes per token, RB_LOGITS logits a lane in registers (one wavefront to every token and 1024 places asked: 61 us for 65536 x 256); PIECES:
 // four consecutive ones (rows begin on 16 bytes).  With renormalize the other experts' logits take no part and are not read.
 constexpr int RB_LOGITS = 16;
@@ -176,7 +180,7 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
     const float *row = logits + (size_t)s * E;
     int e[MOE_MAX_TOPK];
     float dw[MOE_MAX_TOPK], w[MOE_MAX_TOPK];
-    float top = -INFINITY;
+    float top = -FLT_MAX;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
         e[j] = -1, dw[j] = 0.f, w[j] = -INFINITY;
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
         w[j] = e[j] >= 0 ? exp_of<true>(w[j] - top) : 0.f;
         if (renormalize) total += w[j];
     }
-    const float share = 1.f / total;
+    const float share = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
         if (j >= k) continue;

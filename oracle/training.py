@@ -174,7 +174,9 @@ def token_logprobs_backward(logits, target, dlogprob, dentropy):
     for n in range(N):
         if fw["lse"][n] == -np.inf:
             continue
-        lp = logits[n] - fw["lse"][n]
+        # under the maximum: beside 3e38, float64's lse too has lost the logarithm of the sum
+        lp = logits[n] - logits[n].max()
+        lp = lp - np.log(np.exp(lp).sum())
         p = np.exp(lp)
         on = p > 0
         d[n, on] = -dentropy[n] * p[on] * (lp[on] + fw["entropy"][n])

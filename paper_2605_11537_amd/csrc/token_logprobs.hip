@@ -401,16 +401,19 @@ __global__ __launch_bounds__(WAVE) void token_logprobs_join_kernel(const float *
     }
 }
 
-// The gradient, elementwise: -p (g + q (log p + H)), and g more at the target.
+// The gradient, elementwise: -p (g + q (log p + H)), and g more at the target.  log p = x - lse - rest: lse = m + log s has been rounded, and beside a
+// large m that takes a part of log s or all of it.  rest is what the row's own sum then says, log sum e^(x - lse); 0 where lse holds.
 template <class X>
 struct LogprobSlope {
     static constexpr bool PRECISE = sizeof(X) == 4;
-    float lse, base, q, g;
+    // from where a row is summed again: an lse below is off by 2^-19 (binary32) or 2^-14 (bfloat16, whose results round by 2^-8) at most
+    static constexpr float FAR = PRECISE ? 64.f : 2048.f;
+    float lse, rest, base, q, g;
     int target;
     bool none;
     __device__ __forceinline__ float at(float x, int i) const
     {
-        const float lp = x - lse, p = exp_of<PRECISE>(lp);
+        const float lp = x - lse - rest, p = exp_of<PRECISE>(lp);
         float d = p * fmaf(-q, lp, base);
         d = p == 0.f || none ? 0.f : d;                  // a masked logit: log p is no number to multiply with
         return i == target && !none ? d + g : d;
@@ -419,7 +422,9 @@ struct LogprobSlope {
 
 constexpr int LP_SLOPE_PIECES = 4;     // pieces of a thread
 
-// 2^lg threads share a row; blockIdx.y: its run of 2^lg * LP_SLOPE_PIECES pieces
+// 2^lg threads share a row; blockIdx.y: its run of 2^lg * LP_SLOPE_PIECES pieces.  A row far from zero is the first run's alone, which reads it twice (8192 x
+// 20000 fp32 259 us, all rows far 396; 8192 x 50257 bf16 340 and 751; 4 x 131072 fp32 5 and 139).  dlogits may lie on it, so all of it is read before any is
+// written: by the threads of one wavefront, or by the workgroup with a barrier, which the two rows of a workgroup do not share.
 template <class X>
 __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(const X *logits, size_t stride, const int32_t *__restrict__ target,
                                                                              const float *__restrict__ lse, const float *__restrict__ entropy,
@@ -428,6 +433,7 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(con
 {
     typedef LogitPiece<X> piece;
     constexpr int P = piece::N;
+    __shared__ float wave_sum[LP_THREADS / WAVE];
     const unsigned n = blockIdx.x * (LP_THREADS >> lg) + (threadIdx.x >> lg);
     const int lanes = 1 << lg, lane = threadIdx.x & (lanes - 1);
     if (n >= (unsigned)N) return;
@@ -440,6 +446,24 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(con
     f.g = f.target < 0 || f.target >= V ? 0.f : dlogprob[n];
     f.q = dentropy ? dentropy[n] : 0.f;
     f.base = -f.g - (dentropy ? f.q * entropy[n] : 0.f);
+    f.rest = 0.f;
+    if (fabsf(f.lse) >= f.FAR && !f.none) {              // the whole group of threads
+        const int sharers = lanes < LP_THREADS ? min(lanes, WAVE) : LP_THREADS;
+        if (blockIdx.y != 0 || lane >= sharers) return;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int c = lane; c < V; c += sharers) sum += exp_of<true>(value_of(row[c]) - f.lse);
+        for (int o = 1; o < sharers && o < WAVE; o <<= 1) sum += __shfl_xor(sum, o, WAVE);
+        if (sharers > WAVE) {
+            if (lane % WAVE == 0) wave_sum[lane / WAVE] = sum;
+            __syncthreads();
+            sum = 0.f;
+            for (int w = 0; w < LP_THREADS / WAVE; ++w) sum += wave_sum[w];
+        }
+        f.rest = logf(sum);
+        for (int c = lane; c < V; c += sharers) store_value(out + c, f.at(value_of(row[c]), c));
+        return;
+    }
     const int run = lanes * LP_SLOPE_PIECES;
     if ((((uintptr_t)row ^ (uintptr_t)out) & 15) == 0) {
         const int head = min(V, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(X)), pieces = (V - head) / P;

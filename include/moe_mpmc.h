@@ -358,6 +358,9 @@ int moe_route_topk_backward(const float *logits, const int32_t *expert_idx, cons
  * h [B, L, H] in dtype, rows behind a sequence's end zero; c_last [B, H] the state after its last token.  States and
  * all arithmetic are binary32.  b_f, b_r [H] binary32, c0 and lengths [B] (int32, taken to 0..L; NULL: all L) may be
  * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H up to 2^22.
+ * Infinities and NaN go through as in these formulas; f stays above 0, so an infinite state stays, and 1-f reaches 0
+ * from a pre-activation of 87 on, where an infinite u0 gives NaN as 0*infinity does.  In bfloat16 the gates' exponents
+ * are rounded once (f and 1-f are off by 2^-23 |pre-activation| of themselves), and tanh is off by up to 2.5e-5 of itself.
  * states (NULL, or sru_scan_states_bytes): what sru_scan_backward needs beside the inputs.
  *
  * sru_scan_backward -- from dh = dL/dh and dc_last = dL/dc_last (binary32, NULL: 0): du [B, L, n_blocks*H], dx [B, L, H]

@@ -1,9 +1,9 @@
 """Plain float64 forms of the gradients and of the calls that train the gate and the predictor, token by token or row by row.
 
 Arguments are float64 numpy arrays (index arrays: integers); nothing is rounded.  Beside a value, the scan gives a bound for the error
-of a binary32 evaluation: ``steps`` half-units in the last place (2^-24) relative for every gate, product and sum, carried along the same recurrence.  With ``bf16``, the bound of what bfloat16 results are made from:
-c = z + f (c - z) and h = w + r (tanh c - w) round the differences and have 1 - f and 1 - r from f and r, 4 half-units of the terms' own
-magnitudes, and tanh is off by up to 2.5e-5 of itself.
+of a binary32 evaluation: ``steps`` half-units in the last place (2^-24) relative for every gate, product and sum, carried along the same recurrence.  With ``bf16``, a wider one, which also holds
+for c = z + f (c - z) and h = w + r (tanh c - w): these round the differences and have 1 - f and 1 - r from f and r, 4 half-units of the values' own
+magnitudes; and tanh may be off by 2.5e-5 of itself.
 """
 from __future__ import annotations
 

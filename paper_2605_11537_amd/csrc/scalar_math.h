@@ -20,32 +20,18 @@ __device__ __forceinline__ float exp_of(float x)
     return fabsf(x) < 126.f ? fmaf(e, low * LN2, e) : e;
 }
 
-// A gate's bias as gate_of and gate_open take it: without PRECISE -b log2(e), so that the exponent is one multiply-add of the
-// pre-activation.
+// A gate's bias as gate_of takes it: without PRECISE -b log2(e), so that the exponent is one multiply-add of the pre-activation.
 template <bool PRECISE>
 __device__ __forceinline__ float gate_bias(float b) { return PRECISE ? b : -LOG2E * b; }
 
-// s = 1 / (1 + e^-(a + b))
-template <bool PRECISE>
-__device__ __forceinline__ float gate_open(float a, float bias)
-{
-    const float e = PRECISE ? exp_of<true>(-(a + bias)) : __builtin_amdgcn_exp2f(fmaf(a, -LOG2E, bias));
-    return __builtin_amdgcn_rcpf(1.f + e);
-}
-
-// The same with 1 - s, each with its own relative accuracy (1 - s taken from s would have lost a closed gate's bits).  The exponential is kept
-// finite, so that the second is no infinity times zero: neither goes below e^-80; a NaN passes.
+// s = 1 / (1 + e^-(a + b)) and 1 - s, each with its own relative accuracy (1 - s taken from s would have lost a closed gate's bits).  The exponential
+// is kept finite, so that 1 - s is no infinity times zero: s stays at e^-80 or above.  1 - s does reach 0, from a + b = 87 on.  A NaN passes.
 template <bool PRECISE>
 __device__ __forceinline__ void gate_of(float a, float bias, float &s, float &rest)
 {
     float e;
-    if (PRECISE) {
-        const float z = a + bias;
-        e = exp_of<true>(z < -80.f ? 80.f : -z);
-    } else {
-        const float y = fmaf(a, -LOG2E, bias);
-        e = __builtin_amdgcn_exp2f(y > 115.4f ? 115.4f : y);
-    }
+    if (PRECISE) e = exp_of<true>(__builtin_elementwise_minimum(-(a + bias), 80.f));
+    else e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(fmaf(a, -LOG2E, bias), 115.4f));
     s = __builtin_amdgcn_rcpf(1.f + e);
     rest = e * s;
 }

@@ -13,6 +13,8 @@
 // One channel a lane: two (in bfloat16 a 4-byte load) took 65 and 124 us for the first, with half the workgroups and more registers.  The next
 // round's rows asked for a round ahead: 70 us, with one workgroup less on a compute unit.  Outputs written past the caches: the calls 6 %
 // faster, the products that read them slower by as much.
+#include <float.h>
+
 #include "scalar_math.h"
 #include "sru_scan_rules.h"
 
@@ -94,26 +96,24 @@ __device__ __forceinline__ void scan_load(T (&to)[STEPS], scan_rows_t rows, unsi
     }
 }
 
-// c_t from c_{t-1}: f c + (1 - f) z with both gates' own accuracy, or z + f (c - z) for bfloat16 results
+// c_t from c_{t-1}: f c + (1 - f) z with both gates' own accuracy.  A blend, z + f (c - z), is an operation shorter, but rounds by the larger of the two
+// where the gate leaves little of it, and takes an infinity from itself.
 template <bool PRECISE>
 struct ScanForward {
     float f, in;
     __device__ __forceinline__ void make(float a, float bias, float z)
     {
-        if (PRECISE) {
-            float rest;
-            gate_of<true>(a, bias, f, rest);
-            in = rest * z;
-        } else {
-            f = gate_open<false>(a, bias);
-            in = z;
-        }
+        float rest;
+        gate_of<PRECISE>(a, bias, f, rest);
+        in = rest * z;
     }
-    __device__ __forceinline__ float next(float c) const { return PRECISE ? fmaf(f, c, in) : fmaf(f, c - in, in); }
+    __device__ __forceinline__ float next(float c) const { return fmaf(f, c, in); }
 };
 
+// A product of gates that underflows stays above 0: an infinite state times it is that state.
+__device__ __forceinline__ float scan_product(float a) { return fmaxf(a, FLT_TRUE_MIN); }
 // what leads from the state before a run to the state behind two runs
-__device__ __forceinline__ float2 scan_then(float2 a, float2 b) { return make_float2(b.x * a.x, fmaf(b.x, a.y, b.y)); }
+__device__ __forceinline__ float2 scan_then(float2 a, float2 b) { return make_float2(scan_product(b.x * a.x), fmaf(b.x, a.y, b.y)); }
 __device__ __forceinline__ float scan_through(float2 a, float c) { return fmaf(a.x, c, a.y); }
 
 // Pairs of tiles in memory.  A pair is one word of 64 bits, written and read whole by atomic operations of device scope (the eight L2 caches do
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
         };
         if (count >= STEPS) gates(ScanFull());
         else gates(ScanPart());
-        sums[parity][p.base + p.wave][p.lane] = make_float2(A, C);
+        sums[parity][p.base + p.wave][p.lane] = make_float2(scan_product(A), C);
         __syncthreads();
         float2 all = make_float2(1.f, 0.f), before = all;
         for (int j = 0; j < p.waves; ++j) {
@@ -294,15 +294,9 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
                 }
                 c = s[i].next(c);
                 const float wv = value_of(w[i]), t = tanh_of<PRECISE>(c);
-                float out;
-                if (PRECISE) {
-                    float on, rest;
-                    gate_of<true>(value_of(r[i]), br, on, rest);
-                    out = fmaf(on, t, rest * wv);
-                } else {
-                    out = fmaf(gate_open<false>(value_of(r[i]), br), t - wv, wv);
-                }
-                scan_put<T>(out, hr, p.at, i * p.block);
+                float on, rest;
+                gate_of<PRECISE>(value_of(r[i]), br, on, rest);
+                scan_put<T>(fmaf(on, t, rest * wv), hr, p.at, i * p.block);
             }
         };
         if (count >= STEPS) outputs(ScanFull());
@@ -392,7 +386,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
         };
         if (count >= STEPS) forward(ScanFull());
         else forward(ScanPart());
-        sums[parity][p.base + p.wave][p.lane] = make_float2(A, D);
+        sums[parity][p.base + p.wave][p.lane] = make_float2(scan_product(A), D);
         __syncthreads();
         float2 all = make_float2(1.f, 0.f), before = all;
         for (int j = p.waves - 1; j >= 0; --j) {

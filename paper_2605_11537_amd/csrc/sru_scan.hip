@@ -1,6 +1,7 @@
 // sru_scan and its gradient: the recurrence of an SRU layer over pre-activations that lie in memory.
 //
 // c_t = f_t c_{t-1} + b_t composes: a run of steps is a pair (A, C), c_out = A c_in + C, and the pair of two runs is (A2 A1, A2 C1 + C2).
+// 1 - A goes along with its own accuracy (ScanRun): a channel that forgets little is all in it.
 // The gradient dc_{t-1} = f_t (dc_t + e_t) is the same from the other end.  So a wavefront takes 8 or 16 steps of 64 lanes' channels with
 // everything they read in registers, finds its pair from zero, and learns its start from the pairs of the wavefronts before it, through
 // LDS: the wavefronts of a workgroup lie one behind the other on the sequence, and a round of them is read once and written once.
@@ -8,8 +9,8 @@
 // from tile to tile through memory: see scan_look_back.
 //
 // Memory binds: 10 bytes a channel and step forward in bfloat16, 18 backward (and half a byte of saved states each), against some 30 and 50 vector
-// operations, six of them transcendental.  Measured, bfloat16 with the highway: 64 x 512 x 768 forward 58 us (4.5 TB/s), gradient 107 us (4.3
-// TB/s); 2 x 16384 x 768 in tiles 73 us (3.5 TB/s) and 126 us (3.7 TB/s); 1 x 300 x 256 9 and 14 us, two and three launches.
+// operations, six of them transcendental.  Measured, bfloat16 with the highway: 64 x 512 x 768 forward 59 us (4.4 TB/s), gradient 107 us (4.3
+// TB/s); 2 x 16384 x 768 in tiles 73 us (3.5 TB/s) and 125 us (3.7 TB/s); 1 x 300 x 256 8.4 and 13 us, two and three launches.
 // One channel a lane: two (in bfloat16 a 4-byte load) took 65 and 124 us for the first, with half the workgroups and more registers.  The next
 // round's rows asked for a round ahead: 70 us, with one workgroup less on a compute unit.  Outputs written past the caches: the calls 6 %
 // faster, the products that read them slower by as much.
@@ -50,11 +51,12 @@ struct ScanPlace {
     unsigned ch, col;                                       // this lane's channel; one that exists
     unsigned at, block;                                     // its offset in a row of one block, and a block's length, in bytes
     bool on;
-    template <bool TILES>
+    // WHOLE: a tile's eight wavefronts as a constant, where that is no slower (2 x 16384 x 768 bf16: gradient 128 -> 125 us; the forward of 16 steps 72 -> 80)
+    template <bool TILES, bool WHOLE>
     __device__ __forceinline__ void find(const ScanShape &g, const int32_t *lengths, unsigned line, int which)
     {
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-        waves = g.waves;
+        waves = WHOLE ? SCAN_MAX_WAVES : g.waves;
         wave = TILES ? w : w & (waves - 1);
         base = w - wave;
         if (!TILES) line = line * g.pack + (w >> g.waves_lg);
@@ -101,22 +103,46 @@ __device__ __forceinline__ void scan_load(T (&to)[STEPS], scan_rows_t rows, unsi
 template <bool PRECISE>
 struct ScanForward {
     float f, in;
-    __device__ __forceinline__ void make(float a, float bias, float z)
+    __device__ __forceinline__ float make(float a, float bias, float z)     // -> 1 - f
     {
         float rest;
         gate_of<PRECISE>(a, bias, f, rest);
         in = rest * z;
+        return rest;
     }
     __device__ __forceinline__ float next(float c) const { return fmaf(f, c, in); }
 };
 
-// A product of gates that underflows stays above 0: an infinite state times it is that state.
-__device__ __forceinline__ float scan_product(float a) { return fmaxf(a, FLT_TRUE_MIN); }
-// what leads from the state before a run to the state behind two runs
-__device__ __forceinline__ float2 scan_then(float2 a, float2 b) { return make_float2(scan_product(b.x * a.x), fmaf(b.x, a.y, b.y)); }
-__device__ __forceinline__ float scan_through(float2 a, float c) { return fmaf(a.x, c, a.y); }
+// What leads from the state before a run to the state behind it: c -> A c + C, R = 1 - A.  Gates near 1 are rounded by 2^-25 each, always the same way
+// where they do not change, and a product of them has drifted by as much a step: held against R, whose sum of small shares has its own relative
+// accuracy, a state would settle beside where its inputs are (1.1e-3 off after 10^5 steps of f = 1 - e^-9; with R 5e-7).
+struct ScanRun {
+    float A, R, C;
+};
+__device__ __forceinline__ ScanRun scan_none() { return {1.f, 0.f, 0.f}; }
+// A product that underflows stays above 0: an infinite state times it is that state.
+__device__ __forceinline__ float scan_kept(float a) { return fmaxf(a, FLT_TRUE_MIN); }
+// a run of steps from its product, its shares and its state from zero
+__device__ __forceinline__ ScanRun scan_run(float a, float r, float c) { return {r < 0.5f ? 1.f - r : scan_kept(a), r, c}; }
+// a, then b, whose A is above 0
+__device__ __forceinline__ ScanRun scan_then(ScanRun a, ScanRun b) { return {b.A * a.A, fmaf(b.R, a.A, a.R), fmaf(b.A, a.C, b.C)}; }
+// The state behind it.  c + (C - R c) rounds once by c's last place, where A c + C would round A and the product; an infinite state would be taken from
+// itself.
+__device__ __forceinline__ float scan_through(ScanRun a, float c)
+{
+    const float slow = c + fmaf(-a.R, c, a.C), fast = fmaf(scan_kept(a.A), c, a.C);
+    return a.R < 0.5f && fabsf(c) <= FLT_MAX ? slow : fast;
+}
+// In two words: minus R, which has the sign bit even at 0, or A.
+__device__ __forceinline__ float2 scan_packed(ScanRun a) { return make_float2(a.R < 0.5f ? -a.R : scan_kept(a.A), a.C); }
+__device__ __forceinline__ ScanRun scan_unpacked(float2 p)
+{
+    const float v = fabsf(p.x), w = 1.f - v;
+    const bool r = __float_as_int(p.x) < 0;
+    return {r ? w : v, r ? v : w, p.y};
+}
 
-// Pairs of tiles in memory.  A pair is one word of 64 bits, written and read whole by atomic operations of device scope (the eight L2 caches do
+// Pairs of tiles in memory: a scan in one pass by decoupled look-back, in an arrangement with runs and stretches of tiles.  A pair is one word of 64 bits, written and read whole by atomic operations of device scope (the eight L2 caches do
 // not see each other's ordinary writes), and SCAN_UNKNOWN until then: the word is its own flag, so no order between two words is relied on.
 // A workgroup draws its tile with a ticket, tile 0 of all chains first, and waits only for tiles whose tickets were drawn before its own: their
 // workgroups run already, and publish their own pair before they wait themselves.  So the tile of the lowest unfinished ticket waits for no one,
@@ -155,22 +181,24 @@ __device__ __forceinline__ float2 scan_await(const unsigned long long *word, uns
     return __builtin_bit_cast(float2, v);                // what never came is two NaNs
 }
 // the pairs of up to two neighbours, the first count of them
-__device__ __forceinline__ float2 scan_await_two(const unsigned long long *words, unsigned long long v0, unsigned long long v1, int count)
+__device__ __forceinline__ ScanRun scan_await_two(const unsigned long long *words, unsigned long long v0, unsigned long long v1, int count)
 {
-    float2 a = make_float2(1.f, 0.f);
-    if (count > 0) a = scan_await(words, v0);
-    if (count > 1) a = scan_then(a, scan_await(words + WAVE, v1));
+    ScanRun a = scan_none();
+    if (count > 0) a = scan_unpacked(scan_await(words, v0));
+    if (count > 1) a = scan_then(a, scan_unpacked(scan_await(words + WAVE, v1)));
+    a.A = scan_kept(a.A);
     return a;
 }
 
 // The state at the start of the tile at `at` (its place in the order of the recurrence), from the sequence's own start and the tile's pair, which
 // every wavefront knows.  Each wavefront looks for two tiles and two runs.
-__device__ float scan_look_back(const ScanChain &chain, int tiles, int at, int lane, int wave, float2 own, float start,
-                                float2 (*of_tiles)[WAVE], float2 (*of_runs)[WAVE])
+__device__ float scan_look_back(const ScanChain &chain, int tiles, int at, int lane, int wave, ScanRun own, float start,
+                                ScanRun (*of_tiles)[WAVE], ScanRun (*of_runs)[WAVE])
 {
+    own.A = scan_kept(own.A);
     const int run = at / SCAN_RUN, in_run = at % SCAN_RUN, stretch = run / SCAN_RUN, in_stretch = run % SCAN_RUN;
     const bool last = at + 1 == tiles;
-    if (wave == 0 && !last && in_run + 1 < SCAN_RUN) scan_publish(chain.tiles + (size_t)at * WAVE + lane, own);
+    if (wave == 0 && !last && in_run + 1 < SCAN_RUN) scan_publish(chain.tiles + (size_t)at * WAVE + lane, scan_packed(own));
     const unsigned long long *t = chain.tiles + ((size_t)run * SCAN_RUN + 2 * wave) * WAVE + lane;
     const unsigned long long *r = chain.runs + ((size_t)stretch * SCAN_RUN + 2 * wave) * WAVE + lane;
     const unsigned long long *s = chain.stretches + (size_t)(stretch > 0 ? stretch - 1 : 0) * WAVE + lane;
@@ -183,15 +211,17 @@ __device__ float scan_look_back(const ScanChain &chain, int tiles, int at, int l
     if (stretch > 0) s0 = scan_look(s);
     of_tiles[wave][lane] = scan_await_two(t, t0, t1, n_t);
     __syncthreads();
-    float2 before = make_float2(1.f, 0.f);
+    ScanRun before = scan_none();
     for (int w = 0; w < SCAN_MAX_WAVES; ++w) before = scan_then(before, of_tiles[w][lane]);
-    const float2 whole = scan_then(before, own);         // a run's pair needs no other run's, and is out before one is waited for
+    const ScanRun whole = scan_then(before, own);        // a run's pair needs no other run's, and is out before one is waited for
     const bool ends = !last && in_run + 1 == SCAN_RUN, ends_stretch = ends && in_stretch + 1 == SCAN_RUN;
-    if (wave == 0 && ends && !ends_stretch) scan_publish(chain.runs + (size_t)run * WAVE + lane, whole);
+    if (wave == 0 && ends && !ends_stretch) scan_publish(chain.runs + (size_t)run * WAVE + lane, scan_packed(whole));
     of_runs[wave][lane] = scan_await_two(r, r0, r1, n_r);
     float c = stretch > 0 ? scan_await(s, s0).y : start;
     __syncthreads();
-    for (int w = 0; w < SCAN_MAX_WAVES; ++w) c = scan_through(of_runs[w][lane], c);
+    ScanRun runs_before = scan_none();
+    for (int w = 0; w < SCAN_MAX_WAVES; ++w) runs_before = scan_then(runs_before, of_runs[w][lane]);
+    c = scan_through(runs_before, c);
     if (wave == 0 && ends_stretch) scan_publish(chain.stretches + (size_t)stretch * WAVE + lane, make_float2(0.f, scan_through(whole, c)));
     return scan_through(before, c);
 }
@@ -234,13 +264,13 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    __shared__ float2 sums[3][SCAN_MAX_WAVES][WAVE];
+    __shared__ ScanRun sums[3][SCAN_MAX_WAVES][WAVE];
     __shared__ unsigned drawn;
     unsigned line;
     int at;
     if (!scan_draw<TILES>(g, ticket, &drawn, line, at)) return;
     ScanPlace<T> p;
-    p.template find<TILES>(g, lengths, line, at);
+    p.template find<TILES, TILES && STEPS == SCAN_SAVED>(g, lengths, line, at);
     ScanChain chain;
     if (TILES) chain.find(g, words, line);
     const size_t H = g.H, row_len = K * H;
@@ -252,7 +282,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
         const size_t row = (size_t)p.b * g.L + t0;
         T z[STEPS], a[STEPS], r[STEPS], w[STEPS];
         ScanForward<PRECISE> s[STEPS];
-        float A = 1.f, C = 0.f;
+        float A = 1.f, R = 0.f, C = 0.f;
         auto gates = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
             const scan_rows_t ur = scan_rows(u + row * row_len), xr = HIGHWAY ? scan_rows(x + row * H) : ur;
@@ -264,16 +294,16 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_kernel(ScanS
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
                 if (!scan_in<FULL>(i, count)) continue;
-                s[i].make(value_of(a[i]), bf, value_of(z[i]));
+                R = fmaf(s[i].make(value_of(a[i]), bf, value_of(z[i])), A, R);
                 A *= s[i].f;
                 C = s[i].next(C);
             }
         };
         if (count >= STEPS) gates(ScanFull());
         else gates(ScanPart());
-        sums[parity][p.base + p.wave][p.lane] = make_float2(scan_product(A), C);
+        sums[parity][p.base + p.wave][p.lane] = scan_run(A, R, C);
         __syncthreads();
-        float2 all = make_float2(1.f, 0.f), before = all;
+        ScanRun all = scan_none(), before = all;
         for (int j = 0; j < p.waves; ++j) {
             if (j == p.wave) before = all;
             all = scan_then(all, sums[parity][p.base + j][p.lane]);
@@ -332,13 +362,13 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    __shared__ float2 sums[3][SCAN_MAX_WAVES][WAVE];
+    __shared__ ScanRun sums[3][SCAN_MAX_WAVES][WAVE];
     __shared__ unsigned drawn;
     unsigned line;
     int at;
     if (!scan_draw<TILES>(g, ticket, &drawn, line, at)) return;
     ScanPlace<T> p;
-    p.template find<TILES>(g, lengths, line, g.tiles - 1 - at);
+    p.template find<TILES, TILES && STEPS == SCAN_SAVED>(g, lengths, line, g.tiles - 1 - at);
     ScanChain chain;
     if (TILES) chain.find(g, words, line);
     const size_t H = g.H, row_len = K * H;
@@ -351,7 +381,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
         const scan_rows_t ur = scan_rows(u + row * row_len), dr = scan_rows(dh + row * H), out = scan_rows(du + row * row_len);
         const scan_rows_t xr = HIGHWAY ? scan_rows(x + row * H) : ur, out_w = HIGHWAY ? scan_rows(dx + row * H) : out;
         const unsigned at_w = HIGHWAY ? p.at : p.at + 3 * p.block, row_bytes = K * p.block, w_bytes = HIGHWAY ? p.block : row_bytes;
-        float f[STEPS], rest[STEPS], e[STEPS], gap[STEPS], A = 1.f, D = 0.f;
+        float f[STEPS], rest[STEPS], e[STEPS], gap[STEPS], A = 1.f, R = 0.f, D = 0.f;
         auto forward = [&](auto how) {
             constexpr bool FULL = decltype(how)::FULL;
             T z[STEPS], a[STEPS], r[STEPS], w[STEPS], d[STEPS];
@@ -381,14 +411,15 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
             for (int i = STEPS - 1; i >= 0; --i) {
                 if (!scan_in<FULL>(i, count)) continue;
                 D = (D + e[i]) * f[i];
+                R = fmaf(rest[i], A, R);
                 A *= f[i];
             }
         };
         if (count >= STEPS) forward(ScanFull());
         else forward(ScanPart());
-        sums[parity][p.base + p.wave][p.lane] = make_float2(scan_product(A), D);
+        sums[parity][p.base + p.wave][p.lane] = scan_run(A, R, D);
         __syncthreads();
-        float2 all = make_float2(1.f, 0.f), before = all;
+        ScanRun all = scan_none(), before = all;
         for (int j = p.waves - 1; j >= 0; --j) {
             if (j == p.wave) before = all;
             all = scan_then(all, sums[parity][p.base + j][p.lane]);
@@ -415,11 +446,12 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
     if (!db) return;
     // the wavefronts' sums in their order, a row of [2 H] for each sequence and tile
     __syncthreads();
-    sums[0][p.base + p.wave][p.lane] = make_float2(sum_f, sum_r);
+    float2 (*const biases)[WAVE] = reinterpret_cast<float2 (*)[WAVE]>(sums);
+    biases[p.base + p.wave][p.lane] = make_float2(sum_f, sum_r);
     __syncthreads();
     if (p.wave != 0 || !p.on) return;
     for (int j = 1; j < p.waves; ++j) {
-        const float2 q = sums[0][p.base + j][p.lane];
+        const float2 q = biases[p.base + j][p.lane];
         sum_f += q.x;
         sum_r += q.y;
     }

@@ -391,7 +391,8 @@ int sru_scan_backward(const void *dh, const float *dc_last, const void *u, const
  *     among equals, and their log probabilities (0 <= k <= min(MOE_MAX_TOPK, V); NULL with k = 0)
  * Logits of -infinity are masked: probability 0, nothing to the entropy.  Where all are, log probabilities and lse are
  * -infinity and the entropy is 0.  A NaN or +infinity makes the row's numbers NaN; among the alternatives a NaN counts as
- * masked.  Sums in binary32, in an order that the shape fixes.  V <= 2^21.
+ * masked.  Sums in binary32, in an order that the shape fixes.  V <= 2^21; N up to 2^28 for V <= 64, 2^26 up to 256,
+ * 2^24 up to 1024 and 2^21 beyond (more where a launch holds their threads).
  * moe_token_logprobs_backward -- dL/dlogits (dtype) from dlogprob [N] and dentropy [N] (NULL: 0), with the lse and
  * entropy that the forward wrote (entropy may be NULL without dentropy):
  *     dlogits_i = g ([i = target] - p_i) - dentropy p_i (log p_i + entropy),   g = dlogprob, 0 for a padded position

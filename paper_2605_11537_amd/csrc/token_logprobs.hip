@@ -420,8 +420,6 @@ struct LogprobSlope {
     }
 };
 
-constexpr int LP_SLOPE_PIECES = 4;     // pieces of a thread
-
 // 2^lg threads share a row; blockIdx.y: its run of 2^lg * LP_SLOPE_PIECES pieces.  A row far from zero is the first run's alone, which reads it twice (8192 x
 // 20000 fp32 259 us, all rows far 396; 8192 x 50257 bf16 340 and 751; 4 x 131072 fp32 5 and 139).  dlogits may lie on it, so all of it is read before any is
 // written: by the threads of one wavefront, or by the workgroup with a barrier, which the two rows of a workgroup do not share.
@@ -580,10 +578,9 @@ extern "C" int moe_token_logprobs_backward(const void *logits, long long row_str
                 "moe_token_logprobs_backward: null pointer");
     MOE_REQUIRE(dlogits != logits || dlogits_stride == row_stride, MOE_ERR_INVALID_ARG,
                 "moe_token_logprobs_backward: dlogits lies on logits with another stride");
-    const int size = dtype == MOE_F32 ? 4 : 2, pieces = V / (16 / size) + 1;
+    static_assert(LP_THREADS == 1 << LP_SLOPE_LG, "");
+    const int size = dtype == MOE_F32 ? 4 : 2, pieces = logprob_slope_pieces(V, dtype), lg = logprob_slope_lanes(V, dtype);
     MOE_REQUIRE((uintptr_t)logits % size == 0 && (uintptr_t)dlogits % size == 0, MOE_ERR_INVALID_ARG, "moe_token_logprobs_backward: tensor misaligned");
-    int lg = 0;
-    while ((1 << lg) < LP_THREADS && (LP_SLOPE_PIECES << lg) < pieces) ++lg;
     const dim3 grid(ceil_div(N, LP_THREADS >> lg), ceil_div(pieces, LP_SLOPE_PIECES << lg));
     hipStream_t st = (hipStream_t)stream;
     if (dtype == MOE_BF16)

@@ -44,14 +44,25 @@ static inline LogprobShape logprob_shape(int N, int V, int dtype)
     return g;
 }
 
+// The gradient: log2 of the threads that share a row, LP_SLOPE_PIECES pieces of 16 bytes each; what does not fit them goes to further workgroups.
+constexpr int LP_SLOPE_PIECES = 4;
+constexpr int LP_SLOPE_LG = 8;                // a workgroup of 256
+static inline int logprob_slope_pieces(int V, int dtype) { return V / (dtype == MOE_BF16 ? 8 : 4) + 1; }
+static inline int logprob_slope_lanes(int V, int dtype)
+{
+    int lg = 0;
+    while (lg < LP_SLOPE_LG && (LP_SLOPE_PIECES << lg) < logprob_slope_pieces(V, dtype)) ++lg;
+    return lg;
+}
+
 // a launch holds fewer than 2^32 threads in a dimension: short rows `lanes` each, long ones a workgroup each and their parts across the other
-// dimension; the gradient gives a row at most 256 threads
+// dimension; the gradient's 2^lg
 static inline bool logprob_takes(int N, int V, int dtype)
 {
     if (V > LP_MAX_V) return false;
     const LogprobShape g = logprob_shape(N > 0 ? N : 1, V, dtype);
-    const int each = g.lanes ? g.lanes : g.threads;
-    return (long long)N * (each > 256 ? each : 256) < (1ll << 32) - 1024;
+    const int each = g.lanes ? g.lanes : g.threads, slope = 1 << logprob_slope_lanes(V, dtype);
+    return (long long)N * (each > slope ? each : slope) < (1ll << 32) - 1024;
 }
 
 }  // namespace moe

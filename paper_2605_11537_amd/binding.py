@@ -663,12 +663,15 @@ def moe_token_logprobs(logits, target, k=0, out=None, ws=None):
     """logits [N,V] (rows contiguous, any distance apart), target int32[N] -> dict(logprob, entropy, lse f32[N], top_idx int32[N,k],
     top_logprob f32[N,k]).  A target outside [0,V) is a padded position: logprob 0.  Logits of -inf are masked."""
     N, V = logits.shape
+    if not -2 ** 31 <= k < 2 ** 31:
+        raise ValueError(f"moe_token_logprobs: k={k} does not fit an int")
     f32, dt, c = torch.float32, _dt(logits), _c()
     c.expect("moe_token_logprobs", _device, logits, "target", target, torch.int32, (N,))
     room = _room(ws, "moe_token_logprobs_workspace_bytes", N, V, k, dt)
     if out is None:
-        logprob, entropy, lse, top_idx, top_logprob, made = c.fresh(logits, f32, (N,), f32, (N,), f32, (N,), torch.int32, (N, max(k, 0)),
-                                                                    f32, (N, max(k, 0)), *room)
+        room_k = min(max(k, 0), V)                      # a k that the library refuses asks for no memory
+        logprob, entropy, lse, top_idx, top_logprob, made = c.fresh(logits, f32, (N,), f32, (N,), f32, (N,), torch.int32, (N, room_k),
+                                                                    f32, (N, room_k), *room)
         out = dict(logprob=logprob, entropy=entropy, lse=lse, top_idx=top_idx, top_logprob=top_logprob)
     else:
         logprob, entropy, lse = out["logprob"], out["entropy"], out["lse"]

@@ -1,8 +1,12 @@
-"""How many rows of logits a call takes: the host rule, compiled from the library's header, against the launch limit and the documented sizes."""
+"""How many rows of logits a call takes: the host rule, compiled from the library's header, against the launch limit and the documented sizes; and
+numbers that do not fit the library's."""
 import os
 import subprocess
 
 import pytest
+import torch
+
+import paper_2605_11537_amd as moe
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -55,3 +59,10 @@ def test_the_documented_sizes_are_taken(ask):
     cases = [(N, V, t) for t in (0, 1) for N, top in ((1 << 28, 64), (1 << 26, 256), (1 << 24, 1024), (1 << 21, 1 << 21))
              for V in (1, 8, 64, 65, 100, 256, 257, 1000, 1024, 1025, 50257, 1 << 21) if V <= top]
     assert all(row[0] for row in ask(cases))
+
+
+@pytest.mark.parametrize("k", [2 ** 32 + 3, 2 ** 31, -2 ** 31 - 1, 2 ** 64 + 1])
+def test_a_number_of_alternatives_past_an_int_is_refused(k):
+    """It was reduced to the int's width: 2^32 + 3 asked for 2^32 + 3 columns, of which 3 were written."""
+    with pytest.raises(ValueError, match="does not fit an int"):
+        moe.moe_token_logprobs(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32), k)

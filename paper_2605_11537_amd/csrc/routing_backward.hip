@@ -249,12 +249,14 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
 }
 
 // combine's gradient: log2 of the lanes per row, one piece per lane and trip, a wavefront's at most or a whole workgroup; -1: 32 lanes with
-// three pieces each, for many rows with one choice (with more, their rows keep a lane's loads in flight).
-static int combine_backward_lanes(int T, int k, int vec_per_row)
+// three pieces each, for one choice (with more, their rows keep a lane's loads in flight) and rows that they hold at once: bf16, 64 lanes and these in
+// us, 4096 x 640 5.9 and 5.1, 20000 x 640 22.1 and 18.6, 20000 x 768 27.2 and 25.4, 65536 x 512 52.3 and 51.8, x 768 78.3 and 75.6, fewer tokens
+// alike.  Wider rows take them two trips: 4096 x 896 6.7 and 7.1, 65536 x 1024 99.6 and 100.5, 131072 x 1024 196 and 198.
+static int combine_backward_lanes(int k, int vec_per_row)
 {
     const int lg = row_lanes(vec_per_row);
     if (lg <= 5) return lg;
-    return lg > 7 ? 8 : k == 1 && T > 16384 ? -1 : 6;
+    return lg > 7 ? 8 : k == 1 && vec_per_row <= 3 * 32 ? -1 : 6;
 }
 static int dispatch_backward_lanes(int T, int vec_per_row)
 {
@@ -290,7 +292,7 @@ extern "C" int moe_combine_topk_backward(const void *dout, const void *y_perm, c
     MOE_REQUIRE(aligned16(dout) && aligned16(y_perm) && aligned16(dy_perm) && aligned16(dx), MOE_ERR_INVALID_ARG,
                 "moe_combine_topk_backward: tensor misaligned");
     const int vec = (int)((size_t)d * (dtype == MOE_F32 ? 4 : 2) / 16);
-    const int lg = combine_backward_lanes(T, k, vec), wide = lg < 0;
+    const int lg = combine_backward_lanes(k, vec), wide = lg < 0;
 #define MOE_CMB_BACK(B)                                               \
     (wide     ? combine_backward_kernel<B, 3, 1>                      \
      : k == 1 ? combine_backward_kernel<B, 1, 1>                      \

@@ -357,7 +357,8 @@ int moe_route_topk_backward(const float *logits, const int32_t *expert_idx, cons
  *     f = sigmoid(u1 + b_f);  r = sigmoid(u2 + b_r);  c_t = f*c_{t-1} + (1-f)*u0;  h_t = r*tanh(c_t) + (1-r)*w_t
  * h [B, L, H] in dtype, rows behind a sequence's end zero; c_last [B, H] the state after its last token.  States and
  * all arithmetic are binary32.  b_f, b_r [H] binary32, c0 and lengths [B] (int32, taken to 0..L; NULL: all L) may be
- * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H up to 2^22.
+ * NULL, c_last too, and c_last may be c0: one token per call carries the predictor through decoding.  Any H up to 2^22
+ * (with L up to 2^30 and B ceil(H/64) below 2^26).
  * Infinities and NaN go through as in these formulas; f stays above 0, so an infinite state stays, and 1-f reaches 0
  * from a pre-activation of 87 on, where an infinite u0 gives NaN as 0*infinity does.  In bfloat16 the gates' exponents
  * are rounded once (f and 1-f are off by 2^-23 |pre-activation| of themselves), and tanh is off by up to 2.5e-5 of itself.

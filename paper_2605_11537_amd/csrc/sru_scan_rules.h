@@ -5,15 +5,15 @@
 namespace moe {
 
 // Steps of a wavefront: 16 in the forward where there is work for the card (2 x 16384 x 768 bf16 72 us, with 8 93 us: more tiles to wait for), 8 in the
-// gradient, whose registers hold more for each (126 us, with 16 and no more than two workgroups' registers 132 us; 8 x 1000 x 768 43 and 61 us).
+// gradient, whose registers hold more for each (126 us, with 16 133 us; 8 x 1000 x 768 43 and 61 us).
 // States are saved every 8 steps: 5 % of the forward's bytes.
 constexpr int SCAN_LONG = 16;
 constexpr int SCAN_SAVED = 8;
 constexpr int SCAN_MAX_WAVES = 8;      // wavefronts of a workgroup, one behind the other on the sequence
 // Lines (sequences by 64 channels) from which on a sequence is walked by one workgroup instead of cut into tiles: 32 x 512 x 1024, 512 lines, 42 us
-// walked, 50 us in tiles; 16 x 2048 x 1024, 256 lines, 84 and 93; 12 x 1024 x 1024 fp32, 192 lines, 64 and 62 (gradient 112 and 103).
+// walked, 50 us in tiles; 16 x 2048 x 1024, 256 lines, 87 and 94; 12 x 1024 x 1024 fp32, 192 lines, 65 and 63 (gradient 110 and 101).
 constexpr int SCAN_ENOUGH = 256;
-// Tiles below which the forward's are cut finer: 16 of them (1 x 200 x 512) 11 us, finer 9; 210 (5 x 777 x 321 fp32) 13.5 and 16.
+// Tiles below which the forward's are cut finer: 16 of them (1 x 200 x 512) 11 us, finer 8; 210 (5 x 777 x 321 fp32) 14 and 16.
 constexpr int SCAN_FEW = 64;
 
 // tiles (sru_scan.hip)
@@ -59,8 +59,8 @@ static inline ScanShape scan_shape(int B, int L, int H, int steps)
     g.across = (int)(g.workgroups < (1 << 22) ? g.workgroups : 1 << 22);
     return g;
 }
-// One token: builds of one step, which are small and take none for the others (64 x 256 bf16 4.8 us with sixteen, 2.8 with one).  Few steps or few
-// tiles: eight (200 x 8 x 320 6.8 us with sixteen, 3.9 with eight; 1 x 300 x 256 11 and 9).
+// One token: builds of one step, which are small and take none for the others (1000 x 1 x 1024 bf16 21 us with sixteen, 9 with one).  Few steps or few
+// tiles: eight (200 x 8 x 320 7 us with sixteen, 5 with eight; 1 x 300 x 256 11 and 8).
 static inline ScanShape scan_forward_shape(int B, int L, int H)
 {
     if (L <= 1) return scan_shape(B, L, H, 1);

@@ -4,10 +4,12 @@
 // of a row join by bringing (m, s, t) to the larger maximum: s e^(m - M), (t + (m - M) s) e^(m - M).
 // A row is read once, into registers.  The sums are found while it arrives.  The alternatives then cost next to nothing: a bound that k logits
 // reach for certain (the k-th largest of the maxima of sixteen groups of threads), the few logits that reach it collected, and each ranked
-// among them.  Rows where more than LP_LIST reach it (equal logits) or fewer than k lie above minus infinity take k searches of the registers.
-// Measured: 8192 x 50257 bf16, k = 4, 170 us (4.8 TB/s; memory, and some nine vector operations a logit beside it), 2048 x 32000 fp32 46 us (5.7
-// TB/s); 32768 x 256 fp32, k = 1, 9 us (3.8 TB/s), 65536 x 256 bf16, k = 8, 21 us (the searches' operations bind).  The gradient reads and writes once:
-// 342 us (4.8 TB/s) for the first, 13 us (5.2 TB/s) for the third.
+// among them.  Rows where more than LP_LIST reach it (equal logits) or fewer than k lie above minus infinity take k searches of the registers:
+// 8192 x 50257 bf16, k = 4, 1150 us for equal logits and 1030 for rows with five left, 179 else; 2048 x 32000 fp32, k = 8, 374, 352 and 49.
+// Measured: 8192 x 50257 bf16, k = 4, 170 to 179 us (4.6 to 4.8 TB/s; memory, and some nine vector operations a logit beside it), 2048 x 32000 fp32 48 us
+// (5.5 TB/s); 32768 x 256 fp32, k = 1, 9 us (3.7 TB/s); k = 8, where the searches' operations bind, 65536 x 256 22 us bf16 and 29 fp32, 32768 x 1000 40
+// and 52.  In parts: 1500 x 131072 bf16 98 us (4.0 TB/s), 4000 x 50257 fp32 179 us (4.5 TB/s), 3 x 131072 12 us.  The gradient reads and writes once: 342
+// us (4.8 TB/s) for the first, 13 us (5.2 TB/s) for the third.
 #include <float.h>
 
 #include "scalar_math.h"
@@ -203,7 +205,8 @@ __device__ __forceinline__ void lp_rank(const float *value, const int *id, int c
 }
 
 // Long rows: a workgroup takes a part of a row, LP_VECS pieces a thread in registers; 64 registers, so that two workgroups of 1024 share a compute unit
-// and one loads while the other sums (one alone: 8192 x 50257 400 us).  WHOLE: the part is the row; else its numbers go to
+// and one loads while the other sums (one alone: 8192 x 50257 400 us); the builds for parts spill 50 of
+// them in bf16 and 11 in fp32, most of it for the search behind a full list.  WHOLE: the part is the row; else its numbers go to
 // a record of LP_RECORD floats.
 template <class X, bool WHOLE>
 __global__ __launch_bounds__(LP_MAX_THREADS, 8) void token_logprobs_kernel(const X *__restrict__ logits, size_t stride,

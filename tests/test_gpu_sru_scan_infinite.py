@@ -119,3 +119,24 @@ def test_a_nearly_shut_gate_lets_its_share_through(dtype, gate):
     _near(c_last, want["c_last"], want["c_err"][:, -1], "f32", "c_last")
     one = moe.sru_scan(c["u"][:, :1].contiguous(), c["x"][:, :1].contiguous(), c["b_f"], c["b_r"], c["c0"])[1]
     _near(one, want["c"][:, 1], want["c_err"][:, 1], "f32", "one token")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("block", [0, 1, 2])
+def test_a_nan_goes_from_tile_to_tile(dtype, block):
+    """In the state's own blocks it reaches every later token of its channel and every earlier one's gradient; in the reset gate's its token alone."""
+    import paper_2605_11537_amd as moe
+    L, at = 9000, 4321
+    c = _inputs(dtype, 1, L, 8, 3, 80)
+    c["u"].view(1, L, 3, 8)[0, at, block, 3] = float("nan")
+    h, c_last, states = moe.sru_scan(c["u"], c["x"], c["b_f"], c["b_r"], c["c0"], want_states=True)
+    bad = torch.isnan(h[0])
+    others = [0, 1, 2, 4, 5, 6, 7]
+    assert not bad[:, others].any() and not bad[:at].any() and bad[at, 3]
+    assert bool(bad[at + 1:, 3].all()) == (block < 2) and bool(bad[at + 1:, 3].any()) == (block < 2)
+    assert bool(torch.isnan(c_last[0, 3])) == (block < 2) and torch.isfinite(c_last[0, others]).all()
+    g = moe.sru_scan_backward(c["dh"], c["u"], states, c["x"], c["b_f"], c["b_r"], c["dc_last"])
+    du = torch.isnan(g["du"].view(L, 3, 8))
+    assert not du[..., others].any() and torch.isfinite(g["dc0"][0, others]).all()
+    assert du[:at + 1, 0, 3].all() and torch.isnan(g["dc0"][0, 3])
+    assert not torch.isnan(g["db_f"][others]).any() and torch.isnan(g["db_f"][3])

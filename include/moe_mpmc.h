@@ -338,7 +338,8 @@ int moe_layer_forward(const moe_layer_args *args, void *stream);
  *   of expert_weight: p = softmax(logits[s]); renormalize = 0: dlogits_i = [i = e_j] dw_j p_i - p_i sum_j dw_j p_ej;
  *   renormalize = 1: w_j (dw_j - sum_l dw_l w_l) at i = e_j with w the weights, 0 elsewhere.  E <= MOE_MAX_EXPERTS.  An
  *   id outside [0,E) is taken as a choice that was not made.  Logits of -infinity are masked; a row that is masked
- *   throughout (with renormalize = 1: all of whose chosen logits are) has gradient 0.  dlogits must not lie on logits.
+ *   throughout (with renormalize = 1: all of whose chosen logits are) has gradient 0, and so has a token none of whose
+ *   choices was made, whatever its logits hold.  dlogits must not lie on logits.
  * Ids of a token must differ from each other, and so must the rows that inv names (as moe_route_topk and
  * moe_dispatch_topk give them).  y_perm, dy_perm and dx_perm have k*T rows; an entry of inv outside them names none.
  */

@@ -162,7 +162,8 @@ __global__ __launch_bounds__(RB_THREADS) void dispatch_backward_kernel(const rb_
 }
 
 // The largest logit is never below the lowest finite value: a row (with renormalize, its chosen logits) that is masked throughout has exponentials of
-// 0, a total of 0 and a gradient of 0, and no infinity is taken from another.  A NaN passes into the total.
+// 0, a total of 0 and a gradient of 0, and no infinity is taken from another.  A NaN passes into the total.  A token without a choice has none of either,
+// whatever its logits hold.
 // LANES lanes per token, RB_LOGITS logits a lane in registers (one wavefront to every token and 1024 places asked: 61 us for 65536 x 256); PIECES:
 // four consecutive ones (rows begin on 16 bytes).  With renormalize the other experts' logits take no part and are not read.
 constexpr int RB_LOGITS = 16;
@@ -181,13 +182,14 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
     int e[MOE_MAX_TOPK];
     float dw[MOE_MAX_TOPK], w[MOE_MAX_TOPK];
     float top = -FLT_MAX;
+    bool any = false;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
         e[j] = -1, dw[j] = 0.f, w[j] = -INFINITY;
         if (j >= k) continue;
         const int id = idx[(size_t)j * T + s];
         const float d = dweight[(size_t)j * T + s];
-        if (id >= 0 && id < E) e[j] = id, dw[j] = d, w[j] = row[id];
+        if (id >= 0 && id < E) e[j] = id, dw[j] = d, w[j] = row[id], any = true;
         top = fmaxf(top, w[j]);
     }
     const auto place = [&](int i) { return i / P * P * LANES + lane * P; };     // of the piece that i lies in
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(RB_THREADS) void route_backward_kernel(const float 
     }
     const float all = renormalize ? 0.f : -mean * share, off = renormalize ? mean : 0.f;
 #pragma unroll
-    for (int i = 0; i < RB_LOGITS; ++i) v[i] = renormalize ? 0.f : v[i] * all;
+    for (int i = 0; i < RB_LOGITS; ++i) v[i] = renormalize || !any ? 0.f : v[i] * all;
 #pragma unroll
     for (int j = 0; j < MOE_MAX_TOPK; ++j) {
         if (j >= k) break;

@@ -55,3 +55,21 @@ def test_a_nan_stays_in_its_row():
     x[1, 7] = np.nan
     got = moe.moe_route_topk_backward(x.cuda(), torch.zeros(1, 3, dtype=torch.int32).cuda(), torch.ones(1, 3).cuda()).cpu()
     assert torch.isnan(got[1]).all() and torch.isfinite(got[[0, 2]]).all()
+
+
+@pytest.mark.parametrize("E", [6, 64, 100, 300])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_a_token_without_a_choice_has_no_gradient(E, renorm):
+    """Whatever its logits hold: a padded token's are nobody's."""
+    import paper_2605_11537_amd as moe
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(6, E, generator=g)
+    x[1], x[2, 3], x[4, 0] = np.nan, np.inf, np.nan
+    idx = torch.stack([torch.arange(6) % E, (torch.arange(6) + 1) % E]).int()
+    idx[:, [1, 2]] = torch.tensor([-1, E], dtype=torch.int32)[:, None]
+    dw = torch.randn(2, 6, generator=g)
+    dw[:, 1] = np.nan
+    got = moe.moe_route_topk_backward(x.cuda(), idx.cuda(), dw.cuda(), renorm).cpu()
+    assert (got[[1, 2]] == 0).all() and torch.isfinite(got[[0, 3, 5]]).all()
+    if not renorm:
+        assert torch.isnan(got[4]).all()

@@ -398,7 +398,8 @@ int sru_scan_backward(const void *dh, const float *dc_last, const void *u, const
  * moe_token_logprobs_backward -- dL/dlogits (dtype) from dlogprob [N] and dentropy [N] (NULL: 0), with the lse and
  * entropy that the forward wrote (entropy may be NULL without dentropy):
  *     dlogits_i = g ([i = target] - p_i) - dentropy p_i (log p_i + entropy),   g = dlogprob, 0 for a padded position
- * 0 at masked logits other than the target and in rows that are masked throughout.  dlogits may lie on logits with the same stride.
+ * 0 at masked logits other than the target, in rows that are masked throughout, and at padded positions with dentropy 0,
+ * whatever their logits hold.  dlogits may lie on logits with the same stride.
  * log p = logits - lse where lse holds it; a row whose |lse| is 64 (binary32) or 2048 (bfloat16) and more, masks of the
  * lowest value or of -1e9 among them, is summed once more, so that its p add up to 1.
  */

@@ -443,9 +443,11 @@ __global__ __launch_bounds__(LP_THREADS) void token_logprobs_backward_kernel(con
     LogprobSlope<X> f;
     f.target = target[n];
     f.lse = lse[n];
-    f.none = f.lse == -INFINITY;
-    f.g = f.target < 0 || f.target >= V ? 0.f : dlogprob[n];
     f.q = dentropy ? dentropy[n] : 0.f;
+    const float slope = dlogprob[n];                     // asked for with the others, not behind the target
+    const bool padded = f.target < 0 || f.target >= V;
+    f.g = padded ? 0.f : slope;
+    f.none = f.lse == -INFINITY || (padded && f.q == 0.f);     // nothing to pass on, whatever a padded position's logits hold
     f.base = -f.g - (dentropy ? f.q * entropy[n] : 0.f);
     f.rest = 0.f;
     if (fabsf(f.lse) >= f.FAR && !f.none) {              // the whole group of threads

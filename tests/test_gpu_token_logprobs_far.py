@@ -102,3 +102,25 @@ def test_many_rows_among_others():
         some = [0, 1, 2, 8, 9, 15, 498, 499]
         alone = moe.moe_token_logprobs_backward(x[some], t[some], s["lse"][some], s["entropy"][some], dl[some], de[some])
         assert torch.equal(alone, d[some])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 1000, 5000, 40000])
+def test_a_padded_position_has_no_gradient(dtype, V):
+    """Whatever its logits hold, where the entropy has no gradient either; with one, the row is one like the others."""
+    import paper_2605_11537_amd as moe
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn(6, V, generator=g).to(DT[dtype])
+    x[1], x[2, V // 2], x[3] = np.nan, np.inf, -1e9
+    t = torch.tensor([3, -1, V, -1, 5, -7], dtype=torch.int32)
+    x, t, dl = x.cuda(), t.cuda(), torch.randn(6, generator=g).cuda()
+    dl[1] = np.nan
+    s = moe.moe_token_logprobs(x, t)
+    assert (s["logprob"][[1, 2, 3, 5]] == 0).all()
+    want = moe.moe_token_logprobs_backward(x, t, s["lse"], s["entropy"], dl)
+    assert (want[[1, 2, 3, 5]] == 0).all() and torch.isfinite(want).all() and (want[0] != 0).any()
+    de = torch.tensor([0.5, 0.0, 0.0, 0.0, 0.5, 0.5], device="cuda")
+    d = moe.moe_token_logprobs_backward(x, t, s["lse"], s["entropy"], dl, de)
+    assert (d[[1, 2, 3]] == 0).all() and torch.isfinite(d).all() and (d[5] != 0).any()
+    de[1] = 0.5
+    assert torch.isnan(moe.moe_token_logprobs_backward(x, t, s["lse"], s["entropy"], dl, de)[1]).all()

@@ -362,7 +362,7 @@ __global__ __launch_bounds__(SCAN_MAX_WAVES *WAVE, 4) void sru_scan_backward_ker
 {
     constexpr bool PRECISE = sizeof(T) == 4;
     constexpr int K = HIGHWAY ? 3 : 4;
-    __shared__ ScanRun sums[3][SCAN_MAX_WAVES][WAVE];
+    __shared__ alignas(sizeof(float2)) ScanRun sums[3][SCAN_MAX_WAVES][WAVE];      // the biases' sums too, in pairs
     __shared__ unsigned drawn;
     unsigned line;
     int at;

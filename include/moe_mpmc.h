@@ -411,6 +411,71 @@ int moe_token_logprobs_backward(const void *logits, long long row_stride, const 
                                 const float *entropy, const float *dlogprob, const float *dentropy, int N, int V,
                                 int dtype, void *dlogits, long long dlogits_stride, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * moe_gated_ffn -- gated experts (or, with E = 1 and expert_offset NULL, one block that every row takes) over rows sorted by expert:
+ * x [R, d] and expert_offset [E+1] as moe_dispatch_topk writes x_perm and expert_offset; rows expert_offset[e] ..
+ * expert_offset[e+1]-1 are expert e's:
+ *     g = x W_gate[e],  u = x W_up[e]   (binary32),   h = act(g) * u  (rounded once to dtype),   y = h W_down[e]  (rounded once)
+ * w_gate, w_up [E, d, F], w_down [E, F, d] row-major (they change with every step of a training run and are not packed).  act: silu
+ * g sigmoid(g), gelu g Phi(g) with the normal distribution's Phi, or relu.  Rows behind expert_offset[E] are not read and y is left as it was
+ * there.  An entry of expert_offset that goes back or past R is taken for the nearest that does not.
+ * d and F are multiples of 8, d up to 2^20, F up to 2^19, E up to MOE_MAX_EXPERTS.
+ * states (NULL, or moe_gated_ffn_states_bytes): h, and g and u in binary32, for moe_gated_ffn_backward.  With states no workspace is needed.
+ *
+ * moe_gated_ffn_backward -- from dy = dL/dy [R, d]:
+ *     dh = dy W_down^T  (binary32);   du = dh act(g),  dg = dh u act'(g)  (rounded once);   dx = dg W_gate^T + du W_up^T
+ *     dw_gate = x^T dg,  dw_up = x^T du,  dw_down = h^T dy   over an expert's rows; zeros for one without rows
+ * dx [R, d] is left as it was behind the last row.  dx, dw_down and the pair dw_gate, dw_up may be NULL.  Sums are binary32 in an order that the
+ * sizes fix.
+ */
+#define MOE_ACT_SILU 0
+#define MOE_ACT_GELU 1
+#define MOE_ACT_RELU 2
+size_t moe_gated_ffn_states_bytes(int R, int F, int dtype);
+size_t moe_gated_ffn_workspace_bytes(int R, int E, int d, int F, int dtype);
+int moe_gated_ffn(const void *x, const int32_t *expert_offset, const void *w_gate, const void *w_up, const void *w_down, int R,
+                  int E, int d, int F, int dtype, int activation, void *y, void *states, void *ws, size_t ws_bytes, void *stream);
+size_t moe_gated_ffn_backward_workspace_bytes(int R, int E, int d, int F, int dtype);
+int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_offset, const void *w_gate, const void *w_up,
+                           const void *w_down, const void *states, int R, int E, int d, int F, int dtype, int activation,
+                           void *dx, void *dw_gate, void *dw_up, void *dw_down, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_head_logprobs -- moe_token_logprobs for logits that are never in memory: a head over a large vocabulary (a predictor's over
+ * experts, a language model's), w_head [V, d] with one row per id (the transpose of sru_predict's w_head; tied embeddings as they are), b_head
+ * [V] binary32 or NULL, h [N, d], target [N]:
+ *     z = h w_head^T + b_head  (binary32);   lse = log sum exp(z);   logprob = z[target] - lse  (0 for a target outside [0,V): a padded position)
+ * A bias of -infinity masks its id, as long as its product is finite; where all are masked, lse and logprob are -infinity.  A NaN or +infinity among
+ * a row's logits makes its numbers NaN.  d a multiple of 8 up to 2^20, V up to 2^24, N up to 2^24, any V and N.
+ *
+ * moe_head_logprobs_backward -- from dlogprob [N], with the lse that the forward wrote:
+ *     dz = dlogprob ([v = target] - exp(z - lse)), 0 at padded positions whatever h holds there;
+ *     dh = dz w_head,   dw_head = dz^T h,   db_head = sum of dz over the rows  (binary32)
+ * The logits are made again, in pieces of the vocabulary: the workspace grows with N times a piece, about 512 MiB of dz at most (256 ids for very
+ * large N) and as much of sums.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
+ * N = 0 dw_head and db_head are zeros.  Sums in binary32 in an order that the sizes fix.
+ */
+size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype);
+int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V,
+                      int dtype, float *logprob, float *lse, void *ws, size_t ws_bytes, void *stream);
+size_t moe_head_logprobs_backward_workspace_bytes(int N, int d, int V, int dtype);
+int moe_head_logprobs_backward(const void *h, const void *w_head, const float *b_head, const int32_t *target, const float *lse,
+                               const float *dlogprob, int N, int d, int V, int dtype, void *dh, void *dw_head, float *db_head,
+                               void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * moe_clip_gradients -- the norm over all gradients of a step, and the gradients clipped by it:
+ *     norm = sqrt(sum over all n tensors of g^2)  (sums in binary64, in an order that the sizes fix; rounded once);
+ *     out_i = g_i * (max_norm / norm) where norm > max_norm (binary32, rounded once to the tensor's type), else g_i bit for bit.
+ * A norm that is infinite or NaN scales nothing: the caller reads it and drops the step.
+ * gradients, out, counts (elements) and dtypes are arrays of n entries in HOST memory; the tensors they name are contiguous, aligned to their
+ * element only.  out[i] may be gradients[i]; any other overlap with what is written, a tensor named twice among it, is refused.  max_norm above
+ * 0 (infinity: the norm alone, with copies where out differs).  n up to 4096; n = 0 gives norm 0.
+ */
+size_t moe_clip_gradients_workspace_bytes(int n);
+int moe_clip_gradients(const void *const *gradients, void *const *out, const long long *counts, const int *dtypes, int n,
+                       float max_norm, float *norm, void *ws, size_t ws_bytes, void *stream);
+
 /* =======================================================================================
  * Measurement (not part of the method; used by the benchmark only).
  * moe_expert_ffn_timed: moe_expert_ffn_rows (with row_index NULL: moe_expert_ffn, n_x_rows =

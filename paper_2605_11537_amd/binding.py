@@ -18,6 +18,7 @@ import torch
 MOE_F32, MOE_BF16 = 0, 1
 LAYOUT_PLAIN, LAYOUT_PACKED = 0, 1
 SCHEDULE_SLOTS, SCHEDULE_EXPERTS = 0, 1
+ACT_SILU, ACT_GELU, ACT_RELU = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmoe_mpmc.so")
@@ -38,6 +39,9 @@ EXPORTS = (
     "moe_combine_topk_backward", "moe_dispatch_topk_backward", "moe_route_topk_backward",
     "sru_scan_states_bytes", "sru_scan_workspace_bytes", "sru_scan", "sru_scan_backward_workspace_bytes", "sru_scan_backward",
     "moe_token_logprobs_workspace_bytes", "moe_token_logprobs", "moe_token_logprobs_backward",
+    "moe_gated_ffn_states_bytes", "moe_gated_ffn_workspace_bytes", "moe_gated_ffn", "moe_gated_ffn_backward_workspace_bytes",
+    "moe_gated_ffn_backward", "moe_head_logprobs_workspace_bytes", "moe_head_logprobs", "moe_head_logprobs_backward_workspace_bytes",
+    "moe_head_logprobs_backward", "moe_clip_gradients_workspace_bytes", "moe_clip_gradients",
     "moe_measure_sink_bytes", "moe_measure_stream_read", "moe_measure_mfma_bf16_flops", "moe_measure_mfma_bf16",
 )
 
@@ -46,7 +50,8 @@ EXPORTS = (
 MARSHALLED = ("moe_route", "moe_route_topk", "sru_predict", "replica_plan", "moe_dispatch", "moe_dispatch_static", "moe_dispatch_topk",
               "moe_plan_dispatch", "moe_pack_weights", "moe_expert_ffn", "moe_expert_ffn_rows", "moe_combine", "moe_combine_topk",
               "moe_layer_forward", "moe_combine_topk_backward", "moe_dispatch_topk_backward", "moe_route_topk_backward", "sru_scan",
-              "sru_scan_backward", "moe_token_logprobs", "moe_token_logprobs_backward")
+              "sru_scan_backward", "moe_token_logprobs", "moe_token_logprobs_backward", "moe_gated_ffn", "moe_gated_ffn_backward",
+              "moe_head_logprobs", "moe_head_logprobs_backward", "moe_clip_gradients")
 
 
 class MoeError(RuntimeError):
@@ -138,6 +143,17 @@ def lib():
         _lib.moe_token_logprobs_workspace_bytes.argtypes = [I, I, I, I]
         _lib.moe_token_logprobs.argtypes = [P, Q, P, I, I, I, I, P, P, P, P, P, P, S, P]
         _lib.moe_token_logprobs_backward.argtypes = [P, Q, P, P, P, P, P, I, I, I, P, Q, P]
+        _lib.moe_gated_ffn_states_bytes.argtypes = [I, I, I]
+        _lib.moe_gated_ffn_workspace_bytes.argtypes = [I] * 5
+        _lib.moe_gated_ffn.argtypes = [P] * 5 + [I] * 6 + [P] * 3 + [S, P]
+        _lib.moe_gated_ffn_backward_workspace_bytes.argtypes = [I] * 5
+        _lib.moe_gated_ffn_backward.argtypes = [P] * 7 + [I] * 6 + [P] * 5 + [S, P]
+        _lib.moe_head_logprobs_workspace_bytes.argtypes = [I] * 4
+        _lib.moe_head_logprobs.argtypes = [P] * 4 + [I] * 4 + [P] * 3 + [S, P]
+        _lib.moe_head_logprobs_backward_workspace_bytes.argtypes = [I] * 4
+        _lib.moe_head_logprobs_backward.argtypes = [P] * 6 + [I] * 4 + [P] * 4 + [S, P]
+        _lib.moe_clip_gradients_workspace_bytes.argtypes = [I]
+        _lib.moe_clip_gradients.argtypes = [P, P, P, P, I, C.c_float, P, P, S, P]
     return _lib
 
 
@@ -699,6 +715,137 @@ def moe_token_logprobs_backward(logits, target, lse, entropy, dlogprob, dentropy
     to, dstride = _rows(out)
     _check(c.moe_token_logprobs_backward(rows, stride, target, lse, entropy, dlogprob, dentropy, N, V, dt, to, dstride, _stream()))
     return out
+
+
+def _gated_sizes(who, x, w_gate, w_up, w_down, expert_offset):
+    """(R, E, d, F, dtype) of a gated layer's tensors, checked."""
+    if x.dim() != 2 or w_gate.dim() != 3:
+        raise ValueError(f"{who}: x must be [R,d] and the weights [E,d,F] and [E,F,d], not {list(x.shape)} and {list(w_gate.shape)}")
+    (R, d), (E, _, F) = x.shape, w_gate.shape
+    if expert_offset is None and E != 1:
+        raise ValueError(f"{who}: {E} experts need expert_offset")
+    t = x.dtype
+    _c().expect(who, _device, x, "expert_offset", expert_offset, torch.int32, (E + 1,), "w_gate", w_gate, t, (E, d, F), "w_up", w_up, t, (E, d, F),
+                "w_down", w_down, t, (E, F, d))
+    return R, E, d, F, _dt(x)
+
+
+def _check_gated_states(who, x, states, R, F, dt):
+    _c().expect(who, _device, x, "states", states, torch.uint8, (_size("moe_gated_ffn_states_bytes", R, F, dt),))
+
+
+def moe_gated_ffn(x, w_gate, w_up, w_down, expert_offset=None, activation=ACT_SILU, want_states=False, out=None, states=None, ws=None):
+    """Gated experts: rows expert_offset[e] .. expert_offset[e+1]-1 of x [R,d] (moe_dispatch_topk's x_perm and expert_offset int32[E+1]) through
+    w_gate, w_up [E,d,F] and w_down [E,F,d]; without expert_offset (E = 1) all rows.  -> (y [R,d], states or None).  Rows of y behind the last
+    expert's are left as they were (zero when allocated here).  states go to moe_gated_ffn_backward; a tensor of an earlier call may be given to
+    write them to."""
+    R, E, d, F, dt = _gated_sizes("moe_gated_ffn", x, w_gate, w_up, w_down, expert_offset)
+    t, c = x.dtype, _c()
+    want_states = want_states or states is not None
+    room = (None, ()) if want_states else _room(ws, "moe_gated_ffn_workspace_bytes", R, E, d, F, dt)
+    if states is not None:
+        _check_gated_states("moe_gated_ffn", x, states, R, F, dt)
+    if out is None:
+        if expert_offset is not None:
+            out = torch.zeros(R, d, dtype=t, device=x.device)
+    else:
+        c.expect("moe_gated_ffn", _device, x, "out", out, t, (R, d))
+    y, kept, made = c.fresh(x, t if out is None else None, (R, d),
+                            torch.uint8 if want_states and states is None else None,
+                            (_size("moe_gated_ffn_states_bytes", R, F, dt) if want_states else 0,), *room)
+    y = out if out is not None else y
+    states = states if states is not None else kept
+    ws, ws_bytes = (None, 0) if want_states else _workspace("moe_gated_ffn", x, ws, made)
+    _check(c.moe_gated_ffn(x, expert_offset, w_gate, w_up, w_down, R, E, d, F, dt, activation, y, states, ws, ws_bytes, _stream()))
+    return y, states
+
+
+def moe_gated_ffn_backward(dy, x, w_gate, w_up, w_down, states, expert_offset=None, activation=ACT_SILU, out=None, ws=None):
+    """Gradient of moe_gated_ffn: dy [R,d] with the forward's inputs and states -> dict(dx [R,d], dw_gate, dw_up [E,d,F], dw_down [E,F,d]).  Rows
+    of dx behind the last expert's are left as they were (zero when allocated here).  With ``out``, dx, dw_down and the pair dw_gate, dw_up may be
+    None: they are not computed."""
+    who = "moe_gated_ffn_backward"
+    R, E, d, F, dt = _gated_sizes(who, x, w_gate, w_up, w_down, expert_offset)
+    t, c = x.dtype, _c()
+    c.expect(who, _device, x, "dy", dy, t, (R, d))
+    if R:
+        _check_gated_states(who, x, states, R, F, dt)
+    room = _room(ws, "moe_gated_ffn_backward_workspace_bytes", R, E, d, F, dt)
+    if out is None:
+        dx = None if expert_offset is None else torch.zeros(R, d, dtype=t, device=x.device)
+        fresh_dx, dw_gate, dw_up, dw_down, made = c.fresh(x, t if dx is None else None, (R, d), t, (E, d, F), t, (E, d, F), t, (E, F, d), *room)
+        out = dict(dx=fresh_dx if dx is None else dx, dw_gate=dw_gate, dw_up=dw_up, dw_down=dw_down)
+    else:
+        c.expect(who, _device, x, "dx", out["dx"], t, (R, d), "dw_gate", out["dw_gate"], t, (E, d, F), "dw_up", out["dw_up"], t, (E, d, F),
+                 "dw_down", out["dw_down"], t, (E, F, d))
+        made, = c.fresh(x, *room)
+    ws, ws_bytes = _workspace(who, x, ws, made)
+    _check(c.moe_gated_ffn_backward(dy, x, expert_offset, w_gate, w_up, w_down, states if R else None, R, E, d, F, dt, activation, out["dx"],
+                                    out["dw_gate"], out["dw_up"], out["dw_down"], ws, ws_bytes, _stream()))
+    return out
+
+
+def moe_head_logprobs(h, w_head, target, b_head=None, out=None, ws=None):
+    """h [N,d] under the head w_head [V,d] (one row per id) with b_head f32[V] or None, target int32[N] -> dict(logprob, lse f32[N]): the logits
+    h w_head^T + b_head are not kept.  A target outside [0,V) is a padded position: logprob 0.  A bias of -inf masks its id."""
+    who, f32, c = "moe_head_logprobs", torch.float32, _c()
+    N, d, V, dt = _head_sizes(who, h, w_head, target, b_head)
+    room = _room(ws, "moe_head_logprobs_workspace_bytes", N, d, V, dt)
+    if out is None:
+        logprob, lse, made = c.fresh(h, f32, (N,), f32, (N,), *room)
+        out = dict(logprob=logprob, lse=lse)
+    else:
+        c.expect(who, _device, h, "logprob", out["logprob"], f32, (N,), "lse", out["lse"], f32, (N,))
+        made, = c.fresh(h, *room)
+    ws, ws_bytes = _workspace(who, h, ws, made)
+    _check(c.moe_head_logprobs(h, w_head, b_head, target, N, d, V, dt, out["logprob"], out["lse"], ws, ws_bytes, _stream()))
+    return out
+
+
+def _head_sizes(who, h, w_head, target, b_head):
+    """(N, d, V, dtype) of a head's tensors, checked."""
+    if h.dim() != 2 or w_head.dim() != 2:
+        raise ValueError(f"{who}: h must be [N,d] and w_head [V,d], not {list(h.shape)} and {list(w_head.shape)}")
+    (N, d), V = h.shape, w_head.shape[0]
+    _c().expect(who, _device, h, "w_head", w_head, h.dtype, (V, d), "target", target, torch.int32, (N,), "b_head", b_head, torch.float32, (V,))
+    return N, d, V, _dt(h)
+
+
+def moe_head_logprobs_backward(h, w_head, target, lse, dlogprob, b_head=None, out=None, ws=None):
+    """Gradient of moe_head_logprobs' logprob (dlogprob f32[N]), with the forward's inputs and lse -> dict(dh [N,d], dw_head [V,d],
+    db_head f32[V] or None without b_head).  With ``out``, each may be None: it is not computed."""
+    who, f32, t, c = "moe_head_logprobs_backward", torch.float32, h.dtype, _c()
+    N, d, V, dt = _head_sizes(who, h, w_head, target, b_head)
+    c.expect(who, _device, h, "lse", lse, f32, (N,), "dlogprob", dlogprob, f32, (N,))
+    room = _room(ws, "moe_head_logprobs_backward_workspace_bytes", N, d, V, dt)
+    if out is None:
+        dh, dw, db, made = c.fresh(h, t, (N, d), t, (V, d), f32 if b_head is not None else None, (V,), *room)
+        out = dict(dh=dh, dw_head=dw, db_head=db)
+    else:
+        c.expect(who, _device, h, "dh", out["dh"], t, (N, d), "dw_head", out["dw_head"], t, (V, d), "db_head", out["db_head"], f32, (V,))
+        made, = c.fresh(h, *room)
+    ws, ws_bytes = _workspace(who, h, ws, made)
+    _check(c.moe_head_logprobs_backward(h, w_head, b_head, target, lse, dlogprob, N, d, V, dt, out["dh"], out["dw_head"], out["db_head"], ws, ws_bytes,
+                                        _stream()))
+    return out
+
+
+def moe_clip_gradients(gradients, max_norm, out=None, norm=None, ws=None):
+    """The norm over all gradients (a sequence of contiguous f32 or bf16 tensors of any shapes) and the gradients times max_norm / norm where
+    that is below 1 -> (norm f32[1], list of tensors).  out: tensors of the same sizes and types to write, the gradients themselves to clip in place.
+    A norm that is infinite or NaN scales nothing."""
+    who, c = "moe_clip_gradients", _c()
+    lead = gradients[0] if len(gradients) else norm
+    if lead is None:
+        raise ValueError(f"{who}: no gradients")
+    if out is None:
+        out = [torch.empty_like(g, memory_format=torch.contiguous_format) for g in gradients]
+    c.expect(who, _device, lead, "norm", norm, torch.float32, (1,))
+    made_norm, made = c.fresh(lead, torch.float32 if norm is None else None, (1,), *_room(ws, "moe_clip_gradients_workspace_bytes", len(gradients)))
+    norm = made_norm if norm is None else norm
+    ws, _ = _workspace(who, lead, ws, made)
+    _check(c.moe_clip_gradients(gradients, out, max_norm, norm, ws, _stream(), _device))
+    return norm, out
 
 
 class MoeLayerTopK:

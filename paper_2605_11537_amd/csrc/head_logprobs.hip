@@ -1,0 +1,567 @@
+// Log probabilities of given ids under a head over a large vocabulary, z = h W^T + b, without the logits in memory, and their gradient.
+//
+// Forward: a workgroup makes a tile of logits in registers and leaves of each of its rows the maximum, the sum of e^(z - maximum) and, where it has
+// the target's column, that logit; a second launch joins a row's tiles.  Backward: the logits are made again, piece of the vocabulary by piece, and
+// leave as dz = dlogprob ([v = target] - p), from which two products make the rows' part of dh and the piece's rows of dW.
+//
+// dz is rounded once to the tensors' type, as the operand of those products.  It is divided by the largest |dlogprob| first, and dh and dW are multiplied by
+// it in binary32: with the loss a mean all rows have the same dlogprob, which would put the same rounding error on every target's -1.
+#include "product.h"
+#include "scalar_math.h"
+#include "head_logprobs_rules.h"
+
+namespace moe {
+namespace {
+
+constexpr float HEAD_NONE = -__builtin_inff();
+
+struct HeadArgs {
+    const void *h, *w;
+    const float *b, *lse, *dlogprob;
+    const int32_t *target;
+    int N, d, V;
+    int v0, columns, ld;                       // backward: the piece's first id, its ids, and the row of dz it is kept in
+    int n_n;                                   // forward: tiles of a row
+    float2 *tiles;                             // forward [N, n_n]: maximum, sum
+    float *at_target;                          // forward [N]
+    const float *largest;                      // backward: |dlogprob|
+    void *dz;
+    float *db;                                 // backward [rows of tiles x wavefront rows, V], or NULL
+};
+
+__device__ __forceinline__ float finite_or(float m, float other) { return m == HEAD_NONE ? other : m; }
+
+// the tile's logits with their bias; columns behind the vocabulary are masked
+template <class TILE>
+__device__ __forceinline__ void add_bias(const TILE &tile, const Job &j, const float *b, int V, typename TILE::Sums &z)
+{
+#pragma unroll
+    for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int v = j.n0 + tile.of_column(nb) + i;
+            const float bias = v >= V ? HEAD_NONE : b ? b[v] : 0.f;
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) z[0][mb][nb][i] = v >= V ? HEAD_NONE : z[0][mb][nb][i] + bias;
+        }
+}
+
+// over the four lane groups that hold a row's columns
+__device__ __forceinline__ float row_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float row_sum(float v)
+{
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_forward_kernel(HeadArgs p, int tall)
+{
+    typedef typename TILE::T T;
+    constexpr int WN = TILE::BN / TILE::WAVE_N;
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    __shared__ float2 parts[WN][TILE::BM];
+    const unsigned d_bytes = p.d * sizeof(T);
+    const int n_m = tiles_of(p.N, TILE::BM);
+    const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
+    Units units(n_m * p.n_n);
+    tile.run(
+        [&](Job &j) {
+            int u, m, n;
+            if (!units.take(u)) return false;
+            product_place(u, n_m, p.n_n, tall, m, n);
+            j.m0 = m * TILE::BM;
+            j.n0 = n * TILE::BN;
+            j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
+            j.columns = p.V - j.n0 < TILE::BN ? p.V - j.n0 : TILE::BN;
+            j.k = p.d;
+            j.runs = 1;
+            j.group = n;
+            j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
+            j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
+            return true;
+        },
+        [&](const Job &j, typename TILE::Sums &z) {
+            add_bias(tile, j, p.b, p.V, z);
+            const int lane = threadIdx.x & 63;
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = tile.of_row(mb);
+                const int target = row < j.rows ? p.target[j.m0 + row] : -1;
+                float m = HEAD_NONE;
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        m = fmaxf(m, z[0][mb][nb][i]);
+                        if (target == j.n0 + tile.of_column(nb) + i && target < p.V) p.at_target[j.m0 + row] = z[0][mb][nb][i];
+                    }
+                m = row_max(m);
+                const float beside = finite_or(m, 0.f);
+                float s = 0.f;
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s += exp_of<true>(z[0][mb][nb][i] - beside);
+                s = row_sum(s);
+                if (lane < 16) parts[tile.wn][row] = make_float2(m, s);
+            }
+            __syncthreads();
+            for (int row = threadIdx.x; row < j.rows; row += TILE::THREADS) {
+                float m = HEAD_NONE, s = 0.f;
+#pragma unroll
+                for (int w = 0; w < WN; ++w) m = fmaxf(m, parts[w][row].x);
+#pragma unroll
+                for (int w = 0; w < WN; ++w) s += parts[w][row].y * exp_of<true>(finite_or(parts[w][row].x, 0.f) - finite_or(m, 0.f));
+                p.tiles[(size_t)(j.m0 + row) * p.n_n + j.group] = make_float2(m, s);
+            }
+        });
+}
+
+// One wavefront per row: its tiles' maxima and sums -> lse and the target's log probability.
+__global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, const float *at_target, const int32_t *target, int N, int V, int n_n,
+                                                        float *logprob, float *lse)
+{
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (row >= N) return;
+    const float2 *t = tiles + (size_t)row * n_n;
+    float m = HEAD_NONE, s = 0.f;
+    for (int i = lane; i < n_n; i += 64) {
+        const float2 v = t[i];
+        const float both = fmaxf(m, v.x), beside = finite_or(both, 0.f);
+        s = s * exp_of<true>(finite_or(m, beside) - beside) + v.y * exp_of<true>(finite_or(v.x, beside) - beside);
+        m = both;
+    }
+    float all = m;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
+    const float beside = finite_or(all, 0.f);
+    s *= exp_of<true>(finite_or(m, beside) - beside);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) {
+        const float l = logf(s);               // -infinity where every id is masked
+        lse[row] = beside + l;
+        const int id = target[row];
+        const bool on = id >= 0 && id < V;
+        const float z = on ? at_target[row] : 0.f;
+        logprob[row] = !on ? 0.f : z == HEAD_NONE && s == s ? z : (z - beside) - l;
+    }
+}
+
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dlogits_kernel(HeadArgs p, int tall)
+{
+    typedef typename TILE::T T;
+    constexpr int WM = TILE::BM / TILE::WAVE_M;
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    const unsigned d_bytes = p.d * sizeof(T);
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
+    const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
+    const float largest = *p.largest;
+    Units units(n_m * n_n);
+    tile.run(
+        [&](Job &j) {
+            int u, m, n;
+            if (!units.take(u)) return false;
+            product_place(u, n_m, n_n, tall, m, n);
+            j.m0 = m * TILE::BM;
+            j.n0 = p.v0 + n * TILE::BN;
+            j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
+            const int left = p.v0 + p.columns - j.n0;
+            j.columns = left < TILE::BN ? left : TILE::BN;
+            j.k = p.d;
+            j.runs = 1;
+            j.group = m;
+            j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
+            j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
+            return true;
+        },
+        [&](const Job &j, typename TILE::Sums &z) {
+            add_bias(tile, j, p.b, p.V, z);
+            product_f32x4 down[TILE::NB];      // sums over this lane's rows
+#pragma unroll
+            for (int nb = 0; nb < TILE::NB; ++nb) down[nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = tile.of_row(mb);
+                const bool there = row < j.rows;
+                const int target = there ? p.target[j.m0 + row] : -1;
+                const bool on = target >= 0 && target < p.V;
+                const float g = on ? p.dlogprob[j.m0 + row] / largest : 0.f;
+                const float lse = on ? p.lse[j.m0 + row] : 0.f;
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb) {
+                    const int column = tile.of_column(nb);
+                    product_f32x4 dz;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float x = z[0][mb][nb][i];
+                        const float prob = x == HEAD_NONE ? 0.f : exp_of<true>(x - lse);
+                        dz[i] = on ? g * ((j.n0 + column + i == target ? 1.f : 0.f) - prob) : 0.f;
+                    }
+                    down[nb] += dz;
+                    // a row of dz ends with zeros up to a whole piece of 16 bytes
+                    if (there && j.n0 - p.v0 + column < p.ld) store4((T *)p.dz + (size_t)(j.m0 + row) * p.ld + (j.n0 - p.v0 + column), dz);
+                }
+            }
+            if (p.db) {
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float s = down[nb][i];
+#pragma unroll
+                        for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o, 64);
+                        const int v = j.n0 + tile.of_column(nb) + i;
+                        if ((threadIdx.x & 15) == 0 && v < p.V) p.db[(size_t)(j.group * WM + tile.wm) * p.V + v] = s;
+                    }
+            }
+        });
+}
+
+// ------------------------------------------------------------------------------------------------- the two products of the gradient
+struct HeadGradArgs {
+    const void *dz, *h, *w;
+    int N, d, columns, ld, v0;
+    int parts, part;                           // dh: k in so many parts of so many columns
+    bool add;                                  // dh: behind an earlier piece
+    float *dh;                                 // [parts, N, d]
+    void *dw;
+    const float *largest;
+};
+
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dh_kernel(HeadGradArgs p, int tall)
+{
+    typedef typename TILE::T T;
+    constexpr int Z = sizeof(T);
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    const unsigned lda = p.ld * Z, ldb = p.d * Z;
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
+    const TILE tile((product_lds_t *)smem, lda, ldb);
+    Units units(p.parts * n_m * n_n);
+    tile.run(
+        [&](Job &j) {
+            int u, m, n;
+            if (!units.take(u)) return false;
+            const int part = u / (n_m * n_n), k0 = part * p.part;
+            product_place(u - part * n_m * n_n, n_m, n_n, tall, m, n);
+            j.group = part;
+            j.m0 = m * TILE::BM;
+            j.n0 = n * TILE::BN;
+            j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
+            j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
+            j.runs = 1;
+            j.k = p.columns - k0 < p.part ? (p.columns - k0 > 0 ? p.columns - k0 : 0) : p.part;
+            j.a[0] = source_along(p.dz, (size_t)j.m0 * lda, lda, j.rows, TILE::BM);
+            j.a[0].base += (unsigned)k0 * Z;
+            j.a[0].records -= (unsigned)k0 * Z;
+            j.b[0] = source_across(p.w, (size_t)(p.v0 + k0) * ldb, ldb, j.n0 * Z);
+            return true;
+        },
+        [&](const Job &j, typename TILE::Sums &sums) {
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = tile.of_row(mb);
+                if (row >= j.rows) continue;
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb) {
+                    const int column = tile.of_column(nb);
+                    if (column >= j.columns) continue;
+                    float *to = p.dh + ((size_t)j.group * p.N + j.m0 + row) * p.d + j.n0 + column;
+                    product_f32x4 v = sums[0][mb][nb];
+                    if (p.add) v += *reinterpret_cast<const product_f32x4 *>(to);
+                    store4(to, v);
+                }
+            }
+        });
+}
+
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dw_kernel(HeadGradArgs p, int tall)
+{
+    typedef typename TILE::T T;
+    constexpr int Z = sizeof(T);
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    const unsigned lda = p.ld * Z, ldb = p.d * Z;
+    const int n_m = tiles_of(p.columns, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
+    const TILE tile((product_lds_t *)smem, lda, ldb);
+    const float largest = *p.largest;
+    Units units(n_m * n_n);
+    tile.run(
+        [&](Job &j) {
+            int u, m, n;
+            if (!units.take(u)) return false;
+            product_place(u, n_m, n_n, tall, m, n);
+            j.group = 0;
+            j.m0 = m * TILE::BM;
+            j.n0 = n * TILE::BN;
+            j.rows = p.columns - j.m0 < TILE::BM ? p.columns - j.m0 : TILE::BM;
+            j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
+            j.runs = 1;
+            j.k = p.N;
+            j.a[0] = source_across(p.dz, 0, lda, j.m0 * Z);
+            j.b[0] = source_across(p.h, 0, ldb, j.n0 * Z);
+            return true;
+        },
+        [&](const Job &j, typename TILE::Sums &sums) {
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = tile.of_row(mb);
+                if (row >= j.rows) continue;
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb) {
+                    const int column = tile.of_column(nb);
+                    if (column >= j.columns) continue;
+                    store4((T *)p.dw + (size_t)(p.v0 + j.m0 + row) * p.d + j.n0 + column, sums[0][mb][nb] * largest);
+                }
+            }
+        });
+}
+
+// ------------------------------------------------------------------------------------------------- rows
+// The largest |dlogprob| of a row that counts; 1 where that is 0 or no number.  One workgroup.
+__global__ __launch_bounds__(1024) void head_largest_kernel(const int32_t *target, const float *dlogprob, int N, int V, float *largest)
+{
+    __shared__ float waves[16];
+    float m = 0.f;
+    for (int i = threadIdx.x; i < N; i += 1024) {
+        const int id = target[i];
+        if (id >= 0 && id < V) m = fmaxf(m, fabsf(dlogprob[i]));
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 16; ++w) m = fmaxf(m, waves[w]);
+        *largest = m > 0.f && m < __builtin_inff() ? m : 1.f;
+    }
+}
+
+// h with zeros for the padded rows, which may hold anything: what dW's sums are made of.  pieces: of 16 bytes, to a row
+__global__ __launch_bounds__(256) void head_rows_kernel(const uint4 *h, const int32_t *target, int N, int V, int pieces, uint4 *to)
+{
+    const size_t total = (size_t)N * pieces, step = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const int id = target[i / pieces];
+        to[i] = id >= 0 && id < V ? h[i] : make_uint4(0, 0, 0, 0);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void head_dh_join_kernel(const float *parts, int n_parts, const int32_t *target, int N, int V, int d,
+                                                           const float *largest, T *dh)
+{
+    const size_t total = (size_t)N * d, step = (size_t)gridDim.x * 1024;
+    const float scale = *largest;
+    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < total; i += step) {
+        const int id = target[i / d];
+        product_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (id >= 0 && id < V)
+            for (int s = 0; s < n_parts; ++s) v += *reinterpret_cast<const product_f32x4 *>(parts + s * total + i);
+        store4(dh + i, v * scale);
+    }
+}
+
+__global__ __launch_bounds__(256) void head_db_kernel(const float *parts, int n_parts, int V, const float *largest, float *db)
+{
+    const int v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= V) return;
+    double s = 0.;
+    for (int i = 0; i < n_parts; ++i) s += parts[(size_t)i * V + v];
+    db[v] = (float)(s * *largest);
+}
+
+__global__ __launch_bounds__(256) void head_clear_kernel(unsigned *p, size_t words)
+{
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < words; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// ------------------------------------------------------------------------------------------------- host
+void launch_clear(void *p, size_t bytes, hipStream_t st)
+{
+    const size_t words = bytes / 4;            // rows are multiples of 16 bytes
+    hipLaunchKernelGGL(head_clear_kernel, dim3((unsigned)(words / 256 < 2048 ? words / 256 + 1 : 2048)), dim3(256), 0, st, (unsigned *)p, words);
+}
+
+template <class T>
+struct Tiles;
+template <>
+struct Tiles<bf16_t> {
+    template <Order A, Order B>
+    using Tall = Tile<bf16_t, A, B, HEAD_TALL, 256, 2, 4>;
+    template <Order A, Order B>
+    using Flat = Tile<bf16_t, A, B, 64, 128, 1, 4>;
+    template <Order A, Order B>
+    using Few = Tile<bf16_t, A, B, 16, 128, 1, 4>;
+};
+template <>
+struct Tiles<float> {
+    template <Order A, Order B>
+    using Tall = Tile<float, A, B, 128, 128, 2, 2>;
+    template <Order A, Order B>
+    using Flat = Tile<float, A, B, 64, 128, 1, 4>;
+    template <Order A, Order B>
+    using Few = Tile<float, A, B, 16, 128, 1, 4>;
+};
+
+template <class TILE>
+int grid_of(long long units, int more_lds)
+{
+    return product_grid(units, 256 * (160 * 1024 / (TILE::LDS + more_lds)));
+}
+
+template <class TILE>
+void launch_forward(const HeadArgs &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(head_forward_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.N, TILE::BM) * p.n_n, 8 * TILE::BM * 4)), dim3(TILE::THREADS),
+                       0, st, p, 8);
+}
+template <class TILE>
+void launch_dlogits(const HeadArgs &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(head_dlogits_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.N, TILE::BM) * tiles_of(p.columns, TILE::BN), 0)),
+                       dim3(TILE::THREADS), 0, st, p, 8);
+}
+template <class TILE>
+void launch_dh(const HeadGradArgs &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(head_dh_kernel<TILE>, dim3(grid_of<TILE>((long long)p.parts * tiles_of(p.N, TILE::BM) * tiles_of(p.d, TILE::BN), 0)),
+                       dim3(TILE::THREADS), 0, st, p, 8);
+}
+template <class TILE>
+void launch_dw(const HeadGradArgs &p, hipStream_t st)
+{
+    hipLaunchKernelGGL(head_dw_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.columns, TILE::BM) * tiles_of(p.d, TILE::BN), 0)),
+                       dim3(TILE::THREADS), 0, st, p, 8);
+}
+
+// the tile by the number of rows
+#define HEAD_BY_ROWS(LAUNCH, A, B, ARGS, ST)                                                        \
+    switch (head_rows(N, dtype)) {                                                                  \
+    case HEAD_TALL_TILES: LAUNCH<typename Tiles<T>::template Tall<A, B>>(ARGS, ST); break;          \
+    case HEAD_FLAT_TILES: LAUNCH<typename Tiles<T>::template Flat<A, B>>(ARGS, ST); break;          \
+    default: LAUNCH<typename Tiles<T>::template Few<A, B>>(ARGS, ST);                               \
+    }
+
+template <class T>
+void forward(HeadArgs p, int N, int dtype, float *logprob, float *lse, hipStream_t st)
+{
+    HEAD_BY_ROWS(launch_forward, ALONG_K, ALONG_K, p, st)
+    hipLaunchKernelGGL(head_join_kernel, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
+}
+
+template <class T>
+void backward(HeadArgs p, const HeadShape &g, char *ws, int dtype, T *dh, T *dw, float *db, hipStream_t st)
+{
+    const int N = p.N;
+    float *const largest = (float *)ws, *const dh_parts = (float *)(ws + g.dh_at), *const db_parts = (float *)(ws + g.db_at);
+    p.largest = largest;
+    p.dz = ws + g.dz_at;
+    p.db = db ? db_parts : nullptr;
+    hipLaunchKernelGGL(head_largest_kernel, dim3(1), dim3(1024), 0, st, p.target, p.dlogprob, N, p.V, largest);
+    const int pieces = p.d * (int)sizeof(T) / 16;
+    if (dw)
+        hipLaunchKernelGGL(head_rows_kernel, dim3((int)((size_t)N * pieces / 256 < 4096 ? (size_t)N * pieces / 256 + 1 : 4096)), dim3(256), 0, st,
+                           (const uint4 *)p.h, p.target, N, p.V, pieces, (uint4 *)(ws + g.rows_at));
+    for (int v0 = 0; v0 < p.V; v0 += g.piece) {
+        p.v0 = v0;
+        p.columns = p.V - v0 < g.piece ? p.V - v0 : g.piece;
+        p.ld = (int)align_up(p.columns, 8);
+        HEAD_BY_ROWS(launch_dlogits, ALONG_K, ALONG_K, p, st)
+        HeadGradArgs q = {};
+        q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.ld = p.ld, q.v0 = v0;
+        q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), 64), q.add = v0 > 0;
+        q.dh = dh_parts, q.dw = dw, q.largest = largest;
+        if (dh) HEAD_BY_ROWS(launch_dh, ALONG_K, ACROSS_K, q, st)
+        if (dw) launch_dw<typename Tiles<T>::template Tall<ACROSS_K, ACROSS_K>>(q, st);
+    }
+    if (dh)
+        hipLaunchKernelGGL(head_dh_join_kernel<T>, dim3((int)((size_t)N * p.d / 1024 < 4096 ? (size_t)N * p.d / 1024 + 1 : 4096)), dim3(256), 0, st,
+                           dh_parts, g.parts, p.target, N, p.V, p.d, largest, dh);
+    if (db) hipLaunchKernelGGL(head_db_kernel, dim3(tiles_of(p.V, 256)), dim3(256), 0, st, db_parts, g.db_parts, p.V, largest, db);
+}
+
+int head_check(const char *who, int N, int d, int V, int dtype)
+{
+    MOE_REQUIRE(N >= 0 && d > 0 && V > 0, MOE_ERR_INVALID_ARG, "%s: N=%d d=%d V=%d out of range", who, N, d, V);
+    MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
+    MOE_REQUIRE(d % 8 == 0, MOE_ERR_INVALID_ARG, "%s: d=%d must be a multiple of 8", who, d);
+    MOE_REQUIRE(d <= HEAD_MAX_WIDTH && V <= HEAD_MAX_IDS && N <= HEAD_MAX_ROWS, MOE_ERR_UNSUPPORTED, "%s: N=%d d=%d V=%d beyond the kernels", who, N, d, V);
+    return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype)
+{
+    (void)d;
+    if (N <= 0 || V <= 0) return 0;
+    return align_up((size_t)N * 4, 256) + (size_t)N * head_row_tiles(N, V, dtype) * 8;
+}
+
+extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V, int dtype,
+                                 float *logprob, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = head_check("moe_head_logprobs", N, d, V, dtype);
+    if (rc != MOE_OK || N == 0) return rc;
+    MOE_REQUIRE(h && w_head && target && logprob && lse, MOE_ERR_INVALID_ARG, "moe_head_logprobs: null pointer");
+    MOE_REQUIRE(aligned16(h) && aligned16(w_head), MOE_ERR_INVALID_ARG, "moe_head_logprobs: tensor misaligned");
+    MOE_REQUIRE(logprob != lse, MOE_ERR_INVALID_ARG, "moe_head_logprobs: logprob aliases lse");
+    const size_t need = moe_head_logprobs_workspace_bytes(N, d, V, dtype);
+    MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "moe_head_logprobs: workspace of %zu bytes given, %zu needed",
+                ws ? ws_bytes : 0, need);
+    HeadArgs p = {};
+    p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.N = N, p.d = d, p.V = V;
+    p.n_n = head_row_tiles(N, V, dtype);
+    p.at_target = (float *)ws;
+    p.tiles = (float2 *)((char *)ws + align_up((size_t)N * 4, 256));
+    if (dtype == MOE_BF16) forward<bf16_t>(p, N, dtype, logprob, lse, (hipStream_t)stream);
+    else forward<float>(p, N, dtype, logprob, lse, (hipStream_t)stream);
+    MOE_CHECK_LAUNCH("moe_head_logprobs");
+    return MOE_OK;
+}
+
+extern "C" size_t moe_head_logprobs_backward_workspace_bytes(int N, int d, int V, int dtype)
+{
+    return N <= 0 || d <= 0 || V <= 0 ? 0 : head_shape(N, d, V, dtype).bytes;
+}
+
+extern "C" int moe_head_logprobs_backward(const void *h, const void *w_head, const float *b_head, const int32_t *target, const float *lse,
+                                          const float *dlogprob, int N, int d, int V, int dtype, void *dh, void *dw_head, float *db_head, void *ws,
+                                          size_t ws_bytes, void *stream)
+{
+    const int rc = head_check("moe_head_logprobs_backward", N, d, V, dtype);
+    if (rc != MOE_OK) return rc;
+    MOE_REQUIRE(N == 0 || (h && w_head && target && lse && dlogprob), MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: null pointer");
+    MOE_REQUIRE((!dh || (dh != h && dh != w_head && dh != dw_head)) && (!dw_head || (dw_head != h && dw_head != w_head)) &&
+                    (!db_head || (db_head != b_head && db_head != lse && db_head != dlogprob)),
+                MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: an output aliases another tensor");
+    MOE_REQUIRE(aligned16(h) && aligned16(w_head) && aligned16(dh) && aligned16(dw_head), MOE_ERR_INVALID_ARG,
+                "moe_head_logprobs_backward: tensor misaligned");
+    hipStream_t st = (hipStream_t)stream;
+    if (N == 0) {                              // sums over nothing
+        if (dw_head) launch_clear(dw_head, (size_t)V * d * (dtype == MOE_F32 ? 4 : 2), st);
+        if (db_head) launch_clear(db_head, (size_t)V * 4, st);
+        MOE_CHECK_LAUNCH("moe_head_logprobs_backward");
+        return MOE_OK;
+    }
+    const HeadShape g = head_shape(N, d, V, dtype);
+    MOE_REQUIRE(ws && ws_bytes >= g.bytes && aligned16(ws), MOE_ERR_WORKSPACE, "moe_head_logprobs_backward: workspace of %zu bytes given, %zu needed",
+                ws ? ws_bytes : 0, g.bytes);
+    HeadArgs p = {};
+    p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.lse = lse, p.dlogprob = dlogprob, p.N = N, p.d = d, p.V = V;
+    if (dtype == MOE_BF16) backward<bf16_t>(p, g, (char *)ws, dtype, (bf16_t *)dh, (bf16_t *)dw_head, db_head, st);
+    else backward<float>(p, g, (char *)ws, dtype, (float *)dh, (float *)dw_head, db_head, st);
+    MOE_CHECK_LAUNCH("moe_head_logprobs_backward");
+    return MOE_OK;
+}

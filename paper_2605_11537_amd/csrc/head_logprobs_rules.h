@@ -1,0 +1,62 @@
+// Sizes of the head's calls: tiles by the number of rows, pieces of the vocabulary, parts of a sum.  Host code.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+constexpr int HEAD_MAX_WIDTH = 1 << 20;        // byte offsets inside a tile's rows fit 31 bits
+constexpr int HEAD_MAX_IDS = 1 << 24, HEAD_MAX_ROWS = 1 << 24;
+constexpr size_t HEAD_PIECE_BYTES = 512u << 20;
+constexpr int HEAD_TALL = 256;
+
+enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
+static inline HeadRows head_rows(int N, int dtype)
+{
+    (void)dtype;
+    return N <= 16 ? HEAD_FEW_TILES : N <= 128 ? HEAD_FLAT_TILES : HEAD_TALL_TILES;
+}
+static inline int head_tile_rows(int N, int dtype)
+{
+    const HeadRows r = head_rows(N, dtype);
+    return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : HEAD_TALL;
+}
+static inline int head_tile_columns(int N, int dtype) { return head_rows(N, dtype) == HEAD_TALL_TILES && dtype != MOE_F32 ? 256 : 128; }
+static inline int head_row_tiles(int N, int V, int dtype) { return ceil_div(V, head_tile_columns(N, dtype)); }
+
+// The gradient's pieces and workspace.
+struct HeadShape {
+    int piece;                                 // ids of the vocabulary whose dz is in memory at a time
+    int parts;                                 // of a piece's sum for dh
+    int db_parts;                              // rows of partial sums for db
+    size_t rows_at, dz_at, dh_at, db_at, bytes;
+};
+static inline HeadShape head_shape(int N, int d, int V, int dtype)
+{
+    HeadShape g;
+    const int z = dtype == MOE_F32 ? 4 : 2;
+    const size_t most = HEAD_PIECE_BYTES / ((size_t)N * z) / 256 * 256;
+    const int fits = most < 256 ? 256 : most > (size_t)V ? V : (int)most;
+    const int pieces = ceil_div(V, fits);
+    g.piece = pieces == 1 ? V : (int)align_up(ceil_div(V, pieces), 256);
+    // Parts of dh's sum: as many as fill the chip evenly.  A tile costs its k and some 512 beside, for its first stage and its writes.
+    const long long tiles = (long long)ceil_div(N, head_tile_rows(N, dtype)) * ceil_div(d, head_tile_columns(N, dtype));
+    double best = 0;
+    g.parts = 1;
+    for (int s = 1; s <= 64; ++s) {
+        if (s > 1 && (g.piece / s < 512 || (size_t)s * N * d * 4 > HEAD_PIECE_BYTES)) break;
+        const double cost = (double)((tiles * s + 255) / 256) * ((double)g.piece / s + 512);
+        if (s == 1 || cost < best * 0.97) {
+            best = cost;
+            g.parts = s;
+        }
+    }
+    g.db_parts = ceil_div(N, head_tile_rows(N, dtype)) * (head_rows(N, dtype) == HEAD_TALL_TILES ? 2 : 1);
+    g.rows_at = 256;
+    g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
+    g.dh_at = g.dz_at + align_up((size_t)N * align_up(g.piece, 8) * z, 256);
+    g.db_at = g.dh_at + align_up((size_t)g.parts * N * d * 4, 256);
+    g.bytes = g.db_at + align_up((size_t)g.db_parts * V * 4, 256);
+    return g;
+}
+
+}  // namespace moe

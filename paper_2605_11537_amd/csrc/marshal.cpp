@@ -15,6 +15,7 @@
 #include <exception>
 #include <tuple>
 #include <utility>
+#include <vector>
 
 #include "../../include/moe_mpmc.h"
 
@@ -162,7 +163,8 @@ PyObject *call(const char *name, int (*f)(A...), PyObject *const *args, Py_ssize
     X(moe_route) X(moe_route_topk) X(sru_predict) X(replica_plan) X(moe_dispatch) X(moe_dispatch_static) X(moe_dispatch_topk)  \
     X(moe_plan_dispatch) X(moe_pack_weights) X(moe_expert_ffn) X(moe_expert_ffn_rows) X(moe_combine) X(moe_combine_topk)   \
     X(moe_combine_topk_backward) X(moe_dispatch_topk_backward) X(moe_route_topk_backward) X(sru_scan) X(sru_scan_backward) \
-    X(moe_token_logprobs) X(moe_token_logprobs_backward)
+    X(moe_token_logprobs) X(moe_token_logprobs_backward) X(moe_gated_ffn) X(moe_gated_ffn_backward) \
+    X(moe_head_logprobs) X(moe_head_logprobs_backward)
 
 #define DECLARE(NAME)                                                                                                     \
     decltype(&NAME) bound_##NAME = nullptr;                                                                               \
@@ -196,6 +198,70 @@ PyObject *py_moe_layer_forward(PyObject *, PyObject *const *args, Py_ssize_t n)
         memcpy(&layer, &fields, sizeof layer);
         void *stream = address_of(*at);
         return unlocked([&] { return bound_moe_layer_forward(&layer, stream); });
+    });
+}
+
+// moe_clip_gradients(gradients, out, max_norm, norm, ws, stream, device): two sequences of contiguous tensors of equal sizes and types, on the current device.
+// A tensor read from Python takes 0.5 us for its pointer, size and type each; a call has dozens.
+decltype(&moe_clip_gradients) bound_moe_clip_gradients = nullptr;
+PyObject *py_moe_clip_gradients(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (!bound_moe_clip_gradients) {
+        PyErr_SetString(PyExc_RuntimeError, "moe_clip_gradients is not bound");
+        return nullptr;
+    }
+    if (!counted("moe_clip_gradients", n, 7)) return nullptr;
+    return guarded([&] {
+        struct Kept {
+            PyObject *o;
+            explicit Kept(PyObject *s) : o(PySequence_Fast(s, "moe_clip_gradients: sequences of tensors")) { if (!o) throw Failed(); }
+            ~Kept() { Py_DECREF(o); }
+        };
+        const Kept from(args[0]), to(args[1]);
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(from.o);
+        auto refuse = [](const char *what, Py_ssize_t i) {
+            PyErr_Format(PyExc_ValueError, "moe_clip_gradients: tensor %zd %s", i, what);
+            throw Failed();
+        };
+        if (PySequence_Fast_GET_SIZE(to.o) != count) {
+            PyErr_SetString(PyExc_ValueError, "moe_clip_gradients: as many outputs as gradients");
+            throw Failed();
+        }
+        if (count > INT_MAX) refuse("is one too many", count);
+        PyObject *current = PyObject_CallNoArgs(args[6]);
+        if (!current) throw Failed();
+        const long here = PyLong_AsLong(current);
+        Py_DECREF(current);
+        if (here == -1 && PyErr_Occurred()) throw Failed();
+        std::vector<const void *> in(count);
+        std::vector<void *> out(count);
+        std::vector<long long> counts(count);
+        std::vector<int> dtypes(count);
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            PyObject *a = PySequence_Fast_GET_ITEM(from.o, i), *b = PySequence_Fast_GET_ITEM(to.o, i);
+            if (!THPVariable_Check(a) || !THPVariable_Check(b)) {
+                PyErr_Format(PyExc_TypeError, "moe_clip_gradients: tensor %zd is none", i);
+                throw Failed();
+            }
+            const at::Tensor &s = THPVariable_Unpack(a), &t = THPVariable_Unpack(b);
+            if (!s.is_cuda() || !t.is_cuda() || !s.is_contiguous() || !t.is_contiguous()) refuse("must be device-resident and contiguous, and so must its output", i);
+            if (s.get_device() != here || t.get_device() != here) refuse("or its output is not on the current device", i);
+            if (s.scalar_type() != t.scalar_type() || s.numel() != t.numel()) refuse("and its output differ in type or size", i);
+            if (s.scalar_type() != at::kFloat && s.scalar_type() != at::kBFloat16) refuse("is neither float32 nor bfloat16", i);
+            in[i] = s.data_ptr();
+            out[i] = t.data_ptr();
+            counts[i] = s.numel();
+            dtypes[i] = s.scalar_type() == at::kBFloat16 ? MOE_BF16 : MOE_F32;
+        }
+        const double most = PyFloat_AsDouble(args[2]);
+        if (most == -1. && PyErr_Occurred()) throw Failed();
+        float *norm = static_cast<float *>(pointer_of(args[3]));
+        void *ws = pointer_of(args[4]);
+        const size_t ws_bytes = ws ? THPVariable_Unpack(args[4]).numel() : 0;
+        void *stream = address_of(args[5]);
+        return unlocked([&] {
+            return bound_moe_clip_gradients(in.data(), out.data(), counts.data(), dtypes.data(), (int)count, (float)most, norm, ws, ws_bytes, stream);
+        });
     });
 }
 
@@ -361,6 +427,7 @@ PyObject *py_bind(PyObject *, PyObject *args)
     }
     CALLS(BIND)
     BIND(moe_layer_forward)
+    BIND(moe_clip_gradients)
 #undef BIND
     PyErr_Format(PyExc_ValueError, "no call named %s", name);
     return nullptr;
@@ -368,7 +435,7 @@ PyObject *py_bind(PyObject *, PyObject *args)
 
 PyMethodDef methods[] = {
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))py_##NAME, METH_FASTCALL, nullptr},
-    CALLS(METHOD) METHOD(moe_layer_forward)
+    CALLS(METHOD) METHOD(moe_layer_forward) METHOD(moe_clip_gradients)
 #undef METHOD
     {"expect", (PyCFunction)(void (*)(void))py_expect, METH_FASTCALL, nullptr},
     {"fresh", (PyCFunction)(void (*)(void))py_fresh, METH_FASTCALL, nullptr},

@@ -1,0 +1,402 @@
+// Tiles of matrix products whose operands lie in memory as their owners keep them: D[m][n] = sum over k of A(m, k) B(n, k), in bfloat16 or binary32,
+// summed in binary32.  Each operand has k along its rows (ALONG_K: element (m, k) at m * ld + k) or rows along k (ACROSS_K: at k * ld + m), so that the
+// products of a layer and of its gradient need no transposed copies.
+//
+// A stage is 128 bytes of k for every row of the two tiles (64 k of bfloat16, 32 of binary32), and goes from memory to LDS directly, 16 bytes a lane.  It
+// lies there as the loads bring it, in the order of the operand in memory, its pieces permuted by an XOR so that the reads of a fragment meet no bank
+// twice:
+//   ALONG_K   row r's 16-byte piece p (of 8) lies at r * 8 + (p ^ (r >> 1 & 7)); a fragment is one 16-byte read a lane
+//   ACROSS_K  bfloat16: the 32-byte piece q of step k lies at q ^ (k & 3 | k >> 1 & 4) of that step's row; a fragment is two reads that transpose 4 k x
+//             16 rows among 16 lanes.  binary32: the 64-byte piece q lies at q ^ (k >> 2 & 3); a fragment is four reads of 4 bytes
+// The order of k inside a matrix instruction is free as long as both operands have the same: lane group g holds k = 8 g .. 8 g + 7 of 32 in bfloat16,
+// and in binary32 instruction j takes k = 4 g + j of 16.
+//
+// Operands are read as buffers: what lies behind the last row of k or of the tile comes as zero.  ALONG_K the pieces behind the last k are sent out of
+// the buffer's range.  Both operands are zero there, so that memory which holds a NaN does not reach a sum.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+typedef unsigned product_u32x4 __attribute__((ext_vector_type(4)));
+typedef float product_f32x4 __attribute__((ext_vector_type(4)));
+typedef short product_s16x4 __attribute__((ext_vector_type(4)));
+typedef short product_s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 product_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char product_lds_t;
+typedef __attribute__((address_space(3))) product_s16x4 product_lds_s16x4;
+
+enum Order { ALONG_K, ACROSS_K };
+
+constexpr int PRODUCT_STAGE_ROW = 128;         // bytes of k a stage holds for every row
+
+template <class T>
+struct Fragment;
+template <>
+struct Fragment<bf16_t> {
+    typedef product_s16x8 type;
+    static constexpr int K = 32;               // k of a step: two to a stage
+};
+template <>
+struct Fragment<float> {
+    typedef product_f32x4 type;
+    static constexpr int K = 16;
+};
+
+__device__ __forceinline__ void product_mma(product_f32x4 &d, product_s16x8 b, product_s16x8 a)
+{
+    d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(product_bf16x8, b), __builtin_bit_cast(product_bf16x8, a), d, 0, 0, 0);
+}
+__device__ __forceinline__ void product_mma(product_f32x4 &d, product_f32x4 b, product_f32x4 a)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) d = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[j], d, 0, 0, 0);
+}
+
+// 1 KB from a buffer to LDS: lane l's 16 bytes at `at` go to lds + 16 l.  No register is written, so nothing has to wait but the readers of that LDS.
+// Inline assembly: in front of every LDS read that the compiler sees it would wait for all such loads, those of later stages too.
+// (m0 may be read one instruction after it is written.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load_to_lds(product_u32x4 buffer, unsigned at, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// where one operand's tile begins in memory: its first row's (ALONG_K: first k's) address and how many rows (ALONG_K) or k (ACROSS_K) are there
+struct Source {
+    uint64_t base;
+    unsigned records;                          // bytes from base that may be read
+};
+
+template <class T, Order ORDER, int ROWS, int WAVES>
+struct Operand {
+    typedef typename Fragment<T>::type fragment;
+    static constexpr int STAGE_K = PRODUCT_STAGE_ROW / (int)sizeof(T);
+    static constexpr int BYTES = ROWS * PRODUCT_STAGE_ROW;
+    static constexpr int LOADS = BYTES / 1024;
+    static constexpr int MINE = LOADS >= WAVES ? LOADS / WAVES : 1;       // with fewer loads than wavefronts some are made twice, the same bytes
+    static_assert(LOADS % WAVES == 0 || WAVES % LOADS == 0, "every wavefront has the same number of loads");
+    static constexpr int PIECES = ROWS * (int)sizeof(T) / 16;             // ACROSS_K: 16-byte pieces of a step of k
+    static constexpr int ROW_MASK = sizeof(T) == 2 ? (PIECES / 2 < 8 ? PIECES / 2 - 1 : 7) : 3;      // ... that the XOR permutes
+
+    unsigned at[MINE];                         // byte offsets of this lane's pieces from the stage's base
+    unsigned k_of[MINE];                       // ALONG_K: the piece's first k in its stage
+    unsigned read_at[2];                       // where this lane's fragment of row block 0 begins in a stage, for each of its two steps
+    unsigned swizzle;                          // ACROSS_K: this lane's XOR
+
+    __device__ __forceinline__ static unsigned permute(unsigned k)
+    {
+        if (sizeof(T) == 4) return (k >> 2) & 3;
+        if (ROW_MASK == 7) return (k & 3) | ((k >> 1) & 4);
+        return ((k >> 1) & 1) | ((k >> 2) & 2);                            // rows of 128 bytes: neighbouring k alternate between the halves of the banks
+    }
+
+    // row: this wavefront's first row in the tile
+    __device__ __forceinline__ void set_up(unsigned ld_bytes, int row)
+    {
+        const unsigned lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned c = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const unsigned q = ((w * MINE + i) % LOADS) * 64 + lane;
+            if (ORDER == ALONG_K) {
+                const unsigned r = q >> 3, p = (q & 7) ^ ((r >> 1) & 7);
+                at[i] = r * ld_bytes + p * 16;
+                k_of[i] = p * (16 / sizeof(T));
+            } else if (sizeof(T) == 2) {
+                const unsigned k = q / PIECES, p = q % PIECES;
+                at[i] = k * ld_bytes + (p ^ (permute(k) << 1)) * 16;
+            } else {
+                const unsigned k = q / PIECES, p = q % PIECES;
+                at[i] = k * ld_bytes + (p ^ (permute(k) << 2)) * 16;
+            }
+        }
+        if (ORDER == ALONG_K) {
+            const unsigned s = (c >> 1) & 7;
+            read_at[0] = (row + c) * 128 + ((g ^ s) << 4);
+            read_at[1] = read_at[0] ^ 64;
+            swizzle = 0;
+        } else if (sizeof(T) == 2) {
+            const unsigned k = 8 * g + (c >> 2);
+            swizzle = permute(k) * 32;
+            read_at[0] = k * ROWS * 2 + (c & 3) * 8 + row * 2;
+            read_at[1] = read_at[0] + 32 * ROWS * 2;
+        } else {
+            swizzle = g * 64;
+            read_at[0] = 4 * g * ROWS * 4 + c * 4 + row * 4;
+            read_at[1] = read_at[0] + 16 * ROWS * 4;
+        }
+    }
+
+    // stage `step` (of STAGE_K k each) of k_total
+    __device__ __forceinline__ void issue(Source s, int step, int k_total, unsigned ld_bytes, unsigned lds) const
+    {
+        const unsigned w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint64_t skip = ORDER == ALONG_K ? (uint64_t)step * PRODUCT_STAGE_ROW : (uint64_t)step * STAGE_K * ld_bytes;
+        const uint64_t base = s.base + skip;
+        const int left = k_total - step * STAGE_K;
+        unsigned records;
+        if (ORDER == ALONG_K) records = s.records - (unsigned)skip;         // every k of a row lies within its records
+        else {
+            // the columns in front of the tile are not in the buffer: the last row ends with the matrix
+            const uint64_t rows = (uint64_t)(left < STAGE_K ? left : STAGE_K) * ld_bytes;
+            const uint64_t end = s.records;                                  // ACROSS_K: bytes of a row from the tile's first on
+            records = (unsigned)(rows - ld_bytes + end);
+        }
+        const product_u32x4 buffer = {(unsigned)base, (unsigned)(base >> 32), records, 0x27000};
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            unsigned a = at[i];
+            if (ORDER == ALONG_K) a = (int)k_of[i] < left ? a : 0x80000000u;
+            load_to_lds(buffer, a, lds + ((w * MINE + i) % LOADS) * 1024);
+        }
+    }
+
+    // fragment of rows 16 rb .. 16 rb + 15 of this wavefront's, step ks of the stage at lds
+    __device__ __forceinline__ fragment read(product_lds_t *lds, int rb, int ks) const
+    {
+        if constexpr (ORDER == ALONG_K) {
+            return *reinterpret_cast<__attribute__((address_space(3))) fragment *>(lds + read_at[ks] + rb * 2048);
+        } else if constexpr (sizeof(T) == 2) {
+            // row is a multiple of 16 rows, so that the XOR meets the place of the 32-byte piece alone
+            const unsigned a = (read_at[ks] + rb * 32) ^ swizzle;
+            const product_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds_s16x4 *)(lds + a));
+            const product_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((product_lds_s16x4 *)(lds + a + 4 * ROWS * 2));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const unsigned a = (read_at[ks] + rb * 64) ^ swizzle;
+            fragment f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = *reinterpret_cast<__attribute__((address_space(3))) float *>(lds + a + j * ROWS * 4);
+            return f;
+        }
+    }
+};
+
+// four neighbouring values of a row, rounded once
+__device__ __forceinline__ void store4(float *p, product_f32x4 v) { *reinterpret_cast<product_f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, product_f32x4 v)
+{
+    uint2 two;
+    two.x = pack_bf16x2(v[0], v[1]);
+    two.y = pack_bf16x2(v[2], v[3]);
+    *reinterpret_cast<uint2 *>(p) = two;
+}
+
+// What a workgroup computes next: a tile of D, from one or two runs of k (the second behind the first in the same sum).
+struct Job {
+    Source a[2], b[2];                         // of the runs; with two column halves b holds the halves' and there is one run
+    int k, runs;                               // k of a run, 0 .. : D = 0 without
+    int m0, n0, rows, columns;                 // the tile's origin in D and how much of it there is
+    int group;                                 // expert, or part of a split sum
+};
+
+__device__ __forceinline__ Source source_along(const void *p, size_t first_byte, unsigned ld_bytes, int rows, int most)
+{
+    return {reinterpret_cast<uint64_t>(p) + first_byte, (unsigned)(rows < most ? rows : most) * ld_bytes};
+}
+__device__ __forceinline__ Source source_across(const void *p, size_t first_byte, unsigned ld_bytes, unsigned column_bytes)
+{
+    return {reinterpret_cast<uint64_t>(p) + first_byte + column_bytes, ld_bytes - column_bytes};
+}
+
+// BM x BN of D by WM x WN wavefronts.  HALVES = 2: columns come from two operands of BN / 2 rows each, and a wavefront has the same columns of both.
+// The loop waits for a stage, asks for the one behind it, and multiplies; the first stage of the next tile is asked for in front of a tile's last
+// products, so that it lands while the tile is written.
+template <class T_, Order OA, Order OB, int BM_, int BN_, int WM, int WN, int HALVES_ = 1>
+struct Tile {
+    typedef T_ T;
+    static constexpr int BM = BM_, BN = BN_, HALVES = HALVES_, WAVES = WM * WN, THREADS = WAVES * WAVE;
+    static constexpr int HALF_N = BN / HALVES, WAVE_M = BM / WM, WAVE_N = HALF_N / WN;       // rows and columns (of a half) of a wavefront
+    static constexpr int MB = WAVE_M / 16, NB = WAVE_N / 16;                                 // blocks of 16
+    typedef Operand<T, OA, BM, WAVES> A;
+    typedef Operand<T, OB, HALF_N, WAVES> B;
+    static constexpr int STAGE_K = A::STAGE_K;
+    static constexpr int STAGE = A::BYTES + HALVES * B::BYTES, LDS = 2 * STAGE;
+
+    typedef product_f32x4 Sums[HALVES][MB][NB];          // register i of [h][mb][nb]: row of_row(mb), column of_column(nb) + i of half h
+
+    A a;
+    B b;
+    unsigned lda, ldb;
+    int wm, wn;
+    product_lds_t *lds;
+
+    __device__ __forceinline__ Tile(product_lds_t *smem, unsigned lda_bytes, unsigned ldb_bytes) : lda(lda_bytes), ldb(ldb_bytes), lds(smem)
+    {
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = w / WN;
+        wn = w % WN;
+        a.set_up(lda, wm * WAVE_M);
+        b.set_up(ldb, wn * WAVE_N);
+    }
+    __device__ __forceinline__ int of_row(int mb) const { return wm * WAVE_M + mb * 16 + (threadIdx.x & 15); }
+    __device__ __forceinline__ int of_column(int nb) const { return wn * WAVE_N + nb * 16 + ((threadIdx.x & 63) >> 4) * 4; }
+
+    __device__ __forceinline__ static int steps_of(const Job &j) { return (j.k + STAGE_K - 1) / STAGE_K; }
+
+    __device__ __forceinline__ void issue(const Job &j, int step, int per_run, int buffer) const
+    {
+        const unsigned at = (unsigned)(uintptr_t)lds + buffer * STAGE;
+        const bool second = j.runs == 2 && step >= per_run;
+        const int s = second ? step - per_run : step;
+        a.issue(second ? j.a[1] : j.a[0], s, j.k, lda, at);
+        if (HALVES == 2) {
+            b.issue(j.b[0], s, j.k, ldb, at + A::BYTES);
+            b.issue(j.b[1], s, j.k, ldb, at + A::BYTES + B::BYTES);
+        } else b.issue(second ? j.b[1] : j.b[0], s, j.k, ldb, at + A::BYTES);
+    }
+
+    __device__ __forceinline__ void multiply(Sums &sums, int buffer) const
+    {
+        product_lds_t *at = lds + buffer * STAGE;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            typename A::fragment fa[MB];
+            typename B::fragment fb[HALVES][NB];
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) fb[h][nb] = b.read(at + A::BYTES + h * B::BYTES, nb, ks);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) fa[mb] = a.read(at, mb, ks);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) product_mma(sums[h][mb][nb], fb[h][nb], fa[mb]);
+        }
+    }
+
+    // next(job) -> whether there is one; finish(job, sums) writes a tile.  Both are reached by the whole workgroup.
+    template <class Next, class Finish>
+    __device__ __forceinline__ void run(Next &&next, Finish &&finish) const
+    {
+        Job job, then;
+        bool more = next(job);
+        int buffer = 0;
+        if (more && job.k > 0) issue(job, 0, steps_of(job), 0);
+        while (more) {
+            const int per_run = steps_of(job), steps = per_run * job.runs;
+            Sums sums;
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) sums[h][mb][nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
+            more = next(then);
+            for (int s = 0; s < steps; ++s) {
+                // this wavefront's loads of stage s have landed and its reads of the stage before are done; behind the barrier everyone's
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                if (s + 1 < steps) issue(job, s + 1, per_run, buffer ^ 1);
+                else if (more && then.k > 0) issue(then, 0, steps_of(then), buffer ^ 1);
+                multiply(sums, buffer);
+                buffer ^= 1;
+            }
+            finish(job, sums);
+            if (steps == 0 && more && then.k > 0) {
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // nobody reads that buffer any more
+                issue(then, 0, steps_of(then), buffer);
+            }
+            job = then;
+        }
+    }
+};
+
+// Where the row tiles of groups lie: prefix[e] tiles in front of group e's, as many as its rows ask for.  offset [E + 1] is the caller's table; an entry
+// that goes back, or past the rows there are, is taken for the nearest that does not.
+struct RowTiles {
+    int *prefix;                               // LDS, E + 1
+    const int32_t *offset;
+    int E, rows, tile;                         // rows of the matrix, of a tile
+
+    __device__ __forceinline__ int first(int e) const
+    {
+        if (!offset) return 0;
+        const int v = offset[e];
+        return v < 0 ? 0 : v > rows ? rows : v;
+    }
+    __device__ __forceinline__ int end(int e, int from) const
+    {
+        if (!offset) return rows;
+        const int v = offset[e + 1];
+        return v < from ? from : v > rows ? rows : v;
+    }
+    // by the first wavefront; the workgroup's barrier follows.  -> total
+    __device__ __forceinline__ void count() const
+    {
+        const int lane = threadIdx.x;
+        if (lane < WAVE) {
+            int before = 0;
+            for (int e0 = 0; e0 < E; e0 += WAVE) {
+                const int e = e0 + lane;
+                int n = 0;
+                if (e < E) {
+                    const int lo = first(e);
+                    n = (end(e, lo) - lo + tile - 1) / tile;
+                }
+                const int upto = wave_scan_incl(n);
+                if (e < E) prefix[e] = before + upto - n;
+                before += __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (lane == 0) prefix[E] = before;
+        }
+        __syncthreads();
+    }
+    // the group of row tile t and its rows
+    __device__ __forceinline__ int find(int t, int &lo, int &hi) const
+    {
+        int e = 0, past = E;                   // prefix[e] <= t < prefix[past]
+        while (past - e > 1) {
+            const int mid = (e + past) >> 1;
+            if (prefix[mid] <= t) e = mid;
+            else past = mid;
+        }
+        e = __builtin_amdgcn_readfirstlane(e);
+        const int from = first(e), until = end(e, from);
+        lo = __builtin_amdgcn_readfirstlane(from + (t - prefix[e]) * tile);
+        hi = __builtin_amdgcn_readfirstlane(until);
+        return e;
+    }
+};
+
+// Unit u of n_m x n_n tiles: neighbours in groups of `tall` rows of tiles, column after column, so that the workgroups which run side by side on an XCD
+// share the operands' tiles in its L2.
+__device__ __forceinline__ void product_place(int u, int n_m, int n_n, int tall, int &m, int &n)
+{
+    const int per = tall * n_n, group = u / per, in = u - group * per;
+    const int first = group * tall, h = n_m - first < tall ? n_m - first : tall;
+    n = in / h;
+    m = first + in - n * h;
+}
+
+// The units of a persistent workgroup: the ids that the hardware deals to one XCD take a contiguous range of them, side by side.
+struct Units {
+    int at, end, by;
+    __device__ __forceinline__ Units(int total)
+    {
+        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = (total + 7) >> 3;
+        at = xcd * per + slot;
+        end = (xcd + 1) * per < total ? (xcd + 1) * per : total;
+        by = gridDim.x >> 3;                   // grids are multiples of 8
+    }
+    __device__ __forceinline__ bool take(int &u)
+    {
+        if (at >= end) return false;
+        u = at;
+        at += by;
+        return true;
+    }
+};
+__host__ __device__ constexpr int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
+static inline int product_grid(long long units, int resident)
+{
+    const long long n = units < resident ? units : resident;
+    return (int)((n + 7) / 8 * 8);
+}
+
+}  // namespace moe

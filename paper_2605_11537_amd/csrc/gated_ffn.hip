@@ -66,8 +66,9 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
     return g > 0.f ? g : g != g ? g : 0.f;
 }
 
-// g and u of four neighbouring columns lie side by side, so that both products' lanes read and write 32 bytes
-__device__ __forceinline__ float *states_at(float *gu, size_t row, int F, int column) { return gu + (row * F + column) * 2; }
+// Sixteen columns' g, then their u: what the four lanes of a row write and read lies in runs of 64 bytes.
+__host__ __device__ constexpr int states_width(int F) { return (F + 15) / 16 * 32; }
+__device__ __forceinline__ float *states_at(float *gu, size_t row, int F, int column) { return gu + row * states_width(F) + (column >> 4) * 32 + (column & 15); }
 
 struct GatedArgs {
     const void *x, *w_gate, *w_up, *w_down, *dy;
@@ -80,32 +81,31 @@ struct GatedArgs {
 // ------------------------------------------------------------------------------------------------- products over rows sorted by expert
 enum GatedStep { GATED_HIDDEN, GATED_DOWN, GATED_DHIDDEN, GATED_DX };
 
-template <int STEP, class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void gated_rows_kernel(GatedArgs p, int tall)
+// STEP's tiles of type TILE in the units first .. past-1 of n_m x n_n tiles of BIG_M rows x BIG_N columns (of a half), each cut into TILEs
+template <int STEP, class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int Z = sizeof(T);
-    __shared__ __align__(1024) char smem[TILE::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1];
-    const RowTiles tiles = {prefix, p.offset, p.E, p.R, TILE::BM};
-    tiles.count();
+    constexpr int Z = sizeof(T), PARTS_M = BIG_M / TILE::BM, PARTS_N = BIG_N / TILE::HALF_N, PARTS = PARTS_M * PARTS_N;
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
-    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(N, TILE::HALF_N);
     const unsigned d_bytes = p.d * Z, f_bytes = p.F * Z;
     const unsigned lda = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? d_bytes : STEP == GATED_DOWN ? f_bytes : 2 * f_bytes;
     const unsigned ldb = STEP == GATED_HIDDEN || STEP == GATED_DX ? f_bytes : d_bytes;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const bool with_states = p.gu != nullptr;
-    Units units(n_m * n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
             int u, m, n, lo, hi;
-            if (!units.take(u)) return false;
-            product_place(u, n_m, n_n, tall, m, n);
-            j.group = tiles.find(m, lo, hi);
+            do {
+                if (!units.take(u)) return false;
+                product_place(first + u / PARTS, n_m, n_n, tall, m, n);
+                j.group = tiles.find(m, lo, hi);
+                lo += u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = n * BIG_N + u % PARTS_N * TILE::HALF_N;
+            } while (PARTS > 1 && (lo >= hi || j.n0 >= N));             // a part behind the last row or column
             j.m0 = lo;
             j.rows = hi - lo < TILE::BM ? hi - lo : TILE::BM;
-            j.n0 = n * TILE::HALF_N;
             j.columns = N - j.n0 < TILE::HALF_N ? N - j.n0 : TILE::HALF_N;
             j.runs = 1;
             const size_t w = (size_t)j.group * p.d * f_bytes;          // the expert's first byte in each of its matrices
@@ -134,71 +134,119 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void gated_rows_ker
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
+            const int left = j.columns - tile.first_column();          // columns of D from this wavefront's first on
+            const int n0 = j.n0 + tile.first_column(), g4 = ((threadIdx.x & 63) >> 4) * 4;
+            if constexpr (STEP == GATED_DHIDDEN) {
+                // the states of a row of blocks are asked for a row ahead
+                product_f32x4 gate[2][TILE::NB], up[2][TILE::NB];
+                auto ask = [&](int mb) {
+                    const int row = tile.of_row(mb);
+                    const float *gu = states_at(p.gu, (size_t)(j.m0 + (row < j.rows ? row : 0)), p.F, n0 + g4);
 #pragma unroll
-            for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                if (row >= j.rows) continue;
-                const size_t r = (size_t)(j.m0 + row);
+                    for (int nb = 0; nb < TILE::NB; ++nb) {
+                        const bool there = nb * 16 + g4 < left;
+                        const product_f32x4 *at = reinterpret_cast<const product_f32x4 *>(there ? gu + nb * 32 : p.gu);
+                        gate[mb & 1][nb] = at[0];
+                        up[mb & 1][nb] = at[4];
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                ask(0);
 #pragma unroll
-                for (int nb = 0; nb < TILE::NB; ++nb) {
-                    const int column = tile.of_column(nb);
-                    if (column >= j.columns) continue;
-                    const int n = j.n0 + column;
-                    const product_f32x4 v = sums[0][mb][nb];
-                    if constexpr (STEP == GATED_HIDDEN) {
-                        const product_f32x4 up = sums[1][mb][nb];
-                        product_f32x4 h;
+                for (int mb = 0; mb < TILE::MB; ++mb) {
+                    if (mb + 1 < TILE::MB) ask(mb + 1);
+                    product_f32x4 dg[TILE::NB], du[TILE::NB];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) h[i] = act_of<Z == 4>(p.activation, v[i]) * up[i];
-                        store4((T *)p.h + r * p.F + n, h);
-                        if (with_states) {
-                            float *gu = states_at(p.gu, r, p.F, n);
-                            store4(gu, v);
-                            store4(gu + 4, up);
-                        }
-                    } else if constexpr (STEP == GATED_DHIDDEN) {
-                        const float *gu = states_at(p.gu, r, p.F, n);
-                        const product_f32x4 g = *reinterpret_cast<const product_f32x4 *>(gu), up = *reinterpret_cast<const product_f32x4 *>(gu + 4);
-                        product_f32x4 dg, du;
+                    for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             float slope;
-                            du[i] = v[i] * act_of<Z == 4>(p.activation, g[i], slope);
-                            dg[i] = v[i] * up[i] * slope;
+                            const float v = sums[0][mb][nb][i];
+                            du[nb][i] = v * act_of<Z == 4>(p.activation, gate[mb & 1][nb][i], slope);
+                            dg[nb][i] = v * up[mb & 1][nb][i] * slope;
                         }
-                        T *to = (T *)p.dgu + r * 2 * p.F + n;
-                        store4(to, dg);
-                        store4(to + p.F, du);
-                    } else store4((T *)(STEP == GATED_DOWN ? p.y : p.dx) + r * p.d + n, v);
+                    const int row = tile.of_row(mb);
+                    T *to = (T *)p.dgu + (size_t)(j.m0 + row) * 2 * p.F + n0;
+                    auto fits = [&](int column) { return row < j.rows && column < left; };
+                    write_row(to, dg, fits);
+                    write_row(to + p.F, du, fits);
                 }
+                return;
+            }
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = tile.of_row(mb);
+                const size_t r = (size_t)(j.m0 + row);
+                auto fits = [&](int column) { return row < j.rows && column < left; };
+                if constexpr (STEP == GATED_HIDDEN) {
+                    product_f32x4 h[TILE::NB];
+#pragma unroll
+                    for (int nb = 0; nb < TILE::NB; ++nb) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) h[nb][i] = act_of<Z == 4>(p.activation, sums[0][mb][nb][i]) * sums[1][mb][nb][i];
+                        if (with_states && fits(nb * 16 + g4)) {
+                            float *gu = states_at(p.gu, r, p.F, n0 + nb * 16 + g4);
+                            store4(gu, sums[0][mb][nb]);
+                            store4(gu + 16, sums[1][mb][nb]);
+                        }
+                    }
+                    write_row((T *)p.h + r * p.F + n0, h, fits);
+                } else write_row((T *)(STEP == GATED_DOWN ? p.y : p.dx) + r * p.d + n0, sums[0][mb], fits);
             }
         });
 }
 
+template <int STEP, class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(GatedArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    __shared__ int prefix[MAX_GROUPS + 1];
+    const RowTiles tiles = {prefix, p.offset, p.E, p.R, Big::BM};
+    tiles.count();
+    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, Big::HALF_N);
+    in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
+        gated_rows<STEP, typename decltype(sized)::Type, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, past, tall);
+    });
+}
+
+// tiles of few rows, one size
+template <int STEP, class TILE>
+__global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedArgs p)
+{
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    __shared__ int prefix[MAX_GROUPS + 1];
+    const RowTiles tiles = {prefix, p.offset, p.E, p.R, TILE::BM};
+    tiles.count();
+    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
+    gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N>(p, tiles, smem, n_m, n_n, 0, n_m * n_n, 8);
+}
+
 // ------------------------------------------------------------------------------------------------- the weights' gradients
 // DOWN: dW_down = h^T dy, F x d; else dW_gate and dW_up = x^T [dg | du], d x 2F.  An expert without rows gets zeros.
-template <bool DOWN, class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void gated_weights_kernel(GatedArgs p, int tall)
+template <bool DOWN, class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int Z = sizeof(T);
-    __shared__ __align__(1024) char smem[TILE::LDS];
+    constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const RowTiles tiles = {nullptr, p.offset, p.E, p.R, 1};
     const int M = DOWN ? p.F : p.d, N = DOWN ? p.d : 2 * p.F;
-    const int n_m = tiles_of(M, TILE::BM), n_n = tiles_of(N, TILE::BN);
     const unsigned lda = M * Z, ldb = N * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
-    Units units(p.E * n_m * n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
-            int u, m, n;
-            if (!units.take(u)) return false;
-            const int e = u / (n_m * n_n);
-            product_place(u - e * n_m * n_n, n_m, n_n, tall, m, n);
+            int u, m, n, e;
+            do {
+                if (!units.take(u)) return false;
+                const int big = first + u / PARTS;
+                e = big / (n_m * n_n);
+                product_place(big - e * n_m * n_n, n_m, n_n, tall, m, n);
+                j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
+            } while (PARTS > 1 && (j.m0 >= M || j.n0 >= N));
             const int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e, lo));
             j.group = e;
-            j.m0 = m * TILE::BM;
-            j.n0 = n * TILE::BN;
             j.rows = M - j.m0 < TILE::BM ? M - j.m0 : TILE::BM;
             j.columns = N - j.n0 < TILE::BN ? N - j.n0 : TILE::BN;
             j.runs = 1;
@@ -209,74 +257,84 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void gated_weights_
         },
         [&](const Job &j, typename TILE::Sums &sums) {
             const size_t w = (size_t)j.group * p.d * p.F;
+            const int left = j.columns - tile.first_column(), n = j.n0 + tile.first_column();
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
                 const int row = tile.of_row(mb);
-                if (row >= j.rows) continue;
-#pragma unroll
-                for (int nb = 0; nb < TILE::NB; ++nb) {
-                    const int column = tile.of_column(nb);
-                    if (column >= j.columns) continue;
-                    const int n = j.n0 + column;
-                    T *to;
-                    if (DOWN) to = (T *)p.dw_down + w + (size_t)(j.m0 + row) * p.d + n;
-                    else to = (T *)(n < p.F ? p.dw_gate : p.dw_up) + w + (size_t)(j.m0 + row) * p.F + (n < p.F ? n : n - p.F);
-                    store4(to, sums[0][mb][nb]);
+                const size_t at = w + (size_t)(j.m0 + row) * (DOWN ? p.d : p.F) + n;
+                if (DOWN) write_row((T *)p.dw_down + at, sums[0][mb], [&](int c) { return row < j.rows && c < left; });
+                else {
+                    // columns of the two matrices side by side
+                    if (n < p.F) write_row((T *)p.dw_gate + at, sums[0][mb], [&](int c) { return row < j.rows && c < left && n + c < p.F; });
+                    if (n + TILE::WAVE_N > p.F)
+                        write_row((T *)p.dw_up + at - p.F, sums[0][mb], [&](int c) { return row < j.rows && c < left && n + c >= p.F; });
                 }
             }
         });
 }
 
-// ------------------------------------------------------------------------------------------------- host
-template <class TILE>
-constexpr int resident() { return 256 * (160 * 1024 / (TILE::LDS + 4 * (MAX_GROUPS + 4))); }
+template <bool DOWN, class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel(GatedArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    const int n_m = tiles_of(DOWN ? p.F : p.d, Big::BM), n_n = tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
+    in_rounds<SIZES>(p.E * n_m * n_n, [&](auto sized, int first, int past) {
+        gated_weights<DOWN, typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+    });
+}
 
-template <int STEP, class TILE>
+// ------------------------------------------------------------------------------------------------- host
+template <int STEP, class SIZES>
 void launch_rows(const GatedArgs &p, hipStream_t st)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
+    const long long units = ((long long)p.R / Big::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, Big::HALF_N);
+    hipLaunchKernelGGL((gated_rows_kernel<STEP, SIZES>), dim3(product_grid(units, PRODUCT_CUS * SIZES::PER_CU)), dim3(Big::THREADS), 0, st, p, 8);
+}
+template <int STEP, class TILE>
+void launch_few_rows(const GatedArgs &p, hipStream_t st)
 {
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
     const long long units = ((long long)p.R / TILE::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, TILE::HALF_N);
-    hipLaunchKernelGGL((gated_rows_kernel<STEP, TILE>), dim3(product_grid(units, resident<TILE>())), dim3(TILE::THREADS), 0, st, p, 8);
+    constexpr int per_cu = 160 * 1024 / (TILE::LDS + 4 * (MAX_GROUPS + 4));
+    const long long grid = units < PRODUCT_CUS * per_cu ? units : PRODUCT_CUS * per_cu;
+    hipLaunchKernelGGL((gated_few_rows_kernel<STEP, TILE>), dim3((unsigned)((grid + 7) / 8 * 8)), dim3(TILE::THREADS), 0, st, p);
 }
-template <bool DOWN, class TILE>
+template <bool DOWN, class SIZES>
 void launch_weights(const GatedArgs &p, hipStream_t st)
 {
-    const int M = DOWN ? p.F : p.d, N = DOWN ? p.d : 2 * p.F;
-    const long long units = (long long)p.E * tiles_of(M, TILE::BM) * tiles_of(N, TILE::BN);
-    hipLaunchKernelGGL((gated_weights_kernel<DOWN, TILE>), dim3(product_grid(units, resident<TILE>())), dim3(TILE::THREADS), 0, st, p, 8);
+    typedef typename Whole<SIZES>::Tile Big;
+    const long long units = (long long)p.E * tiles_of(DOWN ? p.F : p.d, Big::BM) * tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
+    hipLaunchKernelGGL((gated_weights_kernel<DOWN, SIZES>), dim3(product_grid(units, PRODUCT_CUS * SIZES::PER_CU)), dim3(Big::THREADS), 0, st, p, 8);
 }
 
 // rows of an expert for which a tile of so many rows is taken
 bool tall_tiles(int R, int E) { return R / E >= 96; }
 
 template <class T>
-struct Tiles;
+struct Few;
 template <>
-struct Tiles<bf16_t> {
+struct Few<bf16_t> {
     template <Order B, int HALVES = 1>
-    using Tall = Tile<bf16_t, ALONG_K, B, 256, 256, 2, 4, HALVES>;
-    template <Order B, int HALVES = 1>
-    using Flat = Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES>;
-    using Weights = Tile<bf16_t, ACROSS_K, ACROSS_K, 256, 256, 2, 4>;
+    using Tile = moe::Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES>;
 };
 template <>
-struct Tiles<float> {
+struct Few<float> {
     template <Order B, int HALVES = 1>
-    using Tall = Tile<float, ALONG_K, B, 128, 128, 2, 2, HALVES>;
-    template <Order B, int HALVES = 1>
-    using Flat = Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES>;
-    using Weights = Tile<float, ACROSS_K, ACROSS_K, 128, 128, 2, 2>;
+    using Tile = moe::Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES>;
 };
 
 template <class T>
 void forward(const GatedArgs &p, hipStream_t st)
 {
     if (tall_tiles(p.R, p.E)) {
-        launch_rows<GATED_HIDDEN, typename Tiles<T>::template Tall<ACROSS_K, 2>>(p, st);
-        launch_rows<GATED_DOWN, typename Tiles<T>::template Tall<ACROSS_K>>(p, st);
+        launch_rows<GATED_HIDDEN, Sizes<T, ALONG_K, ACROSS_K, 2>>(p, st);
+        launch_rows<GATED_DOWN, Sizes<T, ALONG_K, ACROSS_K>>(p, st);
     } else {
-        launch_rows<GATED_HIDDEN, typename Tiles<T>::template Flat<ACROSS_K, 2>>(p, st);
-        launch_rows<GATED_DOWN, typename Tiles<T>::template Flat<ACROSS_K>>(p, st);
+        launch_few_rows<GATED_HIDDEN, typename Few<T>::template Tile<ACROSS_K, 2>>(p, st);
+        launch_few_rows<GATED_DOWN, typename Few<T>::template Tile<ACROSS_K>>(p, st);
     }
 }
 template <class T>
@@ -284,14 +342,14 @@ void backward(const GatedArgs &p, hipStream_t st)
 {
     if (p.R == 0) {                            // zeros for every weight
     } else if (tall_tiles(p.R, p.E)) {
-        launch_rows<GATED_DHIDDEN, typename Tiles<T>::template Tall<ALONG_K>>(p, st);
-        if (p.dx) launch_rows<GATED_DX, typename Tiles<T>::template Tall<ALONG_K>>(p, st);
+        launch_rows<GATED_DHIDDEN, Sizes<T, ALONG_K, ALONG_K>>(p, st);
+        if (p.dx) launch_rows<GATED_DX, Sizes<T, ALONG_K, ALONG_K>>(p, st);
     } else {
-        launch_rows<GATED_DHIDDEN, typename Tiles<T>::template Flat<ALONG_K>>(p, st);
-        if (p.dx) launch_rows<GATED_DX, typename Tiles<T>::template Flat<ALONG_K>>(p, st);
+        launch_few_rows<GATED_DHIDDEN, typename Few<T>::template Tile<ALONG_K>>(p, st);
+        if (p.dx) launch_few_rows<GATED_DX, typename Few<T>::template Tile<ALONG_K>>(p, st);
     }
-    if (p.dw_gate) launch_weights<false, typename Tiles<T>::Weights>(p, st);
-    if (p.dw_down) launch_weights<true, typename Tiles<T>::Weights>(p, st);
+    if (p.dw_gate) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
+    if (p.dw_down) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
 }
 
 size_t hidden_bytes(int R, int F, int dtype) { return align_up((size_t)R * F * (dtype == MOE_F32 ? 4 : 2), 256); }
@@ -317,7 +375,7 @@ using namespace moe;
 
 extern "C" size_t moe_gated_ffn_states_bytes(int R, int F, int dtype)
 {
-    return R <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype) + (size_t)R * F * 8;
+    return R <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype) + (size_t)R * states_width(F) * 4;
 }
 
 extern "C" size_t moe_gated_ffn_workspace_bytes(int R, int E, int d, int F, int dtype)

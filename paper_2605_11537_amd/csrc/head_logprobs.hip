@@ -21,12 +21,12 @@ struct HeadArgs {
     const int32_t *target;
     int N, d, V;
     int v0, columns, ld;                       // backward: the piece's first id, its ids, and the row of dz it is kept in
-    int n_n;                                   // forward: tiles of a row
+    int n_n;                                   // forward: slots of a row
     float2 *tiles;                             // forward [N, n_n]: maximum, sum
     float *at_target;                          // forward [N]
     const float *largest;                      // backward: |dlogprob|
     void *dz;
-    float *db;                                 // backward [rows of tiles x wavefront rows, V], or NULL
+    float *db;                                 // backward [slots of a wavefront's rows, V], or NULL
 };
 
 __device__ __forceinline__ float finite_or(float m, float other) { return m == HEAD_NONE ? other : m; }
@@ -35,6 +35,7 @@ __device__ __forceinline__ float finite_or(float m, float other) { return m == H
 template <class TILE>
 __device__ __forceinline__ void add_bias(const TILE &tile, const Job &j, const float *b, int V, typename TILE::Sums &z)
 {
+    if (!b && j.columns == TILE::BN) return;
 #pragma unroll
     for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
@@ -46,41 +47,54 @@ __device__ __forceinline__ void add_bias(const TILE &tile, const Job &j, const f
         }
 }
 
-// over the four lane groups that hold a row's columns
+// over the four lane groups that hold a row's columns: rows of 16 lanes, then halves of 32, exchanged among registers
 __device__ __forceinline__ float row_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 __device__ __forceinline__ float row_sum(float v)
 {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+// e^x for x <= 0 up to some tens (a logit beside its row's maximum or log sum): the exponent's product is off by |x| 2^-24
+__device__ __forceinline__ float exp_beside(float z, float beside) { return __builtin_amdgcn_exp2f((z - beside) * LOG2E); }
+
+// where column `in` of a wavefront's is one of this lane's: block, register
+template <class TILE>
+__device__ __forceinline__ bool holds_column(int in)
+{
+    return in >= 0 && in < TILE::WAVE_N && ((in >> 2) & 3) == (int)((threadIdx.x & 63) >> 4);
 }
 
-template <class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_forward_kernel(HeadArgs p, int tall)
+// The units first .. past-1 of n_m x n_n tiles of BIG_M x BIG_N, each cut into TILEs (below likewise); here all have BIG_N columns, for which a row has one
+// slot.
+template <class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, float2 *parts, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int WN = TILE::BN / TILE::WAVE_N;
-    __shared__ __align__(1024) char smem[TILE::LDS];
-    __shared__ float2 parts[WN][TILE::BM];
+    constexpr int WN = TILE::BN / TILE::WAVE_N, PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned d_bytes = p.d * sizeof(T);
-    const int n_m = tiles_of(p.N, TILE::BM);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
-    Units units(n_m * p.n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
             int u, m, n;
-            if (!units.take(u)) return false;
-            product_place(u, n_m, p.n_n, tall, m, n);
-            j.m0 = m * TILE::BM;
-            j.n0 = n * TILE::BN;
+            do {
+                if (!units.take(u)) return false;
+                product_place(first + u / PARTS, n_m, n_n, tall, m, n);
+                j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
+            } while (PARTS > 1 && (j.m0 >= p.N || j.n0 >= p.V));
             j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
             j.columns = p.V - j.n0 < TILE::BN ? p.V - j.n0 : TILE::BN;
             j.k = p.d;
             j.runs = 1;
-            j.group = n;
             j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
             j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
             return true;
@@ -96,30 +110,60 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_forward_k
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        m = fmaxf(m, z[0][mb][nb][i]);
-                        if (target == j.n0 + tile.of_column(nb) + i && target < p.V) p.at_target[j.m0 + row] = z[0][mb][nb][i];
-                    }
+                    for (int i = 0; i < 4; ++i) m = fmaxf(m, z[0][mb][nb][i]);
+                const int in = target - j.n0 - tile.wn * TILE::WAVE_N;
+                if (holds_column<TILE>(in) && target < p.V) {
+                    float hit = 0.f;
+#pragma unroll
+                    for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) hit = in >> 4 == nb && (in & 3) == i ? z[0][mb][nb][i] : hit;
+                    p.at_target[j.m0 + row] = hit;
+                }
                 m = row_max(m);
                 const float beside = finite_or(m, 0.f);
                 float s = 0.f;
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s += exp_of<true>(z[0][mb][nb][i] - beside);
+                    for (int i = 0; i < 4; ++i) s += exp_beside(z[0][mb][nb][i], beside);
                 s = row_sum(s);
-                if (lane < 16) parts[tile.wn][row] = make_float2(m, s);
+                if (lane < 16) parts[tile.wn * TILE::BM + row] = make_float2(m, s);
             }
             __syncthreads();
             for (int row = threadIdx.x; row < j.rows; row += TILE::THREADS) {
                 float m = HEAD_NONE, s = 0.f;
 #pragma unroll
-                for (int w = 0; w < WN; ++w) m = fmaxf(m, parts[w][row].x);
+                for (int w = 0; w < WN; ++w) m = fmaxf(m, parts[w * TILE::BM + row].x);
 #pragma unroll
-                for (int w = 0; w < WN; ++w) s += parts[w][row].y * exp_of<true>(finite_or(parts[w][row].x, 0.f) - finite_or(m, 0.f));
-                p.tiles[(size_t)(j.m0 + row) * p.n_n + j.group] = make_float2(m, s);
+                for (int w = 0; w < WN; ++w) {
+                    const float2 part = parts[w * TILE::BM + row];
+                    s += part.y * exp_beside(finite_or(part.x, 0.f), finite_or(m, 0.f));
+                }
+                p.tiles[(size_t)(j.m0 + row) * n_n + j.n0 / TILE::BN] = make_float2(m, s);
             }
         });
+}
+
+template <class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(HeadArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    __shared__ float2 parts[4 * Big::BM];
+    const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.V, Big::BN);
+    in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
+        static_assert(decltype(sized)::Type::BN == Big::BN, "one slot for a row's columns of a tile");
+        head_forward<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, parts, n_m, n_n, first, past, tall);
+    });
+}
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(HeadArgs p)
+{
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    __shared__ float2 parts[4 * TILE::BM];
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
+    head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, n_m * n_n, 8);
 }
 
 // One wavefront per row: its tiles' maxima and sums -> lse and the target's log probability.
@@ -153,30 +197,29 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, con
     }
 }
 
-template <class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dlogits_kernel(HeadArgs p, int tall)
+template <class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int WM = TILE::BM / TILE::WAVE_M;
-    __shared__ __align__(1024) char smem[TILE::LDS];
+    constexpr int PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned d_bytes = p.d * sizeof(T);
-    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     const float largest = *p.largest;
-    Units units(n_m * n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
             int u, m, n;
-            if (!units.take(u)) return false;
-            product_place(u, n_m, n_n, tall, m, n);
-            j.m0 = m * TILE::BM;
-            j.n0 = p.v0 + n * TILE::BN;
+            do {
+                if (!units.take(u)) return false;
+                product_place(first + u / PARTS, n_m, n_n, tall, m, n);
+                j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = p.v0 + n * BIG_N + u % PARTS_N * TILE::BN;
+            } while (PARTS > 1 && (j.m0 >= p.N || j.n0 >= p.v0 + p.columns));
             j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
             const int left = p.v0 + p.columns - j.n0;
             j.columns = left < TILE::BN ? left : TILE::BN;
             j.k = p.d;
             j.runs = 1;
-            j.group = m;
             j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
             j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
             return true;
@@ -193,21 +236,24 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dlogits_k
                 const int target = there ? p.target[j.m0 + row] : -1;
                 const bool on = target >= 0 && target < p.V;
                 const float g = on ? p.dlogprob[j.m0 + row] / largest : 0.f;
-                const float lse = on ? p.lse[j.m0 + row] : 0.f;
+                const float lse = on ? finite_or(p.lse[j.m0 + row], 0.f) : 0.f;
+                product_f32x4 dz[TILE::NB];
 #pragma unroll
-                for (int nb = 0; nb < TILE::NB; ++nb) {
-                    const int column = tile.of_column(nb);
-                    product_f32x4 dz;
+                for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = z[0][mb][nb][i];
-                        const float prob = x == HEAD_NONE ? 0.f : exp_of<true>(x - lse);
-                        dz[i] = on ? g * ((j.n0 + column + i == target ? 1.f : 0.f) - prob) : 0.f;
-                    }
-                    down[nb] += dz;
-                    // a row of dz ends with zeros up to a whole piece of 16 bytes
-                    if (there && j.n0 - p.v0 + column < p.ld) store4((T *)p.dz + (size_t)(j.m0 + row) * p.ld + (j.n0 - p.v0 + column), dz);
+                    for (int i = 0; i < 4; ++i) dz[nb][i] = on ? -g * exp_beside(z[0][mb][nb][i], lse) : 0.f;
+                const int in = target - j.n0 - tile.wn * TILE::WAVE_N;
+                if (on && holds_column<TILE>(in)) {
+#pragma unroll
+                    for (int nb = 0; nb < TILE::NB; ++nb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) dz[nb][i] += in >> 4 == nb && (in & 3) == i ? g : 0.f;
                 }
+#pragma unroll
+                for (int nb = 0; nb < TILE::NB; ++nb) down[nb] += dz[nb];
+                // a row of dz ends with zeros up to a whole piece of 16 bytes
+                const int at = j.n0 - p.v0 + tile.first_column();
+                write_row((T *)p.dz + (size_t)(j.m0 + row) * p.ld + at, dz, [&](int c) { return there && at + c < p.ld; });
             }
             if (p.db) {
 #pragma unroll
@@ -218,10 +264,31 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dlogits_k
 #pragma unroll
                         for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o, 64);
                         const int v = j.n0 + tile.of_column(nb) + i;
-                        if ((threadIdx.x & 15) == 0 && v < p.V) p.db[(size_t)(j.group * WM + tile.wm) * p.V + v] = s;
+                        // a slot for a wavefront's rows, of which all tiles of the launch have the same number
+                        if ((threadIdx.x & 15) == 0 && v < p.V && j.m0 + tile.wm * TILE::WAVE_M < p.N)
+                            p.db[(size_t)(j.m0 / TILE::WAVE_M + tile.wm) * p.V + v] = s;
                     }
             }
         });
+}
+
+template <class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dlogits_kernel(HeadArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.columns, Big::BN);
+    in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
+        static_assert(decltype(sized)::Type::WAVE_M == Big::WAVE_M, "one slot for a wavefront's rows");
+        head_dlogits<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+    });
+}
+template <class TILE>
+__global__ __launch_bounds__(TILE::THREADS, 2) void head_dlogits_few_kernel(HeadArgs p)
+{
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
+    head_dlogits<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, n_m * n_n, 8);
 }
 
 // ------------------------------------------------------------------------------------------------- the two products of the gradient
@@ -235,25 +302,26 @@ struct HeadGradArgs {
     const float *largest;
 };
 
-template <class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dh_kernel(HeadGradArgs p, int tall)
+template <class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int Z = sizeof(T);
-    __shared__ __align__(1024) char smem[TILE::LDS];
+    constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned lda = p.ld * Z, ldb = p.d * Z;
-    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
     const TILE tile((product_lds_t *)smem, lda, ldb);
-    Units units(p.parts * n_m * n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
             int u, m, n;
-            if (!units.take(u)) return false;
-            const int part = u / (n_m * n_n), k0 = part * p.part;
-            product_place(u - part * n_m * n_n, n_m, n_n, tall, m, n);
-            j.group = part;
-            j.m0 = m * TILE::BM;
-            j.n0 = n * TILE::BN;
+            do {
+                if (!units.take(u)) return false;
+                const int big = first + u / PARTS;
+                j.group = big / (n_m * n_n);
+                product_place(big - j.group * n_m * n_n, n_m, n_n, tall, m, n);
+                j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
+            } while (PARTS > 1 && (j.m0 >= p.N || j.n0 >= p.d));
+            const int k0 = j.group * p.part;
             j.rows = p.N - j.m0 < TILE::BM ? p.N - j.m0 : TILE::BM;
             j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
             j.runs = 1;
@@ -282,25 +350,42 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dh_kernel
         });
 }
 
+template <class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dh_kernel(HeadGradArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.d, Big::BN);
+    in_rounds<SIZES>(p.parts * n_m * n_n, [&](auto sized, int first, int past) {
+        head_dh<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+    });
+}
 template <class TILE>
-__global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dw_kernel(HeadGradArgs p, int tall)
+__global__ __launch_bounds__(TILE::THREADS, 2) void head_dh_few_kernel(HeadGradArgs p)
+{
+    __shared__ __align__(1024) char smem[TILE::LDS];
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
+    head_dh<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, p.parts * n_m * n_n, 8);
+}
+
+template <class TILE, int BIG_M, int BIG_N>
+__device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
 {
     typedef typename TILE::T T;
-    constexpr int Z = sizeof(T);
-    __shared__ __align__(1024) char smem[TILE::LDS];
+    constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned lda = p.ld * Z, ldb = p.d * Z;
-    const int n_m = tiles_of(p.columns, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const float largest = *p.largest;
-    Units units(n_m * n_n);
+    Units units((past - first) * PARTS);
     tile.run(
         [&](Job &j) {
             int u, m, n;
-            if (!units.take(u)) return false;
-            product_place(u, n_m, n_n, tall, m, n);
-            j.group = 0;
-            j.m0 = m * TILE::BM;
-            j.n0 = n * TILE::BN;
+            do {
+                if (!units.take(u)) return false;
+                product_place(first + u / PARTS, n_m, n_n, tall, m, n);
+                j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
+                j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
+            } while (PARTS > 1 && (j.m0 >= p.columns || j.n0 >= p.d));
             j.rows = p.columns - j.m0 < TILE::BM ? p.columns - j.m0 : TILE::BM;
             j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
             j.runs = 1;
@@ -310,18 +395,27 @@ __global__ __launch_bounds__(TILE::THREADS, TILE::WAVES / 4) void head_dw_kernel
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
+            const int left = j.columns - tile.first_column();
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
                 const int row = tile.of_row(mb);
-                if (row >= j.rows) continue;
 #pragma unroll
-                for (int nb = 0; nb < TILE::NB; ++nb) {
-                    const int column = tile.of_column(nb);
-                    if (column >= j.columns) continue;
-                    store4((T *)p.dw + (size_t)(p.v0 + j.m0 + row) * p.d + j.n0 + column, sums[0][mb][nb] * largest);
-                }
+                for (int nb = 0; nb < TILE::NB; ++nb) sums[0][mb][nb] *= largest;
+                write_row((T *)p.dw + (size_t)(p.v0 + j.m0 + row) * p.d + j.n0 + tile.first_column(), sums[0][mb],
+                          [&](int c) { return row < j.rows && c < left; });
             }
         });
+}
+
+template <class SIZES>
+__global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dw_kernel(HeadGradArgs p, int tall)
+{
+    typedef typename Whole<SIZES>::Tile Big;
+    __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    const int n_m = tiles_of(p.columns, Big::BM), n_n = tiles_of(p.d, Big::BN);
+    in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
+        head_dw<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+    });
 }
 
 // ------------------------------------------------------------------------------------------------- rows
@@ -390,75 +484,80 @@ void launch_clear(void *p, size_t bytes, hipStream_t st)
     hipLaunchKernelGGL(head_clear_kernel, dim3((unsigned)(words / 256 < 2048 ? words / 256 + 1 : 2048)), dim3(256), 0, st, (unsigned *)p, words);
 }
 
+// tiles of 64 and of 16 rows
+template <class T, Order A, Order B>
+using Flat = Tile<T, A, B, 64, HEAD_FEW_COLUMNS, 1, 4>;
+template <class T, Order A, Order B>
+using Few = Tile<T, A, B, 16, HEAD_FEW_COLUMNS, 1, 4>;
+
+// parts of a tile with all of its columns, and with all of its rows
 template <class T>
-struct Tiles;
+struct RowParts;
 template <>
-struct Tiles<bf16_t> {
-    template <Order A, Order B>
-    using Tall = Tile<bf16_t, A, B, HEAD_TALL, 256, 2, 4>;
-    template <Order A, Order B>
-    using Flat = Tile<bf16_t, A, B, 64, 128, 1, 4>;
-    template <Order A, Order B>
-    using Few = Tile<bf16_t, A, B, 16, 128, 1, 4>;
+struct RowParts<bf16_t> : Sizes<bf16_t, ALONG_K, ALONG_K> {
+    typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 64, 256, 2, 4, 1, 3>> Quarter;
+    typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 32, 256, 2, 4, 1, 4>> Eighth;
 };
 template <>
-struct Tiles<float> {
-    template <Order A, Order B>
-    using Tall = Tile<float, A, B, 128, 128, 2, 2>;
-    template <Order A, Order B>
-    using Flat = Tile<float, A, B, 64, 128, 1, 4>;
-    template <Order A, Order B>
-    using Few = Tile<float, A, B, 16, 128, 1, 4>;
+struct RowParts<float> : Sizes<float, ALONG_K, ALONG_K> {
+    typedef Sized<Tile<float, ALONG_K, ALONG_K, 32, 128, 2, 2, 1, 3>> Quarter;
+    typedef Sized<Tile<float, ALONG_K, ALONG_K, 16, 128, 1, 4, 1, 4>> Eighth;
 };
+template <class T>
+struct ColumnParts;
+template <>
+struct ColumnParts<bf16_t> : Sizes<bf16_t, ALONG_K, ALONG_K> {
+    typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 256, 128, 2, 4, 1, 3>> Half;
+    typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 256, 64, 2, 4, 1, 3>> Quarter;
+    typedef Quarter Eighth;
+};
+template <>
+struct ColumnParts<float> : Sizes<float, ALONG_K, ALONG_K> {
+    typedef Sized<Tile<float, ALONG_K, ALONG_K, 128, 64, 2, 2, 1, 3>> Half;
+    typedef Sized<Tile<float, ALONG_K, ALONG_K, 128, 32, 2, 2, 1, 3>> Quarter;
+    typedef Quarter Eighth;
+};
+template <class T>
+struct AllParts : Sizes<T, ALONG_K, ACROSS_K> {};
 
 template <class TILE>
-int grid_of(long long units, int more_lds)
+dim3 few_grid(long long units, int more_lds)
 {
-    return product_grid(units, 256 * (160 * 1024 / (TILE::LDS + more_lds)));
+    const long long most = PRODUCT_CUS * (160 * 1024 / (TILE::LDS + more_lds));
+    return dim3((unsigned)(((units < most ? units : most) + 7) / 8 * 8));
 }
 
-template <class TILE>
-void launch_forward(const HeadArgs &p, hipStream_t st)
-{
-    hipLaunchKernelGGL(head_forward_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.N, TILE::BM) * p.n_n, 8 * TILE::BM * 4)), dim3(TILE::THREADS),
-                       0, st, p, 8);
-}
-template <class TILE>
-void launch_dlogits(const HeadArgs &p, hipStream_t st)
-{
-    hipLaunchKernelGGL(head_dlogits_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.N, TILE::BM) * tiles_of(p.columns, TILE::BN), 0)),
-                       dim3(TILE::THREADS), 0, st, p, 8);
-}
-template <class TILE>
-void launch_dh(const HeadGradArgs &p, hipStream_t st)
-{
-    hipLaunchKernelGGL(head_dh_kernel<TILE>, dim3(grid_of<TILE>((long long)p.parts * tiles_of(p.N, TILE::BM) * tiles_of(p.d, TILE::BN), 0)),
-                       dim3(TILE::THREADS), 0, st, p, 8);
-}
-template <class TILE>
-void launch_dw(const HeadGradArgs &p, hipStream_t st)
-{
-    hipLaunchKernelGGL(head_dw_kernel<TILE>, dim3(grid_of<TILE>((long long)tiles_of(p.columns, TILE::BM) * tiles_of(p.d, TILE::BN), 0)),
-                       dim3(TILE::THREADS), 0, st, p, 8);
-}
-
-// the tile by the number of rows
-#define HEAD_BY_ROWS(LAUNCH, A, B, ARGS, ST)                                                        \
-    switch (head_rows(N, dtype)) {                                                                  \
-    case HEAD_TALL_TILES: LAUNCH<typename Tiles<T>::template Tall<A, B>>(ARGS, ST); break;          \
-    case HEAD_FLAT_TILES: LAUNCH<typename Tiles<T>::template Flat<A, B>>(ARGS, ST); break;          \
-    default: LAUNCH<typename Tiles<T>::template Few<A, B>>(ARGS, ST);                               \
-    }
+// KERNEL for tiles of PARTS' sizes, or KERNEL_few for tiles of 64 or 16 rows, by the number of rows; M, N, TIMES: D and how often
+#define HEAD_BY_ROWS(KERNEL, PARTS, A, B, ARGS, ST, M, N, TIMES, LDS_ROWS)                                                                            \
+    do {                                                                                                                                       \
+        typedef PARTS<T> sizes;                                                                                                                \
+        typedef typename Whole<sizes>::Tile big;                                                                                               \
+        typedef Flat<T, A, B> flat;                                                                                                            \
+        typedef Few<T, A, B> few;                                                                                                              \
+        const HeadRows rows = head_rows(M);                                                                                                    \
+        if (rows == HEAD_TALL_TILES)                                                                                                           \
+            hipLaunchKernelGGL((KERNEL##_kernel<sizes>),                                                                                       \
+                               dim3(product_grid((long long)TIMES * tiles_of(M, big::BM) * tiles_of(N, big::BN), PRODUCT_CUS * sizes::PER_CU)), \
+                               dim3(big::THREADS), 0, ST, ARGS, 8);                                                                            \
+        else if (rows == HEAD_FLAT_TILES)                                                                                                      \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<flat>),                                                                                    \
+                               few_grid<flat>((long long)TIMES * tiles_of(M, flat::BM) * tiles_of(N, flat::BN), LDS_ROWS * flat::BM),          \
+                               dim3(flat::THREADS), 0, ST, ARGS);                                                                              \
+        else                                                                                                                                   \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<few>),                                                                                     \
+                               few_grid<few>((long long)TIMES * tiles_of(M, few::BM) * tiles_of(N, few::BN), LDS_ROWS * few::BM),              \
+                               dim3(few::THREADS), 0, ST, ARGS);                                                                               \
+    } while (0)
 
 template <class T>
-void forward(HeadArgs p, int N, int dtype, float *logprob, float *lse, hipStream_t st)
+void forward(const HeadArgs &p, int N, float *logprob, float *lse, hipStream_t st)
 {
-    HEAD_BY_ROWS(launch_forward, ALONG_K, ALONG_K, p, st)
+    HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
     hipLaunchKernelGGL(head_join_kernel, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
 }
 
 template <class T>
-void backward(HeadArgs p, const HeadShape &g, char *ws, int dtype, T *dh, T *dw, float *db, hipStream_t st)
+void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db, hipStream_t st)
 {
     const int N = p.N;
     float *const largest = (float *)ws, *const dh_parts = (float *)(ws + g.dh_at), *const db_parts = (float *)(ws + g.db_at);
@@ -474,18 +573,24 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, int dtype, T *dh, T *dw,
         p.v0 = v0;
         p.columns = p.V - v0 < g.piece ? p.V - v0 : g.piece;
         p.ld = (int)align_up(p.columns, 8);
-        HEAD_BY_ROWS(launch_dlogits, ALONG_K, ALONG_K, p, st)
+        HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
         HeadGradArgs q = {};
         q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.ld = p.ld, q.v0 = v0;
         q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), 64), q.add = v0 > 0;
         q.dh = dh_parts, q.dw = dw, q.largest = largest;
-        if (dh) HEAD_BY_ROWS(launch_dh, ALONG_K, ACROSS_K, q, st)
-        if (dw) launch_dw<typename Tiles<T>::template Tall<ACROSS_K, ACROSS_K>>(q, st);
+        if (dh) HEAD_BY_ROWS(head_dh, AllParts, ALONG_K, ACROSS_K, q, st, N, p.d, g.parts, 0);
+        if (dw) {
+            typedef Sizes<T, ACROSS_K, ACROSS_K> sizes;
+            typedef typename Whole<sizes>::Tile big;
+            hipLaunchKernelGGL((head_dw_kernel<sizes>),
+                               dim3(product_grid((long long)tiles_of(p.columns, big::BM) * tiles_of(p.d, big::BN), PRODUCT_CUS * sizes::PER_CU)),
+                               dim3(big::THREADS), 0, st, q, 8);
+        }
     }
     if (dh)
         hipLaunchKernelGGL(head_dh_join_kernel<T>, dim3((int)((size_t)N * p.d / 1024 < 4096 ? (size_t)N * p.d / 1024 + 1 : 4096)), dim3(256), 0, st,
                            dh_parts, g.parts, p.target, N, p.V, p.d, largest, dh);
-    if (db) hipLaunchKernelGGL(head_db_kernel, dim3(tiles_of(p.V, 256)), dim3(256), 0, st, db_parts, g.db_parts, p.V, largest, db);
+    if (db) hipLaunchKernelGGL(head_db_kernel, dim3(tiles_of(p.V, 256)), dim3(256), 0, st, db_parts, g.db_rows, p.V, largest, db);
 }
 
 int head_check(const char *who, int N, int d, int V, int dtype)
@@ -506,7 +611,7 @@ extern "C" size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dty
 {
     (void)d;
     if (N <= 0 || V <= 0) return 0;
-    return align_up((size_t)N * 4, 256) + (size_t)N * head_row_tiles(N, V, dtype) * 8;
+    return align_up((size_t)N * 4, 256) + (size_t)N * head_row_slots(N, V, dtype) * 8;
 }
 
 extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V, int dtype,
@@ -522,11 +627,11 @@ extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float 
                 ws ? ws_bytes : 0, need);
     HeadArgs p = {};
     p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.N = N, p.d = d, p.V = V;
-    p.n_n = head_row_tiles(N, V, dtype);
+    p.n_n = head_row_slots(N, V, dtype);
     p.at_target = (float *)ws;
     p.tiles = (float2 *)((char *)ws + align_up((size_t)N * 4, 256));
-    if (dtype == MOE_BF16) forward<bf16_t>(p, N, dtype, logprob, lse, (hipStream_t)stream);
-    else forward<float>(p, N, dtype, logprob, lse, (hipStream_t)stream);
+    if (dtype == MOE_BF16) forward<bf16_t>(p, N, logprob, lse, (hipStream_t)stream);
+    else forward<float>(p, N, logprob, lse, (hipStream_t)stream);
     MOE_CHECK_LAUNCH("moe_head_logprobs");
     return MOE_OK;
 }
@@ -560,8 +665,8 @@ extern "C" int moe_head_logprobs_backward(const void *h, const void *w_head, con
                 ws ? ws_bytes : 0, g.bytes);
     HeadArgs p = {};
     p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.lse = lse, p.dlogprob = dlogprob, p.N = N, p.d = d, p.V = V;
-    if (dtype == MOE_BF16) backward<bf16_t>(p, g, (char *)ws, dtype, (bf16_t *)dh, (bf16_t *)dw_head, db_head, st);
-    else backward<float>(p, g, (char *)ws, dtype, (float *)dh, (float *)dw_head, db_head, st);
+    if (dtype == MOE_BF16) backward<bf16_t>(p, g, (char *)ws, (bf16_t *)dh, (bf16_t *)dw_head, db_head, st);
+    else backward<float>(p, g, (char *)ws, (float *)dh, (float *)dw_head, db_head, st);
     MOE_CHECK_LAUNCH("moe_head_logprobs_backward");
     return MOE_OK;
 }

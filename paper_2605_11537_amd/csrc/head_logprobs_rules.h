@@ -7,27 +7,26 @@ namespace moe {
 constexpr int HEAD_MAX_WIDTH = 1 << 20;        // byte offsets inside a tile's rows fit 31 bits
 constexpr int HEAD_MAX_IDS = 1 << 24, HEAD_MAX_ROWS = 1 << 24;
 constexpr size_t HEAD_PIECE_BYTES = 512u << 20;
-constexpr int HEAD_TALL = 256;
+constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 
 enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
-static inline HeadRows head_rows(int N, int dtype)
-{
-    (void)dtype;
-    return N <= 16 ? HEAD_FEW_TILES : N <= 128 ? HEAD_FLAT_TILES : HEAD_TALL_TILES;
-}
+static inline HeadRows head_rows(int N) { return N <= 16 ? HEAD_FEW_TILES : N <= 128 ? HEAD_FLAT_TILES : HEAD_TALL_TILES; }
 static inline int head_tile_rows(int N, int dtype)
 {
-    const HeadRows r = head_rows(N, dtype);
-    return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : HEAD_TALL;
+    const HeadRows r = head_rows(N);
+    return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : 256;
 }
-static inline int head_tile_columns(int N, int dtype) { return head_rows(N, dtype) == HEAD_TALL_TILES && dtype != MOE_F32 ? 256 : 128; }
-static inline int head_row_tiles(int N, int V, int dtype) { return ceil_div(V, head_tile_columns(N, dtype)); }
+static inline int head_tile_columns(int N, int dtype) { return head_rows(N) != HEAD_TALL_TILES ? HEAD_FEW_COLUMNS : dtype == MOE_F32 ? 128 : 256; }
+// forward: slots of maximum and sum that a row has, one for a tile's columns
+static inline int head_row_slots(int N, int V, int dtype) { return ceil_div(V, head_tile_columns(N, dtype)); }
+// backward: rows of a wavefront, for which the bias has a slot of partial sums
+static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dtype) / (head_rows(N) == HEAD_TALL_TILES ? 2 : 1); }
 
 // The gradient's pieces and workspace.
 struct HeadShape {
     int piece;                                 // ids of the vocabulary whose dz is in memory at a time
     int parts;                                 // of a piece's sum for dh
-    int db_parts;                              // rows of partial sums for db
+    int db_rows;                               // rows of partial sums for db
     size_t rows_at, dz_at, dh_at, db_at, bytes;
 };
 static inline HeadShape head_shape(int N, int d, int V, int dtype)
@@ -50,12 +49,12 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
             g.parts = s;
         }
     }
-    g.db_parts = ceil_div(N, head_tile_rows(N, dtype)) * (head_rows(N, dtype) == HEAD_TALL_TILES ? 2 : 1);
+    g.db_rows = ceil_div(N, head_wave_rows(N, dtype));
     g.rows_at = 256;
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
     g.dh_at = g.dz_at + align_up((size_t)N * align_up(g.piece, 8) * z, 256);
     g.db_at = g.dh_at + align_up((size_t)g.parts * N * d * 4, 256);
-    g.bytes = g.db_at + align_up((size_t)g.db_parts * V * 4, 256);
+    g.bytes = g.db_at + align_up((size_t)g.db_rows * V * 4, 256);
     return g;
 }
 

@@ -7,7 +7,8 @@
 // twice:
 //   ALONG_K   row r's 16-byte piece p (of 8) lies at r * 8 + (p ^ (r >> 1 & 7)); a fragment is one 16-byte read a lane
 //   ACROSS_K  bfloat16: the 32-byte piece q of step k lies at q ^ (k & 3 | k >> 1 & 4) of that step's row; a fragment is two reads that transpose 4 k x
-//             16 rows among 16 lanes.  binary32: the 64-byte piece q lies at q ^ (k >> 2 & 3); a fragment is four reads of 4 bytes
+//             16 rows among 16 lanes.  binary32: the 64-byte piece q lies at q ^ (k >> 2 & 3); a fragment is four reads of 4 bytes.  (Rows of less than
+//             256 bytes have fewer pieces to permute.)
 // The order of k inside a matrix instruction is free as long as both operands have the same: lane group g holds k = 8 g .. 8 g + 7 of 32 in bfloat16,
 // and in binary32 instruction j takes k = 4 g + j of 16.
 //
@@ -27,8 +28,6 @@ typedef __attribute__((address_space(3))) char product_lds_t;
 typedef __attribute__((address_space(3))) product_s16x4 product_lds_s16x4;
 
 enum Order { ALONG_K, ACROSS_K };
-
-constexpr int PRODUCT_STAGE_ROW = 128;         // bytes of k a stage holds for every row
 
 template <class T>
 struct Fragment;
@@ -72,26 +71,31 @@ struct Source {
 
 template <class T, Order ORDER, int ROWS, int WAVES>
 struct Operand {
+    static constexpr int ROW = 128;            // bytes of k that a stage holds for every row
     typedef typename Fragment<T>::type fragment;
-    static constexpr int STAGE_K = PRODUCT_STAGE_ROW / (int)sizeof(T);
-    static constexpr int BYTES = ROWS * PRODUCT_STAGE_ROW;
+    static constexpr int STAGE_K = ROW / (int)sizeof(T), STEPS = STAGE_K / Fragment<T>::K;
+    static constexpr int BYTES = ROWS * ROW;
     static constexpr int LOADS = BYTES / 1024;
     static constexpr int MINE = LOADS >= WAVES ? LOADS / WAVES : 1;       // with fewer loads than wavefronts some are made twice, the same bytes
     static_assert(LOADS % WAVES == 0 || WAVES % LOADS == 0, "every wavefront has the same number of loads");
     static constexpr int PIECES = ROWS * (int)sizeof(T) / 16;             // ACROSS_K: 16-byte pieces of a step of k
-    static constexpr int ROW_MASK = sizeof(T) == 2 ? (PIECES / 2 < 8 ? PIECES / 2 - 1 : 7) : 3;      // ... that the XOR permutes
+    static_assert(ORDER == ALONG_K || ROWS >= 32, "what the XOR permutes");
 
     unsigned at[MINE];                         // byte offsets of this lane's pieces from the stage's base
     unsigned k_of[MINE];                       // ALONG_K: the piece's first k in its stage
-    unsigned read_at[2];                       // where this lane's fragment of row block 0 begins in a stage, for each of its two steps
+    unsigned read_at[STEPS];                   // where this lane's fragment of row block 0 begins in a stage, for each of its steps
     unsigned swizzle;                          // ACROSS_K: this lane's XOR
 
     __device__ __forceinline__ static unsigned permute(unsigned k)
     {
-        if (sizeof(T) == 4) return (k >> 2) & 3;
-        if (ROW_MASK == 7) return (k & 3) | ((k >> 1) & 4);
-        return ((k >> 1) & 1) | ((k >> 2) & 2);                            // rows of 128 bytes: neighbouring k alternate between the halves of the banks
+        if (sizeof(T) == 4) return (k >> 2) & (ROWS >= 64 ? 3 : 1);
+        if (ROWS >= 128) return (k & 3) | ((k >> 1) & 4);
+        if (ROWS >= 64) return ((k >> 1) & 1) | ((k >> 2) & 2);            // rows of 128 bytes: neighbouring k alternate between the halves of the banks
+        return (k >> 3) & 1;
     }
+
+    // ALONG_K: the XOR of row r's pieces
+    __device__ __forceinline__ static unsigned turn(unsigned r) { return (r >> 1) & 7; }
 
     // row: this wavefront's first row in the tile
     __device__ __forceinline__ void set_up(unsigned ld_bytes, int row)
@@ -102,7 +106,7 @@ struct Operand {
         for (int i = 0; i < MINE; ++i) {
             const unsigned q = ((w * MINE + i) % LOADS) * 64 + lane;
             if (ORDER == ALONG_K) {
-                const unsigned r = q >> 3, p = (q & 7) ^ ((r >> 1) & 7);
+                const unsigned r = q >> 3, p = (q & 7) ^ turn(r);
                 at[i] = r * ld_bytes + p * 16;
                 k_of[i] = p * (16 / sizeof(T));
             } else if (sizeof(T) == 2) {
@@ -114,19 +118,18 @@ struct Operand {
             }
         }
         if (ORDER == ALONG_K) {
-            const unsigned s = (c >> 1) & 7;
-            read_at[0] = (row + c) * 128 + ((g ^ s) << 4);
-            read_at[1] = read_at[0] ^ 64;
+#pragma unroll
+            for (int ks = 0; ks < STEPS; ++ks) read_at[ks] = (row + c) * ROW + (((4 * ks + g) ^ turn(c)) << 4);
             swizzle = 0;
         } else if (sizeof(T) == 2) {
             const unsigned k = 8 * g + (c >> 2);
             swizzle = permute(k) * 32;
-            read_at[0] = k * ROWS * 2 + (c & 3) * 8 + row * 2;
-            read_at[1] = read_at[0] + 32 * ROWS * 2;
+#pragma unroll
+            for (int ks = 0; ks < STEPS; ++ks) read_at[ks] = (k + 32 * ks) * ROWS * 2 + (c & 3) * 8 + row * 2;
         } else {
-            swizzle = g * 64;
-            read_at[0] = 4 * g * ROWS * 4 + c * 4 + row * 4;
-            read_at[1] = read_at[0] + 16 * ROWS * 4;
+            swizzle = permute(4 * g) * 64;
+#pragma unroll
+            for (int ks = 0; ks < STEPS; ++ks) read_at[ks] = (4 * g + 16 * ks) * ROWS * 4 + c * 4 + row * 4;
         }
     }
 
@@ -134,7 +137,7 @@ struct Operand {
     __device__ __forceinline__ void issue(Source s, int step, int k_total, unsigned ld_bytes, unsigned lds) const
     {
         const unsigned w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const uint64_t skip = ORDER == ALONG_K ? (uint64_t)step * PRODUCT_STAGE_ROW : (uint64_t)step * STAGE_K * ld_bytes;
+        const uint64_t skip = ORDER == ALONG_K ? (uint64_t)step * ROW : (uint64_t)step * STAGE_K * ld_bytes;
         const uint64_t base = s.base + skip;
         const int left = k_total - step * STAGE_K;
         unsigned records;
@@ -158,7 +161,7 @@ struct Operand {
     __device__ __forceinline__ fragment read(product_lds_t *lds, int rb, int ks) const
     {
         if constexpr (ORDER == ALONG_K) {
-            return *reinterpret_cast<__attribute__((address_space(3))) fragment *>(lds + read_at[ks] + rb * 2048);
+            return *reinterpret_cast<__attribute__((address_space(3))) fragment *>(lds + read_at[ks] + rb * 16 * ROW);
         } else if constexpr (sizeof(T) == 2) {
             // row is a multiple of 16 rows, so that the XOR meets the place of the 32-byte piece alone
             const unsigned a = (read_at[ks] + rb * 32) ^ swizzle;
@@ -185,6 +188,36 @@ __device__ __forceinline__ void store4(bf16_t *p, product_f32x4 v)
     *reinterpret_cast<uint2 *>(p) = two;
 }
 
+// One row of a wavefront's sums, blocks 0 .. NB-1, to memory; fits(column): whether the eight (binary32, or one block: four) columns from there on are in D.
+// Two blocks' lane groups exchange their halves, so that a lane has 16 bytes of bfloat16 to write and a row's four lanes 64 in a run.  Every lane of
+// the wavefront has to be here.
+template <int NB, class F>
+__device__ __forceinline__ void write_row(bf16_t *row, const product_f32x4 (&v)[NB], F &&fits)
+{
+    const int g = (threadIdx.x & 63) >> 4;
+    if constexpr (NB % 2 == 0) {
+#pragma unroll
+        for (int nb = 0; nb < NB; nb += 2) {
+            const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb + 1][0], v[nb + 1][1]), false, false);
+            const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][2], v[nb][3]), pack_bf16x2(v[nb + 1][2], v[nb + 1][3]), false, false);
+            const int column = (nb + (g & 1)) * 16 + (g >> 1) * 8;
+            if (fits(column)) *reinterpret_cast<product_u32x4 *>(row + column) = product_u32x4{lo[0], hi[0], lo[1], hi[1]};
+        }
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+            if (fits(nb * 16 + g * 4)) store4(row + nb * 16 + g * 4, v[nb]);
+    }
+}
+template <int NB, class F>
+__device__ __forceinline__ void write_row(float *row, const product_f32x4 (&v)[NB], F &&fits)
+{
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+        if (fits(nb * 16 + g * 4)) store4(row + nb * 16 + g * 4, v[nb]);
+}
+
 // What a workgroup computes next: a tile of D, from one or two runs of k (the second behind the first in the same sum).
 struct Job {
     Source a[2], b[2];                         // of the runs; with two column halves b holds the halves' and there is one run
@@ -203,9 +236,9 @@ __device__ __forceinline__ Source source_across(const void *p, size_t first_byte
 }
 
 // BM x BN of D by WM x WN wavefronts.  HALVES = 2: columns come from two operands of BN / 2 rows each, and a wavefront has the same columns of both.
-// The loop waits for a stage, asks for the one behind it, and multiplies; the first stage of the next tile is asked for in front of a tile's last
-// products, so that it lands while the tile is written.
-template <class T_, Order OA, Order OB, int BM_, int BN_, int WM, int WN, int HALVES_ = 1>
+// A ring of STAGES stages: the loop waits for a stage, asks for the one STAGES - 1 further on, which may be the next tile's, and
+// multiplies, so that a tile's first stages land while the one before is written.
+template <class T_, Order OA, Order OB, int BM_, int BN_, int WM, int WN, int HALVES_ = 1, int STAGES = 2>
 struct Tile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, HALVES = HALVES_, WAVES = WM * WN, THREADS = WAVES * WAVE;
@@ -214,9 +247,23 @@ struct Tile {
     typedef Operand<T, OA, BM, WAVES> A;
     typedef Operand<T, OB, HALF_N, WAVES> B;
     static constexpr int STAGE_K = A::STAGE_K;
-    static constexpr int STAGE = A::BYTES + HALVES * B::BYTES, LDS = 2 * STAGE;
+    static constexpr int STAGE = A::BYTES + HALVES * B::BYTES, LDS = STAGES * STAGE;
+    static constexpr int LOADS = A::MINE + HALVES * B::MINE;                                 // of a wavefront for a stage
 
     typedef product_f32x4 Sums[HALVES][MB][NB];          // register i of [h][mb][nb]: row of_row(mb), column of_column(nb) + i of half h
+
+    // binary32: sums of eight stages (256 k) are added up by themselves.  One sum over 5632 k was off by 1.1e-6 of the result, a library's by 6e-7.
+    static constexpr int APART = sizeof(T) == 4 ? 8 : 0;
+    template <class F>
+    __device__ __forceinline__ static void each(Sums &x, F &&f, Sums &y)
+    {
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) f(x[h][mb][nb], y[h][mb][nb]);
+    }
 
     A a;
     B b;
@@ -233,13 +280,15 @@ struct Tile {
         b.set_up(ldb, wn * WAVE_N);
     }
     __device__ __forceinline__ int of_row(int mb) const { return wm * WAVE_M + mb * 16 + (threadIdx.x & 15); }
+    __device__ __forceinline__ int first_column() const { return wn * WAVE_N; }
     __device__ __forceinline__ int of_column(int nb) const { return wn * WAVE_N + nb * 16 + ((threadIdx.x & 63) >> 4) * 4; }
 
-    __device__ __forceinline__ static int steps_of(const Job &j) { return (j.k + STAGE_K - 1) / STAGE_K; }
+    __device__ __forceinline__ static int steps_of(const Job &j) { return (j.k + STAGE_K - 1) / STAGE_K * j.runs; }
 
-    __device__ __forceinline__ void issue(const Job &j, int step, int per_run, int buffer) const
+    __device__ __forceinline__ void issue(const Job &j, int step, int buffer) const
     {
         const unsigned at = (unsigned)(uintptr_t)lds + buffer * STAGE;
+        const int per_run = (j.k + STAGE_K - 1) / STAGE_K;
         const bool second = j.runs == 2 && step >= per_run;
         const int s = second ? step - per_run : step;
         a.issue(second ? j.a[1] : j.a[0], s, j.k, lda, at);
@@ -253,7 +302,7 @@ struct Tile {
     {
         product_lds_t *at = lds + buffer * STAGE;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < A::STEPS; ++ks) {
             typename A::fragment fa[MB];
             typename B::fragment fb[HALVES][NB];
 #pragma unroll
@@ -271,38 +320,65 @@ struct Tile {
         }
     }
 
+    // this wavefront's loads of the oldest of `pending` stages have landed (what was issued behind them only makes the wait longer) and its reads
+    // of the stage before are done; behind the barrier everyone's
+    __device__ __forceinline__ static void wait(int pending)
+    {
+#define MOE_PRODUCT_WAIT(N) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory")
+        if (STAGES > 4 && pending > 3) MOE_PRODUCT_WAIT(3 * LOADS);
+        else if (STAGES > 3 && pending > 2) MOE_PRODUCT_WAIT(2 * LOADS);
+        else if (STAGES > 2 && pending > 1) MOE_PRODUCT_WAIT(LOADS);
+        else MOE_PRODUCT_WAIT(0);
+#undef MOE_PRODUCT_WAIT
+    }
+
     // next(job) -> whether there is one; finish(job, sums) writes a tile.  Both are reached by the whole workgroup.
     template <class Next, class Finish>
     __device__ __forceinline__ void run(Next &&next, Finish &&finish) const
     {
         Job job, then;
-        bool more = next(job);
-        int buffer = 0;
-        if (more && job.k > 0) issue(job, 0, steps_of(job), 0);
-        while (more) {
-            const int per_run = steps_of(job), steps = per_run * job.runs;
-            Sums sums;
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) sums[h][mb][nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
-            more = next(then);
+        if (!next(job)) return;
+        bool more = next(then);
+        int asked = 0, asked_then = 0;         // stages of job and then that were asked for
+        int pending = 0, to = 0, from = 0;     // asked for and not multiplied yet; the ring's buffers for the next of either
+        auto ask = [&](int most) {
+            while (pending < most) {
+                if (asked < steps_of(job)) issue(job, asked++, to);
+                else if (more && asked_then < steps_of(then)) issue(then, asked_then++, to);
+                else break;
+                ++pending;
+                to = to + 1 == STAGES ? 0 : to + 1;
+            }
+        };
+        ask(STAGES - 1);
+        while (true) {
+            const int steps = steps_of(job);
+            Sums sums, part;                   // part: binary32's last stages, by themselves
+            each(sums, [](product_f32x4 &v, product_f32x4 &) { v = product_f32x4{0.f, 0.f, 0.f, 0.f}; }, sums);
+            if (APART) each(part, [](product_f32x4 &v, product_f32x4 &) { v = product_f32x4{0.f, 0.f, 0.f, 0.f}; }, part);
             for (int s = 0; s < steps; ++s) {
-                // this wavefront's loads of stage s have landed and its reads of the stage before are done; behind the barrier everyone's
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                if (s + 1 < steps) issue(job, s + 1, per_run, buffer ^ 1);
-                else if (more && then.k > 0) issue(then, 0, steps_of(then), buffer ^ 1);
-                multiply(sums, buffer);
-                buffer ^= 1;
+                wait(pending);
+                ask(STAGES);                   // the buffer of the stage before this one is free
+                multiply(APART ? part : sums, from);
+                if (APART && (s % APART == APART - 1 || s + 1 == steps))
+                    each(sums, [](product_f32x4 &v, product_f32x4 &w) {
+                        v += w;
+                        w = product_f32x4{0.f, 0.f, 0.f, 0.f};
+                    }, part);
+                from = from + 1 == STAGES ? 0 : from + 1;
+                --pending;
             }
             finish(job, sums);
-            if (steps == 0 && more && then.k > 0) {
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // nobody reads that buffer any more
-                issue(then, 0, steps_of(then), buffer);
-            }
+            if (!more) break;
             job = then;
+            asked = asked_then;
+            asked_then = 0;
+            more = next(then);
+            // stages behind a tile without any: its buffers are free, everyone has passed the barrier of the last multiplied stage
+            if (pending == 0) {
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                ask(STAGES - 1);
+            }
         }
     }
 };
@@ -392,10 +468,55 @@ struct Units {
         return true;
     }
 };
+
+// A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half, a quarter or an eighth of that
+// size, if one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.
+// run(tile type, first unit, past the last)
+template <class SIZES, class Run>
+__device__ __forceinline__ void in_rounds(int units, Run &&run)
+{
+    const int grid = gridDim.x, rest = units % grid, whole = 2 * rest > grid ? units : units - rest;
+    if (whole > 0) run(typename SIZES::Whole(), 0, whole);
+    if (whole == units) return;
+    if (whole > 0) __syncthreads();            // the buffers change their sizes
+    if (4 * rest > grid) run(typename SIZES::Half(), whole, units);
+    else if (8 * rest > grid) run(typename SIZES::Quarter(), whole, units);
+    else run(typename SIZES::Eighth(), whole, units);
+}
+template <class TILE>
+struct Sized {
+    typedef TILE Type;
+};
+template <class T, Order A, Order B, int HALVES = 1>
+struct Sizes;
+template <Order A, Order B, int HALVES>
+struct Sizes<bf16_t, A, B, HALVES> {
+    typedef Sized<Tile<bf16_t, A, B, 256, 256, 2, 4, HALVES>> Whole;
+    typedef Sized<Tile<bf16_t, A, B, 128, 256, 2, 4, HALVES, 3>> Half;
+    typedef Sized<Tile<bf16_t, A, B, 128, 128, 2, 4, HALVES, 4>> Quarter;
+    typedef Sized<Tile<bf16_t, A, B, 128, 64, 4, 2, HALVES, 5>> Eighth;
+    static constexpr int PER_CU = 1;
+};
+template <Order A, Order B, int HALVES>
+struct Sizes<float, A, B, HALVES> {
+    typedef Sized<Tile<float, A, B, 128, 128, 2, 2, HALVES>> Whole;
+    typedef Sized<Tile<float, A, B, 64, 128, 2, 2, HALVES, 3>> Half;
+    typedef Sized<Tile<float, A, B, 64, 64, 2, 2, HALVES, 4>> Quarter;
+    typedef Sized<Tile<float, A, B, 32, 64, 2, 2, HALVES, 5>> Eighth;
+    static constexpr int PER_CU = 2;
+};
+template <class SIZES>
+struct Whole {
+    typedef typename SIZES::Whole::Type Tile;
+    static constexpr int THREADS = Tile::THREADS, WAVES = Tile::WAVES, LDS_HALF = SIZES::Half::Type::LDS, LDS = LDS_HALF > Tile::LDS ? LDS_HALF : Tile::LDS;
+};
+
 __host__ __device__ constexpr int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
+constexpr int PRODUCT_CUS = 256, PRODUCT_PARTS = 8;
+// workgroups for at most so many units of the largest size
 static inline int product_grid(long long units, int resident)
 {
-    const long long n = units < resident ? units : resident;
+    const long long n = units * PRODUCT_PARTS < resident ? units * PRODUCT_PARTS : resident;
     return (int)((n + 7) / 8 * 8);
 }
 

@@ -68,7 +68,6 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
 
 // Sixteen columns' g, then their u: what the four lanes of a row write and read lies in runs of 64 bytes.
 __host__ __device__ constexpr int states_width(int F) { return (F + 15) / 16 * 32; }
-__device__ __forceinline__ float *states_at(float *gu, size_t row, int F, int column) { return gu + row * states_width(F) + (column >> 4) * 32 + (column & 15); }
 
 struct GatedArgs {
     const void *x, *w_gate, *w_up, *w_down, *dy;
@@ -94,7 +93,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const bool with_states = p.gu != nullptr;
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n, lo, hi;
             do {
@@ -134,20 +133,45 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
-            const int left = j.columns - tile.first_column();          // columns of D from this wavefront's first on
-            const int n0 = j.n0 + tile.first_column(), g4 = ((threadIdx.x & 63) >> 4) * 4;
-            if constexpr (STEP == GATED_DHIDDEN) {
-                // the states of a row of blocks are asked for a row ahead
-                product_f32x4 gate[2][TILE::NB], up[2][TILE::NB];
-                auto ask = [&](int mb) {
-                    const int row = tile.of_row(mb);
-                    const float *gu = states_at(p.gu, (size_t)(j.m0 + (row < j.rows ? row : 0)), p.F, n0 + g4);
+            if constexpr (STEP == GATED_HIDDEN) {
+                const Writer<TILE, T> h(tile, (T *)p.h + (size_t)j.m0 * p.F + j.n0, f_bytes, j.rows, j.columns);
+                // rows of g and u in turn, 16 columns each
+                const unsigned gu_bytes = states_width(p.F) * 4;
+                const int g4 = ((threadIdx.x & 63) >> 4) * 4, first = tile.first_column();
+                const auto gu = __builtin_amdgcn_make_buffer_rsrc(p.gu + (size_t)j.m0 * states_width(p.F) + (j.n0 + first) * 2, 0, 0x7fffffff, 0x27000);
+                const unsigned at = (unsigned)tile.of_row(0) * gu_bytes + g4 * 4;
+#pragma unroll
+                for (int mb = 0; mb < TILE::MB; ++mb) {
+                    product_f32x4 v[TILE::NB];
+                    const bool there = tile.of_row(mb) < j.rows;
 #pragma unroll
                     for (int nb = 0; nb < TILE::NB; ++nb) {
-                        const bool there = nb * 16 + g4 < left;
-                        const product_f32x4 *at = reinterpret_cast<const product_f32x4 *>(there ? gu + nb * 32 : p.gu);
-                        gate[mb & 1][nb] = at[0];
-                        up[mb & 1][nb] = at[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[nb][i] = act_of<Z == 4>(p.activation, sums[0][mb][nb][i]) * sums[1][mb][nb][i];
+                        if (with_states) {                             // uniform
+                            const unsigned where = there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u;
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[0][mb][nb]), gu, where, mb * 16 * gu_bytes, 0);
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[1][mb][nb]), gu, where + 64, mb * 16 * gu_bytes, 0);
+                        }
+                    }
+                    h.row(mb, v);
+                }
+            } else if constexpr (STEP == GATED_DHIDDEN) {
+                T *const to = (T *)p.dgu + (size_t)j.m0 * 2 * p.F + j.n0;
+                const Writer<TILE, T> dg(tile, to, 2 * f_bytes, j.rows, j.columns), du(tile, to + p.F, 2 * f_bytes, j.rows, j.columns);
+                const unsigned gu_bytes = states_width(p.F) * 4;
+                const int g4 = ((threadIdx.x & 63) >> 4) * 4, first = tile.first_column();
+                const auto gu = __builtin_amdgcn_make_buffer_rsrc(p.gu + (size_t)j.m0 * states_width(p.F) + (j.n0 + first) * 2, 0, 0x7fffffff, 0x27000);
+                const unsigned at = (unsigned)tile.of_row(0) * gu_bytes + g4 * 4;
+                // the states of a row of blocks are asked for a row ahead
+                product_u32x4 gate[2][TILE::NB], up[2][TILE::NB];
+                auto ask = [&](int mb) {
+                    const bool there = tile.of_row(mb) < j.rows;
+#pragma unroll
+                    for (int nb = 0; nb < TILE::NB; ++nb) {
+                        const unsigned where = there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u;
+                        gate[mb & 1][nb] = __builtin_amdgcn_raw_buffer_load_b128(gu, where, mb * 16 * gu_bytes, 0);
+                        up[mb & 1][nb] = __builtin_amdgcn_raw_buffer_load_b128(gu, where + 64, mb * 16 * gu_bytes, 0);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -155,43 +179,23 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
 #pragma unroll
                 for (int mb = 0; mb < TILE::MB; ++mb) {
                     if (mb + 1 < TILE::MB) ask(mb + 1);
-                    product_f32x4 dg[TILE::NB], du[TILE::NB];
+                    product_f32x4 vg[TILE::NB], vu[TILE::NB];
 #pragma unroll
                     for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             float slope;
                             const float v = sums[0][mb][nb][i];
-                            du[nb][i] = v * act_of<Z == 4>(p.activation, gate[mb & 1][nb][i], slope);
-                            dg[nb][i] = v * up[mb & 1][nb][i] * slope;
+                            vu[nb][i] = v * act_of<Z == 4>(p.activation, __uint_as_float(gate[mb & 1][nb][i]), slope);
+                            vg[nb][i] = v * __uint_as_float(up[mb & 1][nb][i]) * slope;
                         }
-                    const int row = tile.of_row(mb);
-                    T *to = (T *)p.dgu + (size_t)(j.m0 + row) * 2 * p.F + n0;
-                    auto fits = [&](int column) { return row < j.rows && column < left; };
-                    write_row(to, dg, fits);
-                    write_row(to + p.F, du, fits);
+                    dg.row(mb, vg);
+                    du.row(mb, vu);
                 }
-                return;
-            }
+            } else {
+                const Writer<TILE, T> to(tile, (T *)(STEP == GATED_DOWN ? p.y : p.dx) + (size_t)j.m0 * p.d + j.n0, d_bytes, j.rows, j.columns);
 #pragma unroll
-            for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                const size_t r = (size_t)(j.m0 + row);
-                auto fits = [&](int column) { return row < j.rows && column < left; };
-                if constexpr (STEP == GATED_HIDDEN) {
-                    product_f32x4 h[TILE::NB];
-#pragma unroll
-                    for (int nb = 0; nb < TILE::NB; ++nb) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) h[nb][i] = act_of<Z == 4>(p.activation, sums[0][mb][nb][i]) * sums[1][mb][nb][i];
-                        if (with_states && fits(nb * 16 + g4)) {
-                            float *gu = states_at(p.gu, r, p.F, n0 + nb * 16 + g4);
-                            store4(gu, sums[0][mb][nb]);
-                            store4(gu + 16, sums[1][mb][nb]);
-                        }
-                    }
-                    write_row((T *)p.h + r * p.F + n0, h, fits);
-                } else write_row((T *)(STEP == GATED_DOWN ? p.y : p.dx) + r * p.d + n0, sums[0][mb], fits);
+                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
             }
         });
 }
@@ -234,7 +238,7 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
     const unsigned lda = M * Z, ldb = N * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n, e;
             do {
@@ -257,18 +261,17 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
         },
         [&](const Job &j, typename TILE::Sums &sums) {
             const size_t w = (size_t)j.group * p.d * p.F;
-            const int left = j.columns - tile.first_column(), n = j.n0 + tile.first_column();
+            const unsigned ld = (DOWN ? p.d : p.F) * Z;
+            const size_t at = w + (size_t)j.m0 * (DOWN ? p.d : p.F) + j.n0;
+            if (DOWN || j.n0 < p.F) {          // two matrices' columns side by side
+                const Writer<TILE, T> to(tile, (T *)(DOWN ? p.dw_down : p.dw_gate) + at, ld, j.rows, DOWN || j.columns < p.F - j.n0 ? j.columns : p.F - j.n0);
 #pragma unroll
-            for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                const size_t at = w + (size_t)(j.m0 + row) * (DOWN ? p.d : p.F) + n;
-                if (DOWN) write_row((T *)p.dw_down + at, sums[0][mb], [&](int c) { return row < j.rows && c < left; });
-                else {
-                    // columns of the two matrices side by side
-                    if (n < p.F) write_row((T *)p.dw_gate + at, sums[0][mb], [&](int c) { return row < j.rows && c < left && n + c < p.F; });
-                    if (n + TILE::WAVE_N > p.F)
-                        write_row((T *)p.dw_up + at - p.F, sums[0][mb], [&](int c) { return row < j.rows && c < left && n + c >= p.F; });
-                }
+                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
+            }
+            if (!DOWN && j.n0 + j.columns > p.F) {
+                const Writer<TILE, T> to(tile, (T *)p.dw_up + at - p.F, ld, j.rows, j.columns, p.F - j.n0);
+#pragma unroll
+                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
             }
         });
 }

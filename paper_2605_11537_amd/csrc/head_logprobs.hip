@@ -82,7 +82,7 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
     const unsigned d_bytes = p.d * sizeof(T);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<0>(
         [&](Job &j) {
             int u, m, n;
             do {
@@ -206,7 +206,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     const float largest = *p.largest;
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n;
             do {
@@ -226,6 +226,8 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
         },
         [&](const Job &j, typename TILE::Sums &z) {
             add_bias(tile, j, p.b, p.V, z);
+            // a row of dz ends with zeros up to a whole piece of 16 bytes
+            const Writer<TILE, T> to(tile, (T *)p.dz + (size_t)j.m0 * p.ld + (j.n0 - p.v0), p.ld * sizeof(T), j.rows, p.ld - (j.n0 - p.v0));
             product_f32x4 down[TILE::NB];      // sums over this lane's rows
 #pragma unroll
             for (int nb = 0; nb < TILE::NB; ++nb) down[nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -251,9 +253,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
                 }
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb) down[nb] += dz[nb];
-                // a row of dz ends with zeros up to a whole piece of 16 bytes
-                const int at = j.n0 - p.v0 + tile.first_column();
-                write_row((T *)p.dz + (size_t)(j.m0 + row) * p.ld + at, dz, [&](int c) { return there && at + c < p.ld; });
+                to.row(mb, dz);
             }
             if (p.db) {
 #pragma unroll
@@ -310,7 +310,7 @@ __device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n
     const unsigned lda = p.ld * Z, ldb = p.d * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<TILE::MB * Writer<TILE, float>::STORES>(
         [&](Job &j) {
             int u, m, n;
             do {
@@ -333,19 +333,18 @@ __device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
+            float *const first = p.dh + ((size_t)j.group * p.N + j.m0) * p.d + j.n0;
+            const Writer<TILE, float> to(tile, first, p.d * 4, j.rows, j.columns);
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                if (row >= j.rows) continue;
+                if (p.add) {                   // uniform
+                    const int row = tile.of_row(mb);
 #pragma unroll
-                for (int nb = 0; nb < TILE::NB; ++nb) {
-                    const int column = tile.of_column(nb);
-                    if (column >= j.columns) continue;
-                    float *to = p.dh + ((size_t)j.group * p.N + j.m0 + row) * p.d + j.n0 + column;
-                    product_f32x4 v = sums[0][mb][nb];
-                    if (p.add) v += *reinterpret_cast<const product_f32x4 *>(to);
-                    store4(to, v);
+                    for (int nb = 0; nb < TILE::NB; ++nb)
+                        if (row < j.rows && tile.of_column(nb) < j.columns)
+                            sums[0][mb][nb] += *reinterpret_cast<const product_f32x4 *>(first + (size_t)row * p.d + tile.of_column(nb));
                 }
+                to.row(mb, sums[0][mb]);
             }
         });
 }
@@ -377,7 +376,7 @@ __device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const float largest = *p.largest;
     Units units((past - first) * PARTS);
-    tile.run(
+    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n;
             do {
@@ -395,14 +394,12 @@ __device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
-            const int left = j.columns - tile.first_column();
+            const Writer<TILE, T> to(tile, (T *)p.dw + (size_t)(p.v0 + j.m0) * p.d + j.n0, p.d * Z, j.rows, j.columns);
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb) sums[0][mb][nb] *= largest;
-                write_row((T *)p.dw + (size_t)(p.v0 + j.m0 + row) * p.d + j.n0 + tile.first_column(), sums[0][mb],
-                          [&](int c) { return row < j.rows && c < left; });
+                to.row(mb, sums[0][mb]);
             }
         });
 }

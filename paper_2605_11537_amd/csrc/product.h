@@ -20,6 +20,7 @@
 namespace moe {
 
 typedef unsigned product_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned product_u32x2 __attribute__((ext_vector_type(2)));
 typedef float product_f32x4 __attribute__((ext_vector_type(4)));
 typedef short product_s16x4 __attribute__((ext_vector_type(4)));
 typedef short product_s16x8 __attribute__((ext_vector_type(8)));
@@ -59,7 +60,7 @@ __device__ __forceinline__ void product_mma(product_f32x4 &d, product_f32x4 b, p
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(product_u32x4 buffer, unsigned at, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "m0");
 }
 #pragma clang diagnostic pop
 
@@ -133,28 +134,35 @@ struct Operand {
         }
     }
 
-    // stage `step` (of STAGE_K k each) of k_total
-    __device__ __forceinline__ void issue(Source s, int step, int k_total, unsigned ld_bytes, unsigned lds) const
+    // the buffer of a run's first stage, of k in all, and of the stage behind it with `left` k from there on
+    __device__ __forceinline__ static unsigned records_of(Source s, int left, unsigned ld_bytes)
+    {
+        // ALONG_K every k of a row lies within the row.  ACROSS_K the columns in front of the tile are not in the buffer: the last row ends with the matrix
+        return ORDER == ALONG_K ? s.records : ((unsigned)(left < STAGE_K ? left : STAGE_K) - 1) * ld_bytes + s.records;
+    }
+    __device__ __forceinline__ static product_u32x4 first_buffer(Source s, int k, unsigned ld_bytes)
+    {
+        product_u32x4 v = {(unsigned)s.base, (unsigned)(s.base >> 32), records_of(s, k, ld_bytes), 0x27000};
+#pragma unroll
+        for (int i = 0; i < 3; ++i) v[i] = __builtin_amdgcn_readfirstlane(v[i]);      // scalar, whatever the compiler has made of the job
+        return v;
+    }
+    __device__ __forceinline__ static void next_buffer(product_u32x4 &v, int left, unsigned ld_bytes)
+    {
+        const unsigned by = ORDER == ALONG_K ? ROW : STAGE_K * ld_bytes;
+        const uint64_t base = (((uint64_t)v[1] << 32) | v[0]) + by;
+        v[0] = (unsigned)base;
+        v[1] = (unsigned)(base >> 32);
+        if (ORDER == ALONG_K) v[2] -= ROW;
+        else if (left < STAGE_K) v[2] -= (STAGE_K - left) * ld_bytes;                 // the run's last
+    }
+    // this wavefront's load i of a stage; left: k from the stage's first on
+    __device__ __forceinline__ void load(int i, product_u32x4 buffer, int left, unsigned lds) const
     {
         const unsigned w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        const uint64_t skip = ORDER == ALONG_K ? (uint64_t)step * ROW : (uint64_t)step * STAGE_K * ld_bytes;
-        const uint64_t base = s.base + skip;
-        const int left = k_total - step * STAGE_K;
-        unsigned records;
-        if (ORDER == ALONG_K) records = s.records - (unsigned)skip;         // every k of a row lies within its records
-        else {
-            // the columns in front of the tile are not in the buffer: the last row ends with the matrix
-            const uint64_t rows = (uint64_t)(left < STAGE_K ? left : STAGE_K) * ld_bytes;
-            const uint64_t end = s.records;                                  // ACROSS_K: bytes of a row from the tile's first on
-            records = (unsigned)(rows - ld_bytes + end);
-        }
-        const product_u32x4 buffer = {(unsigned)base, (unsigned)(base >> 32), records, 0x27000};
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-            unsigned a = at[i];
-            if (ORDER == ALONG_K) a = (int)k_of[i] < left ? a : 0x80000000u;
-            load_to_lds(buffer, a, lds + ((w * MINE + i) % LOADS) * 1024);
-        }
+        unsigned a = at[i];
+        if (ORDER == ALONG_K) a = (int)k_of[i] < left ? a : 0x80000000u;
+        load_to_lds(buffer, a, lds + ((w * MINE + i) % LOADS) * 1024);
     }
 
     // fragment of rows 16 rb .. 16 rb + 15 of this wavefront's, step ks of the stage at lds
@@ -186,36 +194,6 @@ __device__ __forceinline__ void store4(bf16_t *p, product_f32x4 v)
     two.x = pack_bf16x2(v[0], v[1]);
     two.y = pack_bf16x2(v[2], v[3]);
     *reinterpret_cast<uint2 *>(p) = two;
-}
-
-// One row of a wavefront's sums, blocks 0 .. NB-1, to memory; fits(column): whether the eight (binary32, or one block: four) columns from there on are in D.
-// Two blocks' lane groups exchange their halves, so that a lane has 16 bytes of bfloat16 to write and a row's four lanes 64 in a run.  Every lane of
-// the wavefront has to be here.
-template <int NB, class F>
-__device__ __forceinline__ void write_row(bf16_t *row, const product_f32x4 (&v)[NB], F &&fits)
-{
-    const int g = (threadIdx.x & 63) >> 4;
-    if constexpr (NB % 2 == 0) {
-#pragma unroll
-        for (int nb = 0; nb < NB; nb += 2) {
-            const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb + 1][0], v[nb + 1][1]), false, false);
-            const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][2], v[nb][3]), pack_bf16x2(v[nb + 1][2], v[nb + 1][3]), false, false);
-            const int column = (nb + (g & 1)) * 16 + (g >> 1) * 8;
-            if (fits(column)) *reinterpret_cast<product_u32x4 *>(row + column) = product_u32x4{lo[0], hi[0], lo[1], hi[1]};
-        }
-    } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-            if (fits(nb * 16 + g * 4)) store4(row + nb * 16 + g * 4, v[nb]);
-    }
-}
-template <int NB, class F>
-__device__ __forceinline__ void write_row(float *row, const product_f32x4 (&v)[NB], F &&fits)
-{
-    const int g = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-        if (fits(nb * 16 + g * 4)) store4(row + nb * 16 + g * 4, v[nb]);
 }
 
 // What a workgroup computes next: a tile of D, from one or two runs of k (the second behind the first in the same sum).
@@ -285,71 +263,127 @@ struct Tile {
 
     __device__ __forceinline__ static int steps_of(const Job &j) { return (j.k + STAGE_K - 1) / STAGE_K * j.runs; }
 
-    __device__ __forceinline__ void issue(const Job &j, int step, int buffer) const
+    // the stage that is asked for next or was last: its operands' buffers, k from its first on, the ring's buffer it goes to
+    struct Cursor {
+        product_u32x4 a, b[HALVES];
+        int left, runs;                        // runs behind this one
+        unsigned lds;
+    };
+    __device__ __forceinline__ void begin(Cursor &c, const Job &j, bool second) const
     {
-        const unsigned at = (unsigned)(uintptr_t)lds + buffer * STAGE;
-        const int per_run = (j.k + STAGE_K - 1) / STAGE_K;
-        const bool second = j.runs == 2 && step >= per_run;
-        const int s = second ? step - per_run : step;
-        a.issue(second ? j.a[1] : j.a[0], s, j.k, lda, at);
-        if (HALVES == 2) {
-            b.issue(j.b[0], s, j.k, ldb, at + A::BYTES);
-            b.issue(j.b[1], s, j.k, ldb, at + A::BYTES + B::BYTES);
-        } else b.issue(second ? j.b[1] : j.b[0], s, j.k, ldb, at + A::BYTES);
+        c.left = __builtin_amdgcn_readfirstlane(j.k);
+        c.runs = second ? 0 : __builtin_amdgcn_readfirstlane(j.runs) - 1;
+        Source sa = j.a[0], sb = j.b[0];
+        if (second) sa = j.a[1], sb = j.b[1];
+        c.a = A::first_buffer(sa, c.left, lda);
+        c.b[0] = B::first_buffer(sb, c.left, ldb);
+        if (HALVES == 2) c.b[HALVES - 1] = B::first_buffer(j.b[1], c.left, ldb);
+    }
+    // whether there is a stage behind this one
+    __device__ __forceinline__ bool advance(Cursor &c, const Job &j) const
+    {
+        c.left -= STAGE_K;
+        if (c.left > 0) {
+            A::next_buffer(c.a, c.left, lda);
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) B::next_buffer(c.b[h], c.left, ldb);
+            return true;
+        }
+        if (c.runs <= 0) return false;
+        begin(c, j, true);
+        return true;
+    }
+    // load i of the stage (there = false: the buffers have no records, and zeros go to LDS that nobody reads)
+    __device__ __forceinline__ void load(const Cursor &c, int i) const
+    {
+        if (i < A::MINE) a.load(i, c.a, c.left, c.lds);
+        else if (i < A::MINE + B::MINE) b.load(i - A::MINE, c.b[0], c.left, c.lds + A::BYTES);
+        else b.load(i - A::MINE - B::MINE, c.b[HALVES - 1], c.left, c.lds + A::BYTES + B::BYTES);
     }
 
-    __device__ __forceinline__ void multiply(Sums &sums, int buffer) const
+    // Groups of a fragment of A with all of B's: the reads of a group are two groups ahead of its products, the next step's fragments of B spread
+    // over this step's groups, the loads of the stage asked for over the whole.
+    __device__ __forceinline__ void multiply(Sums &sums, int buffer, const Cursor &st) const
     {
         product_lds_t *at = lds + buffer * STAGE;
+        constexpr int S = A::STEPS, Q = S * MB, NBH = HALVES * NB, AHEAD = MB < 2 ? 1 : 2;
+        typename A::fragment fa[S][MB];
+        typename B::fragment fb[S][HALVES][NB];
 #pragma unroll
-        for (int ks = 0; ks < A::STEPS; ++ks) {
-            typename A::fragment fa[MB];
-            typename B::fragment fb[HALVES][NB];
+        for (int i = 0; i < NBH; ++i) fb[0][i / NB][i % NB] = b.read(at + A::BYTES + i / NB * B::BYTES, i % NB, 0);
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h)
+        for (int q = 0; q < AHEAD; ++q) fa[q / MB][q % MB] = a.read(at, q % MB, q / MB);
+        int asked = 0, read = 0;
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb) fb[h][nb] = b.read(at + A::BYTES + h * B::BYTES, nb, ks);
+        for (int q = 0; q < Q; ++q) {
+            const int ks = q / MB, mb = q % MB;
+            if (q + AHEAD < Q) fa[(q + AHEAD) / MB][(q + AHEAD) % MB] = a.read(at, (q + AHEAD) % MB, (q + AHEAD) / MB);
+            if (mb == 0) read = 0;
+            if (ks + 1 < S) {
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) fa[mb] = a.read(at, mb, ks);
+                for (; read < NBH * (mb + 1) / MB; ++read) fb[ks + 1][read / NB][read % NB] = b.read(at + A::BYTES + read / NB * B::BYTES, read % NB, ks + 1);
+            }
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
+            for (; asked < 4 * LOADS * (q + 1) / Q && asked < LOADS; ++asked) load(st, asked);
 #pragma unroll
-                for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) product_mma(sums[h][mb][nb], fb[h][nb], fa[mb]);
+            for (int i = 0; i < NBH; ++i) product_mma(sums[i / NB][mb][i % NB], fb[ks][i / NB][i % NB], fa[ks][mb]);
+            if (q + 1 < Q) __builtin_amdgcn_sched_barrier(0);
         }
     }
 
     // this wavefront's loads of the oldest of `pending` stages have landed (what was issued behind them only makes the wait longer) and its reads
     // of the stage before are done; behind the barrier everyone's
-    __device__ __forceinline__ static void wait(int pending)
+    // behind: a tile's STORES or more are younger than all of those loads
+    template <int STORES>
+    __device__ __forceinline__ static void wait(int pending, bool behind)
     {
 #define MOE_PRODUCT_WAIT(N) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory")
         if (STAGES > 4 && pending > 3) MOE_PRODUCT_WAIT(3 * LOADS);
         else if (STAGES > 3 && pending > 2) MOE_PRODUCT_WAIT(2 * LOADS);
         else if (STAGES > 2 && pending > 1) MOE_PRODUCT_WAIT(LOADS);
+        else if (STORES > 0 && behind) MOE_PRODUCT_WAIT(STORES < 63 ? STORES : 63);
         else MOE_PRODUCT_WAIT(0);
 #undef MOE_PRODUCT_WAIT
     }
 
     // next(job) -> whether there is one; finish(job, sums) writes a tile.  Both are reached by the whole workgroup.
-    template <class Next, class Finish>
+    // STORES: the fewest vector memory operations that finish issues.  Reads and writes complete in the order of their issue, so the first stage behind a
+    // tile, which was asked for before its stores, has landed while they are on their way.
+    template <int STORES, class Next, class Finish>
     __device__ __forceinline__ void run(Next &&next, Finish &&finish) const
     {
         Job job, then;
         if (!next(job)) return;
         bool more = next(then);
-        int asked = 0, asked_then = 0;         // stages of job and then that were asked for
-        int pending = 0, to = 0, from = 0;     // asked for and not multiplied yet; the ring's buffers for the next of either
+        int pending = 0, to = 0, from = 0;     // stages asked for and not multiplied yet; the ring's buffers for the next of either
+        Cursor at;
+        bool in_then = false, fresh = true;    // the cursor is in `then`; it stands on a stage that was not asked for yet
+        begin(at, job, false);
+        // moves the cursor to the next stage to ask for, if there is one
+        auto following = [&] {
+            if (!fresh && !advance(at, in_then ? then : job)) {
+                at.left = 0;
+                at.runs = 0;
+            }
+            fresh = false;
+            if (at.left <= 0) {
+                if (in_then || !more) return false;
+                begin(at, then, false);
+                in_then = true;
+                if (at.left <= 0) return false;
+            }
+            at.lds = (unsigned)(uintptr_t)lds + to * STAGE;
+            ++pending;
+            to = to + 1 == STAGES ? 0 : to + 1;
+            return true;
+        };
         auto ask = [&](int most) {
-            while (pending < most) {
-                if (asked < steps_of(job)) issue(job, asked++, to);
-                else if (more && asked_then < steps_of(then)) issue(then, asked_then++, to);
-                else break;
-                ++pending;
-                to = to + 1 == STAGES ? 0 : to + 1;
+            while (pending < most && following()) {
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) load(at, i);
             }
         };
+        bool stored = false;
         ask(STAGES - 1);
         while (true) {
             const int steps = steps_of(job);
@@ -357,9 +391,15 @@ struct Tile {
             each(sums, [](product_f32x4 &v, product_f32x4 &) { v = product_f32x4{0.f, 0.f, 0.f, 0.f}; }, sums);
             if (APART) each(part, [](product_f32x4 &v, product_f32x4 &) { v = product_f32x4{0.f, 0.f, 0.f, 0.f}; }, part);
             for (int s = 0; s < steps; ++s) {
-                wait(pending);
-                ask(STAGES);                   // the buffer of the stage before this one is free
-                multiply(APART ? part : sums, from);
+                wait<STORES>(pending, stored && s == 0);
+                ask(STAGES - 1);
+                if (!following()) {            // the buffer of the stage before this one is free
+                    at.lds = (unsigned)(uintptr_t)lds + to * STAGE;
+                    at.a[2] = 0;
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) at.b[h][2] = 0;
+                }
+                multiply(APART ? part : sums, from, at);
                 if (APART && (s % APART == APART - 1 || s + 1 == steps))
                     each(sums, [](product_f32x4 &v, product_f32x4 &w) {
                         v += w;
@@ -369,16 +409,60 @@ struct Tile {
                 --pending;
             }
             finish(job, sums);
-            if (!more) break;
+            if (!more) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no load may reach LDS that others have by then
+                break;
+            }
+            stored = pending > 0;
             job = then;
-            asked = asked_then;
-            asked_then = 0;
+            if (!in_then) {
+                begin(at, job, false);
+                fresh = true;
+            }
+            in_then = false;
             more = next(then);
             // stages behind a tile without any: its buffers are free, everyone has passed the barrier of the last multiplied stage
             if (pending == 0) {
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
                 ask(STAGES - 1);
             }
+        }
+    }
+};
+
+// Where a tile's rows go, in U: row(mb, v) writes the columns `from` .. columns-1 of block row mb.  bfloat16: two blocks' lane groups exchange their halves,
+// so that a lane has 16 bytes to write and a row's four lanes 64 in a run; every lane of the wavefront has to be there.  What is not in D goes to an offset
+// behind the buffer's end, so that a row is always the same number of stores.
+template <class TILE, class U>
+struct Writer {
+    static constexpr bool PAIRS = sizeof(U) == 2 && TILE::NB % 2 == 0;
+    static constexpr int STEP = PAIRS ? 2 : 1, STORES = TILE::NB / STEP;     // of a row
+    __amdgpu_buffer_rsrc_t to;
+    unsigned at, ld;
+    int row0, rows, column, from, columns;     // column: of this lane's first store in the tile
+
+    // first: the tile's first element (of columns in front of `from` no address is used)
+    __device__ __forceinline__ Writer(const TILE &tile, U *first, unsigned ld_bytes, int rows_, int columns_, int from_ = 0)
+        : to(__builtin_amdgcn_make_buffer_rsrc(first, 0, 0x7fffffff, 0x27000)), ld(ld_bytes), row0(tile.of_row(0)), rows(rows_), from(from_), columns(columns_)
+    {
+        const int g = (threadIdx.x & 63) >> 4;
+        column = tile.first_column() + (PAIRS ? (g & 1) * 16 + (g >> 1) * 8 : g * 4);
+        at = (unsigned)row0 * ld + (unsigned)column * sizeof(U);
+    }
+    __device__ __forceinline__ void row(int mb, const product_f32x4 (&v)[TILE::NB]) const
+    {
+        const bool there = row0 + mb * 16 < rows;
+#pragma unroll
+        for (int nb = 0; nb < TILE::NB; nb += STEP) {
+            const int c = column + nb * 16;
+            const unsigned where = there && c >= from && c < columns ? at + nb * 16 * (unsigned)sizeof(U) : 0x80000000u, behind = mb * 16 * ld;
+            if constexpr (PAIRS) {
+                const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb + 1][0], v[nb + 1][1]), false, false);
+                const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][2], v[nb][3]), pack_bf16x2(v[nb + 1][2], v[nb + 1][3]), false, false);
+                __builtin_amdgcn_raw_buffer_store_b128(product_u32x4{lo[0], hi[0], lo[1], hi[1]}, to, where, behind, 0);
+            } else if constexpr (sizeof(U) == 2) {
+                __builtin_amdgcn_raw_buffer_store_b64(product_u32x2{pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb][2], v[nb][3])}, to, where, behind, 0);
+            } else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, v[nb]), to, where, behind, 0);
         }
     }
 };

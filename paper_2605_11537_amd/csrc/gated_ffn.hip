@@ -80,9 +80,9 @@ struct GatedArgs {
 // ------------------------------------------------------------------------------------------------- products over rows sorted by expert
 enum GatedStep { GATED_HIDDEN, GATED_DOWN, GATED_DHIDDEN, GATED_DX };
 
-// STEP's tiles of type TILE in the units first .. past-1 of n_m x n_n tiles of BIG_M rows x BIG_N columns (of a half), each cut into TILEs
+// STEP's tiles of type TILE: `units` of the parts of n_m x n_n tiles of BIG_M rows x BIG_N columns (of a half), from tile `first` on
 template <int STEP, class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_M = BIG_M / TILE::BM, PARTS_N = BIG_N / TILE::HALF_N, PARTS = PARTS_M * PARTS_N;
@@ -92,7 +92,6 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
     const unsigned ldb = STEP == GATED_HIDDEN || STEP == GATED_DX ? f_bytes : d_bytes;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const bool with_states = p.gu != nullptr;
-    Units units((past - first) * PARTS);
     tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n, lo, hi;
@@ -149,9 +148,9 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v[nb][i] = act_of<Z == 4>(p.activation, sums[0][mb][nb][i]) * sums[1][mb][nb][i];
                         if (with_states) {                             // uniform
-                            const unsigned where = there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u;
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[0][mb][nb]), gu, where, mb * 16 * gu_bytes, 0);
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[1][mb][nb]), gu, where + 64, mb * 16 * gu_bytes, 0);
+                            const unsigned where = (there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u) + mb * 16 * gu_bytes;
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[0][mb][nb]), gu, where, 0, 0);
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[1][mb][nb]), gu, where + 64, 0, 0);
                         }
                     }
                     h.row(mb, v);
@@ -210,7 +209,9 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
     tiles.count();
     const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, Big::HALF_N);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
-        gated_rows<STEP, typename decltype(sized)::Type, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, past, tall);
+        typedef typename decltype(sized)::Type Part;
+        constexpr int parts = Big::BM / Part::BM * (Big::HALF_N / Part::HALF_N);
+        gated_rows<STEP, Part, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, Units((past - first) * parts), tall);
     });
 }
 
@@ -223,13 +224,16 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedA
     const RowTiles tiles = {prefix, p.offset, p.E, p.R, TILE::BM};
     tiles.count();
     const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
-    gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N>(p, tiles, smem, n_m, n_n, 0, n_m * n_n, 8);
+    gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
 // ------------------------------------------------------------------------------------------------- the weights' gradients
+// Experts have different numbers of rows: an XCD's range of units holds an eighth of every expert's tiles.
+__host__ __device__ constexpr int gated_weights_share(int tiles) { return (tiles + 7) / 8; }
+
 // DOWN: dW_down = h^T dy, F x d; else dW_gate and dW_up = x^T [dg | du], d x 2F.  An expert without rows gets zeros.
 template <bool DOWN, class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
@@ -237,18 +241,20 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
     const int M = DOWN ? p.F : p.d, N = DOWN ? p.d : 2 * p.F;
     const unsigned lda = M * Z, ldb = N * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
-    Units units((past - first) * PARTS);
+    const int per = gated_weights_share(n_m * n_n);
     tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
-            int u, m, n, e;
+            int u, m, n, e, t;
             do {
                 if (!units.take(u)) return false;
-                const int big = first + u / PARTS;
-                e = big / (n_m * n_n);
-                product_place(big - e * n_m * n_n, n_m, n_n, tall, m, n);
+                const int big = first + u / PARTS, xcd = big / (p.E * per), in = big - xcd * p.E * per;
+                e = in / per;
+                t = xcd * per + in - e * per;
+                if (t >= n_m * n_n) continue;
+                product_place(t, n_m, n_n, tall, m, n);
                 j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
                 j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
-            } while (PARTS > 1 && (j.m0 >= M || j.n0 >= N));
+            } while (t >= n_m * n_n || (PARTS > 1 && (j.m0 >= M || j.n0 >= N)));
             const int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e, lo));
             j.group = e;
             j.rows = M - j.m0 < TILE::BM ? M - j.m0 : TILE::BM;
@@ -282,9 +288,34 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     const int n_m = tiles_of(DOWN ? p.F : p.d, Big::BM), n_n = tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
-    in_rounds<SIZES>(p.E * n_m * n_n, [&](auto sized, int first, int past) {
-        gated_weights<DOWN, typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+    in_rounds<SIZES>(8 * p.E * gated_weights_share(n_m * n_n), [&](auto sized, int first, int past) {
+        typedef typename decltype(sized)::Type Part;
+        gated_weights<DOWN, Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
+}
+
+// ------------------------------------------------------------------------------------------------- both, where there is work for the whole chip
+// dh with dW_down, dx with dW_gate and dW_up: two products that need nothing of each other share a launch, so that the last round of one does not leave
+// compute units without work, and the tiles that wait for memory (dh's for the states) run beside such as do not.
+template <int STEP, class ROWS, class WEIGHTS>
+__global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(GatedArgs p, int tall)
+{
+    typedef typename Whole<ROWS>::Tile Rows;
+    typedef typename Whole<WEIGHTS>::Tile Weights;
+    constexpr bool DOWN = STEP == GATED_DHIDDEN;
+    __shared__ __align__(1024) char smem[Rows::LDS > Weights::LDS ? Rows::LDS : Weights::LDS];
+    __shared__ int prefix[MAX_GROUPS + 1];
+    const RowTiles tiles = {prefix, p.offset, p.E, p.R, Rows::BM};
+    tiles.count();
+    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_DHIDDEN ? p.F : p.d, Rows::HALF_N);
+    const int w_m = tiles_of(DOWN ? p.F : p.d, Weights::BM), w_n = tiles_of(DOWN ? p.d : 2 * p.F, Weights::BN), per = gated_weights_share(w_m * w_n);
+    // costs in stages: a tile's and what its writes take (dh's with its states)
+    const int rows = __builtin_amdgcn_readfirstlane(tiles.end(p.E - 1, 0));
+    const int cost_rows = STEP == GATED_DHIDDEN ? p.d / Rows::STAGE_K + 20 : 2 * p.F / Rows::STAGE_K + 4, cost_weights = rows / p.E / Weights::STAGE_K + 5;
+    const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
+    const int mine = product_share((n_m * n_n + 7) >> 3, cost_rows, p.E * per, cost_weights, slots);
+    if (slot < mine) gated_rows<STEP, Rows, Rows::BM, Rows::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n, slot, mine), tall);
+    else gated_weights<DOWN, Weights, Weights::BM, Weights::BN>(p, smem, w_m, w_n, 0, Units(8 * p.E * per, slot - mine, slots - mine), tall);
 }
 
 // ------------------------------------------------------------------------------------------------- host
@@ -340,9 +371,25 @@ void forward(const GatedArgs &p, hipStream_t st)
         launch_few_rows<GATED_DOWN, typename Few<T>::template Tile<ACROSS_K>>(p, st);
     }
 }
+template <int STEP, class T>
+void launch_pair(const GatedArgs &p, hipStream_t st)
+{
+    typedef Sizes<T, ALONG_K, ALONG_K> rows;
+    typedef Sizes<T, ACROSS_K, ACROSS_K> weights;
+    hipLaunchKernelGGL((gated_pair_kernel<STEP, rows, weights>), dim3(PRODUCT_CUS * rows::PER_CU), dim3(Whole<rows>::THREADS), 0, st, p, 8);
+}
 template <class T>
 void backward(const GatedArgs &p, hipStream_t st)
 {
+    // tiles of the largest size in a pair's two products
+    typedef typename Whole<Sizes<T, ACROSS_K, ACROSS_K>>::Tile big;
+    const long long of_rows = ((long long)p.R / big::BM + 1), of_weights = (long long)p.E * tiles_of(p.d, big::BM);
+    const bool many = (of_rows + of_weights) * tiles_of(p.F, big::BN) >= 2 * PRODUCT_CUS * Sizes<T, ACROSS_K, ACROSS_K>::PER_CU;
+    if (p.R > 0 && tall_tiles(p.R, p.E) && many && p.dx && p.dw_gate && p.dw_down) {
+        launch_pair<GATED_DHIDDEN, T>(p, st);
+        launch_pair<GATED_DX, T>(p, st);
+        return;
+    }
     if (p.R == 0) {                            // zeros for every weight
     } else if (tall_tiles(p.R, p.E)) {
         launch_rows<GATED_DHIDDEN, Sizes<T, ALONG_K, ALONG_K>>(p, st);

@@ -72,16 +72,14 @@ __device__ __forceinline__ bool holds_column(int in)
     return in >= 0 && in < TILE::WAVE_N && ((in >> 2) & 3) == (int)((threadIdx.x & 63) >> 4);
 }
 
-// The units first .. past-1 of n_m x n_n tiles of BIG_M x BIG_N, each cut into TILEs (below likewise); here all have BIG_N columns, for which a row has one
-// slot.
+// `units` of the parts of n_m x n_n tiles of BIG_M x BIG_N, from tile `first` on (below likewise); here all have BIG_N columns, for which a row has one slot.
 template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, float2 *parts, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, float2 *parts, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int WN = TILE::BN / TILE::WAVE_N, PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned d_bytes = p.d * sizeof(T);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
-    Units units((past - first) * PARTS);
     tile.template run<0>(
         [&](Job &j) {
             int u, m, n;
@@ -154,7 +152,8 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.V, Big::BN);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::BN == Big::BN, "one slot for a row's columns of a tile");
-        head_forward<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, parts, n_m, n_n, first, past, tall);
+        typedef typename decltype(sized)::Type Part;
+        head_forward<Part, Big::BM, Big::BN>(p, smem, parts, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
 }
 template <class TILE>
@@ -163,7 +162,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
     __shared__ __align__(1024) char smem[TILE::LDS];
     __shared__ float2 parts[4 * TILE::BM];
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
-    head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, n_m * n_n, 8);
+    head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
 // One wavefront per row: its tiles' maxima and sums -> lse and the target's log probability.
@@ -198,14 +197,13 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, con
 }
 
 template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned d_bytes = p.d * sizeof(T);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     const float largest = *p.largest;
-    Units units((past - first) * PARTS);
     tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n;
@@ -280,7 +278,8 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dlogits_kernel(
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.columns, Big::BN);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::WAVE_M == Big::WAVE_M, "one slot for a wavefront's rows");
-        head_dlogits<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+        typedef typename decltype(sized)::Type Part;
+        head_dlogits<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
 }
 template <class TILE>
@@ -288,7 +287,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_dlogits_few_kernel(Head
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
-    head_dlogits<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, n_m * n_n, 8);
+    head_dlogits<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
 // ------------------------------------------------------------------------------------------------- the two products of the gradient
@@ -303,13 +302,12 @@ struct HeadGradArgs {
 };
 
 template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned lda = p.ld * Z, ldb = p.d * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
-    Units units((past - first) * PARTS);
     tile.template run<TILE::MB * Writer<TILE, float>::STORES>(
         [&](Job &j) {
             int u, m, n;
@@ -356,7 +354,8 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dh_kernel(HeadG
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.d, Big::BN);
     in_rounds<SIZES>(p.parts * n_m * n_n, [&](auto sized, int first, int past) {
-        head_dh<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+        typedef typename decltype(sized)::Type Part;
+        head_dh<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
 }
 template <class TILE>
@@ -364,18 +363,17 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_dh_few_kernel(HeadGradA
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.d, TILE::BN);
-    head_dh<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, p.parts * n_m * n_n, 8);
+    head_dh<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, Units(p.parts * n_m * n_n), 8);
 }
 
 template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, int past, int tall)
+__device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned lda = p.ld * Z, ldb = p.d * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const float largest = *p.largest;
-    Units units((past - first) * PARTS);
     tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
         [&](Job &j) {
             int u, m, n;
@@ -411,8 +409,24 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dw_kernel(HeadG
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     const int n_m = tiles_of(p.columns, Big::BM), n_n = tiles_of(p.d, Big::BN);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
-        head_dw<typename decltype(sized)::Type, Big::BM, Big::BN>(p, smem, n_m, n_n, first, past, tall);
+        typedef typename decltype(sized)::Type Part;
+        head_dw<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
+}
+
+// Both, where there is work for the whole chip: they need nothing of each other, and the last round of one leaves no compute units without work.
+template <class DH, class DW>
+__global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGradArgs p, int tall)
+{
+    typedef typename Whole<DH>::Tile Dh;
+    typedef typename Whole<DW>::Tile Dw;
+    __shared__ __align__(1024) char smem[Dh::LDS > Dw::LDS ? Dh::LDS : Dw::LDS];
+    const int h_m = tiles_of(p.N, Dh::BM), h_n = tiles_of(p.d, Dh::BN), w_m = tiles_of(p.columns, Dw::BM), w_n = tiles_of(p.d, Dw::BN);
+    const int n1 = p.parts * h_m * h_n, n2 = w_m * w_n;
+    const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
+    const int mine = product_share((n1 + 7) >> 3, p.part / Dh::STAGE_K + 6, (n2 + 7) >> 3, p.N / Dw::STAGE_K + 4, slots);
+    if (slot < mine) head_dh<Dh, Dh::BM, Dh::BN>(p, smem, h_m, h_n, 0, Units(n1, slot, mine), tall);
+    else head_dw<Dw, Dw::BM, Dw::BN>(p, smem, w_m, w_n, 0, Units(n2, slot - mine, slots - mine), tall);
 }
 
 // ------------------------------------------------------------------------------------------------- rows
@@ -575,6 +589,12 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
         q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.ld = p.ld, q.v0 = v0;
         q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), 64), q.add = v0 > 0;
         q.dh = dh_parts, q.dw = dw, q.largest = largest;
+        if (dh && dw && g.paired) {
+            typedef AllParts<T> sizes;
+            hipLaunchKernelGGL((head_pair_kernel<sizes, Sizes<T, ACROSS_K, ACROSS_K>>), dim3(PRODUCT_CUS * sizes::PER_CU),
+                               dim3(Whole<sizes>::THREADS), 0, st, q, 8);
+            continue;
+        }
         if (dh) HEAD_BY_ROWS(head_dh, AllParts, ALONG_K, ACROSS_K, q, st, N, p.d, g.parts, 0);
         if (dw) {
             typedef Sizes<T, ACROSS_K, ACROSS_K> sizes;

@@ -6,7 +6,7 @@ namespace moe {
 
 constexpr int HEAD_MAX_WIDTH = 1 << 20;        // byte offsets inside a tile's rows fit 31 bits
 constexpr int HEAD_MAX_IDS = 1 << 24, HEAD_MAX_ROWS = 1 << 24;
-constexpr size_t HEAD_PIECE_BYTES = 512u << 20;
+constexpr size_t HEAD_PIECE_BYTES = 1u << 30;    // of dz, and of the parts of dh's sum
 constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 
 enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
@@ -26,6 +26,7 @@ static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dt
 struct HeadShape {
     int piece;                                 // ids of the vocabulary whose dz is in memory at a time
     int parts;                                 // of a piece's sum for dh
+    bool paired;                               // dh and dW share a launch
     int db_rows;                               // rows of partial sums for db
     size_t rows_at, dz_at, dh_at, db_at, bytes;
 };
@@ -37,14 +38,25 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     const int fits = most < 256 ? 256 : most > (size_t)V ? V : (int)most;
     const int pieces = ceil_div(V, fits);
     g.piece = pieces == 1 ? V : (int)align_up(ceil_div(V, pieces), 256);
-    // Parts of dh's sum: as many as fill the chip evenly.  A tile costs its k and some 512 beside, for its first stage and its writes.
-    const long long tiles = (long long)ceil_div(N, head_tile_rows(N, dtype)) * ceil_div(d, head_tile_columns(N, dtype));
+    // Parts of dh's sum.  A tile costs its k and some 384 beside, for its first stage and its writes.  Paired with dW, whose tiles are at least as many as
+    // compute units: as many parts as bring both to the same end, for each number of workgroups of an XCD that dW may have.  Alone: as fill the chip evenly.
+    const int rows = head_tile_rows(N, dtype), columns = head_tile_columns(N, dtype), slots = dtype == MOE_F32 ? 64 : 32;
+    const long long tiles = (long long)ceil_div(N, rows) * ceil_div(d, columns), of_dw = (long long)ceil_div(g.piece, rows) * ceil_div(d, columns);
+    g.paired = head_rows(N) == HEAD_TALL_TILES && of_dw + tiles * 2 >= 8 * slots;
     double best = 0;
     g.parts = 1;
     for (int s = 1; s <= 64; ++s) {
         if (s > 1 && (g.piece / s < 512 || (size_t)s * N * d * 4 > HEAD_PIECE_BYTES)) break;
-        const double cost = (double)((tiles * s + 255) / 256) * ((double)g.piece / s + 512);
-        if (s == 1 || cost < best * 0.97) {
+        const double k = (double)g.piece / s + 384;
+        double cost = (double)((tiles * s + 8 * slots - 1) / (8 * slots)) * k;
+        for (int mine = 1; g.paired && mine < slots; ++mine) {
+            const double t1 = (double)(((tiles * s + 7) / 8 + mine - 1) / mine) * k;
+            const double t2 = (double)(((of_dw + 7) / 8 + slots - mine - 1) / (slots - mine)) * (N + 256.0);
+            const double t = t1 > t2 ? t1 : t2;
+            cost = mine == 1 || t < cost ? t : cost;
+        }
+        cost += (double)s * 24;                // a part is written and read again: 8 bytes for every row and column
+        if (s == 1 || cost < best * 0.99) {
             best = cost;
             g.parts = s;
         }

@@ -455,14 +455,16 @@ struct Writer {
 #pragma unroll
         for (int nb = 0; nb < TILE::NB; nb += STEP) {
             const int c = column + nb * 16;
-            const unsigned where = there && c >= from && c < columns ? at + nb * 16 * (unsigned)sizeof(U) : 0x80000000u, behind = mb * 16 * ld;
+            // the whole offset in a vector register: behind a 16-byte store with a part of it in a scalar one the compiler takes the data's registers as free
+            // one instruction later, and the last four lanes of sixteen were seen to write what came into them then
+            const unsigned where = (there && c >= from && c < columns ? at + nb * 16 * (unsigned)sizeof(U) : 0x80000000u) + mb * 16 * ld;
             if constexpr (PAIRS) {
                 const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb + 1][0], v[nb + 1][1]), false, false);
                 const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16x2(v[nb][2], v[nb][3]), pack_bf16x2(v[nb + 1][2], v[nb + 1][3]), false, false);
-                __builtin_amdgcn_raw_buffer_store_b128(product_u32x4{lo[0], hi[0], lo[1], hi[1]}, to, where, behind, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(product_u32x4{lo[0], hi[0], lo[1], hi[1]}, to, where, 0, 0);
             } else if constexpr (sizeof(U) == 2) {
-                __builtin_amdgcn_raw_buffer_store_b64(product_u32x2{pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb][2], v[nb][3])}, to, where, behind, 0);
-            } else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, v[nb]), to, where, behind, 0);
+                __builtin_amdgcn_raw_buffer_store_b64(product_u32x2{pack_bf16x2(v[nb][0], v[nb][1]), pack_bf16x2(v[nb][2], v[nb][3])}, to, where, 0, 0);
+            } else __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, v[nb]), to, where, 0, 0);
         }
     }
 };
@@ -534,16 +536,18 @@ __device__ __forceinline__ void product_place(int u, int n_m, int n_n, int tall,
     m = first + in - n * h;
 }
 
-// The units of a persistent workgroup: the ids that the hardware deals to one XCD take a contiguous range of them, side by side.
+// The units of a persistent workgroup: the ids that the hardware deals to one XCD take a contiguous range of them, side by side.  slot, slots: this
+// workgroup among those of its XCD that have these units.
 struct Units {
     int at, end, by;
-    __device__ __forceinline__ Units(int total)
+    __device__ __forceinline__ Units(int total, int slot, int slots)
     {
-        const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, per = (total + 7) >> 3;
+        const int xcd = blockIdx.x & 7, per = (total + 7) >> 3;
         at = xcd * per + slot;
         end = (xcd + 1) * per < total ? (xcd + 1) * per : total;
-        by = gridDim.x >> 3;                   // grids are multiples of 8
+        by = slots;
     }
+    __device__ __forceinline__ explicit Units(int total) : Units(total, blockIdx.x >> 3, gridDim.x >> 3) {}      // grids are multiples of 8
     __device__ __forceinline__ bool take(int &u)
     {
         if (at >= end) return false;
@@ -552,6 +556,19 @@ struct Units {
         return true;
     }
 };
+
+// Two products in one launch: how many of an XCD's `slots` workgroups (2 .. 64) the first one gets, so that both are done at the same time.  n: units
+// of an XCD, cost: of a unit.  By all lanes of a wavefront.
+__device__ __forceinline__ int product_share(int n1, int cost1, int n2, int cost2, int slots)
+{
+    if (n1 == 0) return 0;
+    if (n2 == 0) return slots;
+    const int lane = threadIdx.x & 63, mine = lane >= 1 && lane < slots ? lane : 1, others = slots - mine;
+    float t = -fmaxf((float)((n1 + mine - 1) / mine) * cost1, (float)((n2 + others - 1) / others) * cost2);
+    int best = mine;
+    argmax_over<64>(t, best);
+    return __builtin_amdgcn_readfirstlane(best);
+}
 
 // A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half, a quarter or an eighth of that
 // size, if one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.

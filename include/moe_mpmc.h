@@ -431,7 +431,7 @@ int moe_token_logprobs_backward(const void *logits, long long row_stride, const 
 #define MOE_ACT_SILU 0
 #define MOE_ACT_GELU 1
 #define MOE_ACT_RELU 2
-size_t moe_gated_ffn_states_bytes(int R, int F, int dtype);
+size_t moe_gated_ffn_states_bytes(int R, int E, int F, int dtype);
 size_t moe_gated_ffn_workspace_bytes(int R, int E, int d, int F, int dtype);
 int moe_gated_ffn(const void *x, const int32_t *expert_offset, const void *w_gate, const void *w_up, const void *w_down, int R,
                   int E, int d, int F, int dtype, int activation, void *y, void *states, void *ws, size_t ws_bytes, void *stream);

@@ -143,7 +143,7 @@ def lib():
         _lib.moe_token_logprobs_workspace_bytes.argtypes = [I, I, I, I]
         _lib.moe_token_logprobs.argtypes = [P, Q, P, I, I, I, I, P, P, P, P, P, P, S, P]
         _lib.moe_token_logprobs_backward.argtypes = [P, Q, P, P, P, P, P, I, I, I, P, Q, P]
-        _lib.moe_gated_ffn_states_bytes.argtypes = [I, I, I]
+        _lib.moe_gated_ffn_states_bytes.argtypes = [I] * 4
         _lib.moe_gated_ffn_workspace_bytes.argtypes = [I] * 5
         _lib.moe_gated_ffn.argtypes = [P] * 5 + [I] * 6 + [P] * 3 + [S, P]
         _lib.moe_gated_ffn_backward_workspace_bytes.argtypes = [I] * 5
@@ -730,8 +730,8 @@ def _gated_sizes(who, x, w_gate, w_up, w_down, expert_offset):
     return R, E, d, F, _dt(x)
 
 
-def _check_gated_states(who, x, states, R, F, dt):
-    _c().expect(who, _device, x, "states", states, torch.uint8, (_size("moe_gated_ffn_states_bytes", R, F, dt),))
+def _check_gated_states(who, x, states, R, E, F, dt):
+    _c().expect(who, _device, x, "states", states, torch.uint8, (_size("moe_gated_ffn_states_bytes", R, E, F, dt),))
 
 
 def moe_gated_ffn(x, w_gate, w_up, w_down, expert_offset=None, activation=ACT_SILU, want_states=False, out=None, states=None, ws=None):
@@ -744,7 +744,7 @@ def moe_gated_ffn(x, w_gate, w_up, w_down, expert_offset=None, activation=ACT_SI
     want_states = want_states or states is not None
     room = (None, ()) if want_states else _room(ws, "moe_gated_ffn_workspace_bytes", R, E, d, F, dt)
     if states is not None:
-        _check_gated_states("moe_gated_ffn", x, states, R, F, dt)
+        _check_gated_states("moe_gated_ffn", x, states, R, E, F, dt)
     if out is None:
         if expert_offset is not None:
             out = torch.zeros(R, d, dtype=t, device=x.device)
@@ -752,7 +752,7 @@ def moe_gated_ffn(x, w_gate, w_up, w_down, expert_offset=None, activation=ACT_SI
         c.expect("moe_gated_ffn", _device, x, "out", out, t, (R, d))
     y, kept, made = c.fresh(x, t if out is None else None, (R, d),
                             torch.uint8 if want_states and states is None else None,
-                            (_size("moe_gated_ffn_states_bytes", R, F, dt) if want_states else 0,), *room)
+                            (_size("moe_gated_ffn_states_bytes", R, E, F, dt) if want_states else 0,), *room)
     y = out if out is not None else y
     states = states if states is not None else kept
     ws, ws_bytes = (None, 0) if want_states else _workspace("moe_gated_ffn", x, ws, made)
@@ -769,7 +769,7 @@ def moe_gated_ffn_backward(dy, x, w_gate, w_up, w_down, states, expert_offset=No
     t, c = x.dtype, _c()
     c.expect(who, _device, x, "dy", dy, t, (R, d))
     if R:
-        _check_gated_states(who, x, states, R, F, dt)
+        _check_gated_states(who, x, states, R, E, F, dt)
     room = _room(ws, "moe_gated_ffn_backward_workspace_bytes", R, E, d, F, dt)
     if out is None:
         dx = None if expert_offset is None else torch.zeros(R, d, dtype=t, device=x.device)

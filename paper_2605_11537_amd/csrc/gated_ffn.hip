@@ -66,8 +66,11 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
     return g > 0.f ? g : g != g ? g : 0.f;
 }
 
-// Sixteen columns' g, then their u: what the four lanes of a row write and read lies in runs of 64 bytes.
-__host__ __device__ constexpr int states_width(int F) { return (F + 15) / 16 * 32; }
+// The states' g and u: blocks of 16 rows (of an expert, from its first) x 16 columns, in the order of the matrix instructions' lanes, u's block behind g's.
+// What a store or a load of a wavefront moves is then 1 KB in a run; rows of 64 bytes took 14 of a tile's 50 us (256 x 128, d 1024).
+constexpr int GATED_BLOCK = 2 * 256;           // floats
+__host__ __device__ constexpr int states_columns(int F) { return (F + 15) / 16; }
+static inline size_t states_blocks(int R, int E) { return (size_t)R / 16 + (E < R ? E : R); }      // of rows, at most
 
 struct GatedArgs {
     const void *x, *w_gate, *w_up, *w_down, *dy;
@@ -79,6 +82,15 @@ struct GatedArgs {
 
 // ------------------------------------------------------------------------------------------------- products over rows sorted by expert
 enum GatedStep { GATED_HIDDEN, GATED_DOWN, GATED_DHIDDEN, GATED_DX };
+
+// this lane's place in the block of the wavefront's first rows and columns
+template <class TILE>
+__device__ __forceinline__ float *gated_states(const TILE &tile, const RowTiles &tiles, const Job &j, const GatedArgs &p)
+{
+    const int row = j.m0 + tile.first_row() - tiles.first(j.group), column = j.n0 + tile.first_column();
+    const size_t block = (size_t)(tiles.blocks[j.group] + row / 16) * states_columns(p.F) + column / 16;
+    return p.gu + block * GATED_BLOCK + (threadIdx.x & 63) * 4;
+}
 
 // STEP's tiles of type TILE: `units` of the parts of n_m x n_n tiles of BIG_M rows x BIG_N columns (of a half), from tile `first` on
 template <int STEP, class TILE, int BIG_M, int BIG_N>
@@ -134,23 +146,21 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
         [&](const Job &j, typename TILE::Sums &sums) {
             if constexpr (STEP == GATED_HIDDEN) {
                 const Writer<TILE, T> h(tile, (T *)p.h + (size_t)j.m0 * p.F + j.n0, f_bytes, j.rows, j.columns);
-                // rows of g and u in turn, 16 columns each
-                const unsigned gu_bytes = states_width(p.F) * 4;
-                const int g4 = ((threadIdx.x & 63) >> 4) * 4, first = tile.first_column();
-                const auto gu = __builtin_amdgcn_make_buffer_rsrc(p.gu + (size_t)j.m0 * states_width(p.F) + (j.n0 + first) * 2, 0, 0x7fffffff, 0x27000);
-                const unsigned at = (unsigned)tile.of_row(0) * gu_bytes + g4 * 4;
+                float *const gu = gated_states(tile, tiles, j, p);
+                const size_t row_of_blocks = (size_t)states_columns(p.F) * GATED_BLOCK;
+                const int last = states_columns(p.F) - 1 - (j.n0 + tile.first_column()) / 16;      // block of columns from this wavefront's first on
 #pragma unroll
                 for (int mb = 0; mb < TILE::MB; ++mb) {
                     product_f32x4 v[TILE::NB];
-                    const bool there = tile.of_row(mb) < j.rows;
+                    const bool there = with_states && tile.first_row() + mb * 16 < j.rows;         // uniform
 #pragma unroll
                     for (int nb = 0; nb < TILE::NB; ++nb) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) v[nb][i] = act_of<Z == 4>(p.activation, sums[0][mb][nb][i]) * sums[1][mb][nb][i];
-                        if (with_states) {                             // uniform
-                            const unsigned where = (there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u) + mb * 16 * gu_bytes;
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[0][mb][nb]), gu, where, 0, 0);
-                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(product_u32x4, sums[1][mb][nb]), gu, where + 64, 0, 0);
+                        if (there && nb <= last) {
+                            float *const at = gu + mb * row_of_blocks + nb * GATED_BLOCK;
+                            store4(at, sums[0][mb][nb]);
+                            store4(at + 256, sums[1][mb][nb]);
                         }
                     }
                     h.row(mb, v);
@@ -158,19 +168,18 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
             } else if constexpr (STEP == GATED_DHIDDEN) {
                 T *const to = (T *)p.dgu + (size_t)j.m0 * 2 * p.F + j.n0;
                 const Writer<TILE, T> dg(tile, to, 2 * f_bytes, j.rows, j.columns), du(tile, to + p.F, 2 * f_bytes, j.rows, j.columns);
-                const unsigned gu_bytes = states_width(p.F) * 4;
-                const int g4 = ((threadIdx.x & 63) >> 4) * 4, first = tile.first_column();
-                const auto gu = __builtin_amdgcn_make_buffer_rsrc(p.gu + (size_t)j.m0 * states_width(p.F) + (j.n0 + first) * 2, 0, 0x7fffffff, 0x27000);
-                const unsigned at = (unsigned)tile.of_row(0) * gu_bytes + g4 * 4;
+                const float *const gu = gated_states(tile, tiles, j, p);
+                const size_t row_of_blocks = (size_t)states_columns(p.F) * GATED_BLOCK;
+                const int last = states_columns(p.F) - 1 - (j.n0 + tile.first_column()) / 16;
                 // the states of a row of blocks are asked for a row ahead
-                product_u32x4 gate[2][TILE::NB], up[2][TILE::NB];
+                product_f32x4 gate[2][TILE::NB], up[2][TILE::NB];
                 auto ask = [&](int mb) {
-                    const bool there = tile.of_row(mb) < j.rows;
+                    const bool there = tile.first_row() + mb * 16 < j.rows;
 #pragma unroll
                     for (int nb = 0; nb < TILE::NB; ++nb) {
-                        const unsigned where = there && first + nb * 16 + g4 < j.columns ? at + nb * 128 : 0x80000000u;
-                        gate[mb & 1][nb] = __builtin_amdgcn_raw_buffer_load_b128(gu, where, mb * 16 * gu_bytes, 0);
-                        up[mb & 1][nb] = __builtin_amdgcn_raw_buffer_load_b128(gu, where + 64, mb * 16 * gu_bytes, 0);
+                        const product_f32x4 *at = reinterpret_cast<const product_f32x4 *>(there && nb <= last ? gu + mb * row_of_blocks + nb * GATED_BLOCK : p.gu);
+                        gate[mb & 1][nb] = at[0];
+                        up[mb & 1][nb] = at[64];
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 };
@@ -185,8 +194,8 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
                         for (int i = 0; i < 4; ++i) {
                             float slope;
                             const float v = sums[0][mb][nb][i];
-                            vu[nb][i] = v * act_of<Z == 4>(p.activation, __uint_as_float(gate[mb & 1][nb][i]), slope);
-                            vg[nb][i] = v * __uint_as_float(up[mb & 1][nb][i]) * slope;
+                            vu[nb][i] = v * act_of<Z == 4>(p.activation, gate[mb & 1][nb][i], slope);
+                            vg[nb][i] = v * up[mb & 1][nb][i] * slope;
                         }
                     dg.row(mb, vg);
                     du.row(mb, vu);
@@ -204,8 +213,8 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
 {
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1];
-    const RowTiles tiles = {prefix, p.offset, p.E, p.R, Big::BM};
+    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
+    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, Big::BM};
     tiles.count();
     const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, Big::HALF_N);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
@@ -220,8 +229,8 @@ template <int STEP, class TILE>
 __global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedArgs p)
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1];
-    const RowTiles tiles = {prefix, p.offset, p.E, p.R, TILE::BM};
+    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
+    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, TILE::BM};
     tiles.count();
     const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
     gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n), 8);
@@ -237,7 +246,7 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
-    const RowTiles tiles = {nullptr, p.offset, p.E, p.R, 1};
+    const RowTiles tiles = {nullptr, nullptr, p.offset, p.E, p.R, 1};
     const int M = DOWN ? p.F : p.d, N = DOWN ? p.d : 2 * p.F;
     const unsigned lda = M * Z, ldb = N * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
@@ -304,8 +313,8 @@ __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(Gat
     typedef typename Whole<WEIGHTS>::Tile Weights;
     constexpr bool DOWN = STEP == GATED_DHIDDEN;
     __shared__ __align__(1024) char smem[Rows::LDS > Weights::LDS ? Rows::LDS : Weights::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1];
-    const RowTiles tiles = {prefix, p.offset, p.E, p.R, Rows::BM};
+    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
+    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, Rows::BM};
     tiles.count();
     const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_DHIDDEN ? p.F : p.d, Rows::HALF_N);
     const int w_m = tiles_of(DOWN ? p.F : p.d, Weights::BM), w_n = tiles_of(DOWN ? p.d : 2 * p.F, Weights::BN), per = gated_weights_share(w_m * w_n);
@@ -313,9 +322,15 @@ __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(Gat
     const int rows = __builtin_amdgcn_readfirstlane(tiles.end(p.E - 1, 0));
     const int cost_rows = STEP == GATED_DHIDDEN ? p.d / Rows::STAGE_K + 20 : 2 * p.F / Rows::STAGE_K + 4, cost_weights = rows / p.E / Weights::STAGE_K + 5;
     const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
-    const int mine = product_share((n_m * n_n + 7) >> 3, cost_rows, p.E * per, cost_weights, slots);
-    if (slot < mine) gated_rows<STEP, Rows, Rows::BM, Rows::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n, slot, mine), tall);
-    else gated_weights<DOWN, Weights, Weights::BM, Weights::BN>(p, smem, w_m, w_n, 0, Units(8 * p.E * per, slot - mine, slots - mine), tall);
+    const Shares shares((n_m * n_n + 7) >> 3, cost_rows, p.E * per, cost_weights, slots);
+    const bool first = slot < shares.mine;
+    if (first) {
+        gated_rows<STEP, Rows, Rows::BM, Rows::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n, slot, shares.mine, 0, n_m * n_n), tall);
+        __syncthreads();                       // the buffers change their sizes
+    }
+    const int total = 8 * p.E * per;
+    gated_weights<DOWN, Weights, Weights::BM, Weights::BN>(
+        p, smem, w_m, w_n, 0, first ? Units(total, slot, shares.mine, shares.rest, total) : Units(total, slot - shares.mine, slots - shares.mine, 0, shares.rest), tall);
 }
 
 // ------------------------------------------------------------------------------------------------- host
@@ -332,7 +347,7 @@ void launch_few_rows(const GatedArgs &p, hipStream_t st)
 {
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
     const long long units = ((long long)p.R / TILE::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, TILE::HALF_N);
-    constexpr int per_cu = 160 * 1024 / (TILE::LDS + 4 * (MAX_GROUPS + 4));
+    constexpr int per_cu = 160 * 1024 / (TILE::LDS + 8 * (MAX_GROUPS + 4));
     const long long grid = units < PRODUCT_CUS * per_cu ? units : PRODUCT_CUS * per_cu;
     hipLaunchKernelGGL((gated_few_rows_kernel<STEP, TILE>), dim3((unsigned)((grid + 7) / 8 * 8)), dim3(TILE::THREADS), 0, st, p);
 }
@@ -423,9 +438,9 @@ int gated_check(const char *who, int R, int E, int d, int F, int dtype, int acti
 
 using namespace moe;
 
-extern "C" size_t moe_gated_ffn_states_bytes(int R, int F, int dtype)
+extern "C" size_t moe_gated_ffn_states_bytes(int R, int E, int F, int dtype)
 {
-    return R <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype) + (size_t)R * states_width(F) * 4;
+    return R <= 0 || E <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype) + states_blocks(R, E) * states_columns(F) * GATED_BLOCK * 4;
 }
 
 extern "C" size_t moe_gated_ffn_workspace_bytes(int R, int E, int d, int F, int dtype)

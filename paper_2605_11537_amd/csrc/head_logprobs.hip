@@ -422,11 +422,16 @@ __global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGr
     typedef typename Whole<DW>::Tile Dw;
     __shared__ __align__(1024) char smem[Dh::LDS > Dw::LDS ? Dh::LDS : Dw::LDS];
     const int h_m = tiles_of(p.N, Dh::BM), h_n = tiles_of(p.d, Dh::BN), w_m = tiles_of(p.columns, Dw::BM), w_n = tiles_of(p.d, Dw::BN);
-    const int n1 = p.parts * h_m * h_n, n2 = w_m * w_n;
+    const int n1 = w_m * w_n, n2 = p.parts * h_m * h_n;
     const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
-    const int mine = product_share((n1 + 7) >> 3, p.part / Dh::STAGE_K + 6, (n2 + 7) >> 3, p.N / Dw::STAGE_K + 4, slots);
-    if (slot < mine) head_dh<Dh, Dh::BM, Dh::BN>(p, smem, h_m, h_n, 0, Units(n1, slot, mine), tall);
-    else head_dw<Dw, Dw::BM, Dw::BN>(p, smem, w_m, w_n, 0, Units(n2, slot - mine, slots - mine), tall);
+    const Shares shares((n1 + 7) >> 3, p.N / Dw::STAGE_K + 4, (n2 + 7) >> 3, p.part / Dh::STAGE_K + 6, slots);
+    const bool first = slot < shares.mine;
+    if (first) {
+        head_dw<Dw, Dw::BM, Dw::BN>(p, smem, w_m, w_n, 0, Units(n1, slot, shares.mine, 0, n1), tall);
+        __syncthreads();                       // the buffers change their sizes
+    }
+    head_dh<Dh, Dh::BM, Dh::BN>(p, smem, h_m, h_n, 0,
+                                first ? Units(n2, slot, shares.mine, shares.rest, n2) : Units(n2, slot - shares.mine, slots - shares.mine, 0, shares.rest), tall);
 }
 
 // ------------------------------------------------------------------------------------------------- rows

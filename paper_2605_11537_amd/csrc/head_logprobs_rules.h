@@ -38,24 +38,17 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     const int fits = most < 256 ? 256 : most > (size_t)V ? V : (int)most;
     const int pieces = ceil_div(V, fits);
     g.piece = pieces == 1 ? V : (int)align_up(ceil_div(V, pieces), 256);
-    // Parts of dh's sum.  A tile costs its k and some 384 beside, for its first stage and its writes.  Paired with dW, whose tiles are at least as many as
-    // compute units: as many parts as bring both to the same end, for each number of workgroups of an XCD that dW may have.  Alone: as fill the chip evenly.
-    const int rows = head_tile_rows(N, dtype), columns = head_tile_columns(N, dtype), slots = dtype == MOE_F32 ? 64 : 32;
+    // Parts of dh's sum.  A tile costs its k and some 384 beside, for its first stage and its writes; a part is written and read again.  Paired with dW, whose
+    // tiles are as many as compute units, the parts fill what is left of the last round: about half a part's time is lost.  Alone: whole rounds.
+    const int rows = head_tile_rows(N, dtype), columns = head_tile_columns(N, dtype), slots = dtype == MOE_F32 ? 512 : 256;
     const long long tiles = (long long)ceil_div(N, rows) * ceil_div(d, columns), of_dw = (long long)ceil_div(g.piece, rows) * ceil_div(d, columns);
-    g.paired = head_rows(N) == HEAD_TALL_TILES && of_dw + tiles * 2 >= 8 * slots;
+    g.paired = head_rows(N) == HEAD_TALL_TILES && of_dw + tiles * 2 >= slots;
     double best = 0;
     g.parts = 1;
     for (int s = 1; s <= 64; ++s) {
         if (s > 1 && (g.piece / s < 512 || (size_t)s * N * d * 4 > HEAD_PIECE_BYTES)) break;
-        const double k = (double)g.piece / s + 384;
-        double cost = (double)((tiles * s + 8 * slots - 1) / (8 * slots)) * k;
-        for (int mine = 1; g.paired && mine < slots; ++mine) {
-            const double t1 = (double)(((tiles * s + 7) / 8 + mine - 1) / mine) * k;
-            const double t2 = (double)(((of_dw + 7) / 8 + slots - mine - 1) / (slots - mine)) * (N + 256.0);
-            const double t = t1 > t2 ? t1 : t2;
-            cost = mine == 1 || t < cost ? t : cost;
-        }
-        cost += (double)s * 24;                // a part is written and read again: 8 bytes for every row and column
+        const double k = (double)g.piece / s + 384, traffic = 3e-5 * s * N * d;
+        const double cost = traffic + (g.paired ? (double)tiles * s * k / slots + k / 2 : (double)((tiles * s + slots - 1) / slots) * k);
         if (s == 1 || cost < best * 0.99) {
             best = cost;
             g.parts = s;

@@ -258,6 +258,7 @@ struct Tile {
         b.set_up(ldb, wn * WAVE_N);
     }
     __device__ __forceinline__ int of_row(int mb) const { return wm * WAVE_M + mb * 16 + (threadIdx.x & 15); }
+    __device__ __forceinline__ int first_row() const { return wm * WAVE_M; }
     __device__ __forceinline__ int first_column() const { return wn * WAVE_N; }
     __device__ __forceinline__ int of_column(int nb) const { return wn * WAVE_N + nb * 16 + ((threadIdx.x & 63) >> 4) * 4; }
 
@@ -473,6 +474,7 @@ struct Writer {
 // that goes back, or past the rows there are, is taken for the nearest that does not.
 struct RowTiles {
     int *prefix;                               // LDS, E + 1
+    int *blocks;                               // LDS, E, or NULL: blocks of 16 rows in front of group e's
     const int32_t *offset;
     int E, rows, tile;                         // rows of the matrix, of a tile
 
@@ -493,17 +495,22 @@ struct RowTiles {
     {
         const int lane = threadIdx.x;
         if (lane < WAVE) {
-            int before = 0;
+            int before = 0, blocks_before = 0;
             for (int e0 = 0; e0 < E; e0 += WAVE) {
                 const int e = e0 + lane;
                 int n = 0;
                 if (e < E) {
                     const int lo = first(e);
-                    n = (end(e, lo) - lo + tile - 1) / tile;
+                    n = end(e, lo) - lo;
                 }
-                const int upto = wave_scan_incl(n);
-                if (e < E) prefix[e] = before + upto - n;
+                const int of = (n + tile - 1) / tile, upto = wave_scan_incl(of);
+                if (e < E) prefix[e] = before + upto - of;
                 before += __builtin_amdgcn_readlane(upto, 63);
+                if (blocks) {
+                    const int b = (n + 15) / 16, b_upto = wave_scan_incl(b);
+                    if (e < E) blocks[e] = blocks_before + b_upto - b;
+                    blocks_before += __builtin_amdgcn_readlane(b_upto, 63);
+                }
             }
             if (lane == 0) prefix[E] = before;
         }
@@ -536,18 +543,18 @@ __device__ __forceinline__ void product_place(int u, int n_m, int n_n, int tall,
     m = first + in - n * h;
 }
 
-// The units of a persistent workgroup: the ids that the hardware deals to one XCD take a contiguous range of them, side by side.  slot, slots: this
-// workgroup among those of its XCD that have these units.
+// The units of a persistent workgroup: the ids that the hardware deals to one XCD take a contiguous range of them, side by side.
 struct Units {
     int at, end, by;
-    __device__ __forceinline__ Units(int total, int slot, int slots)
+    // the units from .. to-1 of an XCD's, for `slots` of its workgroups, of which this is number `slot`
+    __device__ __forceinline__ Units(int total, int slot, int slots, int from, int to)
     {
-        const int xcd = blockIdx.x & 7, per = (total + 7) >> 3;
-        at = xcd * per + slot;
-        end = (xcd + 1) * per < total ? (xcd + 1) * per : total;
+        const int xcd = blockIdx.x & 7, per = (total + 7) >> 3, past = xcd * per + (to < per ? to : per);
+        at = xcd * per + from + slot;
+        end = past < total ? past : total;
         by = slots;
     }
-    __device__ __forceinline__ explicit Units(int total) : Units(total, blockIdx.x >> 3, gridDim.x >> 3) {}      // grids are multiples of 8
+    __device__ __forceinline__ explicit Units(int total) : Units(total, blockIdx.x >> 3, gridDim.x >> 3, 0, total) {}      // grids are multiples of 8
     __device__ __forceinline__ bool take(int &u)
     {
         if (at >= end) return false;
@@ -557,18 +564,26 @@ struct Units {
     }
 };
 
-// Two products in one launch: how many of an XCD's `slots` workgroups (2 .. 64) the first one gets, so that both are done at the same time.  n: units
-// of an XCD, cost: of a unit.  By all lanes of a wavefront.
-__device__ __forceinline__ int product_share(int n1, int cost1, int n2, int cost2, int slots)
-{
-    if (n1 == 0) return 0;
-    if (n2 == 0) return slots;
-    const int lane = threadIdx.x & 63, mine = lane >= 1 && lane < slots ? lane : 1, others = slots - mine;
-    float t = -fmaxf((float)((n1 + mine - 1) / mine) * cost1, (float)((n2 + others - 1) / others) * cost2);
-    int best = mine;
-    argmax_over<64>(t, best);
-    return __builtin_amdgcn_readfirstlane(best);
-}
+// Two products in one launch.  Of an XCD's `slots` workgroups (2 .. 64) `mine` have the n1 units of the first, the others units of the second, of which they
+// leave those from `rest` on to the first ones for when they are done: as brings all to the same end.  n: units of an XCD, cost: of a unit.  By all lanes of
+// a wavefront, of which each tries a number.
+struct Shares {
+    int mine, rest;
+    __device__ __forceinline__ Shares(int n1, float cost1, int n2, float cost2, int slots)
+    {
+        const int lane = threadIdx.x & 63, first = lane >= 1 && lane < slots ? lane : 1, second = slots - first;
+        const float t1 = (float)((n1 + first - 1) / first) * cost1, even = (n2 * cost2 + first * t1) / slots;
+        const float rounds = ceilf(even / cost2) * second;
+        int m = even > t1 && rounds < (float)n2 ? (int)rounds : n2;
+        const float t2 = (float)((m + second - 1) / second) * cost2, t3 = t1 + (float)((n2 - m + first - 1) / first) * cost2;
+        float t = -fmaxf(t2, t3);
+        int best = first;
+        argmax_over<64>(t, best);
+        mine = __builtin_amdgcn_readfirstlane(best);
+        rest = __builtin_amdgcn_readfirstlane(__shfl(m, mine, 64));
+        if (n1 == 0) mine = 0, rest = n2;
+    }
+};
 
 // A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half, a quarter or an eighth of that
 // size, if one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.

@@ -20,7 +20,7 @@ struct HeadArgs {
     const float *b, *lse, *dlogprob;
     const int32_t *target;
     int N, d, V;
-    int v0, columns, ld;                       // backward: the piece's first id, its ids, and the row of dz it is kept in
+    int v0, columns;                           // backward: the piece's first id, its ids
     int n_n;                                   // forward: slots of a row
     float2 *tiles;                             // forward [N, n_n]: maximum, sum
     float *at_target;                          // forward [N]
@@ -196,6 +196,13 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, con
     }
 }
 
+// dz lies in blocks of 512 bytes of columns, all rows of one behind all of the last: both products walk it in long runs.  (As a matrix of 50257 columns each
+// row of a stage was on a page of its own.)
+template <class T>
+struct DZ {
+    static constexpr int COLUMNS = HEAD_DZ_ROW / (int)sizeof(T);
+};
+
 template <class TILE, int BIG_M, int BIG_N>
 __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
@@ -224,8 +231,8 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
         },
         [&](const Job &j, typename TILE::Sums &z) {
             add_bias(tile, j, p.b, p.V, z);
-            // a row of dz ends with zeros up to a whole piece of 16 bytes
-            const Writer<TILE, T> to(tile, (T *)p.dz + (size_t)j.m0 * p.ld + (j.n0 - p.v0), p.ld * sizeof(T), j.rows, p.ld - (j.n0 - p.v0));
+            const int at = j.n0 - p.v0;        // behind the last id there are zeros up to the tile's end
+            const Writer<TILE, T> to(tile, (T *)p.dz + ((size_t)(at / DZ<T>::COLUMNS) * p.N + j.m0) * DZ<T>::COLUMNS + at % DZ<T>::COLUMNS, HEAD_DZ_ROW, j.rows, TILE::BN);
             product_f32x4 down[TILE::NB];      // sums over this lane's rows
 #pragma unroll
             for (int nb = 0; nb < TILE::NB; ++nb) down[nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -293,7 +300,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_dlogits_few_kernel(Head
 // ------------------------------------------------------------------------------------------------- the two products of the gradient
 struct HeadGradArgs {
     const void *dz, *h, *w;
-    int N, d, columns, ld, v0;
+    int N, d, columns, v0;
     int parts, part;                           // dh: k in so many parts of so many columns
     bool add;                                  // dh: behind an earlier piece
     float *dh;                                 // [parts, N, d]
@@ -306,7 +313,7 @@ __device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
-    const unsigned lda = p.ld * Z, ldb = p.d * Z;
+    const unsigned lda = HEAD_DZ_ROW, ldb = p.d * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     tile.template run<TILE::MB * Writer<TILE, float>::STORES>(
         [&](Job &j) {
@@ -324,9 +331,8 @@ __device__ __forceinline__ void head_dh(const HeadGradArgs &p, char *smem, int n
             j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
             j.runs = 1;
             j.k = p.columns - k0 < p.part ? (p.columns - k0 > 0 ? p.columns - k0 : 0) : p.part;
-            j.a[0] = source_along(p.dz, (size_t)j.m0 * lda, lda, j.rows, TILE::BM);
-            j.a[0].base += (unsigned)k0 * Z;
-            j.a[0].records -= (unsigned)k0 * Z;
+            j.block = (size_t)p.N * HEAD_DZ_ROW;
+            j.a[0] = source_along(p.dz, k0 / DZ<T>::COLUMNS * j.block + (size_t)j.m0 * lda, lda, j.rows, TILE::BM);
             j.b[0] = source_across(p.w, (size_t)(p.v0 + k0) * ldb, ldb, j.n0 * Z);
             return true;
         },
@@ -371,7 +377,7 @@ __device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
-    const unsigned lda = p.ld * Z, ldb = p.d * Z;
+    const unsigned lda = HEAD_DZ_ROW, ldb = p.d * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const float largest = *p.largest;
     tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
@@ -387,7 +393,7 @@ __device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n
             j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
             j.runs = 1;
             j.k = p.N;
-            j.a[0] = source_across(p.dz, 0, lda, j.m0 * Z);
+            j.a[0] = source_across(p.dz, (size_t)(j.m0 / DZ<T>::COLUMNS) * p.N * HEAD_DZ_ROW, lda, j.m0 % DZ<T>::COLUMNS * Z);
             j.b[0] = source_across(p.h, 0, ldb, j.n0 * Z);
             return true;
         },
@@ -502,9 +508,9 @@ void launch_clear(void *p, size_t bytes, hipStream_t st)
 
 // tiles of 64 and of 16 rows
 template <class T, Order A, Order B>
-using Flat = Tile<T, A, B, 64, HEAD_FEW_COLUMNS, 1, 4>;
+using Flat = Tile<T, A, B, 64, HEAD_FEW_COLUMNS, 1, 4, 1, 2, A == ALONG_K && B == ACROSS_K ? DZ<T>::COLUMNS : 0>;
 template <class T, Order A, Order B>
-using Few = Tile<T, A, B, 16, HEAD_FEW_COLUMNS, 1, 4>;
+using Few = Tile<T, A, B, 16, HEAD_FEW_COLUMNS, 1, 4, 1, 2, A == ALONG_K && B == ACROSS_K ? DZ<T>::COLUMNS : 0>;
 
 // parts of a tile with all of its columns, and with all of its rows
 template <class T>
@@ -533,8 +539,25 @@ struct ColumnParts<float> : Sizes<float, ALONG_K, ALONG_K> {
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 128, 32, 2, 2, 1, 3>> Quarter;
     typedef Quarter Eighth;
 };
+// dh: A in dz's blocks
 template <class T>
-struct AllParts : Sizes<T, ALONG_K, ACROSS_K> {};
+struct DhParts;
+template <>
+struct DhParts<bf16_t> {
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 256, 256, 2, 4, 1, 2, DZ<bf16_t>::COLUMNS>> Whole;
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 256, 2, 4, 1, 3, DZ<bf16_t>::COLUMNS>> Half;
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 128, 2, 4, 1, 4, DZ<bf16_t>::COLUMNS>> Quarter;
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 64, 4, 2, 1, 5, DZ<bf16_t>::COLUMNS>> Eighth;
+    static constexpr int PER_CU = 1;
+};
+template <>
+struct DhParts<float> {
+    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 128, 128, 2, 2, 1, 2, DZ<float>::COLUMNS>> Whole;
+    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 64, 128, 2, 2, 1, 3, DZ<float>::COLUMNS>> Half;
+    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 64, 64, 2, 2, 1, 4, DZ<float>::COLUMNS>> Quarter;
+    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 32, 64, 2, 2, 1, 5, DZ<float>::COLUMNS>> Eighth;
+    static constexpr int PER_CU = 2;
+};
 
 template <class TILE>
 dim3 few_grid(long long units, int more_lds)
@@ -588,19 +611,18 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     for (int v0 = 0; v0 < p.V; v0 += g.piece) {
         p.v0 = v0;
         p.columns = p.V - v0 < g.piece ? p.V - v0 : g.piece;
-        p.ld = (int)align_up(p.columns, 8);
         HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
         HeadGradArgs q = {};
-        q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.ld = p.ld, q.v0 = v0;
-        q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), 64), q.add = v0 > 0;
+        q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.v0 = v0;
+        q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), DZ<T>::COLUMNS), q.add = v0 > 0;
         q.dh = dh_parts, q.dw = dw, q.largest = largest;
         if (dh && dw && g.paired) {
-            typedef AllParts<T> sizes;
+            typedef DhParts<T> sizes;
             hipLaunchKernelGGL((head_pair_kernel<sizes, Sizes<T, ACROSS_K, ACROSS_K>>), dim3(PRODUCT_CUS * sizes::PER_CU),
                                dim3(Whole<sizes>::THREADS), 0, st, q, 8);
             continue;
         }
-        if (dh) HEAD_BY_ROWS(head_dh, AllParts, ALONG_K, ACROSS_K, q, st, N, p.d, g.parts, 0);
+        if (dh) HEAD_BY_ROWS(head_dh, DhParts, ALONG_K, ACROSS_K, q, st, N, p.d, g.parts, 0);
         if (dw) {
             typedef Sizes<T, ACROSS_K, ACROSS_K> sizes;
             typedef typename Whole<sizes>::Tile big;

@@ -7,6 +7,7 @@ namespace moe {
 constexpr int HEAD_MAX_WIDTH = 1 << 20;        // byte offsets inside a tile's rows fit 31 bits
 constexpr int HEAD_MAX_IDS = 1 << 24, HEAD_MAX_ROWS = 1 << 24;
 constexpr size_t HEAD_PIECE_BYTES = 1u << 30;    // of dz, and of the parts of dh's sum
+constexpr int HEAD_DZ_ROW = 512;               // bytes of a row of dz in one of its blocks
 constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 
 enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
@@ -57,7 +58,7 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     g.db_rows = ceil_div(N, head_wave_rows(N, dtype));
     g.rows_at = 256;
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
-    g.dh_at = g.dz_at + align_up((size_t)N * align_up(g.piece, 8) * z, 256);
+    g.dh_at = g.dz_at + (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW);
     g.db_at = g.dh_at + align_up((size_t)g.parts * N * d * 4, 256);
     g.bytes = g.db_at + align_up((size_t)g.db_rows * V * 4, 256);
     return g;

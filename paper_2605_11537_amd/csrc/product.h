@@ -202,6 +202,7 @@ struct Job {
     int k, runs;                               // k of a run, 0 .. : D = 0 without
     int m0, n0, rows, columns;                 // the tile's origin in D and how much of it there is
     int group;                                 // expert, or part of a split sum
+    size_t block;
 };
 
 __device__ __forceinline__ Source source_along(const void *p, size_t first_byte, unsigned ld_bytes, int rows, int most)
@@ -216,7 +217,8 @@ __device__ __forceinline__ Source source_across(const void *p, size_t first_byte
 // BM x BN of D by WM x WN wavefronts.  HALVES = 2: columns come from two operands of BN / 2 rows each, and a wavefront has the same columns of both.
 // A ring of STAGES stages: the loop waits for a stage, asks for the one STAGES - 1 further on, which may be the next tile's, and
 // multiplies, so that a tile's first stages land while the one before is written.
-template <class T_, Order OA, Order OB, int BM_, int BN_, int WM, int WN, int HALVES_ = 1, int STAGES = 2>
+// BLOCK_K: A lies ALONG_K in blocks of so many k, j.block bytes from one to the next.
+template <class T_, Order OA, Order OB, int BM_, int BN_, int WM, int WN, int HALVES_ = 1, int STAGES = 2, int BLOCK_K = 0>
 struct Tile {
     typedef T_ T;
     static constexpr int BM = BM_, BN = BN_, HALVES = HALVES_, WAVES = WM * WN, THREADS = WAVES * WAVE;
@@ -286,6 +288,13 @@ struct Tile {
         c.left -= STAGE_K;
         if (c.left > 0) {
             A::next_buffer(c.a, c.left, lda);
+            if (BLOCK_K > 0 && (j.k - c.left) % (BLOCK_K > 0 ? BLOCK_K : 1) == 0) {
+                constexpr unsigned row = BLOCK_K * sizeof(T);
+                const uint64_t base = (((uint64_t)c.a[1] << 32) | c.a[0]) + j.block - row;
+                c.a[0] = (unsigned)base;
+                c.a[1] = (unsigned)(base >> 32);
+                c.a[2] += row;
+            }
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) B::next_buffer(c.b[h], c.left, ldb);
             return true;

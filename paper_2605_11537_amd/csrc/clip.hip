@@ -16,6 +16,7 @@ namespace {
 constexpr int CLIP_TENSORS = 96;               // of a launch
 constexpr int CLIP_THREADS = 256, CLIP_AHEAD = 4;
 constexpr int CLIP_CHUNK = CLIP_THREADS * CLIP_AHEAD * 16;
+constexpr int CLIP_KEPT = 12288;               // chunks that the second launch begins with and may find in the cache beside the memory: 192 MB
 constexpr int CLIP_BLOCKS = 2048;              // most of a launch: eight to a compute unit
 constexpr int CLIP_MAX_TENSORS = 4096;
 
@@ -77,7 +78,8 @@ __device__ __forceinline__ void clip_walk(long long left, bool loose, int size, 
     for (int i = pieces * 16 / size + threadIdx.x; i < bytes / size; i += CLIP_THREADS) single(i);
 }
 
-template <bool BF16>
+// PASSING: past the caches
+template <bool BF16, bool PASSING>
 __device__ __forceinline__ double clip_chunk_squares(double s, const char *at, long long left, bool loose)
 {
     clip_walk(
@@ -88,7 +90,8 @@ __device__ __forceinline__ double clip_chunk_squares(double s, const char *at, l
             for (int i = 0; i < CLIP_AHEAD; ++i) {
                 const int p = i * CLIP_THREADS + threadIdx.x;
                 v[i] = clip_u32x4{0, 0, 0, 0};
-                if (p < pieces) v[i] = *reinterpret_cast<const clip_u32x4 *>(at + p * 16);
+                const clip_u32x4 *q = reinterpret_cast<const clip_u32x4 *>(at + p * 16);
+                if (p < pieces) v[i] = PASSING ? __builtin_nontemporal_load(q) : *q;
             }
 #pragma unroll
             for (int i = 0; i < CLIP_AHEAD; ++i) s = squares<BF16>(s, v[i]);
@@ -119,8 +122,11 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_squares_kernel(ClipBatch b,
         const long long first = (long long)(c - b.chunk[i]) * CLIP_CHUNK;
         const char *at = (const char *)b.from[i] + first;
         const bool loose = b.loose[i / 32] >> (i % 32) & 1;
-        if (b.is_bf16[i / 32] >> (i % 32) & 1) s = clip_chunk_squares<true>(s, at, b.bytes[i] - first, loose);
-        else s = clip_chunk_squares<false>(s, at, b.bytes[i] - first, loose);
+        const bool bf16 = b.is_bf16[i / 32] >> (i % 32) & 1, passing = c < chunks - CLIP_KEPT;
+        if (bf16 && passing) s = clip_chunk_squares<true, true>(s, at, b.bytes[i] - first, loose);
+        else if (bf16) s = clip_chunk_squares<true, false>(s, at, b.bytes[i] - first, loose);
+        else if (passing) s = clip_chunk_squares<false, true>(s, at, b.bytes[i] - first, loose);
+        else s = clip_chunk_squares<false, false>(s, at, b.bytes[i] - first, loose);
     }
     s = clip_sum(s);
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
@@ -142,7 +148,7 @@ __device__ __forceinline__ void clip_chunk_scaled(const char *at, char *to, long
             for (int i = 0; i < CLIP_AHEAD; ++i) {
                 const int p = i * CLIP_THREADS + threadIdx.x;
                 // by = 1: bit for bit
-                if (p < pieces) *reinterpret_cast<clip_u32x4 *>(to + p * 16) = by == 1.f ? v[i] : scaled<BF16>(v[i], by);
+                if (p < pieces) __builtin_nontemporal_store(by == 1.f ? v[i] : scaled<BF16>(v[i], by), reinterpret_cast<clip_u32x4 *>(to + p * 16));
             }
         },
         [&](int i) {

@@ -8,11 +8,13 @@
 // second rounding to bfloat16 in the chain would make the gradients' error 1.7 times that of rounding them once, 1.4 times without.
 #include "product.h"
 #include "scalar_math.h"
+#include "gated_ffn_rules.h"
+
+#include <type_traits>
 
 namespace moe {
 namespace {
 
-constexpr int GATED_MAX_WIDTH = 1 << 20;       // byte offsets inside a tile's rows fit 31 bits
 constexpr int MAX_GROUPS = MOE_MAX_EXPERTS;
 
 // ------------------------------------------------------------------------------------------------- activations
@@ -68,16 +70,14 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
 
 // The states' g and u: blocks of 16 rows (of an expert, from its first) x 16 columns, in the order of the matrix instructions' lanes, u's block behind g's.
 // What a store or a load of a wavefront moves is then 1 KB in a run; rows of 64 bytes took 14 of a tile's 50 us (256 x 128, d 1024).
-constexpr int GATED_BLOCK = 2 * 256;           // floats
-__host__ __device__ constexpr int states_columns(int F) { return (F + 15) / 16; }
-static inline size_t states_blocks(int R, int E) { return (size_t)R / 16 + (E < R ? E : R); }      // of rows, at most
-
 struct GatedArgs {
     const void *x, *w_gate, *w_up, *w_down, *dy;
     const int32_t *offset;
     int R, E, d, F, activation;
     void *h, *y, *dgu, *dx, *dw_gate, *dw_up, *dw_down;
     float *gu;
+    int parts;                                 // of an expert's rows, whose weight gradients are summed by themselves ...
+    float *sums;                               // ... here: [parts] of the three gradients behind each other, if there is more than one
 };
 
 // ------------------------------------------------------------------------------------------------- products over rows sorted by expert
@@ -256,16 +256,22 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
             int u, m, n, e, t;
             do {
                 if (!units.take(u)) return false;
-                const int big = first + u / PARTS, xcd = big / (p.E * per), in = big - xcd * p.E * per;
+                const int big = first + u / PARTS, groups = p.E * p.parts, xcd = big / (groups * per), in = big - xcd * groups * per;
                 e = in / per;
                 t = xcd * per + in - e * per;
                 if (t >= n_m * n_n) continue;
+                j.group = e;
+                e /= p.parts;
                 product_place(t, n_m, n_n, tall, m, n);
                 j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
                 j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
             } while (t >= n_m * n_n || (PARTS > 1 && (j.m0 >= M || j.n0 >= N)));
-            const int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e, lo));
-            j.group = e;
+            int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e, lo));
+            if (p.parts > 1) {                 // this part's rows
+                const int part = (tiles_of(hi - lo, p.parts) + 63) / 64 * 64, from = lo + (j.group - e * p.parts) * part;
+                hi = from + part < hi ? from + part : hi;
+                lo = from < hi ? from : hi;
+            }
             j.rows = M - j.m0 < TILE::BM ? M - j.m0 : TILE::BM;
             j.columns = N - j.n0 < TILE::BN ? N - j.n0 : TILE::BN;
             j.runs = 1;
@@ -275,19 +281,25 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
-            const size_t w = (size_t)j.group * p.d * p.F;
-            const unsigned ld = (DOWN ? p.d : p.F) * Z;
-            const size_t at = w + (size_t)j.m0 * (DOWN ? p.d : p.F) + j.n0;
-            if (DOWN || j.n0 < p.F) {          // two matrices' columns side by side
-                const Writer<TILE, T> to(tile, (T *)(DOWN ? p.dw_down : p.dw_gate) + at, ld, j.rows, DOWN || j.columns < p.F - j.n0 ? j.columns : p.F - j.n0);
+            const size_t all = (size_t)p.E * p.d * p.F, e = j.group / p.parts, ld = DOWN ? p.d : p.F;
+            const size_t at = e * p.d * p.F + j.m0 * ld + j.n0;
+            auto write = [&](auto *gate, auto *up, auto *down) {
+                typedef std::remove_pointer_t<decltype(gate)> U;
+                if (DOWN || j.n0 < p.F) {      // two matrices' columns side by side
+                    const Writer<TILE, U> to(tile, (DOWN ? down : gate) + at, ld * sizeof(U), j.rows, DOWN || j.columns < p.F - j.n0 ? j.columns : p.F - j.n0);
 #pragma unroll
-                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
-            }
-            if (!DOWN && j.n0 + j.columns > p.F) {
-                const Writer<TILE, T> to(tile, (T *)p.dw_up + at - p.F, ld, j.rows, j.columns, p.F - j.n0);
+                    for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
+                }
+                if (!DOWN && j.n0 + j.columns > p.F) {
+                    const Writer<TILE, U> to(tile, up + at - p.F, ld * sizeof(U), j.rows, j.columns, p.F - j.n0);
 #pragma unroll
-                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
-            }
+                    for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
+                }
+            };
+            if (p.parts > 1) {
+                float *const part = p.sums + (j.group - e * p.parts) * 3 * all;
+                write(part, part + all, part + 2 * all);
+            } else write((T *)p.dw_gate, (T *)p.dw_up, (T *)p.dw_down);
         });
 }
 
@@ -297,10 +309,24 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     const int n_m = tiles_of(DOWN ? p.F : p.d, Big::BM), n_n = tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
-    in_rounds<SIZES>(8 * p.E * gated_weights_share(n_m * n_n), [&](auto sized, int first, int past) {
+    in_rounds<SIZES>(8 * p.E * p.parts * gated_weights_share(n_m * n_n), [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
         gated_weights<DOWN, Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
+}
+
+// The parts' sums added in their order, rounded once.
+template <class T>
+__global__ __launch_bounds__(256) void gated_join_kernel(const float *sums, int parts, size_t all, T *dw_gate, T *dw_up, T *dw_down)
+{
+    T *const to = blockIdx.y == 0 ? dw_gate : blockIdx.y == 1 ? dw_up : dw_down;
+    if (!to) return;
+    const float *from = sums + blockIdx.y * all;
+    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < all; i += (size_t)gridDim.x * 1024) {
+        product_f32x4 v = *reinterpret_cast<const product_f32x4 *>(from + i);
+        for (int s = 1; s < parts; ++s) v += *reinterpret_cast<const product_f32x4 *>(from + s * 3 * all + i);
+        store4(to + i, v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------- both, where there is work for the whole chip
@@ -355,36 +381,44 @@ template <bool DOWN, class SIZES>
 void launch_weights(const GatedArgs &p, hipStream_t st)
 {
     typedef typename Whole<SIZES>::Tile Big;
-    const long long units = (long long)p.E * tiles_of(DOWN ? p.F : p.d, Big::BM) * tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
+    const long long units = (long long)p.E * p.parts * (tiles_of(DOWN ? p.F : p.d, Big::BM) * tiles_of(DOWN ? p.d : 2 * p.F, Big::BN) + 7);
     hipLaunchKernelGGL((gated_weights_kernel<DOWN, SIZES>), dim3(product_grid(units, PRODUCT_CUS * SIZES::PER_CU)), dim3(Big::THREADS), 0, st, p, 8);
 }
 
-// rows of an expert for which a tile of so many rows is taken
-bool tall_tiles(int R, int E) { return R / E >= 96; }
-
-template <class T>
+template <class T, Order B, int HALVES>
 struct Few;
-template <>
-struct Few<bf16_t> {
-    template <Order B, int HALVES = 1>
-    using Tile = moe::Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES>;
+template <Order B, int HALVES>
+struct Few<bf16_t, B, HALVES> {
+    typedef Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES> Mid;
+    typedef Tile<bf16_t, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Low;
+    typedef Tile<bf16_t, ALONG_K, B, 16, 64, 1, 4 / HALVES, HALVES, 8> Tiny;
 };
-template <>
-struct Few<float> {
-    template <Order B, int HALVES = 1>
-    using Tile = moe::Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES>;
+template <Order B, int HALVES>
+struct Few<float, B, HALVES> {
+    typedef Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Mid;
+    typedef Mid Low;
+    typedef Tile<float, ALONG_K, B, 16, 64, 1, 4 / HALVES, HALVES, 8> Tiny;
 };
+
+template <int STEP, class T>
+void launch_step(const GatedArgs &p, hipStream_t st)
+{
+    constexpr Order B = STEP == GATED_HIDDEN || STEP == GATED_DOWN ? ACROSS_K : ALONG_K;
+    constexpr int HALVES = STEP == GATED_HIDDEN ? 2 : 1;
+    typedef Few<T, B, HALVES> few;
+    switch (gated_rows_rule(p.R, p.E, STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d)) {
+    case GATED_TALL: launch_rows<STEP, Sizes<T, ALONG_K, B, HALVES>>(p, st); break;
+    case GATED_MID: launch_few_rows<STEP, typename few::Mid>(p, st); break;
+    case GATED_LOW: launch_few_rows<STEP, typename few::Low>(p, st); break;
+    default: launch_few_rows<STEP, typename few::Tiny>(p, st);
+    }
+}
 
 template <class T>
 void forward(const GatedArgs &p, hipStream_t st)
 {
-    if (tall_tiles(p.R, p.E)) {
-        launch_rows<GATED_HIDDEN, Sizes<T, ALONG_K, ACROSS_K, 2>>(p, st);
-        launch_rows<GATED_DOWN, Sizes<T, ALONG_K, ACROSS_K>>(p, st);
-    } else {
-        launch_few_rows<GATED_HIDDEN, typename Few<T>::template Tile<ACROSS_K, 2>>(p, st);
-        launch_few_rows<GATED_DOWN, typename Few<T>::template Tile<ACROSS_K>>(p, st);
-    }
+    launch_step<GATED_HIDDEN, T>(p, st);
+    launch_step<GATED_DOWN, T>(p, st);
 }
 template <int STEP, class T>
 void launch_pair(const GatedArgs &p, hipStream_t st)
@@ -400,24 +434,25 @@ void backward(const GatedArgs &p, hipStream_t st)
     typedef typename Whole<Sizes<T, ACROSS_K, ACROSS_K>>::Tile big;
     const long long of_rows = ((long long)p.R / big::BM + 1), of_weights = (long long)p.E * tiles_of(p.d, big::BM);
     const bool many = (of_rows + of_weights) * tiles_of(p.F, big::BN) >= 2 * PRODUCT_CUS * Sizes<T, ACROSS_K, ACROSS_K>::PER_CU;
-    if (p.R > 0 && tall_tiles(p.R, p.E) && many && p.dx && p.dw_gate && p.dw_down) {
-        launch_pair<GATED_DHIDDEN, T>(p, st);
-        launch_pair<GATED_DX, T>(p, st);
+    if (gated_rows_rule(p.R, p.E, p.F) == GATED_TALL && many && p.dx && p.dw_gate && p.dw_down) {
+        GatedArgs q = p;
+        q.parts = 1;
+        launch_pair<GATED_DHIDDEN, T>(q, st);
+        launch_pair<GATED_DX, T>(q, st);
         return;
     }
-    if (p.R == 0) {                            // zeros for every weight
-    } else if (tall_tiles(p.R, p.E)) {
-        launch_rows<GATED_DHIDDEN, Sizes<T, ALONG_K, ALONG_K>>(p, st);
-        if (p.dx) launch_rows<GATED_DX, Sizes<T, ALONG_K, ALONG_K>>(p, st);
-    } else {
-        launch_few_rows<GATED_DHIDDEN, typename Few<T>::template Tile<ALONG_K>>(p, st);
-        if (p.dx) launch_few_rows<GATED_DX, typename Few<T>::template Tile<ALONG_K>>(p, st);
+    if (p.R > 0) {                             // else zeros for every weight
+        launch_step<GATED_DHIDDEN, T>(p, st);
+        if (p.dx) launch_step<GATED_DX, T>(p, st);
     }
     if (p.dw_gate) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
     if (p.dw_down) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
+    if (p.parts > 1) {
+        const size_t all = (size_t)p.E * p.d * p.F;
+        hipLaunchKernelGGL(gated_join_kernel<T>, dim3((unsigned)(all / 1024 < 1024 ? all / 1024 + 1 : 1024), 3), dim3(256), 0, st, p.sums, p.parts, all, (T *)p.dw_gate,
+                           (T *)p.dw_up, (T *)p.dw_down);
+    }
 }
-
-size_t hidden_bytes(int R, int F, int dtype) { return align_up((size_t)R * F * (dtype == MOE_F32 ? 4 : 2), 256); }
 
 int gated_check(const char *who, int R, int E, int d, int F, int dtype, int activation)
 {
@@ -445,16 +480,14 @@ extern "C" size_t moe_gated_ffn_states_bytes(int R, int E, int F, int dtype)
 
 extern "C" size_t moe_gated_ffn_workspace_bytes(int R, int E, int d, int F, int dtype)
 {
-    (void)E;
-    (void)d;
-    return R <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype);
+    return R <= 0 || E <= 0 || d <= 0 || F <= 0 ? 0 : hidden_bytes(R, F, dtype);
 }
 
 extern "C" size_t moe_gated_ffn_backward_workspace_bytes(int R, int E, int d, int F, int dtype)
 {
-    (void)E;
-    (void)d;
-    return R <= 0 || F <= 0 ? 0 : 2 * hidden_bytes(R, F, dtype);
+    if (R <= 0 || E <= 0 || d <= 0 || F <= 0) return 0;
+    const int parts = gated_parts(R, E, d, F, dtype);
+    return 2 * hidden_bytes(R, F, dtype) + (parts > 1 ? (size_t)parts * 3 * E * d * F * 4 : 0);
 }
 
 extern "C" int moe_gated_ffn(const void *x, const int32_t *expert_offset, const void *w_gate, const void *w_up, const void *w_down, int R, int E, int d,
@@ -507,6 +540,8 @@ extern "C" int moe_gated_ffn_backward(const void *dy, const void *x, const int32
     p.x = x, p.w_gate = w_gate, p.w_up = w_up, p.w_down = w_down, p.dy = dy, p.offset = expert_offset;
     p.R = R, p.E = E, p.d = d, p.F = F, p.activation = activation;
     p.h = const_cast<void *>(states), p.gu = (float *)((char *)const_cast<void *>(states) + hidden_bytes(R, F, dtype));
+    p.parts = R > 0 ? gated_parts(R, E, d, F, dtype) : 1;
+    p.sums = (float *)((char *)ws + 2 * hidden_bytes(R, F, dtype));
     p.dgu = ws, p.dx = dx, p.dw_gate = dw_gate, p.dw_up = dw_up, p.dw_down = dw_down;
     if (dtype == MOE_BF16) backward<bf16_t>(p, (hipStream_t)stream);
     else backward<float>(p, (hipStream_t)stream);

@@ -1,0 +1,39 @@
+// Sizes of the gated experts' calls: tiles by the number of rows, parts of the weights' sums, workspaces.
+#pragma once
+#include "common.h"
+
+namespace moe {
+
+constexpr int GATED_MAX_WIDTH = 1 << 20;       // byte offsets inside a tile's rows fit 31 bits
+
+// The states' g and u: blocks of 16 rows (of an expert, from its first) x 16 columns, in the order of the matrix instructions' lanes, u's block behind g's.
+// What a store or a load of a wavefront moves is then 1 KB in a run; in rows of 64 bytes they took 14 of a tile's 50 us (256 x 128 of F, d = 1024).
+constexpr int GATED_BLOCK = 2 * 256;           // floats
+__host__ __device__ constexpr int states_columns(int F) { return (F + 15) / 16; }
+static inline size_t states_blocks(int R, int E) { return (size_t)R / 16 + (E < R ? E : R); }      // of rows, at most
+static inline size_t hidden_bytes(int R, int F, int dtype) { return align_up((size_t)R * F * (dtype == MOE_F32 ? 4 : 2), 256); }
+
+// The tile by the rows that an expert has if all have the same (the table is in device memory) and the columns of D.
+//   TINY  16 rows, narrow, eight stages deep: so few tiles that each has a compute unit to itself, where a stage's way from memory counts
+//   LOW   32 rows, MID 64: bound by the stream of the weights
+//   TALL  up to 256, by the matrix pipes
+// us, one way, the other: 37 rows of 128 experts, 768 x 2048, MID 66, LOW 50; 4096 rows MID 266, LOW 257
+enum GatedRows { GATED_TINY, GATED_LOW, GATED_MID, GATED_TALL };
+static inline GatedRows gated_rows_rule(int R, int E, int N)
+{
+    if (R / E >= 96) return GATED_TALL;
+    if (R <= 16 && (long long)(R < E ? R : E) * ceil_div(N, 128) <= 128) return GATED_TINY;
+    return R / E <= 32 ? GATED_LOW : GATED_MID;
+}
+
+// Parts of an expert's rows for the weights' gradients: where even an eighth of a tile each would leave compute units without work, and rows are many.
+static inline int gated_parts(int R, int E, int d, int F, int dtype)
+{
+    const int big = dtype == MOE_F32 ? 128 : 256, slots = dtype == MOE_F32 ? 512 : 256;
+    const long long tiles = (long long)E * ceil_div(d, big) * ceil_div(F, big);
+    long long parts = slots / (4 * tiles);
+    if (parts > R / E / 512) parts = R / E / 512;
+    return parts < 2 ? 1 : parts > 16 ? 16 : (int)parts;
+}
+
+}  // namespace moe

@@ -305,6 +305,8 @@ struct HeadGradArgs {
     bool add;                                  // dh: behind an earlier piece
     float *dh;                                 // [parts, N, d]
     void *dw;
+    int dw_parts, dw_part;                     // dW: rows in so many parts of so many; with more than one their sums go to
+    float *dw_sums;                            // [dw_parts, columns, d]
     const float *largest;
 };
 
@@ -385,19 +387,28 @@ __device__ __forceinline__ void head_dw(const HeadGradArgs &p, char *smem, int n
             int u, m, n;
             do {
                 if (!units.take(u)) return false;
-                product_place(first + u / PARTS, n_m, n_n, tall, m, n);
+                const int big = first + u / PARTS;
+                j.group = big / (n_m * n_n);
+                product_place(big - j.group * n_m * n_n, n_m, n_n, tall, m, n);
                 j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
                 j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
             } while (PARTS > 1 && (j.m0 >= p.columns || j.n0 >= p.d));
+            const int k0 = j.group * p.dw_part;
             j.rows = p.columns - j.m0 < TILE::BM ? p.columns - j.m0 : TILE::BM;
             j.columns = p.d - j.n0 < TILE::BN ? p.d - j.n0 : TILE::BN;
             j.runs = 1;
-            j.k = p.N;
-            j.a[0] = source_across(p.dz, (size_t)(j.m0 / DZ<T>::COLUMNS) * p.N * HEAD_DZ_ROW, lda, j.m0 % DZ<T>::COLUMNS * Z);
-            j.b[0] = source_across(p.h, 0, ldb, j.n0 * Z);
+            j.k = p.N - k0 < p.dw_part ? (p.N - k0 > 0 ? p.N - k0 : 0) : p.dw_part;
+            j.a[0] = source_across(p.dz, ((size_t)(j.m0 / DZ<T>::COLUMNS) * p.N + k0) * HEAD_DZ_ROW, lda, j.m0 % DZ<T>::COLUMNS * Z);
+            j.b[0] = source_across(p.h, (size_t)k0 * ldb, ldb, j.n0 * Z);
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
+            if (p.dw_parts > 1) {
+                const Writer<TILE, float> to(tile, p.dw_sums + ((size_t)j.group * p.columns + j.m0) * p.d + j.n0, p.d * 4, j.rows, j.columns);
+#pragma unroll
+                for (int mb = 0; mb < TILE::MB; ++mb) to.row(mb, sums[0][mb]);
+                return;
+            }
             const Writer<TILE, T> to(tile, (T *)p.dw + (size_t)(p.v0 + j.m0) * p.d + j.n0, p.d * Z, j.rows, j.columns);
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
@@ -414,7 +425,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dw_kernel(HeadG
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     const int n_m = tiles_of(p.columns, Big::BM), n_n = tiles_of(p.d, Big::BN);
-    in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
+    in_rounds<SIZES>(p.dw_parts * n_m * n_n, [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
         head_dw<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
@@ -441,57 +452,73 @@ __global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGr
 }
 
 // ------------------------------------------------------------------------------------------------- rows
-// The largest |dlogprob| of a row that counts; 1 where that is 0 or no number.  One workgroup.
-__global__ __launch_bounds__(1024) void head_largest_kernel(const int32_t *target, const float *dlogprob, int N, int V, float *largest)
+// What the backward calls begin with.  The first workgroup: the largest |dlogprob| of a row that counts; 1 where that is 0 or no number.  The others, with `to`:
+// h with zeros for the padded rows, which may hold anything: what dW's sums are made of.  pieces: of 16 bytes, to a row
+__global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, const float *dlogprob, int N, int V, float *largest, const uint4 *h, int pieces,
+                                                         uint4 *to)
 {
-    __shared__ float waves[16];
+    if (blockIdx.x > 0) {
+        const size_t total = (size_t)N * pieces, step = (size_t)(gridDim.x - 1) * 512;
+        for (size_t i = (size_t)(blockIdx.x - 1) * 512 + threadIdx.x; i < total; i += step) {
+            const int id = target[i / pieces];
+            to[i] = id >= 0 && id < V ? h[i] : make_uint4(0, 0, 0, 0);
+        }
+        return;
+    }
+    __shared__ float waves[8];
     float m = 0.f;
-    for (int i = threadIdx.x; i < N; i += 1024) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < N; i += 512) {
         const int id = target[i];
-        if (id >= 0 && id < V) m = fmaxf(m, fabsf(dlogprob[i]));
+        const float g = fabsf(dlogprob[i]);
+        if (id >= 0 && id < V) m = fmaxf(m, g);
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 16; ++w) m = fmaxf(m, waves[w]);
+        for (int w = 1; w < 8; ++w) m = fmaxf(m, waves[w]);
         *largest = m > 0.f && m < __builtin_inff() ? m : 1.f;
     }
 }
 
-// h with zeros for the padded rows, which may hold anything: what dW's sums are made of.  pieces: of 16 bytes, to a row
-__global__ __launch_bounds__(256) void head_rows_kernel(const uint4 *h, const int32_t *target, int N, int V, int pieces, uint4 *to)
-{
-    const size_t total = (size_t)N * pieces, step = (size_t)gridDim.x * 256;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
-        const int id = target[i / pieces];
-        to[i] = id >= 0 && id < V ? h[i] : make_uint4(0, 0, 0, 0);
-    }
-}
-
+// What they end with: the parts' sums, in their order, times the largest |dlogprob|.  Workgroups 0 .. dh_blocks-1 dh, then dW (a single piece's, in parts), then
+// db.
 template <class T>
-__global__ __launch_bounds__(256) void head_dh_join_kernel(const float *parts, int n_parts, const int32_t *target, int N, int V, int d,
-                                                           const float *largest, T *dh)
+__global__ __launch_bounds__(256) void head_end_kernel(HeadGradArgs p, const int32_t *target, int V, T *dh, int dh_blocks, int dw_blocks, const float *db_sums,
+                                                       int db_parts, float *db)
 {
-    const size_t total = (size_t)N * d, step = (size_t)gridDim.x * 1024;
-    const float scale = *largest;
-    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < total; i += step) {
-        const int id = target[i / d];
-        product_f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if (id >= 0 && id < V)
-            for (int s = 0; s < n_parts; ++s) v += *reinterpret_cast<const product_f32x4 *>(parts + s * total + i);
-        store4(dh + i, v * scale);
+    const float scale = *p.largest;
+    int block = blockIdx.x;
+    if (block < dh_blocks) {
+        const size_t total = (size_t)p.N * p.d;
+        for (size_t i = ((size_t)block * 256 + threadIdx.x) * 4; i < total; i += (size_t)dh_blocks * 1024) {
+            const int id = target[i / p.d];
+            product_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            if (id >= 0 && id < V)
+                for (int s = 0; s < p.parts; ++s) v += *reinterpret_cast<const product_f32x4 *>(p.dh + s * total + i);
+            store4(dh + i, v * scale);
+        }
+        return;
     }
-}
-
-__global__ __launch_bounds__(256) void head_db_kernel(const float *parts, int n_parts, int V, const float *largest, float *db)
-{
-    const int v = blockIdx.x * 256 + threadIdx.x;
-    if (v >= V) return;
+    block -= dh_blocks;
+    if (block < dw_blocks) {
+        const size_t total = (size_t)p.columns * p.d;
+        for (size_t i = ((size_t)block * 256 + threadIdx.x) * 4; i < total; i += (size_t)dw_blocks * 1024) {
+            product_f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            for (int s = 0; s < p.dw_parts; ++s) v += *reinterpret_cast<const product_f32x4 *>(p.dw_sums + s * total + i);
+            store4((T *)p.dw + (size_t)p.v0 * p.d + i, v * scale);
+        }
+        return;
+    }
+    const int v = (block - dw_blocks) * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;      // four wavefronts share a column's parts
+    __shared__ double quarter[4][64];
     double s = 0.;
-    for (int i = 0; i < n_parts; ++i) s += parts[(size_t)i * V + v];
-    db[v] = (float)(s * *largest);
+    for (int i = w; v < V && i < db_parts; i += 4) s += db_sums[(size_t)i * V + v];
+    quarter[w][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (w == 0 && v < V) db[v] = (float)((((quarter[0][threadIdx.x] + quarter[1][threadIdx.x]) + quarter[2][threadIdx.x]) + quarter[3][threadIdx.x]) * scale);
 }
 
 __global__ __launch_bounds__(256) void head_clear_kernel(unsigned *p, size_t words)
@@ -603,19 +630,19 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     p.largest = largest;
     p.dz = ws + g.dz_at;
     p.db = db ? db_parts : nullptr;
-    hipLaunchKernelGGL(head_largest_kernel, dim3(1), dim3(1024), 0, st, p.target, p.dlogprob, N, p.V, largest);
     const int pieces = p.d * (int)sizeof(T) / 16;
-    if (dw)
-        hipLaunchKernelGGL(head_rows_kernel, dim3((int)((size_t)N * pieces / 256 < 4096 ? (size_t)N * pieces / 256 + 1 : 4096)), dim3(256), 0, st,
-                           (const uint4 *)p.h, p.target, N, p.V, pieces, (uint4 *)(ws + g.rows_at));
+    auto blocks_for = [](size_t work, size_t each) { return (int)(work / each < 2048 ? work / each + 1 : 2048); };
+    hipLaunchKernelGGL(head_begin_kernel, dim3(1 + (dw ? blocks_for((size_t)N * pieces, 512) : 0)), dim3(512), 0, st, p.target, p.dlogprob, N, p.V, largest,
+                       (const uint4 *)p.h, pieces, (uint4 *)(ws + g.rows_at));
+    HeadGradArgs q = {};
     for (int v0 = 0; v0 < p.V; v0 += g.piece) {
         p.v0 = v0;
         p.columns = p.V - v0 < g.piece ? p.V - v0 : g.piece;
         HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
-        HeadGradArgs q = {};
         q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.v0 = v0;
         q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), DZ<T>::COLUMNS), q.add = v0 > 0;
         q.dh = dh_parts, q.dw = dw, q.largest = largest;
+        q.dw_parts = g.dw_parts, q.dw_part = (int)align_up(tiles_of(N, g.dw_parts), 64), q.dw_sums = (float *)(ws + g.dw_at);
         if (dh && dw && g.paired) {
             typedef DhParts<T> sizes;
             hipLaunchKernelGGL((head_pair_kernel<sizes, Sizes<T, ACROSS_K, ACROSS_K>>), dim3(PRODUCT_CUS * sizes::PER_CU),
@@ -627,14 +654,15 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
             typedef Sizes<T, ACROSS_K, ACROSS_K> sizes;
             typedef typename Whole<sizes>::Tile big;
             hipLaunchKernelGGL((head_dw_kernel<sizes>),
-                               dim3(product_grid((long long)tiles_of(p.columns, big::BM) * tiles_of(p.d, big::BN), PRODUCT_CUS * sizes::PER_CU)),
+                               dim3(product_grid((long long)g.dw_parts * tiles_of(p.columns, big::BM) * tiles_of(p.d, big::BN), PRODUCT_CUS * sizes::PER_CU)),
                                dim3(big::THREADS), 0, st, q, 8);
         }
     }
-    if (dh)
-        hipLaunchKernelGGL(head_dh_join_kernel<T>, dim3((int)((size_t)N * p.d / 1024 < 4096 ? (size_t)N * p.d / 1024 + 1 : 4096)), dim3(256), 0, st,
-                           dh_parts, g.parts, p.target, N, p.V, p.d, largest, dh);
-    if (db) hipLaunchKernelGGL(head_db_kernel, dim3(tiles_of(p.V, 256)), dim3(256), 0, st, db_parts, g.db_rows, p.V, largest, db);
+    const int dh_blocks = dh ? blocks_for((size_t)N * p.d, 1024) : 0, dw_blocks = dw && g.dw_parts > 1 ? blocks_for((size_t)q.columns * p.d, 1024) : 0;
+    const int db_blocks = db ? tiles_of(p.V, 64) : 0;
+    if (dh_blocks + dw_blocks + db_blocks)
+        hipLaunchKernelGGL(head_end_kernel<T>, dim3(dh_blocks + dw_blocks + db_blocks), dim3(256), 0, st, q, p.target, p.V, dh, dh_blocks, dw_blocks, db_parts,
+                           g.db_rows, db);
 }
 
 int head_check(const char *who, int N, int d, int V, int dtype)

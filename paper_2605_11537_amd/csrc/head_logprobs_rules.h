@@ -27,9 +27,10 @@ static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dt
 struct HeadShape {
     int piece;                                 // ids of the vocabulary whose dz is in memory at a time
     int parts;                                 // of a piece's sum for dh
+    int dw_parts;                              // of the rows in dW's sum (one piece only)
     bool paired;                               // dh and dW share a launch
     int db_rows;                               // rows of partial sums for db
-    size_t rows_at, dz_at, dh_at, db_at, bytes;
+    size_t rows_at, dz_at, dh_at, db_at, dw_at, bytes;
 };
 static inline HeadShape head_shape(int N, int d, int V, int dtype)
 {
@@ -55,12 +56,17 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
             g.parts = s;
         }
     }
+    // dW alone: parts where even an eighth of a tile each would leave compute units without work, and rows are many
+    long long dw_parts = pieces == 1 && !g.paired ? slots / (4 * of_dw) : 1;
+    if (dw_parts > N / 512) dw_parts = N / 512;
+    g.dw_parts = dw_parts < 2 ? 1 : dw_parts > 16 ? 16 : (int)dw_parts;
     g.db_rows = ceil_div(N, head_wave_rows(N, dtype));
     g.rows_at = 256;
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
     g.dh_at = g.dz_at + (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW);
     g.db_at = g.dh_at + align_up((size_t)g.parts * N * d * 4, 256);
-    g.bytes = g.db_at + align_up((size_t)g.db_rows * V * 4, 256);
+    g.dw_at = g.db_at + align_up((size_t)g.db_rows * V * 4, 256);
+    g.bytes = g.dw_at + (g.dw_parts > 1 ? align_up((size_t)g.dw_parts * V * d * 4, 256) : 0);
     return g;
 }
 

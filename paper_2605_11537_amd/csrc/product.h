@@ -347,13 +347,21 @@ struct Tile {
     template <int STORES>
     __device__ __forceinline__ static void wait(int pending, bool behind)
     {
-#define MOE_PRODUCT_WAIT(N) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory")
-        if (STAGES > 4 && pending > 3) MOE_PRODUCT_WAIT(3 * LOADS);
-        else if (STAGES > 3 && pending > 2) MOE_PRODUCT_WAIT(2 * LOADS);
-        else if (STAGES > 2 && pending > 1) MOE_PRODUCT_WAIT(LOADS);
-        else if (STORES > 0 && behind) MOE_PRODUCT_WAIT(STORES < 63 ? STORES : 63);
-        else MOE_PRODUCT_WAIT(0);
-#undef MOE_PRODUCT_WAIT
+        if (younger<STAGES - 2>(pending)) return;
+        if (STORES > 0 && behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(STORES < 63 ? STORES : 63) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    // N or more stages are younger than the oldest
+    template <int N>
+    __device__ __forceinline__ static bool younger(int pending)
+    {
+        if constexpr (N > 0) {
+            static_assert(N * LOADS < 64, "what the counter holds");
+            if (pending <= N) return younger<N - 1>(pending);
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N * LOADS) : "memory");
+            return true;
+        }
+        return false;
     }
 
     // next(job) -> whether there is one; finish(job, sums) writes a tile.  Both are reached by the whole workgroup.

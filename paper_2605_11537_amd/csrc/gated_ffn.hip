@@ -430,27 +430,23 @@ void launch_pair(const GatedArgs &p, hipStream_t st)
 template <class T>
 void backward(const GatedArgs &p, hipStream_t st)
 {
-    // tiles of the largest size in a pair's two products
-    typedef typename Whole<Sizes<T, ACROSS_K, ACROSS_K>>::Tile big;
-    const long long of_rows = ((long long)p.R / big::BM + 1), of_weights = (long long)p.E * tiles_of(p.d, big::BM);
-    const bool many = (of_rows + of_weights) * tiles_of(p.F, big::BN) >= 2 * PRODUCT_CUS * Sizes<T, ACROSS_K, ACROSS_K>::PER_CU;
-    if (gated_rows_rule(p.R, p.E, p.F) == GATED_TALL && many && p.dx && p.dw_gate && p.dw_down) {
-        GatedArgs q = p;
-        q.parts = 1;
-        launch_pair<GATED_DHIDDEN, T>(q, st);
-        launch_pair<GATED_DX, T>(q, st);
-        return;
-    }
+    const int dtype = sizeof(T) == 4 ? MOE_F32 : MOE_BF16;
+    GatedArgs q = p;
+    q.parts = 1;
+    const bool with_dh = p.dw_down && p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, true);
+    const bool with_dx = p.dw_gate && p.dx && p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, false);
     if (p.R > 0) {                             // else zeros for every weight
-        launch_step<GATED_DHIDDEN, T>(p, st);
-        if (p.dx) launch_step<GATED_DX, T>(p, st);
+        if (with_dh) launch_pair<GATED_DHIDDEN, T>(q, st);
+        else launch_step<GATED_DHIDDEN, T>(p, st);
+        if (with_dx) launch_pair<GATED_DX, T>(q, st);
+        else if (p.dx) launch_step<GATED_DX, T>(p, st);
     }
-    if (p.dw_gate) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
-    if (p.dw_down) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
+    if (p.dw_gate && !with_dx) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
+    if (p.dw_down && !with_dh) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
     if (p.parts > 1) {
         const size_t all = (size_t)p.E * p.d * p.F;
-        hipLaunchKernelGGL(gated_join_kernel<T>, dim3((unsigned)(all / 1024 < 1024 ? all / 1024 + 1 : 1024), 3), dim3(256), 0, st, p.sums, p.parts, all, (T *)p.dw_gate,
-                           (T *)p.dw_up, (T *)p.dw_down);
+        hipLaunchKernelGGL(gated_join_kernel<T>, dim3((unsigned)(all / 1024 < 1024 ? all / 1024 + 1 : 1024), 3), dim3(256), 0, st, p.sums, p.parts, all,
+                           with_dx ? nullptr : (T *)p.dw_gate, with_dx ? nullptr : (T *)p.dw_up, with_dh ? nullptr : (T *)p.dw_down);
     }
 }
 

@@ -22,7 +22,7 @@ enum GatedRows { GATED_TINY, GATED_LOW, GATED_MID, GATED_TALL };
 static inline GatedRows gated_rows_rule(int R, int E, int N)
 {
     if (R / E >= 96) return GATED_TALL;
-    if (R <= 16 && (long long)(R < E ? R : E) * ceil_div(N, 128) <= 128) return GATED_TINY;
+    if (R <= 16ll * E && (long long)(R < E ? R : E) * ceil_div(N, 128) <= 128) return GATED_TINY;
     return R / E <= 32 ? GATED_LOW : GATED_MID;
 }
 
@@ -34,6 +34,15 @@ static inline int gated_parts(int R, int E, int d, int F, int dtype)
     long long parts = slots / (4 * tiles);
     if (parts > R / E / 512) parts = R / E / 512;
     return parts < 2 ? 1 : parts > 16 ? 16 : (int)parts;
+}
+
+// Whether two products share a launch: tiles of rows (n1, of cost1 stages) and of weights.  One tile must not take longer than all of the work does.
+static inline bool gated_pairs(int R, int E, int d, int F, int dtype, bool down)
+{
+    const int big = dtype == MOE_F32 ? 128 : 256, stage = dtype == MOE_F32 ? 32 : 64, slots = dtype == MOE_F32 ? 512 : 256;
+    const double n1 = ((double)R / big + E / 2) * ceil_div(down ? F : d, big), cost1 = down ? d / stage + 20 : 2.0 * F / stage + 4;
+    const double n2 = (double)E * ceil_div(d, big) * ceil_div(down ? F : 2 * F, big), cost2 = (double)R / E / stage + 5;
+    return gated_rows_rule(R, E, F) == GATED_TALL && n1 * cost1 + n2 * cost2 >= 0.95 * slots * (cost1 > cost2 ? cost1 : cost2);
 }
 
 }  // namespace moe

@@ -100,10 +100,12 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
         [&](const Job &j, typename TILE::Sums &z) {
             add_bias(tile, j, p.b, p.V, z);
             const int lane = threadIdx.x & 63;
+            int targets[TILE::MB];
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) targets[mb] = tile.of_row(mb) < j.rows ? p.target[j.m0 + tile.of_row(mb)] : -1;
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                const int target = row < j.rows ? p.target[j.m0 + row] : -1;
+                const int row = tile.of_row(mb), target = targets[mb];
                 float m = HEAD_NONE;
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
@@ -233,17 +235,24 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
             add_bias(tile, j, p.b, p.V, z);
             const int at = j.n0 - p.v0;        // behind the last id there are zeros up to the tile's end
             const Writer<TILE, T> to(tile, (T *)p.dz + ((size_t)(at / DZ<T>::COLUMNS) * p.N + j.m0) * DZ<T>::COLUMNS + at % DZ<T>::COLUMNS, HEAD_DZ_ROW, j.rows, TILE::BN);
+            // what the rows need, asked for at once
+            int targets[TILE::MB];
+            float weights[TILE::MB], lses[TILE::MB];
+#pragma unroll
+            for (int mb = 0; mb < TILE::MB; ++mb) {
+                const int row = j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0);
+                targets[mb] = p.target[row];
+                weights[mb] = p.dlogprob[row];
+                lses[mb] = p.lse[row];
+            }
             product_f32x4 down[TILE::NB];      // sums over this lane's rows
 #pragma unroll
             for (int nb = 0; nb < TILE::NB; ++nb) down[nb] = product_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
-                const int row = tile.of_row(mb);
-                const bool there = row < j.rows;
-                const int target = there ? p.target[j.m0 + row] : -1;
+                const int target = tile.of_row(mb) < j.rows ? targets[mb] : -1;
                 const bool on = target >= 0 && target < p.V;
-                const float g = on ? p.dlogprob[j.m0 + row] / largest : 0.f;
-                const float lse = on ? finite_or(p.lse[j.m0 + row], 0.f) : 0.f;
+                const float g = on ? weights[mb] / largest : 0.f, lse = on ? finite_or(lses[mb], 0.f) : 0.f;
                 product_f32x4 dz[TILE::NB];
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
@@ -265,9 +274,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float s = down[nb][i];
-#pragma unroll
-                        for (int o = 1; o < 16; o <<= 1) s += __shfl_xor(s, o, 64);
+                        const float s = sum_over<16>(down[nb][i]);
                         const int v = j.n0 + tile.of_column(nb) + i;
                         // a slot for a wavefront's rows, of which all tiles of the launch have the same number
                         if ((threadIdx.x & 15) == 0 && v < p.V && j.m0 + tile.wm * TILE::WAVE_M < p.N)
@@ -546,11 +553,13 @@ template <>
 struct RowParts<bf16_t> : Sizes<bf16_t, ALONG_K, ALONG_K> {
     typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 64, 256, 2, 4, 1, 3>> Quarter;
     typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 32, 256, 2, 4, 1, 4>> Eighth;
+    typedef Eighth Sixteenth;
 };
 template <>
 struct RowParts<float> : Sizes<float, ALONG_K, ALONG_K> {
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 32, 128, 2, 2, 1, 3>> Quarter;
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 16, 128, 1, 4, 1, 4>> Eighth;
+    typedef Eighth Sixteenth;
 };
 template <class T>
 struct ColumnParts;
@@ -559,12 +568,14 @@ struct ColumnParts<bf16_t> : Sizes<bf16_t, ALONG_K, ALONG_K> {
     typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 256, 128, 2, 4, 1, 3>> Half;
     typedef Sized<Tile<bf16_t, ALONG_K, ALONG_K, 256, 64, 2, 4, 1, 3>> Quarter;
     typedef Quarter Eighth;
+    typedef Quarter Sixteenth;
 };
 template <>
 struct ColumnParts<float> : Sizes<float, ALONG_K, ALONG_K> {
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 128, 64, 2, 2, 1, 3>> Half;
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 128, 32, 2, 2, 1, 3>> Quarter;
     typedef Quarter Eighth;
+    typedef Quarter Sixteenth;
 };
 // dh: A in dz's blocks
 template <class T>
@@ -574,7 +585,8 @@ struct DhParts<bf16_t> {
     typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 256, 256, 2, 4, 1, 2, DZ<bf16_t>::COLUMNS>> Whole;
     typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 256, 2, 4, 1, 3, DZ<bf16_t>::COLUMNS>> Half;
     typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 128, 2, 4, 1, 4, DZ<bf16_t>::COLUMNS>> Quarter;
-    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 64, 4, 2, 1, 5, DZ<bf16_t>::COLUMNS>> Eighth;
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 128, 64, 4, 2, 1, 6, DZ<bf16_t>::COLUMNS>> Eighth;
+    typedef Sized<Tile<bf16_t, ALONG_K, ACROSS_K, 64, 64, 4, 2, 1, 8, DZ<bf16_t>::COLUMNS>> Sixteenth;
     static constexpr int PER_CU = 1;
 };
 template <>
@@ -582,7 +594,8 @@ struct DhParts<float> {
     typedef Sized<Tile<float, ALONG_K, ACROSS_K, 128, 128, 2, 2, 1, 2, DZ<float>::COLUMNS>> Whole;
     typedef Sized<Tile<float, ALONG_K, ACROSS_K, 64, 128, 2, 2, 1, 3, DZ<float>::COLUMNS>> Half;
     typedef Sized<Tile<float, ALONG_K, ACROSS_K, 64, 64, 2, 2, 1, 4, DZ<float>::COLUMNS>> Quarter;
-    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 32, 64, 2, 2, 1, 5, DZ<float>::COLUMNS>> Eighth;
+    typedef Sized<Tile<float, ALONG_K, ACROSS_K, 32, 64, 2, 2, 1, 6, DZ<float>::COLUMNS>> Eighth;
+    typedef Eighth Sixteenth;
     static constexpr int PER_CU = 2;
 };
 
@@ -600,7 +613,7 @@ dim3 few_grid(long long units, int more_lds)
         typedef typename Whole<sizes>::Tile big;                                                                                               \
         typedef Flat<T, A, B> flat;                                                                                                            \
         typedef Few<T, A, B> few;                                                                                                              \
-        const HeadRows rows = head_rows(M);                                                                                                    \
+        const HeadRows rows = head_rows(M, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);                                                                                                   \
         if (rows == HEAD_TALL_TILES)                                                                                                           \
             hipLaunchKernelGGL((KERNEL##_kernel<sizes>),                                                                                       \
                                dim3(product_grid((long long)TIMES * tiles_of(M, big::BM) * tiles_of(N, big::BN), PRODUCT_CUS * sizes::PER_CU)), \

@@ -11,17 +11,18 @@ constexpr int HEAD_DZ_ROW = 512;               // bytes of a row of dz in one of
 constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 
 enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
-static inline HeadRows head_rows(int N) { return N <= 16 ? HEAD_FEW_TILES : N <= 128 ? HEAD_FLAT_TILES : HEAD_TALL_TILES; }
+// (binary32 is bound by the matrix pipes: 192 rows are three tiles of 64, of 128 two with a quarter of nothing)
+static inline HeadRows head_rows(int N, int dtype) { return N <= 16 ? HEAD_FEW_TILES : N <= (dtype == MOE_F32 ? 192 : 128) ? HEAD_FLAT_TILES : HEAD_TALL_TILES; }
 static inline int head_tile_rows(int N, int dtype)
 {
-    const HeadRows r = head_rows(N);
+    const HeadRows r = head_rows(N, dtype);
     return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : 256;
 }
-static inline int head_tile_columns(int N, int dtype) { return head_rows(N) != HEAD_TALL_TILES ? HEAD_FEW_COLUMNS : dtype == MOE_F32 ? 128 : 256; }
+static inline int head_tile_columns(int N, int dtype) { return head_rows(N, dtype) != HEAD_TALL_TILES ? HEAD_FEW_COLUMNS : dtype == MOE_F32 ? 128 : 256; }
 // forward: slots of maximum and sum that a row has, one for a tile's columns
 static inline int head_row_slots(int N, int V, int dtype) { return ceil_div(V, head_tile_columns(N, dtype)); }
 // backward: rows of a wavefront, for which the bias has a slot of partial sums
-static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dtype) / (head_rows(N) == HEAD_TALL_TILES ? 2 : 1); }
+static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dtype) / (head_rows(N, dtype) == HEAD_TALL_TILES ? 2 : 1); }
 
 // The gradient's pieces and workspace.
 struct HeadShape {
@@ -44,7 +45,8 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     // tiles are as many as compute units, the parts fill what is left of the last round: about half a part's time is lost.  Alone: whole rounds.
     const int rows = head_tile_rows(N, dtype), columns = head_tile_columns(N, dtype), slots = dtype == MOE_F32 ? 512 : 256;
     const long long tiles = (long long)ceil_div(N, rows) * ceil_div(d, columns), of_dw = (long long)ceil_div(g.piece, rows) * ceil_div(d, columns);
-    g.paired = head_rows(N) == HEAD_TALL_TILES && of_dw + tiles * 2 >= slots;
+    // (a tile of dW must not take longer than all of the work does)
+    g.paired = head_rows(N, dtype) == HEAD_TALL_TILES && of_dw * (N + 256.0) + tiles * (g.piece + 384.0) >= slots * (N + 256.0);
     double best = 0;
     g.parts = 1;
     for (int s = 1; s <= 64; ++s) {

@@ -602,8 +602,8 @@ struct Shares {
     }
 };
 
-// A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half, a quarter or an eighth of that
-// size, if one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.
+// A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half down to a sixteenth of that size, as
+// one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.
 // run(tile type, first unit, past the last)
 template <class SIZES, class Run>
 __device__ __forceinline__ void in_rounds(int units, Run &&run)
@@ -614,7 +614,8 @@ __device__ __forceinline__ void in_rounds(int units, Run &&run)
     if (whole > 0) __syncthreads();            // the buffers change their sizes
     if (4 * rest > grid) run(typename SIZES::Half(), whole, units);
     else if (8 * rest > grid) run(typename SIZES::Quarter(), whole, units);
-    else run(typename SIZES::Eighth(), whole, units);
+    else if (16 * rest > grid) run(typename SIZES::Eighth(), whole, units);
+    else run(typename SIZES::Sixteenth(), whole, units);
 }
 template <class TILE>
 struct Sized {
@@ -627,7 +628,8 @@ struct Sizes<bf16_t, A, B, HALVES> {
     typedef Sized<Tile<bf16_t, A, B, 256, 256, 2, 4, HALVES>> Whole;
     typedef Sized<Tile<bf16_t, A, B, 128, 256, 2, 4, HALVES, 3>> Half;
     typedef Sized<Tile<bf16_t, A, B, 128, 128, 2, 4, HALVES, 4>> Quarter;
-    typedef Sized<Tile<bf16_t, A, B, 128, 64, 4, 2, HALVES, 5>> Eighth;
+    typedef Sized<Tile<bf16_t, A, B, 128, 64, 4, 2, HALVES, 6>> Eighth;
+    typedef Sized<Tile<bf16_t, A, B, 64, 64, 4, 2, HALVES, 8>> Sixteenth;
     static constexpr int PER_CU = 1;
 };
 template <Order A, Order B, int HALVES>
@@ -635,7 +637,8 @@ struct Sizes<float, A, B, HALVES> {
     typedef Sized<Tile<float, A, B, 128, 128, 2, 2, HALVES>> Whole;
     typedef Sized<Tile<float, A, B, 64, 128, 2, 2, HALVES, 3>> Half;
     typedef Sized<Tile<float, A, B, 64, 64, 2, 2, HALVES, 4>> Quarter;
-    typedef Sized<Tile<float, A, B, 32, 64, 2, 2, HALVES, 5>> Eighth;
+    typedef Sized<Tile<float, A, B, 32, 64, 2, 2, HALVES, 6>> Eighth;
+    typedef Eighth Sixteenth;
     static constexpr int PER_CU = 2;
 };
 template <class SIZES>
@@ -645,7 +648,7 @@ struct Whole {
 };
 
 __host__ __device__ constexpr int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }
-constexpr int PRODUCT_CUS = 256, PRODUCT_PARTS = 8;
+constexpr int PRODUCT_CUS = 256, PRODUCT_PARTS = 16;
 // workgroups for at most so many units of the largest size
 static inline int product_grid(long long units, int resident)
 {

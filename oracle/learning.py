@@ -7,17 +7,26 @@ instead of half of one).
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
-from math import erf
 
 STEP = 2.0 ** -23
-_erf = np.vectorize(erf, otypes=[float])
+_erf = np.vectorize(math.erf, otypes=[float])
+
+
+def _of(v):
+    """numpy, or torch where the values are its (float64) tensors: for sizes that take too long here."""
+    if isinstance(v, (np.ndarray, float, int)):
+        return np
+    import torch
+    return torch
 
 
 class Bounded:
     def __init__(self, value, off=0.0):
-        self.value = np.asarray(value, dtype=np.float64)
-        self.off = np.broadcast_to(np.asarray(off, dtype=np.float64), self.value.shape)
+        self.value = np.asarray(value, dtype=np.float64) if _of(value) is np else value
+        self.off = off + 0.0 * _of(self.value).abs(_of(self.value).nan_to_num(self.value)) if isinstance(off, float) else off
 
     @property
     def T(self):
@@ -25,45 +34,47 @@ class Bounded:
 
     def __add__(self, o):
         v = self.value + o.value
-        return Bounded(v, self.off + o.off + STEP * np.abs(v))
+        return Bounded(v, self.off + o.off + STEP * abs(v))
 
     def __mul__(self, o):
         v = self.value * o.value
-        off = np.abs(self.value) * o.off + self.off * np.abs(o.value) + self.off * o.off
-        return Bounded(v, off + STEP * (np.abs(v) + off))
+        off = abs(self.value) * o.off + self.off * abs(o.value) + self.off * o.off
+        return Bounded(v, off + STEP * (abs(v) + off))
 
     def __matmul__(self, o):
-        a, b = np.abs(self.value), np.abs(o.value)
+        a, b = abs(self.value), abs(o.value)
         off = a @ o.off + self.off @ b + self.off @ o.off
         return Bounded(self.value @ o.value, off + (self.value.shape[1] + 4) * STEP * (a @ b + off))
 
     def rounded(self, half):
-        return Bounded(self.value, self.off + half * (np.abs(self.value) + self.off))
+        return Bounded(self.value, self.off + half * (abs(self.value) + self.off))
 
 
 def sigmoid(z):
-    e = np.exp(-np.abs(z))
-    return np.where(z >= 0, 1.0 / (1.0 + e), e / (1.0 + e))
+    xp = _of(z)
+    e = xp.exp(-abs(z))
+    return xp.where(z >= 0, 1.0 / (1.0 + e), e / (1.0 + e))
 
 
 def activation(name, g):
     """act(g) and act'(g) of a Bounded g."""
-    v, off = g.value, g.off
+    v, off, xp = g.value, g.off, _of(g.value)
     if name == "silu":
         s = sigmoid(v)
-        rel = (np.abs(v) + 8) * STEP                                 # the exponent's product and the reciprocal
+        rel = (abs(v) + 8) * STEP                                    # the exponent's product and the reciprocal
         # slopes at most 1.1 and 0.5
-        return (Bounded(v * s, 1.1 * off + rel * np.abs(v * s)),
-                Bounded(s * (1 + v * (1 - s)), 0.5 * off + 2 * rel * s * (1 + np.abs(v))))
+        return (Bounded(v * s, 1.1 * off + rel * abs(v * s)),
+                Bounded(s * (1 + v * (1 - s)), 0.5 * off + 2 * rel * s * (1 + abs(v))))
     if name == "gelu":
-        phi, bell = 0.5 * (1 + _erf(v * np.sqrt(0.5))), np.exp(-0.5 * v * v)
+        erf = _erf if xp is np else xp.erf
+        phi, bell = 0.5 * (1 + erf(v * math.sqrt(0.5))), xp.exp(-0.5 * v * v)
         rel = (v * v + 8) * STEP
         phi_off = 1.5e-7 + 4 * STEP * phi + rel * bell               # the published bound of the rational form, its evaluation, its exponential
         # slopes at most 1.13 and 0.8
-        return (Bounded(v * phi, 1.13 * off + np.abs(v) * phi_off),
-                Bounded(phi + v * bell / np.sqrt(2 * np.pi), 0.8 * off + phi_off + np.abs(v) * bell * rel))
-    on = (v > 0).astype(np.float64)
-    return Bounded(v * on, off), Bounded(on, (np.abs(v) <= off).astype(np.float64) * (off > 0))
+        return (Bounded(v * phi, 1.13 * off + abs(v) * phi_off),
+                Bounded(phi + v * bell / math.sqrt(2 * math.pi), 0.8 * off + phi_off + abs(v) * bell * rel))
+    on = (v > 0) * (1.0 + 0.0 * xp.nan_to_num(v))
+    return Bounded(v * on, off), Bounded(on, ((abs(v) <= off) & (off > 0)) * (1.0 + 0.0 * off))
 
 
 def gated_ffn(x, w_gate, w_up, w_down, act, half, dy=None):
@@ -90,7 +101,7 @@ def head_logprobs(h, w, b, target, half, dlogprob=None):
     bias = np.zeros(V) if b is None else b
     masked = np.isneginf(bias)
     value = np.where(masked, -np.inf, z.value + np.where(masked, 0.0, bias))
-    off = np.where(masked, 0.0, z.off + STEP * np.abs(np.where(masked, 0.0, value)))
+    off = np.where(masked, 0.0, z.off + STEP * abs(np.where(masked, 0.0, value)))
     m = value.max(1, keepdims=True)
     none = np.isneginf(m)
     m0 = np.where(none, 0.0, m)
@@ -103,23 +114,23 @@ def head_logprobs(h, w, b, target, half, dlogprob=None):
     with np.errstate(invalid="ignore"):
         far = np.where(p > 0, (m0 - value) + 8, 0.0)
     rel = (p * (1.01 * off + far * STEP)).sum(1, keepdims=True) + (64 + V / 4096) * STEP + 1e-12
-    lse_off = rel + 2 * STEP * np.abs(np.where(none, 0.0, lse))
+    lse_off = rel + 2 * STEP * abs(np.where(none, 0.0, lse))
     at = np.clip(target, 0, V - 1)[:, None]
     zt = np.take_along_axis(value, at, 1)
     gone = np.isneginf(zt)
     lp = np.where(gone, -np.inf, np.where(gone, 0.0, zt) - np.where(none, 0.0, lse))
-    lp_off = np.where(gone, 0.0, np.take_along_axis(off, at, 1) + rel + 4 * STEP * (np.abs(np.where(gone, 0.0, zt - m0)) + np.abs(np.where(none, 0.0, lse - m0))))
+    lp_off = np.where(gone, 0.0, np.take_along_axis(off, at, 1) + rel + 4 * STEP * (abs(np.where(gone, 0.0, zt - m0)) + abs(np.where(none, 0.0, lse - m0))))
     out = dict(logprob=Bounded(np.where(on, lp[:, 0], 0.0), np.where(on, lp_off[:, 0], 0.0)), lse=Bounded(lse[:, 0], lse_off[:, 0]))
     if dlogprob is not None:
         counts = on & np.isfinite(dlogprob) & (dlogprob != 0)
-        top = np.abs(dlogprob[counts]).max() if counts.any() else 1.0
+        top = abs(dlogprob[counts]).max() if counts.any() else 1.0
         g = np.where(on, dlogprob, 0.0)[:, None] / top
         with np.errstate(invalid="ignore"):
-            gap = np.where(p > 0, np.abs(value - np.where(none, 0.0, lse)) + 8, 0.0)
+            gap = np.where(p > 0, abs(value - np.where(none, 0.0, lse)) + 8, 0.0)
         p_off = 1.01 * p * (off + lse_off + gap * STEP)
         hit = np.zeros((N, V))
         np.put_along_axis(hit, at, 1.0, 1)
-        dz = Bounded(g, np.abs(g) * STEP) * Bounded(hit - p, p_off + STEP)
+        dz = Bounded(g, abs(g) * STEP) * Bounded(hit - p, p_off + STEP)
         dzr = dz.rounded(half)
         scale = Bounded(np.full((1, 1), top), 0.0)
         clean = np.where(on[:, None], h, 0.0)

@@ -532,6 +532,7 @@ extern "C" int moe_gated_ffn_backward(const void *dy, const void *x, const int32
     const size_t need = moe_gated_ffn_backward_workspace_bytes(R, E, d, F, dtype);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
                 "moe_gated_ffn_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
+    if (!dw_gate && !dw_down && (!dx || R == 0)) return MOE_OK;        // nothing is wanted
     GatedArgs p = {};
     p.x = x, p.w_gate = w_gate, p.w_up = w_up, p.w_down = w_down, p.dy = dy, p.offset = expert_offset;
     p.R = R, p.E = E, p.d = d, p.F = F, p.activation = activation;

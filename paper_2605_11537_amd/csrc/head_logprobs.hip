@@ -738,6 +738,7 @@ extern "C" int moe_head_logprobs_backward(const void *h, const void *w_head, con
                 MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: an output aliases another tensor");
     MOE_REQUIRE(aligned16(h) && aligned16(w_head) && aligned16(dh) && aligned16(dw_head), MOE_ERR_INVALID_ARG,
                 "moe_head_logprobs_backward: tensor misaligned");
+    if (!dw_head && !db_head && (!dh || N == 0)) return MOE_OK;        // nothing is wanted
     hipStream_t st = (hipStream_t)stream;
     if (N == 0) {                              // sums over nothing
         if (dw_head) launch_clear(dw_head, (size_t)V * d * (dtype == MOE_F32 ? 4 : 2), st);

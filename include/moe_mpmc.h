@@ -446,13 +446,13 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  * [V] binary32 or NULL, h [N, d], target [N]:
  *     z = h w_head^T + b_head  (binary32);   lse = log sum exp(z);   logprob = z[target] - lse  (0 for a target outside [0,V): a padded position)
  * A bias of -infinity masks its id, as long as its product is finite; where all are masked, lse and logprob are -infinity.  A NaN or +infinity among
- * a row's logits makes its numbers NaN.  d a multiple of 8 up to 2^20, V up to 2^24, N up to 2^24, any V and N.
+ * a row's logits makes its numbers NaN.  d a multiple of 8 up to 2^20; any V and N up to 2^24, with N V below 2^41, d V below 2^42 and N d below 2^34.
  *
  * moe_head_logprobs_backward -- from dlogprob [N], with the lse that the forward wrote:
  *     dz = dlogprob ([v = target] - exp(z - lse)), 0 at padded positions whatever h holds there;
  *     dh = dz w_head,   dw_head = dz^T h,   db_head = sum of dz over the rows  (binary32)
- * The logits are made again, in pieces of the vocabulary: the workspace grows with N times a piece, about 512 MiB of dz at most (256 ids for very
- * large N) and as much of sums.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
+ * The logits are made again, in pieces of the vocabulary: the workspace holds N times a piece, 1 GiB of dz at most (256 ids for very
+ * large N), as much of sums and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
  * N = 0 dw_head and db_head are zeros.  Sums in binary32 in an order that the sizes fix.
  */
 size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype);

@@ -213,10 +213,10 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
 {
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
-    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, Big::BM};
+    __shared__ int tables[3][MAX_GROUPS + 1];
+    const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, Big::BM};
     tiles.count();
-    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, Big::HALF_N);
+    const int n_m = __builtin_amdgcn_readfirstlane(tiles.prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, Big::HALF_N);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
         constexpr int parts = Big::BM / Part::BM * (Big::HALF_N / Part::HALF_N);
@@ -229,10 +229,10 @@ template <int STEP, class TILE>
 __global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedArgs p)
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
-    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, TILE::BM};
+    __shared__ int tables[3][MAX_GROUPS + 1];
+    const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, TILE::BM};
     tiles.count();
-    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
+    const int n_m = __builtin_amdgcn_readfirstlane(tiles.prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
     gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N>(p, tiles, smem, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
@@ -242,11 +242,10 @@ __host__ __device__ constexpr int gated_weights_share(int tiles) { return (tiles
 
 // DOWN: dW_down = h^T dy, F x d; else dW_gate and dW_up = x^T [dg | du], d x 2F.  An expert without rows gets zeros.
 template <bool DOWN, class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
+__device__ __forceinline__ void gated_weights(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, Units units, int tall)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
-    const RowTiles tiles = {nullptr, nullptr, p.offset, p.E, p.R, 1};
     const int M = DOWN ? p.F : p.d, N = DOWN ? p.d : 2 * p.F;
     const unsigned lda = M * Z, ldb = N * Z;
     const TILE tile((product_lds_t *)smem, lda, ldb);
@@ -266,7 +265,7 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, char *smem, in
                 j.m0 = m * BIG_M + u % PARTS / PARTS_N * TILE::BM;
                 j.n0 = n * BIG_N + u % PARTS_N * TILE::BN;
             } while (t >= n_m * n_n || (PARTS > 1 && (j.m0 >= M || j.n0 >= N)));
-            int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e, lo));
+            int lo = __builtin_amdgcn_readfirstlane(tiles.first(e)), hi = __builtin_amdgcn_readfirstlane(tiles.end(e));
             if (p.parts > 1) {                 // this part's rows
                 const int part = (tiles_of(hi - lo, p.parts) + 63) / 64 * 64, from = lo + (j.group - e * p.parts) * part;
                 hi = from + part < hi ? from + part : hi;
@@ -308,10 +307,13 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel
 {
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
+    __shared__ int tables[3][MAX_GROUPS + 1];
+    const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, Big::BM};
+    tiles.count();
     const int n_m = tiles_of(DOWN ? p.F : p.d, Big::BM), n_n = tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
     in_rounds<SIZES>(8 * p.E * p.parts * gated_weights_share(n_m * n_n), [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
-        gated_weights<DOWN, Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        gated_weights<DOWN, Part, Big::BM, Big::BN>(p, tiles, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
     });
 }
 
@@ -339,13 +341,13 @@ __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(Gat
     typedef typename Whole<WEIGHTS>::Tile Weights;
     constexpr bool DOWN = STEP == GATED_DHIDDEN;
     __shared__ __align__(1024) char smem[Rows::LDS > Weights::LDS ? Rows::LDS : Weights::LDS];
-    __shared__ int prefix[MAX_GROUPS + 1], blocks[MAX_GROUPS];
-    const RowTiles tiles = {prefix, blocks, p.offset, p.E, p.R, Rows::BM};
+    __shared__ int tables[3][MAX_GROUPS + 1];
+    const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, Rows::BM};
     tiles.count();
-    const int n_m = __builtin_amdgcn_readfirstlane(prefix[p.E]), n_n = tiles_of(STEP == GATED_DHIDDEN ? p.F : p.d, Rows::HALF_N);
+    const int n_m = __builtin_amdgcn_readfirstlane(tiles.prefix[p.E]), n_n = tiles_of(STEP == GATED_DHIDDEN ? p.F : p.d, Rows::HALF_N);
     const int w_m = tiles_of(DOWN ? p.F : p.d, Weights::BM), w_n = tiles_of(DOWN ? p.d : 2 * p.F, Weights::BN), per = gated_weights_share(w_m * w_n);
     // costs in stages: a tile's and what its writes take (dh's with its states)
-    const int rows = __builtin_amdgcn_readfirstlane(tiles.end(p.E - 1, 0));
+    const int rows = __builtin_amdgcn_readfirstlane(tiles.end(p.E - 1));
     const int cost_rows = STEP == GATED_DHIDDEN ? p.d / Rows::STAGE_K + 20 : 2 * p.F / Rows::STAGE_K + 4, cost_weights = rows / p.E / Weights::STAGE_K + 5;
     const int slot = blockIdx.x >> 3, slots = gridDim.x >> 3;
     const Shares shares((n_m * n_n + 7) >> 3, cost_rows, p.E * per, cost_weights, slots);
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(Gat
     }
     const int total = 8 * p.E * per;
     gated_weights<DOWN, Weights, Weights::BM, Weights::BN>(
-        p, smem, w_m, w_n, 0, first ? Units(total, slot, shares.mine, shares.rest, total) : Units(total, slot - shares.mine, slots - shares.mine, 0, shares.rest), tall);
+        p, tiles, smem, w_m, w_n, 0, first ? Units(total, slot, shares.mine, shares.rest, total) : Units(total, slot - shares.mine, slots - shares.mine, 0, shares.rest), tall);
 }
 
 // ------------------------------------------------------------------------------------------------- host
@@ -373,7 +375,7 @@ void launch_few_rows(const GatedArgs &p, hipStream_t st)
 {
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
     const long long units = ((long long)p.R / TILE::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, TILE::HALF_N);
-    constexpr int per_cu = 160 * 1024 / (TILE::LDS + 8 * (MAX_GROUPS + 4));
+    constexpr int per_cu = 160 * 1024 / (TILE::LDS + 12 * (MAX_GROUPS + 4));
     const long long grid = units < PRODUCT_CUS * per_cu ? units : PRODUCT_CUS * per_cu;
     hipLaunchKernelGGL((gated_few_rows_kernel<STEP, TILE>), dim3((unsigned)((grid + 7) / 8 * 8)), dim3(TILE::THREADS), 0, st, p);
 }

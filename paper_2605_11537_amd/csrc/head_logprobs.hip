@@ -683,7 +683,9 @@ int head_check(const char *who, int N, int d, int V, int dtype)
     MOE_REQUIRE(N >= 0 && d > 0 && V > 0, MOE_ERR_INVALID_ARG, "%s: N=%d d=%d V=%d out of range", who, N, d, V);
     MOE_REQUIRE(dtype == MOE_F32 || dtype == MOE_BF16, MOE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, dtype);
     MOE_REQUIRE(d % 8 == 0, MOE_ERR_INVALID_ARG, "%s: d=%d must be a multiple of 8", who, d);
-    MOE_REQUIRE(d <= HEAD_MAX_WIDTH && V <= HEAD_MAX_IDS && N <= HEAD_MAX_ROWS, MOE_ERR_UNSUPPORTED, "%s: N=%d d=%d V=%d beyond the kernels", who, N, d, V);
+    MOE_REQUIRE(d <= HEAD_MAX_WIDTH && V <= HEAD_MAX_IDS && N <= HEAD_MAX_ROWS && (long long)ceil_div(N, 16) * ceil_div(V, 128) < 1ll << 30 &&
+                    (long long)ceil_div(d, 64) * ceil_div(V, 64) < 1ll << 30 && (long long)ceil_div(d, 64) * ceil_div(N, 16) < 1ll << 24,
+                MOE_ERR_UNSUPPORTED, "%s: N=%d d=%d V=%d beyond the kernels", who, N, d, V);
     return MOE_OK;
 }
 

@@ -487,52 +487,50 @@ struct Writer {
     }
 };
 
-// Where the row tiles of groups lie: prefix[e] tiles in front of group e's, as many as its rows ask for.  offset [E + 1] is the caller's table; an entry
-// that goes back, or past the rows there are, is taken for the nearest that does not.
+// Where the rows of groups and their tiles lie, from the caller's table `offset` [E + 1] (NULL: one group of all rows).  An entry that goes back, or past the
+// rows there are, is taken for the nearest that does not, so that no row has two groups.
 struct RowTiles {
-    int *prefix;                               // LDS, E + 1
-    int *blocks;                               // LDS, E, or NULL: blocks of 16 rows in front of group e's
+    int *begin;                                // LDS, E + 1: first row of group e
+    int *prefix;                               // LDS, E + 1: tiles in front of group e's, as many as its rows ask for
+    int *blocks;                               // LDS, E + 1: blocks of 16 rows in front of group e's
     const int32_t *offset;
     int E, rows, tile;                         // rows of the matrix, of a tile
 
-    __device__ __forceinline__ int first(int e) const
-    {
-        if (!offset) return 0;
-        const int v = offset[e];
-        return v < 0 ? 0 : v > rows ? rows : v;
-    }
-    __device__ __forceinline__ int end(int e, int from) const
-    {
-        if (!offset) return rows;
-        const int v = offset[e + 1];
-        return v < from ? from : v > rows ? rows : v;
-    }
-    // by the first wavefront; the workgroup's barrier follows.  -> total
+    __device__ __forceinline__ int first(int e) const { return begin[e]; }
+    __device__ __forceinline__ int end(int e) const { return begin[e + 1]; }
+    // by the first wavefront; the workgroup's barrier follows
     __device__ __forceinline__ void count() const
     {
         const int lane = threadIdx.x;
         if (lane < WAVE) {
-            int before = 0, blocks_before = 0;
+            int last = 0, tiles_before = 0, blocks_before = 0;
+            if (lane == 0) begin[0] = !offset ? 0 : clamped(offset[0]);
+            last = !offset ? 0 : clamped(offset[0]);
             for (int e0 = 0; e0 < E; e0 += WAVE) {
                 const int e = e0 + lane;
-                int n = 0;
+                int past = !offset ? rows : e < E ? clamped(offset[e + 1]) : 0;
+                past = past > last ? past : last;
+#pragma unroll
+                for (int o = 1; o < 64; o <<= 1) {
+                    const int before = __shfl_up(past, o, 64);
+                    past = lane >= o && before > past ? before : past;
+                }
+                const int from = __shfl_up(past, 1, 64), n = past - (lane == 0 ? last : from);
+                const int t = (n + tile - 1) / tile, t_upto = wave_scan_incl(t), b = (n + 15) / 16, b_upto = wave_scan_incl(b);
                 if (e < E) {
-                    const int lo = first(e);
-                    n = end(e, lo) - lo;
+                    begin[e + 1] = past;
+                    prefix[e] = tiles_before + t_upto - t;
+                    blocks[e] = blocks_before + b_upto - b;
                 }
-                const int of = (n + tile - 1) / tile, upto = wave_scan_incl(of);
-                if (e < E) prefix[e] = before + upto - of;
-                before += __builtin_amdgcn_readlane(upto, 63);
-                if (blocks) {
-                    const int b = (n + 15) / 16, b_upto = wave_scan_incl(b);
-                    if (e < E) blocks[e] = blocks_before + b_upto - b;
-                    blocks_before += __builtin_amdgcn_readlane(b_upto, 63);
-                }
+                last = __builtin_amdgcn_readlane(past, 63);
+                tiles_before += __builtin_amdgcn_readlane(t_upto, 63);
+                blocks_before += __builtin_amdgcn_readlane(b_upto, 63);
             }
-            if (lane == 0) prefix[E] = before;
+            if (lane == 0) prefix[E] = tiles_before;
         }
         __syncthreads();
     }
+    __device__ __forceinline__ int clamped(int v) const { return v < 0 ? 0 : v > rows ? rows : v; }
     // the group of row tile t and its rows
     __device__ __forceinline__ int find(int t, int &lo, int &hi) const
     {
@@ -543,9 +541,8 @@ struct RowTiles {
             else past = mid;
         }
         e = __builtin_amdgcn_readfirstlane(e);
-        const int from = first(e), until = end(e, from);
-        lo = __builtin_amdgcn_readfirstlane(from + (t - prefix[e]) * tile);
-        hi = __builtin_amdgcn_readfirstlane(until);
+        lo = __builtin_amdgcn_readfirstlane(first(e) + (t - prefix[e]) * tile);
+        hi = __builtin_amdgcn_readfirstlane(end(e));
         return e;
     }
 };
@@ -635,11 +632,11 @@ struct Sizes<bf16_t, A, B, HALVES> {
 template <Order A, Order B, int HALVES>
 struct Sizes<float, A, B, HALVES> {
     typedef Sized<Tile<float, A, B, 128, 128, 2, 2, HALVES>> Whole;
-    typedef Sized<Tile<float, A, B, 64, 128, 2, 2, HALVES, 3>> Half;
+    typedef Sized<Tile<float, A, B, 64, 128, 2, 2, HALVES>> Half;
     typedef Sized<Tile<float, A, B, 64, 64, 2, 2, HALVES, 4>> Quarter;
-    typedef Sized<Tile<float, A, B, 32, 64, 2, 2, HALVES, 6>> Eighth;
+    typedef Sized<Tile<float, A, B, 32, 64, 2, 2, HALVES, 5>> Eighth;
     typedef Eighth Sixteenth;
-    static constexpr int PER_CU = 2;
+    static constexpr int PER_CU = 2;           // with 13 KB of tables beside 64 KB of stages
 };
 template <class SIZES>
 struct Whole {

@@ -48,6 +48,7 @@ def check(s, dtype, act, y, grads, experts=None):
 CASES = [
     ([1], 0, 8, 8), ([1], 0, 72, 136), ([0, 1, 0], 2, 16, 24), ([3, 0, 5, 1], 1, 64, 64), ([63, 64, 65], 0, 72, 40), ([255], 0, 136, 264), ([257, 200], 3, 128, 256),
     ([100, 0, 0, 513], 5, 264, 200), ([16, 17, 15, 9, 8, 7], 0, 256, 512), ([2] * 40, 7, 48, 72), ([0, 0], 4, 16, 16), ([300, 1, 129, 33], 0, 520, 72), ([5, 120], 0, 1032, 24),
+    ([1, 0, 3] * 300, 2, 24, 40),
 ]
 
 
@@ -113,6 +114,28 @@ def test_a_table_out_of_order():
         assert torch.equal(y[:20], good[:20])
         if rows == 64:
             assert torch.equal(y, good)
+
+
+def test_a_table_that_names_rows_twice():
+    """Groups that would share rows: the later ones have what is left, forward and backward (the states hold each row once)."""
+    import paper_2605_11537_amd as moe
+    s = inputs("bf16", [64] * 5, 64, 64, 64, 8)
+    for table, same in (([0, 64, 0, 64, 0, 64], [0, 64, 64, 64, 64, 64]), ([0, 40, 7, 50, -3, 90], [0, 40, 40, 50, 50, 64]), ([70, 5, 3, 2, 1, 0], [64] * 6)):
+        got = []
+        for t in (table, same):
+            t = torch.tensor(t, dtype=torch.int32, device="cuda")
+            y, states = moe.moe_gated_ffn(s["x"], *s["w"], t, want_states=True)
+            got.append([y] + list(moe.moe_gated_ffn_backward(s["dy"], s["x"], *s["w"], states, t).values()))
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_no_rows():
+    import paper_2605_11537_amd as moe
+    for counts in ([0], [0, 0, 0]):
+        s = inputs("bf16", counts, 0, 64, 96, 9)
+        y, states = moe.moe_gated_ffn(s["x"], *s["w"], s["offset"], want_states=True)
+        grads = moe.moe_gated_ffn_backward(s["dy"], s["x"], *s["w"], states, s["offset"])
+        assert y.shape == (0, 64) and grads["dx"].shape == (0, 64) and not any(grads[k].any() for k in ("dw_gate", "dw_up", "dw_down"))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

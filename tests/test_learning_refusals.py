@@ -67,6 +67,7 @@ def test_head(buf):
 
     assert call(N=-1) == INV and call(d=0) == INV and call(V=0) == INV and call(d=12) == INV and call(dtype=3) == INV
     assert call(d=1 << 21) == UNS and call(V=(1 << 24) + 1) == UNS and call(N=(1 << 24) + 1) == UNS
+    assert call(N=1 << 24, V=1 << 24) == UNS and call(d=1 << 20, V=1 << 24) == UNS and call(d=1 << 20, N=1 << 24) == UNS
     for k in ("h", "w", "t", "lp", "lse"):
         assert call(**{k: None}) == INV, k
     assert call(h=off(h)) == INV and call(w=off(w)) == INV and call(lse=lp) == INV

@@ -558,7 +558,7 @@ struct RowParts<bf16_t> : Sizes<bf16_t, ALONG_K, ALONG_K> {
 template <>
 struct RowParts<float> : Sizes<float, ALONG_K, ALONG_K> {
     typedef Sized<Tile<float, ALONG_K, ALONG_K, 32, 128, 2, 2, 1, 3>> Quarter;
-    typedef Sized<Tile<float, ALONG_K, ALONG_K, 16, 128, 1, 4, 1, 4>> Eighth;
+    typedef Sized<Tile<float, ALONG_K, ALONG_K, 16, 128, 1, 4, 1, 3>> Eighth;
     typedef Eighth Sixteenth;
 };
 template <class T>

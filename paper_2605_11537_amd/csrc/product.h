@@ -638,10 +638,17 @@ struct Sizes<float, A, B, HALVES> {
     typedef Eighth Sixteenth;
     static constexpr int PER_CU = 2;           // with 13 KB of tables beside 64 KB of stages
 };
+constexpr int larger(int a, int b) { return a > b ? a : b; }
 template <class SIZES>
 struct Whole {
     typedef typename SIZES::Whole::Type Tile;
-    static constexpr int THREADS = Tile::THREADS, WAVES = Tile::WAVES, LDS_HALF = SIZES::Half::Type::LDS, LDS = LDS_HALF > Tile::LDS ? LDS_HALF : Tile::LDS;
+    static constexpr int THREADS = Tile::THREADS;
+    // of all sizes, which use the same LDS one after another
+    static constexpr int LDS = larger(larger(larger(Tile::LDS, SIZES::Half::Type::LDS), larger(SIZES::Quarter::Type::LDS, SIZES::Eighth::Type::LDS)),
+                                      SIZES::Sixteenth::Type::LDS);
+    static_assert(SIZES::Half::Type::THREADS == THREADS && SIZES::Quarter::Type::THREADS == THREADS && SIZES::Eighth::Type::THREADS == THREADS &&
+                      SIZES::Sixteenth::Type::THREADS == THREADS,
+                  "one workgroup for all");
 };
 
 __host__ __device__ constexpr int tiles_of(int n, int tile) { return (n + tile - 1) / tile; }

@@ -55,12 +55,13 @@ __device__ __forceinline__ void product_mma(product_f32x4 &d, product_f32x4 b, p
 
 // 1 KB from a buffer to LDS: lane l's 16 bytes at `at` go to lds + 16 l.  No register is written, so nothing has to wait but the readers of that LDS.
 // Inline assembly: in front of every LDS read that the compiler sees it would wait for all such loads, those of later stages too.
-// (m0 may be read one instruction after it is written.)
+// The assembler adds no waits by itself: m0 may be read one instruction after it is written, a buffer's registers five after a vector instruction has (as one
+// that makes a value scalar, or brings a spilled register back).
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(product_u32x4 buffer, unsigned at, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(at), "s"(buffer) : "m0");
 }
 #pragma clang diagnostic pop
 

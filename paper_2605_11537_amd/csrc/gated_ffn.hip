@@ -93,8 +93,10 @@ __device__ __forceinline__ float *gated_states(const TILE &tile, const RowTiles 
 }
 
 // STEP's tiles of type TILE: `units` of the parts of n_m x n_n tiles of BIG_M rows x BIG_N columns (of a half), from tile `first` on
-template <int STEP, class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, Units units, int tall)
+// SPLIT: the workgroup's wavefronts have a tile each, of the same place, and share its k; `shared` holds their sums, which the first one adds and writes.
+template <int STEP, class TILE, int BIG_M, int BIG_N, int SPLIT = 1>
+__device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &tiles, char *smem, int n_m, int n_n, int first, Units units, int tall,
+                                           product_f32x4 *shared = nullptr)
 {
     typedef typename TILE::T T;
     constexpr int Z = sizeof(T), PARTS_M = BIG_M / TILE::BM, PARTS_N = BIG_N / TILE::HALF_N, PARTS = PARTS_M * PARTS_N;
@@ -104,7 +106,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
     const unsigned ldb = STEP == GATED_HIDDEN || STEP == GATED_DX ? f_bytes : d_bytes;
     const TILE tile((product_lds_t *)smem, lda, ldb);
     const bool with_states = p.gu != nullptr;
-    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
+    tile.template run<SPLIT == 1 ? TILE::MB * Writer<TILE, T>::STORES : 0>(
         [&](Job &j) {
             int u, m, n, lo, hi;
             do {
@@ -141,9 +143,35 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
                 j.b[0] = source_along(p.w_gate, w + (size_t)j.n0 * f_bytes, f_bytes, j.columns, TILE::HALF_N);
                 j.b[1] = source_along(p.w_up, w + (size_t)j.n0 * f_bytes, f_bytes, j.columns, TILE::HALF_N);
             }
+            if constexpr (SPLIT > 1) {
+                const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = (tiles_of(j.k, SPLIT) + TILE::STAGE_K - 1) / TILE::STAGE_K * TILE::STAGE_K;
+                const int k0 = wave * part, along = k0 * Z, b_skip = TILE::B_ORDER == ALONG_K ? 1 : ldb;
+                for (int i = 0; i < 2; ++i) {
+                    j.a[i].base += along;
+                    j.a[i].records -= along;
+                    j.b[i].base += TILE::B_ORDER == ALONG_K ? (size_t)along : (size_t)k0 * b_skip;
+                    if (TILE::B_ORDER == ALONG_K) j.b[i].records -= along;
+                }
+                j.k = j.k - k0 < part ? (j.k - k0 > 0 ? j.k - k0 : 0) : part;
+            }
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
+            if constexpr (SPLIT > 1) {
+                constexpr int N = TILE::HALVES * TILE::MB * TILE::NB;
+                const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+                product_f32x4 *const mine = &sums[0][0][0];
+                __syncthreads();               // the sums of the tile before have been read
+                if (wave > 0)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) shared[((wave - 1) * N + i) * 64 + lane] = mine[i];
+                __syncthreads();
+                if (wave > 0) return;
+#pragma unroll
+                for (int w = 0; w < SPLIT - 1; ++w)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) mine[i] += shared[(w * N + i) * 64 + lane];
+            }
             if constexpr (STEP == GATED_HIDDEN) {
                 const Writer<TILE, T> h(tile, (T *)p.h + (size_t)j.m0 * p.F + j.n0, f_bytes, j.rows, j.columns);
                 float *const gu = gated_states(tile, tiles, j, p);
@@ -222,6 +250,22 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
         constexpr int parts = Big::BM / Part::BM * (Big::HALF_N / Part::HALF_N);
         gated_rows<STEP, Part, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, Units((past - first) * parts), tall);
     });
+}
+
+// Tiles of 16 rows x 32 columns, in so few workgroups that a stage's way from memory counts: four wavefronts, each with its quarter of k, its own ring and no
+// barrier while it runs.  One row, 768 x 2048: 6.8 and 7.0 us; with the wavefronts beside each other and one ring 9.8 and 11.0.
+template <int STEP, class TILE>
+__global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
+{
+    constexpr int SPLIT = 4;
+    __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
+    __shared__ product_f32x4 shared[(SPLIT - 1) * TILE::HALVES * TILE::MB * TILE::NB * 64];
+    __shared__ int tables[3][MAX_GROUPS + 1];
+    const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, TILE::BM};
+    tiles.count();
+    const int n_m = __builtin_amdgcn_readfirstlane(tiles.prefix[p.E]), n_n = tiles_of(STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d, TILE::HALF_N);
+    char *const ring = smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * TILE::LDS;
+    gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N, SPLIT>(p, tiles, ring, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
 }
 
 // tiles of few rows, one size
@@ -379,6 +423,13 @@ void launch_few_rows(const GatedArgs &p, hipStream_t st)
     const long long grid = units < PRODUCT_CUS * per_cu ? units : PRODUCT_CUS * per_cu;
     hipLaunchKernelGGL((gated_few_rows_kernel<STEP, TILE>), dim3((unsigned)((grid + 7) / 8 * 8)), dim3(TILE::THREADS), 0, st, p);
 }
+template <int STEP, class TILE>
+void launch_tiny(const GatedArgs &p, hipStream_t st)
+{
+    const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
+    const long long units = ((long long)p.R / TILE::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, TILE::HALF_N);
+    hipLaunchKernelGGL((gated_tiny_kernel<STEP, TILE>), dim3((unsigned)(((units < PRODUCT_CUS ? units : PRODUCT_CUS) + 7) / 8 * 8)), dim3(4 * WAVE), 0, st, p);
+}
 template <bool DOWN, class SIZES>
 void launch_weights(const GatedArgs &p, hipStream_t st)
 {
@@ -393,13 +444,13 @@ template <Order B, int HALVES>
 struct Few<bf16_t, B, HALVES> {
     typedef Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES> Mid;
     typedef Tile<bf16_t, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Low;
-    typedef Tile<bf16_t, ALONG_K, B, 16, 64, 1, 4 / HALVES, HALVES, 8> Tiny;
+    typedef Tile<bf16_t, ALONG_K, B, 16, 32 * HALVES, 1, 1, HALVES, HALVES == 2 ? 3 : 5> Tiny;
 };
 template <Order B, int HALVES>
 struct Few<float, B, HALVES> {
     typedef Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Mid;
     typedef Mid Low;
-    typedef Tile<float, ALONG_K, B, 16, 64, 1, 4 / HALVES, HALVES, 8> Tiny;
+    typedef Tile<float, ALONG_K, B, 16, 32 * HALVES, 1, 1, HALVES, HALVES == 2 ? 3 : 5> Tiny;
 };
 
 template <int STEP, class T>
@@ -412,7 +463,7 @@ void launch_step(const GatedArgs &p, hipStream_t st)
     case GATED_TALL: launch_rows<STEP, Sizes<T, ALONG_K, B, HALVES>>(p, st); break;
     case GATED_MID: launch_few_rows<STEP, typename few::Mid>(p, st); break;
     case GATED_LOW: launch_few_rows<STEP, typename few::Low>(p, st); break;
-    default: launch_few_rows<STEP, typename few::Tiny>(p, st);
+    default: launch_tiny<STEP, typename few::Tiny>(p, st);
     }
 }
 

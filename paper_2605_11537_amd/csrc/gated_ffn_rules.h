@@ -14,7 +14,7 @@ static inline size_t states_blocks(int R, int E) { return (size_t)R / 16 + (E < 
 static inline size_t hidden_bytes(int R, int F, int dtype) { return align_up((size_t)R * F * (dtype == MOE_F32 ? 4 : 2), 256); }
 
 // The tile by the rows that an expert has if all have the same (the table is in device memory) and the columns of D.
-//   TINY  16 rows, narrow, eight stages deep: so few tiles that each has a compute unit to itself, where a stage's way from memory counts
+//   TINY  16 rows x 32 columns: so few tiles that each has a compute unit to itself, where a stage's way from memory counts
 //   LOW   32 rows, MID 64: bound by the stream of the weights
 //   TALL  up to 256, by the matrix pipes
 // us, one way, the other: 37 rows of 128 experts, 768 x 2048, MID 66, LOW 50; 4096 rows MID 266, LOW 257

@@ -99,10 +99,13 @@ struct Operand {
     // ALONG_K: the XOR of row r's pieces
     __device__ __forceinline__ static unsigned turn(unsigned r) { return (r >> 1) & 7; }
 
+    // this wavefront's number among those that share the tile
+    __device__ __forceinline__ static unsigned wave() { return WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
     // row: this wavefront's first row in the tile
     __device__ __forceinline__ void set_up(unsigned ld_bytes, int row)
     {
-        const unsigned lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned lane = threadIdx.x & 63, w = wave();
         const unsigned c = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
@@ -160,7 +163,7 @@ struct Operand {
     // this wavefront's load i of a stage; left: k from the stage's first on
     __device__ __forceinline__ void load(int i, product_u32x4 buffer, int left, unsigned lds) const
     {
-        const unsigned w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const unsigned w = wave();
         unsigned a = at[i];
         if (ORDER == ALONG_K) a = (int)k_of[i] < left ? a : 0x80000000u;
         load_to_lds(buffer, a, lds + ((w * MINE + i) % LOADS) * 1024);
@@ -225,6 +228,7 @@ struct Tile {
     static constexpr int BM = BM_, BN = BN_, HALVES = HALVES_, WAVES = WM * WN, THREADS = WAVES * WAVE;
     static constexpr int HALF_N = BN / HALVES, WAVE_M = BM / WM, WAVE_N = HALF_N / WN;       // rows and columns (of a half) of a wavefront
     static constexpr int MB = WAVE_M / 16, NB = WAVE_N / 16;                                 // blocks of 16
+    static constexpr Order B_ORDER = OB;
     typedef Operand<T, OA, BM, WAVES> A;
     typedef Operand<T, OB, HALF_N, WAVES> B;
     static constexpr int STAGE_K = A::STAGE_K;
@@ -254,7 +258,7 @@ struct Tile {
 
     __device__ __forceinline__ Tile(product_lds_t *smem, unsigned lda_bytes, unsigned ldb_bytes) : lda(lda_bytes), ldb(ldb_bytes), lds(smem)
     {
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int w = A::wave();
         wm = w / WN;
         wn = w % WN;
         a.set_up(lda, wm * WAVE_M);
@@ -349,8 +353,15 @@ struct Tile {
     __device__ __forceinline__ static void wait(int pending, bool behind)
     {
         if (younger<STAGES - 2>(pending)) return;
-        if (STORES > 0 && behind) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(STORES < 63 ? STORES : 63) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (STORES > 0 && behind) landed<(STORES < 63 ? STORES : 63)>();
+        else landed<0>();
+    }
+    // all but the newest N vector memory operations are done; a tile of one wavefront needs no barrier
+    template <int N>
+    __device__ __forceinline__ static void landed()
+    {
+        if constexpr (WAVES > 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
     }
     // N or more stages are younger than the oldest
     template <int N>
@@ -359,7 +370,7 @@ struct Tile {
         if constexpr (N > 0) {
             static_assert(N * LOADS < 64, "what the counter holds");
             if (pending <= N) return younger<N - 1>(pending);
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N * LOADS) : "memory");
+            landed<N * LOADS>();
             return true;
         }
         return false;
@@ -442,7 +453,7 @@ struct Tile {
             more = next(then);
             // stages behind a tile without any: its buffers are free, everyone has passed the barrier of the last multiplied stage
             if (pending == 0) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                landed<0>();
                 ask(STAGES - 1);
             }
         }

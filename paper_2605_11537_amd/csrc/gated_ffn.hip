@@ -248,7 +248,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
         constexpr int parts = Big::BM / Part::BM * (Big::HALF_N / Part::HALF_N);
-        gated_rows<STEP, Part, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, Units((past - first) * parts), tall);
+        gated_rows<STEP, Part, Big::BM, Big::HALF_N>(p, tiles, smem, n_m, n_n, first, Units((past - first) * parts, first > 0), tall);
     });
 }
 
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel
     const int n_m = tiles_of(DOWN ? p.F : p.d, Big::BM), n_n = tiles_of(DOWN ? p.d : 2 * p.F, Big::BN);
     in_rounds<SIZES>(8 * p.E * p.parts * gated_weights_share(n_m * n_n), [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
-        gated_weights<DOWN, Part, Big::BM, Big::BN>(p, tiles, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        gated_weights<DOWN, Part, Big::BM, Big::BN>(p, tiles, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN)), first > 0), tall);
     });
 }
 

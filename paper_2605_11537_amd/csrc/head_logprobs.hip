@@ -155,7 +155,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::BN == Big::BN, "one slot for a row's columns of a tile");
         typedef typename decltype(sized)::Type Part;
-        head_forward<Part, Big::BM, Big::BN>(p, smem, parts, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        head_forward<Part, Big::BM, Big::BN>(p, smem, parts, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN)), first > 0), tall);
     });
 }
 template <class TILE>
@@ -167,15 +167,18 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
     head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
-// One wavefront per row: its tiles' maxima and sums -> lse and the target's log probability.
+// A row's tiles' maxima and sums -> lse and the target's log probability.  ROWS rows to a workgroup of four wavefronts: one each, or with few rows, whose
+// tiles would be many trips one behind another, all four on one (3 x 131072: 5 us, one wavefront 7.7).
+template <int ROWS>
 __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, const float *at_target, const int32_t *target, int N, int V, int n_n,
                                                         float *logprob, float *lse)
 {
-    const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (row >= N) return;
+    constexpr int LANES = 256 / ROWS;
+    const int row = blockIdx.x * ROWS + threadIdx.x / LANES, lane = threadIdx.x & 63;
+    if (ROWS > 1 && row >= N) return;
     const float2 *t = tiles + (size_t)row * n_n;
     float m = HEAD_NONE, s = 0.f;
-    for (int i = lane; i < n_n; i += 64) {
+    for (int i = threadIdx.x % LANES; i < n_n; i += LANES) {
         const float2 v = t[i];
         const float both = fmaxf(m, v.x), beside = finite_or(both, 0.f);
         s = s * exp_of<true>(finite_or(m, beside) - beside) + v.y * exp_of<true>(finite_or(v.x, beside) - beside);
@@ -184,12 +187,20 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, con
     float all = m;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) all = fmaxf(all, __shfl_xor(all, o, 64));
-    const float beside = finite_or(all, 0.f);
-    s *= exp_of<true>(finite_or(m, beside) - beside);
+    s *= exp_of<true>(finite_or(m, finite_or(all, 0.f)) - finite_or(all, 0.f));
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
-    if (lane == 0) {
-        const float l = logf(s);               // -infinity where every id is masked
+    if (ROWS == 1) {
+        __shared__ float2 waves[4];
+        if (lane == 0) waves[threadIdx.x >> 6] = make_float2(all, s);
+        __syncthreads();
+        all = fmaxf(fmaxf(waves[0].x, waves[1].x), fmaxf(waves[2].x, waves[3].x));
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) s += waves[w].y * exp_of<true>(finite_or(waves[w].x, finite_or(all, 0.f)) - finite_or(all, 0.f));
+    }
+    if (threadIdx.x % LANES == 0) {
+        const float beside = finite_or(all, 0.f), l = logf(s);         // -infinity where every id is masked
         lse[row] = beside + l;
         const int id = target[row];
         const bool on = id >= 0 && id < V;
@@ -293,7 +304,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dlogits_kernel(
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::WAVE_M == Big::WAVE_M, "one slot for a wavefront's rows");
         typedef typename decltype(sized)::Type Part;
-        head_dlogits<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        head_dlogits<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN)), first > 0), tall);
     });
 }
 template <class TILE>
@@ -370,7 +381,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dh_kernel(HeadG
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.d, Big::BN);
     in_rounds<SIZES>(p.parts * n_m * n_n, [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
-        head_dh<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        head_dh<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN)), first > 0), tall);
     });
 }
 template <class TILE>
@@ -434,7 +445,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dw_kernel(HeadG
     const int n_m = tiles_of(p.columns, Big::BM), n_n = tiles_of(p.d, Big::BN);
     in_rounds<SIZES>(p.dw_parts * n_m * n_n, [&](auto sized, int first, int past) {
         typedef typename decltype(sized)::Type Part;
-        head_dw<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN))), tall);
+        head_dw<Part, Big::BM, Big::BN>(p, smem, n_m, n_n, first, Units((past - first) * (Big::BM / Part::BM * (Big::BN / Part::BN)), first > 0), tall);
     });
 }
 
@@ -632,7 +643,8 @@ template <class T>
 void forward(const HeadArgs &p, int N, float *logprob, float *lse, hipStream_t st)
 {
     HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
-    hipLaunchKernelGGL(head_join_kernel, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
+    if (N <= 512 && p.n_n > 64) hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
+    else hipLaunchKernelGGL(head_join_kernel<4>, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
 }
 
 template <class T>

@@ -580,7 +580,11 @@ struct Units {
         end = past < total ? past : total;
         by = slots;
     }
-    __device__ __forceinline__ explicit Units(int total) : Units(total, blockIdx.x >> 3, gridDim.x >> 3, 0, total) {}      // grids are multiples of 8
+    // all of them; grids are multiples of 8.  behind: of others, of which the first workgroups may have one more
+    __device__ __forceinline__ explicit Units(int total, bool behind = false)
+        : Units(total, behind ? (gridDim.x >> 3) - 1 - (blockIdx.x >> 3) : blockIdx.x >> 3, gridDim.x >> 3, 0, total)
+    {
+    }
     __device__ __forceinline__ bool take(int &u)
     {
         if (at >= end) return false;
@@ -611,19 +615,35 @@ struct Shares {
     }
 };
 
-// A product's tiles of the largest size in whole rounds over the workgroups, and what is left over in tiles of a half down to a sixteenth of that size, as
-// one round holds them: a last round of a few large tiles would leave the other compute units without work for a whole tile's time.
+// A product's tiles of the largest size in whole rounds over the compute units, and what is left over in tiles of a half down to a sixteenth of that size: a
+// last round of a few large tiles would leave the other compute units without work for a whole tile's time.  bfloat16, one workgroup to a compute unit: as one
+// round holds them (small tiles are bound by LDS).  binary32, whose matrix instructions take the longest, whatever the tile: by the time that the rounds take.
 // run(tile type, first unit, past the last)
 template <class SIZES, class Run>
 __device__ __forceinline__ void in_rounds(int units, Run &&run)
 {
-    const int grid = gridDim.x, rest = units % grid, whole = 2 * rest > grid ? units : units - rest;
+    const int grid = gridDim.x, cus = grid < 256 ? grid : 256, rest = units % cus;
+    int whole = units - rest, size;            // of the rest: a half, 2, ..
+    if (SIZES::PER_CU == 1) {
+        if (2 * rest > cus) whole = units;
+        size = 4 * rest > cus ? 2 : 8 * rest > cus ? 4 : 16 * rest > cus ? 8 : 16;
+    } else {
+        // percent of a whole tile's time; alone on its compute unit a workgroup has nobody to fill its waits
+        auto time = [&](int parts, int each) {
+            const int rounds = (parts * rest + cus - 1) / cus;
+            return (rounds * each + (rounds == 1 ? 15 : 0)) / parts;
+        };
+        const int t2 = time(2, 103), t4 = time(4, 108), t8 = time(8, 120);
+        const int t = t2 < t4 ? t2 : t4;
+        size = t8 < t ? 8 : t4 < t2 ? 4 : 2;
+        if (t >= 100 && t8 >= 100) whole = units;
+    }
     if (whole > 0) run(typename SIZES::Whole(), 0, whole);
     if (whole == units) return;
     if (whole > 0) __syncthreads();            // the buffers change their sizes
-    if (4 * rest > grid) run(typename SIZES::Half(), whole, units);
-    else if (8 * rest > grid) run(typename SIZES::Quarter(), whole, units);
-    else if (16 * rest > grid) run(typename SIZES::Eighth(), whole, units);
+    if (size == 2) run(typename SIZES::Half(), whole, units);
+    else if (size == 4) run(typename SIZES::Quarter(), whole, units);
+    else if (size == 8) run(typename SIZES::Eighth(), whole, units);
     else run(typename SIZES::Sixteenth(), whole, units);
 }
 template <class TILE>

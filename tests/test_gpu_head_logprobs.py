@@ -151,3 +151,25 @@ def test_equal_calls_give_equal_bits(dtype):
     for _ in range(2):
         again = run(moe, s)
         assert all(torch.equal(again[k], first[k]) for k in first)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 2, 511, 512, 513])
+def test_few_rows_of_many_ids(N, dtype):
+    """Rows in few workgroups each, whose tiles are masked as a whole, all but one id, and throughout."""
+    import paper_2605_11537_amd as moe
+    V = 9001
+    s = inputs(dtype, N, 16, V, True, 0.0, 40 + N)
+    s["b"][1000:7000] = -float("inf")
+    s["target"][0] = 500
+    want = want_of(s, dtype)
+    got = moe.moe_head_logprobs(s["h"], s["w"], s["target"], s["b"])
+    check(got, {k: want[k] for k in ("logprob", "lse")}, True)
+    s["b"][:-1] = -float("inf")
+    s["target"].fill_(V - 1)
+    want = want_of(s, dtype)
+    got = moe.moe_head_logprobs(s["h"], s["w"], s["target"], s["b"])
+    check(got, {k: want[k] for k in ("logprob", "lse")}, True)
+    s["b"][-1] = -float("inf")
+    got = moe.moe_head_logprobs(s["h"], s["w"], s["target"], s["b"])
+    assert torch.isneginf(got["lse"]).all() and torch.isneginf(got["logprob"]).all()

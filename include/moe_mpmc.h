@@ -320,8 +320,9 @@ typedef struct moe_layer_args {
 int moe_layer_forward(const moe_layer_args *args, void *stream);
 
 /* =======================================================================================
- * Training the gate and the predictor, and serving the predictor step by step.  The matrix products between these
- * calls are the caller's; what is here moves or scans rows.
+ * Training the gate and the predictor, and serving the predictor step by step.  What follows first moves or scans rows
+ * (the matrix products between those calls are the caller's); behind it are the products of gated experts and of a head, with
+ * their gradients, and the clipping of all gradients.
  *
  * Gradients of the routed layer.  With out = moe_combine_topk(y_perm, x, inv, w) and x_perm =
  * moe_dispatch_topk(x), for dout = dL/dout and dx_perm = dL/dx_perm (k = 1 serves moe_combine and moe_dispatch):

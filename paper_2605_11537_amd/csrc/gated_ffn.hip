@@ -2,7 +2,11 @@
 //
 // Forward, two launches: g and u = x [W_gate | W_up] and h = act(g) u in one (a workgroup has the same columns of both matrices, so that a lane holds g
 // and u of an element), then y = h W_down.  Backward, three: dh = dy W_down^T with dg = dh u act'(g) and du = dh act(g) written as they come, dx = dg
-// W_gate^T + du W_up^T as one sum over both, and the weights' gradients x^T [dg | du] and h^T dy, expert by expert over its rows.
+// W_gate^T + du W_up^T as one sum over both, and the weights' gradients x^T [dg | du] and h^T dy, expert by expert over its rows.  dh goes with dW_down
+// in one launch and dx with the other two where there is work enough.
+//
+// Bound by the matrix instructions with many rows of an expert, by the stream of the weights with few, by launches and round trips with one.  A
+// training step's 18 d F operations a row are beside the states, 10 F bytes a row (bfloat16) written and read.
 //
 // h, dg and du are rounded once to the tensors' type, as operands of the products behind them; g and u are kept in binary32 for the gradient (states): a
 // second rounding to bfloat16 in the chain would make the gradients' error 1.7 times that of rounding them once, 1.4 times without.
@@ -68,8 +72,6 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
     return g > 0.f ? g : g != g ? g : 0.f;
 }
 
-// The states' g and u: blocks of 16 rows (of an expert, from its first) x 16 columns, in the order of the matrix instructions' lanes, u's block behind g's.
-// What a store or a load of a wavefront moves is then 1 KB in a run; rows of 64 bytes took 14 of a tile's 50 us (256 x 128, d 1024).
 struct GatedArgs {
     const void *x, *w_gate, *w_up, *w_down, *dy;
     const int32_t *offset;
@@ -236,6 +238,10 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
         });
 }
 
+// Many rows: tiles of 256 x 256 (hidden: 256 x 128 of both matrices, so that g and u of an element meet in a lane), one workgroup of eight wavefronts to a
+// compute unit that goes from tile to tile; binary32 128 x 128, two workgroups.  Bound by the matrix instructions and, in front of them, by the stages' way from
+// LDS; hidden beside that by the states that a tile writes at its end.  8192 x 1024 x 4096, one expert: hidden 208 us (0.66 PFLOP/s: of a tile's 50 us the
+// products take 26, the states' stores 13, the activation 4.5), down 98 (0.70), dh, which waits for the states at its tiles' ends, 168.
 template <int STEP, class SIZES>
 __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(GatedArgs p, int tall)
 {
@@ -268,7 +274,10 @@ __global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
     gated_rows<STEP, TILE, TILE::BM, TILE::HALF_N, SPLIT>(p, tiles, ring, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
 }
 
-// tiles of few rows, one size
+// Few rows of an expert: tiles of 32 or 64 rows x 128 columns (hidden: 64 of both matrices), several small workgroups to a compute unit, whose rings together
+// keep enough of the weights on their way.  Bound by that stream.  768 x 2048: 34 rows of 26 experts 31 and 19 us (5.3 and 4.2 TB/s; of the second
+// there are 156 tiles for 256 compute units); 2181 rows of 128 179 and 83 (4.5 and 4.9).  In binary32 the products cost as much: 958 rows, 32 experts of 512 x
+// 1376, hidden 58 and dx 82 us.
 template <int STEP, class TILE>
 __global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedArgs p)
 {
@@ -346,6 +355,9 @@ __device__ __forceinline__ void gated_weights(const GatedArgs &p, const RowTiles
         });
 }
 
+// Sums over rows: both operands lie across k and are transposed on their way from LDS, k is an expert's rows, of any number.  Bound by the matrix
+// instructions with some hundred rows to an expert (8192 x 1024 x 4096: dW_down 122 us, 0.56 PFLOP/s: 64 tiles, as 256 quarters), by writing the gradients
+// with few (958 rows, 32 experts of 512 x 1376 in binary32: 72 and 43 us for 180 and 90 MB).
 template <bool DOWN, class SIZES>
 __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_weights_kernel(GatedArgs p, int tall)
 {
@@ -377,7 +389,9 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const float *sums, int 
 
 // ------------------------------------------------------------------------------------------------- both, where there is work for the whole chip
 // dh with dW_down, dx with dW_gate and dW_up: two products that need nothing of each other share a launch, so that the last round of one does not leave
-// compute units without work, and the tiles that wait for memory (dh's for the states) run beside such as do not.
+// compute units without work, and the tiles that wait for memory (dh's for the states) run beside such as do not.  16 experts of 1024 x 2816, 15747
+// rows: 368 and 449 us (0.49 and 0.81 PFLOP/s), as four launches 364 and 525; a step of 8 experts of 2048 x 1408 and 16384 rows 960 us, without the first pair
+// 1020, without both 1095; of 64 of 512 x 1376 and 24576 rows 748, 735 and 731.
 template <int STEP, class ROWS, class WEIGHTS>
 __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(GatedArgs p, int tall)
 {

@@ -87,6 +87,23 @@ def test_one_block(R, d, F, dtype):
     assert torch.equal(y, moe.moe_gated_ffn(s["x"], *s["w"], s["offset"])[0])
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts,d,F", [([1, 2, 0, 1, 3], 200, 3176), ([1, 2, 0, 1, 3], 3176, 72), ([16], 264, 8200), ([1, 0, 1], 4104, 136)])
+def test_few_tiles_of_a_long_sum(counts, d, F, dtype, act):
+    """Tiles whose sum the wavefronts share, several to a workgroup; parts of the sum with one stage, with many, with none."""
+    import paper_2605_11537_amd as moe
+    K = sum(counts)
+    s = inputs(dtype, counts, K + 2, d, F, K + d + F)
+    s["x"][K:], s["dy"][K:] = float("nan"), float("nan")
+    y, states = moe.moe_gated_ffn(s["x"], *s["w"], s["offset"], ACT[act], want_states=True)
+    grads = moe.moe_gated_ffn_backward(s["dy"], s["x"], *s["w"], states, s["offset"], ACT[act])
+    check(s, dtype, act, y, grads)
+    for _ in range(2):
+        again = moe.moe_gated_ffn_backward(s["dy"], s["x"], *s["w"], states, s["offset"], ACT[act])
+        assert torch.equal(moe.moe_gated_ffn(s["x"], *s["w"], s["offset"], ACT[act])[0], y) and all(torch.equal(again[k], grads[k]) for k in grads)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_large_and_special_values(dtype):
     """Gates far on either side, and a NaN and an infinity in one row, which stay in that row (and in the gradients of its expert's weights)."""

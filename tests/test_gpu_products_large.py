@@ -29,6 +29,7 @@ GATED = [
     ("bf16", "silu", [1300, 0, 270, 5, 2049, 700, 1, 300], 768, 1376), ("bf16", "gelu", [5000], 512, 4096), ("bf16", "silu", [16000], 256, 264),
     ("bf16", "relu", [8192], 1024, 4096), ("bf16", "silu", [2100, 900, 1500, 40, 1024, 600, 0, 3000], 1024, 2816), ("bf16", "silu", [20] * 100 + [0] * 20, 256, 2048),
     ("f32", "silu", [91, 8, 16, 94, 0, 30, 10] * 4, 512, 1376), ("f32", "gelu", [3000], 264, 520), ("f32", "silu", [700, 0, 1300, 129], 512, 2048),
+    ("f32", "relu", [2400], 136, 1976), ("f32", "silu", [500, 620, 100], 1544, 1032),
 ]
 
 
@@ -84,7 +85,8 @@ def head_here(s, dtype):
 
 # many tiles of a row, one of each size, dh in many parts, dW in parts of the rows, both in one launch, an odd vocabulary
 HEAD = [("bf16", 3000, 264, 20001, True), ("bf16", 4096, 256, 128, True), ("bf16", 15009, 520, 256, True), ("bf16", 9000, 768, 33001, False),
-        ("bf16", 700, 1024, 9973, False), ("f32", 777, 320, 5003, True), ("f32", 5000, 264, 300, True), ("f32", 2500, 512, 12007, False), ("bf16", 100, 768, 70001, False)]
+        ("bf16", 700, 1024, 9973, False), ("f32", 777, 320, 5003, True), ("f32", 5000, 264, 300, True), ("f32", 2500, 512, 12007, False), ("bf16", 100, 768, 70001, False),
+        ("f32", 900, 136, 6001, True), ("f32", 1400, 72, 5003, False)]
 
 
 @pytest.mark.parametrize("dtype,N,d,V,bias", HEAD, ids=range(len(HEAD)))

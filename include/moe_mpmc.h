@@ -453,7 +453,7 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  *     dz = dlogprob ([v = target] - exp(z - lse)), 0 at padded positions whatever h holds there;
  *     dh = dz w_head,   dw_head = dz^T h,   db_head = sum of dz over the rows  (binary32)
  * The logits are made again, in pieces of the vocabulary: the workspace holds N times a piece, 1 GiB of dz at most (256 ids for very
- * large N), as much of sums and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
+ * large N), as much of dh's sums, N V / 32 bytes of db_head's and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
  * N = 0 dw_head and db_head are zeros.  Sums in binary32 in an order that the sizes fix.
  */
 size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype);

@@ -258,8 +258,9 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
     });
 }
 
-// Tiles of 16 rows x 32 columns, in so few workgroups that a stage's way from memory counts: four wavefronts, each with its quarter of k, its own ring and no
-// barrier while it runs.  One row, 768 x 2048: 6.8 and 7.0 us; with the wavefronts beside each other and one ring 9.8 and 11.0.
+// Tiles of 16 rows x 32 columns (some of binary32: 32 x 64), in so few workgroups that a stage's way from memory counts: four wavefronts, each with its quarter
+// of k, its own ring and no barrier while it runs.  One row, 768 x 2048: 6.8 and 7.0 us; with the wavefronts beside each other and one ring 9.8 and 11.0.  Binary32,
+// 958 rows, 32 experts of 512 x 1376: dx 78 us, 35 TFLOP/s.
 template <int STEP, class TILE>
 __global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
 {
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
 // Few rows of an expert: tiles of 32 or 64 rows x 128 columns (hidden: 64 of both matrices), several small workgroups to a compute unit, whose rings together
 // keep enough of the weights on their way.  Bound by that stream.  768 x 2048: 34 rows of 26 experts 31 and 19 us (5.3 and 4.2 TB/s; of the second
 // there are 156 tiles for 256 compute units); 2181 rows of 128 179 and 83 (4.5 and 4.9).  In binary32 the products cost as much: 958 rows, 32 experts of 512 x
-// 1376, hidden 58 and dx 82 us.
+// 1376, hidden 58 us, 46 TFLOP/s.
 template <int STEP, class TILE>
 __global__ __launch_bounds__(TILE::THREADS, 2) void gated_few_rows_kernel(GatedArgs p)
 {
@@ -464,6 +465,7 @@ template <Order B, int HALVES>
 struct Few<float, B, HALVES> {
     typedef Tile<float, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Mid;
     typedef Mid Low;
+    typedef Tile<float, ALONG_K, B, 32, 64, 1, 1, HALVES, 2> Shared;
     typedef Tile<float, ALONG_K, B, 16, 32 * HALVES, 1, 1, HALVES, HALVES == 2 ? 3 : 5> Tiny;
 };
 
@@ -473,7 +475,11 @@ void launch_step(const GatedArgs &p, hipStream_t st)
     constexpr Order B = STEP == GATED_HIDDEN || STEP == GATED_DOWN ? ACROSS_K : ALONG_K;
     constexpr int HALVES = STEP == GATED_HIDDEN ? 2 : 1;
     typedef Few<T, B, HALVES> few;
-    switch (gated_rows_rule(p.R, p.E, STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d)) {
+    const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
+    const GatedRows rule = gated_rows_rule(p.R, p.E, N);
+    if constexpr (sizeof(T) == 4 && (STEP == GATED_DOWN || STEP == GATED_DX))
+        if ((rule == GATED_LOW || rule == GATED_MID) && gated_few_tiles(p.R, p.E, N)) return launch_tiny<STEP, typename few::Shared>(p, st);
+    switch (rule) {
     case GATED_TALL: launch_rows<STEP, Sizes<T, ALONG_K, B, HALVES>>(p, st); break;
     case GATED_MID: launch_few_rows<STEP, typename few::Mid>(p, st); break;
     case GATED_LOW: launch_few_rows<STEP, typename few::Low>(p, st); break;

@@ -26,6 +26,11 @@ static inline GatedRows gated_rows_rule(int R, int E, int N)
     return R / E <= 32 ? GATED_LOW : GATED_MID;
 }
 
+// Binary32, y and dx, whose columns are few and whose sums are long: where tiles of LOW and MID would not fill the compute units, the wavefronts of narrower
+// ones share their sums.  us of a step, one way, the other: 90 rows of 2048 x 512 137, 218; 90 rows of 512 x 2048 93, 132; with some 500 tiles, 3000 rows of 64
+// experts, 512 x 1024, 495, 462.
+static inline bool gated_few_tiles(int R, int E, int N) { return ((long long)R / 32 + (R < E ? R : E) / 2) * ceil_div(N, 128) <= 256; }
+
 // Parts of an expert's rows for the weights' gradients: where even an eighth of a tile each would leave compute units without work, and rows are many.
 static inline int gated_parts(int R, int E, int d, int F, int dtype)
 {

@@ -145,35 +145,12 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
                 j.b[0] = source_along(p.w_gate, w + (size_t)j.n0 * f_bytes, f_bytes, j.columns, TILE::HALF_N);
                 j.b[1] = source_along(p.w_up, w + (size_t)j.n0 * f_bytes, f_bytes, j.columns, TILE::HALF_N);
             }
-            if constexpr (SPLIT > 1) {
-                const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = (tiles_of(j.k, SPLIT) + TILE::STAGE_K - 1) / TILE::STAGE_K * TILE::STAGE_K;
-                const int k0 = wave * part, along = k0 * Z, b_skip = TILE::B_ORDER == ALONG_K ? 1 : ldb;
-                for (int i = 0; i < 2; ++i) {
-                    j.a[i].base += along;
-                    j.a[i].records -= along;
-                    j.b[i].base += TILE::B_ORDER == ALONG_K ? (size_t)along : (size_t)k0 * b_skip;
-                    if (TILE::B_ORDER == ALONG_K) j.b[i].records -= along;
-                }
-                j.k = j.k - k0 < part ? (j.k - k0 > 0 ? j.k - k0 : 0) : part;
-            }
+            if constexpr (SPLIT > 1) share_k<TILE, SPLIT>(j, ldb);
             return true;
         },
         [&](const Job &j, typename TILE::Sums &sums) {
-            if constexpr (SPLIT > 1) {
-                constexpr int N = TILE::HALVES * TILE::MB * TILE::NB;
-                const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-                product_f32x4 *const mine = &sums[0][0][0];
-                __syncthreads();               // the sums of the tile before have been read
-                if (wave > 0)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) shared[((wave - 1) * N + i) * 64 + lane] = mine[i];
-                __syncthreads();
-                if (wave > 0) return;
-#pragma unroll
-                for (int w = 0; w < SPLIT - 1; ++w)
-#pragma unroll
-                    for (int i = 0; i < N; ++i) mine[i] += shared[(w * N + i) * 64 + lane];
-            }
+            if constexpr (SPLIT > 1)
+                if (!join_sums<TILE, SPLIT>(sums, shared)) return;
             if constexpr (STEP == GATED_HIDDEN) {
                 const Writer<TILE, T> h(tile, (T *)p.h + (size_t)j.m0 * p.F + j.n0, f_bytes, j.rows, j.columns);
                 float *const gu = gated_states(tile, tiles, j, p);
@@ -266,7 +243,7 @@ __global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
 {
     constexpr int SPLIT = 4;
     __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
-    __shared__ product_f32x4 shared[(SPLIT - 1) * TILE::HALVES * TILE::MB * TILE::NB * 64];
+    __shared__ product_f32x4 shared[SHARED_SUMS<TILE, SPLIT>];
     __shared__ int tables[3][MAX_GROUPS + 1];
     const RowTiles tiles = {tables[0], tables[1], tables[2], p.offset, p.E, p.R, TILE::BM};
     tiles.count();

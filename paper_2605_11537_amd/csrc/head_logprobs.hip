@@ -73,8 +73,10 @@ __device__ __forceinline__ bool holds_column(int in)
 }
 
 // `units` of the parts of n_m x n_n tiles of BIG_M x BIG_N, from tile `first` on (below likewise); here all have BIG_N columns, for which a row has one slot.
-template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, float2 *parts, int n_m, int n_n, int first, Units units, int tall)
+// SPLIT: the workgroup's wavefronts share a tile's k.
+template <class TILE, int BIG_M, int BIG_N, int SPLIT = 1>
+__device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, float2 *parts, int n_m, int n_n, int first, Units units, int tall,
+                                             product_f32x4 *shared = nullptr)
 {
     typedef typename TILE::T T;
     constexpr int WN = TILE::BN / TILE::WAVE_N, PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
@@ -95,14 +97,18 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
             j.runs = 1;
             j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
             j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
+            if constexpr (SPLIT > 1) share_k<TILE, SPLIT>(j, d_bytes);
             return true;
         },
         [&](const Job &j, typename TILE::Sums &z) {
-            add_bias(tile, j, p.b, p.V, z);
+            bool mine = true;
+            if constexpr (SPLIT > 1) mine = join_sums<TILE, SPLIT>(z, shared);
+            if (mine) add_bias(tile, j, p.b, p.V, z);
             const int lane = threadIdx.x & 63;
             int targets[TILE::MB];
 #pragma unroll
-            for (int mb = 0; mb < TILE::MB; ++mb) targets[mb] = tile.of_row(mb) < j.rows ? p.target[j.m0 + tile.of_row(mb)] : -1;
+            for (int mb = 0; mb < TILE::MB; ++mb) targets[mb] = mine && tile.of_row(mb) < j.rows ? p.target[j.m0 + tile.of_row(mb)] : -1;
+            if (mine)
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
                 const int row = tile.of_row(mb), target = targets[mb];
@@ -170,6 +176,21 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
     head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
 
+// As tiles of 16 rows x 32 columns, where these are few (a predictor's head over its experts, a few tokens): four wavefronts share a tile's k, and
+// nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more: 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
+// 68, 136, in bfloat16 35, 45; 1000 x 256 x 128 34, 38; 4096 x 256 x 8 40, 39.
+template <class TILE>
+__global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)
+{
+    constexpr int SPLIT = 4;
+    __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
+    __shared__ product_f32x4 shared[SHARED_SUMS<TILE, SPLIT>];
+    __shared__ float2 parts[TILE::BM];
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
+    char *const ring = smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * TILE::LDS;
+    head_forward<TILE, TILE::BM, TILE::BN, SPLIT>(p, ring, parts, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
+}
+
 // A row's tiles' maxima and sums -> lse and the target's log probability.  ROWS rows to a workgroup of four wavefronts: one each, or with few rows, whose
 // tiles would be many trips one behind another, all four on one (3 x 131072: 5 us, one wavefront 7.7).
 template <int ROWS>
@@ -219,15 +240,16 @@ struct DZ {
     static constexpr int COLUMNS = HEAD_DZ_ROW / (int)sizeof(T);
 };
 
-template <class TILE, int BIG_M, int BIG_N>
-__device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall)
+template <class TILE, int BIG_M, int BIG_N, int SPLIT = 1>
+__device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int n_m, int n_n, int first, Units units, int tall,
+                                             product_f32x4 *shared = nullptr)
 {
     typedef typename TILE::T T;
     constexpr int PARTS_N = BIG_N / TILE::BN, PARTS = BIG_M / TILE::BM * PARTS_N;
     const unsigned d_bytes = p.d * sizeof(T);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     const float largest = *p.largest;
-    tile.template run<TILE::MB * Writer<TILE, T>::STORES>(
+    tile.template run<SPLIT == 1 ? TILE::MB * Writer<TILE, T>::STORES : 0>(
         [&](Job &j) {
             int u, m, n;
             do {
@@ -243,9 +265,12 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
             j.runs = 1;
             j.a[0] = source_along(p.h, (size_t)j.m0 * d_bytes, d_bytes, j.rows, TILE::BM);
             j.b[0] = source_along(p.w, (size_t)j.n0 * d_bytes, d_bytes, j.columns, TILE::BN);
+            if constexpr (SPLIT > 1) share_k<TILE, SPLIT>(j, d_bytes);
             return true;
         },
         [&](const Job &j, typename TILE::Sums &z) {
+            if constexpr (SPLIT > 1)
+                if (!join_sums<TILE, SPLIT>(z, shared)) return;
             add_bias(tile, j, p.b, p.V, z);
             const int at = j.n0 - p.v0;        // behind the last id there are zeros up to the tile's end
             const Writer<TILE, T> to(tile, (T *)p.dz + ((size_t)(at / DZ<T>::COLUMNS) * p.N + j.m0) * DZ<T>::COLUMNS + at % DZ<T>::COLUMNS, HEAD_DZ_ROW, j.rows, TILE::BN);
@@ -317,6 +342,16 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_dlogits_few_kernel(Head
     __shared__ __align__(1024) char smem[TILE::LDS];
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
     head_dlogits<TILE, TILE::BM, TILE::BN>(p, smem, n_m, n_n, 0, Units(n_m * n_n), 8);
+}
+template <class TILE>
+__global__ __launch_bounds__(4 * WAVE) void head_dlogits_tiny_kernel(HeadArgs p)
+{
+    constexpr int SPLIT = 4;
+    __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
+    __shared__ product_f32x4 shared[SHARED_SUMS<TILE, SPLIT>];
+    const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.columns, TILE::BN);
+    char *const ring = smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * TILE::LDS;
+    head_dlogits<TILE, TILE::BM, TILE::BN, SPLIT>(p, ring, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
 }
 
 // ------------------------------------------------------------------------------------------------- the two products of the gradient
@@ -650,7 +685,9 @@ dim3 few_grid(long long units, int more_lds)
 template <class T>
 void forward(const HeadArgs &p, int N, float *logprob, float *lse, hipStream_t st)
 {
-    HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
+    typedef Tile<T, ALONG_K, ALONG_K, HEAD_TINY_ROWS, HEAD_TINY_COLUMNS, 1, 1, 1, 5> tiny;
+    if (head_tiny(N, p.V)) hipLaunchKernelGGL(head_forward_tiny_kernel<tiny>, few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS), dim3(4 * WAVE), 0, st, p);
+    else HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
     if (N <= 512 && p.n_n > 64) hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
     else hipLaunchKernelGGL(head_join_kernel<4>, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
 }
@@ -671,7 +708,9 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     for (int v0 = 0; v0 < p.V; v0 += g.piece) {
         p.v0 = v0;
         p.columns = p.V - v0 < g.piece ? p.V - v0 : g.piece;
-        HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
+        typedef Tile<T, ALONG_K, ALONG_K, HEAD_TINY_ROWS, HEAD_TINY_COLUMNS, 1, 1, 1, 5> tiny;
+        if (head_tiny(N, p.V)) hipLaunchKernelGGL(head_dlogits_tiny_kernel<tiny>, few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS), dim3(4 * WAVE), 0, st, p);
+        else HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
         q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.v0 = v0;
         q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), DZ<T>::COLUMNS), q.add = v0 > 0;
         q.dh = dh_parts, q.dw = dw, q.largest = largest;

@@ -19,10 +19,17 @@ static inline int head_tile_rows(int N, int dtype)
     return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : 256;
 }
 static inline int head_tile_columns(int N, int dtype) { return head_rows(N, dtype) != HEAD_TALL_TILES ? HEAD_FEW_COLUMNS : dtype == MOE_F32 ? 128 : 256; }
+// The logits, both ways: tiles of 16 rows x 32 columns where a compute unit has one of them at most.
+constexpr int HEAD_TINY_ROWS = 16, HEAD_TINY_COLUMNS = 32, HEAD_TINY_TILES = 256;
+static inline bool head_tiny(int N, int V) { return (long long)ceil_div(N, HEAD_TINY_ROWS) * ceil_div(V, HEAD_TINY_COLUMNS) <= HEAD_TINY_TILES; }
 // forward: slots of maximum and sum that a row has, one for a tile's columns
-static inline int head_row_slots(int N, int V, int dtype) { return ceil_div(V, head_tile_columns(N, dtype)); }
+static inline int head_row_slots(int N, int V, int dtype) { return ceil_div(V, head_tiny(N, V) ? HEAD_TINY_COLUMNS : head_tile_columns(N, dtype)); }
 // backward: rows of a wavefront, for which the bias has a slot of partial sums
-static inline int head_wave_rows(int N, int dtype) { return head_tile_rows(N, dtype) / (head_rows(N, dtype) == HEAD_TALL_TILES ? 2 : 1); }
+static inline int head_wave_rows(int N, int V, int dtype)
+{
+    if (head_tiny(N, V)) return HEAD_TINY_ROWS;
+    return head_tile_rows(N, dtype) / (head_rows(N, dtype) == HEAD_TALL_TILES ? 2 : 1);
+}
 
 // The gradient's pieces and workspace.
 struct HeadShape {
@@ -62,7 +69,7 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     long long dw_parts = pieces == 1 && !g.paired ? slots / (4 * of_dw) : 1;
     if (dw_parts > N / 512) dw_parts = N / 512;
     g.dw_parts = dw_parts < 2 ? 1 : dw_parts > 16 ? 16 : (int)dw_parts;
-    g.db_rows = ceil_div(N, head_wave_rows(N, dtype));
+    g.db_rows = ceil_div(N, head_wave_rows(N, V, dtype));
     g.rows_at = 256;
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
     g.dh_at = g.dz_at + (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW);

@@ -460,6 +460,43 @@ struct Tile {
     }
 };
 
+// SPLIT wavefronts with a tile of their own each (of one wavefront) share a job's k: this one's part of it.  A lies along k.
+template <class TILE, int SPLIT>
+__device__ __forceinline__ void share_k(Job &j, unsigned ldb)
+{
+    constexpr int STAGE_K = TILE::STAGE_K;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = ((j.k + SPLIT - 1) / SPLIT + STAGE_K - 1) / STAGE_K * STAGE_K;
+    const int k0 = wave * part, along = k0 * (int)sizeof(typename TILE::T);
+    for (int i = 0; i < 2; ++i) {
+        j.a[i].base += along;
+        j.a[i].records -= along;               // (of a part without k nothing is read)
+        j.b[i].base += TILE::B_ORDER == ALONG_K ? (size_t)along : (size_t)k0 * ldb;
+        if (TILE::B_ORDER == ALONG_K) j.b[i].records -= along;
+    }
+    j.k = j.k - k0 < part ? (j.k - k0 > 0 ? j.k - k0 : 0) : part;
+}
+template <class TILE, int SPLIT>
+constexpr int SHARED_SUMS = (SPLIT - 1) * TILE::HALVES * TILE::MB * TILE::NB * 64;
+// The first wavefront's sums become all of them together, in their order; -> whether this is the first.  By the whole workgroup.
+template <class TILE, int SPLIT>
+__device__ __forceinline__ bool join_sums(typename TILE::Sums &sums, product_f32x4 *shared)
+{
+    constexpr int N = TILE::HALVES * TILE::MB * TILE::NB;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    product_f32x4 *const mine = &sums[0][0][0];
+    __syncthreads();                           // the sums of the tile before have been read
+    if (wave > 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) shared[((wave - 1) * N + i) * 64 + lane] = mine[i];
+    __syncthreads();
+    if (wave > 0) return false;
+#pragma unroll
+    for (int w = 0; w < SPLIT - 1; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) mine[i] += shared[(w * N + i) * 64 + lane];
+    return true;
+}
+
 // Where a tile's rows go, in U: row(mb, v) writes the columns `from` .. columns-1 of block row mb.  bfloat16: two blocks' lane groups exchange their halves,
 // so that a lane has 16 bytes to write and a row's four lanes 64 in a run; every lane of the wavefront has to be there.  What is not in D goes to an offset
 // behind the buffer's end, so that a row is always the same number of stores.

@@ -48,6 +48,10 @@ def check(got, want, bias):
 CASES = [
     (1, 8, 1, 0.0), (1, 8, 2, 0.0), (1, 768, 5003, 0.0), (3, 64, 20001, 0.0), (15, 72, 127, 0.2), (16, 128, 129, 0.0), (17, 136, 255, 0.3), (64, 64, 64, 1.0), (65, 200, 257, 0.1),
     (129, 256, 128, 0.05), (255, 264, 1003, 0.5), (257, 512, 513, 0.1), (700, 40, 2049, 0.1), (40, 1032, 300, 0.0), (2000, 16, 8, 0.1), (333, 8, 33, 0.0),
+    # the wavefronts share a tile's sum: parts with one stage, many and none, as many tiles as compute units and one more row of them
+    (18, 2048, 8, 0.1), (1, 2056, 8192, 0.0), (130, 1032, 500, 0.1), (4096, 72, 32, 0.1), (4097, 72, 32, 0.1), (2, 8, 8193, 0.0),
+    # just beyond: tiles of 16, 64 and more rows
+    (16, 24, 9000, 0.1), (100, 136, 1500, 0.1), (150, 40, 1003, 0.1), (350, 72, 400, 0.1),
 ]
 
 
@@ -72,15 +76,15 @@ def test_scores_and_gradient(N, d, V, padded, dtype, bias):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [5, 90, 300])
-def test_masked_ids_and_padded_rows(N, dtype):
+@pytest.mark.parametrize("N,V", [(5, 400), (90, 400), (300, 400), (12, 9000), (90, 4000), (300, 1500)])
+def test_masked_ids_and_padded_rows(N, V, dtype):
     """Biases of -infinity and of the lowest value; rows of NaN and infinity at padded positions, and targets past the vocabulary, leave no trace."""
     import paper_2605_11537_amd as moe
-    s = inputs(dtype, N, 64, 400, True, 0.2, N)
+    s = inputs(dtype, N, 64, V, True, 0.2, N)
     s["b"][::3], s["b"][1::7] = -float("inf"), torch.finfo(torch.float32).min
-    s["target"][0], s["target"][1], s["target"][2], s["target"][3] = 400, 2 ** 31 - 1, -2 ** 31, 3      # the last one is masked
+    s["target"][0], s["target"][1], s["target"][2], s["target"][3] = V, 2 ** 31 - 1, -2 ** 31, 3      # the last one is masked
     clean = want_of(s, dtype)
-    off = (s["target"] < 0) | (s["target"] >= 400)
+    off = (s["target"] < 0) | (s["target"] >= V)
     s["h"][off] = float("nan")
     s["h"][1] = float("inf")
     got = run(moe, s)
@@ -97,10 +101,10 @@ def test_masked_ids_and_padded_rows(N, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [3, 100, 200])
-def test_everything_masked(N, dtype):
+@pytest.mark.parametrize("N,V", [(3, 77), (100, 77), (200, 77), (3, 9000), (100, 2000), (200, 1000)])
+def test_everything_masked(N, V, dtype):
     import paper_2605_11537_amd as moe
-    s = inputs(dtype, N, 32, 77, True, 0.3, N)
+    s = inputs(dtype, N, 32, V, True, 0.3, N)
     s["b"].fill_(-float("inf"))
     got = run(moe, s)
     on = s["target"] >= 0
@@ -125,9 +129,10 @@ def test_equal_weights_and_no_gradient(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_nan_and_infinity_stay_in_their_row(dtype):
+@pytest.mark.parametrize("V", [300, 1300])
+def test_nan_and_infinity_stay_in_their_row(V, dtype):
     import paper_2605_11537_amd as moe
-    s = inputs(dtype, 150, 64, 300, False, 0.0, 10)
+    s = inputs(dtype, 150, 64, V, False, 0.0, 10)
     good = run(moe, s)
     s["h"][4, 3], s["h"][149, 0] = float("nan"), float("inf")
     got = run(moe, s)

@@ -594,9 +594,11 @@ void launch_clear(void *p, size_t bytes, hipStream_t st)
     hipLaunchKernelGGL(head_clear_kernel, dim3((unsigned)(words / 256 < 2048 ? words / 256 + 1 : 2048)), dim3(256), 0, st, (unsigned *)p, words);
 }
 
-// tiles of 64 and of 16 rows
+// tiles of 64, 32 (binary32 only) and 16 rows
 template <class T, Order A, Order B>
 using Flat = Tile<T, A, B, 64, HEAD_FEW_COLUMNS, 1, 4, 1, 2, A == ALONG_K && B == ACROSS_K ? DZ<T>::COLUMNS : 0>;
+template <class T, Order A, Order B>
+using Low = Tile<T, A, B, sizeof(T) == 4 ? 32 : 64, HEAD_FEW_COLUMNS, 1, 4, 1, 2, A == ALONG_K && B == ACROSS_K ? DZ<T>::COLUMNS : 0>;
 template <class T, Order A, Order B>
 using Few = Tile<T, A, B, 16, HEAD_FEW_COLUMNS, 1, 4, 1, 2, A == ALONG_K && B == ACROSS_K ? DZ<T>::COLUMNS : 0>;
 
@@ -660,14 +662,15 @@ dim3 few_grid(long long units, int more_lds)
     return dim3((unsigned)(((units < most ? units : most) + 7) / 8 * 8));
 }
 
-// KERNEL for tiles of PARTS' sizes, or KERNEL_few for tiles of 64 or 16 rows, by the number of rows; M, N, TIMES: D and how often
+// KERNEL for tiles of PARTS' sizes, or KERNEL_few for tiles of 64, 32 or 16 rows, by the number of rows; M, N, TIMES: D and how often
 #define HEAD_BY_ROWS(KERNEL, PARTS, A, B, ARGS, ST, M, N, TIMES, LDS_ROWS)                                                                            \
     do {                                                                                                                                       \
         typedef PARTS<T> sizes;                                                                                                                \
         typedef typename Whole<sizes>::Tile big;                                                                                               \
         typedef Flat<T, A, B> flat;                                                                                                            \
+        typedef Low<T, A, B> low;                                                                                                              \
         typedef Few<T, A, B> few;                                                                                                              \
-        const HeadRows rows = head_rows(M, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);                                                                                                   \
+        const HeadRows rows = head_rows(M, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);                                                               \
         if (rows == HEAD_TALL_TILES)                                                                                                           \
             hipLaunchKernelGGL((KERNEL##_kernel<sizes>),                                                                                       \
                                dim3(product_grid((long long)TIMES * tiles_of(M, big::BM) * tiles_of(N, big::BN), PRODUCT_CUS * sizes::PER_CU)), \
@@ -676,6 +679,10 @@ dim3 few_grid(long long units, int more_lds)
             hipLaunchKernelGGL((KERNEL##_few_kernel<flat>),                                                                                    \
                                few_grid<flat>((long long)TIMES * tiles_of(M, flat::BM) * tiles_of(N, flat::BN), LDS_ROWS * flat::BM),          \
                                dim3(flat::THREADS), 0, ST, ARGS);                                                                              \
+        else if (rows == HEAD_LOW_TILES)                                                                                                       \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<low>),                                                                                     \
+                               few_grid<low>((long long)TIMES * tiles_of(M, low::BM) * tiles_of(N, low::BN), LDS_ROWS * low::BM),             \
+                               dim3(low::THREADS), 0, ST, ARGS);                                                                              \
         else                                                                                                                                   \
             hipLaunchKernelGGL((KERNEL##_few_kernel<few>),                                                                                     \
                                few_grid<few>((long long)TIMES * tiles_of(M, few::BM) * tiles_of(N, few::BN), LDS_ROWS * few::BM),              \

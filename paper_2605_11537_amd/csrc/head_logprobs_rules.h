@@ -10,13 +10,19 @@ constexpr size_t HEAD_PIECE_BYTES = 1u << 30;    // of dz, and of the parts of d
 constexpr int HEAD_DZ_ROW = 512;               // bytes of a row of dz in one of its blocks
 constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 
-enum HeadRows { HEAD_FEW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };
-// (binary32 is bound by the matrix pipes: 192 rows are three tiles of 64, of 128 two with a quarter of nothing)
-static inline HeadRows head_rows(int N, int dtype) { return N <= 16 ? HEAD_FEW_TILES : N <= (dtype == MOE_F32 ? 192 : 128) ? HEAD_FLAT_TILES : HEAD_TALL_TILES; }
+enum HeadRows { HEAD_FEW_TILES, HEAD_LOW_TILES, HEAD_FLAT_TILES, HEAD_TALL_TILES };      // of 16, 32, 64 rows and more
+// (binary32 is bound by the matrix pipes, and rows behind the last cost as much as others: 192 rows are three tiles of 64, of 128 two with a quarter of
+// nothing, and up to 32 rows of a last tile are a tile of 32: 20 x 704 x 45094 with gradient 160 us, in tiles of 64 220; 129 x 512 x 21296 174, 184)
+static inline HeadRows head_rows(int N, int dtype)
+{
+    if (N <= 16) return HEAD_FEW_TILES;
+    if (N > (dtype == MOE_F32 ? 192 : 128)) return HEAD_TALL_TILES;
+    return dtype == MOE_F32 && (N - 1) % 64 < 32 ? HEAD_LOW_TILES : HEAD_FLAT_TILES;
+}
 static inline int head_tile_rows(int N, int dtype)
 {
     const HeadRows r = head_rows(N, dtype);
-    return r == HEAD_FEW_TILES ? 16 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : 256;
+    return r == HEAD_FEW_TILES ? 16 : r == HEAD_LOW_TILES ? 32 : r == HEAD_FLAT_TILES ? 64 : dtype == MOE_F32 ? 128 : 256;
 }
 static inline int head_tile_columns(int N, int dtype) { return head_rows(N, dtype) != HEAD_TALL_TILES ? HEAD_FEW_COLUMNS : dtype == MOE_F32 ? 128 : 256; }
 // The logits, both ways: tiles of 16 rows x 32 columns where a compute unit has one of them at most.

@@ -51,7 +51,7 @@ CASES = [
     # the wavefronts share a tile's sum: parts with one stage, many and none, as many tiles as compute units and one more row of them
     (18, 2048, 8, 0.1), (1, 2056, 8192, 0.0), (130, 1032, 500, 0.1), (4096, 72, 32, 0.1), (4097, 72, 32, 0.1), (2, 8, 8193, 0.0),
     # just beyond: tiles of 16, 64 and more rows
-    (16, 24, 9000, 0.1), (100, 136, 1500, 0.1), (150, 40, 1003, 0.1), (350, 72, 400, 0.1),
+    (16, 24, 9000, 0.1), (100, 136, 1500, 0.1), (150, 40, 1003, 0.1), (350, 72, 400, 0.1), (20, 264, 6000, 0.1), (70, 136, 3001, 0.1), (130, 40, 2000, 0.1), (191, 24, 1500, 0.1),
 ]
 
 

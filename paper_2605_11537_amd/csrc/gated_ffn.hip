@@ -235,11 +235,11 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void gated_rows_kernel(Ga
     });
 }
 
-// Tiles of 16 rows x 32 columns (some of binary32: 32 x 64), in so few workgroups that a stage's way from memory counts: four wavefronts, each with its quarter
-// of k, its own ring and no barrier while it runs.  One row, 768 x 2048: 6.8 and 7.0 us; with the wavefronts beside each other and one ring 9.8 and 11.0.  Binary32,
-// 958 rows, 32 experts of 512 x 1376: dx 78 us, 35 TFLOP/s.
+// Tiles of 16 rows x 32 columns or 32 x 64 (hidden: 32 of both matrices), in so few workgroups that a stage's way from memory counts: four wavefronts, each with
+// its quarter of k, its own ring and no barrier while it runs.  One row, 768 x 2048: 6.8 and 7.0 us; with the wavefronts beside each other and one ring 9.8 and
+// 11.0.  Forward of 60 rows, 768 x 2048, 18 us, in tiles of 64 x 128 34.  Binary32, 958 rows, 32 experts of 512 x 1376: dx 78 us, 35 TFLOP/s.
 template <int STEP, class TILE>
-__global__ __launch_bounds__(4 * WAVE) void gated_tiny_kernel(GatedArgs p)
+__global__ __launch_bounds__(4 * WAVE) void gated_shared_kernel(GatedArgs p)
 {
     constexpr int SPLIT = 4;
     __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
@@ -416,11 +416,11 @@ void launch_few_rows(const GatedArgs &p, hipStream_t st)
     hipLaunchKernelGGL((gated_few_rows_kernel<STEP, TILE>), dim3((unsigned)((grid + 7) / 8 * 8)), dim3(TILE::THREADS), 0, st, p);
 }
 template <int STEP, class TILE>
-void launch_tiny(const GatedArgs &p, hipStream_t st)
+void launch_shared(const GatedArgs &p, hipStream_t st)
 {
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
     const long long units = ((long long)p.R / TILE::BM + (p.E < p.R ? p.E : p.R)) * tiles_of(N, TILE::HALF_N);
-    hipLaunchKernelGGL((gated_tiny_kernel<STEP, TILE>), dim3((unsigned)(((units < PRODUCT_CUS ? units : PRODUCT_CUS) + 7) / 8 * 8)), dim3(4 * WAVE), 0, st, p);
+    hipLaunchKernelGGL((gated_shared_kernel<STEP, TILE>), dim3((unsigned)(((units < PRODUCT_CUS ? units : PRODUCT_CUS) + 7) / 8 * 8)), dim3(4 * WAVE), 0, st, p);
 }
 template <bool DOWN, class SIZES>
 void launch_weights(const GatedArgs &p, hipStream_t st)
@@ -434,8 +434,10 @@ template <class T, Order B, int HALVES>
 struct Few;
 template <Order B, int HALVES>
 struct Few<bf16_t, B, HALVES> {
+    typedef Tile<bf16_t, ALONG_K, B, 64, 64, 2, 2, HALVES, 3> Small;
     typedef Tile<bf16_t, ALONG_K, B, 64, 128, 1, 4, HALVES> Mid;
     typedef Tile<bf16_t, ALONG_K, B, 32, 128, 1, 4, HALVES, 3> Low;
+    typedef Tile<bf16_t, ALONG_K, B, 32, 64, 1, 1, HALVES, 2> Shared;
     typedef Tile<bf16_t, ALONG_K, B, 16, 32 * HALVES, 1, 1, HALVES, HALVES == 2 ? 3 : 5> Tiny;
 };
 template <Order B, int HALVES>
@@ -453,14 +455,18 @@ void launch_step(const GatedArgs &p, hipStream_t st)
     constexpr int HALVES = STEP == GATED_HIDDEN ? 2 : 1;
     typedef Few<T, B, HALVES> few;
     const int N = STEP == GATED_HIDDEN || STEP == GATED_DHIDDEN ? p.F : p.d;
-    const GatedRows rule = gated_rows_rule(p.R, p.E, N);
-    if constexpr (sizeof(T) == 4 && (STEP == GATED_DOWN || STEP == GATED_DX))
-        if ((rule == GATED_LOW || rule == GATED_MID) && gated_few_tiles(p.R, p.E, N)) return launch_tiny<STEP, typename few::Shared>(p, st);
-    switch (rule) {
-    case GATED_TALL: launch_rows<STEP, Sizes<T, ALONG_K, B, HALVES>>(p, st); break;
-    case GATED_MID: launch_few_rows<STEP, typename few::Mid>(p, st); break;
+    constexpr bool long_sum = STEP == GATED_DOWN || STEP == GATED_DX;          // over F or 2 F, few columns
+    switch (gated_rows_rule(p.R, p.E, N, 64 / HALVES, sizeof(T) == 4 ? MOE_F32 : MOE_BF16, long_sum)) {
+    case GATED_TINY: launch_shared<STEP, typename few::Tiny>(p, st); break;
+    case GATED_SHARED: launch_shared<STEP, typename few::Shared>(p, st); break;
     case GATED_LOW: launch_few_rows<STEP, typename few::Low>(p, st); break;
-    default: launch_tiny<STEP, typename few::Tiny>(p, st);
+    case GATED_MID: launch_few_rows<STEP, typename few::Mid>(p, st); break;
+    case GATED_SMALL:
+        if constexpr (sizeof(T) == 2 && long_sum) {
+            launch_few_rows<STEP, typename few::Small>(p, st);
+            break;
+        }
+    default: launch_rows<STEP, Sizes<T, ALONG_K, B, HALVES>>(p, st);
     }
 }
 

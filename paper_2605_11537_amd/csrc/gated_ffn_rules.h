@@ -14,22 +14,26 @@ static inline size_t states_blocks(int R, int E) { return (size_t)R / 16 + (E < 
 static inline size_t hidden_bytes(int R, int F, int dtype) { return align_up((size_t)R * F * (dtype == MOE_F32 ? 4 : 2), 256); }
 
 // The tile by the rows that an expert has if all have the same (the table is in device memory) and the columns of D.
-//   TINY  16 rows x 32 columns: so few tiles that each has a compute unit to itself, where a stage's way from memory counts
-//   LOW   32 rows, MID 64: bound by the stream of the weights
-//   TALL  up to 256, by the matrix pipes
-// us, one way, the other: 37 rows of 128 experts, 768 x 2048, MID 66, LOW 50; 4096 rows MID 266, LOW 257
-enum GatedRows { GATED_TINY, GATED_LOW, GATED_MID, GATED_TALL };
-static inline GatedRows gated_rows_rule(int R, int E, int N)
+//   TINY    16 rows x 32 columns, whose wavefronts share the sum: so few tiles that each has a compute unit to itself, where a stage's way from memory counts
+//   SHARED  32 x 64 likewise
+//   LOW     32 x 128, MID 64 x 128: bound by the stream of the weights
+//   TALL    up to 256 x 256, by the matrix pipes; SMALL 64 x 64, where the sum is long and such tiles are few
+// us, one way, the other.  Forward of 34 rows of 26 experts, 768 x 2048, MID 66, LOW 50; of 2181 of 128 MID 266, LOW 257.  With gradient, bfloat16, SHARED and what
+// would be without: 30 rows of 1024 x 4096 83, 126 (LOW); 60 of 768 x 2048 58, 109 (MID); 200 69, 91 (TALL); 500 of 512 x 512 46, 59.  SMALL and TALL for y and dx:
+// 700 rows of 1024 x 4096 154, 162; 1334 of 512 x 2048 112, 119; 2000 of 16 experts, 256 x 1376, 103, 114; with 756 tiles, 4000 rows of 768 x 2048, 229, 217.
+// Binary32, whose sums take the longest, y and dx in SHARED with up to 256 tiles of LOW: 90 rows of 2048 x 512 137, 218; of 512 x 2048 93, 132; with some
+// 500, 3000 rows of 64 experts, 512 x 1024, 495, 462.
+enum GatedRows { GATED_TINY, GATED_SHARED, GATED_LOW, GATED_MID, GATED_SMALL, GATED_TALL };
+// columns: of a SHARED tile.  long_sum: y's and dx's products
+static inline GatedRows gated_rows_rule(int R, int E, int N, int columns, int dtype, bool long_sum)
 {
-    if (R / E >= 96) return GATED_TALL;
-    if (R <= 16ll * E && (long long)(R < E ? R : E) * ceil_div(N, 128) <= 128) return GATED_TINY;
+    const long long experts = R < E ? R : E;
+    if (R <= 16ll * E && experts * ceil_div(N, 128) <= 128) return GATED_TINY;
+    if ((R / 32 + experts) * ceil_div(N, columns) <= 256) return GATED_SHARED;
+    if (R / E >= 96) return dtype == MOE_BF16 && long_sum && (R / 64 + experts) * ceil_div(N, 64) <= 512 ? GATED_SMALL : GATED_TALL;
+    if (dtype == MOE_F32 && long_sum && (R / 32 + experts / 2) * ceil_div(N, 128) <= 256) return GATED_SHARED;
     return R / E <= 32 ? GATED_LOW : GATED_MID;
 }
-
-// Binary32, y and dx, whose columns are few and whose sums are long: where tiles of LOW and MID would not fill the compute units, the wavefronts of narrower
-// ones share their sums.  us of a step, one way, the other: 90 rows of 2048 x 512 137, 218; 90 rows of 512 x 2048 93, 132; with some 500 tiles, 3000 rows of 64
-// experts, 512 x 1024, 495, 462.
-static inline bool gated_few_tiles(int R, int E, int N) { return ((long long)R / 32 + (R < E ? R : E) / 2) * ceil_div(N, 128) <= 256; }
 
 // Parts of an expert's rows for the weights' gradients: where even an eighth of a tile each would leave compute units without work, and rows are many.
 static inline int gated_parts(int R, int E, int d, int F, int dtype)
@@ -47,7 +51,7 @@ static inline bool gated_pairs(int R, int E, int d, int F, int dtype, bool down)
     const int big = dtype == MOE_F32 ? 128 : 256, stage = dtype == MOE_F32 ? 32 : 64, slots = dtype == MOE_F32 ? 512 : 256;
     const double n1 = ((double)R / big + E / 2) * ceil_div(down ? F : d, big), cost1 = down ? d / stage + 20 : 2.0 * F / stage + 4;
     const double n2 = (double)E * ceil_div(d, big) * ceil_div(down ? F : 2 * F, big), cost2 = (double)R / E / stage + 5;
-    return gated_rows_rule(R, E, F) == GATED_TALL && n1 * cost1 + n2 * cost2 >= 0.95 * slots * (cost1 > cost2 ? cost1 : cost2);
+    return R / E >= 96 && n1 * cost1 + n2 * cost2 >= 0.95 * slots * (cost1 > cost2 ? cost1 : cost2);
 }
 
 }  // namespace moe

@@ -30,6 +30,9 @@ GATED = [
     ("bf16", "relu", [8192], 1024, 4096), ("bf16", "silu", [2100, 900, 1500, 40, 1024, 600, 0, 3000], 1024, 2816), ("bf16", "silu", [20] * 100 + [0] * 20, 256, 2048),
     ("f32", "silu", [91, 8, 16, 94, 0, 30, 10] * 4, 512, 1376), ("f32", "gelu", [3000], 264, 520), ("f32", "silu", [700, 0, 1300, 129], 512, 2048),
     ("f32", "relu", [2400], 136, 1976), ("f32", "silu", [500, 620, 100], 1544, 1032),
+    # tiles of 64 x 64 for long sums, tiles whose wavefronts share the sum
+    ("bf16", "silu", [1334], 512, 2048), ("bf16", "gelu", [300, 0, 1200, 257, 513], 264, 1376), ("bf16", "relu", [30], 1024, 4096), ("bf16", "silu", [200], 768, 2056),
+    ("f32", "silu", [200], 768, 2056), ("f32", "gelu", [40, 0, 90], 264, 1376),
 ]
 
 

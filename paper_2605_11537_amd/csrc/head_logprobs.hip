@@ -141,10 +141,11 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
                 float m = HEAD_NONE, s = 0.f;
 #pragma unroll
                 for (int w = 0; w < WN; ++w) m = fmaxf(m, parts[w * TILE::BM + row].x);
+                const float beside = finite_or(m, 0.f);
 #pragma unroll
                 for (int w = 0; w < WN; ++w) {
-                    const float2 part = parts[w * TILE::BM + row];
-                    s += part.y * exp_beside(finite_or(part.x, 0.f), finite_or(m, 0.f));
+                    const float2 part = parts[w * TILE::BM + row];         // of masked columns alone: a sum of 0, times 1 and not e^-m
+                    s += part.y * exp_beside(finite_or(part.x, beside), beside);
                 }
                 p.tiles[(size_t)(j.m0 + row) * n_n + j.n0 / TILE::BN] = make_float2(m, s);
             }

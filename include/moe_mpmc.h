@@ -450,8 +450,10 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  * a row's logits makes its numbers NaN.  d a multiple of 8 up to 2^20; any V and N up to 2^24, with N V below 2^41, d V below 2^42 and N d below 2^34.
  *
  * moe_head_logprobs_backward -- from dlogprob [N], with the lse that the forward wrote:
- *     dz = dlogprob ([v = target] - exp(z - lse)), 0 at padded positions whatever h holds there;
+ *     dz = dlogprob ([v = target] - p),  p = exp(z - lse);   0 at padded positions whatever h holds there;
  *     dh = dz w_head,   dw_head = dz^T h,   db_head = sum of dz over the rows  (binary32)
+ * p is taken from lse where lse holds it; where the |lse| of a row is 64 (binary32) or 2048 (bfloat16) and more, rows are summed once
+ * more, so that their p add up to 1 (as in moe_token_logprobs_backward).
  * The logits are made again, in pieces of the vocabulary: the workspace holds N times a piece, 1 GiB of dz at most (256 ids for very
  * large N), as much of dh's sums, N V / 32 bytes of db_head's and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
  * N = 0 dw_head and db_head are zeros.  Sums in binary32 in an order that the sizes fix.

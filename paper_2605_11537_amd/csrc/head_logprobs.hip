@@ -6,6 +6,11 @@
 //
 // dz is rounded once to the tensors' type, as the operand of those products.  It is divided by the largest |dlogprob| first, and dh and dW are multiplied by
 // it in binary32: with the loss a mean all rows have the same dlogprob, which would put the same rounding error on every target's -1.
+//
+// p = e^(z - lse), but lse = m + log s has been rounded, and beside a large m that takes a part of log s or all of it: 64 ids of -1e9 had p = 1 each.  Where a
+// row's |lse| is far from zero the backward call makes all rows' m and s once more (two launches that end at once where none is: 4 us of its 34 at 4096 x 256 x
+// 128, 9 of 1980 at 8192 x 768 x 50257; where one is 44 and 2600 us) and takes p = e^(z - m) / s, so that they add up to one.  The logits
+// are the same bits in all passes: every tile adds an element's k in the same order.
 #include "product.h"
 #include "scalar_math.h"
 #include "head_logprobs_rules.h"
@@ -21,6 +26,8 @@ struct HeadArgs {
     const int32_t *target;
     int N, d, V;
     int v0, columns;                           // backward: the piece's first id, its ids
+    const int *far;                            // whether a row is far from zero; forward: NULL, or whether there is anything to do
+    float2 *again;                             // such rows' maximum and sum, [N]
     int n_n;                                   // forward: slots of a row
     float2 *tiles;                             // forward [N, n_n]: maximum, sum
     float *at_target;                          // forward [N]
@@ -30,6 +37,13 @@ struct HeadArgs {
 };
 
 __device__ __forceinline__ float finite_or(float m, float other) { return m == HEAD_NONE ? other : m; }
+
+// Whether a row's lse does not hold log s: below the limit half a step of it is 2^-19 (binary32) or 2^-14 (bfloat16, whose dz is rounded by 2^-8) at most.
+template <class T>
+__device__ __forceinline__ bool far_from_zero(float lse)
+{
+    return fabsf(lse) >= (sizeof(T) == 4 ? 64.f : 2048.f) && fabsf(lse) < __builtin_inff();
+}
 
 // the tile's logits with their bias; columns behind the vocabulary are masked
 template <class TILE>
@@ -160,6 +174,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     __shared__ float2 parts[4 * Big::BM];
+    if (p.far && !*p.far) return;
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.V, Big::BN);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::BN == Big::BN, "one slot for a row's columns of a tile");
@@ -173,6 +188,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
     __shared__ float2 parts[4 * TILE::BM];
+    if (p.far && !*p.far) return;
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
     head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
@@ -187,17 +203,19 @@ __global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)
     __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
     __shared__ product_f32x4 shared[SHARED_SUMS<TILE, SPLIT>];
     __shared__ float2 parts[TILE::BM];
+    if (p.far && !*p.far) return;
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
     char *const ring = smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * TILE::LDS;
     head_forward<TILE, TILE::BM, TILE::BN, SPLIT>(p, ring, parts, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
 }
 
-// A row's tiles' maxima and sums -> lse and the target's log probability.  ROWS rows to a workgroup of four wavefronts: one each, or with few rows, whose
+// A row's tiles' maxima and sums -> lse and the target's log probability, or with `again` the maximum and the sum.  ROWS rows to a workgroup of four wavefronts: one each, or with few rows, whose
 // tiles would be many trips one behind another, all four on one (3 x 131072: 5 us, one wavefront 7.7).
 template <int ROWS>
 __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, const float *at_target, const int32_t *target, int N, int V, int n_n,
-                                                        float *logprob, float *lse)
+                                                        float *logprob, float *lse, const int *far, float2 *again)
 {
+    if (far && !*far) return;
     constexpr int LANES = 256 / ROWS;
     const int row = blockIdx.x * ROWS + threadIdx.x / LANES, lane = threadIdx.x & 63;
     if (ROWS > 1 && row >= N) return;
@@ -225,6 +243,10 @@ __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, con
         for (int w = 0; w < 4; ++w) s += waves[w].y * exp_of<true>(finite_or(waves[w].x, finite_or(all, 0.f)) - finite_or(all, 0.f));
     }
     if (threadIdx.x % LANES == 0) {
+        if (again) {
+            again[row] = make_float2(all, s);
+            return;
+        }
         const float beside = finite_or(all, 0.f), l = logf(s);         // -infinity where every id is masked
         lse[row] = beside + l;
         const int id = target[row];
@@ -250,6 +272,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
     const unsigned d_bytes = p.d * sizeof(T);
     const TILE tile((product_lds_t *)smem, d_bytes, d_bytes);
     const float largest = *p.largest;
+    const bool far = *p.far;
     tile.template run<SPLIT == 1 ? TILE::MB * Writer<TILE, T>::STORES : 0>(
         [&](Job &j) {
             int u, m, n;
@@ -277,13 +300,21 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
             const Writer<TILE, T> to(tile, (T *)p.dz + ((size_t)(at / DZ<T>::COLUMNS) * p.N + j.m0) * DZ<T>::COLUMNS + at % DZ<T>::COLUMNS, HEAD_DZ_ROW, j.rows, TILE::BN);
             // what the rows need, asked for at once
             int targets[TILE::MB];
-            float weights[TILE::MB], lses[TILE::MB];
+            float weights[TILE::MB], lses[TILE::MB], shares[TILE::MB];
 #pragma unroll
             for (int mb = 0; mb < TILE::MB; ++mb) {
                 const int row = j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0);
                 targets[mb] = p.target[row];
                 weights[mb] = p.dlogprob[row];
                 lses[mb] = p.lse[row];
+                shares[mb] = 1.f;
+            }
+            if (far) {                         // uniform
+#pragma unroll
+                for (int mb = 0; mb < TILE::MB; ++mb) {
+                    const float2 again = p.again[j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0)];
+                    if (far_from_zero<T>(lses[mb])) lses[mb] = again.x, shares[mb] = 1.f / again.y;
+                }
             }
             product_f32x4 down[TILE::NB];      // sums over this lane's rows
 #pragma unroll
@@ -293,11 +324,12 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
                 const int target = tile.of_row(mb) < j.rows ? targets[mb] : -1;
                 const bool on = target >= 0 && target < p.V;
                 const float g = on ? weights[mb] / largest : 0.f, lse = on ? finite_or(lses[mb], 0.f) : 0.f;
+                const float gp = g * shares[mb];
                 product_f32x4 dz[TILE::NB];
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dz[nb][i] = on ? -g * exp_beside(z[0][mb][nb][i], lse) : 0.f;
+                    for (int i = 0; i < 4; ++i) dz[nb][i] = on ? -gp * exp_beside(z[0][mb][nb][i], lse) : 0.f;
                 const int in = target - j.n0 - tile.wn * TILE::WAVE_N;
                 if (on && holds_column<TILE>(in)) {
 #pragma unroll
@@ -514,10 +546,12 @@ __global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGr
 }
 
 // ------------------------------------------------------------------------------------------------- rows
-// What the backward calls begin with.  The first workgroup: the largest |dlogprob| of a row that counts; 1 where that is 0 or no number.  The others, with `to`:
+// What the backward calls begin with.  The first workgroup: the largest |dlogprob| of a row that counts; 1 where that is 0 or no number; whether such a row is
+// far from zero.  The others, with `to`:
 // h with zeros for the padded rows, which may hold anything: what dW's sums are made of.  pieces: of 16 bytes, to a row
-__global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, const float *dlogprob, int N, int V, float *largest, const uint4 *h, int pieces,
-                                                         uint4 *to)
+template <class T>
+__global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, const float *dlogprob, const float *lse, int N, int V, float *largest, int *far,
+                                                         const uint4 *h, int pieces, uint4 *to)
 {
     if (blockIdx.x > 0) {
         const size_t total = (size_t)N * pieces, step = (size_t)(gridDim.x - 1) * 512;
@@ -529,12 +563,14 @@ __global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, 
     }
     __shared__ float waves[8];
     float m = 0.f;
+    bool any = false;
 #pragma unroll 8
     for (int i = threadIdx.x; i < N; i += 512) {
         const int id = target[i];
-        const float g = fabsf(dlogprob[i]);
-        if (id >= 0 && id < V) m = fmaxf(m, g);
+        const float g = fabsf(dlogprob[i]), l = lse[i];
+        if (id >= 0 && id < V) m = fmaxf(m, g), any |= far_from_zero<T>(l);
     }
+    any = __syncthreads_or(any);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
@@ -542,6 +578,7 @@ __global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, 
     if (threadIdx.x == 0) {
         for (int w = 1; w < 8; ++w) m = fmaxf(m, waves[w]);
         *largest = m > 0.f && m < __builtin_inff() ? m : 1.f;
+        *far = any;
     }
 }
 
@@ -690,14 +727,19 @@ dim3 few_grid(long long units, int more_lds)
                                dim3(few::THREADS), 0, ST, ARGS);                                                                               \
     } while (0)
 
+// p.tiles, p.at_target -> logprob and lse, or p.again
 template <class T>
-void forward(const HeadArgs &p, int N, float *logprob, float *lse, hipStream_t st)
+void forward(const HeadArgs &p, float *logprob, float *lse, hipStream_t st)
 {
+    const int N = p.N;
     typedef Tile<T, ALONG_K, ALONG_K, HEAD_TINY_ROWS, HEAD_TINY_COLUMNS, 1, 1, 1, 5> tiny;
     if (head_tiny(N, p.V)) hipLaunchKernelGGL(head_forward_tiny_kernel<tiny>, few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS), dim3(4 * WAVE), 0, st, p);
     else HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
-    if (N <= 512 && p.n_n > 64) hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
-    else hipLaunchKernelGGL(head_join_kernel<4>, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse);
+    if (p.tiles == p.again) return;
+    if (N <= 512 && p.n_n > 64)
+        hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse, p.far, p.again);
+    else
+        hipLaunchKernelGGL(head_join_kernel<4>, dim3(tiles_of(N, 4)), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse, p.far, p.again);
 }
 
 template <class T>
@@ -706,12 +748,19 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     const int N = p.N;
     float *const largest = (float *)ws, *const dh_parts = (float *)(ws + g.dh_at), *const db_parts = (float *)(ws + g.db_at);
     p.largest = largest;
+    p.far = (const int *)ws + 1;
+    p.again = (float2 *)(ws + g.again_at);
+    p.n_n = head_row_slots(N, p.V, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);
+    p.at_target = (float *)(ws + g.dz_at);
+    // a row of one tile has its maximum and sum from there
+    p.tiles = p.n_n == 1 ? p.again : (float2 *)(ws + g.dz_at + head_targets_bytes(N));
     p.dz = ws + g.dz_at;
     p.db = db ? db_parts : nullptr;
     const int pieces = p.d * (int)sizeof(T) / 16;
     auto blocks_for = [](size_t work, size_t each) { return (int)(work / each < 2048 ? work / each + 1 : 2048); };
-    hipLaunchKernelGGL(head_begin_kernel, dim3(1 + (dw ? blocks_for((size_t)N * pieces, 512) : 0)), dim3(512), 0, st, p.target, p.dlogprob, N, p.V, largest,
-                       (const uint4 *)p.h, pieces, (uint4 *)(ws + g.rows_at));
+    hipLaunchKernelGGL(head_begin_kernel<T>, dim3(1 + (dw ? blocks_for((size_t)N * pieces, 512) : 0)), dim3(512), 0, st, p.target, p.dlogprob, p.lse, N, p.V, largest,
+                       (int *)ws + 1, (const uint4 *)p.h, pieces, (uint4 *)(ws + g.rows_at));
+    forward<T>(p, nullptr, nullptr, st);       // where a row is far from zero
     HeadGradArgs q = {};
     for (int v0 = 0; v0 < p.V; v0 += g.piece) {
         p.v0 = v0;
@@ -765,7 +814,7 @@ extern "C" size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dty
 {
     (void)d;
     if (N <= 0 || V <= 0) return 0;
-    return align_up((size_t)N * 4, 256) + (size_t)N * head_row_slots(N, V, dtype) * 8;
+    return head_scores_bytes(N, V, dtype);
 }
 
 extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V, int dtype,
@@ -783,9 +832,9 @@ extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float 
     p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.N = N, p.d = d, p.V = V;
     p.n_n = head_row_slots(N, V, dtype);
     p.at_target = (float *)ws;
-    p.tiles = (float2 *)((char *)ws + align_up((size_t)N * 4, 256));
-    if (dtype == MOE_BF16) forward<bf16_t>(p, N, logprob, lse, (hipStream_t)stream);
-    else forward<float>(p, N, logprob, lse, (hipStream_t)stream);
+    p.tiles = (float2 *)((char *)ws + head_targets_bytes(N));
+    if (dtype == MOE_BF16) forward<bf16_t>(p, logprob, lse, (hipStream_t)stream);
+    else forward<float>(p, logprob, lse, (hipStream_t)stream);
     MOE_CHECK_LAUNCH("moe_head_logprobs");
     return MOE_OK;
 }

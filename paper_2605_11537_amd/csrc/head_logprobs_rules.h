@@ -30,6 +30,9 @@ constexpr int HEAD_TINY_ROWS = 16, HEAD_TINY_COLUMNS = 32, HEAD_TINY_TILES = 256
 static inline bool head_tiny(int N, int V) { return (long long)ceil_div(N, HEAD_TINY_ROWS) * ceil_div(V, HEAD_TINY_COLUMNS) <= HEAD_TINY_TILES; }
 // forward: slots of maximum and sum that a row has, one for a tile's columns
 static inline int head_row_slots(int N, int V, int dtype) { return ceil_div(V, head_tiny(N, V) ? HEAD_TINY_COLUMNS : head_tile_columns(N, dtype)); }
+// the logits' maxima and sums, and the targets' logits in front of them
+static inline size_t head_targets_bytes(int N) { return align_up((size_t)N * 4, 256); }
+static inline size_t head_scores_bytes(int N, int V, int dtype) { return head_targets_bytes(N) + (size_t)N * head_row_slots(N, V, dtype) * 8; }
 // backward: rows of a wavefront, for which the bias has a slot of partial sums
 static inline int head_wave_rows(int N, int V, int dtype)
 {
@@ -44,7 +47,7 @@ struct HeadShape {
     int dw_parts;                              // of the rows in dW's sum (one piece only)
     bool paired;                               // dh and dW share a launch
     int db_rows;                               // rows of partial sums for db
-    size_t rows_at, dz_at, dh_at, db_at, dw_at, bytes;
+    size_t again_at, rows_at, dz_at, dh_at, db_at, dw_at, bytes;
 };
 static inline HeadShape head_shape(int N, int d, int V, int dtype)
 {
@@ -76,9 +79,12 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     if (dw_parts > N / 512) dw_parts = N / 512;
     g.dw_parts = dw_parts < 2 ? 1 : dw_parts > 16 ? 16 : (int)dw_parts;
     g.db_rows = ceil_div(N, head_wave_rows(N, V, dtype));
-    g.rows_at = 256;
+    g.again_at = 256;
+    g.rows_at = g.again_at + align_up((size_t)N * 8, 256);
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
-    g.dh_at = g.dz_at + (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW);
+    // before dz is written its place holds what summing the rows again takes
+    const size_t dz = (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW), scores = head_scores_bytes(N, V, dtype);
+    g.dh_at = g.dz_at + align_up(dz > scores ? dz : scores, 256);
     g.db_at = g.dh_at + align_up((size_t)g.parts * N * d * 4, 256);
     g.dw_at = g.db_at + align_up((size_t)g.db_rows * V * 4, 256);
     g.bytes = g.dw_at + (g.dw_parts > 1 ? align_up((size_t)g.dw_parts * V * d * 4, 256) : 0);

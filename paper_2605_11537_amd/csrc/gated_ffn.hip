@@ -22,6 +22,16 @@ namespace {
 constexpr int MAX_GROUPS = MOE_MAX_EXPERTS;
 
 // ------------------------------------------------------------------------------------------------- activations
+// s = 1 / (1 + e^-g) and 1 - s, from an exponential that is at most 1: both keep their relative accuracy, and s reaches 0 (g s would grow again with |g| if it did
+// not).
+template <bool PRECISE>
+__device__ __forceinline__ void sigmoid_of(float g, float &s, float &rest)
+{
+    const float e = exp_of<PRECISE>(-fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e), er = e * r;
+    s = g < 0.f ? er : r;
+    rest = g < 0.f ? r : er;
+}
+
 // e^(-g^2 / 2) and the normal distribution's Phi(g).  For bfloat16 results the rational form of Abramowitz and Stegun, 7.1.26: off by 1.5e-7.
 template <bool PRECISE>
 __device__ __forceinline__ void normal_of(float g, float &bell, float &phi)
@@ -42,7 +52,7 @@ __device__ __forceinline__ float act_of(int activation, float g)
 {
     if (activation == MOE_ACT_SILU) {
         float s, rest;
-        gate_of<PRECISE>(g, 0.f, s, rest);
+        sigmoid_of<PRECISE>(g, s, rest);
         return g * s;
     }
     if (activation == MOE_ACT_GELU) {
@@ -58,7 +68,7 @@ __device__ __forceinline__ float act_of(int activation, float g, float &slope)
 {
     if (activation == MOE_ACT_SILU) {
         float s, rest;
-        gate_of<PRECISE>(g, 0.f, s, rest);
+        sigmoid_of<PRECISE>(g, s, rest);
         slope = s * fmaf(g, rest, 1.f);
         return g * s;
     }

@@ -69,7 +69,7 @@ def activation(name, g):
         erf = _erf if xp is np else xp.erf
         phi, bell = 0.5 * (1 + erf(v * math.sqrt(0.5))), xp.exp(-0.5 * v * v)
         rel = (v * v + 8) * STEP
-        phi_off = 1.5e-7 + 4 * STEP * phi + rel * bell               # the published bound of the rational form, its evaluation, its exponential
+        phi_off = 1.5e-7 + 4 * STEP * phi + rel * bell               # the form of the tail, its evaluation, its exponential
         # slopes at most 1.13 and 0.8
         return (Bounded(v * phi, 1.13 * off + abs(v) * phi_off),
                 Bounded(phi + v * bell / math.sqrt(2 * math.pi), 0.8 * off + phi_off + abs(v) * bell * rel))

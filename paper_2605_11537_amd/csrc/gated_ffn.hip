@@ -32,7 +32,8 @@ __device__ __forceinline__ void sigmoid_of(float g, float &s, float &rest)
     rest = g < 0.f ? r : er;
 }
 
-// e^(-g^2 / 2) and the normal distribution's Phi(g).  For bfloat16 results the rational form of Abramowitz and Stegun, 7.1.26: off by 1.5e-7.
+// e^(-g^2 / 2) and the normal distribution's Phi(g).  For bfloat16 results e^(x^2) erfc(x) = t P(t) with t = 1 / (1 + 0.43 x) and a P of degree 7 that was fitted
+// for the least relative error on 0 <= x <= 9.6 (behind it the bell is no normal number any more): 8.5e-8, evaluated in binary32 4e-7.
 template <bool PRECISE>
 __device__ __forceinline__ void normal_of(float g, float &bell, float &phi)
 {
@@ -41,8 +42,12 @@ __device__ __forceinline__ void normal_of(float g, float &bell, float &phi)
     float tail;                                // erfc(x)
     if (PRECISE) tail = erfcf(x);
     else {
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-        tail = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f) * bell;
+        constexpr float P[8] = {0.242514968f, 0.24436973f, 0.204987422f, 0.246721953f, -0.0854886025f, 0.383441329f, -0.310215741f, 0.0736690089f};
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.43f, x, 1.f));
+        float v = P[7];
+#pragma unroll
+        for (int i = 6; i >= 0; --i) v = fmaf(t, v, P[i]);
+        tail = t * v * bell;
     }
     phi = g < 0.f ? 0.5f * tail : fmaf(-0.5f, tail, 1.f);
 }

@@ -39,7 +39,7 @@ def reference(act, g):
     return a, off_a, slope, off_slope
 
 
-@pytest.mark.parametrize("act", ["silu", "relu"])
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("copies", [1, 30])                          # few rows and many: other tiles
 def test_gates_near_and_far(copies, dtype, act):

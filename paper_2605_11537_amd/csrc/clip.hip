@@ -163,9 +163,10 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipBatch b, c
     double s = 0.;
     for (int i = threadIdx.x; i < n_parts; i += CLIP_THREADS) s += parts[i];
     const double all = sqrt(clip_sum(s));
-    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)all;
-    // a norm that is no finite number scales nothing
-    const float by = all > (double)max_norm && all < __builtin_inf() ? (float)((double)max_norm / all) : 1.f;
+    const float reported = (float)all;
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = reported;
+    // a norm that is no finite number as the caller reads it scales nothing
+    const float by = all > (double)max_norm && reported < __builtin_inff() ? (float)((double)max_norm / all) : 1.f;
     const int chunks = b.chunk[b.n];
     for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const int i = clip_tensor_of(b, c);

@@ -59,13 +59,26 @@ __device__ __forceinline__ double squares(double s, clip_u32x4 v)
     }
     return s;
 }
+// max_norm / norm = by 2^-down.  A quotient near or below the smallest normal number would have lost bits, and the gradients that it brings back into the range
+// with them; by and its products stay inside.
+struct ClipFactor {
+    float by;
+    int down;
+    __device__ __forceinline__ ClipFactor(double f)
+    {
+        down = f >= 0x1p-100 ? 0 : f >= 0x1p-150 ? 64 : 128;
+        by = (float)(down == 0 ? f : f * (down == 64 ? 0x1p64 : 0x1p128));
+    }
+    __device__ __forceinline__ bool one() const { return by == 1.f; }
+    __device__ __forceinline__ float of(float v) const { return __builtin_ldexpf(v * by, -down); }
+};
 template <bool BF16>
-__device__ __forceinline__ clip_u32x4 scaled(clip_u32x4 v, float by)
+__device__ __forceinline__ clip_u32x4 scaled(clip_u32x4 v, ClipFactor f)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (BF16) v[i] = pack_bf16x2(__uint_as_float(v[i] << 16) * by, __uint_as_float(v[i] & 0xffff0000u) * by);
-        else v[i] = __float_as_uint(__uint_as_float(v[i]) * by);
+        if (BF16) v[i] = pack_bf16x2(f.of(__uint_as_float(v[i] << 16)), f.of(__uint_as_float(v[i] & 0xffff0000u)));
+        else v[i] = __float_as_uint(f.of(__uint_as_float(v[i])));
     }
     return v;
 }
@@ -134,7 +147,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_squares_kernel(ClipBatch b,
 }
 
 template <bool BF16>
-__device__ __forceinline__ void clip_chunk_scaled(const char *at, char *to, long long left, bool loose, float by)
+__device__ __forceinline__ void clip_chunk_scaled(const char *at, char *to, long long left, bool loose, ClipFactor f)
 {
     clip_walk(
         left, loose, BF16 ? 2 : 4,
@@ -148,13 +161,13 @@ __device__ __forceinline__ void clip_chunk_scaled(const char *at, char *to, long
 #pragma unroll
             for (int i = 0; i < CLIP_AHEAD; ++i) {
                 const int p = i * CLIP_THREADS + threadIdx.x;
-                // by = 1: bit for bit
-                if (p < pieces) __builtin_nontemporal_store(by == 1.f ? v[i] : scaled<BF16>(v[i], by), reinterpret_cast<clip_u32x4 *>(to + p * 16));
+                // by 1: bit for bit
+                if (p < pieces) __builtin_nontemporal_store(f.one() ? v[i] : scaled<BF16>(v[i], f), reinterpret_cast<clip_u32x4 *>(to + p * 16));
             }
         },
         [&](int i) {
-            if (BF16) ((bf16_t *)to)[i] = by == 1.f ? ((const bf16_t *)at)[i] : f32_to_bf16(bf16_to_f32(((const bf16_t *)at)[i]) * by);
-            else ((unsigned *)to)[i] = by == 1.f ? ((const unsigned *)at)[i] : __float_as_uint(((const float *)at)[i] * by);
+            if (BF16) ((bf16_t *)to)[i] = f.one() ? ((const bf16_t *)at)[i] : f32_to_bf16(f.of(bf16_to_f32(((const bf16_t *)at)[i])));
+            else ((unsigned *)to)[i] = f.one() ? ((const unsigned *)at)[i] : __float_as_uint(f.of(((const float *)at)[i]));
         });
 }
 
@@ -166,17 +179,17 @@ __global__ __launch_bounds__(CLIP_THREADS) void clip_scale_kernel(ClipBatch b, c
     const float reported = (float)all;
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = reported;
     // a norm that is no finite number as the caller reads it scales nothing
-    const float by = all > (double)max_norm && reported < __builtin_inff() ? (float)((double)max_norm / all) : 1.f;
+    const ClipFactor f(all > (double)max_norm && reported < __builtin_inff() ? (double)max_norm / all : 1.);
     const int chunks = b.chunk[b.n];
     for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const int i = clip_tensor_of(b, c);
-        if (by == 1.f && b.from[i] == b.to[i]) continue;
+        if (f.one() && b.from[i] == b.to[i]) continue;
         const long long first = (long long)(c - b.chunk[i]) * CLIP_CHUNK;
         const char *at = (const char *)b.from[i] + first;
         char *to = (char *)b.to[i] + first;
         const bool loose = b.loose[i / 32] >> (i % 32) & 1;
-        if (b.is_bf16[i / 32] >> (i % 32) & 1) clip_chunk_scaled<true>(at, to, b.bytes[i] - first, loose, by);
-        else clip_chunk_scaled<false>(at, to, b.bytes[i] - first, loose, by);
+        if (b.is_bf16[i / 32] >> (i % 32) & 1) clip_chunk_scaled<true>(at, to, b.bytes[i] - first, loose, f);
+        else clip_chunk_scaled<false>(at, to, b.bytes[i] - first, loose, f);
     }
 }
 

@@ -1,6 +1,11 @@
-"""moe_clip_gradients where the norm passes binary32's range."""
+"""moe_clip_gradients where the norm passes binary32's range, and where the factor falls below its smallest normal number.  A scaled element: the factor rounded
+once (2^-24), its product (2^-24), the rounding to the tensor's type (half a step), a result below the smallest normal number twice (a step of 2^-149, in
+bfloat16 2^-133)."""
+import numpy as np
 import pytest
 import torch
+
+from oracle import learning as ol
 
 pytestmark = pytest.mark.gpu
 
@@ -17,3 +22,19 @@ def test_a_norm_above_the_range_scales_nothing(dtype, in_place):
     norm, out = moe.moe_clip_gradients(grads, 1.0, out=grads if in_place else None)
     assert torch.isinf(norm).all() and all(torch.equal(a, b) for a, b in zip(out, kept))
 
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("top,max_norm", [(1e38, 0.01), (1e38, 1e-6), (2e38, 3e-2), (1e30, 1e-20), (1e20, 1e-24), (3e37, 1.0), (1e38, 1e38), (1e-10, 1e-38)])
+def test_small_factors(top, max_norm, dtype):
+    import paper_2605_11537_amd as moe
+    g = torch.Generator(device="cuda").manual_seed(1)
+    powers = torch.linspace(-30, 0, 5003, device="cuda")
+    grads = [(top * 2.0 ** powers * torch.randn(5003, generator=g, device="cuda").clamp(-1, 1) / 40).to(dtype), torch.tensor([top, -top / 3], device="cuda").to(dtype)]
+    want, factor = ol.clip([t.double().cpu().numpy() for t in grads], np.float32(max_norm).item())
+    assert want < 3.4e38 and factor < 1.0
+    norm, out = moe.moe_clip_gradients(grads, max_norm)
+    assert abs(float(norm) - want) <= 2.0 ** -24 * 1.001 * want
+    tiny = 2 * (2.0 ** -149 if dtype == F else 2.0 ** -133)
+    for a, b in zip(grads, out):
+        v = a.double() * factor
+        assert ((b.double() - v).abs() <= v.abs() * (torch.finfo(dtype).eps / 2 + 2.1 * 2.0 ** -24) + tiny).all()

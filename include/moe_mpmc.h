@@ -472,7 +472,7 @@ int moe_head_logprobs_backward(const void *h, const void *w_head, const float *b
  *     out_i = g_i * (max_norm / norm) where norm > max_norm (binary32, rounded once to the tensor's type), else g_i bit for bit.
  * A norm that is infinite or NaN scales nothing: the caller reads it and drops the step.
  * gradients, out, counts (elements) and dtypes are arrays of n entries in HOST memory; the tensors they name are contiguous, aligned to their
- * element only.  out[i] may be gradients[i]; any other overlap with what is written, a tensor named twice among it, is refused.  max_norm above
+ * element only.  out[i] may be gradients[i]; any other overlap with what is written (norm and the workspace too; a tensor named twice) is refused.  max_norm above
  * 0 (infinity: the norm alone, with copies where out differs).  n up to 4096; n = 0 gives norm 0.
  */
 size_t moe_clip_gradients_workspace_bytes(int n);

@@ -238,13 +238,15 @@ extern "C" int moe_clip_gradients(const void *const *gradients, void *const *out
     MOE_REQUIRE(n >= 0, MOE_ERR_INVALID_ARG, "moe_clip_gradients: n=%d", n);
     MOE_REQUIRE(n <= CLIP_MAX_TENSORS, MOE_ERR_UNSUPPORTED, "moe_clip_gradients: n=%d > %d", n, CLIP_MAX_TENSORS);
     MOE_REQUIRE(max_norm > 0.f, MOE_ERR_INVALID_ARG, "moe_clip_gradients: max_norm=%g must be above 0", (double)max_norm);
-    MOE_REQUIRE(norm && (n == 0 || (gradients && out && counts && dtypes)), MOE_ERR_INVALID_ARG, "moe_clip_gradients: null pointer");
+    MOE_REQUIRE(norm && (uintptr_t)norm % 4 == 0 && (n == 0 || (gradients && out && counts && dtypes)), MOE_ERR_INVALID_ARG, "moe_clip_gradients: null or misaligned pointer");
     const size_t need = moe_clip_gradients_workspace_bytes(n);
     MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "moe_clip_gradients: workspace of %zu bytes given, %zu needed",
                 ws ? ws_bytes : 0, need);
     // what is written lies apart from everything else; a gradient may be its own output
-    static thread_local ClipRange ranges[2 * CLIP_MAX_TENSORS];
+    static thread_local ClipRange ranges[2 * CLIP_MAX_TENSORS + 2];
     int m = 0;
+    ranges[m++] = {(uintptr_t)norm, (uintptr_t)norm + 4, true};
+    ranges[m++] = {(uintptr_t)ws, (uintptr_t)ws + need, true};
     for (int i = 0; i < n; ++i) {
         MOE_REQUIRE(dtypes[i] == MOE_F32 || dtypes[i] == MOE_BF16, MOE_ERR_INVALID_ARG, "moe_clip_gradients: unknown dtype %d", dtypes[i]);
         MOE_REQUIRE(counts[i] >= 0 && counts[i] < 1ll << 45, MOE_ERR_INVALID_ARG, "moe_clip_gradients: a tensor of %lld elements", counts[i]);
@@ -260,7 +262,7 @@ extern "C" int moe_clip_gradients(const void *const *gradients, void *const *out
     uintptr_t end = 0, written = 0;
     for (int i = 0; i < m; ++i) {
         MOE_REQUIRE(ranges[i].begin >= (ranges[i].written ? end : written), MOE_ERR_INVALID_ARG,
-                    "moe_clip_gradients: an output lies on another tensor, or one is named twice");
+                    "moe_clip_gradients: an output, norm or the workspace overlaps another tensor, or one is named twice");
         if (ranges[i].end > end) end = ranges[i].end;
         if (ranges[i].written && ranges[i].end > written) written = ranges[i].end;
     }

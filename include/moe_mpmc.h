@@ -426,6 +426,7 @@ int moe_token_logprobs_backward(const void *logits, long long row_stride, const 
  * moe_gated_ffn_backward -- from dy = dL/dy [R, d]:
  *     dh = dy W_down^T  (binary32);   du = dh act(g),  dg = dh u act'(g)  (rounded once);   dx = dg W_gate^T + du W_up^T
  *     dw_gate = x^T dg,  dw_up = x^T du,  dw_down = h^T dy   over an expert's rows; zeros for one without rows
+ * What is written (y, states, the gradients, the workspace) overlaps no other tensor of its call, at any offset: refused.
  * dx [R, d] is left as it was behind the last row.  dx, dw_down and the pair dw_gate, dw_up may be NULL.  Sums are binary32 in an order that the
  * sizes fix.
  */
@@ -456,7 +457,7 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  * more, so that their p add up to 1 (as in moe_token_logprobs_backward).
  * The logits are made again, in pieces of the vocabulary: the workspace holds N times a piece, 1 GiB of dz at most (256 ids for very
  * large N), as much of dh's sums, N V / 32 bytes of db_head's and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
- * N = 0 dw_head and db_head are zeros.  Sums in binary32 in an order that the sizes fix.
+ * N = 0 dw_head and db_head are zeros.  As above, what is written overlaps no other tensor of its call.  Sums in binary32 in an order that the sizes fix.
  */
 size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype);
 int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V,

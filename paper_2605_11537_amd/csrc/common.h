@@ -29,6 +29,24 @@ void set_error(const char *fmt, ...);
     } while (0)
 
 static inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// What a call reads and writes (at: NULL where it has none).  Whether all that is written lies apart from everything else.
+struct Span {
+    const void *at;
+    size_t bytes;
+    bool written;
+};
+template <int N>
+static inline bool spans_apart(const Span (&s)[N])
+{
+    for (int i = 1; i < N; ++i)
+        for (int j = 0; j < i; ++j) {
+            const uintptr_t a = (uintptr_t)s[i].at, b = (uintptr_t)s[j].at;
+            if ((s[i].written || s[j].written) && a && b && a < b + s[j].bytes && b < a + s[i].bytes) return false;
+        }
+    return true;
+}
+
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

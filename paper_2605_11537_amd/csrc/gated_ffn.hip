@@ -563,13 +563,15 @@ extern "C" int moe_gated_ffn(const void *x, const int32_t *expert_offset, const 
     const int rc = gated_check("moe_gated_ffn", R, E, d, F, dtype, activation);
     if (rc != MOE_OK || R == 0) return rc;
     MOE_REQUIRE(x && w_gate && w_up && w_down && y && (expert_offset || E == 1), MOE_ERR_INVALID_ARG, "moe_gated_ffn: null pointer");
-    MOE_REQUIRE(y != x && y != w_gate && y != w_up && y != w_down && y != states && states != x, MOE_ERR_INVALID_ARG,
-                "moe_gated_ffn: an output aliases another tensor");
     MOE_REQUIRE(aligned16(x) && aligned16(w_gate) && aligned16(w_up) && aligned16(w_down) && aligned16(y) && aligned16(states), MOE_ERR_INVALID_ARG,
                 "moe_gated_ffn: tensor misaligned");
     const size_t need = states ? 0 : moe_gated_ffn_workspace_bytes(R, E, d, F, dtype);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE, "moe_gated_ffn: workspace of %zu bytes given, %zu needed",
                 ws ? ws_bytes : 0, need);
+    const size_t z = dtype == MOE_F32 ? 4 : 2, rows = (size_t)R * d * z, weights = (size_t)E * d * F * z;
+    const Span spans[] = {{x, rows, false}, {expert_offset, (E + 1) * sizeof(int32_t), false}, {w_gate, weights, false}, {w_up, weights, false},
+                          {w_down, weights, false}, {y, rows, true}, {states, moe_gated_ffn_states_bytes(R, E, F, dtype), true}, {states ? nullptr : ws, need, true}};
+    MOE_REQUIRE(spans_apart(spans), MOE_ERR_INVALID_ARG, "moe_gated_ffn: an output, the states or the workspace aliases another tensor");
     GatedArgs p = {};
     p.x = x, p.w_gate = w_gate, p.w_up = w_up, p.w_down = w_down, p.offset = expert_offset;
     p.R = R, p.E = E, p.d = d, p.F = F, p.activation = activation;
@@ -590,19 +592,16 @@ extern "C" int moe_gated_ffn_backward(const void *dy, const void *x, const int32
     MOE_REQUIRE(!dw_gate == !dw_up, MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: dw_gate and dw_up come together");
     MOE_REQUIRE((R == 0 || (dy && x && w_gate && w_up && w_down && states)) && (expert_offset || E == 1 || R == 0), MOE_ERR_INVALID_ARG,
                 "moe_gated_ffn_backward: null pointer");
-    const void *in[] = {dy, x, w_gate, w_up, w_down, states};
-    void *out[] = {dx, dw_gate, dw_up, dw_down};
-    for (int i = 0; i < 4; ++i) {
-        for (int j = 0; out[i] && j < 6; ++j)
-            MOE_REQUIRE(out[i] != in[j], MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: an output aliases another tensor");
-        for (int j = 0; out[i] && j < i; ++j)
-            MOE_REQUIRE(out[i] != out[j], MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: an output aliases another tensor");
-        MOE_REQUIRE(aligned16(out[i]), MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: tensor misaligned");
-    }
+    const void *in[] = {dy, x, w_gate, w_up, w_down, states, dx, dw_gate, dw_up, dw_down};
     for (const void *p : in) MOE_REQUIRE(aligned16(p), MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: tensor misaligned");
     const size_t need = moe_gated_ffn_backward_workspace_bytes(R, E, d, F, dtype);
     MOE_REQUIRE(need == 0 || (ws && ws_bytes >= need && aligned16(ws)), MOE_ERR_WORKSPACE,
                 "moe_gated_ffn_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, need);
+    const size_t z = dtype == MOE_F32 ? 4 : 2, rows = (size_t)R * d * z, weights = (size_t)E * d * F * z;
+    const Span spans[] = {{dy, rows, false}, {x, rows, false}, {expert_offset, (E + 1) * sizeof(int32_t), false}, {w_gate, weights, false}, {w_up, weights, false},
+                          {w_down, weights, false}, {states, moe_gated_ffn_states_bytes(R, E, F, dtype), false}, {dx, rows, true}, {dw_gate, weights, true},
+                          {dw_up, weights, true}, {dw_down, weights, true}, {ws, need, true}};
+    MOE_REQUIRE(spans_apart(spans), MOE_ERR_INVALID_ARG, "moe_gated_ffn_backward: an output or the workspace aliases another tensor");
     if (!dw_gate && !dw_down && (!dx || R == 0)) return MOE_OK;        // nothing is wanted
     GatedArgs p = {};
     p.x = x, p.w_gate = w_gate, p.w_up = w_up, p.w_down = w_down, p.dy = dy, p.offset = expert_offset;

@@ -824,10 +824,13 @@ extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float 
     if (rc != MOE_OK || N == 0) return rc;
     MOE_REQUIRE(h && w_head && target && logprob && lse, MOE_ERR_INVALID_ARG, "moe_head_logprobs: null pointer");
     MOE_REQUIRE(aligned16(h) && aligned16(w_head), MOE_ERR_INVALID_ARG, "moe_head_logprobs: tensor misaligned");
-    MOE_REQUIRE(logprob != lse, MOE_ERR_INVALID_ARG, "moe_head_logprobs: logprob aliases lse");
     const size_t need = moe_head_logprobs_workspace_bytes(N, d, V, dtype);
     MOE_REQUIRE(ws && ws_bytes >= need && aligned16(ws), MOE_ERR_WORKSPACE, "moe_head_logprobs: workspace of %zu bytes given, %zu needed",
                 ws ? ws_bytes : 0, need);
+    const size_t z = dtype == MOE_F32 ? 4 : 2;
+    const Span spans[] = {{h, (size_t)N * d * z, false}, {w_head, (size_t)V * d * z, false}, {b_head, (size_t)V * 4, false}, {target, (size_t)N * 4, false},
+                          {logprob, (size_t)N * 4, true}, {lse, (size_t)N * 4, true}, {ws, need, true}};
+    MOE_REQUIRE(spans_apart(spans), MOE_ERR_INVALID_ARG, "moe_head_logprobs: an output or the workspace aliases another tensor");
     HeadArgs p = {};
     p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.N = N, p.d = d, p.V = V;
     p.n_n = head_row_slots(N, V, dtype);
@@ -851,12 +854,17 @@ extern "C" int moe_head_logprobs_backward(const void *h, const void *w_head, con
     const int rc = head_check("moe_head_logprobs_backward", N, d, V, dtype);
     if (rc != MOE_OK) return rc;
     MOE_REQUIRE(N == 0 || (h && w_head && target && lse && dlogprob), MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: null pointer");
-    MOE_REQUIRE((!dh || (dh != h && dh != w_head && dh != dw_head)) && (!dw_head || (dw_head != h && dw_head != w_head)) &&
-                    (!db_head || (db_head != b_head && db_head != lse && db_head != dlogprob)),
-                MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: an output aliases another tensor");
     MOE_REQUIRE(aligned16(h) && aligned16(w_head) && aligned16(dh) && aligned16(dw_head), MOE_ERR_INVALID_ARG,
                 "moe_head_logprobs_backward: tensor misaligned");
     if (!dw_head && !db_head && (!dh || N == 0)) return MOE_OK;        // nothing is wanted
+    const HeadShape g = N > 0 ? head_shape(N, d, V, dtype) : HeadShape();
+    MOE_REQUIRE(N == 0 || (ws && ws_bytes >= g.bytes && aligned16(ws)), MOE_ERR_WORKSPACE,
+                "moe_head_logprobs_backward: workspace of %zu bytes given, %zu needed", ws ? ws_bytes : 0, g.bytes);
+    const size_t z = dtype == MOE_F32 ? 4 : 2, n = (size_t)N * 4;
+    const Span spans[] = {{h, (size_t)N * d * z, false}, {w_head, (size_t)V * d * z, false}, {b_head, (size_t)V * 4, false}, {target, n, false}, {lse, n, false},
+                          {dlogprob, n, false}, {dh, (size_t)N * d * z, true}, {dw_head, (size_t)V * d * z, true}, {db_head, (size_t)V * 4, true},
+                          {ws, N > 0 ? g.bytes : 0, true}};
+    MOE_REQUIRE(spans_apart(spans), MOE_ERR_INVALID_ARG, "moe_head_logprobs_backward: an output or the workspace aliases another tensor");
     hipStream_t st = (hipStream_t)stream;
     if (N == 0) {                              // sums over nothing
         if (dw_head) launch_clear(dw_head, (size_t)V * d * (dtype == MOE_F32 ? 4 : 2), st);
@@ -864,9 +872,6 @@ extern "C" int moe_head_logprobs_backward(const void *h, const void *w_head, con
         MOE_CHECK_LAUNCH("moe_head_logprobs_backward");
         return MOE_OK;
     }
-    const HeadShape g = head_shape(N, d, V, dtype);
-    MOE_REQUIRE(ws && ws_bytes >= g.bytes && aligned16(ws), MOE_ERR_WORKSPACE, "moe_head_logprobs_backward: workspace of %zu bytes given, %zu needed",
-                ws ? ws_bytes : 0, g.bytes);
     HeadArgs p = {};
     p.h = h, p.w = w_head, p.b = b_head, p.target = target, p.lse = lse, p.dlogprob = dlogprob, p.N = N, p.d = d, p.V = V;
     if (dtype == MOE_BF16) backward<bf16_t>(p, g, (char *)ws, (bf16_t *)dh, (bf16_t *)dw_head, db_head, st);

@@ -504,20 +504,23 @@ void backward(const GatedArgs &p, hipStream_t st)
     const int dtype = sizeof(T) == 4 ? MOE_F32 : MOE_BF16;
     GatedArgs q = p;
     q.parts = 1;
-    const bool with_dh = p.dw_down && p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, true);
-    const bool with_dx = p.dw_gate && p.dx && p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, false);
+    // By the sizes alone.  Where only one product of a pair is wanted it has the pair's tiles and parts, so that its sums have the same order.
+    typedef Sizes<T, ALONG_K, ALONG_K> rows;
+    const bool down = p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, true), up = p.R > 0 && gated_pairs(p.R, p.E, p.d, p.F, dtype, false);
     if (p.R > 0) {                             // else zeros for every weight
-        if (with_dh) launch_pair<GATED_DHIDDEN, T>(q, st);
+        if (down && p.dw_down) launch_pair<GATED_DHIDDEN, T>(q, st);
+        else if (down) launch_rows<GATED_DHIDDEN, rows>(q, st);
         else launch_step<GATED_DHIDDEN, T>(p, st);
-        if (with_dx) launch_pair<GATED_DX, T>(q, st);
+        if (up && p.dx && p.dw_gate) launch_pair<GATED_DX, T>(q, st);
+        else if (up && p.dx) launch_rows<GATED_DX, rows>(q, st);
         else if (p.dx) launch_step<GATED_DX, T>(p, st);
     }
-    if (p.dw_gate && !with_dx) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
-    if (p.dw_down && !with_dh) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
-    if (p.parts > 1) {
+    if (p.dw_gate && !(up && p.dx)) launch_weights<false, Sizes<T, ACROSS_K, ACROSS_K>>(up ? q : p, st);
+    if (p.dw_down && !down) launch_weights<true, Sizes<T, ACROSS_K, ACROSS_K>>(p, st);
+    if (p.parts > 1 && ((p.dw_gate && !up) || (p.dw_down && !down))) {
         const size_t all = (size_t)p.E * p.d * p.F;
         hipLaunchKernelGGL(gated_join_kernel<T>, dim3((unsigned)(all / 1024 < 1024 ? all / 1024 + 1 : 1024), 3), dim3(256), 0, st, p.sums, p.parts, all,
-                           with_dx ? nullptr : (T *)p.dw_gate, with_dx ? nullptr : (T *)p.dw_up, with_dh ? nullptr : (T *)p.dw_down);
+                           up ? nullptr : (T *)p.dw_gate, up ? nullptr : (T *)p.dw_up, down ? nullptr : (T *)p.dw_down);
     }
 }
 

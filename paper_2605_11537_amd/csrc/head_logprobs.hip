@@ -76,8 +76,13 @@ __device__ __forceinline__ float row_sum(float v)
     const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
-// e^x for x <= 0 up to some tens (a logit beside its row's maximum or log sum): the exponent's product is off by |x| 2^-24
-__device__ __forceinline__ float exp_beside(float z, float beside) { return __builtin_amdgcn_exp2f((z - beside) * LOG2E); }
+// e^x for x <= 0 up to some tens, a logit beside its row's maximum or log sum.  Binary32: with the exponent's product taken along.  bfloat16: one rounding, off by
+// |x| 2^-24 of an e^x that counts the less the larger |x| is; x 2^-24 e^x is at most 0.4 of that step of lse, and dz is rounded by 2^-8 behind it.
+template <class T>
+__device__ __forceinline__ float exp_beside(float z, float beside)
+{
+    return exp_of<sizeof(T) == 4>(z - beside);
+}
 
 // where column `in` of a wavefront's is one of this lane's: block, register
 template <class TILE>
@@ -146,7 +151,7 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s += exp_beside(z[0][mb][nb][i], beside);
+                    for (int i = 0; i < 4; ++i) s += exp_beside<T>(z[0][mb][nb][i], beside);
                 s = row_sum(s);
                 if (lane < 16) parts[tile.wn * TILE::BM + row] = make_float2(m, s);
             }
@@ -159,7 +164,7 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
 #pragma unroll
                 for (int w = 0; w < WN; ++w) {
                     const float2 part = parts[w * TILE::BM + row];         // of masked columns alone: a sum of 0, times 1 and not e^-m
-                    s += part.y * exp_beside(finite_or(part.x, beside), beside);
+                    s += part.y * exp_of<true>(finite_or(part.x, beside) - beside);
                 }
                 p.tiles[(size_t)(j.m0 + row) * n_n + j.n0 / TILE::BN] = make_float2(m, s);
             }
@@ -329,7 +334,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
 #pragma unroll
                 for (int nb = 0; nb < TILE::NB; ++nb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dz[nb][i] = on ? -gp * exp_beside(z[0][mb][nb][i], lse) : 0.f;
+                    for (int i = 0; i < 4; ++i) dz[nb][i] = on ? -gp * exp_beside<T>(z[0][mb][nb][i], lse) : 0.f;
                 const int in = target - j.n0 - tile.wn * TILE::WAVE_N;
                 if (on && holds_column<TILE>(in)) {
 #pragma unroll

@@ -108,6 +108,22 @@ def test_rows_far_and_near_side_by_side(N, d, V, dtype):
     assert torch.equal(alone[near], got["dh"][near])
 
 
+@pytest.mark.parametrize("N,V", [(1, 700), (1, 9001), (40, 9001), (300, 2049)])
+def test_binary32_exponentials(N, V):
+    """Far below the largest logit, whose sum is 1: an exponential keeps binary32's accuracy whatever its argument (exact here).  A step each for the exponential, what
+    its exponent's product has lost, three products; the rows' sum is of N equal terms."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    b = 4096.0 - torch.randint(40 * 8, 84 * 8, (V,), generator=g, device="cuda").float() / 8
+    b[5] = 4096.0
+    s = dict(h=torch.zeros(N, 16, device="cuda"), w=torch.zeros(V, 16, device="cuda"), b=b, target=torch.full((N,), 5, dtype=torch.int32, device="cuda"),
+             dlogprob=torch.ones(N, device="cuda"))
+    db = run(s)[1]["db_head"].double()
+    want = -N * torch.exp(b.double() - 4096.0)
+    off = (db - want).abs() > (5 + N.bit_length()) * ol.STEP * want.abs()
+    off[5] = False
+    assert not off.any(), float(((db - want) / want).abs()[off].max())
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_pieces_and_equal_bits(dtype):
     """Far rows in a vocabulary of which one piece's gradient is in memory at a time, and one gradient alone."""

@@ -428,7 +428,8 @@ int moe_token_logprobs_backward(const void *logits, long long row_stride, const 
  *     dw_gate = x^T dg,  dw_up = x^T du,  dw_down = h^T dy   over an expert's rows; zeros for one without rows
  * What is written (y, states, the gradients, the workspace) overlaps no other tensor of its call, at any offset: refused.
  * dx [R, d] is left as it was behind the last row.  dx, dw_down and the pair dw_gate, dw_up may be NULL.  Sums are binary32 in an order that the
- * sizes fix.
+ * sizes fix: in bfloat16 32 terms at a time go to one accumulator, so that a sum over R rows is off by R 2^-29 of itself at most if all are equal, by
+ * about the root of that many steps if they differ; 2^20 rows of one sign were within 2^-12.
  */
 #define MOE_ACT_SILU 0
 #define MOE_ACT_GELU 1

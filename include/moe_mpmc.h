@@ -456,9 +456,12 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  *     dh = dz w_head,   dw_head = dz^T h,   db_head = sum of dz over the rows  (binary32)
  * p is taken from lse where lse holds it; where the |lse| of a row is 64 (binary32) or 2048 (bfloat16) and more, rows are summed once
  * more, so that their p add up to 1 (as in moe_token_logprobs_backward).
- * The logits are made again, in pieces of the vocabulary: the workspace holds N times a piece, 1 GiB of dz at most (256 ids for very
- * large N), as much of dh's sums, N V / 32 bytes of db_head's and a copy of h.  dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With
- * N = 0 dw_head and db_head are zeros.  As above, what is written overlaps no other tensor of its call.  Sums in binary32 in an order that the sizes fix.
+ * The logits are made again, in pieces of the vocabulary.  The workspace, whatever is wanted: dz of a piece, 1 GiB at most (256 ids for very
+ * large N), or 8 N bytes for every 256 ids (binary32 or few rows: 128) where that is more; dh's sum in binary32, 4 N d bytes, up to 1 GiB of it in parts where tiles are few; db_head's in parts, N V / 32 bytes with more than 128
+ * rows of bfloat16, N V / 16 with more than 16 or in binary32 (N V / 8 where a last tile is half empty), N V / 4 with few; dw_head's in up to 16 parts of
+ * 4 V d bytes where rows are many and tiles few; a copy of h; 8 bytes a row.
+ * dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With N = 0 dw_head and db_head are
+ * zeros.  As above, what is written overlaps no other tensor of its call.  Sums in binary32 in an order that the sizes fix.
  */
 size_t moe_head_logprobs_workspace_bytes(int N, int d, int V, int dtype);
 int moe_head_logprobs(const void *h, const void *w_head, const float *b_head, const int32_t *target, int N, int d, int V,

@@ -217,7 +217,7 @@ __device__ __forceinline__ void gated_rows(const GatedArgs &p, const RowTiles &t
                             float slope;
                             const float v = sums[0][mb][nb][i];
                             vu[nb][i] = v * act_of<Z == 4>(p.activation, gate[mb & 1][nb][i], slope);
-                            vg[nb][i] = v * up[mb & 1][nb][i] * slope;
+                            vg[nb][i] = v * (up[mb & 1][nb][i] * slope);       // behind a shut gate 0, whatever dh u is
                         }
                     dg.row(mb, vg);
                     du.row(mb, vu);

@@ -60,3 +60,19 @@ def test_gates_near_and_far(copies, dtype, act):
         room = off + (half + 3 * STEP) * (abs(want) + off) + 2 * TINY * (1 + np.minimum(abs(f64(x[:, 0])), 200.0))
         ok = abs(f64(got) - want) <= room
         assert ok.all(), (what, [(f64(x[i, 0]).item(), f64(got[i]).item(), want[i]) for i in np.nonzero(~ok)[0][:6]])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_closed_gate_beside_large_values(dtype, act):
+    """dh u passes the range; behind a gate that is shut the gradient is 0 all the same."""
+    import paper_2605_11537_amd as moe
+    t = DT[dtype]
+    x, dy = torch.zeros(3, 16, dtype=t, device="cuda"), torch.zeros(3, 16, dtype=t, device="cuda")
+    x[:, 0], x[:, 8], dy[:, 0] = torch.tensor([-1e25, -1e3, 2.0], device="cuda").to(t), 1e30, 1e10
+    w_gate, w_up, w_down = (torch.zeros(1, *s, dtype=t, device="cuda") for s in ((16, 8), (16, 8), (8, 16)))
+    w_gate[0, 0, 0] = w_up[0, 8, 0] = w_down[0, 0, 0] = 1.0
+    _, states = moe.moe_gated_ffn(x, w_gate, w_up, w_down, activation=ACT[act], want_states=True)
+    dx = moe.moe_gated_ffn_backward(dy, x, w_gate, w_up, w_down, states, activation=ACT[act])["dx"]
+    assert not dx[:2, 0].any() and not dx[:2, 8].any()
+    assert torch.isinf(dx[2, 0])                                     # and infinite where the gate is open

@@ -459,7 +459,7 @@ int moe_gated_ffn_backward(const void *dy, const void *x, const int32_t *expert_
  * The logits are made again, in pieces of the vocabulary.  The workspace, whatever is wanted: dz of a piece, 1 GiB at most (256 ids for very
  * large N), or 8 N bytes for every 256 ids (binary32 or few rows: 128) where that is more; dh's sum in binary32, 4 N d bytes, up to 1 GiB of it in parts where tiles are few; db_head's in parts, N V / 32 bytes with more than 128
  * rows of bfloat16, N V / 16 with more than 16 or in binary32 (N V / 8 where a last tile is half empty), N V / 4 with few; dw_head's in up to 16 parts of
- * 4 V d bytes where rows are many and tiles few; a copy of h; 8 bytes a row.
+ * 4 V d bytes where rows are many and tiles few; a copy of h; 8 to 512 bytes a row.
  * dz is rounded once to dtype for the two products, db_head is not.  dh, dw_head and db_head may each be NULL.  With N = 0 dw_head and db_head are
  * zeros.  As above, what is written overlaps no other tensor of its call.  Sums in binary32 in an order that the sizes fix.
  */

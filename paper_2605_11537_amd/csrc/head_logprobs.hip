@@ -8,8 +8,8 @@
 // it in binary32: with the loss a mean all rows have the same dlogprob, which would put the same rounding error on every target's -1.
 //
 // p = e^(z - lse), but lse = m + log s has been rounded, and beside a large m that takes a part of log s or all of it: 64 ids of -1e9 had p = 1 each.  Where a
-// row's |lse| is far from zero the backward call makes all rows' m and s once more (two launches that end at once where none is: 4 us of its 34 at 4096 x 256 x
-// 128, 9 of 1980 at 8192 x 768 x 50257; where one is 44 and 2600 us) and takes p = e^(z - m) / s, so that they add up to one.  The logits
+// row's |lse| is far from zero the backward call makes all rows' m and s once more (a launch that ends at once where none is, with many tiles two: 2.7 of the
+// 44 us that 4096 x 256 x 128 take with gradient, 9 of 2430 at 8192 x 768 x 50257) and takes p = e^(z - m) / s, so that they add up to one.  The logits
 // are the same bits in all passes: every tile adds an element's k in the same order.
 #include "product.h"
 #include "scalar_math.h"
@@ -27,7 +27,8 @@ struct HeadArgs {
     int N, d, V;
     int v0, columns;                           // backward: the piece's first id, its ids
     const int *far;                            // whether a row is far from zero; forward: NULL, or whether there is anything to do
-    float2 *again;                             // such rows' maximum and sum, [N]
+    float2 *again;                             // a row's maxima and sums made again, [N, n_again]
+    int n_again;
     int n_n;                                   // forward: slots of a row
     float2 *tiles;                             // forward [N, n_n]: maximum, sum
     float *at_target;                          // forward [N]
@@ -317,8 +318,15 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
             if (far) {                         // uniform
 #pragma unroll
                 for (int mb = 0; mb < TILE::MB; ++mb) {
-                    const float2 again = p.again[j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0)];
-                    if (far_from_zero<T>(lses[mb])) lses[mb] = again.x, shares[mb] = 1.f / again.y;
+                    const float2 *again = p.again + (size_t)(j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0)) * p.n_again;
+                    float m = again[0].x, s = again[0].y;
+                    for (int i = 1; i < p.n_again; ++i) {
+                        const float2 v = again[i];
+                        const float both = fmaxf(m, v.x), beside = finite_or(both, 0.f);
+                        s = s * exp_of<true>(finite_or(m, beside) - beside) + v.y * exp_of<true>(finite_or(v.x, beside) - beside);
+                        m = both;
+                    }
+                    if (far_from_zero<T>(lses[mb])) lses[mb] = m, shares[mb] = 1.f / s;
                 }
             }
             product_f32x4 down[TILE::NB];      // sums over this lane's rows
@@ -740,7 +748,7 @@ void forward(const HeadArgs &p, float *logprob, float *lse, hipStream_t st)
     typedef Tile<T, ALONG_K, ALONG_K, HEAD_TINY_ROWS, HEAD_TINY_COLUMNS, 1, 1, 1, 5> tiny;
     if (head_tiny(N, p.V)) hipLaunchKernelGGL(head_forward_tiny_kernel<tiny>, few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS), dim3(4 * WAVE), 0, st, p);
     else HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
-    if (p.tiles == p.again) return;
+    if (p.tiles == p.again) return;            // who needs them joins them
     if (N <= 512 && p.n_n > 64)
         hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse, p.far, p.again);
     else
@@ -755,10 +763,10 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     p.largest = largest;
     p.far = (const int *)ws + 1;
     p.again = (float2 *)(ws + g.again_at);
+    p.n_again = g.n_again;
     p.n_n = head_row_slots(N, p.V, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);
     p.at_target = (float *)(ws + g.dz_at);
-    // a row of one tile has its maximum and sum from there
-    p.tiles = p.n_n == 1 ? p.again : (float2 *)(ws + g.dz_at + head_targets_bytes(N));
+    p.tiles = p.n_again == p.n_n ? p.again : (float2 *)(ws + g.dz_at + head_targets_bytes(N));
     p.dz = ws + g.dz_at;
     p.db = db ? db_parts : nullptr;
     const int pieces = p.d * (int)sizeof(T) / 16;

@@ -47,6 +47,7 @@ struct HeadShape {
     int dw_parts;                              // of the rows in dW's sum (one piece only)
     bool paired;                               // dh and dW share a launch
     int db_rows;                               // rows of partial sums for db
+    int n_again;                               // maxima and sums of a row made again, as dz is made from them: a row's tiles', up to 64, or one behind a join
     size_t again_at, rows_at, dz_at, dh_at, db_at, dw_at, bytes;
 };
 static inline HeadShape head_shape(int N, int d, int V, int dtype)
@@ -80,7 +81,8 @@ static inline HeadShape head_shape(int N, int d, int V, int dtype)
     g.dw_parts = dw_parts < 2 ? 1 : dw_parts > 16 ? 16 : (int)dw_parts;
     g.db_rows = ceil_div(N, head_wave_rows(N, V, dtype));
     g.again_at = 256;
-    g.rows_at = g.again_at + align_up((size_t)N * 8, 256);
+    g.n_again = head_row_slots(N, V, dtype) <= 64 ? head_row_slots(N, V, dtype) : 1;
+    g.rows_at = g.again_at + align_up((size_t)N * g.n_again * 8, 256);
     g.dz_at = g.rows_at + align_up((size_t)N * d * z, 256);
     // before dz is written its place holds what summing the rows again takes
     const size_t dz = (size_t)N * align_up((size_t)g.piece * z, HEAD_DZ_ROW), scores = head_scores_bytes(N, V, dtype);

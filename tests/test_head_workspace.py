@@ -21,6 +21,6 @@ def test_terms():
             dz = N * min(-(-V * z // 512) * 512, max(256 * z, GIB // N + 512))
             dz = max(dz, 8 * N * -(-V // (256 if z == 2 and N > 128 else 128)))
             parts = max(4 * N * d, GIB)
-            most = dz + N * 512 + parts + db + 64 * V * d + N * d * z + 8 * N + 4 * N + 8 * N * -(-V // 32) * few + 4096
+            most = dz + N * 512 + parts + db + 64 * V * d + N * d * z + 512 * N + 4 * N + 4096
             assert 4 * N * d + db + N * d * z + 8 * N <= need <= most, (N, d, V, z, need, most)
     assert L.moe_head_logprobs_backward_workspace_bytes(4194309, 520, 8, moe.MOE_BF16) > 8 * GIB

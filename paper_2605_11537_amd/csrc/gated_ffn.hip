@@ -384,7 +384,8 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const float *sums, int 
 // dh with dW_down, dx with dW_gate and dW_up: two products that need nothing of each other share a launch, so that the last round of one does not leave
 // compute units without work, and the tiles that wait for memory (dh's for the states) run beside such as do not.  16 experts of 1024 x 2816, 15747
 // rows: 368 and 449 us (0.49 and 0.81 PFLOP/s), as four launches 364 and 525; a step of 8 experts of 2048 x 1408 and 16384 rows 960 us, without the first pair
-// 1020, without both 1095; of 64 of 512 x 1376 and 24576 rows 748, 735 and 731.
+// 1020, without both 1095; of 64 of 512 x 1376 and 24576 rows 748, 735 and 731: there the
+// rule that pairs them loses 2 %.
 template <int STEP, class ROWS, class WEIGHTS>
 __global__ __launch_bounds__(Whole<ROWS>::THREADS, 2) void gated_pair_kernel(GatedArgs p, int tall)
 {

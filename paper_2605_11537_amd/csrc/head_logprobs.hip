@@ -173,7 +173,7 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
 }
 
 // Bound by the matrix instructions and their stages' way from LDS: 8192 x 768 x 50257 653 us, 0.97 PFLOP/s; the same tiles without
-// maxima and exponentials, which have no product beside them, reach 1.15 to 1.2 (k = 1024).  Binary32, 777 x 320 x 5003: 31 us, 80 TFLOP/s.
+// maxima and exponentials, which have no product beside them, reach 1.15 to 1.2 (k = 1024).  Binary32, 777 x 320 x 5003: 33 us, 75 TFLOP/s.
 template <class SIZES>
 __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(HeadArgs p, int tall)
 {
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
 }
 
 // As tiles of 16 rows x 32 columns, where these are few (a predictor's head over its experts, a few tokens): four wavefronts share a tile's k, and
-// nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more: 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
+// nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more (both with a launch less): 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
 // 68, 136, in bfloat16 35, 45; 1000 x 256 x 128 34, 38; 4096 x 256 x 8 40, 39.
 template <class TILE>
 __global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)
@@ -215,8 +215,8 @@ __global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)
     head_forward<TILE, TILE::BM, TILE::BN, SPLIT>(p, ring, parts, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
 }
 
-// A row's tiles' maxima and sums -> lse and the target's log probability, or with `again` the maximum and the sum.  ROWS rows to a workgroup of four wavefronts: one each, or with few rows, whose
-// tiles would be many trips one behind another, all four on one (3 x 131072: 5 us, one wavefront 7.7).
+// A row's tiles' maxima and sums -> lse and the target's log probability, or with `again` the maximum and the sum.  ROWS rows to a workgroup of four
+// wavefronts: one each, or with few rows, whose tiles would be many trips one behind another, all four on one (3 x 131072: 5 us, one wavefront 7.7).
 template <int ROWS>
 __global__ __launch_bounds__(256) void head_join_kernel(const float2 *tiles, const float *at_target, const int32_t *target, int N, int V, int n_n,
                                                         float *logprob, float *lse, const int *far, float2 *again)
@@ -319,13 +319,9 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
 #pragma unroll
                 for (int mb = 0; mb < TILE::MB; ++mb) {
                     const float2 *again = p.again + (size_t)(j.m0 + (tile.of_row(mb) < j.rows ? tile.of_row(mb) : 0)) * p.n_again;
-                    float m = again[0].x, s = again[0].y;
-                    for (int i = 1; i < p.n_again; ++i) {
-                        const float2 v = again[i];
-                        const float both = fmaxf(m, v.x), beside = finite_or(both, 0.f);
-                        s = s * exp_of<true>(finite_or(m, beside) - beside) + v.y * exp_of<true>(finite_or(v.x, beside) - beside);
-                        m = both;
-                    }
+                    float m = HEAD_NONE, s = 0.f;          // of a far row finite
+                    for (int i = 0; i < p.n_again; ++i) m = fmaxf(m, again[i].x);
+                    for (int i = 0; i < p.n_again; ++i) s += again[i].y * exp_of<true>(again[i].x - m);
                     if (far_from_zero<T>(lses[mb])) lses[mb] = m, shares[mb] = 1.f / s;
                 }
             }
@@ -369,7 +365,7 @@ __device__ __forceinline__ void head_dlogits(const HeadArgs &p, char *smem, int 
         });
 }
 
-// The forward's product again, and dz of its tile to memory: 8192 x 768 x 50257 722 us, 0.88 PFLOP/s; the exponentials and 800 MB of dz beside the product.
+// The forward's product again, and dz of its tile to memory: 8192 x 768 x 50257 727 us, 0.87 PFLOP/s; the exponentials and 800 MB of dz beside the product.
 template <class SIZES>
 __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dlogits_kernel(HeadArgs p, int tall)
 {

@@ -8,8 +8,7 @@
 // it in binary32: with the loss a mean all rows have the same dlogprob, which would put the same rounding error on every target's -1.
 //
 // p = e^(z - lse), but lse = m + log s has been rounded, and beside a large m that takes a part of log s or all of it: 64 ids of -1e9 had p = 1 each.  Where a
-// row's |lse| is far from zero the backward call makes all rows' m and s once more (a launch that ends at once where none is, with many tiles two: 2.7 of the
-// 44 us that 4096 x 256 x 128 take with gradient, 9 of 2430 at 8192 x 768 x 50257) and takes p = e^(z - m) / s, so that they add up to one.  The logits
+// row's |lse| is far from zero the backward call makes all rows' m and s once more (the launch that prepares the rows otherwise ends where none is far) and takes p = e^(z - m) / s, so that they add up to one.  The logits
 // are the same bits in all passes: every tile adds an element's k in the same order.
 #include "product.h"
 #include "scalar_math.h"
@@ -26,13 +25,15 @@ struct HeadArgs {
     const int32_t *target;
     int N, d, V;
     int v0, columns;                           // backward: the piece's first id, its ids
-    const int *far;                            // whether a row is far from zero; forward: NULL, or whether there is anything to do
+    int *far;                                  // backward: whether a row is far from zero
     float2 *again;                             // a row's maxima and sums made again, [N, n_again]
     int n_again;
     int n_n;                                   // forward: slots of a row
     float2 *tiles;                             // forward [N, n_n]: maximum, sum
     float *at_target;                          // forward [N]
-    const float *largest;                      // backward: |dlogprob|
+    float *largest;                            // backward: |dlogprob|
+    void *clean;                               // backward: h with zeros for the padded rows, or NULL
+    bool scan;                                 // backward: every workgroup of the first launch looks at all rows
     void *dz;
     float *db;                                 // backward [slots of a wavefront's rows, V], or NULL
 };
@@ -90,6 +91,60 @@ template <class TILE>
 __device__ __forceinline__ bool holds_column(int in)
 {
     return in >= 0 && in < TILE::WAVE_N && ((in >> 2) & 3) == (int)((threadIdx.x & 63) >> 4);
+}
+
+// What the backward calls begin with.  Workgroups from `first` on: h with zeros for the padded rows, which may hold anything: what dW's sums are made of.
+template <int THREADS>
+__device__ __forceinline__ void head_clean(const HeadArgs &p, int pieces, int first)
+{
+    const uint4 *const h = (const uint4 *)p.h;
+    uint4 *const to = (uint4 *)p.clean;
+    const size_t total = (size_t)p.N * pieces, step = (size_t)(gridDim.x - first) * THREADS;
+    for (size_t i = (size_t)(blockIdx.x - first) * THREADS + threadIdx.x; i < total; i += step) {
+        const int id = p.target[i / pieces];
+        to[i] = id >= 0 && id < p.V ? h[i] : make_uint4(0, 0, 0, 0);
+    }
+}
+// The first workgroup writes the largest |dlogprob| of a row that counts, 1 where that is 0 or no number, and whether such a row is far from zero.  -> that.
+template <class T, int THREADS>
+__device__ __forceinline__ bool head_scan(const HeadArgs &p)
+{
+    __shared__ float waves[THREADS / WAVE];
+    float m = 0.f;
+    bool any = false;
+#pragma unroll 8
+    for (int i = threadIdx.x; i < p.N; i += THREADS) {
+        const int id = p.target[i];
+        const float g = blockIdx.x > 0 ? 0.f : fabsf(p.dlogprob[i]), l = p.lse[i];
+        if (id >= 0 && id < p.V) m = fmaxf(m, g), any |= far_from_zero<T>(l);
+    }
+    any = __syncthreads_or(any);
+    if (blockIdx.x > 0) return any;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < THREADS / WAVE; ++w) m = fmaxf(m, waves[w]);
+        *p.largest = m > 0.f && m < __builtin_inff() ? m : 1.f;
+        *p.far = any;
+    }
+    return any;
+}
+// In a launch of its own, where rows are many.
+template <class T>
+__global__ __launch_bounds__(512) void head_begin_kernel(HeadArgs p)
+{
+    if (blockIdx.x > 0) head_clean<512>(p, p.d * (int)sizeof(T) / 16, 1);
+    else head_scan<T, 512>(p);
+}
+// By the kernels that make rows again, -> whether they have to.
+template <class T, int THREADS>
+__device__ __forceinline__ bool head_begin(const HeadArgs &p)
+{
+    if (!p.scan) return *p.far;
+    if (p.clean) head_clean<THREADS>(p, p.d * (int)sizeof(T) / 16, 0);
+    return head_scan<T, THREADS>(p);
 }
 
 // `units` of the parts of n_m x n_n tiles of BIG_M x BIG_N, from tile `first` on (below likewise); here all have BIG_N columns, for which a row has one slot.
@@ -174,13 +229,14 @@ __device__ __forceinline__ void head_forward(const HeadArgs &p, char *smem, floa
 
 // Bound by the matrix instructions and their stages' way from LDS: 8192 x 768 x 50257 653 us, 0.97 PFLOP/s; the same tiles without
 // maxima and exponentials, which have no product beside them, reach 1.15 to 1.2 (k = 1024).  Binary32, 777 x 320 x 5003: 33 us, 75 TFLOP/s.
-template <class SIZES>
+template <class SIZES, bool AGAIN>
 __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(HeadArgs p, int tall)
 {
     typedef typename Whole<SIZES>::Tile Big;
     __shared__ __align__(1024) char smem[Whole<SIZES>::LDS];
     __shared__ float2 parts[4 * Big::BM];
-    if (p.far && !*p.far) return;
+    if constexpr (AGAIN)
+        if (!head_begin<typename Big::T, Big::THREADS>(p)) return;
     const int n_m = tiles_of(p.N, Big::BM), n_n = tiles_of(p.V, Big::BN);
     in_rounds<SIZES>(n_m * n_n, [&](auto sized, int first, int past) {
         static_assert(decltype(sized)::Type::BN == Big::BN, "one slot for a row's columns of a tile");
@@ -189,12 +245,13 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_forward_kernel(
     });
 }
 // Few rows: bound by the stream of W.  3 x 768 x 131072: 30 us, 6.7 TB/s (a part of W is still in the cache beside the memory).
-template <class TILE>
+template <class TILE, bool AGAIN>
 __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(HeadArgs p)
 {
     __shared__ __align__(1024) char smem[TILE::LDS];
     __shared__ float2 parts[4 * TILE::BM];
-    if (p.far && !*p.far) return;
+    if constexpr (AGAIN)
+        if (!head_begin<typename TILE::T, TILE::THREADS>(p)) return;
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
     head_forward<TILE, TILE::BM, TILE::BN>(p, smem, parts, n_m, n_n, 0, Units(n_m * n_n), 8);
 }
@@ -202,14 +259,15 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
 // As tiles of 16 rows x 32 columns, where these are few (a predictor's head over its experts, a few tokens): four wavefronts share a tile's k, and
 // nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more (both with a launch less): 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
 // 68, 136, in bfloat16 35, 45; 1000 x 256 x 128 34, 38; 4096 x 256 x 8 40, 39.
-template <class TILE>
+template <class TILE, bool AGAIN>
 __global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)
 {
     constexpr int SPLIT = 4;
     __shared__ __align__(1024) char smem[SPLIT * TILE::LDS];
     __shared__ product_f32x4 shared[SHARED_SUMS<TILE, SPLIT>];
     __shared__ float2 parts[TILE::BM];
-    if (p.far && !*p.far) return;
+    if constexpr (AGAIN)
+        if (!head_begin<typename TILE::T, 4 * WAVE>(p)) return;
     const int n_m = tiles_of(p.N, TILE::BM), n_n = tiles_of(p.V, TILE::BN);
     char *const ring = smem + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * TILE::LDS;
     head_forward<TILE, TILE::BM, TILE::BN, SPLIT>(p, ring, parts, n_m, n_n, 0, Units(n_m * n_n), 8, shared);
@@ -555,42 +613,6 @@ __global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGr
 }
 
 // ------------------------------------------------------------------------------------------------- rows
-// What the backward calls begin with.  The first workgroup: the largest |dlogprob| of a row that counts; 1 where that is 0 or no number; whether such a row is
-// far from zero.  The others, with `to`:
-// h with zeros for the padded rows, which may hold anything: what dW's sums are made of.  pieces: of 16 bytes, to a row
-template <class T>
-__global__ __launch_bounds__(512) void head_begin_kernel(const int32_t *target, const float *dlogprob, const float *lse, int N, int V, float *largest, int *far,
-                                                         const uint4 *h, int pieces, uint4 *to)
-{
-    if (blockIdx.x > 0) {
-        const size_t total = (size_t)N * pieces, step = (size_t)(gridDim.x - 1) * 512;
-        for (size_t i = (size_t)(blockIdx.x - 1) * 512 + threadIdx.x; i < total; i += step) {
-            const int id = target[i / pieces];
-            to[i] = id >= 0 && id < V ? h[i] : make_uint4(0, 0, 0, 0);
-        }
-        return;
-    }
-    __shared__ float waves[8];
-    float m = 0.f;
-    bool any = false;
-#pragma unroll 8
-    for (int i = threadIdx.x; i < N; i += 512) {
-        const int id = target[i];
-        const float g = fabsf(dlogprob[i]), l = lse[i];
-        if (id >= 0 && id < V) m = fmaxf(m, g), any |= far_from_zero<T>(l);
-    }
-    any = __syncthreads_or(any);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) m = fmaxf(m, waves[w]);
-        *largest = m > 0.f && m < __builtin_inff() ? m : 1.f;
-        *far = any;
-    }
-}
-
 // What they end with: the parts' sums, in their order, times the largest |dlogprob|.  Workgroups 0 .. dh_blocks-1 dh, then dW (a single piece's, in parts), then
 // db.
 template <class T>
@@ -709,8 +731,8 @@ dim3 few_grid(long long units, int more_lds)
     return dim3((unsigned)(((units < most ? units : most) + 7) / 8 * 8));
 }
 
-// KERNEL for tiles of PARTS' sizes, or KERNEL_few for tiles of 64, 32 or 16 rows, by the number of rows; M, N, TIMES: D and how often
-#define HEAD_BY_ROWS(KERNEL, PARTS, A, B, ARGS, ST, M, N, TIMES, LDS_ROWS)                                                                            \
+// KERNEL for tiles of PARTS' sizes, or KERNEL_few for tiles of 64, 32 or 16 rows, by the number of rows; M, N, TIMES: D and how often; further template arguments
+#define HEAD_BY_ROWS(KERNEL, PARTS, A, B, ARGS, ST, M, N, TIMES, LDS_ROWS, ...)                                                                       \
     do {                                                                                                                                       \
         typedef PARTS<T> sizes;                                                                                                                \
         typedef typename Whole<sizes>::Tile big;                                                                                               \
@@ -719,32 +741,34 @@ dim3 few_grid(long long units, int more_lds)
         typedef Few<T, A, B> few;                                                                                                              \
         const HeadRows rows = head_rows(M, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);                                                               \
         if (rows == HEAD_TALL_TILES)                                                                                                           \
-            hipLaunchKernelGGL((KERNEL##_kernel<sizes>),                                                                                       \
+            hipLaunchKernelGGL((KERNEL##_kernel<sizes, ##__VA_ARGS__>),                                                                        \
                                dim3(product_grid((long long)TIMES * tiles_of(M, big::BM) * tiles_of(N, big::BN), PRODUCT_CUS * sizes::PER_CU)), \
                                dim3(big::THREADS), 0, ST, ARGS, 8);                                                                            \
         else if (rows == HEAD_FLAT_TILES)                                                                                                      \
-            hipLaunchKernelGGL((KERNEL##_few_kernel<flat>),                                                                                    \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<flat, ##__VA_ARGS__>),                                                                     \
                                few_grid<flat>((long long)TIMES * tiles_of(M, flat::BM) * tiles_of(N, flat::BN), LDS_ROWS * flat::BM),          \
                                dim3(flat::THREADS), 0, ST, ARGS);                                                                              \
         else if (rows == HEAD_LOW_TILES)                                                                                                       \
-            hipLaunchKernelGGL((KERNEL##_few_kernel<low>),                                                                                     \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<low, ##__VA_ARGS__>),                                                                      \
                                few_grid<low>((long long)TIMES * tiles_of(M, low::BM) * tiles_of(N, low::BN), LDS_ROWS * low::BM),             \
                                dim3(low::THREADS), 0, ST, ARGS);                                                                              \
         else                                                                                                                                   \
-            hipLaunchKernelGGL((KERNEL##_few_kernel<few>),                                                                                     \
+            hipLaunchKernelGGL((KERNEL##_few_kernel<few, ##__VA_ARGS__>),                                                                      \
                                few_grid<few>((long long)TIMES * tiles_of(M, few::BM) * tiles_of(N, few::BN), LDS_ROWS * few::BM),              \
                                dim3(few::THREADS), 0, ST, ARGS);                                                                               \
     } while (0)
 
-// p.tiles, p.at_target -> logprob and lse, or p.again
-template <class T>
+// p.tiles, p.at_target -> logprob and lse; AGAIN: what the backward calls begin with, and p.again where a row is far from zero
+template <class T, bool AGAIN>
 void forward(const HeadArgs &p, float *logprob, float *lse, hipStream_t st)
 {
     const int N = p.N;
     typedef Tile<T, ALONG_K, ALONG_K, HEAD_TINY_ROWS, HEAD_TINY_COLUMNS, 1, 1, 1, 5> tiny;
-    if (head_tiny(N, p.V)) hipLaunchKernelGGL(head_forward_tiny_kernel<tiny>, few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS), dim3(4 * WAVE), 0, st, p);
-    else HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32);
-    if (p.tiles == p.again) return;            // who needs them joins them
+    if (head_tiny(N, p.V))
+        hipLaunchKernelGGL((head_forward_tiny_kernel<tiny, AGAIN>), few_grid<tiny>((long long)tiles_of(N, tiny::BM) * tiles_of(p.V, tiny::BN), 3 * tiny::LDS),
+                           dim3(4 * WAVE), 0, st, p);
+    else HEAD_BY_ROWS(head_forward, RowParts, ALONG_K, ALONG_K, p, st, N, p.V, 1, 32, AGAIN);
+    if (AGAIN && p.tiles == p.again) return;   // who needs them joins them
     if (N <= 512 && p.n_n > 64)
         hipLaunchKernelGGL(head_join_kernel<1>, dim3(N), dim3(256), 0, st, p.tiles, p.at_target, p.target, N, p.V, p.n_n, logprob, lse, p.far, p.again);
     else
@@ -755,9 +779,11 @@ template <class T>
 void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db, hipStream_t st)
 {
     const int N = p.N;
-    float *const largest = (float *)ws, *const dh_parts = (float *)(ws + g.dh_at), *const db_parts = (float *)(ws + g.db_at);
-    p.largest = largest;
-    p.far = (const int *)ws + 1;
+    float *const dh_parts = (float *)(ws + g.dh_at), *const db_parts = (float *)(ws + g.db_at);
+    p.largest = (float *)ws;
+    p.far = (int *)ws + 1;
+    p.clean = dw ? ws + g.rows_at : nullptr;
+    p.scan = N <= HEAD_SCAN_ROWS;
     p.again = (float2 *)(ws + g.again_at);
     p.n_again = g.n_again;
     p.n_n = head_row_slots(N, p.V, sizeof(T) == 4 ? MOE_F32 : MOE_BF16);
@@ -765,11 +791,9 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
     p.tiles = p.n_again == p.n_n ? p.again : (float2 *)(ws + g.dz_at + head_targets_bytes(N));
     p.dz = ws + g.dz_at;
     p.db = db ? db_parts : nullptr;
-    const int pieces = p.d * (int)sizeof(T) / 16;
     auto blocks_for = [](size_t work, size_t each) { return (int)(work / each < 2048 ? work / each + 1 : 2048); };
-    hipLaunchKernelGGL(head_begin_kernel<T>, dim3(1 + (dw ? blocks_for((size_t)N * pieces, 512) : 0)), dim3(512), 0, st, p.target, p.dlogprob, p.lse, N, p.V, largest,
-                       (int *)ws + 1, (const uint4 *)p.h, pieces, (uint4 *)(ws + g.rows_at));
-    forward<T>(p, nullptr, nullptr, st);       // where a row is far from zero
+    if (!p.scan) hipLaunchKernelGGL(head_begin_kernel<T>, dim3(1 + (dw ? blocks_for((size_t)N * p.d * sizeof(T) / 16, 512) : 0)), dim3(512), 0, st, p);
+    forward<T, true>(p, nullptr, nullptr, st);
     HeadGradArgs q = {};
     for (int v0 = 0; v0 < p.V; v0 += g.piece) {
         p.v0 = v0;
@@ -779,7 +803,7 @@ void backward(HeadArgs p, const HeadShape &g, char *ws, T *dh, T *dw, float *db,
         else HEAD_BY_ROWS(head_dlogits, ColumnParts, ALONG_K, ALONG_K, p, st, N, p.columns, 1, 0);
         q.dz = p.dz, q.h = ws + g.rows_at, q.w = p.w, q.N = N, q.d = p.d, q.columns = p.columns, q.v0 = v0;
         q.parts = g.parts, q.part = (int)align_up(tiles_of(p.columns, g.parts), DZ<T>::COLUMNS), q.add = v0 > 0;
-        q.dh = dh_parts, q.dw = dw, q.largest = largest;
+        q.dh = dh_parts, q.dw = dw, q.largest = p.largest;
         q.dw_parts = g.dw_parts, q.dw_part = (int)align_up(tiles_of(N, g.dw_parts), 64), q.dw_sums = (float *)(ws + g.dw_at);
         if (dh && dw && g.paired) {
             typedef DhParts<T> sizes;
@@ -845,8 +869,8 @@ extern "C" int moe_head_logprobs(const void *h, const void *w_head, const float 
     p.n_n = head_row_slots(N, V, dtype);
     p.at_target = (float *)ws;
     p.tiles = (float2 *)((char *)ws + head_targets_bytes(N));
-    if (dtype == MOE_BF16) forward<bf16_t>(p, logprob, lse, (hipStream_t)stream);
-    else forward<float>(p, logprob, lse, (hipStream_t)stream);
+    if (dtype == MOE_BF16) forward<bf16_t, false>(p, logprob, lse, (hipStream_t)stream);
+    else forward<float, false>(p, logprob, lse, (hipStream_t)stream);
     MOE_CHECK_LAUNCH("moe_head_logprobs");
     return MOE_OK;
 }

@@ -7,6 +7,10 @@ namespace moe {
 constexpr int HEAD_MAX_WIDTH = 1 << 20;        // byte offsets inside a tile's rows fit 31 bits
 constexpr int HEAD_MAX_IDS = 1 << 24, HEAD_MAX_ROWS = 1 << 24;
 constexpr size_t HEAD_PIECE_BYTES = 1u << 30;    // of dz, and of the parts of dh's sum
+// Backward: rows up to which the launch that would make rows again also prepares them and every workgroup of it looks at all of them for one that is far from
+// zero; beyond, where that looking takes longer than a launch, another one does so first.  With gradient, us, one way, the other: 4096 x 256 x 128 43.9, 44.2 and,
+// where it is waited for, 59, 62 to 70; 15009 x 256 x 256 68, 64; 777 x 320 x 5003 in binary32 157, 156, waited for 172, 174.
+constexpr int HEAD_SCAN_ROWS = 4096;
 constexpr int HEAD_DZ_ROW = 512;               // bytes of a row of dz in one of its blocks
 constexpr int HEAD_FEW_COLUMNS = 128;          // of a tile of few rows
 

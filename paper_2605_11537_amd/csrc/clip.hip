@@ -5,8 +5,8 @@
 // over a billion values would lose digits.  In the second every workgroup adds those sums, in the same order, and scales its chunks.
 //
 // Bound by memory: 4 or 2 bytes an element are read twice and written once.  The second launch walks the chunks from the last to the first, so that what
-// the first has read last is still in the 256 MB cache beside the memory.  1.29 GB of bfloat16: 193 and 473 us (6.7 TB/s read, 5.4 read and written); 8 MB of
-// binary32: 4.5 and 6.2 us, a launch and a round trip to memory each, the second with the sum over the first's workgroups.
+// the first has read last is still in the 256 MB cache beside the memory.  1.29 GB of bfloat16: 193 and 469 us (6.7 TB/s read, 5.5 read and written); 8 MB of
+// binary32: 4.4 and 5.5 us, a launch and a round trip to memory each, the second with the sum over the first's workgroups.
 #include <algorithm>
 
 #include "common.h"

@@ -592,7 +592,7 @@ __global__ __launch_bounds__(Whole<SIZES>::THREADS, 2) void head_dw_kernel(HeadG
 }
 
 // Both, where there is work for the whole chip: they need nothing of each other, and the last round of one leaves no compute units without work.
-// 8192 x 768 x 50257: 1195 us (1.06 PFLOP/s), one after the other 1226 and 8 more for the parts of dh, which are more then.
+// 8192 x 768 x 50257: 1195 to 1240 us (1.04 PFLOP/s), one after the other 1226 and 8 more for the parts of dh, which are more then.
 template <class DH, class DW>
 __global__ __launch_bounds__(Whole<DH>::THREADS, 2) void head_pair_kernel(HeadGradArgs p, int tall)
 {

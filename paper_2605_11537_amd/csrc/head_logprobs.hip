@@ -8,8 +8,9 @@
 // it in binary32: with the loss a mean all rows have the same dlogprob, which would put the same rounding error on every target's -1.
 //
 // p = e^(z - lse), but lse = m + log s has been rounded, and beside a large m that takes a part of log s or all of it: 64 ids of -1e9 had p = 1 each.  Where a
-// row's |lse| is far from zero the backward call makes all rows' m and s once more (the launch that prepares the rows otherwise ends where none is far) and takes p = e^(z - m) / s, so that they add up to one.  The logits
-// are the same bits in all passes: every tile adds an element's k in the same order.
+// row's |lse| is far from zero the backward call makes all rows' m and s once more (a launch that only prepares the rows where none is) and takes p = e^(z - m) / s,
+// so that they add up to one: 8192 x 768 x 50257 2000 us, where rows are far 2620.  The logits are the same bits in all passes: every tile adds an element's k in the
+// same order.
 #include "product.h"
 #include "scalar_math.h"
 #include "head_logprobs_rules.h"
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(TILE::THREADS, 2) void head_forward_few_kernel(Head
 }
 
 // As tiles of 16 rows x 32 columns, where these are few (a predictor's head over its experts, a few tokens): four wavefronts share a tile's k, and
-// nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more (both with a launch less): 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
+// nothing is computed beside 32 ids.  With gradient, us, and in tiles of 64 x 128 or more (both without the 2 us in which rows are looked at): 18 x 2048 x 8 in binary32 40, 177; 60 x 1024 x 2000 in binary32
 // 68, 136, in bfloat16 35, 45; 1000 x 256 x 128 34, 38; 4096 x 256 x 8 40, 39.
 template <class TILE, bool AGAIN>
 __global__ __launch_bounds__(4 * WAVE) void head_forward_tiny_kernel(HeadArgs p)

@@ -93,8 +93,17 @@ def test_biases_far_from_zero(N, d, V, dtype, base):
     check(s, dtype, got)
 
 
+@pytest.mark.parametrize("base", [3000.0, -1e9])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("N,d,V", [(18, 64, 64), (20, 40, 9001), (100, 136, 1500), (700, 264, 2049)])
+@pytest.mark.parametrize("N,d,V", [(600, 16, 20001), (4096, 16, 300), (4097, 16, 300), (9001, 24, 77)])
+def test_many_rows_and_many_ids(N, d, V, dtype, base):
+    """More than 64 tiles to a row, and as many rows as the launch that makes them again looks at, or more."""
+    s = make(dtype, N, d, V, base, N + V)
+    check(s, dtype, run(s)[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,d,V", [(18, 64, 64), (20, 40, 9001), (100, 136, 1500), (700, 264, 2049), (600, 16, 20001), (5000, 16, 300)])
 def test_rows_far_and_near_side_by_side(N, d, V, dtype):
     """Rows near zero get the same bits whether others are far or not."""
     s = make(dtype, N, d, V, 2560.0, N + V, bias_on=False)
